@@ -20,6 +20,7 @@ EPS = 1e-6
 ADAM = dict(lr=3e-4, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, step=1000, seed=12345)
 BLOCK = 256      # values that share a scale where the states are held in 8 bits
 E4M3_MAX = 448.0
+MOST_FLOPS = 8.1e11  # of a drawn attention: the longest listed case's
 
 
 # ---- cases ------------------------------------------------------------------
@@ -88,10 +89,12 @@ def draw(rng):
         case = attention("", direction, seqs, log_int(rng, 1, longest), longest, heads, kv,
                          rng.choice([16, 40, 64, 64, 96, 128]), causal=rng.random() < 0.75,
                          past=rng.choice([0, 0, log_int(rng, 1, 500)]), short_keys=rng.random() < 0.25)
-        if case["past"]:  # more keys than queries: no more pairs than the longest listed case
-            case["longest"] = min(case["longest"], 8000)
-            case["shortest"] = min(case["shortest"], case["longest"])
-            case["seqs"] = max(1, min(seqs, int(12 * 12289 ** 2 / (heads * (case["longest"] + 500) ** 2))))
+        while work(case)["flops"] > MOST_FLOPS:  # fewer sequences, then shorter ones
+            if case["seqs"] > 1:
+                case["seqs"] -= 1
+            else:
+                case["longest"] = int(case["longest"] * 0.9)
+                case["shortest"] = min(case["shortest"], case["longest"])
     elif op == "rotary":
         heads, kv = rng.choice([(4, 4), (12, 12), (16, 4), (8, 1), (5, 3)])
         dim = rng.choice([16, 24, 64, 64, 96, 128])

@@ -28,33 +28,33 @@ MOST_FLOPS = 8.1e11  # of a drawn attention: the longest listed case's
 def listed():
     return [
         # four prompts of 32 tokens through the small ParityTransformer of the tests: latency alone
-        attention("attention, four short prompts", "forward", seqs=4, shortest=32, longest=32, heads=4, kv=4, dim=16),
+        attention("attention: short prompts", "forward", seqs=4, shortest=32, longest=32, heads=4, kv=4, dim=16),
         # an evaluation batch at the GPT-2-small shape of the bench: 8 sequences of 1024 tokens
-        attention("attention, evaluation batch", "forward", seqs=8, shortest=1024, longest=1024, heads=12, kv=12, dim=64),
+        attention("attention: evaluation batch", "forward", seqs=8, shortest=1024, longest=1024, heads=12, kv=12, dim=64),
         # the attention of one layer of the bench's training step, forward and backward
-        attention("attention step, 8 x 1024", "step", seqs=8, shortest=1024, longest=1024, heads=12, kv=12, dim=64),
+        attention("attention step: 8 x 1024", "step", seqs=8, shortest=1024, longest=1024, heads=12, kv=12, dim=64),
         # documents of odd lengths packed into one batch, grouped heads of 128
-        attention("attention step, packed documents", "step", seqs=12, shortest=1, longest=3001, heads=16, kv=4, dim=128),
+        attention("attention step: documents", "step", seqs=12, shortest=1, longest=3001, heads=16, kv=4, dim=128),
         # one long document of odd length
-        attention("attention step, one long document", "step", seqs=1, shortest=12289, longest=12289, heads=12, kv=12,
+        attention("attention step: one long", "step", seqs=1, shortest=12289, longest=12289, heads=12, kv=12,
                   dim=64),
         # the small model's queries and keys in 32 bits: latency alone
-        rotary("rotation, small model", "forward", tokens=128, heads=4, kv=4, dim=16, rot=16, interleaved=False,
+        rotary("rotation: small model", "forward", tokens=128, heads=4, kv=4, dim=16, rot=16, interleaved=False,
                dtype="f32"),
         # the wide workload's 65536 tokens at the GPT-2-small head layout
-        rotary("rotation, 65536 tokens", "forward", tokens=65536, heads=12, kv=12, dim=64, rot=64, interleaved=False,
+        rotary("rotation: 65536 tokens", "forward", tokens=65536, heads=12, kv=12, dim=64, rot=64, interleaved=False,
                dtype="bf16"),
         # gradient at grouped heads of 128, three quarters of the head rotated, interleaved pairs, odd token count
-        rotary("rotation gradient, grouped heads", "backward", tokens=49999, heads=16, kv=4, dim=128, rot=96,
+        rotary("rotation gradient", "backward", tokens=49999, heads=16, kv=4, dim=128, rot=96,
                interleaved=True, dtype="bf16"),
         # the small ParityTransformer of the tests, everything in 32 bits: latency alone
-        adamw("AdamW, small model", layers=2, d=64, mlp=128, vocab=97, context=32, dtype="f32", state="f32"),
+        adamw("AdamW: small model", layers=2, d=64, mlp=128, vocab=97, context=32, dtype="f32", state="f32"),
         # the paper's small width (d = 1024, 12 layers), bf16 parameters, 32-bit states
-        adamw("AdamW, d = 1024 model", layers=12, d=1024, mlp=4096, vocab=50257, context=1024, dtype="bf16", state="f32"),
+        adamw("AdamW: d = 1024 model", layers=12, d=1024, mlp=4096, vocab=50257, context=1024, dtype="bf16", state="f32"),
         # odd widths and tails shorter than a block, 8-bit states
-        adamw("AdamW 8-bit, odd widths", layers=5, d=500, mlp=1303, vocab=5003, context=257, dtype="f32", state="f8"),
+        adamw("AdamW 8-bit: odd widths", layers=5, d=500, mlp=1303, vocab=5003, context=257, dtype="f32", state="f8"),
         # the paper's small width with 8-bit states
-        adamw("AdamW 8-bit, d = 1024 model", layers=12, d=1024, mlp=4096, vocab=50257, context=1024, dtype="bf16",
+        adamw("AdamW 8-bit: d = 1024 model", layers=12, d=1024, mlp=4096, vocab=50257, context=1024, dtype="bf16",
               state="f8"),
     ]
 

@@ -329,6 +329,178 @@ dpb_status dpb_encode_noalloc(const dpb_plan *plan, const void *x, int64_t T, co
  */
 dpb_status dpb_debug_set_wait_limit(int32_t tries);
 
+/* ---- the training step around the bottleneck ------------------------------
+ *
+ * A ParityTransformer (§3) trains the bottleneck inside an ordinary GPT-2
+ * style step. These entry points are that step's other operators: the norm of
+ * every head's query and key with the position rotation in the same pass,
+ * attention over packed sequences with its gradient, and AdamW over many
+ * tensors at once. The paper names none of them; they follow the library's
+ * conventions (caller-owned memory, host-side checks, asynchronous on
+ * `stream`, sticky device bits in the workspace's first word).
+ */
+
+/* An index of a sequence list or a position outside its range was met: the
+ * sequence is treated as empty, the token's rotation is left out. */
+#define DPB_DEV_BAD_LENGTH 0x10
+
+/* Head rows [tokens][heads][head_dim]: element (t, h, i) lies at
+ * data + t * token_stride + h * head_stride + i (strides in elements), so the
+ * parts of one packed projection can be passed without a copy. */
+typedef struct dpb_heads {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} dpb_heads;
+
+/*
+ * dpb_qk_norm_rope -- RMS norm of each query and key head, then the rotation
+ * of its first rot_dim coordinates by the token's position:
+ *   n_i = w_i x_i (mean_j x_j^2 + eps)^{-1/2}
+ *   (n_a, n_b) -> (n_a cos - n_b sin, n_b cos + n_a sin)
+ * with the pairs (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) when
+ * `interleaved`, and cos, sin = row `position` of the two tables, column i.
+ * Tables scaled for longer contexts are the caller's (any values).
+ *   tokens      T
+ *   heads_q, heads_k  heads of q and of k (either may be 0)
+ *   head_dim    even, 2..256
+ *   rot_dim     even, 0..head_dim; 0 = no rotation
+ *   normalise   0: no norm (weights must be NULL)
+ *   positions_n rows of the tables
+ *   dtype       dpb_dtype of q, k, the weights, the outputs and the gradients
+ * weight_q, weight_k: [head_dim], nullable (ones). cos_tab, sin_tab: fp32
+ * [positions_n][rot_dim / 2]. positions: int32 [T], nullable (token t has
+ * position t). A position outside [0, positions_n) sets DPB_DEV_BAD_LENGTH and
+ * that token's heads are normalised but not rotated. q_out and k_out may be q
+ * and k themselves (same strides).
+ * Sums are in fp32; each output is rounded once.
+ */
+typedef struct dpb_rope_config {
+    int64_t tokens;
+    int32_t heads_q, heads_k, head_dim, rot_dim;
+    int32_t interleaved, normalise, positions_n, dtype;
+    float eps;
+    int32_t reserved; /* 0 */
+} dpb_rope_config;
+
+dpb_status dpb_qk_norm_rope(const dpb_rope_config *cfg, const dpb_heads *q, const dpb_heads *k,
+                            const void *weight_q, const void *weight_k, const float *cos_tab,
+                            const float *sin_tab, const int32_t *positions, const dpb_heads *q_out,
+                            const dpb_heads *k_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dpb_qk_norm_rope_backward -- gradients of dpb_qk_norm_rope: with g the
+ * output gradient rotated back and r = (mean x^2 + eps)^{-1/2},
+ *   dx = r w g - x r^3 mean(w g x),   dw = sum over tokens and heads of g x r.
+ * q and k are the forward's inputs. grad_weight_q, grad_weight_k: fp32
+ * [head_dim], nullable, written (not added to); their sums are taken in a
+ * fixed order, so equal inputs give equal bits. grad_q and grad_k may be the
+ * output gradients themselves (same strides).
+ */
+dpb_status dpb_qk_norm_rope_backward(const dpb_rope_config *cfg, const dpb_heads *q, const dpb_heads *k,
+                                     const dpb_heads *grad_q_out, const dpb_heads *grad_k_out,
+                                     const void *weight_q, const void *weight_k, const float *cos_tab,
+                                     const float *sin_tab, const int32_t *positions, const dpb_heads *grad_q,
+                                     const dpb_heads *grad_k, float *grad_weight_q, float *grad_weight_k,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace bytes of the two calls above (256-byte aligned, zeroed once). */
+dpb_status dpb_rope_workspace_size(const dpb_rope_config *cfg, size_t *bytes);
+
+/*
+ * dpb_attention_forward -- softmax attention over packed sequences:
+ * S = scale q k^T, o = softmax(S over the visible keys) v, and
+ * lse = log sum exp S of each row, kept for the backward.
+ *   seqs        sequences; cu_q and cu_k (device int32 [seqs + 1], from 0,
+ *               not decreasing) give each one's tokens in q and in k, v. Both
+ *               NULL with seqs = 1: the whole of q and k.
+ *   total_q, total_k  tokens of q and of k, v (each below 2^31)
+ *   max_q, max_k      at least the longest sequence's tokens
+ *   heads_q, heads_kv heads; heads_q a multiple of heads_kv, query head h
+ *               reads key head h / (heads_q / heads_kv)
+ *   head_dim    a multiple of 8, 8..128
+ *   causal      query i of n sees key j of m when j <= i + m - n
+ *   dtype       DPB_BF16
+ * q, k, v, o, and the gradients are bf16, 16-byte aligned, with strides that
+ * are multiples of 8 elements. lse: fp32 [heads_q][total_q]. A row that sees no key
+ * gives o = 0, lse = -inf and no gradient. A sequence reads nothing of its
+ * neighbours', whatever they hold; within a sequence a masked key or value
+ * takes part with weight 0, so it has to be finite. scale > 0.
+ * Scores, softmax and sums are fp32; the probabilities enter their product
+ * with v in bf16. Offsets out of range, or a sequence longer than max_q or
+ * max_k, set DPB_DEV_BAD_LENGTH and that sequence is skipped.
+ */
+typedef struct dpb_attention_config {
+    int64_t total_q, total_k;
+    int32_t seqs, max_q, max_k;
+    int32_t heads_q, heads_kv, head_dim;
+    int32_t causal, dtype;
+    float scale;
+    int32_t reserved; /* 0 */
+} dpb_attention_config;
+
+dpb_status dpb_attention_forward(const dpb_attention_config *cfg, const dpb_heads *q, const dpb_heads *k,
+                                 const dpb_heads *v, const int32_t *cu_q, const int32_t *cu_k,
+                                 const dpb_heads *o, float *lse, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/*
+ * dpb_attention_backward -- gradients of dpb_attention_forward. The
+ * probabilities are recomputed from q, k and lse:
+ *   P = exp(S - lse), delta_i = <grad_o_i, o_i>, dS = P (grad_o v^T - delta),
+ *   grad_v = P^T grad_o, grad_q = scale dS k, grad_k = scale dS^T q,
+ * with grad_k and grad_v summed over the query heads of their group. No
+ * atomics: equal inputs give equal bits. P and dS enter their products in
+ * bf16, sums are fp32.
+ */
+dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_heads *q, const dpb_heads *k,
+                                  const dpb_heads *v, const dpb_heads *o, const float *lse,
+                                  const dpb_heads *grad_o, const int32_t *cu_q, const int32_t *cu_k,
+                                  const dpb_heads *grad_q, const dpb_heads *grad_k, const dpb_heads *grad_v,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace bytes of the two calls above (256-byte aligned, zeroed once). */
+dpb_status dpb_attention_workspace_size(const dpb_attention_config *cfg, size_t *bytes);
+
+/*
+ * dpb_adamw_step -- one AdamW step of `n` tensors in place, in one launch for
+ * every few hundred tensors:
+ *   g = grad_scale grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *   dtype       dpb_dtype of the parameters and their gradients
+ *   state_bits  32: exp_avg and exp_avg_sq are fp32 [count], the scales NULL.
+ *               8: both are e4m3 codes [count] with an fp32 scale for each 256
+ *               values ([ceil(count / 256)]), value = code x scale; exp_avg_sq
+ *               then holds sqrt(v). A stored value is rounded up or down to a
+ *               neighbouring code with the probability of its place between
+ *               them (a hash of seed, step and the value's place in the list),
+ *               so changes smaller than a step of the code are kept on
+ *               average; a sqrt(v) above 0 never becomes 0. The step itself
+ *               uses the values before rounding.
+ *   step        1, 2, ... (bias correction)
+ *   grad_scale  device fp32, nullable (1); where it is not finite, nothing
+ *               is changed (a loss scaler's skipped step)
+ * Tensors may have any alignment their type allows; 16-byte aligned ones are
+ * faster.
+ */
+typedef struct dpb_adamw_tensor {
+    void *param;
+    const void *grad;
+    void *exp_avg, *exp_avg_sq;
+    float *exp_avg_scale, *exp_avg_sq_scale;
+    int64_t count;
+} dpb_adamw_tensor;
+
+typedef struct dpb_adamw_config {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+    uint64_t seed;
+    const float *grad_scale;
+    int32_t dtype, state_bits;
+} dpb_adamw_config;
+
+dpb_status dpb_adamw_step(const dpb_adamw_config *cfg, const dpb_adamw_tensor *tensors, int32_t n, void *stream);
+
 /* Static description of a status code. */
 const char *dpb_status_string(dpb_status s);
 

@@ -1,0 +1,1051 @@
+// dpb_attention.cu -- softmax attention over packed sequences and its
+// gradient, on the tcgen05 tensor cores.
+//
+// All three kernels have one shape. A block holds 128-row tiles of one side
+// (queries in the forward and in the query gradient, keys in the key and
+// value gradient) and streams blocks of the other side past them; nothing of
+// size queries x keys is ever in memory. Warps have roles: one copies tiles by
+// tensor maps into a ring of slots, one thread issues every matrix product,
+// and a warpgroup of 128 threads for each tile does the arithmetic, one row a
+// thread, so that a row's maximum, sum or delta needs no exchange. A product's
+// result comes from TMEM by rows; the probabilities (and their gradients) go
+// back to TMEM in bf16, where the next product takes them as its A operand
+// without a pass through shared memory:
+//   forward         S = Q K^T;  O += P V
+//   query gradient  S = Q K^T, dP = dO V^T;  dQ += dS K
+//   key gradient    S^T = K Q^T, dP^T = V dO^T;  dV += P^T dO, dK += dS^T Q
+// The gradient takes seven products where five would do with one kernel that
+// added its dQ shares in memory: each result then has one owner, so sums are
+// in a fixed order and no fp32 copy of dQ is kept.
+//
+// Two tiles (or two blocks on an SM) are in flight, so the products of one run
+// while the other's rows are computed.
+//
+// Rows of a neighbouring sequence that a tile's box reaches into are set to
+// zero in shared memory where a product would sum over them (0 x NaN), and
+// masked by comparison elsewhere.
+#include <cuda_bf16.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "dpb_checks.h"
+#include "dpb_device.cuh"
+#include "dpb_tensor_core.cuh"
+
+namespace dpb {
+namespace {
+
+using namespace tc;
+using bf16 = __nv_bfloat16;
+
+constexpr uint32_t kTries = 1u << 20;  // polls of a wait before it gives up
+constexpr int kRows = 128;             // rows of a tile (M of the products)
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Out {
+    bf16 *p;
+    int64_t ts, hs;
+};
+struct In {
+    const bf16 *p;
+    int64_t ts, hs;
+};
+
+struct AttnArgs {
+    CUtensorMap q, k, v, g;  // g: grad_o
+    const int32_t *cu_q, *cu_k;
+    int64_t total_q, total_k;
+    int seqs, max_q, max_k, hq, hkv, group, D, causal, tiles;
+    float scale, scale2;  // scale, and scale x log2 e
+    In o, go;
+    Out out, dq, dk, dv;
+    float *lse;
+    float *delta;
+    int32_t *status;
+};
+
+// One sequence: its tokens [q0, q0 + n) and [k0, k0 + m).
+struct Seq {
+    int q0, n, k0, m;
+    bool ok;
+};
+
+__device__ __forceinline__ Seq sequence(const AttnArgs &a, int s) {
+    int64_t q0 = 0, q1 = a.total_q, k0 = 0, k1 = a.total_k;
+    if (a.cu_q) q0 = a.cu_q[s], q1 = a.cu_q[s + 1];
+    if (a.cu_k) k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
+    Seq r;
+    r.ok = q0 >= 0 && q1 >= q0 && q1 <= a.total_q && k0 >= 0 && k1 >= k0 && k1 <= a.total_k && q1 - q0 <= a.max_q &&
+           k1 - k0 <= a.max_k;
+    r.q0 = (int)q0, r.n = (int)(q1 - q0), r.k0 = (int)k0, r.m = (int)(k1 - k0);
+    return r;
+}
+
+// A tile of `rows` rows of one head: DP / 64 boxes of 64 columns.
+template <int DP>
+__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap *map, int head, int token, int rows,
+                                          uint32_t bar) {
+#pragma unroll
+    for (int h = 0; h < DP / 64; ++h) copy_box(dst + h * rows * 128, map, 64 * h, head, token, bar);
+}
+
+// Zeroes rows [from, rows) of a tile. One warp.
+template <int DP>
+__device__ __forceinline__ void zero_rows(uint8_t *tile, int from, int rows) {
+    const int lane = threadIdx.x & 31;
+    for (int h = 0; h < DP / 64; ++h)
+        for (int i = from * 8 + lane; i < rows * 8; i += 32)
+            *reinterpret_cast<uint4 *>(tile + h * rows * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// The ring of slots that the copying warp fills and the products empty. Tile i
+// uses slot i % N for the (i / N)-th time.
+template <int N, int BYTES>
+struct Ring {
+    uint8_t *data;
+    uint32_t full, empty, tail;  // full[N], empty[N], tail
+    __device__ __forceinline__ uint32_t full_bar(int i) const { return full + 8 * (i % N); }
+    __device__ __forceinline__ uint32_t empty_bar(int i) const { return empty + 8 * (i % N); }
+    __device__ __forceinline__ uint32_t parity(int i) const { return (i / N) & 1; }
+    __device__ __forceinline__ uint8_t *slot(int i) const { return data + (i % N) * BYTES; }
+    __device__ __forceinline__ uint32_t addr(int i) const { return smem_addr(slot(i)); }
+    // All lanes: slot i is free (its previous products are done).
+    __device__ __forceinline__ bool wait_free(int i) const {
+        return i < N || __all_sync(kFull, bar_wait(empty_bar(i), parity(i) ^ 1, kTries));
+    }
+    // All lanes: copies rows [token, token + rows) of a head into slot i; where
+    // only `live` of them belong to the sequence (and `sums`: a product sums
+    // over them), the others are zeroed before the slot counts as full.
+    template <int DP>
+    __device__ __forceinline__ bool fill(int i, const CUtensorMap *map, int head, int token, int rows, int live,
+                                         bool sums, int &tails) const {
+        const bool leader = (threadIdx.x & 31) == 0;
+        if (!sums || live >= rows) {
+            if (leader) {
+                bar_arrive_expect(full_bar(i), BYTES);
+                copy_tile<DP>(addr(i), map, head, token, rows, full_bar(i));
+            }
+            __syncwarp();
+            return true;
+        }
+        if (leader) {
+            bar_arrive_expect(tail, BYTES);
+            copy_tile<DP>(addr(i), map, head, token, rows, tail);
+        }
+        __syncwarp();
+        const bool ok = __all_sync(kFull, bar_wait(tail, tails & 1, kTries));
+        ++tails;
+        if (!ok) return false;
+        zero_rows<DP>(slot(i), live, rows);
+        fence_async_shared();
+        __syncwarp();
+        if (leader) bar_arrive(full_bar(i));
+        __syncwarp();
+        return true;
+    }
+    // After a wait that gave up: every copy issued so far has landed (tiles
+    // [0, issued); bounded).
+    __device__ __forceinline__ void drain(int issued) const {
+        for (int i = max(0, issued - N); i < issued; ++i) bar_wait(full_bar(i), parity(i), kTries);
+    }
+};
+
+// 32 fp32 of a row as 32 bf16, 16 bytes at a time up to column D.
+__device__ __forceinline__ void write_row32(bf16 *row, int col, int D, const uint32_t (&v)[32], float f) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+        if (col + i < D) {
+            uint4 u;
+            u.x = pack_bf16(__uint_as_float(v[i]) * f, __uint_as_float(v[i + 1]) * f);
+            u.y = pack_bf16(__uint_as_float(v[i + 2]) * f, __uint_as_float(v[i + 3]) * f);
+            u.z = pack_bf16(__uint_as_float(v[i + 4]) * f, __uint_as_float(v[i + 5]) * f);
+            u.w = pack_bf16(__uint_as_float(v[i + 6]) * f, __uint_as_float(v[i + 7]) * f);
+            *reinterpret_cast<uint4 *>(row + col + i) = u;
+        }
+    }
+}
+
+__device__ __forceinline__ void write_zero_row(bf16 *row, int D) {
+    for (int i = 0; i < D; i += 8) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// Reads a row of DP fp32 from TMEM, scales it and writes its D columns; the
+// whole warp calls it, rows that are not live write nothing.
+template <int DP>
+__device__ __forceinline__ void write_tmem_row(uint32_t tmem, bf16 *row, int D, float f, bool live) {
+#pragma unroll
+    for (int c = 0; c < DP; c += 32) {
+        uint32_t v[32];
+        tmem_load(tmem + c, v);
+        load_wait(v);
+        if (live) write_row32(row, c, D, v, f);
+    }
+}
+
+// ---- forward ------------------------------------------------------------------
+
+template <int DP_, int BN_, int NS_>
+struct FwdShape {
+    static constexpr int DP = DP_, BN = BN_, NS = NS_;
+    static constexpr int kTile = kRows * DP * 2, kSlot = BN * DP * 2;
+    static constexpr int kColumns = 2 * (BN + DP);  // S (then P) and O of both tiles: a power of two
+    static constexpr int kBars = 1 + 2 * NS + 1 + 2 + 2 + 2 + 1;
+    static constexpr int kSmem = 1024 + 2 * kTile + NS * kSlot + 8 * kBars + 16;
+    static constexpr int kThreads = 320;
+};
+
+// Visible keys of query row i (of n, against m keys).
+__device__ __forceinline__ int visible(const AttnArgs &a, const Seq &q, int i) {
+    return a.causal ? max(0, min(q.m, i + q.m - q.n + 1)) : q.m;
+}
+
+// Blocks of BN keys that query tile `tile` has to see (0 where it has no rows).
+template <int BN>
+__device__ __forceinline__ int tile_blocks(const AttnArgs &a, const Seq &q, int tile) {
+    const int r0 = tile * kRows;
+    return r0 < q.n ? (visible(a, q, min(r0 + kRows, q.n) - 1) + BN - 1) / BN : 0;
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_forward_kernel(
+    const __grid_constant__ AttnArgs a) {
+    constexpr int DP = C::DP, BN = C::BN;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    // the longest rows first; the heads of a group side by side
+    const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
+    const int si = rest % a.seqs, pair = a.tiles - 1 - rest / a.seqs;
+    const Seq q = sequence(a, si);
+    if (!q.ok) {
+        if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
+        return;
+    }
+    if (pair * 2 * kRows >= q.n) return;
+
+    const int nb0 = tile_blocks<BN>(a, q, 2 * pair), nb1 = tile_blocks<BN>(a, q, 2 * pair + 1);
+    const int blocks = max(nb0, nb1);
+
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * C::kTile + C::NS * C::kSlot);
+    const uint32_t bar0 = smem_addr(bars);
+    const uint32_t q_full = bar0;
+    Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
+    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 16, o_full = p_full + 16, done = o_full + 16;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
+    if (threadIdx.x == 0) {
+        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < o_full ? 4 : 1);
+        bar_init_fence();
+    }
+    if (warp == 9) tmem_alloc(smem_addr(slot), C::kColumns);
+    if (warp == 8 && lane == 0 && blocks > 0) {
+        prefetch_map(&a.q);
+        prefetch_map(&a.k);
+        prefetch_map(&a.v);
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *slot;
+    bool failed = false;
+
+    if (warp == 8) {
+        // ---- copies: Q's tiles, then K_0, V_0, K_1, V_1, ...
+        const int kv_head = head / a.group;
+        if (blocks > 0) {
+            if (lane == 0) {
+                const int tiles = (2 * pair + 1) * kRows < q.n ? 2 : 1;
+                bar_arrive_expect(q_full, tiles * C::kTile);
+                for (int t = 0; t < tiles; ++t)
+                    copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * pair + t) * kRows, kRows,
+                                  q_full);
+            }
+            __syncwarp();
+        }
+        int issued = 0, tails = 0;
+        for (int j = 0; j < blocks && !failed; ++j) {
+            const int live = q.m - j * BN;
+            for (int kind = 0; kind < 2 && !failed; ++kind) {
+                failed = !ring.wait_free(issued) ||
+                         !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN, live,
+                                                 kind == 1, tails);
+                if (!failed) ++issued;
+            }
+        }
+        if (failed) {
+            ring.drain(issued);
+            bar_wait(q_full, 0, kTries);
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && blocks > 0) {
+            // ---- products: S of both tiles, then for each block O += P V and
+            // the next S of a tile as soon as its P is there
+            const uint32_t q_addr = smem_addr(smem);
+            auto scores = [&](int t, int j) {
+                const uint32_t kb = ring.addr(2 * j), qb = q_addr + t * C::kTile;
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k)
+                    mma_ss(tmem + t * BN, desc_k_inside(qb + (k / 4) * kRows * 128 + (k % 4) * 32),
+                           desc_k_inside(kb + (k / 4) * BN * 128 + (k % 4) * 32), mma_shape(BN, false), k > 0);
+                mma_commit(s_full + 8 * t);
+            };
+            failed = !bar_wait(q_full, 0, kTries) || !bar_wait(ring.full_bar(0), 0, kTries);
+            if (!failed) {
+                fence_after();
+                for (int t = 0; t < 2; ++t)
+                    if ((t ? nb1 : nb0) > 0) scores(t, 0);
+                mma_commit(ring.empty_bar(0));
+            }
+            for (int j = 0; j < blocks && !failed; ++j) {
+                const int vi = 2 * j + 1, ki = 2 * j + 2;
+                failed = !bar_wait(ring.full_bar(vi), ring.parity(vi), kTries) ||
+                         (j + 1 < blocks && !bar_wait(ring.full_bar(ki), ring.parity(ki), kTries));
+                const uint32_t vb = ring.addr(vi);
+                for (int t = 0; t < 2 && !failed; ++t) {
+                    if (j >= (t ? nb1 : nb0)) continue;
+                    failed = !bar_wait(p_full + 8 * t, j & 1, kTries);
+                    if (failed) break;
+                    fence_after();
+#pragma unroll
+                    for (int k = 0; k < BN / 16; ++k)
+                        mma_ts(tmem + 2 * BN + t * DP, tmem + t * BN + 8 * k, desc_k_rows(vb + k * 2048, BN * 128),
+                               mma_shape(DP, true), j > 0 || k > 0);
+                    if (j + 1 < (t ? nb1 : nb0))
+                        scores(t, j + 1);
+                    else
+                        mma_commit(o_full + 8 * t);
+                }
+                if (failed) break;
+                mma_commit(ring.empty_bar(vi));
+                if (j + 1 < blocks) mma_commit(ring.empty_bar(ki));
+            }
+            // every product, and every arrival that it makes, is done before
+            // the block's memory is given back
+            mma_commit(done);
+            failed |= !bar_wait(done, 0, kTries);
+        }
+        __syncwarp();
+    } else {
+        // ---- softmax: a row a thread
+        const int t = warp / 4, nb = t ? nb1 : nb0;
+        const int i = (2 * pair + t) * kRows + (threadIdx.x & 127);
+        const bool live = i < q.n;
+        const int lim = visible(a, q, i);
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 TMEM lanes
+        const uint32_t s_addr = tmem + lanes + t * BN, o_addr = tmem + lanes + 2 * BN + t * DP;
+        float top = 0.f, sum = 0.f;  // reference maximum (of scale2 S), sum of 2^(scale2 S - top)
+        for (int j = 0; j < nb; ++j) {
+            if (!__all_sync(kFull, bar_wait(s_full + 8 * t, j & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+            uint32_t s[BN / 32][32];
+#pragma unroll
+            for (int c = 0; c < BN / 32; ++c) tmem_load(s_addr + 32 * c, s[c]);
+#pragma unroll
+            for (int c = 0; c < BN / 32; ++c) load_wait(s[c]);
+            const int seen = lim - j * BN;  // visible columns of this block
+            if (!__all_sync(kFull, seen >= BN)) {
+#pragma unroll
+                for (int c = 0; c < BN; ++c)
+                    if (c >= seen) s[c / 32][c % 32] = 0xff800000u;  // -inf
+            }
+            float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < BN; c += 4) {
+                m0 = fmaxf(m0, fmaxf(__uint_as_float(s[c / 32][c % 32]), __uint_as_float(s[c / 32][c % 32 + 1])));
+                m1 = fmaxf(m1, fmaxf(__uint_as_float(s[c / 32][c % 32 + 2]), __uint_as_float(s[c / 32][c % 32 + 3])));
+            }
+            const float mx = fmaxf(m0, m1) * a.scale2;
+            if (j == 0) {
+                top = mx == -INFINITY ? 0.f : mx;
+            } else if (__any_sync(kFull, mx > top + 8.f)) {
+                // The running maximum is only followed when it has grown by a
+                // factor of 2^8: until then the sums stay far from overflow,
+                // and O is not touched. Products so far are done: this
+                // block's S came after them.
+                const float next = mx > top + 8.f ? mx : top, f = exp2_approx(top - next);
+                top = next;
+                sum *= f;
+#pragma unroll
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t v[32];
+                    tmem_load(o_addr + c, v);
+                    load_wait(v);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
+                    tmem_store(o_addr + c, v);
+                }
+            }
+            float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < BN; c += 64) {
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                    const int x = c + e;
+                    const float p0 = exp2_approx(fmaf(__uint_as_float(s[x / 32][x % 32]), a.scale2, -top));
+                    const float p1 = exp2_approx(fmaf(__uint_as_float(s[x / 32][x % 32 + 1]), a.scale2, -top));
+                    sums[e & 2] += p0;
+                    sums[(e & 2) + 1] += p1;
+                    p[e / 2] = pack_bf16(p0, p1);
+                }
+                tmem_store(s_addr + c / 2, p);
+            }
+            sum += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            store_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(p_full + 8 * t);
+        }
+        if (!failed && nb > 0) {
+            failed = !__all_sync(kFull, bar_wait(o_full + 8 * t, 0, kTries));
+            fence_after();
+        }
+        if (!failed) {
+            const int64_t token = q.q0 + (int64_t)i;
+            bf16 *row = a.out.p + token * a.out.ts + head * a.out.hs;
+            if (nb > 0)
+                write_tmem_row<DP>(o_addr, row, a.D, sum > 0.f || sum != sum ? 1.f / sum : 0.f, live);
+            else if (live)
+                write_zero_row(row, a.D);
+            if (live)
+                a.lse[(int64_t)head * a.total_q + token] =
+                    lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
+        }
+    }
+    if (failed && lane == 0) set_status(a.status, DPB_DEV_TIMEOUT);
+    fence_before();
+    __syncthreads();
+    if (warp == 9) tmem_free(tmem, C::kColumns);
+}
+
+// ---- gradient of the queries ------------------------------------------------------
+
+constexpr int kGradCols = 64;  // keys (or queries) of a streamed block in the gradients
+
+template <int DP_, int NT_, int NS_>
+struct GradShape {
+    static constexpr int DP = DP_, NT = NT_, NS = NS_;
+    static constexpr int kTile = kRows * DP * 2, kSlot = kGradCols * DP * 2;
+    static constexpr int kThreads = NT * 128 + 64;
+    static constexpr int kBars = 1 + 2 * NS + 1 + 2 * NT + 1;
+    static constexpr int kVec = NT * 4 * 2 * kGradCols * 4;  // a warp's lse and delta of a block of queries
+    // query gradient: S and dP (then dS) of each tile, dQ; key gradient: S^T
+    // (then P^T) and dP^T (then dS^T) of each buffer, dV and dK
+    static constexpr int kColumnsQ = NT * (128 + DP) <= 256 ? 256 : 512;
+    static constexpr int kColumnsK = NT * 128 + 2 * DP <= 256 ? 256 : 512;
+    static constexpr int kSmemQ = 1024 + 2 * NT * kTile + NS * kSlot + 8 * kBars + 16;
+    static constexpr int kSmemK = 1024 + 2 * kTile + NS * kSlot + kVec + 8 * kBars + 16;
+};
+
+// scores and grad_o V^T of a tile against one streamed block, into TMEM
+// columns [d, d + 64) and [d + 64, d + 128).
+template <int DP>
+__device__ __forceinline__ void two_products(uint32_t d, uint32_t a0, uint32_t b0, uint32_t a1, uint32_t b1) {
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+        mma_ss(d, desc_k_inside(a0 + (k / 4) * kRows * 128 + (k % 4) * 32),
+               desc_k_inside(b0 + (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+        mma_ss(d + kGradCols, desc_k_inside(a1 + (k / 4) * kRows * 128 + (k % 4) * 32),
+               desc_k_inside(b1 + (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
+}
+
+// d += a (TMEM, 64 columns of bf16) x a streamed block of 64 rows.
+template <int DP>
+__device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t b, bool add) {
+#pragma unroll
+    for (int k = 0; k < kGradCols / 16; ++k)
+        mma_ts(d, a + 8 * k, desc_k_rows(b + k * 2048, kGradCols * 128), mma_shape(DP, true), add || k > 0);
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) attention_grad_q_kernel(
+    const __grid_constant__ AttnArgs a) {
+    constexpr int DP = C::DP, NT = C::NT, BN = kGradCols;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
+    const int si = rest % a.seqs, first = (a.tiles - 1 - rest / a.seqs) * NT;
+    const Seq q = sequence(a, si);
+    if (!q.ok) {
+        if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
+        return;
+    }
+    if (first * kRows >= q.n) return;
+    const int nb0 = tile_blocks<BN>(a, q, first), nb1 = NT == 2 ? tile_blocks<BN>(a, q, first + 1) : 0;
+    const int blocks = max(nb0, nb1);
+
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * NT * C::kTile + C::NS * C::kSlot);
+    const uint32_t bar0 = smem_addr(bars), q_full = bar0;
+    Ring<C::NS, C::kSlot> ring{smem + 2 * NT * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
+    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 8 * NT, done = p_full + 8 * NT;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
+    constexpr int kCopier = 4 * NT, kIssuer = 4 * NT + 1;
+    if (threadIdx.x == 0) {
+        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < done ? 4 : 1);
+        bar_init_fence();
+    }
+    if (warp == kIssuer) tmem_alloc(smem_addr(slot), C::kColumnsQ);
+    if (warp == kCopier && lane == 0 && blocks > 0) {
+        prefetch_map(&a.q);
+        prefetch_map(&a.k);
+        prefetch_map(&a.v);
+        prefetch_map(&a.g);
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *slot;
+    const uint32_t dq_cols = NT * 128;
+    bool failed = false;
+
+    if (warp == kCopier) {
+        const int kv_head = head / a.group;
+        if (blocks > 0 && lane == 0) {
+            int tiles = 0;
+            for (int t = 0; t < NT; ++t) tiles += (first + t) * kRows < q.n;
+            bar_arrive_expect(q_full, 2 * tiles * C::kTile);
+            for (int t = 0; t < tiles; ++t) {
+                const int token = q.q0 + (first + t) * kRows;
+                copy_tile<DP>(smem_addr(smem) + 2 * t * C::kTile, &a.q, head, token, kRows, q_full);
+                copy_tile<DP>(smem_addr(smem) + (2 * t + 1) * C::kTile, &a.g, head, token, kRows, q_full);
+            }
+        }
+        __syncwarp();
+        int issued = 0, tails = 0;
+        for (int j = 0; j < blocks && !failed; ++j)
+            for (int kind = 0; kind < 2 && !failed; ++kind) {
+                failed = !ring.wait_free(issued) ||
+                         !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN,
+                                                 q.m - j * BN, kind == 0, tails);
+                if (!failed) ++issued;
+            }
+        if (failed) {
+            ring.drain(issued);
+            bar_wait(q_full, 0, kTries);
+        }
+    } else if (warp == kIssuer) {
+        if (lane == 0 && blocks > 0) {
+            const uint32_t q_addr = smem_addr(smem);
+            auto products = [&](int t, int j) {
+                two_products<DP>(tmem + 128 * t, q_addr + 2 * t * C::kTile, ring.addr(2 * j),
+                                 q_addr + (2 * t + 1) * C::kTile, ring.addr(2 * j + 1));
+                mma_commit(s_full + 8 * t);
+            };
+            auto wait_block = [&](int j) {
+                return bar_wait(ring.full_bar(2 * j), ring.parity(2 * j), kTries) &&
+                       bar_wait(ring.full_bar(2 * j + 1), ring.parity(2 * j + 1), kTries);
+            };
+            failed = !bar_wait(q_full, 0, kTries) || !wait_block(0);
+            if (!failed) {
+                fence_after();
+                for (int t = 0; t < NT; ++t)
+                    if ((t ? nb1 : nb0) > 0) products(t, 0);
+                mma_commit(ring.empty_bar(1));
+            }
+            for (int j = 0; j < blocks && !failed; ++j) {
+                failed = j + 1 < blocks && !wait_block(j + 1);
+                for (int t = 0; t < NT && !failed; ++t) {
+                    if (j >= (t ? nb1 : nb0)) continue;
+                    failed = !bar_wait(p_full + 8 * t, j & 1, kTries);
+                    if (failed) break;
+                    fence_after();
+                    sum_product<DP>(tmem + dq_cols + t * DP, tmem + 128 * t, ring.addr(2 * j), j > 0);
+                    if (j + 1 < (t ? nb1 : nb0)) products(t, j + 1);
+                }
+                if (failed) break;
+                mma_commit(ring.empty_bar(2 * j));
+                if (j + 1 < blocks) mma_commit(ring.empty_bar(2 * j + 3));
+            }
+            mma_commit(done);
+            failed |= !bar_wait(done, 0, kTries);
+        }
+        __syncwarp();
+    } else {
+        const int t = warp / 4, nb = t ? nb1 : nb0;
+        const int i = (first + t) * kRows + (threadIdx.x & 127);
+        const bool live = i < q.n;
+        const int64_t token = q.q0 + (int64_t)i;
+        const int lim = visible(a, q, i);
+        float lse2 = INFINITY, delta = 0.f;  // a row that sees nothing: every probability 0
+        if (live) {
+            const uint4 *o = reinterpret_cast<const uint4 *>(a.o.p + token * a.o.ts + head * a.o.hs);
+            const uint4 *g = reinterpret_cast<const uint4 *>(a.go.p + token * a.go.ts + head * a.go.hs);
+            for (int c = 0; c < a.D / 8; ++c) {
+                const uint4 x = o[c], y = g[c];
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    delta = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), delta);
+                    delta = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), delta);
+                }
+            }
+            a.delta[(int64_t)head * a.total_q + token] = delta;
+            const float l = a.lse[(int64_t)head * a.total_q + token];
+            lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
+        }
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        const uint32_t s_addr = tmem + lanes + 128 * t;
+        for (int j = 0; j < nb; ++j) {
+            if (!__all_sync(kFull, bar_wait(s_full + 8 * t, j & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+            uint32_t s[2][32], p[2][32], ds[32];
+            tmem_load(s_addr, s[0]);
+            tmem_load(s_addr + 32, s[1]);
+            tmem_load(s_addr + 64, p[0]);
+            tmem_load(s_addr + 96, p[1]);
+            load_wait(s[0]);
+            load_wait(s[1]);
+            load_wait(p[0]);
+            load_wait(p[1]);
+            const int seen = lim - j * BN;
+            const bool whole = __all_sync(kFull, seen >= BN);
+#pragma unroll
+            for (int c = 0; c < BN; c += 2) {
+                float d[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float pr = exp2_approx(fmaf(__uint_as_float(s[c / 32][c % 32 + e]), a.scale2, -lse2));
+                    d[e] = pr * (__uint_as_float(p[c / 32][c % 32 + e]) - delta);
+                    if (!whole && c + e >= seen) d[e] = 0.f;
+                }
+                ds[c / 2] = pack_bf16(d[0], d[1]);
+            }
+            tmem_store(s_addr, ds);
+            store_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(p_full + 8 * t);
+        }
+        bf16 *row = a.dq.p + token * a.dq.ts + head * a.dq.hs;
+        if (nb > 0) {
+            if (!failed) failed = !__all_sync(kFull, bar_wait(done, 0, kTries));
+            fence_after();
+            if (!failed) write_tmem_row<DP>(tmem + lanes + dq_cols + t * DP, row, a.D, a.scale, live);
+        } else if (live) {
+            write_zero_row(row, a.D);
+        }
+    }
+    if (failed && lane == 0) set_status(a.status, DPB_DEV_TIMEOUT);
+    fence_before();
+    __syncthreads();
+    if (warp == kIssuer) tmem_free(tmem, C::kColumnsQ);
+}
+
+// ---- gradient of keys and values ----------------------------------------------------
+
+template <class C>
+__global__ void __launch_bounds__(C::kThreads, C::kColumnsK == 256 ? 2 : 1) attention_grad_kv_kernel(
+    const __grid_constant__ AttnArgs a) {
+    constexpr int DP = C::DP, NT = C::NT, BN = kGradCols;
+    static_assert(C::NS >= 2 * (NT + 1), "a block being summed and the next of every buffer are held at once");
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const int head = blockIdx.x % a.hkv, rest = blockIdx.x / a.hkv;
+    const int si = rest % a.seqs, tile = rest / a.seqs;  // causal: the first keys are seen by most queries
+    const Seq q = sequence(a, si);
+    if (!q.ok) {
+        if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
+        return;
+    }
+    const int j0 = tile * kRows;
+    if (j0 >= q.m) return;
+    // blocks of queries from the first that sees a key of this tile, of every
+    // query head of the group in turn
+    const int off = q.m - q.n;
+    const int b0 = a.causal ? max(0, j0 - off) / BN : 0;
+    const int per_head = max(0, (q.n + BN - 1) / BN - b0);
+    const int blocks = per_head * a.group;
+
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * C::kTile + C::NS * C::kSlot + C::kVec);
+    const uint32_t bar0 = smem_addr(bars), k_full = bar0;
+    Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
+    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 8 * NT, done = p_full + 8 * NT;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
+    constexpr int kCopier = 4 * NT, kIssuer = 4 * NT + 1;
+    if (threadIdx.x == 0) {
+        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < done ? 4 : 1);
+        bar_init_fence();
+    }
+    if (warp == kIssuer) tmem_alloc(smem_addr(slot), C::kColumnsK);
+    if (warp == kCopier && lane == 0 && blocks > 0) {
+        prefetch_map(&a.q);
+        prefetch_map(&a.k);
+        prefetch_map(&a.v);
+        prefetch_map(&a.g);
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *slot;
+    const uint32_t dv_cols = NT * 128, dk_cols = dv_cols + DP;
+    bool failed = false;
+
+    if (warp == kCopier) {
+        if (blocks > 0 && lane == 0) {
+            bar_arrive_expect(k_full, 2 * C::kTile);
+            copy_tile<DP>(smem_addr(smem), &a.k, head, q.k0 + j0, kRows, k_full);
+            copy_tile<DP>(smem_addr(smem) + C::kTile, &a.v, head, q.k0 + j0, kRows, k_full);
+        }
+        __syncwarp();
+        int issued = 0, tails = 0;
+        for (int it = 0; it < blocks && !failed; ++it) {
+            const int h = head * a.group + it / per_head, i0 = (b0 + it % per_head) * BN;
+            for (int kind = 0; kind < 2 && !failed; ++kind) {
+                failed = !ring.wait_free(issued) ||
+                         !ring.template fill<DP>(issued, kind ? &a.g : &a.q, h, q.q0 + i0, BN, q.n - i0, true, tails);
+                if (!failed) ++issued;
+            }
+        }
+        if (failed) {
+            ring.drain(issued);
+            bar_wait(k_full, 0, kTries);
+        }
+    } else if (warp == kIssuer) {
+        if (lane == 0 && blocks > 0) {
+            const uint32_t k_addr = smem_addr(smem), v_addr = k_addr + C::kTile;
+            // S^T and dP^T of block `it` into buffer it % NT
+            auto products = [&](int it) {
+                if (!bar_wait(ring.full_bar(2 * it), ring.parity(2 * it), kTries) ||
+                    !bar_wait(ring.full_bar(2 * it + 1), ring.parity(2 * it + 1), kTries))
+                    return false;
+                fence_after();
+                two_products<DP>(tmem + 128 * (it % NT), k_addr, ring.addr(2 * it), v_addr, ring.addr(2 * it + 1));
+                mma_commit(s_full + 8 * (it % NT));
+                return true;
+            };
+            failed = !bar_wait(k_full, 0, kTries);
+            for (int it = 0; it < NT && it < blocks && !failed; ++it) failed = !products(it);
+            for (int it = 0; it < blocks && !failed; ++it) {
+                const int t = it % NT;
+                failed = !bar_wait(p_full + 8 * t, (it / NT) & 1, kTries);
+                if (failed) break;
+                fence_after();
+                sum_product<DP>(tmem + dv_cols, tmem + 128 * t, ring.addr(2 * it + 1), it > 0);
+                sum_product<DP>(tmem + dk_cols, tmem + 128 * t + 64, ring.addr(2 * it), it > 0);
+                mma_commit(ring.empty_bar(2 * it));
+                mma_commit(ring.empty_bar(2 * it + 1));
+                if (it + NT < blocks) failed = !products(it + NT);
+            }
+            mma_commit(done);
+            failed |= !bar_wait(done, 0, kTries);
+        }
+        __syncwarp();
+    } else {
+        const int t = warp / 4;
+        const int j = j0 + (threadIdx.x & 127);
+        const bool live = j < q.m;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        const uint32_t s_addr = tmem + lanes + 128 * t;
+        float *vec = reinterpret_cast<float *>(smem + 2 * C::kTile + C::NS * C::kSlot) + warp * 2 * BN;
+        // lane's share of a block's lse x log2 e (infinite for rows that are
+        // not there or see nothing: probability 0) and delta
+        float nl[2], nd[2];
+        auto fetch = [&](int it) {
+            const int h = head * a.group + it / per_head, i0 = (b0 + it % per_head) * BN;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int i = i0 + lane + 32 * e;
+                nl[e] = INFINITY, nd[e] = 0.f;
+                if (i < q.n) {
+                    const int64_t at = (int64_t)h * a.total_q + q.q0 + i;
+                    const float l = a.lse[at];
+                    nl[e] = l == -INFINITY ? INFINITY : l * kLog2e;
+                    nd[e] = a.delta[at];
+                }
+            }
+        };
+        if (t < blocks) fetch(t);
+        for (int it = t; it < blocks; it += NT) {
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                vec[lane + 32 * e] = nl[e];
+                vec[BN + lane + 32 * e] = nd[e];
+            }
+            __syncwarp();
+            if (it + NT < blocks) fetch(it + NT);
+            if (!__all_sync(kFull, bar_wait(s_full + 8 * t, (it / NT) & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+            // masked: query i sees key j when i >= j - off
+            const int low = a.causal ? j - off - (b0 + it % per_head) * BN : 0;
+            const bool whole = __all_sync(kFull, low <= 0);
+            uint32_t pp[32], ds[32];
+#pragma unroll
+            for (int c0 = 0; c0 < BN; c0 += 32) {
+                uint32_t s[32], p[32];
+                tmem_load(s_addr + c0, s);
+                tmem_load(s_addr + 64 + c0, p);
+                load_wait(s);
+                load_wait(p);
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 l4 = *reinterpret_cast<const float4 *>(vec + c0 + c);
+                    const float4 d4 = *reinterpret_cast<const float4 *>(vec + BN + c0 + c);
+                    const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
+                    float pr[4], d[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        pr[e] = exp2_approx(fmaf(__uint_as_float(s[c + e]), a.scale2, -ls[e]));
+                        d[e] = pr[e] * (__uint_as_float(p[c + e]) - dl[e]);
+                        if (!whole && c0 + c + e < low) pr[e] = d[e] = 0.f;
+                    }
+                    pp[(c0 + c) / 2] = pack_bf16(pr[0], pr[1]);
+                    pp[(c0 + c) / 2 + 1] = pack_bf16(pr[2], pr[3]);
+                    ds[(c0 + c) / 2] = pack_bf16(d[0], d[1]);
+                    ds[(c0 + c) / 2 + 1] = pack_bf16(d[2], d[3]);
+                }
+            }
+            tmem_store(s_addr, pp);
+            tmem_store(s_addr + 64, ds);
+            store_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(p_full + 8 * t);
+        }
+        const int64_t token = q.k0 + (int64_t)j;
+        bf16 *rv = a.dv.p + token * a.dv.ts + head * a.dv.hs, *rk = a.dk.p + token * a.dk.ts + head * a.dk.hs;
+        if (blocks > 0) {
+            if (!failed) failed = !__all_sync(kFull, bar_wait(done, 0, kTries));
+            fence_after();
+            if (!failed && t == 0) write_tmem_row<DP>(tmem + lanes + dv_cols, rv, a.D, 1.f, live);
+            if (!failed && t == NT - 1) write_tmem_row<DP>(tmem + lanes + dk_cols, rk, a.D, a.scale, live);
+        } else if (live && t == 0) {
+            write_zero_row(rv, a.D);
+            write_zero_row(rk, a.D);
+        }
+    }
+    if (failed && lane == 0) set_status(a.status, DPB_DEV_TIMEOUT);
+    fence_before();
+    __syncthreads();
+    if (warp == kIssuer) tmem_free(tmem, C::kColumnsK);
+}
+
+// ---- host side ------------------------------------------------------------------
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) !=
+                cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    }();
+    return fn;
+}
+
+// Map of a [tokens][heads][D] tensor in boxes of 64 columns x `rows` tokens of
+// one head; columns past D read as zero.
+dpb_status make_map(CUtensorMap *map, const dpb_heads *h, int64_t tokens, int heads, int D, int rows) {
+    std::memset(map, 0, sizeof(*map));
+    if (tokens == 0) return DPB_OK;
+    const auto fn = encoder();
+    if (!fn) return fail(DPB_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+    const int64_t hs = heads > 1 ? h->head_stride : 64, ts = tokens > 1 ? h->token_stride : 64;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)hs * 2, (cuuint64_t)ts * 2};
+    const cuuint32_t box[3] = {64, 1, (cuuint32_t)rows}, one[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, h->data, dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(DPB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+    return DPB_OK;
+}
+
+dpb_status check_rows(const dpb_heads *h, const char *name, int64_t tokens, int heads) {
+    if (tokens == 0) return DPB_OK;
+    if (!h) return fail(DPB_ERR_INVALID_ARG, "%s is NULL", name);
+    DPB_CHECK(need(h->data, name, 16));
+    if ((tokens > 1 && (h->token_stride <= 0 || h->token_stride % 8)) ||
+        (heads > 1 && (h->head_stride <= 0 || h->head_stride % 8)))
+        return fail(DPB_ERR_INVALID_ARG, "the strides of %s must be positive multiples of 8", name);
+    if (h->token_stride >= (1ll << 38) || h->head_stride >= (1ll << 38))
+        return fail(DPB_ERR_UNSUPPORTED, "the strides of %s are too large", name);
+    return DPB_OK;
+}
+
+dpb_status check_attention(const dpb_attention_config *c) {
+    if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->dtype != DPB_BF16) return fail(DPB_ERR_UNSUPPORTED, "attention takes bf16 rows");
+    if (c->seqs < 0 || c->total_q < 0 || c->total_k < 0 || c->max_q < 0 || c->max_k < 0)
+        return fail(DPB_ERR_INVALID_ARG, "a size is negative");
+    if (c->total_q > 0x7fffff00ll || c->total_k > 0x7fffff00ll)
+        return fail(DPB_ERR_UNSUPPORTED, "at most 2^31 - 256 tokens");
+    if (c->heads_q < 1 || c->heads_kv < 1 || c->heads_q % c->heads_kv)
+        return fail(DPB_ERR_INVALID_ARG, "heads_q must be a positive multiple of heads_kv");
+    if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8)
+        return fail(DPB_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 in [8, 128]");
+    if (!(c->scale > 0.f) || !std::isfinite(c->scale))
+        return fail(DPB_ERR_INVALID_ARG, "scale must be positive and finite");
+    return DPB_OK;
+}
+
+dpb_status check_offsets(const dpb_attention_config *c, const int32_t *cu_q, const int32_t *cu_k) {
+    if ((cu_q == nullptr) != (cu_k == nullptr))
+        return fail(DPB_ERR_INVALID_ARG, "cu_q and cu_k must both be given or both be NULL");
+    if (!cu_q && c->seqs != 1) return fail(DPB_ERR_INVALID_ARG, "without offsets there is one sequence");
+    if (cu_q) {
+        DPB_CHECK(need(cu_q, "cu_q", 4));
+        DPB_CHECK(need(cu_k, "cu_k", 4));
+    }
+    return DPB_OK;
+}
+
+size_t attention_workspace(const dpb_attention_config *c) {
+    return kStatusBytes + sizeof(float) * (size_t)c->heads_q * (size_t)c->total_q;
+}
+
+void fill_args(AttnArgs &a, const dpb_attention_config *c, const int32_t *cu_q, const int32_t *cu_k, void *ws) {
+    a.cu_q = cu_q;
+    a.cu_k = cu_k;
+    a.total_q = c->total_q;
+    a.total_k = c->total_k;
+    a.seqs = c->seqs;
+    a.max_q = c->max_q;
+    a.max_k = c->max_k;
+    a.hq = c->heads_q;
+    a.hkv = c->heads_kv;
+    a.group = c->heads_q / c->heads_kv;
+    a.D = c->head_dim;
+    a.causal = c->causal != 0;
+    a.scale = c->scale;
+    a.scale2 = c->scale * kLog2e;
+    a.status = static_cast<int32_t *>(ws);
+}
+
+In in_rows(const dpb_heads *h) { return h ? In{static_cast<const bf16 *>(h->data), h->token_stride, h->head_stride} : In{}; }
+Out out_rows(const dpb_heads *h) { return h ? Out{static_cast<bf16 *>(h->data), h->token_stride, h->head_stride} : Out{}; }
+
+template <typename K>
+cudaError_t launch_tiles(K kernel, AttnArgs &a, int tiles, int heads, int threads, int smem, cudaStream_t s) {
+    a.tiles = tiles;
+    const int64_t blocks = (int64_t)tiles * heads * a.seqs;
+    if (blocks == 0) return cudaSuccess;
+    if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(kernel), smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<(unsigned)blocks, threads, smem, s>>>(a);
+    return cudaGetLastError();
+}
+
+using Fwd64 = FwdShape<64, 64, 8>;
+using Fwd128 = FwdShape<128, 128, 4>;
+using Grad64 = GradShape<64, 1, 8>;
+using Grad128 = GradShape<128, 2, 4>;   // queries: 4 slots of K, V
+using GradK128 = GradShape<128, 2, 8>;  // keys: a block more for each buffer
+
+template <class C>
+cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
+    return launch_tiles(attention_forward_kernel<C>, a, (a.max_q + 2 * kRows - 1) / (2 * kRows), a.hq, C::kThreads,
+                        C::kSmem, s);
+}
+
+}  // namespace
+}  // namespace dpb
+
+using namespace dpb;
+
+extern "C" {
+
+dpb_status dpb_attention_workspace_size(const dpb_attention_config *cfg, size_t *bytes) {
+    DPB_CHECK(check_attention(cfg));
+    if (!bytes) return fail(DPB_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = attention_workspace(cfg);
+    return DPB_OK;
+}
+
+dpb_status dpb_attention_forward(const dpb_attention_config *cfg, const dpb_heads *q, const dpb_heads *k,
+                                 const dpb_heads *v, const int32_t *cu_q, const int32_t *cu_k, const dpb_heads *o,
+                                 float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    DPB_CHECK(check_attention(cfg));
+    if (cfg->total_q == 0 || cfg->seqs == 0) return DPB_OK;
+    DPB_CHECK(check_rows(q, "q", cfg->total_q, cfg->heads_q));
+    DPB_CHECK(check_rows(k, "k", cfg->total_k, cfg->heads_kv));
+    DPB_CHECK(check_rows(v, "v", cfg->total_k, cfg->heads_kv));
+    DPB_CHECK(check_rows(o, "o", cfg->total_q, cfg->heads_q));
+    DPB_CHECK(check_offsets(cfg, cu_q, cu_k));
+    DPB_CHECK(need(lse, "lse", 4));
+    DPB_CHECK(need_workspace(workspace, workspace_bytes, kStatusBytes));
+    AttnArgs a{};
+    fill_args(a, cfg, cu_q, cu_k, workspace);
+    const bool small = cfg->head_dim <= 64;
+    DPB_CHECK(make_map(&a.q, q, cfg->total_q, cfg->heads_q, cfg->head_dim, kRows));
+    DPB_CHECK(make_map(&a.k, k, cfg->total_k, cfg->heads_kv, cfg->head_dim, small ? Fwd64::BN : Fwd128::BN));
+    DPB_CHECK(make_map(&a.v, v, cfg->total_k, cfg->heads_kv, cfg->head_dim, small ? Fwd64::BN : Fwd128::BN));
+    a.out = out_rows(o);
+    a.lse = lse;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return launch_status(small ? launch_attention_forward<Fwd64>(a, s) : launch_attention_forward<Fwd128>(a, s),
+                         "attention_forward");
+}
+
+dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_heads *q, const dpb_heads *k,
+                                  const dpb_heads *v, const dpb_heads *o, const float *lse, const dpb_heads *grad_o,
+                                  const int32_t *cu_q, const int32_t *cu_k, const dpb_heads *grad_q,
+                                  const dpb_heads *grad_k, const dpb_heads *grad_v, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+    DPB_CHECK(check_attention(cfg));
+    if (cfg->seqs == 0 || (cfg->total_q == 0 && cfg->total_k == 0)) return DPB_OK;
+    DPB_CHECK(check_rows(q, "q", cfg->total_q, cfg->heads_q));
+    DPB_CHECK(check_rows(k, "k", cfg->total_k, cfg->heads_kv));
+    DPB_CHECK(check_rows(v, "v", cfg->total_k, cfg->heads_kv));
+    DPB_CHECK(check_rows(o, "o", cfg->total_q, cfg->heads_q));
+    DPB_CHECK(check_rows(grad_o, "grad_o", cfg->total_q, cfg->heads_q));
+    DPB_CHECK(check_rows(grad_q, "grad_q", cfg->total_q, cfg->heads_q));
+    DPB_CHECK(check_rows(grad_k, "grad_k", cfg->total_k, cfg->heads_kv));
+    DPB_CHECK(check_rows(grad_v, "grad_v", cfg->total_k, cfg->heads_kv));
+    DPB_CHECK(check_offsets(cfg, cu_q, cu_k));
+    if (cfg->total_q > 0) DPB_CHECK(need(lse, "lse", 4));
+    DPB_CHECK(need_workspace(workspace, workspace_bytes, attention_workspace(cfg)));
+    AttnArgs a{};
+    fill_args(a, cfg, cu_q, cu_k, workspace);
+    a.delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + kStatusBytes);
+    a.lse = const_cast<float *>(lse);
+    a.o = in_rows(o);
+    a.go = in_rows(grad_o);
+    a.dq = out_rows(grad_q);
+    a.dk = out_rows(grad_k);
+    a.dv = out_rows(grad_v);
+    const bool small = cfg->head_dim <= 64;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int D = cfg->head_dim;
+    // queries in tiles, keys in blocks; then the other way round
+    DPB_CHECK(make_map(&a.q, q, cfg->total_q, cfg->heads_q, D, kRows));
+    DPB_CHECK(make_map(&a.g, grad_o, cfg->total_q, cfg->heads_q, D, kRows));
+    DPB_CHECK(make_map(&a.k, k, cfg->total_k, cfg->heads_kv, D, kGradCols));
+    DPB_CHECK(make_map(&a.v, v, cfg->total_k, cfg->heads_kv, D, kGradCols));
+    const int nt = small ? Grad64::NT : Grad128::NT, qt = (cfg->max_q + nt * kRows - 1) / (nt * kRows);
+    DPB_CHECK(launch_status(
+        small ? launch_tiles(attention_grad_q_kernel<Grad64>, a, qt, a.hq, Grad64::kThreads, Grad64::kSmemQ, s)
+              : launch_tiles(attention_grad_q_kernel<Grad128>, a, qt, a.hq, Grad128::kThreads, Grad128::kSmemQ, s),
+        "attention_backward (queries)"));
+    DPB_CHECK(make_map(&a.q, q, cfg->total_q, cfg->heads_q, D, kGradCols));
+    DPB_CHECK(make_map(&a.g, grad_o, cfg->total_q, cfg->heads_q, D, kGradCols));
+    DPB_CHECK(make_map(&a.k, k, cfg->total_k, cfg->heads_kv, D, kRows));
+    DPB_CHECK(make_map(&a.v, v, cfg->total_k, cfg->heads_kv, D, kRows));
+    const int kt = (cfg->max_k + kRows - 1) / kRows;
+    return launch_status(
+        small ? launch_tiles(attention_grad_kv_kernel<Grad64>, a, kt, a.hkv, Grad64::kThreads, Grad64::kSmemK, s)
+              : launch_tiles(attention_grad_kv_kernel<GradK128>, a, kt, a.hkv, GradK128::kThreads, GradK128::kSmemK, s),
+        "attention_backward (keys and values)");
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@ library has not been built: there is no CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -22,6 +23,8 @@ F32, BF16 = 0, 1
 SELECT_GLOBAL, SELECT_PER_LEVEL = 0, 1
 SCORING_CONTRACTION, SCORING_COSET_WHT = 0, 1
 DEV_BAD_INDEX, DEV_BAD_SIGMA, DEV_SHORT_CODE, DEV_TIMEOUT = 0x1, 0x2, 0x4, 0x8
+DEV_BAD_LENGTH = 0x10
+STATE_BLOCK = 256  # values of an 8-bit optimiser state that share a scale
 
 _STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported configuration", 3: "CUDA error",
            4: "device wait timed out", 5: "out of memory", 6: "device-side error flagged"}
@@ -62,11 +65,38 @@ class Config(ctypes.Structure):
                 "field_poly": self.field_poly, "generator_seed": self.generator_seed, "scoring": self.scoring}
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("heads_q", ctypes.c_int32), ("heads_k", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("normalise", ctypes.c_int32), ("positions_n", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class AttentionConfig(ctypes.Structure):
+    _fields_ = [("total_q", ctypes.c_int64), ("total_k", ctypes.c_int64), ("seqs", ctypes.c_int32),
+                ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32), ("heads_q", ctypes.c_int32),
+                ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class AdamWConfig(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64),
+                ("seed", ctypes.c_uint64), ("grad_scale", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32)]
+
+
 _lib = None
 EXPORTS = ("dpb_plan_create", "dpb_plan_destroy", "dpb_plan_config", "dpb_plan_tables",
            "dpb_code_length", "dpb_workspace_size", "dpb_encode", "dpb_decode", "dpb_backward",
            "dpb_workspace_status", "dpb_status_string", "dpb_last_error", "dpb_encode_noalloc",
-           "dpb_stats_accumulate", "dpb_stats_update", "dpb_forward", "dpb_debug_set_wait_limit")
+           "dpb_stats_accumulate", "dpb_stats_update", "dpb_forward", "dpb_debug_set_wait_limit",
+           "dpb_qk_norm_rope", "dpb_qk_norm_rope_backward", "dpb_rope_workspace_size",
+           "dpb_attention_forward", "dpb_attention_backward", "dpb_attention_workspace_size", "dpb_adamw_step")
 
 
 def library_path() -> str:
@@ -100,6 +130,14 @@ def load(path: Optional[str] = None):
     lib.dpb_stats_accumulate.argtypes = [vp, vp, i64, vp, vp, vp, ctypes.c_int32, vp, vp, sz, vp]
     lib.dpb_stats_update.argtypes = [vp, vp, ctypes.c_float, vp, vp, vp]
     lib.dpb_forward.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    hp, rc, ac = ctypes.POINTER(Heads), ctypes.POINTER(RopeConfig), ctypes.POINTER(AttentionConfig)
+    lib.dpb_qk_norm_rope.argtypes = [rc, hp, hp, vp, vp, vp, vp, vp, hp, hp, vp, sz, vp]
+    lib.dpb_qk_norm_rope_backward.argtypes = [rc, hp, hp, hp, hp, vp, vp, vp, vp, vp, hp, hp, vp, vp, vp, sz, vp]
+    lib.dpb_rope_workspace_size.argtypes = [rc, ctypes.POINTER(sz)]
+    lib.dpb_attention_forward.argtypes = [ac, hp, hp, hp, vp, vp, hp, vp, vp, sz, vp]
+    lib.dpb_attention_backward.argtypes = [ac, hp, hp, hp, hp, vp, hp, vp, vp, hp, hp, hp, vp, sz, vp]
+    lib.dpb_attention_workspace_size.argtypes = [ac, ctypes.POINTER(sz)]
+    lib.dpb_adamw_step.argtypes = [ctypes.POINTER(AdamWConfig), vp, ctypes.c_int32, vp]
     lib.dpb_status_string.argtypes = [st]
     lib.dpb_status_string.restype = ctypes.c_char_p
     lib.dpb_last_error.argtypes = []
@@ -404,3 +442,321 @@ def workspace_status(workspace: torch.Tensor, clear: bool = False, stream=None) 
     v = ctypes.c_int32()
     load().dpb_workspace_status(_ptr(workspace), int(clear), ctypes.byref(v), _stream(stream))
     return v.value
+
+
+# ---- the training step around the bottleneck -------------------------------
+
+_shared_ws: dict = {}
+
+
+def _enter(device, stream):
+    """(torch stream, context) of a call: a stream given that is not the
+    current one is entered, so that outputs and workspaces are allocated on it."""
+    if device.type != "cuda":
+        raise ValueError("tensors must be on a CUDA device")
+    cur = torch.cuda.current_stream(device)
+    if torch.cuda.current_device() == device.index and (stream is None or stream == cur):
+        return cur, contextlib.nullcontext()
+    s = cur if stream is None else stream
+    return s, torch.cuda.stream(s)
+
+
+def _lend(stream, current, *tensors):
+    """Tells the allocator of tensors that another stream than the current one reads."""
+    if stream is not None and stream != current:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _shared_workspace(nbytes: int, device, stream) -> torch.Tensor:
+    """The workspace of the calls below made without one: one per (device,
+    stream), grown as needed; its status bits accumulate until read (status())."""
+    key = (device.index, stream.cuda_stream)
+    ws = _shared_ws.get(key)
+    if ws is None or ws.numel() < nbytes:
+        new = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        if ws is not None:
+            new[:256].copy_(ws[:256])
+        ws = _shared_ws[key] = new
+    return ws
+
+
+def status(device=None, stream=None, clear: bool = True) -> int:
+    """The DPB_DEV_* bits that the calls below, made without a workspace, left
+    on ``stream`` (synchronises it); cleared by default."""
+    dev = torch.device(device or "cuda")
+    s = stream if stream is not None else torch.cuda.current_stream(dev)
+    ws = _shared_ws.get((dev.index if dev.index is not None else torch.cuda.current_device(), s.cuda_stream))
+    return 0 if ws is None else workspace_status(ws, clear=clear, stream=s)
+
+
+def _heads(t: torch.Tensor, name: str, dtype, shape) -> Heads:
+    """A [tokens, heads, dim] tensor whose last dimension is dense, as the library takes it."""
+    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a CUDA {dtype} tensor of shape {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"the last dimension of {name} must be dense")
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, device):
+    if t is not None and (t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() != numel):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} values on {device}")
+    return _ptr(t)
+
+
+def rope_tables(positions: int, rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None,
+                factor: float = 1.0, original: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                device=None):
+    """(cos, sin) fp32 [positions, rot_dim / 2] for qk_norm_rope, from angles in
+    64 bits: position x base^(-2 i / rot_dim). For contexts ``factor`` times
+    longer than trained on, ``scaling``: "linear" (positions divided by factor),
+    "ntk" (a larger base: base x factor^(R / (R - 2))), or "yarn" (pairs that
+    turn fewer than beta_slow times in ``original`` positions are divided by
+    factor, those above beta_fast turns are kept, a ramp between, and both
+    tables are multiplied by 0.1 ln(factor) + 1)."""
+    import math
+    if rot_dim <= 0 or rot_dim % 2 or positions < 1:
+        raise ValueError("rot_dim must be even and positive, positions at least 1")
+    if scaling not in (None, "linear", "ntk", "yarn") or (scaling and factor < 1.0):
+        raise ValueError("scaling must be None, 'linear', 'ntk' or 'yarn', with factor >= 1")
+    if scaling == "ntk":
+        if rot_dim == 2:
+            raise ValueError("'ntk' needs rot_dim above 2")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    freq = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    gain = 1.0
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "yarn":
+        if original < 1:
+            raise ValueError("'yarn' needs original, the trained context")
+        turns = original * freq / (2 * math.pi)
+        keep = ((turns - beta_slow) / (beta_fast - beta_slow)).clamp(0.0, 1.0)
+        freq = freq * keep + freq / factor * (1 - keep)
+        gain = 0.1 * math.log(factor) + 1.0
+    ang = torch.arange(positions, dtype=torch.float64)[:, None] * freq
+    cos, sin = (ang.cos() * gain).float(), (ang.sin() * gain).float()
+    return cos.to(device or "cuda"), sin.to(device or "cuda")
+
+
+def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise):
+    T, hq, D = q.shape
+    if k.dim() != 3 or k.shape[0] != T or k.shape[2] != D or k.dtype != q.dtype:
+        raise ValueError("q and k must be [tokens, heads, dim] with the same tokens, dim and dtype")
+    if q.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"q and k must be float32 or bfloat16, got {q.dtype}")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin must both be given or both be None")
+    rot, rows = 0, 0
+    if cos is not None:
+        if cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must be [positions, rot_dim / 2] of the same shape")
+        rows, rot = cos.shape[0], 2 * cos.shape[1]
+        _dense(cos, "cos", torch.float32, cos.numel(), q.device)
+        _dense(sin, "sin", torch.float32, cos.numel(), q.device)
+    _dense(weight_q, "weight_q", q.dtype, D, q.device)
+    _dense(weight_k, "weight_k", q.dtype, D, q.device)
+    _dense(positions, "positions", torch.int32, T, q.device)
+    return RopeConfig(T, hq, k.shape[1], D, rot, int(interleaved), int(normalise), rows,
+                      F32 if q.dtype == torch.float32 else BF16, eps, 0)
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, weight_q=None, weight_k=None, cos=None, sin=None, positions=None,
+                 eps: float = 1e-6, interleaved: bool = False, normalise: bool = True, q_out=None, k_out=None,
+                 workspace=None, stream=None):
+    """dpb_qk_norm_rope. q [T, Hq, D], k [T, Hk, D], fp32 or bf16 (views of one
+    packed projection are fine); cos, sin from rope_tables() (None: no
+    rotation); positions int32 [T] (None: 0, 1, ...). Returns (q, k) normalised
+    and rotated."""
+    c = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
+    lib = load()
+    s, ctx = _enter(q.device, stream)
+    with ctx:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+        ws = _shared_workspace(256, q.device, s) if workspace is None else workspace
+        hs = [_heads(t, n, q.dtype, like.shape) for t, n, like in
+              ((q, "q", q), (k, "k", k), (q_out, "q_out", q), (k_out, "k_out", k))]
+        _check(lib.dpb_qk_norm_rope(c, hs[0], hs[1], _ptr(weight_q), _ptr(weight_k), _ptr(cos), _ptr(sin),
+                                    _ptr(positions), hs[2], hs[3], _ptr(ws), ws.numel() * ws.element_size(),
+                                    s.cuda_stream))
+    _lend(stream, torch.cuda.current_stream(q.device), q, k, weight_q, weight_k, cos, sin, positions)
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Tensor, grad_k_out: torch.Tensor,
+                          weight_q=None, weight_k=None, cos=None, sin=None, positions=None, eps: float = 1e-6,
+                          interleaved: bool = False, normalise: bool = True, weight_grads: bool = True, grad_q=None,
+                          grad_k=None, workspace=None, stream=None):
+    """dpb_qk_norm_rope_backward. Returns (grad_q, grad_k, grad_weight_q,
+    grad_weight_k): the last two fp32 [D], or None without ``normalise`` or
+    ``weight_grads``."""
+    c = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
+    lib = load()
+    D = q.shape[2]
+    s, ctx = _enter(q.device, stream)
+    with ctx:
+        grad_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if grad_q is None else grad_q
+        grad_k = torch.empty(k.shape, dtype=k.dtype, device=k.device) if grad_k is None else grad_k
+        gw = torch.empty((2, D), dtype=torch.float32, device=q.device) if normalise and weight_grads else None
+        if workspace is None:
+            n = ctypes.c_size_t()
+            _check(lib.dpb_rope_workspace_size(c, n))
+            workspace = _shared_workspace(n.value, q.device, s)
+        hs = [_heads(t, n, q.dtype, like.shape) for t, n, like in
+              ((q, "q", q), (k, "k", k), (grad_q_out, "grad_q_out", q), (grad_k_out, "grad_k_out", k),
+               (grad_q, "grad_q", q), (grad_k, "grad_k", k))]
+        _check(lib.dpb_qk_norm_rope_backward(
+            c, hs[0], hs[1], hs[2], hs[3], _ptr(weight_q), _ptr(weight_k), _ptr(cos), _ptr(sin), _ptr(positions), hs[4],
+            hs[5], None if gw is None else gw.data_ptr(), None if gw is None else gw.data_ptr() + 4 * D,
+            _ptr(workspace), workspace.numel() * workspace.element_size(), s.cuda_stream))
+    _lend(stream, torch.cuda.current_stream(q.device), q, k, grad_q_out, grad_k_out, weight_q, weight_k, cos, sin,
+          positions)
+    return (grad_q, grad_k) + ((None, None) if gw is None else (gw[0], gw[1]))
+
+
+def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        if t.dim() != 3 or t.dtype != torch.bfloat16:
+            raise ValueError(f"{n} must be a bfloat16 tensor [tokens, heads, dim], got {t.dtype} {list(t.shape)}")
+    if cu_k is None and cu_q is not None:
+        if q.shape[0] != k.shape[0]:
+            raise ValueError("cu_k is needed: q and k have different token counts")
+        cu_k, max_k = cu_q, max_q
+    if (cu_q is None) != (cu_k is None):
+        raise ValueError("cu_q and cu_k must both be given or both be None")
+    seqs = 1
+    if cu_q is not None:
+        seqs = cu_q.numel() - 1
+        if seqs < 0 or cu_q.dim() != 1:
+            raise ValueError("cu_q must be 1-D with one entry more than there are sequences")
+        _dense(cu_q, "cu_q", torch.int32, seqs + 1, q.device)
+        _dense(cu_k, "cu_k", torch.int32, seqs + 1, q.device)
+    max_q = q.shape[0] if max_q is None else min(int(max_q), q.shape[0])
+    max_k = k.shape[0] if max_k is None else min(int(max_k), k.shape[0])
+    c = AttentionConfig(q.shape[0], k.shape[0], seqs, max_q, max_k, q.shape[1], k.shape[1], q.shape[2], int(causal),
+                        BF16, q.shape[2] ** -0.5 if scale is None else float(scale), 0)
+    return c, cu_q, cu_k
+
+
+def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, cu_k=None,
+                      max_q: Optional[int] = None, max_k: Optional[int] = None, causal: bool = True,
+                      scale: Optional[float] = None, out=None, lse=None, workspace=None, stream=None):
+    """dpb_attention_forward. q [Tq, Hq, D], k and v [Tk, Hkv, D] bf16 (views
+    of one packed projection are fine); cu_q, cu_k int32 [sequences + 1] token
+    offsets (None: one sequence; cu_k None: as cu_q), max_q, max_k the longest
+    sequences' lengths (None: the token count, which only costs empty blocks);
+    scale defaults to D^-1/2. Returns (o [Tq, Hq, D], lse fp32 [Hq, Tq])."""
+    c, cu_q, cu_k = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
+    lib = load()
+    Tq, Hq, D = q.shape
+    s, ctx = _enter(q.device, stream)
+    with ctx:
+        out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device) if out is None else out
+        lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device) if lse is None else lse
+        ws = _shared_workspace(256, q.device, s) if workspace is None else workspace
+        kv = (k.shape[0], k.shape[1], D)
+        hs = [_heads(t, n, q.dtype, shape) for t, n, shape in
+              ((q, "q", q.shape), (k, "k", kv), (v, "v", kv), (out, "out", q.shape))]
+        _check(lib.dpb_attention_forward(c, hs[0], hs[1], hs[2], _ptr(cu_q), _ptr(cu_k), hs[3],
+                                         _dense(lse, "lse", torch.float32, Hq * Tq, q.device), _ptr(ws),
+                                         ws.numel() * ws.element_size(), s.cuda_stream))
+    _lend(stream, torch.cuda.current_stream(q.device), q, k, v, cu_q, cu_k)
+    return out, lse
+
+
+def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       grad_o: torch.Tensor, cu_q=None, cu_k=None, max_q: Optional[int] = None,
+                       max_k: Optional[int] = None, causal: bool = True, scale: Optional[float] = None, grad_q=None,
+                       grad_k=None, grad_v=None, workspace=None, stream=None):
+    """dpb_attention_backward with the forward's inputs, its o and lse, and the
+    gradient of o. Returns (grad_q, grad_k, grad_v)."""
+    c, cu_q, cu_k = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
+    lib = load()
+    s, ctx = _enter(q.device, stream)
+    with ctx:
+        grad_q, grad_k, grad_v = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g
+                                  for g, x in ((grad_q, q), (grad_k, k), (grad_v, v)))
+        if workspace is None:
+            n = ctypes.c_size_t()
+            _check(lib.dpb_attention_workspace_size(c, n))
+            workspace = _shared_workspace(n.value, q.device, s)
+        kv = (k.shape[0], k.shape[1], q.shape[2])
+        hs = [_heads(t, n, q.dtype, shape) for t, n, shape in
+              ((q, "q", q.shape), (k, "k", kv), (v, "v", kv), (o, "o", q.shape), (grad_o, "grad_o", q.shape),
+               (grad_q, "grad_q", q.shape), (grad_k, "grad_k", kv), (grad_v, "grad_v", kv))]
+        _check(lib.dpb_attention_backward(
+            c, hs[0], hs[1], hs[2], hs[3], _dense(lse, "lse", torch.float32, q.shape[0] * q.shape[1], q.device), hs[4],
+            _ptr(cu_q), _ptr(cu_k), hs[5], hs[6], hs[7], _ptr(workspace),
+            workspace.numel() * workspace.element_size(), s.cuda_stream))
+    _lend(stream, torch.cuda.current_stream(q.device), q, k, v, o, lse, grad_o, cu_q, cu_k)
+    return grad_q, grad_k, grad_v
+
+
+class AdamWGroup:
+    """What dpb_adamw_step takes of a list of parameters and their states: the
+    states are one flat tensor each of the parameter's size, float32, or
+    float8_e4m3fn codes with a float32 scale for each STATE_BLOCK values
+    (ceil(n / STATE_BLOCK) of them). Tensors are held, addresses are read anew
+    at every step."""
+
+    def __init__(self, params, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_scale=None):
+        import numpy as np
+        self.params, self.exp_avg, self.exp_avg_sq = list(params), list(exp_avg), list(exp_avg_sq)
+        self.scales = (None if exp_avg_scale is None else list(exp_avg_scale),
+                       None if exp_avg_sq_scale is None else list(exp_avg_sq_scale))
+        if not self.params:
+            raise ValueError("no parameters")
+        p0 = self.params[0]
+        if p0.dtype not in (torch.float32, torch.bfloat16) or not p0.is_cuda:
+            raise ValueError("parameters must be float32 or bfloat16 CUDA tensors")
+        self.dtype, self.device = p0.dtype, p0.device
+        self.state_bits = 32 if exp_avg_scale is None and exp_avg_sq_scale is None else 8
+        sd = torch.float32 if self.state_bits == 32 else torch.float8_e4m3fn
+        kinds = [(self.exp_avg, "exp_avg"), (self.exp_avg_sq, "exp_avg_sq")]
+        if self.state_bits == 8:
+            if None in self.scales:
+                raise ValueError("8-bit states need both scales")
+            kinds += [(self.scales[0], "exp_avg_scale"), (self.scales[1], "exp_avg_sq_scale")]
+        for ts, name in kinds:
+            if len(ts) != len(self.params):
+                raise ValueError(f"{len(ts)} tensors of {name} for {len(self.params)} parameters")
+        for i, p in enumerate(self.params):
+            if p.dtype != self.dtype or p.device != self.device or not p.is_contiguous():
+                raise ValueError(f"parameter {i} must be a contiguous {self.dtype} tensor on {self.device}")
+            for ts, name in kinds:
+                scale = name.endswith("scale")
+                n = -(-p.numel() // STATE_BLOCK) if scale else p.numel()
+                _dense(ts[i], f"{name}[{i}]", torch.float32 if scale else sd, n, self.device)
+        self._numel = [p.numel() for p in self.params]
+        self._table = np.zeros((len(self.params), 7), dtype=np.int64)  # rows of dpb_adamw_tensor
+
+    def step(self, grads, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, step: int = 1,
+             seed: int = 0, grad_scale: Optional[torch.Tensor] = None, stream=None):
+        """dpb_adamw_step: one step of every parameter that has a gradient (None
+        leaves it as it is). ``grad_scale``: a float32 tensor of one value that
+        multiplies the gradients; where it is not finite nothing changes."""
+        t = self._table
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
+        dt, dev = self.dtype, self.device
+        for i, (g, n) in enumerate(zip(grads, self._numel)):
+            if g is not None and (g.dtype != dt or g.device != dev or g.numel() != n or not g.is_contiguous()):
+                raise ValueError(f"gradient {i} must be a contiguous {dt} tensor of {n} values on {dev}")
+        gs = _dense(grad_scale, "grad_scale", torch.float32, 1, dev)
+        for col, ts in ((0, self.params), (2, self.exp_avg), (3, self.exp_avg_sq), (4, self.scales[0]),
+                        (5, self.scales[1])):
+            if ts is not None:
+                t[:, col] = [x.data_ptr() for x in ts]
+        t[:, 1] = [0 if g is None else g.data_ptr() for g in grads]
+        t[:, 6] = [0 if g is None else n for g, n in zip(grads, self._numel)]
+        c = AdamWConfig(lr, betas[0], betas[1], eps, weight_decay, step, seed & (2**64 - 1), gs,
+                        F32 if dt == torch.float32 else BF16, self.state_bits)
+        s, ctx = _enter(dev, stream)
+        with ctx:
+            _check(load().dpb_adamw_step(c, t.ctypes.data, len(self.params), s.cuda_stream))
+        if stream is not None:
+            _lend(stream, torch.cuda.current_stream(dev), grad_scale, *grads, *self.params, *self.exp_avg,
+                  *self.exp_avg_sq, *(self.scales[0] or ()), *(self.scales[1] or ()))

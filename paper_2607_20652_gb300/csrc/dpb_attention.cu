@@ -110,6 +110,7 @@ struct Ring {
     __device__ __forceinline__ uint32_t full_bar(int i) const { return full + 8 * (i % N); }
     __device__ __forceinline__ uint32_t empty_bar(int i) const { return empty + 8 * (i % N); }
     __device__ __forceinline__ uint32_t parity(int i) const { return (i / N) & 1; }
+    __device__ __forceinline__ bool wait_full(int i) const { return bar_wait(full_bar(i), parity(i), kTries); }
     __device__ __forceinline__ uint8_t *slot(int i) const { return data + (i % N) * BYTES; }
     __device__ __forceinline__ uint32_t addr(int i) const { return smem_addr(slot(i)); }
     // All lanes: slot i is free (its previous products are done).
@@ -190,11 +191,18 @@ __device__ __forceinline__ void write_tmem_row(uint32_t tmem, bf16 *row, int D, 
 template <int DP_, int BN_, int NS_>
 struct FwdShape {
     static constexpr int DP = DP_, BN = BN_, NS = NS_;
+    // P has columns of its own where there is room beside S and O: the next S
+    // is then computed as soon as this one has been read. Otherwise P takes
+    // the place of S, and the next S comes after its product.
+    static constexpr bool kOwnP = 2 * (BN + DP + BN / 2) <= 512;
     static constexpr int kTile = kRows * DP * 2, kSlot = BN * DP * 2;
-    static constexpr int kColumns = 2 * (BN + DP);  // S (then P) and O of both tiles: a power of two
-    static constexpr int kBars = 1 + 2 * NS + 1 + 2 + 2 + 2 + 1;
+    static constexpr int kColumns = 512;
+    static constexpr int kColO = 2 * BN, kColP = kOwnP ? 2 * (BN + DP) : 0, kStepP = kOwnP ? BN / 2 : BN;
+    static constexpr int kBars = 1 + 2 * NS + 1 + 2 * 5 + 1;
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kSlot + 8 * kBars + 16;
-    static constexpr int kThreads = 320;
+    static constexpr int kThreads = 384;  // two softmax warpgroups, one of the copying and the issuing warp
+    // registers of a softmax thread and of the others: 2 x 128 x 232 + 128 x 40 = 384 x 168
+    static constexpr int kRegsRow = 232, kRegsOther = 40;
 };
 
 // Visible keys of query row i (of n, against m keys).
@@ -210,7 +218,7 @@ __device__ __forceinline__ int tile_blocks(const AttnArgs &a, const Seq &q, int 
 }
 
 template <class C>
-__global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_forward_kernel(
+__global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(
     const __grid_constant__ AttnArgs a) {
     constexpr int DP = C::DP, BN = C::BN;
     extern __shared__ uint8_t smem_raw[];
@@ -218,25 +226,27 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     // the longest rows first; the heads of a group side by side
     const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
-    const int si = rest % a.seqs, pair = a.tiles - 1 - rest / a.seqs;
+    const int si = rest % a.seqs, rows2 = a.tiles - 1 - rest / a.seqs;
     const Seq q = sequence(a, si);
     if (!q.ok) {
         if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
         return;
     }
-    if (pair * 2 * kRows >= q.n) return;
+    if (rows2 * 2 * kRows >= q.n) return;
 
-    const int nb0 = tile_blocks<BN>(a, q, 2 * pair), nb1 = tile_blocks<BN>(a, q, 2 * pair + 1);
+    const int nb0 = tile_blocks<BN>(a, q, 2 * rows2), nb1 = tile_blocks<BN>(a, q, 2 * rows2 + 1);
     const int blocks = max(nb0, nb1);
 
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * C::kTile + C::NS * C::kSlot);
     const uint32_t bar0 = smem_addr(bars);
     const uint32_t q_full = bar0;
     Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
-    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 16, o_full = p_full + 16, done = o_full + 16;
+    // per tile: S is there, P is there, S has been read, P's product is done, O is done
+    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 16, s_read = p_full + 16,
+                   p_done = s_read + 16, o_full = p_done + 16, done = o_full + 16;
     uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
     if (threadIdx.x == 0) {
-        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < o_full ? 4 : 1);
+        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < p_done ? 4 : 1);
         bar_init_fence();
     }
     if (warp == 9) tmem_alloc(smem_addr(slot), C::kColumns);
@@ -251,15 +261,17 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
     const uint32_t tmem = *slot;
     bool failed = false;
 
-    if (warp == 8) {
+    if (warp >= 8) {
+        give_registers<C::kRegsOther>();
+        if (warp == 8) {
         // ---- copies: Q's tiles, then K_0, V_0, K_1, V_1, ...
         const int kv_head = head / a.group;
         if (blocks > 0) {
             if (lane == 0) {
-                const int tiles = (2 * pair + 1) * kRows < q.n ? 2 : 1;
+                const int tiles = (2 * rows2 + 1) * kRows < q.n ? 2 : 1;
                 bar_arrive_expect(q_full, tiles * C::kTile);
                 for (int t = 0; t < tiles; ++t)
-                    copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * pair + t) * kRows, kRows,
+                    copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * rows2 + t) * kRows, kRows,
                                   q_full);
             }
             __syncwarp();
@@ -278,18 +290,24 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
             ring.drain(issued);
             bar_wait(q_full, 0, kTries);
         }
-    } else if (warp == 9) {
-        if (lane == 0 && blocks > 0) {
-            // ---- products: S of both tiles, then for each block O += P V and
-            // the next S of a tile as soon as its P is there
+        } else if (warp == 9) {
+        if (blocks > 0 && elect_one()) {
+            // ---- products
             const uint32_t q_addr = smem_addr(smem);
             auto scores = [&](int t, int j) {
-                const uint32_t kb = ring.addr(2 * j), qb = q_addr + t * C::kTile;
+                const uint64_t kd = desc_k_inside(ring.addr(2 * j)), qd = desc_k_inside(q_addr + t * C::kTile);
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
-                    mma_ss(tmem + t * BN, desc_k_inside(qb + (k / 4) * kRows * 128 + (k % 4) * 32),
-                           desc_k_inside(kb + (k / 4) * BN * 128 + (k % 4) * 32), mma_shape(BN, false), k > 0);
+                    mma_ss(tmem + t * BN, desc_at(qd, (k / 4) * kRows * 128 + (k % 4) * 32),
+                           desc_at(kd, (k / 4) * BN * 128 + (k % 4) * 32), mma_shape(BN, false), k > 0);
                 mma_commit(s_full + 8 * t);
+            };
+            auto values = [&](int t, int j) {
+                const uint64_t vd = desc_k_rows(ring.addr(2 * j + 1), BN * 128);
+#pragma unroll
+                for (int k = 0; k < BN / 16; ++k)
+                    mma_ts(tmem + C::kColO + t * DP, tmem + C::kColP + t * C::kStepP + 8 * k, desc_at(vd, k * 2048),
+                           mma_shape(DP, true), j > 0 || k > 0);
             };
             failed = !bar_wait(q_full, 0, kTries) || !bar_wait(ring.full_bar(0), 0, kTries);
             if (!failed) {
@@ -300,26 +318,35 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
             }
             for (int j = 0; j < blocks && !failed; ++j) {
                 const int vi = 2 * j + 1, ki = 2 * j + 2;
-                failed = !bar_wait(ring.full_bar(vi), ring.parity(vi), kTries) ||
-                         (j + 1 < blocks && !bar_wait(ring.full_bar(ki), ring.parity(ki), kTries));
-                const uint32_t vb = ring.addr(vi);
+                if (j + 1 < blocks) failed = !bar_wait(ring.full_bar(ki), ring.parity(ki), kTries);
+                if (C::kOwnP) {
+                    for (int t = 0; t < 2 && !failed; ++t)
+                        if (j + 1 < (t ? nb1 : nb0)) {
+                            failed = !bar_wait(s_read + 8 * t, j & 1, kTries);
+                            if (failed) break;
+                            fence_after();
+                            scores(t, j + 1);
+                        }
+                    if (failed) break;
+                    if (j + 1 < blocks) mma_commit(ring.empty_bar(ki));
+                }
+                failed = failed || !bar_wait(ring.full_bar(vi), ring.parity(vi), kTries);
                 for (int t = 0; t < 2 && !failed; ++t) {
-                    if (j >= (t ? nb1 : nb0)) continue;
+                    const int nb = t ? nb1 : nb0;
+                    if (j >= nb) continue;
                     failed = !bar_wait(p_full + 8 * t, j & 1, kTries);
                     if (failed) break;
                     fence_after();
-#pragma unroll
-                    for (int k = 0; k < BN / 16; ++k)
-                        mma_ts(tmem + 2 * BN + t * DP, tmem + t * BN + 8 * k, desc_k_rows(vb + k * 2048, BN * 128),
-                               mma_shape(DP, true), j > 0 || k > 0);
-                    if (j + 1 < (t ? nb1 : nb0))
-                        scores(t, j + 1);
-                    else
+                    values(t, j);
+                    if (C::kOwnP) mma_commit(p_done + 8 * t);
+                    if (j + 1 == nb)
                         mma_commit(o_full + 8 * t);
+                    else if (!C::kOwnP)
+                        scores(t, j + 1);  // takes P's place: products run in the order of their issue
                 }
                 if (failed) break;
                 mma_commit(ring.empty_bar(vi));
-                if (j + 1 < blocks) mma_commit(ring.empty_bar(ki));
+                if (!C::kOwnP && j + 1 < blocks) mma_commit(ring.empty_bar(ki));
             }
             // every product, and every arrival that it makes, is done before
             // the block's memory is given back
@@ -327,15 +354,20 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
             failed |= !bar_wait(done, 0, kTries);
         }
         __syncwarp();
+        }
     } else {
+        take_registers<C::kRegsRow>();
         // ---- softmax: a row a thread
         const int t = warp / 4, nb = t ? nb1 : nb0;
-        const int i = (2 * pair + t) * kRows + (threadIdx.x & 127);
+        const int i = (2 * rows2 + t) * kRows + (threadIdx.x & 127);
         const bool live = i < q.n;
         const int lim = visible(a, q, i);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 TMEM lanes
-        const uint32_t s_addr = tmem + lanes + t * BN, o_addr = tmem + lanes + 2 * BN + t * DP;
-        float top = 0.f, sum = 0.f;  // reference maximum (of scale2 S), sum of 2^(scale2 S - top)
+        const uint32_t s_addr = tmem + lanes + t * BN, o_addr = tmem + lanes + C::kColO + t * DP;
+        const uint32_t p_addr = tmem + lanes + C::kColP + t * C::kStepP;
+        float top = 0.f;  // reference maximum, of scale2 S
+        uint64_t sum2[2] = {0, 0};  // four shares of the sum of 2^(scale2 S - top)
+        const uint64_t scale2 = pair(a.scale2, a.scale2);
         for (int j = 0; j < nb; ++j) {
             if (!__all_sync(kFull, bar_wait(s_full + 8 * t, j & 1, kTries))) {
                 failed = true;
@@ -347,30 +379,44 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
             for (int c = 0; c < BN / 32; ++c) tmem_load(s_addr + 32 * c, s[c]);
 #pragma unroll
             for (int c = 0; c < BN / 32; ++c) load_wait(s[c]);
+            if (C::kOwnP) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(s_read + 8 * t);
+            }
             const int seen = lim - j * BN;  // visible columns of this block
             if (!__all_sync(kFull, seen >= BN)) {
 #pragma unroll
                 for (int c = 0; c < BN; ++c)
                     if (c >= seen) s[c / 32][c % 32] = 0xff800000u;  // -inf
             }
-            float m0 = -INFINITY, m1 = -INFINITY;
+            float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < BN; c += 4) {
-                m0 = fmaxf(m0, fmaxf(__uint_as_float(s[c / 32][c % 32]), __uint_as_float(s[c / 32][c % 32 + 1])));
-                m1 = fmaxf(m1, fmaxf(__uint_as_float(s[c / 32][c % 32 + 2]), __uint_as_float(s[c / 32][c % 32 + 3])));
+            for (int c = 0; c < BN; c += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    m[e] = max3(m[e], __uint_as_float(s[c / 32][c % 32 + 2 * e]),
+                                __uint_as_float(s[c / 32][c % 32 + 2 * e + 1]));
+            const float mx = fmaxf(max3(m[0], m[1], m[2]), m[3]) * a.scale2;
+            // this tile's products so far have to be done before P is written
+            // or O is scaled (with P in place of S, this block's S came after them)
+            if (C::kOwnP && j > 0 && !__all_sync(kFull, bar_wait(p_done + 8 * t, (j - 1) & 1, kTries))) {
+                failed = true;
+                break;
             }
-            const float mx = fmaxf(m0, m1) * a.scale2;
+            fence_after();
             if (j == 0) {
                 top = mx == -INFINITY ? 0.f : mx;
             } else if (__any_sync(kFull, mx > top + 8.f)) {
                 // The running maximum is only followed when it has grown by a
                 // factor of 2^8: until then the sums stay far from overflow,
-                // and O is not touched. Products so far are done: this
-                // block's S came after them.
+                // and O is not touched.
                 const float next = mx > top + 8.f ? mx : top, f = exp2_approx(top - next);
                 top = next;
-                sum *= f;
-#pragma unroll
+                const uint64_t f2 = pair(f, f);
+                sum2[0] = mul2(sum2[0], f2);
+                sum2[1] = mul2(sum2[1], f2);
+#pragma unroll 1
                 for (int c = 0; c < DP; c += 32) {
                     uint32_t v[32];
                     tmem_load(o_addr + c, v);
@@ -380,27 +426,27 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
                     tmem_store(o_addr + c, v);
                 }
             }
-            float sums[4] = {0.f, 0.f, 0.f, 0.f};
+            const uint64_t top2 = pair(-top, -top);
 #pragma unroll
             for (int c = 0; c < BN; c += 64) {
                 uint32_t p[32];
 #pragma unroll
                 for (int e = 0; e < 64; e += 2) {
                     const int x = c + e;
-                    const float p0 = exp2_approx(fmaf(__uint_as_float(s[x / 32][x % 32]), a.scale2, -top));
-                    const float p1 = exp2_approx(fmaf(__uint_as_float(s[x / 32][x % 32 + 1]), a.scale2, -top));
-                    sums[e & 2] += p0;
-                    sums[(e & 2) + 1] += p1;
+                    const float2 y = unpair(fma2(pair_bits(s[x / 32][x % 32], s[x / 32][x % 32 + 1]), scale2, top2));
+                    const float p0 = exp2_approx(y.x), p1 = exp2_approx(y.y);
+                    sum2[(e / 2) & 1] = add2(sum2[(e / 2) & 1], pair(p0, p1));
                     p[e / 2] = pack_bf16(p0, p1);
                 }
-                tmem_store(s_addr + c / 2, p);
+                tmem_store(p_addr + c / 2, p);
             }
-            sum += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             store_wait();
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(p_full + 8 * t);
         }
+        const float2 sums = unpair(add2(sum2[0], sum2[1]));
+        const float sum = sums.x + sums.y;
         if (!failed && nb > 0) {
             failed = !__all_sync(kFull, bar_wait(o_full + 8 * t, 0, kTries));
             fence_after();
@@ -417,7 +463,7 @@ __global__ void __launch_bounds__(C::kThreads, C::DP == 64 ? 2 : 1) attention_fo
                     lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
         }
     }
-    if (failed && lane == 0) set_status(a.status, DPB_DEV_TIMEOUT);
+    if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
     fence_before();
     __syncthreads();
     if (warp == 9) tmem_free(tmem, C::kColumns);
@@ -446,22 +492,24 @@ struct GradShape {
 // columns [d, d + 64) and [d + 64, d + 128).
 template <int DP>
 __device__ __forceinline__ void two_products(uint32_t d, uint32_t a0, uint32_t b0, uint32_t a1, uint32_t b1) {
+    const uint64_t da0 = desc_k_inside(a0), db0 = desc_k_inside(b0), da1 = desc_k_inside(a1), db1 = desc_k_inside(b1);
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k)
-        mma_ss(d, desc_k_inside(a0 + (k / 4) * kRows * 128 + (k % 4) * 32),
-               desc_k_inside(b0 + (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
+        mma_ss(d, desc_at(da0, (k / 4) * kRows * 128 + (k % 4) * 32),
+               desc_at(db0, (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k)
-        mma_ss(d + kGradCols, desc_k_inside(a1 + (k / 4) * kRows * 128 + (k % 4) * 32),
-               desc_k_inside(b1 + (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
+        mma_ss(d + kGradCols, desc_at(da1, (k / 4) * kRows * 128 + (k % 4) * 32),
+               desc_at(db1, (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
 }
 
 // d += a (TMEM, 64 columns of bf16) x a streamed block of 64 rows.
 template <int DP>
 __device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t b, bool add) {
+    const uint64_t db = desc_k_rows(b, kGradCols * 128);
 #pragma unroll
     for (int k = 0; k < kGradCols / 16; ++k)
-        mma_ts(d, a + 8 * k, desc_k_rows(b + k * 2048, kGradCols * 128), mma_shape(DP, true), add || k > 0);
+        mma_ts(d, a + 8 * k, desc_at(db, k * 2048), mma_shape(DP, true), add || k > 0);
 }
 
 template <class C>
@@ -532,7 +580,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) atte
             bar_wait(q_full, 0, kTries);
         }
     } else if (warp == kIssuer) {
-        if (lane == 0 && blocks > 0) {
+        if (blocks > 0 && elect_one()) {
             const uint32_t q_addr = smem_addr(smem);
             auto products = [&](int t, int j) {
                 two_products<DP>(tmem + 128 * t, q_addr + 2 * t * C::kTile, ring.addr(2 * j),
@@ -636,7 +684,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) atte
             write_zero_row(row, a.D);
         }
     }
-    if (failed && lane == 0) set_status(a.status, DPB_DEV_TIMEOUT);
+    if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
     fence_before();
     __syncthreads();
     if (warp == kIssuer) tmem_free(tmem, C::kColumnsQ);
@@ -713,7 +761,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsK == 256 ? 2 : 1) atte
             bar_wait(k_full, 0, kTries);
         }
     } else if (warp == kIssuer) {
-        if (lane == 0 && blocks > 0) {
+        if (blocks > 0 && elect_one()) {
             const uint32_t k_addr = smem_addr(smem), v_addr = k_addr + C::kTile;
             // S^T and dP^T of block `it` into buffer it % NT
             auto products = [&](int it) {
@@ -829,7 +877,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsK == 256 ? 2 : 1) atte
             write_zero_row(rk, a.D);
         }
     }
-    if (failed && lane == 0) set_status(a.status, DPB_DEV_TIMEOUT);
+    if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
     fence_before();
     __syncthreads();
     if (warp == kIssuer) tmem_free(tmem, C::kColumnsK);
@@ -946,14 +994,28 @@ cudaError_t launch_tiles(K kernel, AttnArgs &a, int tiles, int heads, int thread
     return cudaGetLastError();
 }
 
-using Fwd64 = FwdShape<64, 64, 8>;
+using Fwd64 = FwdShape<64, 128, 6>;
 using Fwd128 = FwdShape<128, 128, 4>;
 using Grad64 = GradShape<64, 1, 8>;
 using Grad128 = GradShape<128, 2, 4>;   // queries: 4 slots of K, V
 using GradK128 = GradShape<128, 2, 8>;  // keys: a block more for each buffer
 
+// A register split draws on what the block is launched with: a build whose
+// kernel got fewer registers must not run it (its threads would wait forever).
+template <class C>
+bool registers_cover(const void *kernel) {
+    cudaFuncAttributes f;
+    if (cudaFuncGetAttributes(&f, kernel) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    return f.numRegs * C::kThreads >= 128 * (C::kThreads / 128 - 1) * C::kRegsRow + 128 * C::kRegsOther;
+}
+
 template <class C>
 cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
+    static const bool covered = registers_cover<C>(reinterpret_cast<const void *>(attention_forward_kernel<C>));
+    if (!covered) return cudaErrorLaunchOutOfResources;
     return launch_tiles(attention_forward_kernel<C>, a, (a.max_q + 2 * kRows - 1) / (2 * kRows), a.hq, C::kThreads,
                         C::kSmem, s);
 }

@@ -154,36 +154,55 @@ struct Ring {
     }
 };
 
-// 32 fp32 of a row as 32 bf16, 16 bytes at a time up to column D.
-__device__ __forceinline__ void write_row32(bf16 *row, int col, int D, const uint32_t (&v)[32], float f) {
-#pragma unroll
-    for (int i = 0; i < 32; i += 8) {
-        if (col + i < D) {
-            uint4 u;
-            u.x = pack_bf16(__uint_as_float(v[i]) * f, __uint_as_float(v[i + 1]) * f);
-            u.y = pack_bf16(__uint_as_float(v[i + 2]) * f, __uint_as_float(v[i + 3]) * f);
-            u.z = pack_bf16(__uint_as_float(v[i + 4]) * f, __uint_as_float(v[i + 5]) * f);
-            u.w = pack_bf16(__uint_as_float(v[i + 6]) * f, __uint_as_float(v[i + 7]) * f);
-            *reinterpret_cast<uint4 *>(row + col + i) = u;
-        }
-    }
-}
-
 __device__ __forceinline__ void write_zero_row(bf16 *row, int D) {
     for (int i = 0; i < D; i += 8) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Reads a row of DP fp32 from TMEM, scales it and writes its D columns; the
-// whole warp calls it, rows that are not live write nothing.
+// Writes this warp's 32 rows of a result from TMEM (DP fp32 a lane, times f)
+// as bf16: through `stage` (32 rows of DP bf16 in shared memory, 16-byte
+// pieces exchanged within 8 so that neither side meets bank conflicts), so
+// that the warp's stores to memory cover whole rows. Rows from `rows` on are
+// left out.
 template <int DP>
-__device__ __forceinline__ void write_tmem_row(uint32_t tmem, bf16 *row, int D, float f, bool live) {
+__device__ __forceinline__ void write_rows(uint32_t tmem, uint8_t *stage, const Out &out, int64_t token, int head,
+                                           int rows, int D, float f) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kPieces = DP / 8;
 #pragma unroll
     for (int c = 0; c < DP; c += 32) {
         uint32_t v[32];
         tmem_load(tmem + c, v);
         load_wait(v);
-        if (live) write_row32(row, c, D, v, f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                u[e] = pack_bf16(__uint_as_float(v[8 * i + 2 * e]) * f, __uint_as_float(v[8 * i + 2 * e + 1]) * f);
+            *reinterpret_cast<uint4 *>(stage + lane * DP * 2 + (((c / 8 + i) ^ (lane & 7)) * 16)) =
+                make_uint4(u[0], u[1], u[2], u[3]);
+        }
     }
+    __syncwarp();
+    bf16 *base = out.p + token * out.ts + head * out.hs;
+#pragma unroll 4
+    for (int i = lane; i < 32 * kPieces; i += 32) {
+        const int r = i / kPieces, piece = i % kPieces;
+        if (r < rows && piece * 8 < D)
+            *reinterpret_cast<uint4 *>(base + r * out.ts + piece * 8) =
+                *reinterpret_cast<const uint4 *>(stage + r * DP * 2 + ((piece ^ (r & 7)) * 16));
+    }
+}
+
+// The block's set-up: the copying warp makes the barriers and goes on at once
+// (its first copies are under way while TMEM is allocated); the others wait.
+template <int THREADS>
+__device__ __forceinline__ void setup_arrive() {
+    asm volatile("barrier.cta.arrive 1, %0;" ::"n"(THREADS) : "memory");
+}
+template <int THREADS>
+__device__ __forceinline__ void setup_wait() {
+    asm volatile("barrier.cta.sync 1, %0;" ::"n"(THREADS) : "memory");
 }
 
 // ---- forward ------------------------------------------------------------------
@@ -198,7 +217,7 @@ struct FwdShape {
     static constexpr int kTile = kRows * DP * 2, kSlot = BN * DP * 2;
     static constexpr int kColumns = 512;
     static constexpr int kColO = 2 * BN, kColP = kOwnP ? 2 * (BN + DP) : 0, kStepP = kOwnP ? BN / 2 : BN;
-    static constexpr int kBars = 1 + 2 * NS + 1 + 2 * 5 + 1;
+    static constexpr int kBars = 1 + 2 * NS + 1 + 2 * 6 + 1;
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kSlot + 8 * kBars + 16;
     static constexpr int kThreads = 384;  // two softmax warpgroups, one of the copying and the issuing warp
     // registers of a softmax thread and of the others: 2 x 128 x 232 + 128 x 40 = 384 x 168
@@ -218,9 +237,9 @@ __device__ __forceinline__ int tile_blocks(const AttnArgs &a, const Seq &q, int 
 }
 
 template <class C>
-__global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(
-    const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int DP = C::DP, BN = C::BN;
+    constexpr int kCopier = 8, kScores = 9, kValues = C::kOwnP ? 10 : 9;  // warps
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
@@ -241,58 +260,55 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(
     const uint32_t bar0 = smem_addr(bars);
     const uint32_t q_full = bar0;
     Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
-    // per tile: S is there, P is there, S has been read, P's product is done, O is done
-    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 16, s_read = p_full + 16,
+    // per tile: S is there, each half of P is there, S has been read, P's
+    // product is done, O is done
+    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 16, s_read = p_full + 32,
                    p_done = s_read + 16, o_full = p_done + 16, done = o_full + 16;
     uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
-    if (threadIdx.x == 0) {
-        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < p_done ? 4 : 1);
-        bar_init_fence();
-    }
-    if (warp == 9) tmem_alloc(smem_addr(slot), C::kColumns);
-    if (warp == 8 && lane == 0 && blocks > 0) {
-        prefetch_map(&a.q);
-        prefetch_map(&a.k);
-        prefetch_map(&a.v);
-    }
-    fence_before();
-    __syncthreads();
-    fence_after();
-    const uint32_t tmem = *slot;
     bool failed = false;
 
     if (warp >= 8) {
         give_registers<C::kRegsOther>();
-        if (warp == 8) {
-        // ---- copies: Q's tiles, then K_0, V_0, K_1, V_1, ...
-        const int kv_head = head / a.group;
-        if (blocks > 0) {
-            if (lane == 0) {
-                const int tiles = (2 * rows2 + 1) * kRows < q.n ? 2 : 1;
-                bar_arrive_expect(q_full, tiles * C::kTile);
-                for (int t = 0; t < tiles; ++t)
-                    copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * rows2 + t) * kRows, kRows,
-                                  q_full);
+        if (warp == kCopier) {
+            // ---- copies: Q's tiles, then K_0, V_0, K_1, V_1, ...
+            for (int i = lane; i < C::kBars; i += 32) {
+                const uint32_t b = bar0 + 8 * i;
+                bar_init(b, b >= p_full && b < p_done ? 4 : b == done && kValues != kScores ? 2 : 1);
             }
+            bar_init_fence();
             __syncwarp();
-        }
-        int issued = 0, tails = 0;
-        for (int j = 0; j < blocks && !failed; ++j) {
-            const int live = q.m - j * BN;
-            for (int kind = 0; kind < 2 && !failed; ++kind) {
-                failed = !ring.wait_free(issued) ||
-                         !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN, live,
-                                                 kind == 1, tails);
-                if (!failed) ++issued;
+            setup_arrive<C::kThreads>();
+            const int kv_head = head / a.group;
+            if (blocks > 0) {
+                if (lane == 0) {
+                    const int tiles = (2 * rows2 + 1) * kRows < q.n ? 2 : 1;
+                    bar_arrive_expect(q_full, tiles * C::kTile);
+                    for (int t = 0; t < tiles; ++t)
+                        copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * rows2 + t) * kRows,
+                                      kRows, q_full);
+                }
+                __syncwarp();
             }
-        }
-        if (failed) {
-            ring.drain(issued);
-            bar_wait(q_full, 0, kTries);
-        }
-        } else if (warp == 9) {
-        if (blocks > 0 && elect_one()) {
-            // ---- products
+            int issued = 0, tails = 0;
+            for (int j = 0; j < blocks && !failed; ++j) {
+                const int live = q.m - j * BN;
+                for (int kind = 0; kind < 2 && !failed; ++kind) {
+                    failed = !ring.wait_free(issued) ||
+                             !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN, live,
+                                                     kind == 1, tails);
+                    if (!failed) ++issued;
+                }
+            }
+            if (failed) {
+                ring.drain(issued);
+                bar_wait(q_full, 0, kTries);
+            }
+        } else {
+            if (warp == kScores) tmem_alloc(smem_addr(slot), C::kColumns);
+            fence_before();
+            setup_wait<C::kThreads>();
+            fence_after();
+            const uint32_t tmem = *slot;
             const uint32_t q_addr = smem_addr(smem);
             auto scores = [&](int t, int j) {
                 const uint64_t kd = desc_k_inside(ring.addr(2 * j)), qd = desc_k_inside(q_addr + t * C::kTile);
@@ -302,61 +318,84 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(
                            desc_at(kd, (k / 4) * BN * 128 + (k % 4) * 32), mma_shape(BN, false), k > 0);
                 mma_commit(s_full + 8 * t);
             };
+            // O += P V of tile t, each half of the keys as soon as its P is there
             auto values = [&](int t, int j) {
                 const uint64_t vd = desc_k_rows(ring.addr(2 * j + 1), BN * 128);
 #pragma unroll
-                for (int k = 0; k < BN / 16; ++k)
-                    mma_ts(tmem + C::kColO + t * DP, tmem + C::kColP + t * C::kStepP + 8 * k, desc_at(vd, k * 2048),
-                           mma_shape(DP, true), j > 0 || k > 0);
-            };
-            failed = !bar_wait(q_full, 0, kTries) || !bar_wait(ring.full_bar(0), 0, kTries);
-            if (!failed) {
-                fence_after();
-                for (int t = 0; t < 2; ++t)
-                    if ((t ? nb1 : nb0) > 0) scores(t, 0);
-                mma_commit(ring.empty_bar(0));
-            }
-            for (int j = 0; j < blocks && !failed; ++j) {
-                const int vi = 2 * j + 1, ki = 2 * j + 2;
-                if (j + 1 < blocks) failed = !bar_wait(ring.full_bar(ki), ring.parity(ki), kTries);
-                if (C::kOwnP) {
-                    for (int t = 0; t < 2 && !failed; ++t)
-                        if (j + 1 < (t ? nb1 : nb0)) {
-                            failed = !bar_wait(s_read + 8 * t, j & 1, kTries);
-                            if (failed) break;
-                            fence_after();
-                            scores(t, j + 1);
-                        }
-                    if (failed) break;
-                    if (j + 1 < blocks) mma_commit(ring.empty_bar(ki));
-                }
-                failed = failed || !bar_wait(ring.full_bar(vi), ring.parity(vi), kTries);
-                for (int t = 0; t < 2 && !failed; ++t) {
-                    const int nb = t ? nb1 : nb0;
-                    if (j >= nb) continue;
-                    failed = !bar_wait(p_full + 8 * t, j & 1, kTries);
-                    if (failed) break;
+                for (int h = 0; h < 2; ++h) {
+                    if (!bar_wait(p_full + 16 * t + 8 * h, j & 1, kTries)) return false;
                     fence_after();
-                    values(t, j);
-                    if (C::kOwnP) mma_commit(p_done + 8 * t);
-                    if (j + 1 == nb)
-                        mma_commit(o_full + 8 * t);
-                    else if (!C::kOwnP)
-                        scores(t, j + 1);  // takes P's place: products run in the order of their issue
+#pragma unroll
+                    for (int k = h * BN / 32; k < (h + 1) * BN / 32; ++k)
+                        mma_ts(tmem + C::kColO + t * DP, tmem + C::kColP + t * C::kStepP + 8 * k,
+                               desc_at(vd, k * 2048), mma_shape(DP, true), j > 0 || k > 0);
                 }
-                if (failed) break;
-                mma_commit(ring.empty_bar(vi));
-                if (!C::kOwnP && j + 1 < blocks) mma_commit(ring.empty_bar(ki));
+                return true;
+            };
+            if (blocks > 0 && warp == kScores && elect_one()) {
+                // ---- scores; where P takes S's place, the values' products too
+                failed = !bar_wait(q_full, 0, kTries) || !ring.wait_full(0);
+                if (!failed) {
+                    fence_after();
+                    for (int t = 0; t < 2; ++t)
+                        if ((t ? nb1 : nb0) > 0) scores(t, 0);
+                    mma_commit(ring.empty_bar(0));
+                }
+                for (int j = 0; j < blocks && !failed; ++j) {
+                    const bool more = j + 1 < blocks;
+                    if (more && !ring.wait_full(2 * j + 2)) failed = true;
+                    if (C::kOwnP) {
+                        for (int t = 0; t < 2 && !failed; ++t)
+                            if (j + 1 < (t ? nb1 : nb0)) {
+                                failed = !bar_wait(s_read + 8 * t, j & 1, kTries);
+                                if (failed) break;
+                                fence_after();
+                                scores(t, j + 1);
+                            }
+                    } else {
+                        failed = failed || !ring.wait_full(2 * j + 1);
+                        for (int t = 0; t < 2 && !failed; ++t) {
+                            const int nb = t ? nb1 : nb0;
+                            if (j >= nb) continue;
+                            failed = !values(t, j);
+                            if (failed) break;
+                            if (j + 1 == nb)
+                                mma_commit(o_full + 8 * t);
+                            else
+                                scores(t, j + 1);  // products run in the order of their issue
+                        }
+                        if (!failed) mma_commit(ring.empty_bar(2 * j + 1));
+                    }
+                    if (!failed && more) mma_commit(ring.empty_bar(2 * j + 2));
+                }
+                // every product, and every arrival that it makes, is done
+                // before the block's memory is given back
+                mma_commit(done);
+                failed |= !bar_wait(done, 0, kTries);
+            } else if (blocks > 0 && C::kOwnP && warp == kValues && elect_one()) {
+                // ---- values
+                for (int j = 0; j < blocks && !failed; ++j) {
+                    failed = !ring.wait_full(2 * j + 1);
+                    for (int t = 0; t < 2 && !failed; ++t) {
+                        const int nb = t ? nb1 : nb0;
+                        if (j >= nb) continue;
+                        failed = !values(t, j);
+                        if (failed) break;
+                        mma_commit(j + 1 == nb ? o_full + 8 * t : p_done + 8 * t);
+                    }
+                    if (!failed) mma_commit(ring.empty_bar(2 * j + 1));
+                }
+                mma_commit(done);
+                failed |= !bar_wait(done, 0, kTries);
             }
-            // every product, and every arrival that it makes, is done before
-            // the block's memory is given back
-            mma_commit(done);
-            failed |= !bar_wait(done, 0, kTries);
-        }
-        __syncwarp();
+            __syncwarp();
         }
     } else {
         take_registers<C::kRegsRow>();
+        fence_before();
+        setup_wait<C::kThreads>();
+        fence_after();
+        const uint32_t tmem = *slot;
         // ---- softmax: a row a thread
         const int t = warp / 4, nb = t ? nb1 : nb0;
         const int i = (2 * rows2 + t) * kRows + (threadIdx.x & 127);
@@ -398,19 +437,23 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(
                     m[e] = max3(m[e], __uint_as_float(s[c / 32][c % 32 + 2 * e]),
                                 __uint_as_float(s[c / 32][c % 32 + 2 * e + 1]));
             const float mx = fmaxf(max3(m[0], m[1], m[2]), m[3]) * a.scale2;
-            // this tile's products so far have to be done before P is written
-            // or O is scaled (with P in place of S, this block's S came after them)
-            if (C::kOwnP && j > 0 && !__all_sync(kFull, bar_wait(p_done + 8 * t, (j - 1) & 1, kTries))) {
-                failed = true;
-                break;
-            }
-            fence_after();
+            // this tile's product of the block before has to be done before P
+            // is written or O is scaled (with P in place of S, S came after it)
+            bool waited = !C::kOwnP || j == 0;
             if (j == 0) {
                 top = mx == -INFINITY ? 0.f : mx;
             } else if (__any_sync(kFull, mx > top + 8.f)) {
                 // The running maximum is only followed when it has grown by a
                 // factor of 2^8: until then the sums stay far from overflow,
                 // and O is not touched.
+                if (!waited) {
+                    if (!__all_sync(kFull, bar_wait(p_done + 8 * t, (j - 1) & 1, kTries))) {
+                        failed = true;
+                        break;
+                    }
+                    fence_after();
+                    waited = true;
+                }
                 const float next = mx > top + 8.f ? mx : top, f = exp2_approx(top - next);
                 top = next;
                 const uint64_t f2 = pair(f, f);
@@ -428,22 +471,32 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(
             }
             const uint64_t top2 = pair(-top, -top);
 #pragma unroll
-            for (int c = 0; c < BN; c += 64) {
+            for (int h = 0; h < 2; ++h) {
+                static_assert(BN == 128, "a half of P is one store of 32 columns");
                 uint32_t p[32];
 #pragma unroll
                 for (int e = 0; e < 64; e += 2) {
-                    const int x = c + e;
+                    const int x = 64 * h + e;
                     const float2 y = unpair(fma2(pair_bits(s[x / 32][x % 32], s[x / 32][x % 32 + 1]), scale2, top2));
                     const float p0 = exp2_approx(y.x), p1 = exp2_approx(y.y);
                     sum2[(e / 2) & 1] = add2(sum2[(e / 2) & 1], pair(p0, p1));
                     p[e / 2] = pack_bf16(p0, p1);
                 }
-                tmem_store(p_addr + c / 2, p);
+                if (!waited) {
+                    if (!__all_sync(kFull, bar_wait(p_done + 8 * t, (j - 1) & 1, kTries))) {
+                        failed = true;
+                        break;
+                    }
+                    fence_after();
+                    waited = true;
+                }
+                tmem_store(p_addr + 32 * h, p);
+                store_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full + 16 * t + 8 * h);
             }
-            store_wait();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(p_full + 8 * t);
+            if (failed) break;
         }
         const float2 sums = unpair(add2(sum2[0], sum2[1]));
         const float sum = sums.x + sums.y;
@@ -453,20 +506,21 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(
         }
         if (!failed) {
             const int64_t token = q.q0 + (int64_t)i;
-            bf16 *row = a.out.p + token * a.out.ts + head * a.out.hs;
-            if (nb > 0)
-                write_tmem_row<DP>(o_addr, row, a.D, sum > 0.f || sum != sum ? 1.f / sum : 0.f, live);
-            else if (live)
-                write_zero_row(row, a.D);
+            if (nb > 0) {
+                // Q's tile is read for the last time: its memory takes the rows
+                write_rows<DP>(o_addr, smem + t * C::kTile + (warp & 3) * 32 * DP * 2, a.out, token - lane, head,
+                               q.n - (i - lane), a.D, sum > 0.f || sum != sum ? 1.f / sum : 0.f);
+            } else if (live) {
+                write_zero_row(a.out.p + token * a.out.ts + head * a.out.hs, a.D);
+            }
             if (live)
-                a.lse[(int64_t)head * a.total_q + token] =
-                    lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
+                a.lse[(int64_t)head * a.total_q + token] = lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
     fence_before();
     __syncthreads();
-    if (warp == 9) tmem_free(tmem, C::kColumns);
+    if (warp == kScores) tmem_free(*slot, C::kColumns);
 }
 
 // ---- gradient of the queries ------------------------------------------------------
@@ -675,13 +729,14 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) atte
             __syncwarp();
             if (lane == 0) bar_arrive(p_full + 8 * t);
         }
-        bf16 *row = a.dq.p + token * a.dq.ts + head * a.dq.hs;
         if (nb > 0) {
             if (!failed) failed = !__all_sync(kFull, bar_wait(done, 0, kTries));
             fence_after();
-            if (!failed) write_tmem_row<DP>(tmem + lanes + dq_cols + t * DP, row, a.D, a.scale, live);
+            if (!failed)
+                write_rows<DP>(tmem + lanes + dq_cols + t * DP, smem + 2 * t * C::kTile + (warp & 3) * 32 * DP * 2, a.dq,
+                               token - lane, head, q.n - (i - lane), a.D, a.scale);
         } else if (live) {
-            write_zero_row(row, a.D);
+            write_zero_row(a.dq.p + token * a.dq.ts + head * a.dq.hs, a.D);
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
@@ -866,15 +921,18 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsK == 256 ? 2 : 1) atte
             if (lane == 0) bar_arrive(p_full + 8 * t);
         }
         const int64_t token = q.k0 + (int64_t)j;
-        bf16 *rv = a.dv.p + token * a.dv.ts + head * a.dv.hs, *rk = a.dk.p + token * a.dk.ts + head * a.dk.hs;
         if (blocks > 0) {
             if (!failed) failed = !__all_sync(kFull, bar_wait(done, 0, kTries));
             fence_after();
-            if (!failed && t == 0) write_tmem_row<DP>(tmem + lanes + dv_cols, rv, a.D, 1.f, live);
-            if (!failed && t == NT - 1) write_tmem_row<DP>(tmem + lanes + dk_cols, rk, a.D, a.scale, live);
+            uint8_t *stage = smem + (warp & 3) * 32 * DP * 2;  // K's and V's tiles are read for the last time
+            if (!failed && t == 0)
+                write_rows<DP>(tmem + lanes + dv_cols, stage + C::kTile, a.dv, token - lane, head, q.m - (j - lane), a.D,
+                               1.f);
+            if (!failed && t == NT - 1)
+                write_rows<DP>(tmem + lanes + dk_cols, stage, a.dk, token - lane, head, q.m - (j - lane), a.D, a.scale);
         } else if (live && t == 0) {
-            write_zero_row(rv, a.D);
-            write_zero_row(rk, a.D);
+            write_zero_row(a.dv.p + token * a.dv.ts + head * a.dv.hs, a.D);
+            write_zero_row(a.dk.p + token * a.dk.ts + head * a.dk.hs, a.D);
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);

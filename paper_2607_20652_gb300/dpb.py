@@ -8,7 +8,6 @@ library has not been built: there is no CPU fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -63,10 +62,6 @@ class Config(ctypes.Structure):
                 "k_per_level": list(self.k_per_level[:L]), "select_mode": self.select_mode,
                 "norm_match": self.norm_match, "dtype": self.dtype, "field_t": self.field_t,
                 "field_poly": self.field_poly, "generator_seed": self.generator_seed, "scoring": self.scoring}
-
-
-class Heads(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class RopeConfig(ctypes.Structure):
@@ -130,7 +125,8 @@ def load(path: Optional[str] = None):
     lib.dpb_stats_accumulate.argtypes = [vp, vp, i64, vp, vp, vp, ctypes.c_int32, vp, vp, sz, vp]
     lib.dpb_stats_update.argtypes = [vp, vp, ctypes.c_float, vp, vp, vp]
     lib.dpb_forward.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    hp, rc, ac = ctypes.POINTER(Heads), ctypes.POINTER(RopeConfig), ctypes.POINTER(AttentionConfig)
+    # dpb_heads arguments are addresses within one array (_rows_array)
+    hp, rc, ac = vp, ctypes.POINTER(RopeConfig), ctypes.POINTER(AttentionConfig)
     lib.dpb_qk_norm_rope.argtypes = [rc, hp, hp, vp, vp, vp, vp, vp, hp, hp, vp, sz, vp]
     lib.dpb_qk_norm_rope_backward.argtypes = [rc, hp, hp, hp, hp, vp, vp, vp, vp, vp, hp, hp, vp, vp, vp, sz, vp]
     lib.dpb_rope_workspace_size.argtypes = [rc, ctypes.POINTER(sz)]
@@ -449,36 +445,39 @@ def workspace_status(workspace: torch.Tensor, clear: bool = False, stream=None) 
 _shared_ws: dict = {}
 
 
-def _enter(device, stream):
-    """(torch stream, context) of a call: a stream given that is not the
-    current one is entered, so that outputs and workspaces are allocated on it."""
+def _elsewhere(call, stream, device, args, kw):
+    """Makes `call` on another stream or device than the current ones: outputs
+    and workspaces are then allocated there, and the allocator is told that
+    the tensors given are read there."""
     if device.type != "cuda":
         raise ValueError("tensors must be on a CUDA device")
-    cur = torch.cuda.current_stream(device)
-    if torch.cuda.current_device() == device.index and (stream is None or stream == cur):
-        return cur, contextlib.nullcontext()
-    s = cur if stream is None else stream
-    return s, torch.cuda.stream(s)
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    with torch.cuda.stream(s):
+        out = call(*args, **kw)
+    if stream is not None:
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(s)
+    return out
 
 
-def _lend(stream, current, *tensors):
-    """Tells the allocator of tensors that another stream than the current one reads."""
-    if stream is not None and stream != current:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+def _away(device, stream) -> bool:
+    return stream is not None or device.index != torch.cuda.current_device()
 
 
-def _shared_workspace(nbytes: int, device, stream) -> torch.Tensor:
+def _raw_stream(device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _shared_workspace(nbytes: int, device, stream: int) -> torch.Tensor:
     """The workspace of the calls below made without one: one per (device,
     stream), grown as needed; its status bits accumulate until read (status())."""
-    key = (device.index, stream.cuda_stream)
-    ws = _shared_ws.get(key)
+    ws = _shared_ws.get((device.index, stream))
     if ws is None or ws.numel() < nbytes:
         new = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         if ws is not None:
             new[:256].copy_(ws[:256])
-        ws = _shared_ws[key] = new
+        ws = _shared_ws[(device.index, stream)] = new
     return ws
 
 
@@ -491,19 +490,27 @@ def status(device=None, stream=None, clear: bool = True) -> int:
     return 0 if ws is None else workspace_status(ws, clear=clear, stream=s)
 
 
-def _heads(t: torch.Tensor, name: str, dtype, shape) -> Heads:
-    """A [tokens, heads, dim] tensor whose last dimension is dense, as the library takes it."""
-    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a CUDA {dtype} tensor of shape {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+def _head_rows(t: torch.Tensor, name: str, dtype, shape, device):
+    """(address, token stride, head stride) of a [tokens, heads, dim] tensor whose last dimension is dense."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {list(shape)} on {device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+    if st[2] != 1 and shape[2] > 1:
         raise ValueError(f"the last dimension of {name} must be dense")
-    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+    return t.data_ptr(), st[0], st[1]
+
+
+_rows_array = ctypes.c_int64 * 24  # up to 8 dpb_heads side by side, 24 bytes each
 
 
 def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, device):
-    if t is not None and (t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() != numel):
+    """Address of a contiguous tensor of `numel` values (None: None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != device or not t.is_contiguous() or t.numel() != numel:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} values on {device}")
-    return _ptr(t)
+    return t.data_ptr()
 
 
 def rope_tables(positions: int, rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None,
@@ -542,11 +549,15 @@ def rope_tables(positions: int, rot_dim: int, base: float = 10000.0, scaling: Op
 
 
 def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise):
+    """(config, addresses of the weights, tables and positions)"""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [tokens, heads, dim]")
     T, hq, D = q.shape
-    if k.dim() != 3 or k.shape[0] != T or k.shape[2] != D or k.dtype != q.dtype:
-        raise ValueError("q and k must be [tokens, heads, dim] with the same tokens, dim and dtype")
-    if q.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"q and k must be float32 or bfloat16, got {q.dtype}")
+    dt, dev = q.dtype, q.device
+    if k.shape[0] != T or k.shape[2] != D or k.dtype is not dt:
+        raise ValueError("q and k must have the same tokens, dim and dtype")
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise ValueError(f"q and k must be float32 or bfloat16, got {dt}")
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin must both be given or both be None")
     rot, rows = 0, 0
@@ -554,13 +565,11 @@ def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved
         if cos.dim() != 2 or cos.shape != sin.shape:
             raise ValueError("cos and sin must be [positions, rot_dim / 2] of the same shape")
         rows, rot = cos.shape[0], 2 * cos.shape[1]
-        _dense(cos, "cos", torch.float32, cos.numel(), q.device)
-        _dense(sin, "sin", torch.float32, cos.numel(), q.device)
-    _dense(weight_q, "weight_q", q.dtype, D, q.device)
-    _dense(weight_k, "weight_k", q.dtype, D, q.device)
-    _dense(positions, "positions", torch.int32, T, q.device)
-    return RopeConfig(T, hq, k.shape[1], D, rot, int(interleaved), int(normalise), rows,
-                      F32 if q.dtype == torch.float32 else BF16, eps, 0)
+    at = (_dense(weight_q, "weight_q", dt, D, dev), _dense(weight_k, "weight_k", dt, D, dev),
+          _dense(cos, "cos", torch.float32, rows * rot // 2, dev), _dense(sin, "sin", torch.float32, rows * rot // 2, dev),
+          _dense(positions, "positions", torch.int32, T, dev))
+    return RopeConfig(T, hq, k.shape[1], D, rot, bool(interleaved), bool(normalise), rows,
+                      BF16 if dt is torch.bfloat16 else F32, eps, 0), at
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, weight_q=None, weight_k=None, cos=None, sin=None, positions=None,
@@ -570,19 +579,19 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, weight_q=None, weight_k=None,
     packed projection are fine); cos, sin from rope_tables() (None: no
     rotation); positions int32 [T] (None: 0, 1, ...). Returns (q, k) normalised
     and rotated."""
-    c = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
-    lib = load()
-    s, ctx = _enter(q.device, stream)
-    with ctx:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-        ws = _shared_workspace(256, q.device, s) if workspace is None else workspace
-        hs = [_heads(t, n, q.dtype, like.shape) for t, n, like in
-              ((q, "q", q), (k, "k", k), (q_out, "q_out", q), (k_out, "k_out", k))]
-        _check(lib.dpb_qk_norm_rope(c, hs[0], hs[1], _ptr(weight_q), _ptr(weight_k), _ptr(cos), _ptr(sin),
-                                    _ptr(positions), hs[2], hs[3], _ptr(ws), ws.numel() * ws.element_size(),
-                                    s.cuda_stream))
-    _lend(stream, torch.cuda.current_stream(q.device), q, k, weight_q, weight_k, cos, sin, positions)
+    dev = q.device
+    if _away(dev, stream):
+        return _elsewhere(qk_norm_rope, stream, dev, (q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved,
+                                                      normalise, q_out, k_out, workspace), {})
+    c, at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
+    dt, sq, sk, s = q.dtype, q.shape, k.shape, _raw_stream(dev)
+    q_out = torch.empty(sq, dtype=dt, device=dev) if q_out is None else q_out
+    k_out = torch.empty(sk, dtype=dt, device=dev) if k_out is None else k_out
+    ws = _shared_workspace(256, dev, s) if workspace is None else workspace
+    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+                       *_head_rows(q_out, "q_out", dt, sq, dev), *_head_rows(k_out, "k_out", dt, sk, dev))
+    h = ctypes.addressof(rows)
+    _check(load().dpb_qk_norm_rope(c, h, h + 24, *at, h + 48, h + 72, ws.data_ptr(), ws.nbytes, s))
     return q_out, k_out
 
 
@@ -593,36 +602,40 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Te
     """dpb_qk_norm_rope_backward. Returns (grad_q, grad_k, grad_weight_q,
     grad_weight_k): the last two fp32 [D], or None without ``normalise`` or
     ``weight_grads``."""
-    c = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
-    lib = load()
-    D = q.shape[2]
-    s, ctx = _enter(q.device, stream)
-    with ctx:
-        grad_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if grad_q is None else grad_q
-        grad_k = torch.empty(k.shape, dtype=k.dtype, device=k.device) if grad_k is None else grad_k
-        gw = torch.empty((2, D), dtype=torch.float32, device=q.device) if normalise and weight_grads else None
-        if workspace is None:
-            n = ctypes.c_size_t()
-            _check(lib.dpb_rope_workspace_size(c, n))
-            workspace = _shared_workspace(n.value, q.device, s)
-        hs = [_heads(t, n, q.dtype, like.shape) for t, n, like in
-              ((q, "q", q), (k, "k", k), (grad_q_out, "grad_q_out", q), (grad_k_out, "grad_k_out", k),
-               (grad_q, "grad_q", q), (grad_k, "grad_k", k))]
-        _check(lib.dpb_qk_norm_rope_backward(
-            c, hs[0], hs[1], hs[2], hs[3], _ptr(weight_q), _ptr(weight_k), _ptr(cos), _ptr(sin), _ptr(positions), hs[4],
-            hs[5], None if gw is None else gw.data_ptr(), None if gw is None else gw.data_ptr() + 4 * D,
-            _ptr(workspace), workspace.numel() * workspace.element_size(), s.cuda_stream))
-    _lend(stream, torch.cuda.current_stream(q.device), q, k, grad_q_out, grad_k_out, weight_q, weight_k, cos, sin,
-          positions)
+    dev = q.device
+    if _away(dev, stream):
+        return _elsewhere(qk_norm_rope_backward, stream, dev,
+                          (q, k, grad_q_out, grad_k_out, weight_q, weight_k, cos, sin, positions, eps, interleaved,
+                           normalise, weight_grads, grad_q, grad_k, workspace), {})
+    c, at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
+    lib, dt, sq, sk, s = load(), q.dtype, q.shape, k.shape, _raw_stream(dev)
+    grad_q = torch.empty(sq, dtype=dt, device=dev) if grad_q is None else grad_q
+    grad_k = torch.empty(sk, dtype=dt, device=dev) if grad_k is None else grad_k
+    D = sq[2]
+    gw = torch.empty((2, D), dtype=torch.float32, device=dev) if normalise and weight_grads else None
+    gp = None if gw is None else gw.data_ptr()
+    if workspace is None:
+        n = ctypes.c_size_t()
+        _check(lib.dpb_rope_workspace_size(c, n))
+        workspace = _shared_workspace(n.value, dev, s)
+    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+                       *_head_rows(grad_q_out, "grad_q_out", dt, sq, dev),
+                       *_head_rows(grad_k_out, "grad_k_out", dt, sk, dev),
+                       *_head_rows(grad_q, "grad_q", dt, sq, dev), *_head_rows(grad_k, "grad_k", dt, sk, dev))
+    h = ctypes.addressof(rows)
+    _check(lib.dpb_qk_norm_rope_backward(c, h, h + 24, h + 48, h + 72, *at, h + 96, h + 120, gp,
+                                         None if gp is None else gp + 4 * D, workspace.data_ptr(), workspace.nbytes, s))
     return (grad_q, grad_k) + ((None, None) if gw is None else (gw[0], gw[1]))
 
 
 def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        if t.dim() != 3 or t.dtype != torch.bfloat16:
-            raise ValueError(f"{n} must be a bfloat16 tensor [tokens, heads, dim], got {t.dtype} {list(t.shape)}")
+    """(config, addresses of the offsets)"""
+    if q.dim() != 3 or k.dim() != 3 or q.dtype is not torch.bfloat16:
+        raise ValueError(f"q, k and v must be bfloat16 tensors [tokens, heads, dim], got {q.dtype} {list(q.shape)}")
+    Tq, Hq, D = q.shape
+    Tk, Hk, _ = k.shape
     if cu_k is None and cu_q is not None:
-        if q.shape[0] != k.shape[0]:
+        if Tq != Tk:
             raise ValueError("cu_k is needed: q and k have different token counts")
         cu_k, max_k = cu_q, max_q
     if (cu_q is None) != (cu_k is None):
@@ -630,15 +643,12 @@ def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
     seqs = 1
     if cu_q is not None:
         seqs = cu_q.numel() - 1
-        if seqs < 0 or cu_q.dim() != 1:
-            raise ValueError("cu_q must be 1-D with one entry more than there are sequences")
-        _dense(cu_q, "cu_q", torch.int32, seqs + 1, q.device)
-        _dense(cu_k, "cu_k", torch.int32, seqs + 1, q.device)
-    max_q = q.shape[0] if max_q is None else min(int(max_q), q.shape[0])
-    max_k = k.shape[0] if max_k is None else min(int(max_k), k.shape[0])
-    c = AttentionConfig(q.shape[0], k.shape[0], seqs, max_q, max_k, q.shape[1], k.shape[1], q.shape[2], int(causal),
-                        BF16, q.shape[2] ** -0.5 if scale is None else float(scale), 0)
-    return c, cu_q, cu_k
+        if seqs < 0:
+            raise ValueError("cu_q must have one entry more than there are sequences")
+    at = (_dense(cu_q, "cu_q", torch.int32, seqs + 1, q.device), _dense(cu_k, "cu_k", torch.int32, seqs + 1, q.device))
+    return AttentionConfig(Tq, Tk, seqs, Tq if max_q is None or max_q > Tq else max_q,
+                           Tk if max_k is None or max_k > Tk else max_k, Hq, Hk, D, bool(causal), BF16,
+                           D ** -0.5 if scale is None else scale, 0), at
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, cu_k=None,
@@ -649,21 +659,23 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=No
     offsets (None: one sequence; cu_k None: as cu_q), max_q, max_k the longest
     sequences' lengths (None: the token count, which only costs empty blocks);
     scale defaults to D^-1/2. Returns (o [Tq, Hq, D], lse fp32 [Hq, Tq])."""
-    c, cu_q, cu_k = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
-    lib = load()
-    Tq, Hq, D = q.shape
-    s, ctx = _enter(q.device, stream)
-    with ctx:
-        out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device) if out is None else out
-        lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device) if lse is None else lse
-        ws = _shared_workspace(256, q.device, s) if workspace is None else workspace
-        kv = (k.shape[0], k.shape[1], D)
-        hs = [_heads(t, n, q.dtype, shape) for t, n, shape in
-              ((q, "q", q.shape), (k, "k", kv), (v, "v", kv), (out, "out", q.shape))]
-        _check(lib.dpb_attention_forward(c, hs[0], hs[1], hs[2], _ptr(cu_q), _ptr(cu_k), hs[3],
-                                         _dense(lse, "lse", torch.float32, Hq * Tq, q.device), _ptr(ws),
-                                         ws.numel() * ws.element_size(), s.cuda_stream))
-    _lend(stream, torch.cuda.current_stream(q.device), q, k, v, cu_q, cu_k)
+    dev = q.device
+    if _away(dev, stream):
+        return _elsewhere(attention_forward, stream, dev,
+                          (q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, out, lse, workspace), {})
+    c, at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
+    dt, sq, s = torch.bfloat16, q.shape, _raw_stream(dev)
+    sk = torch.Size((k.shape[0], k.shape[1], sq[2]))
+    if out is None:
+        out = torch.empty(sq, dtype=dt, device=dev)
+    if lse is None:
+        lse = torch.empty((sq[1], sq[0]), dtype=torch.float32, device=dev)
+    ws = _shared_workspace(256, dev, s) if workspace is None else workspace
+    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+                       *_head_rows(v, "v", dt, sk, dev), *_head_rows(out, "out", dt, sq, dev))
+    h = ctypes.addressof(rows)
+    _check(load().dpb_attention_forward(c, h, h + 24, h + 48, *at, h + 72,
+                                        _dense(lse, "lse", torch.float32, sq[0] * sq[1], dev), ws.data_ptr(), ws.nbytes, s))
     return out, lse
 
 
@@ -673,25 +685,29 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
                        grad_k=None, grad_v=None, workspace=None, stream=None):
     """dpb_attention_backward with the forward's inputs, its o and lse, and the
     gradient of o. Returns (grad_q, grad_k, grad_v)."""
-    c, cu_q, cu_k = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
-    lib = load()
-    s, ctx = _enter(q.device, stream)
-    with ctx:
-        grad_q, grad_k, grad_v = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g
-                                  for g, x in ((grad_q, q), (grad_k, k), (grad_v, v)))
-        if workspace is None:
-            n = ctypes.c_size_t()
-            _check(lib.dpb_attention_workspace_size(c, n))
-            workspace = _shared_workspace(n.value, q.device, s)
-        kv = (k.shape[0], k.shape[1], q.shape[2])
-        hs = [_heads(t, n, q.dtype, shape) for t, n, shape in
-              ((q, "q", q.shape), (k, "k", kv), (v, "v", kv), (o, "o", q.shape), (grad_o, "grad_o", q.shape),
-               (grad_q, "grad_q", q.shape), (grad_k, "grad_k", kv), (grad_v, "grad_v", kv))]
-        _check(lib.dpb_attention_backward(
-            c, hs[0], hs[1], hs[2], hs[3], _dense(lse, "lse", torch.float32, q.shape[0] * q.shape[1], q.device), hs[4],
-            _ptr(cu_q), _ptr(cu_k), hs[5], hs[6], hs[7], _ptr(workspace),
-            workspace.numel() * workspace.element_size(), s.cuda_stream))
-    _lend(stream, torch.cuda.current_stream(q.device), q, k, v, o, lse, grad_o, cu_q, cu_k)
+    dev = q.device
+    if _away(dev, stream):
+        return _elsewhere(attention_backward, stream, dev,
+                          (q, k, v, o, lse, grad_o, cu_q, cu_k, max_q, max_k, causal, scale, grad_q, grad_k, grad_v,
+                           workspace), {})
+    c, at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
+    lib, dt, sq, s = load(), torch.bfloat16, q.shape, _raw_stream(dev)
+    sk = torch.Size((k.shape[0], k.shape[1], sq[2]))
+    grad_q = torch.empty(sq, dtype=dt, device=dev) if grad_q is None else grad_q
+    grad_k = torch.empty(sk, dtype=dt, device=dev) if grad_k is None else grad_k
+    grad_v = torch.empty(sk, dtype=dt, device=dev) if grad_v is None else grad_v
+    if workspace is None:
+        n = ctypes.c_size_t()
+        _check(lib.dpb_attention_workspace_size(c, n))
+        workspace = _shared_workspace(n.value, dev, s)
+    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+                       *_head_rows(v, "v", dt, sk, dev), *_head_rows(o, "o", dt, sq, dev),
+                       *_head_rows(grad_o, "grad_o", dt, sq, dev), *_head_rows(grad_q, "grad_q", dt, sq, dev),
+                       *_head_rows(grad_k, "grad_k", dt, sk, dev), *_head_rows(grad_v, "grad_v", dt, sk, dev))
+    h = ctypes.addressof(rows)
+    _check(lib.dpb_attention_backward(c, h, h + 24, h + 48, h + 72,
+                                      _dense(lse, "lse", torch.float32, sq[0] * sq[1], dev), h + 96, *at, h + 120, h + 144,
+                                      h + 168, workspace.data_ptr(), workspace.nbytes, s))
     return grad_q, grad_k, grad_v
 
 
@@ -699,8 +715,9 @@ class AdamWGroup:
     """What dpb_adamw_step takes of a list of parameters and their states: the
     states are one flat tensor each of the parameter's size, float32, or
     float8_e4m3fn codes with a float32 scale for each STATE_BLOCK values
-    (ceil(n / STATE_BLOCK) of them). Tensors are held, addresses are read anew
-    at every step."""
+    (ceil(n / STATE_BLOCK) of them). The tensors are held; a parameter's
+    ``data`` may be rebound (its address is read at every step), the states'
+    may not."""
 
     def __init__(self, params, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_scale=None):
         import numpy as np
@@ -732,31 +749,50 @@ class AdamWGroup:
                 _dense(ts[i], f"{name}[{i}]", torch.float32 if scale else sd, n, self.device)
         self._numel = [p.numel() for p in self.params]
         self._table = np.zeros((len(self.params), 7), dtype=np.int64)  # rows of dpb_adamw_tensor
+        for col, ts in enumerate((self.params, None, self.exp_avg, self.exp_avg_sq, *self.scales)):
+            if ts is not None:
+                self._table[:, col] = [x.data_ptr() for x in ts]
+        self._table[:, 6] = self._numel
+        self._table_at, self._last = self._table.ctypes.data, (self._table[:, 0].tolist(), None)
 
     def step(self, grads, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, step: int = 1,
              seed: int = 0, grad_scale: Optional[torch.Tensor] = None, stream=None):
         """dpb_adamw_step: one step of every parameter that has a gradient (None
         leaves it as it is). ``grad_scale``: a float32 tensor of one value that
         multiplies the gradients; where it is not finite nothing changes."""
+        dt, dev = self.dtype, self.device
+        if _away(dev, stream):
+            _elsewhere(self.step, stream, dev, (grads, lr, betas, eps, weight_decay, step, seed, grad_scale), {})
+            if stream is not None:
+                for ts in (grads, self.params, self.exp_avg, self.exp_avg_sq, *(x or () for x in self.scales)):
+                    for x in ts:
+                        if x is not None:
+                            x.record_stream(stream)
+            return
         t = self._table
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        dt, dev = self.dtype, self.device
-        for i, (g, n) in enumerate(zip(grads, self._numel)):
-            if g is not None and (g.dtype != dt or g.device != dev or g.numel() != n or not g.is_contiguous()):
-                raise ValueError(f"gradient {i} must be a contiguous {dt} tensor of {n} values on {dev}")
-        gs = _dense(grad_scale, "grad_scale", torch.float32, 1, dev)
-        for col, ts in ((0, self.params), (2, self.exp_avg), (3, self.exp_avg_sq), (4, self.scales[0]),
-                        (5, self.scales[1])):
-            if ts is not None:
-                t[:, col] = [x.data_ptr() for x in ts]
-        t[:, 1] = [0 if g is None else g.data_ptr() for g in grads]
-        t[:, 6] = [0 if g is None else n for g, n in zip(grads, self._numel)]
-        c = AdamWConfig(lr, betas[0], betas[1], eps, weight_decay, step, seed & (2**64 - 1), gs,
-                        F32 if dt == torch.float32 else BF16, self.state_bits)
-        s, ctx = _enter(dev, stream)
-        with ctx:
-            _check(load().dpb_adamw_step(c, t.ctypes.data, len(self.params), s.cuda_stream))
-        if stream is not None:
-            _lend(stream, torch.cuda.current_stream(dev), grad_scale, *grads, *self.params, *self.exp_avg,
-                  *self.exp_avg_sq, *(self.scales[0] or ()), *(self.scales[1] or ()))
+        at, left = [], False
+        for g, n in zip(grads, self._numel):
+            if g is None:
+                left = True
+                at.append(0)
+            elif g.dtype is not dt or g.numel() != n or not g.is_contiguous() or g.device != dev:
+                raise ValueError(f"gradient {len(at)} must be a contiguous {dt} tensor of {n} values on {dev}")
+            else:
+                at.append(g.data_ptr())
+        ps = [p.data_ptr() for p in self.params]
+        if ps != self._last[0]:
+            for i in (t[:, 0] != ps).nonzero()[0]:  # rebound since the last step
+                p = self.params[i]
+                if p.dtype is not dt or p.numel() != self._numel[i] or not p.is_contiguous() or p.device != dev:
+                    raise ValueError(f"parameter {i} must be a contiguous {dt} tensor of {self._numel[i]} values on {dev}")
+            t[:, 0] = ps
+        if at != self._last[1]:
+            t[:, 1] = at
+            t[:, 6] = [n if g else 0 for g, n in zip(at, self._numel)] if left else self._numel
+        self._last = (ps, at)
+        c = AdamWConfig(lr, betas[0], betas[1], eps, weight_decay, step, seed & (2**64 - 1),
+                        _dense(grad_scale, "grad_scale", torch.float32, 1, dev), F32 if dt is torch.float32 else BF16,
+                        self.state_bits)
+        _check(load().dpb_adamw_step(c, self._table_at, len(ps), _raw_stream(dev)))

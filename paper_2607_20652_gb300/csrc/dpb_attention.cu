@@ -158,18 +158,18 @@ __device__ __forceinline__ void write_zero_row(bf16 *row, int D) {
     for (int i = 0; i < D; i += 8) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Writes this warp's 32 rows of a result from TMEM (DP fp32 a lane, times f)
-// as bf16: through `stage` (32 rows of DP bf16 in shared memory, 16-byte
-// pieces exchanged within 8 so that neither side meets bank conflicts), so
-// that the warp's stores to memory cover whole rows. Rows from `rows` on are
-// left out.
-template <int DP>
+// Writes this warp's 32 rows of COLS columns of a result from TMEM (fp32,
+// times f) as bf16 to columns [col, min(col + COLS, D)): through `stage` (32
+// rows of COLS bf16 in shared memory, their 16-byte pieces exchanged so that
+// neither side meets bank conflicts), so that the warp's stores to memory cover
+// whole rows. Rows from `rows` on are left out.
+template <int COLS>
 __device__ __forceinline__ void write_rows(uint32_t tmem, uint8_t *stage, const Out &out, int64_t token, int head,
-                                           int rows, int D, float f) {
+                                           int rows, int col, int D, float f) {
     const int lane = threadIdx.x & 31;
-    constexpr int kPieces = DP / 8;
+    constexpr int kPieces = COLS / 8, kSwap = kPieces < 8 ? kPieces - 1 : 7;
 #pragma unroll
-    for (int c = 0; c < DP; c += 32) {
+    for (int c = 0; c < COLS; c += 32) {
         uint32_t v[32];
         tmem_load(tmem + c, v);
         load_wait(v);
@@ -179,18 +179,18 @@ __device__ __forceinline__ void write_rows(uint32_t tmem, uint8_t *stage, const 
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 u[e] = pack_bf16(__uint_as_float(v[8 * i + 2 * e]) * f, __uint_as_float(v[8 * i + 2 * e + 1]) * f);
-            *reinterpret_cast<uint4 *>(stage + lane * DP * 2 + (((c / 8 + i) ^ (lane & 7)) * 16)) =
+            *reinterpret_cast<uint4 *>(stage + lane * COLS * 2 + (((c / 8 + i) ^ (lane & kSwap)) * 16)) =
                 make_uint4(u[0], u[1], u[2], u[3]);
         }
     }
     __syncwarp();
-    bf16 *base = out.p + token * out.ts + head * out.hs;
+    bf16 *base = out.p + token * out.ts + head * out.hs + col;
 #pragma unroll 4
     for (int i = lane; i < 32 * kPieces; i += 32) {
         const int r = i / kPieces, piece = i % kPieces;
-        if (r < rows && piece * 8 < D)
+        if (r < rows && col + piece * 8 < D)
             *reinterpret_cast<uint4 *>(base + r * out.ts + piece * 8) =
-                *reinterpret_cast<const uint4 *>(stage + r * DP * 2 + ((piece ^ (r & 7)) * 16));
+                *reinterpret_cast<const uint4 *>(stage + r * COLS * 2 + ((piece ^ (r & kSwap)) * 16));
     }
 }
 
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
             if (nb > 0) {
                 // Q's tile is read for the last time: its memory takes the rows
                 write_rows<DP>(o_addr, smem + t * C::kTile + (warp & 3) * 32 * DP * 2, a.out, token - lane, head,
-                               q.n - (i - lane), a.D, sum > 0.f || sum != sum ? 1.f / sum : 0.f);
+                               q.n - (i - lane), 0, a.D, sum > 0.f || sum != sum ? 1.f / sum : 0.f);
             } else if (live) {
                 write_zero_row(a.out.p + token * a.out.ts + head * a.out.hs, a.D);
             }
@@ -523,102 +523,107 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
     if (warp == kScores) tmem_free(*slot, C::kColumns);
 }
 
-// ---- gradient of the queries ------------------------------------------------------
+// ---- gradients ------------------------------------------------------------------
 
-constexpr int kGradCols = 64;  // keys (or queries) of a streamed block in the gradients
-
-template <int DP_, int NT_, int NS_>
+// One tile of 128 rows against blocks of 128: S and the gradient of P take 256
+// TMEM columns, the sums the rest. Two warpgroups share a tile, 64 columns
+// each, so that a block's arithmetic takes half as long between its products.
+template <int DP_>
 struct GradShape {
-    static constexpr int DP = DP_, NT = NT_, NS = NS_;
-    static constexpr int kTile = kRows * DP * 2, kSlot = kGradCols * DP * 2;
-    static constexpr int kThreads = NT * 128 + 64;
-    static constexpr int kBars = 1 + 2 * NS + 1 + 2 * NT + 1;
-    static constexpr int kVec = NT * 4 * 2 * kGradCols * 4;  // a warp's lse and delta of a block of queries
-    // query gradient: S and dP (then dS) of each tile, dQ; key gradient: S^T
-    // (then P^T) and dP^T (then dS^T) of each buffer, dV and dK
-    static constexpr int kColumnsQ = NT * (128 + DP) <= 256 ? 256 : 512;
-    static constexpr int kColumnsK = NT * 128 + 2 * DP <= 256 ? 256 : 512;
-    static constexpr int kSmemQ = 1024 + 2 * NT * kTile + NS * kSlot + 8 * kBars + 16;
-    static constexpr int kSmemK = 1024 + 2 * kTile + NS * kSlot + kVec + 8 * kBars + 16;
+    static constexpr int DP = DP_, BN = 128, NS = DP == 64 ? 6 : 4;
+    static constexpr int kTile = kRows * DP * 2;
+    static constexpr int kThreads = 320, kCopier = 8, kIssuer = 9;
+    static constexpr int kColS = 0, kColG = 128, kColSum = 256;  // S, the gradient of P, the sums
+    static constexpr int kColumns = 512;
+    static constexpr int kBars = 1 + 2 * NS + 1 + 8;
+    static constexpr int kVec = 8 * 128 * 4;  // a warp's lse and delta of its 64 columns
+    static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + 8 * kBars + 16;
+    using Slots = Ring<NS, kTile>;
 };
 
-// scores and grad_o V^T of a tile against one streamed block, into TMEM
-// columns [d, d + 64) and [d + 64, d + 128).
+// d = a b^T of two tiles in shared memory (K = DP).
 template <int DP>
-__device__ __forceinline__ void two_products(uint32_t d, uint32_t a0, uint32_t b0, uint32_t a1, uint32_t b1) {
-    const uint64_t da0 = desc_k_inside(a0), db0 = desc_k_inside(b0), da1 = desc_k_inside(a1), db1 = desc_k_inside(b1);
+__device__ __forceinline__ void tile_product(uint32_t d, uint32_t a, uint32_t b) {
+    const uint64_t da = desc_k_inside(a), db = desc_k_inside(b);
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k)
-        mma_ss(d, desc_at(da0, (k / 4) * kRows * 128 + (k % 4) * 32),
-               desc_at(db0, (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k)
-        mma_ss(d + kGradCols, desc_at(da1, (k / 4) * kRows * 128 + (k % 4) * 32),
-               desc_at(db1, (k / 4) * kGradCols * 128 + (k % 4) * 32), mma_shape(kGradCols, false), k > 0);
+        mma_ss(d, desc_at(da, (k / 4) * kRows * 128 + (k % 4) * 32), desc_at(db, (k / 4) * kRows * 128 + (k % 4) * 32),
+               mma_shape(128, false), k > 0);
 }
 
-// d += a (TMEM, 64 columns of bf16) x a streamed block of 64 rows.
+// d += a (TMEM: 128 columns of bf16, the second half of them `half` columns
+// from the first) x a tile in shared memory (K = its 128 rows).
 template <int DP>
-__device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t b, bool add) {
-    const uint64_t db = desc_k_rows(b, kGradCols * 128);
+__device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t half, uint32_t b, bool add) {
+    const uint64_t db = desc_k_rows(b, kRows * 128);
 #pragma unroll
-    for (int k = 0; k < kGradCols / 16; ++k)
-        mma_ts(d, a + 8 * k, desc_at(db, k * 2048), mma_shape(DP, true), add || k > 0);
+    for (int k = 0; k < 8; ++k)
+        mma_ts(d, a + (k / 4) * half + (k % 4) * 8, desc_at(db, k * 2048), mma_shape(DP, true), add || k > 0);
 }
+
+// What both gradient kernels set up: barriers (by the copying warp), TMEM.
+template <class C>
+struct GradBars {
+    // the tile is there; S and the gradient of P are there, have been read; dS
+    // (and P, for the keys' gradient) is there; dS's product is done; all is done
+    uint32_t tile_full, s_full, g_full, w_done, done, s_read, g_read, w_full, v_full;
+    typename C::Slots ring;
+    uint32_t *slot;
+    __device__ __forceinline__ GradBars(uint8_t *smem) {
+        uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (2 + C::NS) * C::kTile + C::kVec);
+        tile_full = smem_addr(bars);
+        ring = {smem + 2 * C::kTile, tile_full + 8, tile_full + 8 + 8 * C::NS, tile_full + 8 + 16 * C::NS};
+        s_full = tile_full + 8 * (2 + 2 * C::NS);
+        g_full = s_full + 8;
+        w_done = s_full + 16;
+        done = s_full + 24;
+        s_read = s_full + 32;  // from here on arrived on by the 8 row warps
+        g_read = s_full + 40;
+        w_full = s_full + 48;
+        v_full = s_full + 56;
+        slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
+    }
+    __device__ __forceinline__ void make() const {
+        for (int i = threadIdx.x & 31; i < C::kBars; i += 32) {
+            const uint32_t b = tile_full + 8 * i;
+            bar_init(b, b >= s_read ? 8 : 1);
+        }
+        bar_init_fence();
+        __syncwarp();
+    }
+};
+
+// ---- gradient of the queries
 
 template <class C>
-__global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) attention_grad_q_kernel(
-    const __grid_constant__ AttnArgs a) {
-    constexpr int DP = C::DP, NT = C::NT, BN = kGradCols;
+__global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const __grid_constant__ AttnArgs a) {
+    constexpr int DP = C::DP, BN = C::BN;
+    constexpr int kColW = C::kColSum + DP;  // dS in bf16, in columns of its own
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
-    const int si = rest % a.seqs, first = (a.tiles - 1 - rest / a.seqs) * NT;
+    const int si = rest % a.seqs, tile = a.tiles - 1 - rest / a.seqs;  // the longest rows first
     const Seq q = sequence(a, si);
     if (!q.ok) {
         if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
         return;
     }
-    if (first * kRows >= q.n) return;
-    const int nb0 = tile_blocks<BN>(a, q, first), nb1 = NT == 2 ? tile_blocks<BN>(a, q, first + 1) : 0;
-    const int blocks = max(nb0, nb1);
-
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * NT * C::kTile + C::NS * C::kSlot);
-    const uint32_t bar0 = smem_addr(bars), q_full = bar0;
-    Ring<C::NS, C::kSlot> ring{smem + 2 * NT * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
-    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 8 * NT, done = p_full + 8 * NT;
-    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
-    constexpr int kCopier = 4 * NT, kIssuer = 4 * NT + 1;
-    if (threadIdx.x == 0) {
-        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < done ? 4 : 1);
-        bar_init_fence();
-    }
-    if (warp == kIssuer) tmem_alloc(smem_addr(slot), C::kColumnsQ);
-    if (warp == kCopier && lane == 0 && blocks > 0) {
-        prefetch_map(&a.q);
-        prefetch_map(&a.k);
-        prefetch_map(&a.v);
-        prefetch_map(&a.g);
-    }
-    fence_before();
-    __syncthreads();
-    fence_after();
-    const uint32_t tmem = *slot;
-    const uint32_t dq_cols = NT * 128;
+    const int i0 = tile * kRows;
+    if (i0 >= q.n) return;
+    const int blocks = tile_blocks<BN>(a, q, tile);
+    const GradBars<C> bars(smem);
+    const auto &ring = bars.ring;
     bool failed = false;
 
-    if (warp == kCopier) {
+    if (warp == C::kCopier) {
+        bars.make();
+        setup_arrive<C::kThreads>();
         const int kv_head = head / a.group;
         if (blocks > 0 && lane == 0) {
-            int tiles = 0;
-            for (int t = 0; t < NT; ++t) tiles += (first + t) * kRows < q.n;
-            bar_arrive_expect(q_full, 2 * tiles * C::kTile);
-            for (int t = 0; t < tiles; ++t) {
-                const int token = q.q0 + (first + t) * kRows;
-                copy_tile<DP>(smem_addr(smem) + 2 * t * C::kTile, &a.q, head, token, kRows, q_full);
-                copy_tile<DP>(smem_addr(smem) + (2 * t + 1) * C::kTile, &a.g, head, token, kRows, q_full);
-            }
+            bar_arrive_expect(bars.tile_full, 2 * C::kTile);
+            copy_tile<DP>(smem_addr(smem), &a.q, head, q.q0 + i0, kRows, bars.tile_full);
+            copy_tile<DP>(smem_addr(smem) + C::kTile, &a.g, head, q.q0 + i0, kRows, bars.tile_full);
         }
         __syncwarp();
         int issued = 0, tails = 0;
@@ -631,48 +636,62 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) atte
             }
         if (failed) {
             ring.drain(issued);
-            bar_wait(q_full, 0, kTries);
+            bar_wait(bars.tile_full, 0, kTries);
         }
-    } else if (warp == kIssuer) {
+    } else if (warp == C::kIssuer) {
+        tmem_alloc(smem_addr(bars.slot), C::kColumns);
+        fence_before();
+        setup_wait<C::kThreads>();
+        fence_after();
+        const uint32_t tmem = *bars.slot;
         if (blocks > 0 && elect_one()) {
-            const uint32_t q_addr = smem_addr(smem);
-            auto products = [&](int t, int j) {
-                two_products<DP>(tmem + 128 * t, q_addr + 2 * t * C::kTile, ring.addr(2 * j),
-                                 q_addr + (2 * t + 1) * C::kTile, ring.addr(2 * j + 1));
-                mma_commit(s_full + 8 * t);
+            const uint32_t q_addr = smem_addr(smem), g_addr = q_addr + C::kTile;
+            auto scores = [&](int j) {
+                tile_product<DP>(tmem + C::kColS, q_addr, ring.addr(2 * j));
+                mma_commit(bars.s_full);
             };
-            auto wait_block = [&](int j) {
-                return bar_wait(ring.full_bar(2 * j), ring.parity(2 * j), kTries) &&
-                       bar_wait(ring.full_bar(2 * j + 1), ring.parity(2 * j + 1), kTries);
+            auto grads = [&](int j) {
+                tile_product<DP>(tmem + C::kColG, g_addr, ring.addr(2 * j + 1));
+                mma_commit(bars.g_full);
+                mma_commit(ring.empty_bar(2 * j + 1));
             };
-            failed = !bar_wait(q_full, 0, kTries) || !wait_block(0);
+            failed = !bar_wait(bars.tile_full, 0, kTries) || !ring.wait_full(0);
             if (!failed) {
                 fence_after();
-                for (int t = 0; t < NT; ++t)
-                    if ((t ? nb1 : nb0) > 0) products(t, 0);
-                mma_commit(ring.empty_bar(1));
+                scores(0);
+                failed = !ring.wait_full(1);
             }
+            if (!failed) grads(0);
             for (int j = 0; j < blocks && !failed; ++j) {
-                failed = j + 1 < blocks && !wait_block(j + 1);
-                for (int t = 0; t < NT && !failed; ++t) {
-                    if (j >= (t ? nb1 : nb0)) continue;
-                    failed = !bar_wait(p_full + 8 * t, j & 1, kTries);
+                if (j + 1 < blocks) {
+                    // the next block's products, as soon as this one's have been read
+                    failed = !ring.wait_full(2 * j + 2) || !bar_wait(bars.s_read, j & 1, kTries);
                     if (failed) break;
                     fence_after();
-                    sum_product<DP>(tmem + dq_cols + t * DP, tmem + 128 * t, ring.addr(2 * j), j > 0);
-                    if (j + 1 < (t ? nb1 : nb0)) products(t, j + 1);
+                    scores(j + 1);
+                    failed = !ring.wait_full(2 * j + 3) || !bar_wait(bars.g_read, j & 1, kTries);
+                    if (failed) break;
+                    fence_after();
+                    grads(j + 1);
                 }
+                failed = !bar_wait(bars.w_full, j & 1, kTries);
                 if (failed) break;
+                fence_after();
+                sum_product<DP>(tmem + C::kColSum, tmem + kColW, 32, ring.addr(2 * j), j > 0);
+                mma_commit(bars.w_done);
                 mma_commit(ring.empty_bar(2 * j));
-                if (j + 1 < blocks) mma_commit(ring.empty_bar(2 * j + 3));
             }
-            mma_commit(done);
-            failed |= !bar_wait(done, 0, kTries);
+            mma_commit(bars.done);
+            failed |= !bar_wait(bars.done, 0, kTries);
         }
         __syncwarp();
     } else {
-        const int t = warp / 4, nb = t ? nb1 : nb0;
-        const int i = (first + t) * kRows + (threadIdx.x & 127);
+        fence_before();
+        setup_wait<C::kThreads>();
+        fence_after();
+        const uint32_t tmem = *bars.slot;
+        const int half = warp / 4;  // of the columns
+        const int i = i0 + (threadIdx.x & 127);
         const bool live = i < q.n;
         const int64_t token = q.q0 + (int64_t)i;
         const int lim = visible(a, q, i);
@@ -680,6 +699,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) atte
         if (live) {
             const uint4 *o = reinterpret_cast<const uint4 *>(a.o.p + token * a.o.ts + head * a.o.hs);
             const uint4 *g = reinterpret_cast<const uint4 *>(a.go.p + token * a.go.ts + head * a.go.hs);
+#pragma unroll 4
             for (int c = 0; c < a.D / 8; ++c) {
                 const uint4 x = o[c], y = g[c];
                 const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
@@ -689,69 +709,91 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsQ == 256 ? 2 : 1) atte
                     delta = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), delta);
                 }
             }
-            a.delta[(int64_t)head * a.total_q + token] = delta;
+            if (half == 0) a.delta[(int64_t)head * a.total_q + token] = delta;
             const float l = a.lse[(int64_t)head * a.total_q + token];
             lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
         }
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        const uint32_t s_addr = tmem + lanes + 128 * t;
-        for (int j = 0; j < nb; ++j) {
-            if (!__all_sync(kFull, bar_wait(s_full + 8 * t, j & 1, kTries))) {
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        const uint64_t scale2 = pair(a.scale2, a.scale2), lse22 = pair(-lse2, -lse2), delta2 = pair(-delta, -delta);
+        for (int j = 0; j < blocks; ++j) {
+            if (!__all_sync(kFull, bar_wait(bars.s_full, j & 1, kTries))) {
                 failed = true;
                 break;
             }
             fence_after();
-            uint32_t s[2][32], p[2][32], ds[32];
-            tmem_load(s_addr, s[0]);
-            tmem_load(s_addr + 32, s[1]);
-            tmem_load(s_addr + 64, p[0]);
-            tmem_load(s_addr + 96, p[1]);
+            uint32_t s[2][32], w[32];
+            tmem_load(lanes + C::kColS + 64 * half, s[0]);
+            tmem_load(lanes + C::kColS + 64 * half + 32, s[1]);
             load_wait(s[0]);
             load_wait(s[1]);
-            load_wait(p[0]);
-            load_wait(p[1]);
-            const int seen = lim - j * BN;
-            const bool whole = __all_sync(kFull, seen >= BN);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(bars.s_read);
+            const int seen = lim - j * BN - 64 * half;
+            const bool whole = __all_sync(kFull, seen >= 64);
 #pragma unroll
-            for (int c = 0; c < BN; c += 2) {
-                float d[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float pr = exp2_approx(fmaf(__uint_as_float(s[c / 32][c % 32 + e]), a.scale2, -lse2));
-                    d[e] = pr * (__uint_as_float(p[c / 32][c % 32 + e]) - delta);
-                    if (!whole && c + e >= seen) d[e] = 0.f;
-                }
-                ds[c / 2] = pack_bf16(d[0], d[1]);
+            for (int c = 0; c < 64; c += 2) {
+                const float2 y = unpair(fma2(pair_bits(s[c / 32][c % 32], s[c / 32][c % 32 + 1]), scale2, lse22));
+                s[c / 32][c % 32] = __float_as_uint(exp2_approx(y.x));
+                s[c / 32][c % 32 + 1] = __float_as_uint(exp2_approx(y.y));
             }
-            tmem_store(s_addr, ds);
+            if (!__all_sync(kFull, bar_wait(bars.g_full, j & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t g[32];
+                tmem_load(lanes + C::kColG + 64 * half + 32 * h, g);
+                load_wait(g);
+                if (h == 1) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(bars.g_read);
+                }
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    float2 d = unpair(mul2(pair_bits(s[h][c], s[h][c + 1]),
+                                           add2(pair_bits(g[c], g[c + 1]), delta2)));
+                    if (!whole && 32 * h + c >= seen) d.x = 0.f;
+                    if (!whole && 32 * h + c + 1 >= seen) d.y = 0.f;
+                    w[16 * h + c / 2] = pack_bf16(d.x, d.y);
+                }
+            }
+            if (j > 0 && !__all_sync(kFull, bar_wait(bars.w_done, (j - 1) & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+            tmem_store(lanes + kColW + 32 * half, w);
             store_wait();
             fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(p_full + 8 * t);
+            if (lane == 0) bar_arrive(bars.w_full);
         }
-        if (nb > 0) {
-            if (!failed) failed = !__all_sync(kFull, bar_wait(done, 0, kTries));
+        if (blocks > 0) {
+            if (!failed) failed = !__all_sync(kFull, bar_wait(bars.done, 0, kTries));
             fence_after();
-            if (!failed)
-                write_rows<DP>(tmem + lanes + dq_cols + t * DP, smem + 2 * t * C::kTile + (warp & 3) * 32 * DP * 2, a.dq,
-                               token - lane, head, q.n - (i - lane), a.D, a.scale);
-        } else if (live) {
+            if (!failed)  // Q's tile is read for the last time: its memory takes the rows
+                write_rows<DP / 2>(lanes + C::kColSum + DP / 2 * half, smem + warp * 32 * DP, a.dq, token - lane, head,
+                                   q.n - (i - lane), DP / 2 * half, a.D, a.scale);
+        } else if (live && half == 0) {
             write_zero_row(a.dq.p + token * a.dq.ts + head * a.dq.hs, a.D);
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
     fence_before();
     __syncthreads();
-    if (warp == kIssuer) tmem_free(tmem, C::kColumnsQ);
+    if (warp == C::kIssuer) tmem_free(*bars.slot, C::kColumns);
 }
 
-// ---- gradient of keys and values ----------------------------------------------------
+// ---- gradient of keys and values
 
 template <class C>
-__global__ void __launch_bounds__(C::kThreads, C::kColumnsK == 256 ? 2 : 1) attention_grad_kv_kernel(
-    const __grid_constant__ AttnArgs a) {
-    constexpr int DP = C::DP, NT = C::NT, BN = kGradCols;
-    static_assert(C::NS >= 2 * (NT + 1), "a block being summed and the next of every buffer are held at once");
+__global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const __grid_constant__ AttnArgs a) {
+    constexpr int DP = C::DP, BN = C::BN;
+    constexpr int kColV = C::kColSum, kColK = C::kColSum + DP;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
@@ -770,175 +812,204 @@ __global__ void __launch_bounds__(C::kThreads, C::kColumnsK == 256 ? 2 : 1) atte
     const int b0 = a.causal ? max(0, j0 - off) / BN : 0;
     const int per_head = max(0, (q.n + BN - 1) / BN - b0);
     const int blocks = per_head * a.group;
-
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * C::kTile + C::NS * C::kSlot + C::kVec);
-    const uint32_t bar0 = smem_addr(bars), k_full = bar0;
-    Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
-    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 8 * NT, done = p_full + 8 * NT;
-    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
-    constexpr int kCopier = 4 * NT, kIssuer = 4 * NT + 1;
-    if (threadIdx.x == 0) {
-        for (uint32_t b = bar0; b < bar0 + 8 * C::kBars; b += 8) bar_init(b, b >= p_full && b < done ? 4 : 1);
-        bar_init_fence();
-    }
-    if (warp == kIssuer) tmem_alloc(smem_addr(slot), C::kColumnsK);
-    if (warp == kCopier && lane == 0 && blocks > 0) {
-        prefetch_map(&a.q);
-        prefetch_map(&a.k);
-        prefetch_map(&a.v);
-        prefetch_map(&a.g);
-    }
-    fence_before();
-    __syncthreads();
-    fence_after();
-    const uint32_t tmem = *slot;
-    const uint32_t dv_cols = NT * 128, dk_cols = dv_cols + DP;
+    const GradBars<C> bars(smem);
+    const auto &ring = bars.ring;
     bool failed = false;
 
-    if (warp == kCopier) {
+    if (warp == C::kCopier) {
+        bars.make();
+        setup_arrive<C::kThreads>();
         if (blocks > 0 && lane == 0) {
-            bar_arrive_expect(k_full, 2 * C::kTile);
-            copy_tile<DP>(smem_addr(smem), &a.k, head, q.k0 + j0, kRows, k_full);
-            copy_tile<DP>(smem_addr(smem) + C::kTile, &a.v, head, q.k0 + j0, kRows, k_full);
+            bar_arrive_expect(bars.tile_full, 2 * C::kTile);
+            copy_tile<DP>(smem_addr(smem), &a.k, head, q.k0 + j0, kRows, bars.tile_full);
+            copy_tile<DP>(smem_addr(smem) + C::kTile, &a.v, head, q.k0 + j0, kRows, bars.tile_full);
         }
         __syncwarp();
-        int issued = 0, tails = 0;
+        int issued = 0, tails = 0, h = head * a.group, b = b0;
         for (int it = 0; it < blocks && !failed; ++it) {
-            const int h = head * a.group + it / per_head, i0 = (b0 + it % per_head) * BN;
             for (int kind = 0; kind < 2 && !failed; ++kind) {
                 failed = !ring.wait_free(issued) ||
-                         !ring.template fill<DP>(issued, kind ? &a.g : &a.q, h, q.q0 + i0, BN, q.n - i0, true, tails);
+                         !ring.template fill<DP>(issued, kind ? &a.g : &a.q, h, q.q0 + b * BN, BN, q.n - b * BN, true,
+                                                 tails);
                 if (!failed) ++issued;
             }
+            if (++b == b0 + per_head) b = b0, ++h;
         }
         if (failed) {
             ring.drain(issued);
-            bar_wait(k_full, 0, kTries);
+            bar_wait(bars.tile_full, 0, kTries);
         }
-    } else if (warp == kIssuer) {
+    } else if (warp == C::kIssuer) {
+        tmem_alloc(smem_addr(bars.slot), C::kColumns);
+        fence_before();
+        setup_wait<C::kThreads>();
+        fence_after();
+        const uint32_t tmem = *bars.slot;
         if (blocks > 0 && elect_one()) {
             const uint32_t k_addr = smem_addr(smem), v_addr = k_addr + C::kTile;
-            // S^T and dP^T of block `it` into buffer it % NT
-            auto products = [&](int it) {
-                if (!bar_wait(ring.full_bar(2 * it), ring.parity(2 * it), kTries) ||
-                    !bar_wait(ring.full_bar(2 * it + 1), ring.parity(2 * it + 1), kTries))
-                    return false;
+            auto scores = [&](int it) {
+                if (!ring.wait_full(2 * it)) return false;
                 fence_after();
-                two_products<DP>(tmem + 128 * (it % NT), k_addr, ring.addr(2 * it), v_addr, ring.addr(2 * it + 1));
-                mma_commit(s_full + 8 * (it % NT));
+                tile_product<DP>(tmem + C::kColS, k_addr, ring.addr(2 * it));
+                mma_commit(bars.s_full);
                 return true;
             };
-            failed = !bar_wait(k_full, 0, kTries);
-            for (int it = 0; it < NT && it < blocks && !failed; ++it) failed = !products(it);
+            auto grads = [&](int it) {
+                if (!ring.wait_full(2 * it + 1)) return false;
+                fence_after();
+                tile_product<DP>(tmem + C::kColG, v_addr, ring.addr(2 * it + 1));
+                mma_commit(bars.g_full);
+                return true;
+            };
+            failed = !bar_wait(bars.tile_full, 0, kTries) || !scores(0) || !grads(0);
+            // P^T takes the place of S^T, dS^T that of the gradient of P^T:
+            // the next product into either comes after the one that reads
+            // it (products run in the order of their issue). While the rows'
+            // arithmetic makes P^T, dK and the next gradient of P^T are computed;
+            // while it makes dS^T, dV and the next S^T.
             for (int it = 0; it < blocks && !failed; ++it) {
-                const int t = it % NT;
-                failed = !bar_wait(p_full + 8 * t, (it / NT) & 1, kTries);
+                const bool more = it + 1 < blocks;
+                failed = !bar_wait(bars.v_full, it & 1, kTries);
                 if (failed) break;
                 fence_after();
-                sum_product<DP>(tmem + dv_cols, tmem + 128 * t, ring.addr(2 * it + 1), it > 0);
-                sum_product<DP>(tmem + dk_cols, tmem + 128 * t + 64, ring.addr(2 * it), it > 0);
+                sum_product<DP>(tmem + kColV, tmem + C::kColS, 64, ring.addr(2 * it + 1), it > 0);
+                if (more && !scores(it + 1)) failed = true;
+                if (failed || !bar_wait(bars.w_full, it & 1, kTries)) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                sum_product<DP>(tmem + kColK, tmem + C::kColG, 64, ring.addr(2 * it), it > 0);
                 mma_commit(ring.empty_bar(2 * it));
                 mma_commit(ring.empty_bar(2 * it + 1));
-                if (it + NT < blocks) failed = !products(it + NT);
+                if (more && !grads(it + 1)) failed = true;
             }
-            mma_commit(done);
-            failed |= !bar_wait(done, 0, kTries);
+            mma_commit(bars.done);
+            failed |= !bar_wait(bars.done, 0, kTries);
         }
         __syncwarp();
     } else {
-        const int t = warp / 4;
+        fence_before();
+        setup_wait<C::kThreads>();
+        fence_after();
+        const uint32_t tmem = *bars.slot;
+        const int half = warp / 4;  // of the columns
         const int j = j0 + (threadIdx.x & 127);
-        const bool live = j < q.m;
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        const uint32_t s_addr = tmem + lanes + 128 * t;
-        float *vec = reinterpret_cast<float *>(smem + 2 * C::kTile + C::NS * C::kSlot) + warp * 2 * BN;
-        // lane's share of a block's lse x log2 e (infinite for rows that are
-        // not there or see nothing: probability 0) and delta
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        const uint32_t s_addr = lanes + C::kColS + 64 * half, g_addr = lanes + C::kColG + 64 * half;
+        float *vec = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile) + warp * 128;
+        // this lane's share of its columns' -lse x log2 e (minus infinity for
+        // rows that are not there or see nothing: probability 0) and -delta
         float nl[2], nd[2];
-        auto fetch = [&](int it) {
-            const int h = head * a.group + it / per_head, i0 = (b0 + it % per_head) * BN;
+        int h = head * a.group, b = b0;  // of the next block fetched
+        auto fetch = [&]() {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int i = i0 + lane + 32 * e;
-                nl[e] = INFINITY, nd[e] = 0.f;
+                const int i = b * BN + 64 * half + lane + 32 * e;
+                nl[e] = -INFINITY, nd[e] = 0.f;
                 if (i < q.n) {
                     const int64_t at = (int64_t)h * a.total_q + q.q0 + i;
                     const float l = a.lse[at];
-                    nl[e] = l == -INFINITY ? INFINITY : l * kLog2e;
-                    nd[e] = a.delta[at];
+                    nl[e] = l == -INFINITY ? -INFINITY : -l * kLog2e;
+                    nd[e] = -a.delta[at];
                 }
             }
+            if (++b == b0 + per_head) b = b0, ++h;
         };
-        if (t < blocks) fetch(t);
-        for (int it = t; it < blocks; it += NT) {
+        const uint64_t scale2 = pair(a.scale2, a.scale2);
+        if (blocks > 0) fetch();
+        int bi = b0;  // the block at hand
+        for (int it = 0; it < blocks; ++it) {
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 vec[lane + 32 * e] = nl[e];
-                vec[BN + lane + 32 * e] = nd[e];
+                vec[64 + lane + 32 * e] = nd[e];
             }
             __syncwarp();
-            if (it + NT < blocks) fetch(it + NT);
-            if (!__all_sync(kFull, bar_wait(s_full + 8 * t, (it / NT) & 1, kTries))) {
+            if (it + 1 < blocks) fetch();
+            // masked: query i sees key j when i >= j - off
+            const int low = a.causal ? j - off - bi * BN - 64 * half : 0;
+            if (++bi == b0 + per_head) bi = b0;
+            const bool whole = __all_sync(kFull, low <= 0);
+            if (!__all_sync(kFull, bar_wait(bars.s_full, it & 1, kTries))) {
                 failed = true;
                 break;
             }
             fence_after();
-            // masked: query i sees key j when i >= j - off
-            const int low = a.causal ? j - off - (b0 + it % per_head) * BN : 0;
-            const bool whole = __all_sync(kFull, low <= 0);
-            uint32_t pp[32], ds[32];
+            uint32_t s[2][32], w[32];
+            tmem_load(s_addr, s[0]);
+            tmem_load(s_addr + 32, s[1]);
+            load_wait(s[0]);
+            load_wait(s[1]);
 #pragma unroll
-            for (int c0 = 0; c0 < BN; c0 += 32) {
-                uint32_t s[32], p[32];
-                tmem_load(s_addr + c0, s);
-                tmem_load(s_addr + 64 + c0, p);
-                load_wait(s);
-                load_wait(p);
+            for (int c = 0; c < 64; c += 4) {
+                const ulonglong2 l = *reinterpret_cast<const ulonglong2 *>(vec + c);
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    const float4 l4 = *reinterpret_cast<const float4 *>(vec + c0 + c);
-                    const float4 d4 = *reinterpret_cast<const float4 *>(vec + BN + c0 + c);
-                    const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
-                    float pr[4], d[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        pr[e] = exp2_approx(fmaf(__uint_as_float(s[c + e]), a.scale2, -ls[e]));
-                        d[e] = pr[e] * (__uint_as_float(p[c + e]) - dl[e]);
-                        if (!whole && c0 + c + e < low) pr[e] = d[e] = 0.f;
-                    }
-                    pp[(c0 + c) / 2] = pack_bf16(pr[0], pr[1]);
-                    pp[(c0 + c) / 2 + 1] = pack_bf16(pr[2], pr[3]);
-                    ds[(c0 + c) / 2] = pack_bf16(d[0], d[1]);
-                    ds[(c0 + c) / 2 + 1] = pack_bf16(d[2], d[3]);
+                for (int e = 0; e < 4; e += 2) {
+                    const int x = c + e;
+                    const float2 y = unpair(fma2(pair_bits(s[x / 32][x % 32], s[x / 32][x % 32 + 1]), scale2,
+                                                 e ? l.y : l.x));
+                    float p0 = exp2_approx(y.x), p1 = exp2_approx(y.y);
+                    if (!whole && x < low) p0 = 0.f;
+                    if (!whole && x + 1 < low) p1 = 0.f;
+                    s[x / 32][x % 32] = __float_as_uint(p0);
+                    s[x / 32][x % 32 + 1] = __float_as_uint(p1);
+                    w[x / 2] = pack_bf16(p0, p1);
                 }
             }
-            tmem_store(s_addr, pp);
-            tmem_store(s_addr + 64, ds);
+            tmem_store(s_addr, w);
             store_wait();
             fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(p_full + 8 * t);
+            if (lane == 0) bar_arrive(bars.v_full);
+            if (!__all_sync(kFull, bar_wait(bars.g_full, it & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                uint32_t g[32];
+                tmem_load(g_addr + 32 * hh, g);
+                load_wait(g);
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(vec + 64 + 32 * hh + c);
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        float2 y = unpair(mul2(pair_bits(s[hh][c + e], s[hh][c + e + 1]),
+                                               add2(pair_bits(g[c + e], g[c + e + 1]), e ? d.y : d.x)));
+                        if (!whole && 32 * hh + c + e < low) y.x = 0.f;
+                        if (!whole && 32 * hh + c + e + 1 < low) y.y = 0.f;
+                        w[16 * hh + (c + e) / 2] = pack_bf16(y.x, y.y);
+                    }
+                }
+            }
+            tmem_store(g_addr, w);
+            store_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(bars.w_full);
         }
         const int64_t token = q.k0 + (int64_t)j;
         if (blocks > 0) {
-            if (!failed) failed = !__all_sync(kFull, bar_wait(done, 0, kTries));
+            if (!failed) failed = !__all_sync(kFull, bar_wait(bars.done, 0, kTries));
             fence_after();
-            uint8_t *stage = smem + (warp & 3) * 32 * DP * 2;  // K's and V's tiles are read for the last time
-            if (!failed && t == 0)
-                write_rows<DP>(tmem + lanes + dv_cols, stage + C::kTile, a.dv, token - lane, head, q.m - (j - lane), a.D,
-                               1.f);
-            if (!failed && t == NT - 1)
-                write_rows<DP>(tmem + lanes + dk_cols, stage, a.dk, token - lane, head, q.m - (j - lane), a.D, a.scale);
-        } else if (live && t == 0) {
-            write_zero_row(a.dv.p + token * a.dv.ts + head * a.dv.hs, a.D);
-            write_zero_row(a.dk.p + token * a.dk.ts + head * a.dk.hs, a.D);
+            if (!failed) {  // K's and V's tiles are read for the last time: dK and dV go through their memory
+                const Out &out = half ? a.dk : a.dv;
+                write_rows<DP>(lanes + (half ? kColK : kColV), smem + half * C::kTile + (warp & 3) * 32 * DP * 2, out,
+                               token - lane, head, q.m - (j - lane), 0, a.D, half ? a.scale : 1.f);
+            }
+        } else if (j < q.m) {
+            const Out &out = half ? a.dk : a.dv;
+            write_zero_row(out.p + token * out.ts + head * out.hs, a.D);
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
     fence_before();
     __syncthreads();
-    if (warp == kIssuer) tmem_free(tmem, C::kColumnsK);
+    if (warp == C::kIssuer) tmem_free(*bars.slot, C::kColumns);
 }
 
 // ---- host side ------------------------------------------------------------------
@@ -1054,9 +1125,8 @@ cudaError_t launch_tiles(K kernel, AttnArgs &a, int tiles, int heads, int thread
 
 using Fwd64 = FwdShape<64, 128, 6>;
 using Fwd128 = FwdShape<128, 128, 4>;
-using Grad64 = GradShape<64, 1, 8>;
-using Grad128 = GradShape<128, 2, 4>;   // queries: 4 slots of K, V
-using GradK128 = GradShape<128, 2, 8>;  // keys: a block more for each buffer
+using Grad64 = GradShape<64>;
+using Grad128 = GradShape<128>;
 
 // A register split draws on what the block is launched with: a build whose
 // kernel got fewer registers must not run it (its threads would wait forever).
@@ -1074,7 +1144,7 @@ template <class C>
 cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
     static const bool covered = registers_cover<C>(reinterpret_cast<const void *>(attention_forward_kernel<C>));
     if (!covered) return cudaErrorLaunchOutOfResources;
-    return launch_tiles(attention_forward_kernel<C>, a, (a.max_q + 2 * kRows - 1) / (2 * kRows), a.hq, C::kThreads,
+    return launch_tiles(attention_forward_kernel<C>, a, (int)(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows)), a.hq, C::kThreads,
                         C::kSmem, s);
 }
 
@@ -1147,24 +1217,18 @@ dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_hea
     const bool small = cfg->head_dim <= 64;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int D = cfg->head_dim;
-    // queries in tiles, keys in blocks; then the other way round
     DPB_CHECK(make_map(&a.q, q, cfg->total_q, cfg->heads_q, D, kRows));
     DPB_CHECK(make_map(&a.g, grad_o, cfg->total_q, cfg->heads_q, D, kRows));
-    DPB_CHECK(make_map(&a.k, k, cfg->total_k, cfg->heads_kv, D, kGradCols));
-    DPB_CHECK(make_map(&a.v, v, cfg->total_k, cfg->heads_kv, D, kGradCols));
-    const int nt = small ? Grad64::NT : Grad128::NT, qt = (cfg->max_q + nt * kRows - 1) / (nt * kRows);
-    DPB_CHECK(launch_status(
-        small ? launch_tiles(attention_grad_q_kernel<Grad64>, a, qt, a.hq, Grad64::kThreads, Grad64::kSmemQ, s)
-              : launch_tiles(attention_grad_q_kernel<Grad128>, a, qt, a.hq, Grad128::kThreads, Grad128::kSmemQ, s),
-        "attention_backward (queries)"));
-    DPB_CHECK(make_map(&a.q, q, cfg->total_q, cfg->heads_q, D, kGradCols));
-    DPB_CHECK(make_map(&a.g, grad_o, cfg->total_q, cfg->heads_q, D, kGradCols));
     DPB_CHECK(make_map(&a.k, k, cfg->total_k, cfg->heads_kv, D, kRows));
     DPB_CHECK(make_map(&a.v, v, cfg->total_k, cfg->heads_kv, D, kRows));
-    const int kt = (cfg->max_k + kRows - 1) / kRows;
+    const int qt = (int)(((int64_t)cfg->max_q + kRows - 1) / kRows), kt = (int)(((int64_t)cfg->max_k + kRows - 1) / kRows);
+    DPB_CHECK(launch_status(
+        small ? launch_tiles(attention_grad_q_kernel<Grad64>, a, qt, a.hq, Grad64::kThreads, Grad64::kSmem, s)
+              : launch_tiles(attention_grad_q_kernel<Grad128>, a, qt, a.hq, Grad128::kThreads, Grad128::kSmem, s),
+        "attention_backward (queries)"));
     return launch_status(
-        small ? launch_tiles(attention_grad_kv_kernel<Grad64>, a, kt, a.hkv, Grad64::kThreads, Grad64::kSmemK, s)
-              : launch_tiles(attention_grad_kv_kernel<GradK128>, a, kt, a.hkv, GradK128::kThreads, GradK128::kSmemK, s),
+        small ? launch_tiles(attention_grad_kv_kernel<Grad64>, a, kt, a.hkv, Grad64::kThreads, Grad64::kSmem, s)
+              : launch_tiles(attention_grad_kv_kernel<Grad128>, a, kt, a.hkv, Grad128::kThreads, Grad128::kSmem, s),
         "attention_backward (keys and values)");
 }
 

@@ -220,8 +220,8 @@ struct FwdShape {
     static constexpr int kBars = 1 + 2 * NS + 1 + 2 * 6 + 1;
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kSlot + 8 * kBars + 16;
     static constexpr int kThreads = 384;  // two softmax warpgroups, one of the copying and the issuing warp
-    // registers of a softmax thread and of the others: 2 x 128 x 232 + 128 x 40 = 384 x 168
-    static constexpr int kRegsRow = 232, kRegsOther = 40;
+    // registers of a softmax thread and of the others: 256 x 216 + 128 x 72 = 384 x 168
+    static constexpr int kRegsRow = 216, kRegsOther = 72;
 };
 
 // Visible keys of query row i (of n, against m keys).
@@ -532,7 +532,8 @@ template <int DP_>
 struct GradShape {
     static constexpr int DP = DP_, BN = 128, NS = DP == 64 ? 6 : 4;
     static constexpr int kTile = kRows * DP * 2;
-    static constexpr int kThreads = 320, kCopier = 8, kIssuer = 9;
+    static constexpr int kThreads = 384, kCopier = 8, kIssuer = 9;  // 2 x 4 row warps, then these two (and 2 idle)
+    static constexpr int kRegsRow = 208, kRegsOther = 88;           // 256 x 208 + 128 x 88 = 384 x 168
     static constexpr int kColS = 0, kColG = 128, kColSum = 256;  // S, the gradient of P, the sums
     static constexpr int kColumns = 512;
     static constexpr int kBars = 1 + 2 * NS + 1 + 8;
@@ -616,6 +617,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
     const auto &ring = bars.ring;
     bool failed = false;
 
+    if (warp >= 8) give_registers<C::kRegsOther>();
     if (warp == C::kCopier) {
         bars.make();
         setup_arrive<C::kThreads>();
@@ -685,7 +687,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
             failed |= !bar_wait(bars.done, 0, kTries);
         }
         __syncwarp();
+    } else if (warp > C::kIssuer) {
+        setup_wait<C::kThreads>();
     } else {
+        take_registers<C::kRegsRow>();
         fence_before();
         setup_wait<C::kThreads>();
         fence_after();
@@ -721,45 +726,46 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
                 break;
             }
             fence_after();
-            uint32_t s[2][32], w[32];
-            tmem_load(lanes + C::kColS + 64 * half, s[0]);
-            tmem_load(lanes + C::kColS + 64 * half + 32, s[1]);
-            load_wait(s[0]);
-            load_wait(s[1]);
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(bars.s_read);
-            const int seen = lim - j * BN - 64 * half;
-            const bool whole = __all_sync(kFull, seen >= 64);
+            uint32_t s[64], g[2][32], w[32];
+            {
+                uint32_t x[2][32];
+                tmem_load(lanes + C::kColS + 64 * half, x[0]);
+                tmem_load(lanes + C::kColS + 64 * half + 32, x[1]);
+                load_wait(x[0]);
+                load_wait(x[1]);
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(bars.s_read);
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
-                const float2 y = unpair(fma2(pair_bits(s[c / 32][c % 32], s[c / 32][c % 32 + 1]), scale2, lse22));
-                s[c / 32][c % 32] = __float_as_uint(exp2_approx(y.x));
-                s[c / 32][c % 32 + 1] = __float_as_uint(exp2_approx(y.y));
+                for (int c = 0; c < 64; c += 2) {
+                    const float2 y = unpair(fma2(pair_bits(x[c / 32][c % 32], x[c / 32][c % 32 + 1]), scale2, lse22));
+                    s[c] = __float_as_uint(exp2_approx(y.x));
+                    s[c + 1] = __float_as_uint(exp2_approx(y.y));
+                }
             }
             if (!__all_sync(kFull, bar_wait(bars.g_full, j & 1, kTries))) {
                 failed = true;
                 break;
             }
             fence_after();
+            tmem_load(lanes + C::kColG + 64 * half, g[0]);
+            tmem_load(lanes + C::kColG + 64 * half + 32, g[1]);
+            load_wait(g[0]);
+            load_wait(g[1]);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(bars.g_read);
+            const int seen = lim - j * BN - 64 * half;
+            if (!__all_sync(kFull, seen >= 64)) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t g[32];
-                tmem_load(lanes + C::kColG + 64 * half + 32 * h, g);
-                load_wait(g);
-                if (h == 1) {
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(bars.g_read);
-                }
+                for (int c = 0; c < 64; ++c)
+                    if (c >= seen) s[c] = g[c / 32][c % 32] = 0u;
+            }
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    float2 d = unpair(mul2(pair_bits(s[h][c], s[h][c + 1]),
-                                           add2(pair_bits(g[c], g[c + 1]), delta2)));
-                    if (!whole && 32 * h + c >= seen) d.x = 0.f;
-                    if (!whole && 32 * h + c + 1 >= seen) d.y = 0.f;
-                    w[16 * h + c / 2] = pack_bf16(d.x, d.y);
-                }
+            for (int c = 0; c < 64; c += 2) {
+                const float2 d = unpair(
+                    mul2(pair_bits(s[c], s[c + 1]), add2(pair_bits(g[c / 32][c % 32], g[c / 32][c % 32 + 1]), delta2)));
+                w[c / 2] = pack_bf16(d.x, d.y);
             }
             if (j > 0 && !__all_sync(kFull, bar_wait(bars.w_done, (j - 1) & 1, kTries))) {
                 failed = true;
@@ -816,6 +822,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
     const auto &ring = bars.ring;
     bool failed = false;
 
+    if (warp >= 8) give_registers<C::kRegsOther>();
     if (warp == C::kCopier) {
         bars.make();
         setup_arrive<C::kThreads>();
@@ -888,7 +895,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             failed |= !bar_wait(bars.done, 0, kTries);
         }
         __syncwarp();
+    } else if (warp > C::kIssuer) {
+        setup_wait<C::kThreads>();
     } else {
+        take_registers<C::kRegsRow>();
         fence_before();
         setup_wait<C::kThreads>();
         fence_after();
@@ -937,27 +947,32 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 break;
             }
             fence_after();
-            uint32_t s[2][32], w[32];
-            tmem_load(s_addr, s[0]);
-            tmem_load(s_addr + 32, s[1]);
-            load_wait(s[0]);
-            load_wait(s[1]);
+            uint32_t s[64], w[32];
+            {
+                uint32_t x[2][32];
+                tmem_load(s_addr, x[0]);
+                tmem_load(s_addr + 32, x[1]);
+                load_wait(x[0]);
+                load_wait(x[1]);
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const ulonglong2 l = *reinterpret_cast<const ulonglong2 *>(vec + c);
+                for (int c = 0; c < 64; c += 4) {
+                    const ulonglong2 l = *reinterpret_cast<const ulonglong2 *>(vec + c);
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    const int x = c + e;
-                    const float2 y = unpair(fma2(pair_bits(s[x / 32][x % 32], s[x / 32][x % 32 + 1]), scale2,
-                                                 e ? l.y : l.x));
-                    float p0 = exp2_approx(y.x), p1 = exp2_approx(y.y);
-                    if (!whole && x < low) p0 = 0.f;
-                    if (!whole && x + 1 < low) p1 = 0.f;
-                    s[x / 32][x % 32] = __float_as_uint(p0);
-                    s[x / 32][x % 32 + 1] = __float_as_uint(p1);
-                    w[x / 2] = pack_bf16(p0, p1);
+                    for (int e = c; e < c + 4; e += 2) {
+                        const float2 y = unpair(fma2(pair_bits(x[e / 32][e % 32], x[e / 32][e % 32 + 1]), scale2,
+                                                     e > c ? l.y : l.x));
+                        s[e] = __float_as_uint(exp2_approx(y.x));
+                        s[e + 1] = __float_as_uint(exp2_approx(y.y));
+                    }
                 }
             }
+            if (!whole) {
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    if (c < low) s[c] = 0u;
+            }
+#pragma unroll
+            for (int c = 0; c < 64; c += 2) w[c / 2] = pack_bf16(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
             tmem_store(s_addr, w);
             store_wait();
             fence_before();
@@ -968,22 +983,25 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 break;
             }
             fence_after();
+            uint32_t g[2][32];
+            tmem_load(g_addr, g[0]);
+            tmem_load(g_addr + 32, g[1]);
+            load_wait(g[0]);
+            load_wait(g[1]);
+            if (!whole) {
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                uint32_t g[32];
-                tmem_load(g_addr + 32 * hh, g);
-                load_wait(g);
+                for (int c = 0; c < 64; ++c)
+                    if (c < low) g[c / 32][c % 32] = 0u;
+            }
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(vec + 64 + 32 * hh + c);
+            for (int c = 0; c < 64; c += 4) {
+                const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(vec + 64 + c);
 #pragma unroll
-                    for (int e = 0; e < 4; e += 2) {
-                        float2 y = unpair(mul2(pair_bits(s[hh][c + e], s[hh][c + e + 1]),
-                                               add2(pair_bits(g[c + e], g[c + e + 1]), e ? d.y : d.x)));
-                        if (!whole && 32 * hh + c + e < low) y.x = 0.f;
-                        if (!whole && 32 * hh + c + e + 1 < low) y.y = 0.f;
-                        w[16 * hh + (c + e) / 2] = pack_bf16(y.x, y.y);
-                    }
+                for (int e = c; e < c + 4; e += 2) {
+                    const float2 y = unpair(mul2(pair_bits(s[e], s[e + 1]),
+                                                 add2(pair_bits(g[e / 32][e % 32], g[e / 32][e % 32 + 1]),
+                                                      e > c ? d.y : d.x)));
+                    w[e / 2] = pack_bf16(y.x, y.y);
                 }
             }
             tmem_store(g_addr, w);
@@ -1111,15 +1129,31 @@ void fill_args(AttnArgs &a, const dpb_attention_config *c, const int32_t *cu_q, 
 In in_rows(const dpb_heads *h) { return h ? In{static_cast<const bf16 *>(h->data), h->token_stride, h->head_stride} : In{}; }
 Out out_rows(const dpb_heads *h) { return h ? Out{static_cast<bf16 *>(h->data), h->token_stride, h->head_stride} : Out{}; }
 
-template <typename K>
-cudaError_t launch_tiles(K kernel, AttnArgs &a, int tiles, int heads, int threads, int smem, cudaStream_t s) {
+// A register split draws on what the block is launched with: a build whose
+// kernel got fewer registers must not run it (its threads would wait for ever).
+template <class C>
+cudaError_t registers_cover(const void *kernel) {
+    cudaFuncAttributes f;
+    const cudaError_t e = cudaFuncGetAttributes(&f, kernel);
+    if (e != cudaSuccess) return e;
+    return f.numRegs * C::kThreads >= 256 * C::kRegsRow + (C::kThreads - 256) * C::kRegsOther
+               ? cudaSuccess
+               : cudaErrorLaunchOutOfResources;
+}
+
+// Launches a kernel over tiles x heads x sequences.
+template <class C, void (*KERNEL)(AttnArgs)>
+cudaError_t launch_tiles(AttnArgs &a, int tiles, int heads, cudaStream_t s) {
     a.tiles = tiles;
     const int64_t blocks = (int64_t)tiles * heads * a.seqs;
     if (blocks == 0) return cudaSuccess;
     if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(kernel), smem);
+    const void *kernel = reinterpret_cast<const void *>(KERNEL);
+    static const cudaError_t covered = registers_cover<C>(kernel);
+    if (covered != cudaSuccess) return covered;
+    const cudaError_t e = allow_smem(kernel, C::kSmem);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)blocks, threads, smem, s>>>(a);
+    KERNEL<<<(unsigned)blocks, C::kThreads, C::kSmem, s>>>(a);
     return cudaGetLastError();
 }
 
@@ -1128,24 +1162,16 @@ using Fwd128 = FwdShape<128, 128, 4>;
 using Grad64 = GradShape<64>;
 using Grad128 = GradShape<128>;
 
-// A register split draws on what the block is launched with: a build whose
-// kernel got fewer registers must not run it (its threads would wait forever).
 template <class C>
-bool registers_cover(const void *kernel) {
-    cudaFuncAttributes f;
-    if (cudaFuncGetAttributes(&f, kernel) != cudaSuccess) {
-        cudaGetLastError();
-        return false;
-    }
-    return f.numRegs * C::kThreads >= 128 * (C::kThreads / 128 - 1) * C::kRegsRow + 128 * C::kRegsOther;
+cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
+    return launch_tiles<C, attention_forward_kernel<C>>(a, (int)(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows)), a.hq, s);
 }
 
 template <class C>
-cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
-    static const bool covered = registers_cover<C>(reinterpret_cast<const void *>(attention_forward_kernel<C>));
-    if (!covered) return cudaErrorLaunchOutOfResources;
-    return launch_tiles(attention_forward_kernel<C>, a, (int)(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows)), a.hq, C::kThreads,
-                        C::kSmem, s);
+dpb_status launch_attention_backward(AttnArgs &a, cudaStream_t s) {
+    const int qt = (int)(((int64_t)a.max_q + kRows - 1) / kRows), kt = (int)(((int64_t)a.max_k + kRows - 1) / kRows);
+    DPB_CHECK(launch_status(launch_tiles<C, attention_grad_q_kernel<C>>(a, qt, a.hq, s), "attention_backward (queries)"));
+    return launch_status(launch_tiles<C, attention_grad_kv_kernel<C>>(a, kt, a.hkv, s), "attention_backward (keys)");
 }
 
 }  // namespace
@@ -1221,15 +1247,7 @@ dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_hea
     DPB_CHECK(make_map(&a.g, grad_o, cfg->total_q, cfg->heads_q, D, kRows));
     DPB_CHECK(make_map(&a.k, k, cfg->total_k, cfg->heads_kv, D, kRows));
     DPB_CHECK(make_map(&a.v, v, cfg->total_k, cfg->heads_kv, D, kRows));
-    const int qt = (int)(((int64_t)cfg->max_q + kRows - 1) / kRows), kt = (int)(((int64_t)cfg->max_k + kRows - 1) / kRows);
-    DPB_CHECK(launch_status(
-        small ? launch_tiles(attention_grad_q_kernel<Grad64>, a, qt, a.hq, Grad64::kThreads, Grad64::kSmem, s)
-              : launch_tiles(attention_grad_q_kernel<Grad128>, a, qt, a.hq, Grad128::kThreads, Grad128::kSmem, s),
-        "attention_backward (queries)"));
-    return launch_status(
-        small ? launch_tiles(attention_grad_kv_kernel<Grad64>, a, kt, a.hkv, Grad64::kThreads, Grad64::kSmem, s)
-              : launch_tiles(attention_grad_kv_kernel<Grad128>, a, kt, a.hkv, Grad128::kThreads, Grad128::kSmem, s),
-        "attention_backward (keys and values)");
+    return small ? launch_attention_backward<Grad64>(a, s) : launch_attention_backward<Grad128>(a, s);
 }
 
 }  // extern "C"

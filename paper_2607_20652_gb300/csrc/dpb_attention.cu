@@ -102,16 +102,25 @@ __device__ __forceinline__ void zero_rows(uint8_t *tile, int from, int rows) {
 }
 
 // The ring of slots that the copying warp fills and the products empty. Tile i
-// uses slot i % N for the (i / N)-th time.
-template <int N, int BYTES>
+// uses one of N slots for the (i / N)-th time: slot i % N, or with SWAP (four
+// slots, tiles in pairs) pairs take turns on two slots each and exchange them
+// within the pair from one turn to the next: of a pair, the second tile is
+// done with first, so the first tile of the pair two further on, which is
+// wanted first, gets its slot.
+template <int N, int BYTES, bool SWAP = false>
 struct Ring {
+    static_assert(!SWAP || N == 4, "pairs of tiles in four slots");
     uint8_t *data;
     uint32_t full, empty, tail;  // full[N], empty[N], tail
-    __device__ __forceinline__ uint32_t full_bar(int i) const { return full + 8 * (i % N); }
-    __device__ __forceinline__ uint32_t empty_bar(int i) const { return empty + 8 * (i % N); }
+    __device__ __forceinline__ int index(int i) const {
+        if (SWAP) return (i & 2) | ((i ^ (i >> 2)) & 1);
+        return i % N;
+    }
+    __device__ __forceinline__ uint32_t full_bar(int i) const { return full + 8 * index(i); }
+    __device__ __forceinline__ uint32_t empty_bar(int i) const { return empty + 8 * index(i); }
     __device__ __forceinline__ uint32_t parity(int i) const { return (i / N) & 1; }
     __device__ __forceinline__ bool wait_full(int i) const { return bar_wait(full_bar(i), parity(i), kTries); }
-    __device__ __forceinline__ uint8_t *slot(int i) const { return data + (i % N) * BYTES; }
+    __device__ __forceinline__ uint8_t *slot(int i) const { return data + index(i) * BYTES; }
     __device__ __forceinline__ uint32_t addr(int i) const { return smem_addr(slot(i)); }
     // All lanes: slot i is free (its previous products are done).
     __device__ __forceinline__ bool wait_free(int i) const {
@@ -539,7 +548,7 @@ struct GradShape {
     static constexpr int kBars = 1 + 2 * NS + 1 + 8;
     static constexpr int kVec = 8 * 128 * 4;  // a warp's lse and delta of its 64 columns
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + 8 * kBars + 16;
-    using Slots = Ring<NS, kTile>;
+    using Slots = Ring<NS, kTile, NS == 4>;
 };
 
 // d = a b^T of two tiles in shared memory (K = DP).
@@ -880,6 +889,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 if (failed) break;
                 fence_after();
                 sum_product<DP>(tmem + kColV, tmem + C::kColS, 64, ring.addr(2 * it + 1), it > 0);
+                mma_commit(ring.empty_bar(2 * it + 1));
                 if (more && !scores(it + 1)) failed = true;
                 if (failed || !bar_wait(bars.w_full, it & 1, kTries)) {
                     failed = true;
@@ -888,7 +898,6 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 fence_after();
                 sum_product<DP>(tmem + kColK, tmem + C::kColG, 64, ring.addr(2 * it), it > 0);
                 mma_commit(ring.empty_bar(2 * it));
-                mma_commit(ring.empty_bar(2 * it + 1));
                 if (more && !grads(it + 1)) failed = true;
             }
             mma_commit(bars.done);

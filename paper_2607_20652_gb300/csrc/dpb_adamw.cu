@@ -50,7 +50,7 @@ struct Table {
 };
 
 struct Hyper {
-    float lr, b1, c1, b2, c2, eps, decay, fix1, fix2;
+    float rate, b1, c1, b2, c2, eps, decay, fix2;  // rate: lr / (1 - beta1^step); fix2: (1 - beta2^step)^-1/2
     uint32_t key;
     const float *grad_scale;
 };
@@ -102,10 +102,20 @@ __device__ __forceinline__ F2 operator+(F2 a, F2 b) {
 __device__ __forceinline__ float round_normal(float y, uint32_t r20) {
     return __uint_as_float((__float_as_uint(y) + r20) & 0xfff00000u);
 }
-// Below 2^-6 the codes are multiples of 2^-9.
+// Below 2^-6 the codes are multiples of 2^-9. A NaN stays one.
 __device__ __forceinline__ float round_small(float y, uint32_t r20) {
     const float t = __fadd_rn(fabsf(y) * 512.f, (float)(r20 >> 4) * (1.f / 65536.f));
     return copysignf(floorf(t) * (1.f / 512.f), y);
+}
+
+__device__ __forceinline__ float round_any(float y, uint32_t r20) {
+    return fabsf(y) >= 0.015625f ? round_normal(y, r20) : round_small(y, r20);
+}
+// The smaller of two; a NaN if either is one.
+__device__ __forceinline__ float min_or_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -265,7 +275,7 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
 #pragma unroll
         for (int e = i; e < i + 2; ++e) {
             const float root = __fsqrt_rn(v[e]);
-            p[e] = p[e] * h.decay - h.lr * m[e] * rcp_approx(root * h.fix2 + h.eps);
+            p[e] = p[e] * h.decay - h.rate * m[e] * rcp_approx(root * h.fix2 + h.eps);
             if (F8) {
                 v[e] = root;
                 tm = fmaxf(tm, fabsf(m[e]));
@@ -287,12 +297,12 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
             const float2 m2 = (F2(m[i], m[i + 1]) * F2(im, im)).get(), v2 = (F2(v[i], v[i + 1]) * F2(iv, iv)).get();
             m[i] = m2.x, m[i + 1] = m2.y;
             v[i] = v2.x, v[i + 1] = v2.y;
-            low = fminf(low, fminf(fminf(fabsf(m2.x), fabsf(m2.y)), fminf(v2.x, v2.y)));
+            low = min_or_nan(low, min_or_nan(min_or_nan(fabsf(m2.x), fabsf(m2.y)), min_or_nan(v2.x, v2.y)));
         }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) r[i] = mix32((uint32_t)(at + i) ^ key);
-        // magnitudes below the normal codes are rare (under 2^-6 / 448 of the
-        // block's largest): one test for all of the lane's values
+        // magnitudes below the normal codes (under 2^-6 / 448 of the block's
+        // largest) and NaNs are rare: one test for all of the lane's values
         if (low >= 0.015625f) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -303,8 +313,8 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const uint32_t rm = (r[i] << 4) & 0xffff0u, rv = (r[i] >> 12) & 0xffff0u;
-                m[i] = fabsf(m[i]) < 0.015625f ? round_small(m[i], rm) : round_normal(m[i], rm);
-                const float y = v[i], q = y < 0.015625f ? round_small(y, rv) : round_normal(y, rv);
+                m[i] = round_any(m[i], rm);
+                const float y = v[i], q = round_any(y, rv);
                 v[i] = y > 0.f ? fmaxf(q, 1.f / 512.f) : q;  // 2^-9, the smallest code
             }
         }
@@ -430,14 +440,13 @@ extern "C" dpb_status dpb_adamw_step(const dpb_adamw_config *cfg, const dpb_adam
     DPB_CHECK(check_adamw(cfg, tensors, n));
     if (n == 0) return DPB_OK;
     Hyper h;
-    h.lr = (float)cfg->lr;
+    h.rate = (float)(cfg->lr / (1.0 - std::pow(cfg->beta1, (double)cfg->step)));
     h.b1 = (float)cfg->beta1;
     h.c1 = (float)(1.0 - cfg->beta1);
     h.b2 = (float)cfg->beta2;
     h.c2 = (float)(1.0 - cfg->beta2);
     h.eps = (float)cfg->eps;
     h.decay = (float)(1.0 - cfg->lr * cfg->weight_decay);
-    h.fix1 = (float)(1.0 / (1.0 - std::pow(cfg->beta1, (double)cfg->step)));
     h.fix2 = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, (double)cfg->step)));
     h.key = mix32((uint32_t)cfg->seed ^
                   mix32((uint32_t)cfg->step + 0x9e3779b9u * (1u + (uint32_t)(cfg->seed >> 32))));

@@ -1125,7 +1125,11 @@ def run_transformer(args, world, rank, local):
         torch.manual_seed(0)
         m = transformer.ParityTransformer(layers=c["layers"], d=c["d"], heads=c["heads"], d_mlp=c["d_mlp"],
                                           vocab=c["vocab"], context=c["context"],
-                                          dpb=dpb_kw if with_dpb else None, device=device)
+                                          dpb=dpb_kw if with_dpb else None, device=device,
+                                          attention="dpb" if args.own_step else "torch")
+        if args.own_step:
+            from paper_2607_20652_gb300 import optim
+            return m, optim.AdamW(m.parameters(), lr=1e-4, state_bits=args.state_bits)
         return m, torch.optim.AdamW(m.parameters(), lr=1e-4, fused=True)
 
     def measure(model, opt, dpbs):
@@ -1164,6 +1168,7 @@ def run_transformer(args, world, rank, local):
     from paper_2607_20652_gb300 import dpb as _dpb
     for layer in model.dpb_layers():
         status |= _dpb.workspace_status(layer._ws)
+    status |= _dpb.status(device)
     del model, opt
     torch.cuda.empty_cache()
     dense_ms = None
@@ -1174,6 +1179,7 @@ def run_transformer(args, world, rank, local):
     tokens = B * S
     dpb_ms = parts["forward"] + parts["backward"]
     per_layer = (3 + (4 if args.standardise else 0))
+    own_launches = (6 * c["layers"] + 1) * args.steps if args.own_step else 0  # rope 1 + 2, attention 1 + 2; one AdamW
     line = {
         "metric": "ParityTransformer GPT-2-small training step (fwd + bwd + AdamW), tokens/s; DPB share of the step",
         "value": round(whole_job_rate(tokens, world, 1, ms / 1e3), 1), "unit": "tokens/s", "n_gpus": world,
@@ -1182,12 +1188,14 @@ def run_transformer(args, world, rank, local):
         "config": {"workload": "gpt2small", **c, "tokens_per_step": tokens,
                    "dpb": {**GPT2_DPB, "placement": "before every MLP input (§3)",
                            "standardise": bool(args.standardise)},
-                   "weights": "random init (std 0.02), bf16; AdamW fused", "parallelism": f"dp{world}"},
+                   "weights": "random init (std 0.02), bf16; " + (
+                       f"this library's attention (normalised, rotated queries and keys) and AdamW, {args.state_bits}-bit "
+                       "states" if args.own_step else "AdamW fused"), "parallelism": f"dp{world}"},
         "dpb_ms_per_step": {"forward": round(parts["forward"], 4), "backward": round(parts["backward"], 4),
                             "total": round(dpb_ms, 4)},
         "dpb_share": round(dpb_ms / ms, 4),
         "dense_ms_per_step": round(dense_ms, 4) if dense_ms else None,
-        "loss": round(loss, 4), "gpu_launches": per_layer * c["layers"] * args.steps, "device_status": status,
+        "loss": round(loss, 4), "gpu_launches": per_layer * c["layers"] * args.steps + own_launches, "device_status": status,
     }
     if rank == 0:
         print(json.dumps(line), flush=True)
@@ -1218,6 +1226,9 @@ def main(argv=None):
                     help="chunks of the batch in the host-buffer run (copies overlap kernels across streams)")
     ap.add_argument("--standardise", action="store_true",
                     help="live standardisation tables and the per-step EMA update in the timed step")
+    ap.add_argument("--own-step", action="store_true",
+                    help="gpt2small: this library's attention and AdamW in place of PyTorch's")
+    ap.add_argument("--state-bits", type=int, choices=[32, 8], default=32, help="gpt2small --own-step: AdamW's states")
     ap.add_argument("--no-dense", action="store_true", help="gpt2small: skip the dense model of the same shape")
     ap.add_argument("--workload", default=WORKLOAD,
                     choices=[WORKLOAD, "tiny", "gpt2", "paper3l", "paper2l", "gpt2small", "sweep"],

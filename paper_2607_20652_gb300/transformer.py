@@ -4,9 +4,10 @@
 embedding and unembedding, RMSNorm in place of LayerNorm) with a Deep Parity
 Bottleneck inserted before the input of every MLP. Weights are random
 (nothing here is trained); attention and the dense layers are PyTorch's own
-(cuBLAS / fused attention), the DPB layers are this library's kernels. The
-model exists to measure the DPB's share of a forward + backward + optimiser
-step at the paper's scale; it is not a training recipe.
+(cuBLAS / fused attention), the DPB layers are this library's kernels;
+``attention="dpb"`` takes this library's attention as well. The model exists
+to measure the DPB's share of a forward + backward + optimiser step at the
+paper's scale; it is not a training recipe.
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ import torch
 import torch.nn.functional as F
 from torch import nn
 
+from .attention import Attention
 from .layer import DPBLayer
 
 
@@ -35,10 +37,10 @@ class _Attention(nn.Module):
 
 
 class _Block(nn.Module):
-    def __init__(self, d: int, heads: int, d_mlp: int, dpb: Optional[DPBLayer]):
+    def __init__(self, d: int, heads: int, d_mlp: int, dpb: Optional[DPBLayer], attn: nn.Module):
         super().__init__()
         self.n1 = nn.RMSNorm(d)
-        self.attn = _Attention(d, heads)
+        self.attn = attn
         self.n2 = nn.RMSNorm(d)
         self.dpb = dpb
         self.up = nn.Linear(d, d_mlp, bias=False)
@@ -55,17 +57,26 @@ class _Block(nn.Module):
 class ParityTransformer(nn.Module):
     """GPT-2 shape (12 layers, d = 768, 12 heads, MLP 3072, vocab 50257,
     context 1024 by default) with a DPB before every MLP; ``dpb=None`` gives
-    the dense model of the same shape. ``dpb`` holds DPBLayer arguments."""
+    the dense model of the same shape. ``dpb`` holds DPBLayer arguments.
+    ``attention="dpb"`` uses this library's attention, with normalised queries
+    and keys and rotary positions in place of the learned ones (bf16;
+    ``kv_heads`` key and value heads)."""
 
     def __init__(self, layers: int = 12, d: int = 768, heads: int = 12, d_mlp: int = 3072, vocab: int = 50257,
-                 context: int = 1024, dpb: Optional[dict] = None, device=None, dtype=torch.bfloat16):
+                 context: int = 1024, dpb: Optional[dict] = None, device=None, dtype=torch.bfloat16,
+                 attention: str = "torch", kv_heads: Optional[int] = None):
         super().__init__()
+        if attention not in ("torch", "dpb"):
+            raise ValueError(f"attention must be 'torch' or 'dpb', got {attention!r}")
+        if attention == "torch" and kv_heads not in (None, heads):
+            raise ValueError("kv_heads needs attention='dpb'")
         self.tok = nn.Embedding(vocab, d)
-        self.pos = nn.Embedding(context, d)
+        self.pos = nn.Embedding(context, d) if attention == "torch" else None
         blocks = []
         for i in range(layers):
             layer = DPBLayer(seed=i, device=device, d=d, **dpb) if dpb is not None else None
-            blocks.append(_Block(d, heads, d_mlp, layer))
+            attn = _Attention(d, heads) if attention == "torch" else Attention(d, heads, kv_heads, context=context)
+            blocks.append(_Block(d, heads, d_mlp, layer, attn))
         self.blocks = nn.ModuleList(blocks)
         self.norm = nn.RMSNorm(d)
         std = 0.02
@@ -84,7 +95,9 @@ class ParityTransformer(nn.Module):
 
     def forward(self, ids, targets=None):
         B, S = ids.shape
-        x = self.tok(ids) + self.pos(torch.arange(S, device=ids.device))
+        x = self.tok(ids)
+        if self.pos is not None:
+            x = x + self.pos(torch.arange(S, device=ids.device))
         for b in self.blocks:
             x = b(x)
         logits = F.linear(self.norm(x), self.tok.weight)  # tied unembedding

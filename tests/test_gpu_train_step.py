@@ -1,0 +1,156 @@
+"""The training step's operators together: the autograd functions, the
+attention module, the optimiser and the ParityTransformer built from them."""
+import copy
+
+import numpy as np
+import pytest
+import torch
+import torch.nn.functional as F
+
+from paper_2607_20652_gb300 import build, dpb
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _library():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    build.build()
+    dpb.load()
+
+
+def plain(m, x, cu):
+    """The module in 64 bits on packed rows."""
+    w = {n: p.detach().double() for n, p in m.named_parameters()}
+    qkv = (x @ w["qkv.weight"].T).view(-1, m.heads + 2 * m.kv_heads, m.dim)
+    out = []
+    for a, b in zip(cu[:-1], cu[1:]):
+        q, k, v = qkv[a:b].split([m.heads, m.kv_heads, m.kv_heads], 1)
+        if m.q_norm is not None:
+            q, k = (t * torch.rsqrt(t.square().mean(-1, keepdim=True) + 1e-6) * w[n] for t, n in ((q, "q_norm"), (k, "k_norm")))
+        if m.cos is not None:
+            c, s = (t[:b - a].double()[:, None] for t in (m.cos, m.sin))
+            h = m.dim // 2
+            q, k = (torch.cat([t[..., :h] * c - t[..., h:] * s, t[..., h:] * c + t[..., :h] * s], -1) for t in (q, k))
+        k, v = (t.repeat_interleave(m.heads // m.kv_heads, 1) for t in (k, v))
+        s = torch.einsum("ihd,jhd->hij", q, k) * m.dim ** -0.5
+        s = s.masked_fill(torch.ones(b - a, b - a, dtype=torch.bool, device=s.device).triu(1), -torch.inf)
+        out.append(torch.einsum("hij,jhd->ihd", torch.softmax(s, -1), v))
+    return torch.cat(out).flatten(1) @ w["out.weight"].T
+
+
+@pytest.mark.parametrize("kv,qk_norm,rotary", [(4, True, True), (2, True, False), (1, False, True), (4, False, False)])
+def test_module_and_its_gradients(kv, qk_norm, rotary):
+    from paper_2607_20652_gb300.attention import Attention
+    torch.manual_seed(0)
+    m = Attention(256, 4, kv, qk_norm, rotary, context=128, device="cuda", dtype=torch.bfloat16)
+    assert m.cos is None or m.cos.dtype == torch.float32
+    x = torch.randn(3, 100, 256, device="cuda").bfloat16().requires_grad_()
+    gy = torch.randn(3, 100, 256, device="cuda").bfloat16()
+    y = m(x)
+    y.backward(gy)
+    xd = x.detach().double().view(-1, 256).requires_grad_()
+    want = plain(m, xd, [0, 100, 200, 300])
+    want.backward(gy.double().view(-1, 256))
+    # bf16 throughout: the projections' outputs, q and k after their norm, P, dS and every gradient are each rounded by
+    # at most 2^-8; independent, about ten of them in a row stay within ten times that
+    assert float((y.double().view(-1, 256) - want).norm() / want.norm()) < 10 * 2.0 ** -8
+    assert float((x.grad.double().view(-1, 256) - xd.grad).norm() / xd.grad.norm()) < 10 * 2.0 ** -8
+    assert all(torch.isfinite(p.grad).all() and p.grad.any() for p in m.parameters())
+    assert dpb.status() == 0
+
+
+def test_packed_rows_equal_the_batch():
+    from paper_2607_20652_gb300.attention import Attention
+    torch.manual_seed(1)
+    m = Attention(128, 2, device="cuda", dtype=torch.bfloat16, context=64)
+    x = torch.randn(2, 50, 128, device="cuda").bfloat16()
+    cu = torch.tensor([0, 50, 100], dtype=torch.int32, device="cuda")
+    assert torch.equal(m(x).view(100, 128), m(x.view(100, 128), cu, 50))
+    with pytest.raises(ValueError):
+        m(torch.randn(1, 65, 128, device="cuda").bfloat16())
+
+
+def test_functions_match_the_calls():
+    from paper_2607_20652_gb300 import attention as A
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v = (torch.randn(90, h, 64, device="cuda", generator=g).bfloat16().requires_grad_() for h in (4, 2, 2))
+    w = torch.rand(64, device="cuda", generator=g).bfloat16().requires_grad_()
+    cos, sin = dpb.rope_tables(90, 64)
+    qr, kr = A.qk_norm_rope(q, k, w, w, cos, sin)
+    o = A.attention(qr, kr, v)
+    go = torch.randn(90, 4, 64, device="cuda", generator=g).bfloat16()
+    o.backward(go)
+    q1, k1 = dpb.qk_norm_rope(q.detach(), k.detach(), w.detach(), w.detach(), cos, sin)
+    o1, lse = dpb.attention_forward(q1, k1, v.detach())
+    dq, dk, dv = dpb.attention_backward(q1, k1, v.detach(), o1, lse, go)
+    dq, dk, dwq, dwk = dpb.qk_norm_rope_backward(q.detach(), k.detach(), dq, dk, w.detach(), w.detach(), cos, sin)
+    assert torch.equal(o, o1) and torch.equal(v.grad, dv) and torch.equal(q.grad, dq) and torch.equal(k.grad, dk)
+    assert torch.equal(w.grad, dwq.bfloat16() + dwk.bfloat16())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_optimiser_follows_torch(bits):
+    """Ten steps beside torch's AdamW on the same gradients; one parameter joins late. 32-bit states: fp32 rounding only.
+    8-bit states: a moment is off by at most a sixteenth each step, so a step by less than a fifth."""
+    from paper_2607_20652_gb300.optim import AdamW
+    torch.manual_seed(3)
+    a = [torch.nn.Parameter(torch.randn(s, device="cuda")) for s in ((300, 7), (513,), (64, 64))]
+    b = [torch.nn.Parameter(p.detach().clone()) for p in a]
+    kw = dict(lr=1e-2, betas=(0.9, 0.95), weight_decay=0.1)
+    mine, ref = AdamW(a, state_bits=bits, **kw), torch.optim.AdamW(b, **kw)
+    for s in range(10):
+        for p, r in zip(a, b):
+            g = torch.randn_like(p) + 1
+            p.grad, r.grad = (g, g.clone()) if s >= 2 or p is not a[1] else (None, None)
+        mine.step()
+        ref.step()
+    for p, r in zip(a, b):
+        tol = 1e-5 if bits == 32 else 0.2 * 10 * 1e-2
+        assert float((p - r).abs().max()) < tol
+    # states as torch's keep them, and a run that goes on from a saved state goes on the same
+    keep = copy.deepcopy(mine.state_dict())
+    c = [torch.nn.Parameter(p.detach().clone()) for p in a]
+    other = AdamW(c, state_bits=bits, **kw)
+    other.load_state_dict(keep)
+    for p, q in zip(a, c):
+        p.grad = torch.ones_like(p)
+        q.grad = torch.ones_like(q)
+    mine.step()
+    other.step()
+    assert all(torch.equal(p, q) for p, q in zip(a, c))
+
+
+@pytest.mark.parametrize("bits,kv", [(32, 4), (8, 2)])
+def test_small_parity_transformer_trains(bits, kv):
+    from paper_2607_20652_gb300.optim import AdamW
+    from paper_2607_20652_gb300.transformer import ParityTransformer
+    dev = torch.device("cuda")
+    torch.manual_seed(0)
+    model = ParityTransformer(layers=2, d=64, heads=4, d_mlp=128, vocab=97, context=32, attention="dpb", kv_heads=kv,
+                              dpb=dict(levels=3, m_bits=12, children=16, beam=8, k=8), device=dev)
+    opt = AdamW(model.parameters(), lr=3e-3, state_bits=bits)
+    g = torch.Generator().manual_seed(1)
+    ids = torch.randint(0, 97, (4, 32), generator=g).to(dev)
+    tgt = torch.randint(0, 97, (4, 32), generator=g).to(dev)
+    losses = []
+    for _ in range(30):
+        opt.zero_grad(set_to_none=True)
+        loss = model(ids, tgt)
+        loss.backward()
+        assert all(p.grad is None or torch.isfinite(p.grad).all() for p in model.parameters())
+        opt.step()
+        losses.append(float(loss.detach()))
+    assert np.isfinite(losses).all() and losses[-1] < losses[0] - 0.5, losses
+    assert dpb.status() == 0
+
+
+def test_default_model_is_as_before():
+    from paper_2607_20652_gb300.transformer import ParityTransformer
+    torch.manual_seed(0)
+    m = ParityTransformer(layers=1, d=64, heads=4, d_mlp=128, vocab=97, context=32, device="cuda")
+    assert m.pos is not None and [n for n, _ in m.blocks[0].attn.named_parameters()] == ["qkv.weight", "out.weight"]
+    for kw in (dict(attention="other"), dict(kv_heads=2)):
+        with pytest.raises(ValueError):
+            ParityTransformer(layers=1, d=64, heads=4, d_mlp=128, vocab=97, context=32, **kw)

@@ -67,20 +67,29 @@ struct AttnArgs {
     int32_t *status;
 };
 
-// One sequence: its tokens [q0, q0 + n) and [k0, k0 + m).
+// One sequence: its tokens [q0, q0 + n) and [k0, k0 + m). Loading its offsets
+// and looking at them are apart, so that a block's set-up runs meanwhile.
+struct Offsets {
+    int64_t q0, q1, k0, k1;
+};
 struct Seq {
     int q0, n, k0, m;
     bool ok;
 };
 
-__device__ __forceinline__ Seq sequence(const AttnArgs &a, int s) {
-    int64_t q0 = 0, q1 = a.total_q, k0 = 0, k1 = a.total_k;
-    if (a.cu_q) q0 = a.cu_q[s], q1 = a.cu_q[s + 1];
-    if (a.cu_k) k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
+__device__ __forceinline__ Offsets load_offsets(const AttnArgs &a, int s) {
+    Offsets r{0, a.total_q, 0, a.total_k};
+    if (a.cu_q) {
+        r.q0 = __ldg(a.cu_q + s), r.q1 = __ldg(a.cu_q + s + 1);
+        r.k0 = __ldg(a.cu_k + s), r.k1 = __ldg(a.cu_k + s + 1);
+    }
+    return r;
+}
+__device__ __forceinline__ Seq sequence(const AttnArgs &a, const Offsets &o) {
     Seq r;
-    r.ok = q0 >= 0 && q1 >= q0 && q1 <= a.total_q && k0 >= 0 && k1 >= k0 && k1 <= a.total_k && q1 - q0 <= a.max_q &&
-           k1 - k0 <= a.max_k;
-    r.q0 = (int)q0, r.n = (int)(q1 - q0), r.k0 = (int)k0, r.m = (int)(k1 - k0);
+    r.ok = o.q0 >= 0 && o.q1 >= o.q0 && o.q1 <= a.total_q && o.k0 >= 0 && o.k1 >= o.k0 && o.k1 <= a.total_k &&
+           o.q1 - o.q0 <= a.max_q && o.k1 - o.k0 <= a.max_k;
+    r.q0 = (int)o.q0, r.n = (int)(o.q1 - o.q0), r.k0 = (int)o.k0, r.m = (int)(o.k1 - o.k0);
     return r;
 }
 
@@ -132,16 +141,15 @@ struct Ring {
     template <int DP>
     __device__ __forceinline__ bool fill(int i, const CUtensorMap *map, int head, int token, int rows, int live,
                                          bool sums, int &tails) const {
-        const bool leader = (threadIdx.x & 31) == 0;
         if (!sums || live >= rows) {
-            if (leader) {
+            if (elect_one()) {
                 bar_arrive_expect(full_bar(i), BYTES);
                 copy_tile<DP>(addr(i), map, head, token, rows, full_bar(i));
             }
             __syncwarp();
             return true;
         }
-        if (leader) {
+        if (elect_one()) {
             bar_arrive_expect(tail, BYTES);
             copy_tile<DP>(addr(i), map, head, token, rows, tail);
         }
@@ -152,7 +160,7 @@ struct Ring {
         zero_rows<DP>(slot(i), live, rows);
         fence_async_shared();
         __syncwarp();
-        if (leader) bar_arrive(full_bar(i));
+        if (elect_one()) bar_arrive(full_bar(i));
         __syncwarp();
         return true;
     }
@@ -177,30 +185,37 @@ __device__ __forceinline__ void write_rows(uint32_t tmem, uint8_t *stage, const 
                                            int rows, int col, int D, float f) {
     const int lane = threadIdx.x & 31;
     constexpr int kPieces = COLS / 8, kSwap = kPieces < 8 ? kPieces - 1 : 7;
+    uint32_t v[COLS / 32][32];
 #pragma unroll
-    for (int c = 0; c < COLS; c += 32) {
-        uint32_t v[32];
-        tmem_load(tmem + c, v);
-        load_wait(v);
+    for (int c = 0; c < COLS / 32; ++c) tmem_load(tmem + 32 * c, v[c]);
+#pragma unroll
+    for (int c = 0; c < COLS / 32; ++c) {
+        load_wait(v[c]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t u[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                u[e] = pack_bf16(__uint_as_float(v[8 * i + 2 * e]) * f, __uint_as_float(v[8 * i + 2 * e + 1]) * f);
-            *reinterpret_cast<uint4 *>(stage + lane * COLS * 2 + (((c / 8 + i) ^ (lane & kSwap)) * 16)) =
+                u[e] = pack_bf16(__uint_as_float(v[c][8 * i + 2 * e]) * f, __uint_as_float(v[c][8 * i + 2 * e + 1]) * f);
+            *reinterpret_cast<uint4 *>(stage + lane * COLS * 2 + (((4 * c + i) ^ (lane & kSwap)) * 16)) =
                 make_uint4(u[0], u[1], u[2], u[3]);
         }
     }
     __syncwarp();
-    bf16 *base = out.p + token * out.ts + head * out.hs + col;
-#pragma unroll 4
-    for (int i = lane; i < 32 * kPieces; i += 32) {
-        const int r = i / kPieces, piece = i % kPieces;
-        if (r < rows && col + piece * 8 < D)
-            *reinterpret_cast<uint4 *>(base + r * out.ts + piece * 8) =
-                *reinterpret_cast<const uint4 *>(stage + r * COLS * 2 + ((piece ^ (r & kSwap)) * 16));
+    // piece `lane % kPieces` of rows lane / kPieces, + 32 / kPieces, ...
+    const int piece = lane % kPieces, r0 = lane / kPieces;
+    uint4 x[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int r = r0 + i * (32 / kPieces);
+        x[i] = *reinterpret_cast<const uint4 *>(stage + r * COLS * 2 + ((piece ^ (r & kSwap)) * 16));
     }
+    bf16 *at = out.p + (token + r0) * out.ts + head * out.hs + col + piece * 8;
+    const int64_t step = 32 / kPieces * out.ts;
+    if (col + piece * 8 < D)
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+            if (r0 + i * (32 / kPieces) < rows) *reinterpret_cast<uint4 *>(at + i * step) = x[i];
 }
 
 // The block's set-up: the copying warp makes the barriers and goes on at once
@@ -226,7 +241,7 @@ struct FwdShape {
     static constexpr int kTile = kRows * DP * 2, kSlot = BN * DP * 2;
     static constexpr int kColumns = 512;
     static constexpr int kColO = 2 * BN, kColP = kOwnP ? 2 * (BN + DP) : 0, kStepP = kOwnP ? BN / 2 : BN;
-    static constexpr int kBars = 1 + 2 * NS + 1 + 2 * 6 + 1;
+    static constexpr int kBars = 2 + 2 * NS + 1 + 2 * 6 + 1;
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kSlot + 8 * kBars + 16;
     static constexpr int kThreads = 384;  // two softmax warpgroups, one of the copying and the issuing warp
     // registers of a softmax thread and of the others: 256 x 216 + 128 x 72 = 384 x 168
@@ -255,53 +270,58 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
     // the longest rows first; the heads of a group side by side
     const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
     const int si = rest % a.seqs, rows2 = a.tiles - 1 - rest / a.seqs;
-    const Seq q = sequence(a, si);
+    const Offsets offsets = load_offsets(a, si);
+
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * C::kTile + C::NS * C::kSlot);
+    const uint32_t bar0 = smem_addr(bars);
+    const uint32_t q_full = bar0;  // of each tile
+    Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 16, bar0 + 16 + 8 * C::NS, bar0 + 16 + 16 * C::NS};
+    // per tile: S is there, each half of P is there, S has been read, P's
+    // product is done, O is done
+    const uint32_t s_full = bar0 + 8 * (3 + 2 * C::NS), p_full = s_full + 16, s_read = p_full + 32,
+                   p_done = s_read + 16, o_full = p_done + 16, done = o_full + 16;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
+    if (warp == kCopier) {
+        for (int i = lane; i < C::kBars; i += 32) {
+            const uint32_t b = bar0 + 8 * i;
+            bar_init(b, b >= p_full && b < p_done ? 4 : b == done && kValues != kScores ? 2 : 1);
+        }
+        bar_init_fence();
+        __syncwarp();
+    }
+
+    const Seq q = sequence(a, offsets);
     if (!q.ok) {
         if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
         return;
     }
     if (rows2 * 2 * kRows >= q.n) return;
-
     const int nb0 = tile_blocks<BN>(a, q, 2 * rows2), nb1 = tile_blocks<BN>(a, q, 2 * rows2 + 1);
     const int blocks = max(nb0, nb1);
-
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * C::kTile + C::NS * C::kSlot);
-    const uint32_t bar0 = smem_addr(bars);
-    const uint32_t q_full = bar0;
-    Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 8, bar0 + 8 + 8 * C::NS, bar0 + 8 + 16 * C::NS};
-    // per tile: S is there, each half of P is there, S has been read, P's
-    // product is done, O is done
-    const uint32_t s_full = bar0 + 8 * (2 + 2 * C::NS), p_full = s_full + 16, s_read = p_full + 32,
-                   p_done = s_read + 16, o_full = p_done + 16, done = o_full + 16;
-    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
     bool failed = false;
 
     if (warp >= 8) {
         give_registers<C::kRegsOther>();
         if (warp == kCopier) {
-            // ---- copies: Q's tiles, then K_0, V_0, K_1, V_1, ...
-            for (int i = lane; i < C::kBars; i += 32) {
-                const uint32_t b = bar0 + 8 * i;
-                bar_init(b, b >= p_full && b < p_done ? 4 : b == done && kValues != kScores ? 2 : 1);
-            }
-            bar_init_fence();
-            __syncwarp();
-            setup_arrive<C::kThreads>();
+            // ---- copies: what the first products need first, then V_0, K_1, V_1, ...
             const int kv_head = head / a.group;
-            if (blocks > 0) {
-                if (lane == 0) {
-                    const int tiles = (2 * rows2 + 1) * kRows < q.n ? 2 : 1;
-                    bar_arrive_expect(q_full, tiles * C::kTile);
-                    for (int t = 0; t < tiles; ++t)
-                        copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * rows2 + t) * kRows,
-                                      kRows, q_full);
+            const int tiles = blocks == 0 ? 0 : (2 * rows2 + 1) * kRows < q.n ? 2 : 1;
+            auto queries = [&](int t) {
+                if (t < tiles && elect_one()) {
+                    bar_arrive_expect(q_full + 8 * t, C::kTile);
+                    copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * rows2 + t) * kRows, kRows,
+                                  q_full + 8 * t);
                 }
                 __syncwarp();
-            }
+            };
             int issued = 0, tails = 0;
+            queries(0);
+            if (blocks > 0) failed = !ring.template fill<DP>(issued++, &a.k, kv_head, q.k0, BN, BN, false, tails);
+            queries(1);
+            setup_arrive<C::kThreads>();
             for (int j = 0; j < blocks && !failed; ++j) {
                 const int live = q.m - j * BN;
-                for (int kind = 0; kind < 2 && !failed; ++kind) {
+                for (int kind = j == 0; kind < 2 && !failed; ++kind) {  // K_0 is under way
                     failed = !ring.wait_free(issued) ||
                              !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN, live,
                                                      kind == 1, tails);
@@ -310,7 +330,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
             }
             if (failed) {
                 ring.drain(issued);
-                bar_wait(q_full, 0, kTries);
+                for (int t = 0; t < tiles; ++t) bar_wait(q_full + 8 * t, 0, kTries);
             }
         } else {
             if (warp == kScores) tmem_alloc(smem_addr(slot), C::kColumns);
@@ -343,13 +363,14 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
             };
             if (blocks > 0 && warp == kScores && elect_one()) {
                 // ---- scores; where P takes S's place, the values' products too
-                failed = !bar_wait(q_full, 0, kTries) || !ring.wait_full(0);
-                if (!failed) {
+                failed = !ring.wait_full(0);
+                for (int t = 0; t < 2 && !failed; ++t) {
+                    // a tile with rows is waited for, even where it has no block
+                    if ((2 * rows2 + t) * kRows < q.n) failed = !bar_wait(q_full + 8 * t, 0, kTries);
                     fence_after();
-                    for (int t = 0; t < 2; ++t)
-                        if ((t ? nb1 : nb0) > 0) scores(t, 0);
-                    mma_commit(ring.empty_bar(0));
+                    if (!failed && (t ? nb1 : nb0) > 0) scores(t, 0);
                 }
+                if (!failed) mma_commit(ring.empty_bar(0));
                 for (int j = 0; j < blocks && !failed; ++j) {
                     const bool more = j + 1 < blocks;
                     if (more && !ring.wait_full(2 * j + 2)) failed = true;
@@ -523,7 +544,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
                 write_zero_row(a.out.p + token * a.out.ts + head * a.out.hs, a.D);
             }
             if (live)
-                a.lse[(int64_t)head * a.total_q + token] = lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
+                a.lse[(int64_t)head * a.total_q + token] = lim > 0 ? (top + __log2f(sum)) * kLn2 : -INFINITY;
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
@@ -545,7 +566,7 @@ struct GradShape {
     static constexpr int kRegsRow = 208, kRegsOther = 88;           // 256 x 208 + 128 x 88 = 384 x 168
     static constexpr int kColS = 0, kColG = 128, kColSum = 256;  // S, the gradient of P, the sums
     static constexpr int kColumns = 512;
-    static constexpr int kBars = 1 + 2 * NS + 1 + 8;
+    static constexpr int kBars = 2 + 2 * NS + 1 + 8;
     static constexpr int kVec = 8 * 128 * 4;  // a warp's lse and delta of its 64 columns
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + 8 * kBars + 16;
     using Slots = Ring<NS, kTile, NS == 4>;
@@ -574,7 +595,7 @@ __device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t hal
 // What both gradient kernels set up: barriers (by the copying warp), TMEM.
 template <class C>
 struct GradBars {
-    // the tile is there; S and the gradient of P are there, have been read; dS
+    // each of the two tiles is there; S and the gradient of P are there, have been read; dS
     // (and P, for the keys' gradient) is there; dS's product is done; all is done
     uint32_t tile_full, s_full, g_full, w_done, done, s_read, g_read, w_full, v_full;
     typename C::Slots ring;
@@ -582,8 +603,8 @@ struct GradBars {
     __device__ __forceinline__ GradBars(uint8_t *smem) {
         uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (2 + C::NS) * C::kTile + C::kVec);
         tile_full = smem_addr(bars);
-        ring = {smem + 2 * C::kTile, tile_full + 8, tile_full + 8 + 8 * C::NS, tile_full + 8 + 16 * C::NS};
-        s_full = tile_full + 8 * (2 + 2 * C::NS);
+        ring = {smem + 2 * C::kTile, tile_full + 16, tile_full + 16 + 8 * C::NS, tile_full + 16 + 16 * C::NS};
+        s_full = tile_full + 8 * (3 + 2 * C::NS);
         g_full = s_full + 8;
         w_done = s_full + 16;
         done = s_full + 24;
@@ -614,7 +635,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
     const int si = rest % a.seqs, tile = a.tiles - 1 - rest / a.seqs;  // the longest rows first
-    const Seq q = sequence(a, si);
+    const Offsets offsets = load_offsets(a, si);
+    const GradBars<C> bars(smem);
+    if (warp == C::kCopier) bars.make();
+    const Seq q = sequence(a, offsets);
     if (!q.ok) {
         if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
         return;
@@ -622,24 +646,26 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
     const int i0 = tile * kRows;
     if (i0 >= q.n) return;
     const int blocks = tile_blocks<BN>(a, q, tile);
-    const GradBars<C> bars(smem);
     const auto &ring = bars.ring;
     bool failed = false;
 
     if (warp >= 8) give_registers<C::kRegsOther>();
     if (warp == C::kCopier) {
-        bars.make();
-        setup_arrive<C::kThreads>();
         const int kv_head = head / a.group;
-        if (blocks > 0 && lane == 0) {
-            bar_arrive_expect(bars.tile_full, 2 * C::kTile);
-            copy_tile<DP>(smem_addr(smem), &a.q, head, q.q0 + i0, kRows, bars.tile_full);
-            copy_tile<DP>(smem_addr(smem) + C::kTile, &a.g, head, q.q0 + i0, kRows, bars.tile_full);
-        }
-        __syncwarp();
+        auto rows = [&](const CUtensorMap *map, int t) {
+            if (blocks > 0 && elect_one()) {
+                bar_arrive_expect(bars.tile_full + 8 * t, C::kTile);
+                copy_tile<DP>(smem_addr(smem) + t * C::kTile, map, head, q.q0 + i0, kRows, bars.tile_full + 8 * t);
+            }
+            __syncwarp();
+        };
         int issued = 0, tails = 0;
+        rows(&a.q, 0);
+        if (blocks > 0) failed = !ring.template fill<DP>(issued++, &a.k, kv_head, q.k0, BN, q.m, true, tails);
+        rows(&a.g, 1);
+        setup_arrive<C::kThreads>();
         for (int j = 0; j < blocks && !failed; ++j)
-            for (int kind = 0; kind < 2 && !failed; ++kind) {
+            for (int kind = j == 0; kind < 2 && !failed; ++kind) {  // K_0 is under way
                 failed = !ring.wait_free(issued) ||
                          !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN,
                                                  q.m - j * BN, kind == 0, tails);
@@ -647,7 +673,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
             }
         if (failed) {
             ring.drain(issued);
-            bar_wait(bars.tile_full, 0, kTries);
+            if (blocks > 0)
+                for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
         }
     } else if (warp == C::kIssuer) {
         tmem_alloc(smem_addr(bars.slot), C::kColumns);
@@ -670,9 +697,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
             if (!failed) {
                 fence_after();
                 scores(0);
-                failed = !ring.wait_full(1);
             }
-            if (!failed) grads(0);
+            failed = !bar_wait(bars.tile_full + 8, 0, kTries) || failed || !ring.wait_full(1);
+            if (!failed) {
+                fence_after();
+                grads(0);
+            }
             for (int j = 0; j < blocks && !failed; ++j) {
                 if (j + 1 < blocks) {
                     // the next block's products, as soon as this one's have been read
@@ -709,20 +739,41 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
         const bool live = i < q.n;
         const int64_t token = q.q0 + (int64_t)i;
         const int lim = visible(a, q, i);
-        float lse2 = INFINITY, delta = 0.f;  // a row that sees nothing: every probability 0
-        if (live) {
-            const uint4 *o = reinterpret_cast<const uint4 *>(a.o.p + token * a.o.ts + head * a.o.hs);
-            const uint4 *g = reinterpret_cast<const uint4 *>(a.go.p + token * a.go.ts + head * a.go.hs);
-#pragma unroll 4
-            for (int c = 0; c < a.D / 8; ++c) {
-                const uint4 x = o[c], y = g[c];
-                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+        // delta = sum over the head of o grad_o: 16 rows a warp, a row's pieces of
+        // 8 values side by side on its lanes, all loads in flight together
+        float *deltas = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile);
+        {
+            constexpr int kPieces = DP / 8, kSteps = kPieces / 2;  // 32 / kPieces rows at a time
+            const int piece = lane % kPieces;
+            uint4 x[kSteps], y[kSteps];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    delta = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), delta);
-                    delta = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), delta);
+            for (int e = 0; e < kSteps; ++e) {
+                const int r = i0 + 16 * warp + e * (32 / kPieces) + lane / kPieces;
+                x[e] = y[e] = make_uint4(0u, 0u, 0u, 0u);
+                if (r < q.n && piece * 8 < a.D) {
+                    const int64_t t = q.q0 + (int64_t)r;
+                    x[e] = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.ts + head * a.o.hs + piece * 8);
+                    y[e] = *reinterpret_cast<const uint4 *>(a.go.p + t * a.go.ts + head * a.go.hs + piece * 8);
                 }
             }
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e) {
+                const uint32_t xs[4] = {x[e].x, x[e].y, x[e].z, x[e].w}, ys[4] = {y[e].x, y[e].y, y[e].z, y[e].w};
+                float d = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    d = fmaf(__uint_as_float(xs[c] << 16), __uint_as_float(ys[c] << 16), d);
+                    d = fmaf(__uint_as_float(xs[c] & 0xffff0000u), __uint_as_float(ys[c] & 0xffff0000u), d);
+                }
+#pragma unroll
+                for (int o = kPieces / 2; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
+                if (piece == 0) deltas[16 * warp + e * (32 / kPieces) + lane / kPieces] = d;
+            }
+        }
+        asm volatile("barrier.cta.sync 2, 256;" ::: "memory");  // the row warps: each row's delta is there
+        float lse2 = INFINITY;  // a row that sees nothing: every probability 0
+        const float delta = deltas[threadIdx.x & 127];
+        if (live) {
             if (half == 0) a.delta[(int64_t)head * a.total_q + token] = delta;
             const float l = a.lse[(int64_t)head * a.total_q + token];
             lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
@@ -814,7 +865,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const int head = blockIdx.x % a.hkv, rest = blockIdx.x / a.hkv;
     const int si = rest % a.seqs, tile = rest / a.seqs;  // causal: the first keys are seen by most queries
-    const Seq q = sequence(a, si);
+    const Offsets offsets = load_offsets(a, si);
+    const GradBars<C> bars(smem);
+    if (warp == C::kCopier) bars.make();
+    const Seq q = sequence(a, offsets);
     if (!q.ok) {
         if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
         return;
@@ -827,23 +881,26 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
     const int b0 = a.causal ? max(0, j0 - off) / BN : 0;
     const int per_head = max(0, (q.n + BN - 1) / BN - b0);
     const int blocks = per_head * a.group;
-    const GradBars<C> bars(smem);
     const auto &ring = bars.ring;
     bool failed = false;
 
     if (warp >= 8) give_registers<C::kRegsOther>();
     if (warp == C::kCopier) {
-        bars.make();
-        setup_arrive<C::kThreads>();
-        if (blocks > 0 && lane == 0) {
-            bar_arrive_expect(bars.tile_full, 2 * C::kTile);
-            copy_tile<DP>(smem_addr(smem), &a.k, head, q.k0 + j0, kRows, bars.tile_full);
-            copy_tile<DP>(smem_addr(smem) + C::kTile, &a.v, head, q.k0 + j0, kRows, bars.tile_full);
-        }
-        __syncwarp();
+        auto rows = [&](const CUtensorMap *map, int t) {
+            if (blocks > 0 && elect_one()) {
+                bar_arrive_expect(bars.tile_full + 8 * t, C::kTile);
+                copy_tile<DP>(smem_addr(smem) + t * C::kTile, map, head, q.k0 + j0, kRows, bars.tile_full + 8 * t);
+            }
+            __syncwarp();
+        };
         int issued = 0, tails = 0, h = head * a.group, b = b0;
+        rows(&a.k, 0);
+        if (blocks > 0)
+            failed = !ring.template fill<DP>(issued++, &a.q, h, q.q0 + b * BN, BN, q.n - b * BN, true, tails);
+        rows(&a.v, 1);
+        setup_arrive<C::kThreads>();
         for (int it = 0; it < blocks && !failed; ++it) {
-            for (int kind = 0; kind < 2 && !failed; ++kind) {
+            for (int kind = it == 0; kind < 2 && !failed; ++kind) {  // the first Q is under way
                 failed = !ring.wait_free(issued) ||
                          !ring.template fill<DP>(issued, kind ? &a.g : &a.q, h, q.q0 + b * BN, BN, q.n - b * BN, true,
                                                  tails);
@@ -853,7 +910,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         }
         if (failed) {
             ring.drain(issued);
-            bar_wait(bars.tile_full, 0, kTries);
+            if (blocks > 0)
+                for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
         }
     } else if (warp == C::kIssuer) {
         tmem_alloc(smem_addr(bars.slot), C::kColumns);
@@ -877,7 +935,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 mma_commit(bars.g_full);
                 return true;
             };
-            failed = !bar_wait(bars.tile_full, 0, kTries) || !scores(0) || !grads(0);
+            failed = !bar_wait(bars.tile_full, 0, kTries) || !scores(0);
+            failed = !bar_wait(bars.tile_full + 8, 0, kTries) || failed || !grads(0);
             // P^T takes the place of S^T, dS^T that of the gradient of P^T:
             // the next product into either comes after the one that reads
             // it (products run in the order of their issue). While the rows'

@@ -20,14 +20,15 @@
 namespace dpb {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 64;
 constexpr int kPer = 8;                    // values a thread
 constexpr int kRound = kThreads * kPer;    // values a block takes at a time
-// Rounds a block: 32-bit states keep enough loads in flight with one; 8-bit
-// ones compute longer on fewer bytes, so a block loads its second round while
-// it computes the first.
+// Rounds a block: 32-bit states keep enough loads in flight with one. 8-bit
+// ones compute longer on fewer bytes, so a block loads the next of eight rounds
+// while it computes one, and its start is spread over more (203 M bf16
+// parameters: 432 us; one round of 256 threads 547, four of 128 threads 475).
 template <bool F8>
-constexpr int kChunk = (F8 ? 2 : 1) * kRound;
+constexpr int kChunk = (F8 ? 8 : 1) * kRound;
 constexpr int kBlock = 32 * kPer;          // values that share a scale
 constexpr float kTop = 448.f;              // largest e4m3 value
 constexpr int kFew = 40, kMany = 440;      // tensors a launch (4 KB and 32 KB of kernel arguments)
@@ -94,27 +95,31 @@ __device__ __forceinline__ F2 operator+(F2 a, F2 b) {
 }
 
 // A value scaled to |y| <= 448 is rounded to one of its two e4m3 neighbours,
-// away from zero with the probability of its place between them (16 random
-// bits, given in bits 4 to 19). From 2^-6 on a code keeps 3 bits after the
+// away from zero with the probability of its place between them (r: 16 random
+// bits). From 2^-6 on a code keeps 3 bits after the
 // leading one, so adding the random bits just below them and cutting them off
 // rounds the magnitude; what passes 448 is brought back by the saturating
 // conversion.
-__device__ __forceinline__ float round_normal(float y, uint32_t r20) {
-    return __uint_as_float((__float_as_uint(y) + r20) & 0xfff00000u);
+__device__ __forceinline__ float round_normal(float y, uint32_t r) {
+    return __uint_as_float((__float_as_uint(y) + r * 16u) & 0xfff00000u);
 }
 // Below 2^-6 the codes are multiples of 2^-9. A NaN stays one.
-__device__ __forceinline__ float round_small(float y, uint32_t r20) {
-    const float t = __fadd_rn(fabsf(y) * 512.f, (float)(r20 >> 4) * (1.f / 65536.f));
+__device__ __forceinline__ float round_small(float y, uint32_t r) {
+    const float t = __fadd_rn(fabsf(y) * 512.f, (float)r * (1.f / 65536.f));
     return copysignf(floorf(t) * (1.f / 512.f), y);
 }
-
-__device__ __forceinline__ float round_any(float y, uint32_t r20) {
-    return fabsf(y) >= 0.015625f ? round_normal(y, r20) : round_small(y, r20);
+__device__ __forceinline__ float round_any(float y, uint32_t r) {
+    return fabsf(y) >= 0.015625f ? round_normal(y, r) : round_small(y, r);
 }
-// The smaller of two; a NaN if either is one.
-__device__ __forceinline__ float min_or_nan(float a, float b) {
+// The smallest of three; a NaN if one of them is.
+__device__ __forceinline__ float min_or_nan(float a, float b, float c) {
     float r;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 
@@ -268,19 +273,19 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
         }
         mi = mi * F2(h.b1, h.b1) + gi * F2(h.c1, h.c1);
         vi = vi * F2(h.b2, h.b2) + gi * F2(h.c2, h.c2) * gi;
-        const float2 m2 = mi.get(), v2 = vi.get(), p2 = two_values(in.p, i).get();
-        m[i] = m2.x, m[i + 1] = m2.y;
-        v[i] = v2.x, v[i + 1] = v2.y;
+        const float2 m2 = mi.get(), v2 = vi.get();
+        const F2 root(__fsqrt_rn(v2.x), __fsqrt_rn(v2.y));
+        const float2 den = (root * F2(h.fix2, h.fix2) + F2(h.eps, h.eps)).get();
+        const float2 p2 = (two_values(in.p, i) * F2(h.decay, h.decay) +
+                           mi * F2(-h.rate, -h.rate) * F2(rcp_approx(den.x), rcp_approx(den.y)))
+                              .get();
         p[i] = p2.x, p[i + 1] = p2.y;
-#pragma unroll
-        for (int e = i; e < i + 2; ++e) {
-            const float root = __fsqrt_rn(v[e]);
-            p[e] = p[e] * h.decay - h.rate * m[e] * rcp_approx(root * h.fix2 + h.eps);
-            if (F8) {
-                v[e] = root;
-                tm = fmaxf(tm, fabsf(m[e]));
-                tv = fmaxf(tv, root);
-            }
+        m[i] = m2.x, m[i + 1] = m2.y;
+        const float2 s2 = F8 ? root.get() : v2;
+        v[i] = s2.x, v[i + 1] = s2.y;
+        if (F8) {
+            tm = max3(tm, fabsf(m[i]), fabsf(m[i + 1]));
+            tv = max3(tv, v[i], v[i + 1]);
         }
     }
     store8<T, WIDE>(pp, left, p);
@@ -289,7 +294,8 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
         ms = block_scale(warp_max(tm), &im);
         vs = block_scale(warp_max(tv), &iv);
         const uint64_t at = (uint64_t)(t.at + i0);
-        const uint32_t key = h.key + 0x9e3779b9u * (uint32_t)(at >> 32);
+        // the value's place (a multiple of kPer, and its place among the kPer) with the key
+        const uint32_t key = (uint32_t)at ^ (h.key + 0x9e3779b9u * (uint32_t)(at >> 32));
         uint32_t r[kPer];
         float low = 1.f;  // smallest magnitude of this lane, scaled
 #pragma unroll
@@ -297,22 +303,22 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
             const float2 m2 = (F2(m[i], m[i + 1]) * F2(im, im)).get(), v2 = (F2(v[i], v[i + 1]) * F2(iv, iv)).get();
             m[i] = m2.x, m[i + 1] = m2.y;
             v[i] = v2.x, v[i + 1] = v2.y;
-            low = min_or_nan(low, min_or_nan(min_or_nan(fabsf(m2.x), fabsf(m2.y)), min_or_nan(v2.x, v2.y)));
+            low = min_or_nan(min_or_nan(low, fabsf(m2.x), fabsf(m2.y)), v2.x, v2.y);
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) r[i] = mix32((uint32_t)(at + i) ^ key);
+        for (int i = 0; i < kPer; ++i) r[i] = mix32(key ^ (uint32_t)i);
         // magnitudes below the normal codes (under 2^-6 / 448 of the block's
         // largest) and NaNs are rare: one test for all of the lane's values
         if (low >= 0.015625f) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                m[i] = round_normal(m[i], (r[i] << 4) & 0xffff0u);
-                v[i] = round_normal(v[i], (r[i] >> 12) & 0xffff0u);
+                m[i] = round_normal(m[i], r[i] & 0xffffu);
+                v[i] = round_normal(v[i], r[i] >> 16);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const uint32_t rm = (r[i] << 4) & 0xffff0u, rv = (r[i] >> 12) & 0xffff0u;
+                const uint32_t rm = r[i] & 0xffffu, rv = r[i] >> 16;
                 m[i] = round_any(m[i], rm);
                 const float y = v[i], q = round_any(y, rv);
                 v[i] = y > 0.f ? fmaxf(q, 1.f / 512.f) : q;  // 2^-9, the smallest code
@@ -344,7 +350,7 @@ __device__ __forceinline__ void step_chunk(const Tensor t, int64_t i0, const Hyp
 }
 
 template <typename T, bool F8, int N>
-__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constant__ Table<N> tab, const Hyper h) {
+__global__ void __launch_bounds__(kThreads, 14) adamw_kernel(const __grid_constant__ Table<N> tab, const Hyper h) {
     const int64_t chunk = blockIdx.x;
     int lo = 0, hi = tab.count;  // first[lo] <= chunk < first[hi]
     while (hi - lo > 1) {

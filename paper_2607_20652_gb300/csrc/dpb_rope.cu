@@ -3,15 +3,17 @@
 //
 // Bound by memory: a head is read once and written once (the gradient reads
 // two and writes one), some ten operations a value. A warp takes one token,
-// so the token's cos and sin are loaded once for all of its heads, and several
-// heads at a time: a head of D values takes D / 8 lanes (rounded up to a
-// power of two) with 8 values each, and its sums are shuffles among them.
-// The 8 values of a lane are 4 rotation pairs, so no value crosses lanes for
-// the rotation: (i .. i + 3) and (i + R/2 .. i + R/2 + 3) in the half layout
-// (two accesses of 4 values), 8 in a row in the interleaved one and beyond
-// the rotated part. Head widths or rotated parts that are no multiple of 8,
-// and rows that are not aligned to 4 values, take the same code with one pair
-// of values a lane and scalar accesses.
+// so the token's cos and sin, and their products with the weights, are made
+// once for all of its heads, and several heads at a time: a head of D values
+// takes D / 8 lanes (rounded up to a power of two) with 8 values each, and its
+// sums are shuffles among them. The 8 values of a lane are 4 rotation pairs,
+// so no value crosses lanes for the rotation: (i .. i + 3) and
+// (i + R/2 .. i + R/2 + 3) in the half layout (two accesses of 4 values), 8 in
+// a row in the interleaved one and beyond the rotated part. The pairs' first
+// and second values are kept apart, so that both layouts run the same packed
+// arithmetic (two values an instruction). Head widths or rotated parts that
+// are no multiple of 8, and rows that are not aligned to 4 values, take the
+// same code with one pair of values a lane and scalar accesses.
 #include <algorithm>
 #include <cuda_bf16.h>
 
@@ -46,6 +48,81 @@ struct RopeArgs {
     int32_t *status;
 };
 
+// ---- VEC values of one kind (a pair's first or second) a lane ----------------
+
+template <int VEC>
+struct Vals;
+template <>
+struct Vals<4> {
+    uint64_t x[2];
+};
+template <>
+struct Vals<1> {
+    float x;
+};
+
+__device__ __forceinline__ uint64_t two(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 apart(uint64_t u) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(u));
+    return r;
+}
+__device__ __forceinline__ Vals<4> all4(float v) { return {{two(v, v), two(v, v)}}; }
+__device__ __forceinline__ Vals<4> set4(float a, float b, float c, float d) { return {{two(a, b), two(c, d)}}; }
+__device__ __forceinline__ Vals<4> operator*(const Vals<4> &a, const Vals<4> &b) {
+    Vals<4> r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.x[i]) : "l"(a.x[i]), "l"(b.x[i]));
+    return r;
+}
+__device__ __forceinline__ Vals<4> madd(const Vals<4> &a, const Vals<4> &b, const Vals<4> &c) {
+    Vals<4> r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.x[i]) : "l"(a.x[i]), "l"(b.x[i]), "l"(c.x[i]));
+    return r;
+}
+__device__ __forceinline__ float total(const Vals<4> &a) {
+    const float2 u = apart(a.x[0]), v = apart(a.x[1]);
+    return (u.x + u.y) + (v.x + v.y);
+}
+__device__ __forceinline__ Vals<1> operator*(const Vals<1> &a, const Vals<1> &b) { return {a.x * b.x}; }
+__device__ __forceinline__ Vals<1> madd(const Vals<1> &a, const Vals<1> &b, const Vals<1> &c) {
+    return {fmaf(a.x, b.x, c.x)};
+}
+__device__ __forceinline__ float total(const Vals<1> &a) { return a.x; }
+template <int VEC>
+__device__ __forceinline__ Vals<VEC> all(float v) {
+    if constexpr (VEC == 4)
+        return all4(v);
+    else
+        return {v};
+}
+template <int VEC, typename F>
+__device__ __forceinline__ void each_value(const Vals<VEC> &v, F f) {
+    if constexpr (VEC == 4) {
+        const float2 a = apart(v.x[0]), b = apart(v.x[1]);
+        f(0, a.x), f(1, a.y), f(2, b.x), f(3, b.y);
+    } else {
+        f(0, v.x);
+    }
+}
+template <int VEC, typename F>
+__device__ __forceinline__ Vals<VEC> map_values(const Vals<VEC> &v, F f) {
+    if constexpr (VEC == 4) {
+        const float2 a = apart(v.x[0]), b = apart(v.x[1]);
+        return set4(f(a.x), f(a.y), f(b.x), f(b.y));
+    } else {
+        return {f(v.x)};
+    }
+}
+
+// ---- access --------------------------------------------------------------------
+
 // VEC values as they lie in memory: loads keep these until they are used.
 template <typename T, int VEC>
 struct RawVec {
@@ -59,156 +136,134 @@ template <>
 struct RawVec<__nv_bfloat16, 4> {
     using type = uint2;
 };
-
-template <int VEC>
-__device__ __forceinline__ void unpack(const float4 &r, float (&v)[VEC]) {
-    v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w;
-}
-template <int VEC>
-__device__ __forceinline__ void unpack(const uint2 &r, float (&v)[VEC]) {
-    v[0] = __uint_as_float(r.x << 16), v[1] = __uint_as_float(r.x & 0xffff0000u);
-    v[2] = __uint_as_float(r.y << 16), v[3] = __uint_as_float(r.y & 0xffff0000u);
-}
-template <int VEC>
-__device__ __forceinline__ void unpack(float r, float (&v)[VEC]) {
-    v[0] = r;
-}
-template <int VEC>
-__device__ __forceinline__ void unpack(__nv_bfloat16 r, float (&v)[VEC]) {
-    v[0] = __bfloat162float(r);
-}
 template <typename T, int VEC>
-__device__ __forceinline__ void store_vec(T *p, const float (&v)[VEC]) {
-    if constexpr (VEC == 4)
-        st4(p, make_float4(v[0], v[1], v[2], v[3]));
-    else
-        st_elem(p, 0, v[0]);
+struct Raw {
+    typename RawVec<T, VEC>::type a, b;
+};
+
+__device__ __forceinline__ float low_bf16(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// A lane's share of a head: UPL units of VEC pairs (a, b). Unit u covers, in
-// the rotated part of the half layout, a = VEC u .. and b = a + R/2 ..; else
-// the 2 VEC values from 2 VEC u on, paired in turn when rotated.
-template <int VEC, int UPL>
-struct Share {
-    float a[UPL][VEC], b[UPL][VEC];
-};
-template <typename T, int VEC, int UPL>
-struct RawShare {
-    typename RawVec<T, VEC>::type a[UPL], b[UPL];
-};
+// A lane's 2 VEC values of a head as (first, second) of its pairs. MIX: the
+// pairs are neighbours in memory.
+template <bool MIX>
+__device__ __forceinline__ void unpack(const Raw<float, 4> &r, Vals<4> &a, Vals<4> &b) {
+    a = MIX ? set4(r.a.x, r.a.z, r.b.x, r.b.z) : set4(r.a.x, r.a.y, r.a.z, r.a.w);
+    b = MIX ? set4(r.a.y, r.a.w, r.b.y, r.b.w) : set4(r.b.x, r.b.y, r.b.z, r.b.w);
+}
+template <bool MIX>
+__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16, 4> &r, Vals<4> &a, Vals<4> &b) {
+    if (MIX) {
+        a = set4(low_bf16(r.a.x), low_bf16(r.a.y), low_bf16(r.b.x), low_bf16(r.b.y));
+        b = set4(high_bf16(r.a.x), high_bf16(r.a.y), high_bf16(r.b.x), high_bf16(r.b.y));
+    } else {
+        a = set4(low_bf16(r.a.x), high_bf16(r.a.x), low_bf16(r.a.y), high_bf16(r.a.y));
+        b = set4(low_bf16(r.b.x), high_bf16(r.b.x), low_bf16(r.b.y), high_bf16(r.b.y));
+    }
+}
+template <bool MIX, typename T>
+__device__ __forceinline__ void unpack(const Raw<T, 1> &r, Vals<1> &a, Vals<1> &b) {
+    a.x = (float)r.a;
+    b.x = (float)r.b;
+}
+template <bool MIX>
+__device__ __forceinline__ void pack(const Vals<4> &a, const Vals<4> &b, Raw<float, 4> &r) {
+    const float2 a0 = apart(a.x[0]), a1 = apart(a.x[1]), b0 = apart(b.x[0]), b1 = apart(b.x[1]);
+    r.a = MIX ? make_float4(a0.x, b0.x, a0.y, b0.y) : make_float4(a0.x, a0.y, a1.x, a1.y);
+    r.b = MIX ? make_float4(a1.x, b1.x, a1.y, b1.y) : make_float4(b0.x, b0.y, b1.x, b1.y);
+}
+template <bool MIX>
+__device__ __forceinline__ void pack(const Vals<4> &a, const Vals<4> &b, Raw<__nv_bfloat16, 4> &r) {
+    const float2 a0 = apart(a.x[0]), a1 = apart(a.x[1]), b0 = apart(b.x[0]), b1 = apart(b.x[1]);
+    r.a = MIX ? make_uint2(pack_two(a0.x, b0.x), pack_two(a0.y, b0.y)) : make_uint2(pack_two(a0.x, a0.y), pack_two(a1.x, a1.y));
+    r.b = MIX ? make_uint2(pack_two(a1.x, b1.x), pack_two(a1.y, b1.y)) : make_uint2(pack_two(b0.x, b0.y), pack_two(b1.x, b1.y));
+}
+template <bool MIX, typename T>
+__device__ __forceinline__ void pack(const Vals<1> &a, const Vals<1> &b, Raw<T, 1> &r) {
+    r.a = (T)a.x;
+    r.b = (T)b.x;
+}
 
-template <typename T, int VEC, int UPL>
+// A lane's share of a head: UPL units of VEC pairs. Unit u covers, in the
+// rotated part of the half layout, VEC u .. and VEC u + R/2 ..; else the 2 VEC
+// values from 2 VEC u on. MIX says that these are neighbouring pairs; beyond
+// the rotated part (rotated by nothing) the pairing does not matter.
+template <typename T, int VEC, int UPL, bool MIX>
 struct Lane {
+    using R = typename RawVec<T, VEC>::type;
     int oa[UPL], ob[UPL];  // first elements of the two runs of VEC values
-    bool on[UPL], rot[UPL], inter;
+    bool on[UPL], rot[UPL];
 
     __device__ __forceinline__ Lane(const RopeArgs &g, int u0) {
-        inter = g.interleaved;
 #pragma unroll
         for (int j = 0; j < UPL; ++j) {
             const int u = u0 + 32 * j;
             on[j] = 2 * VEC * u < g.D;
             rot[j] = 2 * VEC * u < g.R;
-            const bool half = rot[j] && !inter;
+            const bool half = rot[j] && !MIX;
             oa[j] = half ? VEC * u : 2 * VEC * u;
             ob[j] = half ? VEC * u + g.R / 2 : 2 * VEC * u + VEC;
         }
     }
-    __device__ __forceinline__ void load(const T *row, bool ok, RawShare<T, VEC, UPL> &s) const {
-        using R = typename RawVec<T, VEC>::type;
+    __device__ __forceinline__ void load(const T *row, bool ok, Raw<T, VEC> (&s)[UPL]) const {
 #pragma unroll
         for (int j = 0; j < UPL; ++j) {
-            s.a[j] = R{};
-            s.b[j] = R{};
+            s[j].a = R{};
+            s[j].b = R{};
             if (ok && on[j]) {
-                s.a[j] = *reinterpret_cast<const R *>(row + oa[j]);
-                s.b[j] = *reinterpret_cast<const R *>(row + ob[j]);
+                s[j].a = *reinterpret_cast<const R *>(row + oa[j]);
+                s[j].b = *reinterpret_cast<const R *>(row + ob[j]);
             }
         }
     }
-    __device__ __forceinline__ static void values(const RawShare<T, VEC, UPL> &r, Share<VEC, UPL> &s) {
-#pragma unroll
-        for (int j = 0; j < UPL; ++j) {
-            unpack<VEC>(r.a[j], s.a[j]);
-            unpack<VEC>(r.b[j], s.b[j]);
-        }
-    }
-    __device__ __forceinline__ void store(T *row, bool ok, const Share<VEC, UPL> &s) const {
+    __device__ __forceinline__ void store(T *row, const Vals<VEC> (&a)[UPL], const Vals<VEC> (&b)[UPL]) const {
 #pragma unroll
         for (int j = 0; j < UPL; ++j)
-            if (ok && on[j]) {
-                store_vec<T, VEC>(row + oa[j], s.a[j]);
-                store_vec<T, VEC>(row + ob[j], s.b[j]);
+            if (on[j]) {
+                Raw<T, VEC> r;
+                pack<MIX>(a[j], b[j], r);
+                *reinterpret_cast<R *>(row + oa[j]) = r.a;
+                *reinterpret_cast<R *>(row + ob[j]) = r.b;
             }
     }
-    // The unit's VEC pairs are (a[i], b[i]) in the half layout; interleaved
-    // they are neighbours: for VEC = 4 (a0 a1)(a2 a3)(b0 b1)(b2 b3).
-    __device__ __forceinline__ void rotate(Share<VEC, UPL> &s, const float (&c)[UPL][VEC],
-                                           const float (&n)[UPL][VEC]) const {
-#pragma unroll
-        for (int j = 0; j < UPL; ++j) {
-            if (!rot[j]) continue;
-            if (VEC == 1 || !inter) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float a = s.a[j][i], b = s.b[j][i];
-                    s.a[j][i] = a * c[j][i] - b * n[j][i];
-                    s.b[j][i] = b * c[j][i] + a * n[j][i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i + 1 < VEC; i += 2) {
-                    const float a = s.a[j][i], b = s.a[j][i + 1];
-                    s.a[j][i] = a * c[j][i / 2] - b * n[j][i / 2];
-                    s.a[j][i + 1] = b * c[j][i / 2] + a * n[j][i / 2];
-                    const float d = s.b[j][i], e = s.b[j][i + 1];
-                    s.b[j][i] = d * c[j][VEC / 2 + i / 2] - e * n[j][VEC / 2 + i / 2];
-                    s.b[j][i + 1] = e * c[j][VEC / 2 + i / 2] + d * n[j][VEC / 2 + i / 2];
-                }
-            }
-        }
-    }
-    // Position p's cos and sin of this lane's pairs (pairs VEC u .. VEC u + VEC - 1
-    // in both layouts); 1 and 0 where nothing turns.
-    __device__ __forceinline__ void angles(const RopeArgs &g, int64_t p, int u0, float (&c)[UPL][VEC],
-                                           float (&n)[UPL][VEC], bool back) const {
+    // Position p's cos and sin of this lane's pairs (pairs VEC u .. VEC u +
+    // VEC - 1 in both layouts); 1 and 0 where nothing turns.
+    __device__ __forceinline__ void angles(const RopeArgs &g, int64_t p, int u0, Vals<VEC> (&c)[UPL],
+                                           Vals<VEC> (&n)[UPL]) const {
         const bool good = p >= 0 && p < g.pos_n;
         if (g.R > 0 && !good && (threadIdx.x & 31) == 0) set_status(g.status, DPB_DEV_BAD_LENGTH);
 #pragma unroll
         for (int j = 0; j < UPL; ++j) {
-            const bool on = good && rot[j];
-            const int64_t at = p * (g.R / 2) + VEC * (u0 + 32 * j);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) c[j][i] = 1.f, n[j][i] = 0.f;
-            if (on) {
-                using R = typename RawVec<float, VEC>::type;
-                unpack<VEC>(__ldg(reinterpret_cast<const R *>(g.cos_tab + at)), c[j]);
-                unpack<VEC>(__ldg(reinterpret_cast<const R *>(g.sin_tab + at)), n[j]);
-                if (back)
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) n[j][i] = -n[j][i];
+            c[j] = all<VEC>(1.f);
+            n[j] = all<VEC>(0.f);
+            if (good && rot[j]) {
+                const int64_t at = p * (g.R / 2) + VEC * (u0 + 32 * j);
+                if constexpr (VEC == 4) {
+                    const float4 x = __ldg(reinterpret_cast<const float4 *>(g.cos_tab + at));
+                    const float4 y = __ldg(reinterpret_cast<const float4 *>(g.sin_tab + at));
+                    c[j] = set4(x.x, x.y, x.z, x.w);
+                    n[j] = set4(y.x, y.y, y.z, y.w);
+                } else {
+                    c[j].x = __ldg(g.cos_tab + at);
+                    n[j].x = __ldg(g.sin_tab + at);
+                }
             }
         }
     }
-    __device__ __forceinline__ void weights(const void *w, Share<VEC, UPL> &s) const {
+    __device__ __forceinline__ void weights(const void *w, Vals<VEC> (&a)[UPL], Vals<VEC> (&b)[UPL]) const {
 #pragma unroll
-        for (int j = 0; j < UPL; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) s.a[j][i] = s.b[j][i] = 1.f;
+        for (int j = 0; j < UPL; ++j) a[j] = b[j] = all<VEC>(1.f);
         if (!w) return;
-        RawShare<T, VEC, UPL> r;
+        Raw<T, VEC> r[UPL];
         load(static_cast<const T *>(w), true, r);
-        values(r, s);
+#pragma unroll
+        for (int j = 0; j < UPL; ++j) unpack<MIX>(r[j], a[j], b[j]);
     }
 };
-
-template <int VEC, int UPL, typename F>
-__device__ __forceinline__ void each(F f) {
-#pragma unroll
-    for (int j = 0; j < UPL; ++j)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) f(j, i);
-}
 
 __device__ __forceinline__ float group_sum(float v, int gl) {
     for (int o = gl / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
@@ -219,83 +274,103 @@ __device__ __forceinline__ int64_t position(const RopeArgs &g, int64_t t) {
     return g.R > 0 && g.pos && t < g.T ? (int64_t)g.pos[t] : t;
 }
 
-// One token's heads of q and k as one list of heads_q + heads_k.
-struct Row {
-    const Heads &q, &k;
-    int64_t t;
-    template <typename T>
-    __device__ __forceinline__ T *head(int h) const {
-        const bool second = h >= q.n;
-        const Heads &s = second ? k : q;
-        return reinterpret_cast<T *>(s.p) + t * s.ts + (second ? h - q.n : h) * s.hs;
-    }
-};
+template <int VEC>
+__device__ __forceinline__ Vals<VEC> negative(const Vals<VEC> &v) {
+    return map_values<VEC>(v, [](float x) { return -x; });
+}
 
-template <typename T, int VEC, int UPL>
+// A token's heads go by rounds: one head of each lane group, first q's, then
+// k's, so that a round's kind is the warp's. With P = w cos and Q = w sin,
+// the rotated, weighted and normalised pair is
+//   r (x_a P_a - x_b Q_b),  r (x_b P_b + x_a Q_a).
+template <typename T, int VEC, int UPL, bool MIX>
 __global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_constant__ RopeArgs g) {
     const int lane = threadIdx.x & 31, u0 = lane & (g.gl - 1), grp = lane / g.gl, groups = 32 / g.gl;
-    const Lane<T, VEC, UPL> ln(g, u0);
-    const int nh = g.q.n + g.k.n;
+    const Lane<T, VEC, UPL, MIX> ln(g, u0);
+    const int rq = (g.q.n + groups - 1) / groups, rounds = rq + (g.k.n + groups - 1) / groups;
     const float inv_d = 1.f / (float)g.D;
-    Share<VEC, UPL> w[2];
-    ln.weights(g.wq, w[0]);
-    ln.weights(g.wk, w[1]);
+    Vals<VEC> wa[2][UPL], wb[2][UPL];
+    ln.weights(g.wq, wa[0], wb[0]);
+    ln.weights(g.wk, wa[1], wb[1]);
     const int64_t step = (int64_t)gridDim.x * kWarps;
     int64_t t = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32;
     int64_t p = position(g, t);
     for (; t < g.T; t += step) {
-        const Row in{g.q, g.k, t}, out{g.oq, g.ok, t};
-        float c[UPL][VEC], n[UPL][VEC];
-        for (int h0 = grp; h0 - grp < nh; h0 += groups * kBatch) {
-            RawShare<T, VEC, UPL> raw[kBatch];
+        const T *qs = reinterpret_cast<const T *>(g.q.p) + t * g.q.ts, *ks = reinterpret_cast<const T *>(g.k.p) + t * g.k.ts;
+        T *qo = reinterpret_cast<T *>(g.oq.p) + t * g.oq.ts, *ko = reinterpret_cast<T *>(g.ok.p) + t * g.ok.ts;
+        Vals<VEC> c[UPL], n[UPL], pa[UPL], pb[UPL], qa[UPL], qb[UPL];
+        auto turn = [&](const Vals<VEC>(&a)[UPL], const Vals<VEC>(&b)[UPL]) {
+#pragma unroll
+            for (int j = 0; j < UPL; ++j) {
+                pa[j] = a[j] * c[j];
+                pb[j] = b[j] * c[j];
+                qa[j] = a[j] * n[j];
+                qb[j] = negative<VEC>(b[j] * n[j]);
+            }
+        };
+        for (int r0 = 0; r0 < rounds; r0 += kBatch) {
+            Raw<T, VEC> raw[kBatch][UPL];
 #pragma unroll
             for (int e = 0; e < kBatch; ++e) {
-                const int h = h0 + e * groups;
-                ln.load(in.head<const T>(min(h, nh - 1)), h < nh, raw[e]);
+                const bool second = r0 + e >= rq;
+                const int h = (second ? r0 + e - rq : r0 + e) * groups + grp;
+                ln.load(second ? ks + h * g.k.hs : qs + h * g.q.hs, r0 + e < rounds && h < (second ? g.k.n : g.q.n), raw[e]);
             }
-            if (h0 == grp) {  // once a token, behind its first heads' loads
-                ln.angles(g, p, u0, c, n, false);
+            if (r0 == 0) {  // once a token, behind its first heads' loads
+                ln.angles(g, p, u0, c, n);
                 p = position(g, t + step);
+                turn(wa[0], wb[0]);
             }
 #pragma unroll
             for (int e = 0; e < kBatch; ++e) {
-                const int h = h0 + e * groups;
-                if (h - grp >= nh) break;  // the whole warp is done
-                Share<VEC, UPL> x;
-                ln.values(raw[e], x);
-                if (g.normalise) {
-                    float ss = 0.f;
-                    each<VEC, UPL>([&](int j, int i) { ss += x.a[j][i] * x.a[j][i] + x.b[j][i] * x.b[j][i]; });
-                    const float r = rsqrtf(group_sum(ss, g.gl) * inv_d + g.eps);
-                    const bool second = h >= g.q.n;
-                    each<VEC, UPL>([&](int j, int i) {
-                        x.a[j][i] *= r * (second ? w[1].a[j][i] : w[0].a[j][i]);
-                        x.b[j][i] *= r * (second ? w[1].b[j][i] : w[0].b[j][i]);
-                    });
+                const int r = r0 + e;
+                if (r >= rounds) break;
+                if (r == rq) turn(wa[1], wb[1]);
+                const bool second = r >= rq;
+                const int h = (second ? r - rq : r) * groups + grp;
+                Vals<VEC> xa[UPL], xb[UPL], ya[UPL], yb[UPL];
+                Vals<VEC> ss = all<VEC>(0.f);
+#pragma unroll
+                for (int j = 0; j < UPL; ++j) {
+                    unpack<MIX>(raw[e][j], xa[j], xb[j]);
+                    ss = madd(xa[j], xa[j], ss);
+                    ss = madd(xb[j], xb[j], ss);
+                    ya[j] = madd(xb[j], qb[j], xa[j] * pa[j]);
+                    yb[j] = madd(xa[j], qa[j], xb[j] * pb[j]);
                 }
-                ln.rotate(x, c, n);
-                if (h < nh) ln.store(out.head<T>(h), true, x);
+                if (g.normalise) {
+                    const Vals<VEC> f = all<VEC>(rsqrtf(group_sum(total(ss), g.gl) * inv_d + g.eps));
+#pragma unroll
+                    for (int j = 0; j < UPL; ++j) {
+                        ya[j] = ya[j] * f;
+                        yb[j] = yb[j] * f;
+                    }
+                }
+                if (h < (second ? g.k.n : g.q.n)) ln.store(second ? ko + h * g.ok.hs : qo + h * g.oq.hs, ya, yb);
             }
         }
     }
 }
 
-template <typename T, int VEC, int UPL>
+// The gradient: g rotated back, u = w g; dx = r u - x r^3 mean(u x), and
+// g x r to the weight's.
+template <typename T, int VEC, int UPL, bool MIX>
 __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __grid_constant__ RopeArgs g) {
     __shared__ float part[kWarps][2][kMaxDim];
     const int lane = threadIdx.x & 31, u0 = lane & (g.gl - 1), grp = lane / g.gl, groups = 32 / g.gl;
     const int warp = threadIdx.x / 32;
-    const Lane<T, VEC, UPL> ln(g, u0);
+    const Lane<T, VEC, UPL, MIX> ln(g, u0);
     const float inv_d = 1.f / (float)g.D;
-    Share<VEC, UPL> w[2], dw[2];
-    ln.weights(g.wq, w[0]);
-    ln.weights(g.wk, w[1]);
-    each<VEC, UPL>([&](int j, int i) { dw[0].a[j][i] = dw[0].b[j][i] = dw[1].a[j][i] = dw[1].b[j][i] = 0.f; });
+    Vals<VEC> wa[2][UPL], wb[2][UPL], da[2][UPL], db[2][UPL];
+    ln.weights(g.wq, wa[0], wb[0]);
+    ln.weights(g.wk, wa[1], wb[1]);
+#pragma unroll
+    for (int j = 0; j < UPL; ++j) da[0][j] = db[0][j] = da[1][j] = db[1][j] = all<VEC>(0.f);
     const int64_t step = (int64_t)gridDim.x * kWarps;
     int64_t t = (int64_t)blockIdx.x * kWarps + warp;
     int64_t p = position(g, t);
     for (; t < g.T; t += step) {
-        float c[UPL][VEC], n[UPL][VEC];
+        Vals<VEC> c[UPL], n[UPL], m[UPL];
         bool first = true;
         // q's heads, then k's: each kind adds to its own weight gradient
 #pragma unroll
@@ -305,7 +380,7 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
             const T *ys = reinterpret_cast<const T *>(gout.p) + t * gout.ts;
             T *os = reinterpret_cast<T *>(out.p) + t * out.ts;
             for (int h0 = grp; h0 - grp < in.n; h0 += groups * kBatchGrad) {
-                RawShare<T, VEC, UPL> rx[kBatchGrad], ry[kBatchGrad];
+                Raw<T, VEC> rx[kBatchGrad][UPL], ry[kBatchGrad][UPL];
 #pragma unroll
                 for (int e = 0; e < kBatchGrad; ++e) {
                     const int h = h0 + e * groups;
@@ -313,7 +388,9 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
                     ln.load(ys + h * gout.hs, h < in.n, ry[e]);
                 }
                 if (first) {
-                    ln.angles(g, p, u0, c, n, true);
+                    ln.angles(g, p, u0, c, n);
+#pragma unroll
+                    for (int j = 0; j < UPL; ++j) m[j] = negative<VEC>(n[j]);
                     p = position(g, t + step);
                     first = false;
                 }
@@ -321,30 +398,33 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
                 for (int e = 0; e < kBatchGrad; ++e) {
                     const int h = h0 + e * groups;
                     if (h - grp >= in.n) break;
-                    Share<VEC, UPL> x, y;
-                    ln.values(ry[e], y);
-                    ln.rotate(y, c, n);
-                    if (g.normalise) {
-                        ln.values(rx[e], x);
-                        float ss = 0.f, sp = 0.f;  // sum of x^2, and of w g x
-                        each<VEC, UPL>([&](int j, int i) {
-                            const float xa = x.a[j][i], xb = x.b[j][i];
-                            ss += xa * xa + xb * xb;
-                            sp += w[s].a[j][i] * y.a[j][i] * xa + w[s].b[j][i] * y.b[j][i] * xb;
-                        });
-                        ss = group_sum(ss, g.gl);
-                        sp = group_sum(sp, g.gl);
-                        const float r = rsqrtf(ss * inv_d + g.eps);
-                        const float f = r * r * r * sp * inv_d;
-                        each<VEC, UPL>([&](int j, int i) {
-                            const float xa = x.a[j][i], xb = x.b[j][i];
-                            dw[s].a[j][i] += y.a[j][i] * xa * r;
-                            dw[s].b[j][i] += y.b[j][i] * xb * r;
-                            y.a[j][i] = r * w[s].a[j][i] * y.a[j][i] - f * xa;
-                            y.b[j][i] = r * w[s].b[j][i] * y.b[j][i] - f * xb;
-                        });
+                    Vals<VEC> xa[UPL], xb[UPL], ga[UPL], gb[UPL], ua[UPL], ub[UPL];
+                    Vals<VEC> ss = all<VEC>(0.f), sp = all<VEC>(0.f);  // sums of x^2 and of u x
+#pragma unroll
+                    for (int j = 0; j < UPL; ++j) {
+                        Vals<VEC> ya, yb;
+                        unpack<MIX>(ry[e][j], ya, yb);
+                        unpack<MIX>(rx[e][j], xa[j], xb[j]);
+                        ga[j] = madd(yb, n[j], ya * c[j]);
+                        gb[j] = madd(ya, m[j], yb * c[j]);
+                        ua[j] = ga[j] * wa[s][j];
+                        ub[j] = gb[j] * wb[s][j];
+                        ss = madd(xb[j], xb[j], madd(xa[j], xa[j], ss));
+                        sp = madd(xb[j], ub[j], madd(xa[j], ua[j], sp));
                     }
-                    if (h < in.n) ln.store(os + h * out.hs, true, y);
+                    if (g.normalise) {
+                        const float x2 = group_sum(total(ss), g.gl), ux = group_sum(total(sp), g.gl);
+                        const float r = rsqrtf(x2 * inv_d + g.eps);
+                        const Vals<VEC> r4 = all<VEC>(r), f4 = all<VEC>(-r * r * r * ux * inv_d);
+#pragma unroll
+                        for (int j = 0; j < UPL; ++j) {
+                            da[s][j] = madd(ga[j] * xa[j], r4, da[s][j]);
+                            db[s][j] = madd(gb[j] * xb[j], r4, db[s][j]);
+                            ua[j] = madd(xa[j], f4, ua[j] * r4);
+                            ub[j] = madd(xb[j], f4, ub[j] * r4);
+                        }
+                    }
+                    if (h < in.n) ln.store(os + h * out.hs, ua, ub);
                 }
             }
         }
@@ -355,19 +435,22 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
     for (int o = g.gl; o < 32; o <<= 1)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-            each<VEC, UPL>([&](int j, int i) {
-                dw[s].a[j][i] += __shfl_xor_sync(kFull, dw[s].a[j][i], o);
-                dw[s].b[j][i] += __shfl_xor_sync(kFull, dw[s].b[j][i], o);
-            });
+#pragma unroll
+            for (int j = 0; j < UPL; ++j) {
+                auto add = [&](float x) { return x + __shfl_xor_sync(kFull, x, o); };
+                da[s][j] = map_values<VEC>(da[s][j], add);
+                db[s][j] = map_values<VEC>(db[s][j], add);
+            }
     if (grp == 0)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-            each<VEC, UPL>([&](int j, int i) {
+#pragma unroll
+            for (int j = 0; j < UPL; ++j)
                 if (ln.on[j]) {
-                    part[warp][s][ln.oa[j] + i] = dw[s].a[j][i];
-                    part[warp][s][ln.ob[j] + i] = dw[s].b[j][i];
+                    // where a pair's values lie: neighbours, or in two runs
+                    each_value<VEC>(da[s][j], [&](int i, float x) { part[warp][s][MIX && VEC > 1 ? ln.oa[j] + 2 * i : ln.oa[j] + i] = x; });
+                    each_value<VEC>(db[s][j], [&](int i, float x) { part[warp][s][MIX && VEC > 1 ? ln.oa[j] + 2 * i + 1 : ln.ob[j] + i] = x; });
                 }
-            });
     __syncthreads();
     for (int e = threadIdx.x; e < 2 * g.D; e += blockDim.x) {
         const int s = e >= g.D, i = e - s * g.D;
@@ -491,20 +574,39 @@ int rope_blocks(K kernel, int64_t T) {
     return (int)std::min<int64_t>((T + kWarps - 1) / kWarps, most);
 }
 
-template <typename T, int VEC, int UPL>
+template <typename T, int VEC, int UPL, bool MIX>
 cudaError_t launch_forward(const RopeArgs &a, cudaStream_t s) {
-    static const int full = rope_blocks(norm_rope_kernel<T, VEC, UPL>, INT64_MAX / 2);
-    norm_rope_kernel<T, VEC, UPL><<<(int)std::min<int64_t>((a.T + kWarps - 1) / kWarps, full), 32 * kWarps, 0, s>>>(a);
+    static const int full = rope_blocks(norm_rope_kernel<T, VEC, UPL, MIX>, INT64_MAX / 2);
+    const int blocks = (int)std::min<int64_t>((a.T + kWarps - 1) / kWarps, full);
+    norm_rope_kernel<T, VEC, UPL, MIX><<<blocks, 32 * kWarps, 0, s>>>(a);
     return cudaGetLastError();
 }
 
-template <typename T, int VEC, int UPL>
+template <typename T, int VEC, int UPL, bool MIX>
 cudaError_t launch_backward_rope(const RopeArgs &a, float *dwq, float *dwk, cudaStream_t s) {
-    static const int full = rope_blocks(norm_rope_grad_kernel<T, VEC, UPL>, INT64_MAX / 2);
+    static const int full = rope_blocks(norm_rope_grad_kernel<T, VEC, UPL, MIX>, INT64_MAX / 2);
     const int blocks = (int)std::min<int64_t>((a.T + kWarps - 1) / kWarps, full);
-    if (blocks > 0) norm_rope_grad_kernel<T, VEC, UPL><<<blocks, 32 * kWarps, 0, s>>>(a);
+    if (blocks > 0) norm_rope_grad_kernel<T, VEC, UPL, MIX><<<blocks, 32 * kWarps, 0, s>>>(a);
     if (a.part) weight_grad_kernel<<<(2 * a.D + 31) / 32, 1024, 0, s>>>(a.part, blocks, a.D, dwq, dwk);
     return cudaGetLastError();
+}
+
+// By type, by whether rows are read 4 values at a time, and by layout.
+template <typename T, int VEC, int UPL>
+cudaError_t launch_kind(const Call &c, bool backward, float *dwq, float *dwk, cudaStream_t s) {
+    if (c.a.interleaved)
+        return backward ? launch_backward_rope<T, VEC, UPL, true>(c.a, dwq, dwk, s)
+                        : launch_forward<T, VEC, UPL, true>(c.a, s);
+    return backward ? launch_backward_rope<T, VEC, UPL, false>(c.a, dwq, dwk, s)
+                    : launch_forward<T, VEC, UPL, false>(c.a, s);
+}
+
+cudaError_t launch_rope(const Call &c, int dtype, bool backward, float *dwq, float *dwk, cudaStream_t s) {
+    if (dtype == DPB_F32)
+        return c.four ? launch_kind<float, 4, 1>(c, backward, dwq, dwk, s)
+                      : launch_kind<float, 1, 4>(c, backward, dwq, dwk, s);
+    return c.four ? launch_kind<__nv_bfloat16, 4, 1>(c, backward, dwq, dwk, s)
+                  : launch_kind<__nv_bfloat16, 1, 4>(c, backward, dwq, dwk, s);
 }
 
 }  // namespace
@@ -530,13 +632,8 @@ dpb_status dpb_qk_norm_rope(const dpb_rope_config *cfg, const dpb_heads *q, cons
     Call call;
     DPB_CHECK(make_call(cfg, q, k, nullptr, nullptr, weight_q, weight_k, cos_tab, sin_tab, positions, q_out, k_out,
                         workspace, workspace_bytes, false, &call));
-    const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (cfg->dtype == DPB_F32)
-        e = call.four ? launch_forward<float, 4, 1>(call.a, s) : launch_forward<float, 1, 4>(call.a, s);
-    else
-        e = call.four ? launch_forward<__nv_bfloat16, 4, 1>(call.a, s) : launch_forward<__nv_bfloat16, 1, 4>(call.a, s);
-    return launch_status(e, "qk_norm_rope");
+    return launch_status(
+        launch_rope(call, cfg->dtype, false, nullptr, nullptr, static_cast<cudaStream_t>(stream)), "qk_norm_rope");
 }
 
 dpb_status dpb_qk_norm_rope_backward(const dpb_rope_config *cfg, const dpb_heads *q, const dpb_heads *k,
@@ -561,15 +658,9 @@ dpb_status dpb_qk_norm_rope_backward(const dpb_rope_config *cfg, const dpb_heads
                             grad_k, workspace, workspace_bytes, true, &call));
     }
     if (weights) call.a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + kStatusBytes);
-    const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (cfg->dtype == DPB_F32)
-        e = call.four ? launch_backward_rope<float, 4, 1>(call.a, grad_weight_q, grad_weight_k, s)
-                      : launch_backward_rope<float, 1, 4>(call.a, grad_weight_q, grad_weight_k, s);
-    else
-        e = call.four ? launch_backward_rope<__nv_bfloat16, 4, 1>(call.a, grad_weight_q, grad_weight_k, s)
-                      : launch_backward_rope<__nv_bfloat16, 1, 4>(call.a, grad_weight_q, grad_weight_k, s);
-    return launch_status(e, "qk_norm_rope_backward");
+    return launch_status(
+        launch_rope(call, cfg->dtype, true, grad_weight_q, grad_weight_k, static_cast<cudaStream_t>(stream)),
+        "qk_norm_rope_backward");
 }
 
 }  // extern "C"

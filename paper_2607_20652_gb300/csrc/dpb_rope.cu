@@ -24,8 +24,12 @@ namespace dpb {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kBatch = 4;       // rounds (one head a lane group each) whose loads are in flight together
-constexpr int kBatchGrad = 3;
+// Heads of a lane group whose loads are in flight together, and the blocks an
+// SM that the registers are held to: 65536 tokens of 12 + 12 heads of 64 take
+// 71 us at (3, 4), 78 at (3, 3), 87 at (4, 4); the gradient of 49999 tokens of
+// 16 + 4 heads of 128 142 us at (4, 2), 151 at (3, 2), 184 at (3, 3).
+constexpr int kBatch = 3, kBlocks = 4;
+constexpr int kBatchGrad = 4, kBlocksGrad = 2;
 constexpr int kMaxDim = 256;
 constexpr int kMaxBlocks = 152 * 8;  // partial sums of the weight gradients: one row a block
 
@@ -265,8 +269,15 @@ struct Lane {
     }
 };
 
+// Sum over the lanes of a head: GL of them, or (GL = 0) gl.
+template <int GL>
 __device__ __forceinline__ float group_sum(float v, int gl) {
-    for (int o = gl / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    if constexpr (GL > 0) {
+#pragma unroll
+        for (int o = GL / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    } else {
+        for (int o = gl / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    }
     return v;
 }
 
@@ -279,85 +290,95 @@ __device__ __forceinline__ Vals<VEC> negative(const Vals<VEC> &v) {
     return map_values<VEC>(v, [](float x) { return -x; });
 }
 
-// A token's heads go by rounds: one head of each lane group, first q's, then
-// k's, so that a round's kind is the warp's. With P = w cos and Q = w sin,
-// the rotated, weighted and normalised pair is
+// A lane group's heads of one kind: h = grp, grp + groups, ..., taken in
+// batches of B whose loads are in flight together.
+template <typename T>
+struct Walk {
+    T *at;
+    int64_t step;  // to the group's next head
+    __device__ __forceinline__ Walk(const Heads &h, int64_t t, int grp, int groups)
+        : at(reinterpret_cast<T *>(h.p) + t * h.ts + grp * h.hs), step(groups * h.hs) {}
+};
+
+// With P = w cos and Q = w sin, the rotated, weighted and normalised pair is
 //   r (x_a P_a - x_b Q_b),  r (x_b P_b + x_a Q_a).
-template <typename T, int VEC, int UPL, bool MIX>
-__global__ void __launch_bounds__(32 * kWarps) norm_rope_kernel(const __grid_constant__ RopeArgs g) {
-    const int lane = threadIdx.x & 31, u0 = lane & (g.gl - 1), grp = lane / g.gl, groups = 32 / g.gl;
+template <typename T, int VEC, int UPL, bool MIX, int GL>
+__global__ void __launch_bounds__(32 * kWarps, VEC == 4 ? kBlocks : 1) norm_rope_kernel(
+    const __grid_constant__ RopeArgs g) {
+    const int gl = GL > 0 ? GL : g.gl;
+    const int lane = threadIdx.x & 31, u0 = lane & (gl - 1), grp = lane / gl, groups = 32 / gl;
     const Lane<T, VEC, UPL, MIX> ln(g, u0);
-    const int rq = (g.q.n + groups - 1) / groups, rounds = rq + (g.k.n + groups - 1) / groups;
     const float inv_d = 1.f / (float)g.D;
-    Vals<VEC> wa[2][UPL], wb[2][UPL];
-    ln.weights(g.wq, wa[0], wb[0]);
-    ln.weights(g.wk, wa[1], wb[1]);
     const int64_t step = (int64_t)gridDim.x * kWarps;
     int64_t t = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32;
     int64_t p = position(g, t);
     for (; t < g.T; t += step) {
-        const T *qs = reinterpret_cast<const T *>(g.q.p) + t * g.q.ts, *ks = reinterpret_cast<const T *>(g.k.p) + t * g.k.ts;
-        T *qo = reinterpret_cast<T *>(g.oq.p) + t * g.oq.ts, *ko = reinterpret_cast<T *>(g.ok.p) + t * g.ok.ts;
-        Vals<VEC> c[UPL], n[UPL], pa[UPL], pb[UPL], qa[UPL], qb[UPL];
-        auto turn = [&](const Vals<VEC>(&a)[UPL], const Vals<VEC>(&b)[UPL]) {
+        const int64_t next = position(g, t + step);
 #pragma unroll
-            for (int j = 0; j < UPL; ++j) {
-                pa[j] = a[j] * c[j];
-                pb[j] = b[j] * c[j];
-                qa[j] = a[j] * n[j];
-                qb[j] = negative<VEC>(b[j] * n[j]);
-            }
-        };
-        for (int r0 = 0; r0 < rounds; r0 += kBatch) {
-            Raw<T, VEC> raw[kBatch][UPL];
+        for (int s = 0; s < 2; ++s) {
+            const Heads &in = s ? g.k : g.q;
+            Walk<const T> src(in, t, grp, groups);
+            Walk<T> dst(s ? g.ok : g.oq, t, grp, groups);
+            // weights and angles are read for either kind (from the L1 cache)
+            // rather than held in registers, which more warps need
+            Vals<VEC> pa[UPL], pb[UPL], qa[UPL], qb[UPL];
+            for (int h0 = grp; h0 - grp < in.n; h0 += groups * kBatch) {
+                Raw<T, VEC> raw[kBatch][UPL];
 #pragma unroll
-            for (int e = 0; e < kBatch; ++e) {
-                const bool second = r0 + e >= rq;
-                const int h = (second ? r0 + e - rq : r0 + e) * groups + grp;
-                ln.load(second ? ks + h * g.k.hs : qs + h * g.q.hs, r0 + e < rounds && h < (second ? g.k.n : g.q.n), raw[e]);
-            }
-            if (r0 == 0) {  // once a token, behind its first heads' loads
-                ln.angles(g, p, u0, c, n);
-                p = position(g, t + step);
-                turn(wa[0], wb[0]);
-            }
-#pragma unroll
-            for (int e = 0; e < kBatch; ++e) {
-                const int r = r0 + e;
-                if (r >= rounds) break;
-                if (r == rq) turn(wa[1], wb[1]);
-                const bool second = r >= rq;
-                const int h = (second ? r - rq : r) * groups + grp;
-                Vals<VEC> xa[UPL], xb[UPL], ya[UPL], yb[UPL];
-                Vals<VEC> ss = all<VEC>(0.f);
-#pragma unroll
-                for (int j = 0; j < UPL; ++j) {
-                    unpack<MIX>(raw[e][j], xa[j], xb[j]);
-                    ss = madd(xa[j], xa[j], ss);
-                    ss = madd(xb[j], xb[j], ss);
-                    ya[j] = madd(xb[j], qb[j], xa[j] * pa[j]);
-                    yb[j] = madd(xa[j], qa[j], xb[j] * pb[j]);
+                for (int e = 0; e < kBatch; ++e) {
+                    ln.load(src.at, h0 + e * groups < in.n, raw[e]);
+                    src.at += src.step;
                 }
-                if (g.normalise) {
-                    const Vals<VEC> f = all<VEC>(rsqrtf(group_sum(total(ss), g.gl) * inv_d + g.eps));
+                if (h0 == grp) {  // behind the first heads' loads
+                    Vals<VEC> c[UPL], n[UPL], a[UPL], b[UPL];
+                    ln.angles(g, p, u0, c, n);
+                    ln.weights(s ? g.wk : g.wq, a, b);
 #pragma unroll
                     for (int j = 0; j < UPL; ++j) {
-                        ya[j] = ya[j] * f;
-                        yb[j] = yb[j] * f;
+                        pa[j] = a[j] * c[j];
+                        pb[j] = b[j] * c[j];
+                        qa[j] = a[j] * n[j];
+                        qb[j] = negative<VEC>(b[j] * n[j]);
                     }
                 }
-                if (h < (second ? g.k.n : g.q.n)) ln.store(second ? ko + h * g.ok.hs : qo + h * g.oq.hs, ya, yb);
+#pragma unroll
+                for (int e = 0; e < kBatch; ++e) {
+                    const int h = h0 + e * groups;
+                    if (h - grp >= in.n) break;
+                    Vals<VEC> ya[UPL], yb[UPL], ss = all<VEC>(0.f);
+#pragma unroll
+                    for (int j = 0; j < UPL; ++j) {
+                        Vals<VEC> xa, xb;
+                        unpack<MIX>(raw[e][j], xa, xb);
+                        ss = madd(xb, xb, j ? madd(xa, xa, ss) : xa * xa);
+                        ya[j] = madd(xb, qb[j], xa * pa[j]);
+                        yb[j] = madd(xa, qa[j], xb * pb[j]);
+                    }
+                    if (g.normalise) {
+                        const Vals<VEC> f = all<VEC>(rsqrtf(group_sum<GL>(total(ss), gl) * inv_d + g.eps));
+#pragma unroll
+                        for (int j = 0; j < UPL; ++j) {
+                            ya[j] = ya[j] * f;
+                            yb[j] = yb[j] * f;
+                        }
+                    }
+                    if (h < in.n) ln.store(dst.at, ya, yb);
+                    dst.at += dst.step;
+                }
             }
         }
+        p = next;
     }
 }
 
 // The gradient: g rotated back, u = w g; dx = r u - x r^3 mean(u x), and
 // g x r to the weight's.
-template <typename T, int VEC, int UPL, bool MIX>
-__global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __grid_constant__ RopeArgs g) {
+template <typename T, int VEC, int UPL, bool MIX, int GL>
+__global__ void __launch_bounds__(32 * kWarps, VEC == 4 ? kBlocksGrad : 1) norm_rope_grad_kernel(
+    const __grid_constant__ RopeArgs g) {
     __shared__ float part[kWarps][2][kMaxDim];
-    const int lane = threadIdx.x & 31, u0 = lane & (g.gl - 1), grp = lane / g.gl, groups = 32 / g.gl;
+    const int gl = GL > 0 ? GL : g.gl;
+    const int lane = threadIdx.x & 31, u0 = lane & (gl - 1), grp = lane / gl, groups = 32 / gl;
     const int warp = threadIdx.x / 32;
     const Lane<T, VEC, UPL, MIX> ln(g, u0);
     const float inv_d = 1.f / (float)g.D;
@@ -375,17 +396,18 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
         // q's heads, then k's: each kind adds to its own weight gradient
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const Heads &in = s ? g.k : g.q, &gout = s ? g.gk : g.gq, &out = s ? g.ok : g.oq;
-            const T *xs = reinterpret_cast<const T *>(in.p) + t * in.ts;
-            const T *ys = reinterpret_cast<const T *>(gout.p) + t * gout.ts;
-            T *os = reinterpret_cast<T *>(out.p) + t * out.ts;
+            const Heads &in = s ? g.k : g.q;
+            Walk<const T> xs(in, t, grp, groups), ys(s ? g.gk : g.gq, t, grp, groups);
+            Walk<T> os(s ? g.ok : g.oq, t, grp, groups);
             for (int h0 = grp; h0 - grp < in.n; h0 += groups * kBatchGrad) {
                 Raw<T, VEC> rx[kBatchGrad][UPL], ry[kBatchGrad][UPL];
 #pragma unroll
                 for (int e = 0; e < kBatchGrad; ++e) {
                     const int h = h0 + e * groups;
-                    ln.load(xs + h * in.hs, g.normalise && h < in.n, rx[e]);
-                    ln.load(ys + h * gout.hs, h < in.n, ry[e]);
+                    ln.load(xs.at, g.normalise && h < in.n, rx[e]);
+                    ln.load(ys.at, h < in.n, ry[e]);
+                    xs.at += xs.step;
+                    ys.at += ys.step;
                 }
                 if (first) {
                     ln.angles(g, p, u0, c, n);
@@ -409,11 +431,11 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
                         gb[j] = madd(ya, m[j], yb * c[j]);
                         ua[j] = ga[j] * wa[s][j];
                         ub[j] = gb[j] * wb[s][j];
-                        ss = madd(xb[j], xb[j], madd(xa[j], xa[j], ss));
-                        sp = madd(xb[j], ub[j], madd(xa[j], ua[j], sp));
+                        ss = madd(xb[j], xb[j], j ? madd(xa[j], xa[j], ss) : xa[j] * xa[j]);
+                        sp = madd(xb[j], ub[j], j ? madd(xa[j], ua[j], sp) : xa[j] * ua[j]);
                     }
                     if (g.normalise) {
-                        const float x2 = group_sum(total(ss), g.gl), ux = group_sum(total(sp), g.gl);
+                        const float x2 = group_sum<GL>(total(ss), gl), ux = group_sum<GL>(total(sp), gl);
                         const float r = rsqrtf(x2 * inv_d + g.eps);
                         const Vals<VEC> r4 = all<VEC>(r), f4 = all<VEC>(-r * r * r * ux * inv_d);
 #pragma unroll
@@ -424,7 +446,8 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
                             ub[j] = madd(xb[j], f4, ub[j] * r4);
                         }
                     }
-                    if (h < in.n) ln.store(os + h * out.hs, ua, ub);
+                    if (h < in.n) ln.store(os.at, ua, ub);
+                    os.at += os.step;
                 }
             }
         }
@@ -432,7 +455,7 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rope_grad_kernel(const __gri
     if (!g.part) return;
     // the lanes of the warp's groups that hold the same values, then the
     // block's warps, always in the same order
-    for (int o = g.gl; o < 32; o <<= 1)
+    for (int o = gl; o < 32; o <<= 1)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -565,40 +588,44 @@ dpb_status make_call(const dpb_rope_config *c, const dpb_heads *q, const dpb_hea
 }
 
 template <typename K>
-int rope_blocks(K kernel, int64_t T) {
+int rope_blocks(K kernel) {
     int dev = 0, sms = 1, occ = 1;
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, kernel, 32 * kWarps, 0);
-    const int64_t most = std::min<int64_t>((int64_t)sms * std::max(occ, 1), kMaxBlocks);
-    return (int)std::min<int64_t>((T + kWarps - 1) / kWarps, most);
+    return std::min(sms * std::max(occ, 1), kMaxBlocks);
 }
 
-template <typename T, int VEC, int UPL, bool MIX>
-cudaError_t launch_forward(const RopeArgs &a, cudaStream_t s) {
-    static const int full = rope_blocks(norm_rope_kernel<T, VEC, UPL, MIX>, INT64_MAX / 2);
-    const int blocks = (int)std::min<int64_t>((a.T + kWarps - 1) / kWarps, full);
-    norm_rope_kernel<T, VEC, UPL, MIX><<<blocks, 32 * kWarps, 0, s>>>(a);
-    return cudaGetLastError();
-}
-
-template <typename T, int VEC, int UPL, bool MIX>
-cudaError_t launch_backward_rope(const RopeArgs &a, float *dwq, float *dwk, cudaStream_t s) {
-    static const int full = rope_blocks(norm_rope_grad_kernel<T, VEC, UPL, MIX>, INT64_MAX / 2);
-    const int blocks = (int)std::min<int64_t>((a.T + kWarps - 1) / kWarps, full);
-    if (blocks > 0) norm_rope_grad_kernel<T, VEC, UPL, MIX><<<blocks, 32 * kWarps, 0, s>>>(a);
+template <typename T, int VEC, int UPL, bool MIX, int GL>
+cudaError_t launch_kernels(const RopeArgs &a, bool backward, float *dwq, float *dwk, cudaStream_t s) {
+    const int64_t wanted = (a.T + kWarps - 1) / kWarps;
+    if (!backward) {
+        static const int full = rope_blocks(norm_rope_kernel<T, VEC, UPL, MIX, GL>);
+        norm_rope_kernel<T, VEC, UPL, MIX, GL><<<(int)std::min<int64_t>(wanted, full), 32 * kWarps, 0, s>>>(a);
+        return cudaGetLastError();
+    }
+    static const int full = rope_blocks(norm_rope_grad_kernel<T, VEC, UPL, MIX, GL>);
+    const int blocks = (int)std::min<int64_t>(wanted, full);
+    if (blocks > 0) norm_rope_grad_kernel<T, VEC, UPL, MIX, GL><<<blocks, 32 * kWarps, 0, s>>>(a);
     if (a.part) weight_grad_kernel<<<(2 * a.D + 31) / 32, 1024, 0, s>>>(a.part, blocks, a.D, dwq, dwk);
     return cudaGetLastError();
 }
 
-// By type, by whether rows are read 4 values at a time, and by layout.
+// By type, by whether rows are read 4 values at a time, by layout, and by the
+// lanes of a head: the usual two counts have their sums unrolled.
+template <typename T, int VEC, int UPL, bool MIX>
+cudaError_t launch_lanes(const Call &c, bool backward, float *dwq, float *dwk, cudaStream_t s) {
+    if constexpr (VEC == 4) {
+        if (c.a.gl == 8) return launch_kernels<T, VEC, UPL, MIX, 8>(c.a, backward, dwq, dwk, s);
+        if (c.a.gl == 16) return launch_kernels<T, VEC, UPL, MIX, 16>(c.a, backward, dwq, dwk, s);
+    }
+    return launch_kernels<T, VEC, UPL, MIX, 0>(c.a, backward, dwq, dwk, s);
+}
+
 template <typename T, int VEC, int UPL>
 cudaError_t launch_kind(const Call &c, bool backward, float *dwq, float *dwk, cudaStream_t s) {
-    if (c.a.interleaved)
-        return backward ? launch_backward_rope<T, VEC, UPL, true>(c.a, dwq, dwk, s)
-                        : launch_forward<T, VEC, UPL, true>(c.a, s);
-    return backward ? launch_backward_rope<T, VEC, UPL, false>(c.a, dwq, dwk, s)
-                    : launch_forward<T, VEC, UPL, false>(c.a, s);
+    return c.a.interleaved ? launch_lanes<T, VEC, UPL, true>(c, backward, dwq, dwk, s)
+                           : launch_lanes<T, VEC, UPL, false>(c, backward, dwq, dwk, s);
 }
 
 cudaError_t launch_rope(const Call &c, int dtype, bool backward, float *dwq, float *dwk, cudaStream_t s) {

@@ -10,6 +10,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -64,18 +66,24 @@ class Config(ctypes.Structure):
                 "field_poly": self.field_poly, "generator_seed": self.generator_seed, "scoring": self.scoring}
 
 
-class RopeConfig(ctypes.Structure):
-    _fields_ = [("tokens", ctypes.c_int64), ("heads_q", ctypes.c_int32), ("heads_k", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
-                ("normalise", ctypes.c_int32), ("positions_n", ctypes.c_int32), ("dtype", ctypes.c_int32),
-                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+# dpb_rope_config, dpb_attention_config and up to eight dpb_heads, as they lie in memory
+_ROPE = struct.Struct("=q8ifi")
+_ATTENTION = struct.Struct("=qq8ifi")
+_ROWS = {n: struct.Struct(f"={3 * n}q") for n in (4, 6, 8)}
 
 
-class AttentionConfig(ctypes.Structure):
-    _fields_ = [("total_q", ctypes.c_int64), ("total_k", ctypes.c_int64), ("seqs", ctypes.c_int32),
-                ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32), ("heads_q", ctypes.c_int32),
-                ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32),
-                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+class _Arguments(threading.local):
+    """This thread's memory for a call's config (at `at`) and dpb_heads (at
+    `rows`, 24 bytes each): written anew for every call, cheaper than new
+    ctypes objects."""
+
+    def __init__(self):
+        self.buf = ctypes.create_string_buffer(64 + 24 * 8)
+        self.at = ctypes.addressof(self.buf)
+        self.rows = self.at + 64
+
+
+_arguments = _Arguments()
 
 
 class AdamWConfig(ctypes.Structure):
@@ -125,8 +133,7 @@ def load(path: Optional[str] = None):
     lib.dpb_stats_accumulate.argtypes = [vp, vp, i64, vp, vp, vp, ctypes.c_int32, vp, vp, sz, vp]
     lib.dpb_stats_update.argtypes = [vp, vp, ctypes.c_float, vp, vp, vp]
     lib.dpb_forward.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    # dpb_heads arguments are addresses within one array (_rows_array)
-    hp, rc, ac = vp, ctypes.POINTER(RopeConfig), ctypes.POINTER(AttentionConfig)
+    hp = rc = ac = vp  # addresses within _Arguments
     lib.dpb_qk_norm_rope.argtypes = [rc, hp, hp, vp, vp, vp, vp, vp, hp, hp, vp, sz, vp]
     lib.dpb_qk_norm_rope_backward.argtypes = [rc, hp, hp, hp, hp, vp, vp, vp, vp, vp, hp, hp, vp, vp, vp, sz, vp]
     lib.dpb_rope_workspace_size.argtypes = [rc, ctypes.POINTER(sz)]
@@ -501,9 +508,6 @@ def _head_rows(t: torch.Tensor, name: str, dtype, shape, device):
     return t.data_ptr(), st[0], st[1]
 
 
-_rows_array = ctypes.c_int64 * 24  # up to 8 dpb_heads side by side, 24 bytes each
-
-
 def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, device):
     """Address of a contiguous tensor of `numel` values (None: None)."""
     if t is None:
@@ -549,7 +553,7 @@ def rope_tables(positions: int, rot_dim: int, base: float = 10000.0, scaling: Op
 
 
 def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise):
-    """(config, addresses of the weights, tables and positions)"""
+    """Writes the config; addresses of the weights, tables and positions."""
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [tokens, heads, dim]")
     T, hq, D = q.shape
@@ -568,8 +572,9 @@ def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved
     at = (_dense(weight_q, "weight_q", dt, D, dev), _dense(weight_k, "weight_k", dt, D, dev),
           _dense(cos, "cos", torch.float32, rows * rot // 2, dev), _dense(sin, "sin", torch.float32, rows * rot // 2, dev),
           _dense(positions, "positions", torch.int32, T, dev))
-    return RopeConfig(T, hq, k.shape[1], D, rot, bool(interleaved), bool(normalise), rows,
-                      BF16 if dt is torch.bfloat16 else F32, eps, 0), at
+    _ROPE.pack_into(_arguments.buf, 0, T, hq, k.shape[1], D, rot, bool(interleaved), bool(normalise), rows,
+                    BF16 if dt is torch.bfloat16 else F32, eps, 0)
+    return at
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, weight_q=None, weight_k=None, cos=None, sin=None, positions=None,
@@ -583,15 +588,15 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, weight_q=None, weight_k=None,
     if _away(dev, stream):
         return _elsewhere(qk_norm_rope, stream, dev, (q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved,
                                                       normalise, q_out, k_out, workspace), {})
-    c, at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
-    dt, sq, sk, s = q.dtype, q.shape, k.shape, _raw_stream(dev)
+    at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
+    dt, sq, sk, s, a = q.dtype, q.shape, k.shape, _raw_stream(dev), _arguments
     q_out = torch.empty(sq, dtype=dt, device=dev) if q_out is None else q_out
     k_out = torch.empty(sk, dtype=dt, device=dev) if k_out is None else k_out
     ws = _shared_workspace(256, dev, s) if workspace is None else workspace
-    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+    _ROWS[4].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(q_out, "q_out", dt, sq, dev), *_head_rows(k_out, "k_out", dt, sk, dev))
-    h = ctypes.addressof(rows)
-    _check(load().dpb_qk_norm_rope(c, h, h + 24, *at, h + 48, h + 72, ws.data_ptr(), ws.nbytes, s))
+    h = a.rows
+    _check(load().dpb_qk_norm_rope(a.at, h, h + 24, *at, h + 48, h + 72, ws.data_ptr(), ws.nbytes, s))
     return q_out, k_out
 
 
@@ -607,8 +612,8 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Te
         return _elsewhere(qk_norm_rope_backward, stream, dev,
                           (q, k, grad_q_out, grad_k_out, weight_q, weight_k, cos, sin, positions, eps, interleaved,
                            normalise, weight_grads, grad_q, grad_k, workspace), {})
-    c, at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
-    lib, dt, sq, sk, s = load(), q.dtype, q.shape, k.shape, _raw_stream(dev)
+    at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
+    lib, dt, sq, sk, s, a = load(), q.dtype, q.shape, k.shape, _raw_stream(dev), _arguments
     grad_q = torch.empty(sq, dtype=dt, device=dev) if grad_q is None else grad_q
     grad_k = torch.empty(sk, dtype=dt, device=dev) if grad_k is None else grad_k
     D = sq[2]
@@ -616,20 +621,20 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Te
     gp = None if gw is None else gw.data_ptr()
     if workspace is None:
         n = ctypes.c_size_t()
-        _check(lib.dpb_rope_workspace_size(c, n))
+        _check(lib.dpb_rope_workspace_size(a.at, n))
         workspace = _shared_workspace(n.value, dev, s)
-    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+    _ROWS[6].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(grad_q_out, "grad_q_out", dt, sq, dev),
                        *_head_rows(grad_k_out, "grad_k_out", dt, sk, dev),
                        *_head_rows(grad_q, "grad_q", dt, sq, dev), *_head_rows(grad_k, "grad_k", dt, sk, dev))
-    h = ctypes.addressof(rows)
-    _check(lib.dpb_qk_norm_rope_backward(c, h, h + 24, h + 48, h + 72, *at, h + 96, h + 120, gp,
+    h = a.rows
+    _check(lib.dpb_qk_norm_rope_backward(a.at, h, h + 24, h + 48, h + 72, *at, h + 96, h + 120, gp,
                                          None if gp is None else gp + 4 * D, workspace.data_ptr(), workspace.nbytes, s))
     return (grad_q, grad_k) + ((None, None) if gw is None else (gw[0], gw[1]))
 
 
 def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
-    """(config, addresses of the offsets)"""
+    """Writes the config; addresses of the offsets."""
     if q.dim() != 3 or k.dim() != 3 or q.dtype is not torch.bfloat16:
         raise ValueError(f"q, k and v must be bfloat16 tensors [tokens, heads, dim], got {q.dtype} {list(q.shape)}")
     Tq, Hq, D = q.shape
@@ -646,9 +651,10 @@ def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
         if seqs < 0:
             raise ValueError("cu_q must have one entry more than there are sequences")
     at = (_dense(cu_q, "cu_q", torch.int32, seqs + 1, q.device), _dense(cu_k, "cu_k", torch.int32, seqs + 1, q.device))
-    return AttentionConfig(Tq, Tk, seqs, Tq if max_q is None or max_q > Tq else max_q,
-                           Tk if max_k is None or max_k > Tk else max_k, Hq, Hk, D, bool(causal), BF16,
-                           D ** -0.5 if scale is None else scale, 0), at
+    _ATTENTION.pack_into(_arguments.buf, 0, Tq, Tk, seqs, Tq if max_q is None or max_q > Tq else max_q,
+                         Tk if max_k is None or max_k > Tk else max_k, Hq, Hk, D, bool(causal), BF16,
+                         D ** -0.5 if scale is None else scale, 0)
+    return at
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, cu_k=None,
@@ -663,18 +669,18 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=No
     if _away(dev, stream):
         return _elsewhere(attention_forward, stream, dev,
                           (q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, out, lse, workspace), {})
-    c, at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
-    dt, sq, s = torch.bfloat16, q.shape, _raw_stream(dev)
-    sk = torch.Size((k.shape[0], k.shape[1], sq[2]))
+    at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
+    dt, sq, s, a = torch.bfloat16, q.shape, _raw_stream(dev), _arguments
+    sk = k.shape if k.shape[2] == sq[2] else (*k.shape[:2], sq[2])
     if out is None:
         out = torch.empty(sq, dtype=dt, device=dev)
     if lse is None:
         lse = torch.empty((sq[1], sq[0]), dtype=torch.float32, device=dev)
     ws = _shared_workspace(256, dev, s) if workspace is None else workspace
-    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+    _ROWS[4].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(v, "v", dt, sk, dev), *_head_rows(out, "out", dt, sq, dev))
-    h = ctypes.addressof(rows)
-    _check(load().dpb_attention_forward(c, h, h + 24, h + 48, *at, h + 72,
+    h = a.rows
+    _check(load().dpb_attention_forward(a.at, h, h + 24, h + 48, *at, h + 72,
                                         _dense(lse, "lse", torch.float32, sq[0] * sq[1], dev), ws.data_ptr(), ws.nbytes, s))
     return out, lse
 
@@ -690,22 +696,22 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
         return _elsewhere(attention_backward, stream, dev,
                           (q, k, v, o, lse, grad_o, cu_q, cu_k, max_q, max_k, causal, scale, grad_q, grad_k, grad_v,
                            workspace), {})
-    c, at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
-    lib, dt, sq, s = load(), torch.bfloat16, q.shape, _raw_stream(dev)
-    sk = torch.Size((k.shape[0], k.shape[1], sq[2]))
+    at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
+    lib, dt, sq, s, a = load(), torch.bfloat16, q.shape, _raw_stream(dev), _arguments
+    sk = k.shape if k.shape[2] == sq[2] else (*k.shape[:2], sq[2])
     grad_q = torch.empty(sq, dtype=dt, device=dev) if grad_q is None else grad_q
     grad_k = torch.empty(sk, dtype=dt, device=dev) if grad_k is None else grad_k
     grad_v = torch.empty(sk, dtype=dt, device=dev) if grad_v is None else grad_v
     if workspace is None:
         n = ctypes.c_size_t()
-        _check(lib.dpb_attention_workspace_size(c, n))
+        _check(lib.dpb_attention_workspace_size(a.at, n))
         workspace = _shared_workspace(n.value, dev, s)
-    rows = _rows_array(*_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
+    _ROWS[8].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(v, "v", dt, sk, dev), *_head_rows(o, "o", dt, sq, dev),
                        *_head_rows(grad_o, "grad_o", dt, sq, dev), *_head_rows(grad_q, "grad_q", dt, sq, dev),
                        *_head_rows(grad_k, "grad_k", dt, sk, dev), *_head_rows(grad_v, "grad_v", dt, sk, dev))
-    h = ctypes.addressof(rows)
-    _check(lib.dpb_attention_backward(c, h, h + 24, h + 48, h + 72,
+    h = a.rows
+    _check(lib.dpb_attention_backward(a.at, h, h + 24, h + 48, h + 72,
                                       _dense(lse, "lse", torch.float32, sq[0] * sq[1], dev), h + 96, *at, h + 120, h + 144,
                                       h + 168, workspace.data_ptr(), workspace.nbytes, s))
     return grad_q, grad_k, grad_v

@@ -560,13 +560,18 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
 // each, so that a block's arithmetic takes half as long between its products.
 template <int DP_>
 struct GradShape {
-    static constexpr int DP = DP_, BN = 128, NS = DP == 64 ? 6 : 4;
+    static constexpr int DP = DP_, BN = 128, NS = DP == 64 ? 8 : 4;
     static constexpr int kTile = kRows * DP * 2;
-    static constexpr int kThreads = 384, kCopier = 8, kIssuer = 9;  // 2 x 4 row warps, then these two (and 2 idle)
+    // 2 x 4 row warps, the copying warp, and two that issue products: one those
+    // of two tiles in shared memory, one those that sum what the row warps made
+    static constexpr int kThreads = 384, kCopier = 8, kIssuer = 9, kSummer = 10;
     static constexpr int kRegsRow = 208, kRegsOther = 88;           // 256 x 208 + 128 x 88 = 384 x 168
     static constexpr int kColS = 0, kColG = 128, kColSum = 256;  // S, the gradient of P, the sums
     static constexpr int kColumns = 512;
-    static constexpr int kBars = 2 + 2 * NS + 1 + 8;
+    static constexpr int kBars = 2 + 2 * NS + 1 + 9;
+    // the keys' gradient: P and dS have columns of their own where there is room
+    static constexpr bool kOwn = 256 + 2 * DP + 128 <= 512;
+    static constexpr int kColP = kOwn ? 256 + 2 * DP : kColS, kColD = kOwn ? kColP + 64 : kColG, kHalf = kOwn ? 32 : 64;
     static constexpr int kVec = 8 * 128 * 4;  // a warp's lse and delta of its 64 columns
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + 8 * kBars + 16;
     using Slots = Ring<NS, kTile, NS == 4>;
@@ -596,8 +601,8 @@ __device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t hal
 template <class C>
 struct GradBars {
     // each of the two tiles is there; S and the gradient of P are there, have been read; dS
-    // (and P, for the keys' gradient) is there; dS's product is done; all is done
-    uint32_t tile_full, s_full, g_full, w_done, done, s_read, g_read, w_full, v_full;
+    // (and P, for the keys' gradient) is there; its product is done; all is done
+    uint32_t tile_full, s_full, g_full, w_done, v_done, done, s_read, g_read, w_full, v_full;
     typename C::Slots ring;
     uint32_t *slot;
     __device__ __forceinline__ GradBars(uint8_t *smem) {
@@ -607,17 +612,18 @@ struct GradBars {
         s_full = tile_full + 8 * (3 + 2 * C::NS);
         g_full = s_full + 8;
         w_done = s_full + 16;
-        done = s_full + 24;
-        s_read = s_full + 32;  // from here on arrived on by the 8 row warps
-        g_read = s_full + 40;
-        w_full = s_full + 48;
-        v_full = s_full + 56;
+        v_done = s_full + 24;
+        done = s_full + 32;
+        s_read = s_full + 40;  // from here on arrived on by the 8 row warps
+        g_read = s_full + 48;
+        w_full = s_full + 56;
+        v_full = s_full + 64;
         slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
     }
-    __device__ __forceinline__ void make() const {
+    __device__ __forceinline__ void make(int issuers) const {
         for (int i = threadIdx.x & 31; i < C::kBars; i += 32) {
             const uint32_t b = tile_full + 8 * i;
-            bar_init(b, b >= s_read ? 8 : 1);
+            bar_init(b, b >= s_read ? 8 : b == done ? issuers : 1);
         }
         bar_init_fence();
         __syncwarp();
@@ -637,7 +643,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
     const int si = rest % a.seqs, tile = a.tiles - 1 - rest / a.seqs;  // the longest rows first
     const Offsets offsets = load_offsets(a, si);
     const GradBars<C> bars(smem);
-    if (warp == C::kCopier) bars.make();
+    if (warp == C::kCopier) bars.make(2);
     const Seq q = sequence(a, offsets);
     if (!q.ok) {
         if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
@@ -676,45 +682,37 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
             if (blocks > 0)
                 for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
         }
-    } else if (warp == C::kIssuer) {
-        tmem_alloc(smem_addr(bars.slot), C::kColumns);
+    } else if (warp >= 8) {
+        if (warp == C::kIssuer) tmem_alloc(smem_addr(bars.slot), C::kColumns);
         fence_before();
         setup_wait<C::kThreads>();
         fence_after();
         const uint32_t tmem = *bars.slot;
-        if (blocks > 0 && elect_one()) {
+        if (blocks > 0 && warp == C::kIssuer && elect_one()) {
+            // S and the gradient of P of each block, once those of the block
+            // before have been read
             const uint32_t q_addr = smem_addr(smem), g_addr = q_addr + C::kTile;
-            auto scores = [&](int j) {
+            for (int j = 0; j < blocks; ++j) {
+                failed = !ring.wait_full(2 * j) || !bar_wait(j ? bars.s_read : bars.tile_full, j ? (j - 1) & 1 : 0, kTries);
+                if (failed) break;
+                fence_after();
                 tile_product<DP>(tmem + C::kColS, q_addr, ring.addr(2 * j));
                 mma_commit(bars.s_full);
-            };
-            auto grads = [&](int j) {
+                failed = !ring.wait_full(2 * j + 1) ||
+                         !bar_wait(j ? bars.g_read : bars.tile_full + 8, j ? (j - 1) & 1 : 0, kTries);
+                if (failed) break;
+                fence_after();
                 tile_product<DP>(tmem + C::kColG, g_addr, ring.addr(2 * j + 1));
                 mma_commit(bars.g_full);
                 mma_commit(ring.empty_bar(2 * j + 1));
-            };
-            failed = !bar_wait(bars.tile_full, 0, kTries) || !ring.wait_full(0);
-            if (!failed) {
-                fence_after();
-                scores(0);
             }
-            failed = !bar_wait(bars.tile_full + 8, 0, kTries) || failed || !ring.wait_full(1);
-            if (!failed) {
-                fence_after();
-                grads(0);
-            }
-            for (int j = 0; j < blocks && !failed; ++j) {
-                if (j + 1 < blocks) {
-                    // the next block's products, as soon as this one's have been read
-                    failed = !ring.wait_full(2 * j + 2) || !bar_wait(bars.s_read, j & 1, kTries);
-                    if (failed) break;
-                    fence_after();
-                    scores(j + 1);
-                    failed = !ring.wait_full(2 * j + 3) || !bar_wait(bars.g_read, j & 1, kTries);
-                    if (failed) break;
-                    fence_after();
-                    grads(j + 1);
-                }
+            // every product, and every arrival that it makes, is done before
+            // the block's memory is given back
+            mma_commit(bars.done);
+            failed |= !bar_wait(bars.done, 0, kTries);
+        } else if (blocks > 0 && warp == C::kSummer && elect_one()) {
+            // dQ += dS K (K's scores are done: the row warps had them)
+            for (int j = 0; j < blocks; ++j) {
                 failed = !bar_wait(bars.w_full, j & 1, kTries);
                 if (failed) break;
                 fence_after();
@@ -726,8 +724,6 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
             failed |= !bar_wait(bars.done, 0, kTries);
         }
         __syncwarp();
-    } else if (warp > C::kIssuer) {
-        setup_wait<C::kThreads>();
     } else {
         take_registers<C::kRegsRow>();
         fence_before();
@@ -867,7 +863,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
     const int si = rest % a.seqs, tile = rest / a.seqs;  // causal: the first keys are seen by most queries
     const Offsets offsets = load_offsets(a, si);
     const GradBars<C> bars(smem);
-    if (warp == C::kCopier) bars.make();
+    if (warp == C::kCopier) bars.make(C::kOwn ? 2 : 1);
     const Seq q = sequence(a, offsets);
     if (!q.ok) {
         if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
@@ -913,58 +909,89 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             if (blocks > 0)
                 for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
         }
-    } else if (warp == C::kIssuer) {
-        tmem_alloc(smem_addr(bars.slot), C::kColumns);
+    } else if (warp >= 8) {
+        if (warp == C::kIssuer) tmem_alloc(smem_addr(bars.slot), C::kColumns);
         fence_before();
         setup_wait<C::kThreads>();
         fence_after();
         const uint32_t tmem = *bars.slot;
-        if (blocks > 0 && elect_one()) {
-            const uint32_t k_addr = smem_addr(smem), v_addr = k_addr + C::kTile;
-            auto scores = [&](int it) {
-                if (!ring.wait_full(2 * it)) return false;
-                fence_after();
-                tile_product<DP>(tmem + C::kColS, k_addr, ring.addr(2 * it));
-                mma_commit(bars.s_full);
-                return true;
-            };
-            auto grads = [&](int it) {
-                if (!ring.wait_full(2 * it + 1)) return false;
-                fence_after();
-                tile_product<DP>(tmem + C::kColG, v_addr, ring.addr(2 * it + 1));
-                mma_commit(bars.g_full);
-                return true;
-            };
-            failed = !bar_wait(bars.tile_full, 0, kTries) || !scores(0);
-            failed = !bar_wait(bars.tile_full + 8, 0, kTries) || failed || !grads(0);
-            // P^T takes the place of S^T, dS^T that of the gradient of P^T:
-            // the next product into either comes after the one that reads
-            // it (products run in the order of their issue). While the rows'
-            // arithmetic makes P^T, dK and the next gradient of P^T are computed;
-            // while it makes dS^T, dV and the next S^T.
-            for (int it = 0; it < blocks && !failed; ++it) {
-                const bool more = it + 1 < blocks;
+        const uint32_t k_addr = smem_addr(smem), v_addr = k_addr + C::kTile;
+        auto scores = [&](int it) {
+            fence_after();
+            tile_product<DP>(tmem + C::kColS, k_addr, ring.addr(2 * it));
+            mma_commit(bars.s_full);
+        };
+        auto grads = [&](int it) {
+            fence_after();
+            tile_product<DP>(tmem + C::kColG, v_addr, ring.addr(2 * it + 1));
+            mma_commit(bars.g_full);
+        };
+        auto sum_v = [&](int it) {
+            fence_after();
+            sum_product<DP>(tmem + kColV, tmem + C::kColP, C::kHalf, ring.addr(2 * it + 1), it > 0);
+        };
+        auto sum_k = [&](int it) {
+            fence_after();
+            sum_product<DP>(tmem + kColK, tmem + C::kColD, C::kHalf, ring.addr(2 * it), it > 0);
+        };
+        if (C::kOwn && blocks > 0 && warp == C::kIssuer && elect_one()) {
+            // P^T and dS^T have columns of their own: the next S^T and gradient
+            // of P^T are computed as soon as these have been read
+            for (int it = 0; it < blocks; ++it) {
+                failed = !ring.wait_full(2 * it) ||
+                         !bar_wait(it ? bars.s_read : bars.tile_full, it ? (it - 1) & 1 : 0, kTries);
+                if (failed) break;
+                scores(it);
+                failed = !ring.wait_full(2 * it + 1) ||
+                         !bar_wait(it ? bars.g_read : bars.tile_full + 8, it ? (it - 1) & 1 : 0, kTries);
+                if (failed) break;
+                grads(it);
+            }
+            mma_commit(bars.done);
+            failed |= !bar_wait(bars.done, 0, kTries);
+        } else if (C::kOwn && blocks > 0 && warp == C::kSummer && elect_one()) {
+            for (int it = 0; it < blocks; ++it) {
                 failed = !bar_wait(bars.v_full, it & 1, kTries);
                 if (failed) break;
-                fence_after();
-                sum_product<DP>(tmem + kColV, tmem + C::kColS, 64, ring.addr(2 * it + 1), it > 0);
-                mma_commit(ring.empty_bar(2 * it + 1));
-                if (more && !scores(it + 1)) failed = true;
-                if (failed || !bar_wait(bars.w_full, it & 1, kTries)) {
-                    failed = true;
-                    break;
-                }
-                fence_after();
-                sum_product<DP>(tmem + kColK, tmem + C::kColG, 64, ring.addr(2 * it), it > 0);
+                sum_v(it);
+                mma_commit(bars.v_done);
+                failed = !bar_wait(bars.w_full, it & 1, kTries);
+                if (failed) break;
+                sum_k(it);
+                mma_commit(bars.w_done);
+                // the other products of this block are done: the row warps had them
                 mma_commit(ring.empty_bar(2 * it));
-                if (more && !grads(it + 1)) failed = true;
+                mma_commit(ring.empty_bar(2 * it + 1));
+            }
+            mma_commit(bars.done);
+            failed |= !bar_wait(bars.done, 0, kTries);
+        } else if (!C::kOwn && blocks > 0 && warp == C::kIssuer && elect_one()) {
+            // P^T takes the place of S^T, dS^T that of the gradient of P^T,
+            // and the next product into either comes after the one that reads
+            // it (products run in the order of their issue): while the rows'
+            // arithmetic makes P^T, dK and the next gradient are computed, while
+            // it makes dS^T, dV and the next S^T.
+            failed = !bar_wait(bars.tile_full, 0, kTries) || !ring.wait_full(0);
+            if (!failed) scores(0);
+            failed = failed || !bar_wait(bars.tile_full + 8, 0, kTries) || !ring.wait_full(1);
+            if (!failed) grads(0);
+            for (int it = 0; it < blocks && !failed; ++it) {
+                const bool more = it + 1 < blocks;
+                failed = (more && !ring.wait_full(2 * it + 2)) || !bar_wait(bars.v_full, it & 1, kTries);
+                if (failed) break;
+                sum_v(it);
+                mma_commit(ring.empty_bar(2 * it + 1));
+                if (more) scores(it + 1);
+                failed = (more && !ring.wait_full(2 * it + 3)) || !bar_wait(bars.w_full, it & 1, kTries);
+                if (failed) break;
+                sum_k(it);
+                mma_commit(ring.empty_bar(2 * it));
+                if (more) grads(it + 1);
             }
             mma_commit(bars.done);
             failed |= !bar_wait(bars.done, 0, kTries);
         }
         __syncwarp();
-    } else if (warp > C::kIssuer) {
-        setup_wait<C::kThreads>();
     } else {
         take_registers<C::kRegsRow>();
         fence_before();
@@ -975,6 +1002,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         const int j = j0 + (threadIdx.x & 127);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
         const uint32_t s_addr = lanes + C::kColS + 64 * half, g_addr = lanes + C::kColG + 64 * half;
+        const uint32_t p_addr = lanes + C::kColP + C::kHalf * half, d_addr = lanes + C::kColD + C::kHalf * half;
         float *vec = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile) + warp * 128;
         // this lane's share of its columns' -lse x log2 e (minus infinity for
         // rows that are not there or see nothing: probability 0) and -delta
@@ -1022,6 +1050,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 tmem_load(s_addr + 32, x[1]);
                 load_wait(x[0]);
                 load_wait(x[1]);
+                if (C::kOwn) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(bars.s_read);
+                }
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
                     const ulonglong2 l = *reinterpret_cast<const ulonglong2 *>(vec + c);
@@ -1041,7 +1074,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             }
 #pragma unroll
             for (int c = 0; c < 64; c += 2) w[c / 2] = pack_bf16(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
-            tmem_store(s_addr, w);
+            if (C::kOwn && it > 0 && !__all_sync(kFull, bar_wait(bars.v_done, (it - 1) & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+            tmem_store(p_addr, w);
             store_wait();
             fence_before();
             __syncwarp();
@@ -1056,6 +1094,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             tmem_load(g_addr + 32, g[1]);
             load_wait(g[0]);
             load_wait(g[1]);
+            if (C::kOwn) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(bars.g_read);
+            }
             if (!whole) {
 #pragma unroll
                 for (int c = 0; c < 64; ++c)
@@ -1072,7 +1115,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                     w[e / 2] = pack_bf16(y.x, y.y);
                 }
             }
-            tmem_store(g_addr, w);
+            if (C::kOwn && it > 0 && !__all_sync(kFull, bar_wait(bars.w_done, (it - 1) & 1, kTries))) {
+                failed = true;
+                break;
+            }
+            fence_after();
+            tmem_store(d_addr, w);
             store_wait();
             fence_before();
             __syncwarp();
@@ -1225,7 +1273,7 @@ cudaError_t launch_tiles(AttnArgs &a, int tiles, int heads, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-using Fwd64 = FwdShape<64, 128, 6>;
+using Fwd64 = FwdShape<64, 128, 8>;
 using Fwd128 = FwdShape<128, 128, 4>;
 using Grad64 = GradShape<64>;
 using Grad128 = GradShape<128>;

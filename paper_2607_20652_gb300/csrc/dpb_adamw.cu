@@ -24,11 +24,11 @@ constexpr int kThreads = 64;
 constexpr int kPer = 8;                    // values a thread
 constexpr int kRound = kThreads * kPer;    // values a block takes at a time
 // Rounds a block: 32-bit states keep enough loads in flight with one. 8-bit
-// ones compute longer on fewer bytes, so a block loads the next of eight rounds
-// while it computes one, and its start is spread over more (203 M bf16
-// parameters: 432 us; one round of 256 threads 547, four of 128 threads 475).
-template <bool F8>
-constexpr int kChunk = (F8 ? 8 : 1) * kRound;
+// ones compute longer on fewer bytes, so a block loads its next round while it
+// computes one, and its start is spread over up to eight (203 M bf16 parameters:
+// 432 us; one round of 256 threads 547, four of 128 threads 475) as long as
+// there are some waves of blocks (14 M fp32 parameters: 57 us with eight).
+constexpr int kMostRounds = 8, kWaves = 6, kResident = 152 * 14;
 constexpr int kBlock = 32 * kPer;          // values that share a scale
 constexpr float kTop = 448.f;              // largest e4m3 value
 constexpr int kFew = 40, kMany = 440;      // tensors a launch (4 KB and 32 KB of kernel arguments)
@@ -48,6 +48,7 @@ struct Table {
     Tensor t[N];
     uint8_t wide[N];  // every pointer aligned for whole vectors
     int count;
+    int chunk;  // values a block
 };
 
 struct Hyper {
@@ -335,8 +336,8 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
 
 // The next values' loads are under way while these are computed.
 template <typename T, bool F8, bool WIDE>
-__device__ __forceinline__ void step_chunk(const Tensor t, int64_t i0, const Hyper &h, float gs) {
-    const int64_t end = min(i0 + kChunk<F8>, (t.n + kBlock - 1) / kBlock * kBlock);  // whole warps
+__device__ __forceinline__ void step_chunk(const Tensor t, int64_t i0, int chunk, const Hyper &h, float gs) {
+    const int64_t end = min(i0 + chunk, (t.n + kBlock - 1) / kBlock * kBlock);  // whole warps
     if (i0 >= end) return;
     Loaded<T, F8> a, b;
     load_values<T, F8, WIDE>(t, i0, a);
@@ -362,16 +363,17 @@ __global__ void __launch_bounds__(kThreads, 14) adamw_kernel(const __grid_consta
     }
     const float gs = h.grad_scale ? *h.grad_scale : 1.f;
     if (!(fabsf(gs) <= 3.402823466e38f)) return;
-    const int64_t i0 = (chunk - tab.first[lo]) * kChunk<F8> + (int64_t)threadIdx.x * kPer;
+    const int64_t i0 = (chunk - tab.first[lo]) * tab.chunk + (int64_t)threadIdx.x * kPer;
     if (tab.wide[lo])
-        step_chunk<T, F8, true>(tab.t[lo], i0, h, gs);
+        step_chunk<T, F8, true>(tab.t[lo], i0, tab.chunk, h, gs);
     else
-        step_chunk<T, F8, false>(tab.t[lo], i0, h, gs);
+        step_chunk<T, F8, false>(tab.t[lo], i0, tab.chunk, h, gs);
 }
 
 template <typename T, bool F8, int N>
-cudaError_t launch_group(const dpb_adamw_tensor *ts, int n, int64_t at, const Hyper &h, cudaStream_t s) {
+cudaError_t launch_group(const dpb_adamw_tensor *ts, int n, int64_t at, int rounds, const Hyper &h, cudaStream_t s) {
     Table<N> tab;
+    tab.chunk = rounds * kRound;
     tab.count = 0;
     tab.first[0] = 0;
     const size_t sa = F8 ? 8 : 16;
@@ -383,7 +385,7 @@ cudaError_t launch_group(const dpb_adamw_tensor *ts, int n, int64_t at, const Hy
             tab.t[c] = {x.param, x.grad, x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, x.count, at};
             tab.wide[c] = is_aligned(x.param, 16) && is_aligned(x.grad, 16) && is_aligned(x.exp_avg, sa) &&
                           is_aligned(x.exp_avg_sq, sa);
-            tab.first[c + 1] = tab.first[c] + (x.count + kChunk<F8> - 1) / kChunk<F8>;
+            tab.first[c + 1] = tab.first[c] + (x.count + tab.chunk - 1) / tab.chunk;
         }
         at += padded;
     }
@@ -395,11 +397,13 @@ cudaError_t launch_group(const dpb_adamw_tensor *ts, int n, int64_t at, const Hy
 
 template <typename T, bool F8>
 cudaError_t launch_adamw(const dpb_adamw_tensor *ts, int n, const Hyper &h, cudaStream_t s) {
-    int64_t at = 0;
+    int64_t at = 0, all = 0;
+    for (int i = 0; i < n; ++i) all += ts[i].count;
+    const int rounds = F8 ? (int)std::min<int64_t>(kMostRounds, 1 + all / ((int64_t)kWaves * kResident * kRound)) : 1;
     for (int i = 0; i < n; i += kMany) {
         const int k = std::min(kMany, n - i);
-        const cudaError_t e = k <= kFew ? launch_group<T, F8, kFew>(ts + i, k, at, h, s)
-                                        : launch_group<T, F8, kMany>(ts + i, k, at, h, s);
+        const cudaError_t e = k <= kFew ? launch_group<T, F8, kFew>(ts + i, k, at, rounds, h, s)
+                                        : launch_group<T, F8, kMany>(ts + i, k, at, rounds, h, s);
         if (e != cudaSuccess) return e;
         for (int j = 0; j < k; ++j) at += (ts[i + j].count + kBlock - 1) / kBlock * kBlock;
     }

@@ -1004,8 +1004,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         const uint32_t s_addr = lanes + C::kColS + 64 * half, g_addr = lanes + C::kColG + 64 * half;
         const uint32_t p_addr = lanes + C::kColP + C::kHalf * half, d_addr = lanes + C::kColD + C::kHalf * half;
         float *vec = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile) + warp * 128;
-        // this lane's share of its columns' -lse x log2 e (minus infinity for
-        // rows that are not there or see nothing: probability 0) and -delta
+        // this lane's share of its columns' lse and delta, loaded a block ahead
+        // and not looked at before the block is there
         float nl[2], nd[2];
         int h = head * a.group, b = b0;  // of the next block fetched
         auto fetch = [&]() {
@@ -1015,9 +1015,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 nl[e] = -INFINITY, nd[e] = 0.f;
                 if (i < q.n) {
                     const int64_t at = (int64_t)h * a.total_q + q.q0 + i;
-                    const float l = a.lse[at];
-                    nl[e] = l == -INFINITY ? -INFINITY : -l * kLog2e;
-                    nd[e] = -a.delta[at];
+                    nl[e] = a.lse[at];
+                    nd[e] = a.delta[at];
                 }
             }
             if (++b == b0 + per_head) b = b0, ++h;
@@ -1029,8 +1028,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                vec[lane + 32 * e] = nl[e];
-                vec[64 + lane + 32 * e] = nd[e];
+                // -lse x log2 e; minus infinity for rows that are not there or see
+                // nothing: probability 0
+                vec[lane + 32 * e] = nl[e] == -INFINITY ? -INFINITY : -nl[e] * kLog2e;
+                vec[64 + lane + 32 * e] = -nd[e];
             }
             __syncwarp();
             if (it + 1 < blocks) fetch();

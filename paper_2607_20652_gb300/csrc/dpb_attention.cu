@@ -556,23 +556,31 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
 // ---- gradients ------------------------------------------------------------------
 
 // One tile of 128 rows against blocks of 128: S and the gradient of P take 256
-// TMEM columns, the sums the rest. Two warpgroups share a tile, 64 columns
-// each, so that a block's arithmetic takes half as long between its products.
+// TMEM columns, the sums the rest. Warpgroups share a tile's columns. With heads
+// of 64 the rows' arithmetic is what bounds a block: four warpgroups of 32
+// columns each (a thread's chain from S to dS is short, and four warps on each
+// scheduler fill each other's waits): 1 x 12289, 12 heads: 661 us, 708 with two.
+// With heads of 128 the products are, and two are as good (1 x 8192, 16 heads:
+// 587 us, 595 with four).
 template <int DP_>
 struct GradShape {
     static constexpr int DP = DP_, BN = 128, NS = DP == 64 ? 8 : 4;
+    static constexpr int kParts = DP == 64 ? 4 : 2, kWidth = BN / kParts, kRowWarps = 4 * kParts;
     static constexpr int kTile = kRows * DP * 2;
-    // 2 x 4 row warps, the copying warp, and two that issue products: one those
-    // of two tiles in shared memory, one those that sum what the row warps made
-    static constexpr int kThreads = 384, kCopier = 8, kIssuer = 9, kSummer = 10;
-    static constexpr int kRegsRow = 208, kRegsOther = 88;           // 256 x 208 + 128 x 88 = 384 x 168
+    // after the row warps: the copying warp, and two that issue products, one
+    // those of two tiles in shared memory, one those that sum what the row warps made
+    static constexpr int kCopier = kRowWarps, kIssuer = kRowWarps + 1, kSummer = kRowWarps + 2;
+    static constexpr int kThreads = 32 * kRowWarps + 128;
+    // registers: 512 x 104 + 128 x 64 = 640 x 96, or 256 x 208 + 128 x 88 = 384 x 168
+    static constexpr int kRegsRow = kParts == 4 ? 104 : 208, kRegsOther = kParts == 4 ? 64 : 88;
     static constexpr int kColS = 0, kColG = 128, kColSum = 256;  // S, the gradient of P, the sums
     static constexpr int kColumns = 512;
     static constexpr int kBars = 2 + 2 * NS + 1 + 9;
     // the keys' gradient: P and dS have columns of their own where there is room
     static constexpr bool kOwn = 256 + 2 * DP + 128 <= 512;
-    static constexpr int kColP = kOwn ? 256 + 2 * DP : kColS, kColD = kOwn ? kColP + 64 : kColG, kHalf = kOwn ? 32 : 64;
-    static constexpr int kVec = 8 * 128 * 4;  // a warp's lse and delta of its 64 columns
+    static constexpr int kColP = kOwn ? 256 + 2 * DP : kColS, kColD = kOwn ? kColP + 64 : kColG;
+    static constexpr int kStep = kOwn ? kWidth / 2 : kWidth;  // columns from one part's P to the next's
+    static constexpr int kVec = kRowWarps * 2 * kWidth * 4;   // a warp's lse and delta of its columns
     static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + 8 * kBars + 16;
     using Slots = Ring<NS, kTile, NS == 4>;
 };
@@ -587,14 +595,15 @@ __device__ __forceinline__ void tile_product(uint32_t d, uint32_t a, uint32_t b)
                mma_shape(128, false), k > 0);
 }
 
-// d += a (TMEM: 128 columns of bf16, the second half of them `half` columns
-// from the first) x a tile in shared memory (K = its 128 rows).
-template <int DP>
-__device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t half, uint32_t b, bool add) {
+// d += a (TMEM: 128 bf16 a lane, each part's `step` columns from the one before)
+// x a tile in shared memory (K = its 128 rows).
+template <class C>
+__device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t step, uint32_t b, bool add) {
     const uint64_t db = desc_k_rows(b, kRows * 128);
+    constexpr int kPer = C::kWidth / 16;  // products a part
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        mma_ts(d, a + (k / 4) * half + (k % 4) * 8, desc_at(db, k * 2048), mma_shape(DP, true), add || k > 0);
+        mma_ts(d, a + (k / kPer) * step + (k % kPer) * 8, desc_at(db, k * 2048), mma_shape(C::DP, true), add || k > 0);
 }
 
 // What both gradient kernels set up: barriers (by the copying warp), TMEM.
@@ -614,7 +623,7 @@ struct GradBars {
         w_done = s_full + 16;
         v_done = s_full + 24;
         done = s_full + 32;
-        s_read = s_full + 40;  // from here on arrived on by the 8 row warps
+        s_read = s_full + 40;  // from here on arrived on by the row warps
         g_read = s_full + 48;
         w_full = s_full + 56;
         v_full = s_full + 64;
@@ -623,7 +632,7 @@ struct GradBars {
     __device__ __forceinline__ void make(int issuers) const {
         for (int i = threadIdx.x & 31; i < C::kBars; i += 32) {
             const uint32_t b = tile_full + 8 * i;
-            bar_init(b, b >= s_read ? 8 : b == done ? issuers : 1);
+            bar_init(b, b >= s_read ? C::kRowWarps : b == done ? issuers : 1);
         }
         bar_init_fence();
         __syncwarp();
@@ -634,7 +643,7 @@ struct GradBars {
 
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int DP = C::DP, BN = C::BN;
+    constexpr int DP = C::DP, BN = C::BN, W = C::kWidth;
     constexpr int kColW = C::kColSum + DP;  // dS in bf16, in columns of its own
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
@@ -655,7 +664,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
     const auto &ring = bars.ring;
     bool failed = false;
 
-    if (warp >= 8) give_registers<C::kRegsOther>();
+    if (warp >= C::kRowWarps) give_registers<C::kRegsOther>();
     if (warp == C::kCopier) {
         const int kv_head = head / a.group;
         auto rows = [&](const CUtensorMap *map, int t) {
@@ -682,7 +691,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
             if (blocks > 0)
                 for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
         }
-    } else if (warp >= 8) {
+    } else if (warp >= C::kRowWarps) {
         if (warp == C::kIssuer) tmem_alloc(smem_addr(bars.slot), C::kColumns);
         fence_before();
         setup_wait<C::kThreads>();
@@ -716,7 +725,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
                 failed = !bar_wait(bars.w_full, j & 1, kTries);
                 if (failed) break;
                 fence_after();
-                sum_product<DP>(tmem + C::kColSum, tmem + kColW, 32, ring.addr(2 * j), j > 0);
+                sum_product<C>(tmem + C::kColSum, tmem + kColW, W / 2, ring.addr(2 * j), j > 0);
                 mma_commit(bars.w_done);
                 mma_commit(ring.empty_bar(2 * j));
             }
@@ -730,21 +739,22 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
         setup_wait<C::kThreads>();
         fence_after();
         const uint32_t tmem = *bars.slot;
-        const int half = warp / 4;  // of the columns
+        const int part = warp / 4;  // of the columns
         const int i = i0 + (threadIdx.x & 127);
         const bool live = i < q.n;
         const int64_t token = q.q0 + (int64_t)i;
         const int lim = visible(a, q, i);
-        // delta = sum over the head of o grad_o: 16 rows a warp, a row's pieces of
+        // delta = sum over the head of o grad_o: some rows a warp, a row's pieces of
         // 8 values side by side on its lanes, all loads in flight together
         float *deltas = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile);
         {
-            constexpr int kPieces = DP / 8, kSteps = kPieces / 2;  // 32 / kPieces rows at a time
+            constexpr int kPieces = DP / 8, kMine = kRows / C::kRowWarps;  // rows of a warp
+            constexpr int kSteps = kMine * kPieces / 32;                   // 32 / kPieces rows at a time
             const int piece = lane % kPieces;
             uint4 x[kSteps], y[kSteps];
 #pragma unroll
             for (int e = 0; e < kSteps; ++e) {
-                const int r = i0 + 16 * warp + e * (32 / kPieces) + lane / kPieces;
+                const int r = i0 + kMine * warp + e * (32 / kPieces) + lane / kPieces;
                 x[e] = y[e] = make_uint4(0u, 0u, 0u, 0u);
                 if (r < q.n && piece * 8 < a.D) {
                     const int64_t t = q.q0 + (int64_t)r;
@@ -763,14 +773,15 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
                 }
 #pragma unroll
                 for (int o = kPieces / 2; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
-                if (piece == 0) deltas[16 * warp + e * (32 / kPieces) + lane / kPieces] = d;
+                if (piece == 0) deltas[kMine * warp + e * (32 / kPieces) + lane / kPieces] = d;
             }
         }
-        asm volatile("barrier.cta.sync 2, 256;" ::: "memory");  // the row warps: each row's delta is there
+        // the row warps: each row's delta is there
+        asm volatile("barrier.cta.sync 2, %0;" ::"n"(32 * C::kRowWarps) : "memory");
         float lse2 = INFINITY;  // a row that sees nothing: every probability 0
         const float delta = deltas[threadIdx.x & 127];
         if (live) {
-            if (half == 0) a.delta[(int64_t)head * a.total_q + token] = delta;
+            if (part == 0) a.delta[(int64_t)head * a.total_q + token] = delta;
             const float l = a.lse[(int64_t)head * a.total_q + token];
             lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
         }
@@ -782,18 +793,18 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
                 break;
             }
             fence_after();
-            uint32_t s[64], g[2][32], w[32];
+            uint32_t s[W], g[W / 32][32], w[W / 2];
             {
-                uint32_t x[2][32];
-                tmem_load(lanes + C::kColS + 64 * half, x[0]);
-                tmem_load(lanes + C::kColS + 64 * half + 32, x[1]);
-                load_wait(x[0]);
-                load_wait(x[1]);
+                uint32_t x[W / 32][32];
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) tmem_load(lanes + C::kColS + W * part + 32 * c, x[c]);
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) load_wait(x[c]);
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(bars.s_read);
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) {
+                for (int c = 0; c < W; c += 2) {
                     const float2 y = unpair(fma2(pair_bits(x[c / 32][c % 32], x[c / 32][c % 32 + 1]), scale2, lse22));
                     s[c] = __float_as_uint(exp2_approx(y.x));
                     s[c + 1] = __float_as_uint(exp2_approx(y.y));
@@ -804,21 +815,21 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
                 break;
             }
             fence_after();
-            tmem_load(lanes + C::kColG + 64 * half, g[0]);
-            tmem_load(lanes + C::kColG + 64 * half + 32, g[1]);
-            load_wait(g[0]);
-            load_wait(g[1]);
+#pragma unroll
+            for (int c = 0; c < W / 32; ++c) tmem_load(lanes + C::kColG + W * part + 32 * c, g[c]);
+#pragma unroll
+            for (int c = 0; c < W / 32; ++c) load_wait(g[c]);
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(bars.g_read);
-            const int seen = lim - j * BN - 64 * half;
-            if (!__all_sync(kFull, seen >= 64)) {
+            const int seen = lim - j * BN - W * part;
+            if (!__all_sync(kFull, seen >= W)) {
 #pragma unroll
-                for (int c = 0; c < 64; ++c)
+                for (int c = 0; c < W; ++c)
                     if (c >= seen) s[c] = g[c / 32][c % 32] = 0u;
             }
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
+            for (int c = 0; c < W; c += 2) {
                 const float2 d = unpair(
                     mul2(pair_bits(s[c], s[c + 1]), add2(pair_bits(g[c / 32][c % 32], g[c / 32][c % 32 + 1]), delta2)));
                 w[c / 2] = pack_bf16(d.x, d.y);
@@ -828,7 +839,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
                 break;
             }
             fence_after();
-            tmem_store(lanes + kColW + 32 * half, w);
+            tmem_store(lanes + kColW + W / 2 * part, w);
             store_wait();
             fence_before();
             __syncwarp();
@@ -837,10 +848,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
         if (blocks > 0) {
             if (!failed) failed = !__all_sync(kFull, bar_wait(bars.done, 0, kTries));
             fence_after();
-            if (!failed)  // Q's tile is read for the last time: its memory takes the rows
-                write_rows<DP / 2>(lanes + C::kColSum + DP / 2 * half, smem + warp * 32 * DP, a.dq, token - lane, head,
-                                   q.n - (i - lane), DP / 2 * half, a.D, a.scale);
-        } else if (live && half == 0) {
+            if (!failed && part < 2)  // Q's tile is read for the last time: its memory takes the rows
+                write_rows<DP / 2>(lanes + C::kColSum + DP / 2 * part, smem + warp * 32 * DP, a.dq, token - lane, head,
+                                   q.n - (i - lane), DP / 2 * part, a.D, a.scale);
+        } else if (live && part == 0) {
             write_zero_row(a.dq.p + token * a.dq.ts + head * a.dq.hs, a.D);
         }
     }
@@ -854,7 +865,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const 
 
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int DP = C::DP, BN = C::BN;
+    constexpr int DP = C::DP, BN = C::BN, W = C::kWidth;
     constexpr int kColV = C::kColSum, kColK = C::kColSum + DP;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
@@ -880,7 +891,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
     const auto &ring = bars.ring;
     bool failed = false;
 
-    if (warp >= 8) give_registers<C::kRegsOther>();
+    if (warp >= C::kRowWarps) give_registers<C::kRegsOther>();
     if (warp == C::kCopier) {
         auto rows = [&](const CUtensorMap *map, int t) {
             if (blocks > 0 && elect_one()) {
@@ -909,7 +920,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             if (blocks > 0)
                 for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
         }
-    } else if (warp >= 8) {
+    } else if (warp >= C::kRowWarps) {
         if (warp == C::kIssuer) tmem_alloc(smem_addr(bars.slot), C::kColumns);
         fence_before();
         setup_wait<C::kThreads>();
@@ -928,11 +939,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         };
         auto sum_v = [&](int it) {
             fence_after();
-            sum_product<DP>(tmem + kColV, tmem + C::kColP, C::kHalf, ring.addr(2 * it + 1), it > 0);
+            sum_product<C>(tmem + kColV, tmem + C::kColP, C::kStep, ring.addr(2 * it + 1), it > 0);
         };
         auto sum_k = [&](int it) {
             fence_after();
-            sum_product<DP>(tmem + kColK, tmem + C::kColD, C::kHalf, ring.addr(2 * it), it > 0);
+            sum_product<C>(tmem + kColK, tmem + C::kColD, C::kStep, ring.addr(2 * it), it > 0);
         };
         if (C::kOwn && blocks > 0 && warp == C::kIssuer && elect_one()) {
             // P^T and dS^T have columns of their own: the next S^T and gradient
@@ -998,20 +1009,20 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         setup_wait<C::kThreads>();
         fence_after();
         const uint32_t tmem = *bars.slot;
-        const int half = warp / 4;  // of the columns
+        const int part = warp / 4;  // of the columns
         const int j = j0 + (threadIdx.x & 127);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
-        const uint32_t s_addr = lanes + C::kColS + 64 * half, g_addr = lanes + C::kColG + 64 * half;
-        const uint32_t p_addr = lanes + C::kColP + C::kHalf * half, d_addr = lanes + C::kColD + C::kHalf * half;
-        float *vec = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile) + warp * 128;
+        const uint32_t s_addr = lanes + C::kColS + W * part, g_addr = lanes + C::kColG + W * part;
+        const uint32_t p_addr = lanes + C::kColP + C::kStep * part, d_addr = lanes + C::kColD + C::kStep * part;
+        float *vec = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile) + warp * 2 * W;
         // this lane's share of its columns' lse and delta, loaded a block ahead
         // and not looked at before the block is there
-        float nl[2], nd[2];
+        float nl[W / 32], nd[W / 32];
         int h = head * a.group, b = b0;  // of the next block fetched
         auto fetch = [&]() {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int i = b * BN + 64 * half + lane + 32 * e;
+            for (int e = 0; e < W / 32; ++e) {
+                const int i = b * BN + W * part + lane + 32 * e;
                 nl[e] = -INFINITY, nd[e] = 0.f;
                 if (i < q.n) {
                     const int64_t at = (int64_t)h * a.total_q + q.q0 + i;
@@ -1027,16 +1038,16 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         for (int it = 0; it < blocks; ++it) {
             __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < W / 32; ++e) {
                 // -lse x log2 e; minus infinity for rows that are not there or see
                 // nothing: probability 0
                 vec[lane + 32 * e] = nl[e] == -INFINITY ? -INFINITY : -nl[e] * kLog2e;
-                vec[64 + lane + 32 * e] = -nd[e];
+                vec[W + lane + 32 * e] = -nd[e];
             }
             __syncwarp();
             if (it + 1 < blocks) fetch();
             // masked: query i sees key j when i >= j - off
-            const int low = a.causal ? j - off - bi * BN - 64 * half : 0;
+            const int low = a.causal ? j - off - bi * BN - W * part : 0;
             if (++bi == b0 + per_head) bi = b0;
             const bool whole = __all_sync(kFull, low <= 0);
             if (!__all_sync(kFull, bar_wait(bars.s_full, it & 1, kTries))) {
@@ -1044,20 +1055,20 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 break;
             }
             fence_after();
-            uint32_t s[64], w[32];
+            uint32_t s[W], w[W / 2];
             {
-                uint32_t x[2][32];
-                tmem_load(s_addr, x[0]);
-                tmem_load(s_addr + 32, x[1]);
-                load_wait(x[0]);
-                load_wait(x[1]);
+                uint32_t x[W / 32][32];
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) tmem_load(s_addr + 32 * c, x[c]);
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) load_wait(x[c]);
                 if (C::kOwn) {
                     fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive(bars.s_read);
                 }
 #pragma unroll
-                for (int c = 0; c < 64; c += 4) {
+                for (int c = 0; c < W; c += 4) {
                     const ulonglong2 l = *reinterpret_cast<const ulonglong2 *>(vec + c);
 #pragma unroll
                     for (int e = c; e < c + 4; e += 2) {
@@ -1070,11 +1081,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             }
             if (!whole) {
 #pragma unroll
-                for (int c = 0; c < 64; ++c)
+                for (int c = 0; c < W; ++c)
                     if (c < low) s[c] = 0u;
             }
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) w[c / 2] = pack_bf16(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+            for (int c = 0; c < W; c += 2) w[c / 2] = pack_bf16(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
             if (C::kOwn && it > 0 && !__all_sync(kFull, bar_wait(bars.v_done, (it - 1) & 1, kTries))) {
                 failed = true;
                 break;
@@ -1090,11 +1101,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
                 break;
             }
             fence_after();
-            uint32_t g[2][32];
-            tmem_load(g_addr, g[0]);
-            tmem_load(g_addr + 32, g[1]);
-            load_wait(g[0]);
-            load_wait(g[1]);
+            uint32_t g[W / 32][32];
+#pragma unroll
+            for (int c = 0; c < W / 32; ++c) tmem_load(g_addr + 32 * c, g[c]);
+#pragma unroll
+            for (int c = 0; c < W / 32; ++c) load_wait(g[c]);
             if (C::kOwn) {
                 fence_before();
                 __syncwarp();
@@ -1102,12 +1113,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             }
             if (!whole) {
 #pragma unroll
-                for (int c = 0; c < 64; ++c)
+                for (int c = 0; c < W; ++c)
                     if (c < low) g[c / 32][c % 32] = 0u;
             }
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(vec + 64 + c);
+            for (int c = 0; c < W; c += 4) {
+                const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(vec + W + c);
 #pragma unroll
                 for (int e = c; e < c + 4; e += 2) {
                     const float2 y = unpair(mul2(pair_bits(s[e], s[e + 1]),
@@ -1132,12 +1143,13 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
             if (!failed) failed = !__all_sync(kFull, bar_wait(bars.done, 0, kTries));
             fence_after();
             if (!failed) {  // K's and V's tiles are read for the last time: dK and dV go through their memory
-                const Out &out = half ? a.dk : a.dv;
-                write_rows<DP>(lanes + (half ? kColK : kColV), smem + half * C::kTile + (warp & 3) * 32 * DP * 2, out,
-                               token - lane, head, q.m - (j - lane), 0, a.D, half ? a.scale : 1.f);
+                const bool second = part >= 2;  // dV by the first two parts, half of its columns each; dK by the others
+                const int col = DP / 2 * (part & 1);
+                write_rows<DP / 2>(lanes + (second ? kColK : kColV) + col, smem + warp * 32 * DP, second ? a.dk : a.dv,
+                                   token - lane, head, q.m - (j - lane), col, a.D, second ? a.scale : 1.f);
             }
-        } else if (j < q.m) {
-            const Out &out = half ? a.dk : a.dv;
+        } else if (j < q.m && part < 2) {
+            const Out &out = part ? a.dk : a.dv;
             write_zero_row(out.p + token * out.ts + head * out.hs, a.D);
         }
     }
@@ -1253,7 +1265,7 @@ cudaError_t registers_cover(const void *kernel) {
     cudaFuncAttributes f;
     const cudaError_t e = cudaFuncGetAttributes(&f, kernel);
     if (e != cudaSuccess) return e;
-    return f.numRegs * C::kThreads >= 256 * C::kRegsRow + (C::kThreads - 256) * C::kRegsOther
+    return f.numRegs * C::kThreads >= (C::kThreads - 128) * C::kRegsRow + 128 * C::kRegsOther
                ? cudaSuccess
                : cudaErrorLaunchOutOfResources;
 }

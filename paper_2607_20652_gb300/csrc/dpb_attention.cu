@@ -1142,11 +1142,13 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         if (blocks > 0) {
             if (!failed) failed = !__all_sync(kFull, bar_wait(bars.done, 0, kTries));
             fence_after();
-            if (!failed) {  // K's and V's tiles are read for the last time: dK and dV go through their memory
-                const bool second = part >= 2;  // dV by the first two parts, half of its columns each; dK by the others
-                const int col = DP / 2 * (part & 1);
-                write_rows<DP / 2>(lanes + (second ? kColK : kColV) + col, smem + warp * 32 * DP, second ? a.dk : a.dv,
-                                   token - lane, head, q.m - (j - lane), col, a.D, second ? a.scale : 1.f);
+            // K's and V's tiles are read for the last time: dK and dV go through
+            // their memory, half of the columns at a time
+            for (int c = part; c < 4 && !failed; c += C::kParts) {
+                const int col = DP / 2 * (c & 1);
+                write_rows<DP / 2>(lanes + (c >= 2 ? kColK : kColV) + col, smem + warp * 32 * DP, c >= 2 ? a.dk : a.dv,
+                                   token - lane, head, q.m - (j - lane), col, a.D, c >= 2 ? a.scale : 1.f);
+                __syncwarp();
             }
         } else if (j < q.m && part < 2) {
             const Out &out = part ? a.dk : a.dv;

@@ -1,25 +1,26 @@
 // dpb_attention.cu -- softmax attention over packed sequences and its
 // gradient, on the tcgen05 tensor cores.
 //
-// All three kernels have one shape. A block holds 128-row tiles of one side
-// (queries in the forward and in the query gradient, keys in the key and
-// value gradient) and streams blocks of the other side past them; nothing of
-// size queries x keys is ever in memory. Warps have roles: one copies tiles by
-// tensor maps into a ring of slots, one thread issues every matrix product,
-// and a warpgroup of 128 threads for each tile does the arithmetic, one row a
-// thread, so that a row's maximum, sum or delta needs no exchange. A product's
+// Both kernels have one shape. A block holds 128-row tiles of one side (queries
+// in the forward and in the query gradient, keys in the key and value gradient)
+// and streams blocks of 128 rows of the other side past them; nothing of size
+// queries x keys is ever in memory. Warps have roles: one copies tiles by
+// tensor maps into a ring of slots, one or two threads issue the matrix
+// products, and warpgroups do the arithmetic, a row of a tile to a thread (or
+// to one thread of each warpgroup, which then share its columns). A product's
 // result comes from TMEM by rows; the probabilities (and their gradients) go
 // back to TMEM in bf16, where the next product takes them as its A operand
 // without a pass through shared memory:
 //   forward         S = Q K^T;  O += P V
 //   query gradient  S = Q K^T, dP = dO V^T;  dQ += dS K
 //   key gradient    S^T = K Q^T, dP^T = V dO^T;  dV += P^T dO, dK += dS^T Q
-// The gradient takes seven products where five would do with one kernel that
+// The gradient takes seven products where five would do with one pass that
 // added its dQ shares in memory: each result then has one owner, so sums are
 // in a fixed order and no fp32 copy of dQ is kept.
 //
-// Two tiles (or two blocks on an SM) are in flight, so the products of one run
-// while the other's rows are computed.
+// Scores, sums and the statistics of a row are fp32. P and dS are rounded to
+// bf16, because that is what the tensor cores take; what they are summed into
+// is fp32 again, and each result is rounded once when it is written.
 //
 // Rows of a neighbouring sequence that a tile's box reaches into are set to
 // zero in shared memory where a product would sum over them (0 x NaN), and
@@ -64,6 +65,9 @@ struct AttnArgs {
     Out out, dq, dk, dv;
     float *lse;
     float *delta;
+    struct Plan *plan;  // of the gradient
+    struct Task *tasks_k, *tasks_q;
+    int64_t cap_k, cap_q;
     int32_t *status;
 };
 
@@ -559,9 +563,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
 // TMEM columns, the sums the rest. Warpgroups share a tile's columns. With heads
 // of 64 the rows' arithmetic is what bounds a block: four warpgroups of 32
 // columns each (a thread's chain from S to dS is short, and four warps on each
-// scheduler fill each other's waits): 1 x 12289, 12 heads: 661 us, 708 with two.
-// With heads of 128 the products are, and two are as good (1 x 8192, 16 heads:
-// 587 us, 595 with four).
+// scheduler fill each other's waits): 1 x 12289 causal, 12 heads: 661 us, 708
+// with two. With heads of 128 the products are, and two are as good (1 x 8192
+// causal, 16 heads: 587 us, 595 with four). These four are of a kernel with a
+// block for each tile.
 template <int DP_>
 struct GradShape {
     static constexpr int DP = DP_, BN = 128, NS = DP == 64 ? 8 : 4;
@@ -575,13 +580,16 @@ struct GradShape {
     static constexpr int kRegsRow = kParts == 4 ? 104 : 208, kRegsOther = kParts == 4 ? 64 : 88;
     static constexpr int kColS = 0, kColG = 128, kColSum = 256;  // S, the gradient of P, the sums
     static constexpr int kColumns = 512;
-    static constexpr int kBars = 2 + 2 * NS + 1 + 9;
+    static constexpr int kItems = 4;  // of the list of items that the copying warp hands on
+    static constexpr int kBars = 4 + 2 * NS + 1 + 11 + 2 * kItems;
     // the keys' gradient: P and dS have columns of their own where there is room
     static constexpr bool kOwn = 256 + 2 * DP + 128 <= 512;
     static constexpr int kColP = kOwn ? 256 + 2 * DP : kColS, kColD = kOwn ? kColP + 64 : kColG;
+    static constexpr int kColW = 256 + DP;  // dS of the queries' gradient
     static constexpr int kStep = kOwn ? kWidth / 2 : kWidth;  // columns from one part's P to the next's
     static constexpr int kVec = kRowWarps * 2 * kWidth * 4;   // a warp's lse and delta of its columns
-    static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + 8 * kBars + 16;
+    static constexpr int kStage = 32 * 32 * 2;                // a warp's rows of 32 result columns
+    static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + kRowWarps * kStage + 32 * kItems + 8 * kBars + 16;
     using Slots = Ring<NS, kTile, NS == 4>;
 };
 
@@ -606,398 +614,528 @@ __device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t ste
         mma_ts(d, a + (k / kPer) * step + (k % kPer) * 8, desc_at(db, k * 2048), mma_shape(C::DP, true), add || k > 0);
 }
 
-// What both gradient kernels set up: barriers (by the copying warp), TMEM.
+// A tile of the gradient's work: of keys or of queries of one sequence.
+struct Task {
+    int q0, n, k0, m, tile, pad[3];
+};
+// How many there are, and the next item (a tile of a head) that no block has.
+struct Plan {
+    unsigned long long next;
+    int keys, queries;
+};
+
+// What a block takes on: a tile of keys, a tile of queries, or the end.
+enum { kKeys, kQueries, kEnd };
+struct Item {
+    int kind, head, tile;
+    Seq q;
+};
+
+// Barriers and memory of the gradient kernel.
 template <class C>
 struct GradBars {
-    // each of the two tiles is there; S and the gradient of P are there, have been read; dS
-    // (and P, for the keys' gradient) is there; its product is done; all is done
-    uint32_t tile_full, s_full, g_full, w_done, v_done, done, s_read, g_read, w_full, v_full;
+    // each of the two tiles is there, has been used for the last time; S and the
+    // gradient of P are there, have been read; dS (and P, for the keys' gradient)
+    // is there; its product is done; the sums are there, have been read; all is
+    // done; an item of the list is there, has been read by all
+    uint32_t tile_full, tile_free, s_full, g_full, w_done, v_done, acc_full, done, s_read, g_read, w_full, v_full, acc_free,
+        item_full, item_free;
     typename C::Slots ring;
+    int4 *items;
     uint32_t *slot;
     __device__ __forceinline__ GradBars(uint8_t *smem) {
-        uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (2 + C::NS) * C::kTile + C::kVec);
+        items = reinterpret_cast<int4 *>(smem + (2 + C::NS) * C::kTile + C::kVec + C::kRowWarps * C::kStage);
+        uint64_t *bars = reinterpret_cast<uint64_t *>(items + 2 * C::kItems);
         tile_full = smem_addr(bars);
-        ring = {smem + 2 * C::kTile, tile_full + 16, tile_full + 16 + 8 * C::NS, tile_full + 16 + 16 * C::NS};
-        s_full = tile_full + 8 * (3 + 2 * C::NS);
+        tile_free = tile_full + 16;
+        ring = {smem + 2 * C::kTile, tile_full + 32, tile_full + 32 + 8 * C::NS, tile_full + 32 + 16 * C::NS};
+        s_full = tile_full + 8 * (5 + 2 * C::NS);
         g_full = s_full + 8;
         w_done = s_full + 16;
         v_done = s_full + 24;
-        done = s_full + 32;
-        s_read = s_full + 40;  // from here on arrived on by the row warps
-        g_read = s_full + 48;
-        w_full = s_full + 56;
-        v_full = s_full + 64;
+        acc_full = s_full + 32;
+        done = s_full + 40;
+        s_read = s_full + 48;  // from here on arrived on by the row warps
+        g_read = s_full + 56;
+        w_full = s_full + 64;
+        v_full = s_full + 72;
+        acc_free = s_full + 80;
+        item_full = s_full + 88;
+        item_free = item_full + 8 * C::kItems;
         slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
     }
-    __device__ __forceinline__ void make(int issuers) const {
+    __device__ __forceinline__ void make() const {
         for (int i = threadIdx.x & 31; i < C::kBars; i += 32) {
             const uint32_t b = tile_full + 8 * i;
-            bar_init(b, b >= s_read ? C::kRowWarps : b == done ? issuers : 1);
+            bar_init(b, b >= item_free ? C::kRowWarps + 2
+                        : b >= item_full ? 1
+                        : b >= s_read    ? C::kRowWarps
+                        : b == done      ? 2
+                                         : 1);
         }
         bar_init_fence();
         __syncwarp();
     }
-};
-
-// ---- gradient of the queries
-
-template <class C>
-__global__ void __launch_bounds__(C::kThreads, 1) attention_grad_q_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int DP = C::DP, BN = C::BN, W = C::kWidth;
-    constexpr int kColW = C::kColSum + DP;  // dS in bf16, in columns of its own
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
-    const int si = rest % a.seqs, tile = a.tiles - 1 - rest / a.seqs;  // the longest rows first
-    const Offsets offsets = load_offsets(a, si);
-    const GradBars<C> bars(smem);
-    if (warp == C::kCopier) bars.make(2);
-    const Seq q = sequence(a, offsets);
-    if (!q.ok) {
-        if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
-        return;
-    }
-    const int i0 = tile * kRows;
-    if (i0 >= q.n) return;
-    const int blocks = tile_blocks<BN>(a, q, tile);
-    const auto &ring = bars.ring;
-    bool failed = false;
-
-    if (warp >= C::kRowWarps) give_registers<C::kRegsOther>();
-    if (warp == C::kCopier) {
-        const int kv_head = head / a.group;
-        auto rows = [&](const CUtensorMap *map, int t) {
-            if (blocks > 0 && elect_one()) {
-                bar_arrive_expect(bars.tile_full + 8 * t, C::kTile);
-                copy_tile<DP>(smem_addr(smem) + t * C::kTile, map, head, q.q0 + i0, kRows, bars.tile_full + 8 * t);
-            }
-            __syncwarp();
-        };
-        int issued = 0, tails = 0;
-        rows(&a.q, 0);
-        if (blocks > 0) failed = !ring.template fill<DP>(issued++, &a.k, kv_head, q.k0, BN, q.m, true, tails);
-        rows(&a.g, 1);
-        setup_arrive<C::kThreads>();
-        for (int j = 0; j < blocks && !failed; ++j)
-            for (int kind = j == 0; kind < 2 && !failed; ++kind) {  // K_0 is under way
-                failed = !ring.wait_free(issued) ||
-                         !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN,
-                                                 q.m - j * BN, kind == 0, tails);
-                if (!failed) ++issued;
-            }
-        if (failed) {
-            ring.drain(issued);
-            if (blocks > 0)
-                for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
-        }
-    } else if (warp >= C::kRowWarps) {
-        if (warp == C::kIssuer) tmem_alloc(smem_addr(bars.slot), C::kColumns);
-        fence_before();
-        setup_wait<C::kThreads>();
-        fence_after();
-        const uint32_t tmem = *bars.slot;
-        if (blocks > 0 && warp == C::kIssuer && elect_one()) {
-            // S and the gradient of P of each block, once those of the block
-            // before have been read
-            const uint32_t q_addr = smem_addr(smem), g_addr = q_addr + C::kTile;
-            for (int j = 0; j < blocks; ++j) {
-                failed = !ring.wait_full(2 * j) || !bar_wait(j ? bars.s_read : bars.tile_full, j ? (j - 1) & 1 : 0, kTries);
-                if (failed) break;
-                fence_after();
-                tile_product<DP>(tmem + C::kColS, q_addr, ring.addr(2 * j));
-                mma_commit(bars.s_full);
-                failed = !ring.wait_full(2 * j + 1) ||
-                         !bar_wait(j ? bars.g_read : bars.tile_full + 8, j ? (j - 1) & 1 : 0, kTries);
-                if (failed) break;
-                fence_after();
-                tile_product<DP>(tmem + C::kColG, g_addr, ring.addr(2 * j + 1));
-                mma_commit(bars.g_full);
-                mma_commit(ring.empty_bar(2 * j + 1));
-            }
-            // every product, and every arrival that it makes, is done before
-            // the block's memory is given back
-            mma_commit(bars.done);
-            failed |= !bar_wait(bars.done, 0, kTries);
-        } else if (blocks > 0 && warp == C::kSummer && elect_one()) {
-            // dQ += dS K (K's scores are done: the row warps had them)
-            for (int j = 0; j < blocks; ++j) {
-                failed = !bar_wait(bars.w_full, j & 1, kTries);
-                if (failed) break;
-                fence_after();
-                sum_product<C>(tmem + C::kColSum, tmem + kColW, W / 2, ring.addr(2 * j), j > 0);
-                mma_commit(bars.w_done);
-                mma_commit(ring.empty_bar(2 * j));
-            }
-            mma_commit(bars.done);
-            failed |= !bar_wait(bars.done, 0, kTries);
+    // All lanes of the copying warp: hands on item c.
+    __device__ __forceinline__ bool put(const Item &it, int c) const {
+        const int at = c % C::kItems;
+        if (c >= C::kItems && !__all_sync(kFull, bar_wait(item_free + 8 * at, ((c / C::kItems) & 1) ^ 1, kTries)))
+            return false;
+        if (elect_one()) {
+            items[2 * at] = make_int4(it.kind, it.head, it.tile, it.q.q0);
+            items[2 * at + 1] = make_int4(it.q.n, it.q.k0, it.q.m, 0);
+            bar_arrive(item_full + 8 * at);
         }
         __syncwarp();
-    } else {
-        take_registers<C::kRegsRow>();
-        fence_before();
-        setup_wait<C::kThreads>();
-        fence_after();
-        const uint32_t tmem = *bars.slot;
-        const int part = warp / 4;  // of the columns
-        const int i = i0 + (threadIdx.x & 127);
-        const bool live = i < q.n;
-        const int64_t token = q.q0 + (int64_t)i;
-        const int lim = visible(a, q, i);
-        // delta = sum over the head of o grad_o: some rows a warp, a row's pieces of
-        // 8 values side by side on its lanes, all loads in flight together
-        float *deltas = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile);
-        {
-            constexpr int kPieces = DP / 8, kMine = kRows / C::kRowWarps;  // rows of a warp
-            constexpr int kSteps = kMine * kPieces / 32;                   // 32 / kPieces rows at a time
-            const int piece = lane % kPieces;
-            uint4 x[kSteps], y[kSteps];
-#pragma unroll
-            for (int e = 0; e < kSteps; ++e) {
-                const int r = i0 + kMine * warp + e * (32 / kPieces) + lane / kPieces;
-                x[e] = y[e] = make_uint4(0u, 0u, 0u, 0u);
-                if (r < q.n && piece * 8 < a.D) {
-                    const int64_t t = q.q0 + (int64_t)r;
-                    x[e] = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.ts + head * a.o.hs + piece * 8);
-                    y[e] = *reinterpret_cast<const uint4 *>(a.go.p + t * a.go.ts + head * a.go.hs + piece * 8);
-                }
+        return true;
+    }
+    __device__ __forceinline__ void read(Item &it, int at) const {
+        const int4 x = items[2 * at], y = items[2 * at + 1];
+        it.kind = x.x, it.head = x.y, it.tile = x.z;
+        it.q.q0 = x.w, it.q.n = y.x, it.q.k0 = y.y, it.q.m = y.z;
+    }
+    // One thread, or all lanes of a warp: item c.
+    __device__ __forceinline__ bool get_one(Item &it, int &c) const {
+        const int at = c % C::kItems;
+        if (!bar_wait(item_full + 8 * at, (c / C::kItems) & 1, kTries)) return false;
+        read(it, at);
+        bar_arrive(item_free + 8 * at);
+        ++c;
+        return true;
+    }
+    __device__ __forceinline__ bool get_warp(Item &it, int &c) const {
+        const int at = c % C::kItems;
+        if (!__all_sync(kFull, bar_wait(item_full + 8 * at, (c / C::kItems) & 1, kTries))) return false;
+        read(it, at);
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(item_free + 8 * at);
+        ++c;
+        return true;
+    }
+};
+
+// The queries' blocks that a tile of keys meets: from the first that sees one of
+// its keys, of every query head of the group in turn.
+struct KeyBlocks {
+    int b0, per_head, count;
+    template <int BN>
+    __device__ __forceinline__ static KeyBlocks of(const AttnArgs &a, const Seq &q, int tile) {
+        KeyBlocks k;
+        k.b0 = a.causal ? max(0, tile * kRows - (q.m - q.n)) / BN : 0;
+        k.per_head = max(0, (q.n + BN - 1) / BN - k.b0);
+        k.count = k.per_head * a.group;
+        return k;
+    }
+};
+
+// Lists the tiles of keys and of queries of all sequences, those with the most
+// blocks first (to 1/256 of the longest; their order within that does not
+// matter to any result). One block of THREADS.
+template <int THREADS>
+__device__ void make_plan(const AttnArgs &a) {
+    constexpr int kBuckets = 256;
+    __shared__ int place[2][kBuckets];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    int shift = 0;
+    while ((((max(a.max_q, a.max_k) - 1) / kRows + 1) >> shift) >= kBuckets) ++shift;
+    for (int i = threadIdx.x; i < 2 * kBuckets; i += THREADS) place[i / kBuckets][i % kBuckets] = 0;
+    __syncthreads();
+    // f(side, sequence, tile, blocks)
+    auto each = [&](auto f, bool report) {
+        for (int s = warp; s < a.seqs; s += THREADS / 32) {
+            const Seq q = sequence(a, load_offsets(a, s));
+            if (!q.ok) {
+                if (report && lane == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
+                continue;
             }
-#pragma unroll
-            for (int e = 0; e < kSteps; ++e) {
-                const uint32_t xs[4] = {x[e].x, x[e].y, x[e].z, x[e].w}, ys[4] = {y[e].x, y[e].y, y[e].z, y[e].w};
-                float d = 0.f;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    d = fmaf(__uint_as_float(xs[c] << 16), __uint_as_float(ys[c] << 16), d);
-                    d = fmaf(__uint_as_float(xs[c] & 0xffff0000u), __uint_as_float(ys[c] & 0xffff0000u), d);
-                }
-#pragma unroll
-                for (int o = kPieces / 2; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
-                if (piece == 0) deltas[kMine * warp + e * (32 / kPieces) + lane / kPieces] = d;
-            }
+            for (int t = lane; t * kRows < q.m; t += 32) f(0, q, t, KeyBlocks::of<kRows>(a, q, t).per_head);
+            for (int t = lane; t * kRows < q.n; t += 32) f(1, q, t, tile_blocks<kRows>(a, q, t));
         }
-        // the row warps: each row's delta is there
-        asm volatile("barrier.cta.sync 2, %0;" ::"n"(32 * C::kRowWarps) : "memory");
-        float lse2 = INFINITY;  // a row that sees nothing: every probability 0
-        const float delta = deltas[threadIdx.x & 127];
-        if (live) {
-            if (part == 0) a.delta[(int64_t)head * a.total_q + token] = delta;
-            const float l = a.lse[(int64_t)head * a.total_q + token];
-            lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
+    };
+    each([&](int side, const Seq &, int, int blocks) { atomicAdd(&place[side][kBuckets - 1 - (blocks >> shift)], 1); }, true);
+    __syncthreads();
+    if (warp < 2) {
+        int before = 0;
+        for (int i = lane; i < kBuckets; i += 32) {
+            const int v = place[warp][i];
+            int sum = v;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int x = __shfl_up_sync(kFull, sum, o);
+                if (lane >= o) sum += x;
+            }
+            place[warp][i] = before + sum - v;
+            before += __shfl_sync(kFull, sum, 31);
         }
-        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
-        const uint64_t scale2 = pair(a.scale2, a.scale2), lse22 = pair(-lse2, -lse2), delta2 = pair(-delta, -delta);
-        for (int j = 0; j < blocks; ++j) {
-            if (!__all_sync(kFull, bar_wait(bars.s_full, j & 1, kTries))) {
-                failed = true;
-                break;
+        if (lane == 0) {
+            if (warp == 0) {
+                a.plan->next = 0;
+                a.plan->keys = (int)min((int64_t)before, a.cap_k);
+            } else {
+                a.plan->queries = (int)min((int64_t)before, a.cap_q);
             }
-            fence_after();
-            uint32_t s[W], g[W / 32][32], w[W / 2];
-            {
-                uint32_t x[W / 32][32];
-#pragma unroll
-                for (int c = 0; c < W / 32; ++c) tmem_load(lanes + C::kColS + W * part + 32 * c, x[c]);
-#pragma unroll
-                for (int c = 0; c < W / 32; ++c) load_wait(x[c]);
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(bars.s_read);
-#pragma unroll
-                for (int c = 0; c < W; c += 2) {
-                    const float2 y = unpair(fma2(pair_bits(x[c / 32][c % 32], x[c / 32][c % 32 + 1]), scale2, lse22));
-                    s[c] = __float_as_uint(exp2_approx(y.x));
-                    s[c + 1] = __float_as_uint(exp2_approx(y.y));
-                }
-            }
-            if (!__all_sync(kFull, bar_wait(bars.g_full, j & 1, kTries))) {
-                failed = true;
-                break;
-            }
-            fence_after();
-#pragma unroll
-            for (int c = 0; c < W / 32; ++c) tmem_load(lanes + C::kColG + W * part + 32 * c, g[c]);
-#pragma unroll
-            for (int c = 0; c < W / 32; ++c) load_wait(g[c]);
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(bars.g_read);
-            const int seen = lim - j * BN - W * part;
-            if (!__all_sync(kFull, seen >= W)) {
-#pragma unroll
-                for (int c = 0; c < W; ++c)
-                    if (c >= seen) s[c] = g[c / 32][c % 32] = 0u;
-            }
-#pragma unroll
-            for (int c = 0; c < W; c += 2) {
-                const float2 d = unpair(
-                    mul2(pair_bits(s[c], s[c + 1]), add2(pair_bits(g[c / 32][c % 32], g[c / 32][c % 32 + 1]), delta2)));
-                w[c / 2] = pack_bf16(d.x, d.y);
-            }
-            if (j > 0 && !__all_sync(kFull, bar_wait(bars.w_done, (j - 1) & 1, kTries))) {
-                failed = true;
-                break;
-            }
-            fence_after();
-            tmem_store(lanes + kColW + W / 2 * part, w);
-            store_wait();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(bars.w_full);
-        }
-        if (blocks > 0) {
-            if (!failed) failed = !__all_sync(kFull, bar_wait(bars.done, 0, kTries));
-            fence_after();
-            if (!failed && part < 2)  // Q's tile is read for the last time: its memory takes the rows
-                write_rows<DP / 2>(lanes + C::kColSum + DP / 2 * part, smem + warp * 32 * DP, a.dq, token - lane, head,
-                                   q.n - (i - lane), DP / 2 * part, a.D, a.scale);
-        } else if (live && part == 0) {
-            write_zero_row(a.dq.p + token * a.dq.ts + head * a.dq.hs, a.D);
         }
     }
-    if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
-    fence_before();
     __syncthreads();
-    if (warp == C::kIssuer) tmem_free(*bars.slot, C::kColumns);
+    each(
+        [&](int side, const Seq &q, int t, int blocks) {
+            const int at = atomicAdd(&place[side][kBuckets - 1 - (blocks >> shift)], 1);
+            // more than sound offsets can have
+            if (at >= (side ? a.cap_q : a.cap_k)) return set_status(a.status, DPB_DEV_BAD_LENGTH);
+            (side ? a.tasks_q : a.tasks_k)[at] = Task{q.q0, q.n, q.k0, q.m, t, {0, 0, 0}};
+        },
+        false);
 }
 
-// ---- gradient of keys and values
+// Writes CH x 32 columns of this warp's 32 rows of a result from TMEM (fp32,
+// times f) as bf16 to columns [col, min(col + 32 CH, D)), 32 at a time through
+// `stage` (their 16-byte pieces exchanged so that neither side meets bank
+// conflicts), so that a store covers whole stretches of rows. Rows from `rows`
+// on are left out. read() is called once TMEM has been read.
+template <int CH, typename F>
+__device__ __forceinline__ void write_columns(uint32_t tmem, uint8_t *stage, const Out &out, int64_t token, int head,
+                                              int rows, int col, int D, float f, F read) {
+    const int lane = threadIdx.x & 31;
+    uint32_t u[CH][16];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        uint32_t v[32];
+        tmem_load(tmem + 32 * c, v);
+        load_wait(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            u[c][e] = pack_bf16(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f);
+    }
+    read();
+    const int piece = lane & 3, r0 = lane >> 2;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4 *>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) =
+                make_uint4(u[c][4 * i], u[c][4 * i + 1], u[c][4 * i + 2], u[c][4 * i + 3]);
+        __syncwarp();
+        uint4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 8 * i;
+            x[i] = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((piece ^ ((r >> 1) & 3)) * 16));
+        }
+        const int at = col + 32 * c + 8 * piece;
+        if (at < D)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r0 + 8 * i < rows)
+                    *reinterpret_cast<uint4 *>(out.p + (token + r0 + 8 * i) * out.ts + head * out.hs + at) = x[i];
+    }
+}
 
+// What the gradient kernel needs first: the list of tiles (block 0), and (the
+// others) delta = sum over the head of o grad_o, for every query row: LANES lanes
+// a row, 8 values each.
+template <int LANES>
+__global__ void __launch_bounds__(512) attention_delta_kernel(const __grid_constant__ AttnArgs a) {
+    if (blockIdx.x == 0) return make_plan<512>(a);
+    constexpr int kRowsAtOnce = 512 / LANES;
+    const int64_t rows = a.total_q * a.hq, stride = (int64_t)(gridDim.x - 1) * kRowsAtOnce;
+    const int piece = threadIdx.x % LANES, mine = threadIdx.x / LANES;
+    for (int64_t first = (int64_t)(blockIdx.x - 1) * kRowsAtOnce; first < rows; first += stride) {
+        const int64_t r = first + mine, t = r / a.hq;
+        const int h = (int)(r % a.hq);
+        float d = 0.f;
+        if (r < rows && piece * 8 < a.D) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.ts + h * a.o.hs + piece * 8);
+            const uint4 y = *reinterpret_cast<const uint4 *>(a.go.p + t * a.go.ts + h * a.go.hs + piece * 8);
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                d = fmaf(__uint_as_float(xs[c] << 16), __uint_as_float(ys[c] << 16), d);
+                d = fmaf(__uint_as_float(xs[c] & 0xffff0000u), __uint_as_float(ys[c] & 0xffff0000u), d);
+            }
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
+        if (r < rows && piece == 0) a.delta[(int64_t)h * a.total_q + t] = d;
+    }
+}
+
+// ---- the gradient kernel ----------------------------------------------------------
+
+// Blocks stay, and take items (a tile of a head) from the list one after the
+// other: the tiles of keys first, then those of queries, either with the longest
+// first, so that what comes last is short. The copying warp takes an item and
+// hands it on; a block's barriers count on from one item to the next, so that an
+// item's copies and first products run while the one before is being finished.
+//
+// Measured, with the delta kernel (causal; rate of the five products that are
+// the least: 2.5 x the forward's), against a kernel for each side with a block
+// for each tile: 1 x 12289, 12 heads of 64: 641 us (666), 904 TFLOP/s; 8 x 1024,
+// 12 heads of 64: 71 us (98); 1 x 8192, 16 heads of 128: 573 us (590), 1199
+// TFLOP/s, of seven products done 1679; 12 sequences of 1 to 3001, 16 heads of
+// 128 on 4: 140 us (215). Bound by the tensor cores at 128; at 64 by the
+// exponentials and the conversions beside them; the ragged batch by its
+// longest tile of keys, which meets all its group's queries on one SM (128 us).
 template <class C>
-__global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int DP = C::DP, BN = C::BN, W = C::kWidth;
     constexpr int kColV = C::kColSum, kColK = C::kColSum + DP;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    const int head = blockIdx.x % a.hkv, rest = blockIdx.x / a.hkv;
-    const int si = rest % a.seqs, tile = rest / a.seqs;  // causal: the first keys are seen by most queries
-    const Offsets offsets = load_offsets(a, si);
     const GradBars<C> bars(smem);
-    if (warp == C::kCopier) bars.make(C::kOwn ? 2 : 1);
-    const Seq q = sequence(a, offsets);
-    if (!q.ok) {
-        if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
-        return;
-    }
-    const int j0 = tile * kRows;
-    if (j0 >= q.m) return;
-    // blocks of queries from the first that sees a key of this tile, of every
-    // query head of the group in turn
-    const int off = q.m - q.n;
-    const int b0 = a.causal ? max(0, j0 - off) / BN : 0;
-    const int per_head = max(0, (q.n + BN - 1) / BN - b0);
-    const int blocks = per_head * a.group;
     const auto &ring = bars.ring;
+    Item it;
     bool failed = false;
+    int c = 0;  // items taken
 
     if (warp >= C::kRowWarps) give_registers<C::kRegsOther>();
     if (warp == C::kCopier) {
-        auto rows = [&](const CUtensorMap *map, int t) {
-            if (blocks > 0 && elect_one()) {
-                bar_arrive_expect(bars.tile_full + 8 * t, C::kTile);
-                copy_tile<DP>(smem_addr(smem) + t * C::kTile, map, head, q.k0 + j0, kRows, bars.tile_full + 8 * t);
-            }
-            __syncwarp();
-        };
-        int issued = 0, tails = 0, h = head * a.group, b = b0;
-        rows(&a.k, 0);
-        if (blocks > 0)
-            failed = !ring.template fill<DP>(issued++, &a.q, h, q.q0 + b * BN, BN, q.n - b * BN, true, tails);
-        rows(&a.v, 1);
+        bars.make();
         setup_arrive<C::kThreads>();
-        for (int it = 0; it < blocks && !failed; ++it) {
-            for (int kind = it == 0; kind < 2 && !failed; ++kind) {  // the first Q is under way
-                failed = !ring.wait_free(issued) ||
-                         !ring.template fill<DP>(issued, kind ? &a.g : &a.q, h, q.q0 + b * BN, BN, q.n - b * BN, true,
-                                                 tails);
-                if (!failed) ++issued;
+        const int64_t keys = (int64_t)a.plan->keys * a.hkv, all = keys + (int64_t)a.plan->queries * a.hq;
+        int64_t at = blockIdx.x;
+        // ring's tiles copied, items with blocks, copies of each of the two tiles
+        int i = 0, tails = 0, n = 0, sent0 = 0, sent1 = 0;
+        for (;;) {
+            it = Item{};
+            it.kind = at < keys ? kKeys : at < all ? kQueries : kEnd;
+            const bool queries = it.kind == kQueries;
+            if (it.kind != kEnd) {
+                const int64_t rest = queries ? at - keys : at;
+                const int heads = queries ? a.hq : a.hkv;
+                const int4 *t = reinterpret_cast<const int4 *>((queries ? a.tasks_q : a.tasks_k) + rest / heads);
+                const int4 x = t[0];
+                it.q.q0 = x.x, it.q.n = x.y, it.q.k0 = x.z, it.q.m = x.w;
+                it.tile = t[1].x;
+                it.head = (int)(rest % heads);
             }
-            if (++b == b0 + per_head) b = b0, ++h;
+            failed = !bars.put(it, c);
+            if (failed || it.kind == kEnd) break;
+            ++c;
+            const Seq &q = it.q;
+            const KeyBlocks kb = KeyBlocks::of<BN>(a, q, it.tile);
+            const int count = queries ? tile_blocks<BN>(a, q, it.tile) : kb.count;
+            if (count > 0) {
+                auto rows = [&](const CUtensorMap *map, int t) {
+                    failed = failed ||
+                             (n > 0 && !__all_sync(kFull, bar_wait(bars.tile_free + 8 * t, (n - 1) & 1, kTries)));
+                    if (failed) return;
+                    ++(t ? sent1 : sent0);
+                    if (elect_one()) {
+                        bar_arrive_expect(bars.tile_full + 8 * t, C::kTile);
+                        copy_tile<DP>(smem_addr(smem) + t * C::kTile, map, it.head,
+                                      (queries ? q.q0 : q.k0) + it.tile * kRows, kRows, bars.tile_full + 8 * t);
+                    }
+                    __syncwarp();
+                };
+                int h = queries ? it.head / a.group : it.head * a.group, b = queries ? 0 : kb.b0;
+                const int first = queries ? q.k0 : q.q0, length = queries ? q.m : q.n;
+                // V's product sums over columns of the head alone
+                auto block = [&](const CUtensorMap *map, bool sums) {
+                    failed = failed || !ring.wait_free(i) ||
+                             !ring.template fill<DP>(i, map, h, first + b * BN, BN, length - b * BN, sums, tails);
+                    if (!failed) ++i;
+                };
+                const CUtensorMap *const x = queries ? &a.k : &a.q, *const y = queries ? &a.v : &a.g;
+                // what the first products need first
+                rows(queries ? &a.q : &a.k, 0);
+                block(x, true);
+                rows(queries ? &a.g : &a.v, 1);
+                block(y, !queries);
+                for (int e = 1; e < count && !failed; ++e) {
+                    ++b;
+                    if (!queries && b == kb.b0 + kb.per_head) b = kb.b0, ++h;
+                    block(x, true);
+                    block(y, !queries);
+                }
+                ++n;
+            }
+            if (failed) break;
+            if (lane == 0) at = (int64_t)(gridDim.x + atomicAdd(&a.plan->next, 1ull));
+            at = __shfl_sync(kFull, at, 0);
         }
-        if (failed) {
-            ring.drain(issued);
-            if (blocks > 0)
-                for (int t = 0; t < 2; ++t) bar_wait(bars.tile_full + 8 * t, 0, kTries);
-        }
+        // no copy is in flight when the block ends, whatever gave up
+        ring.drain(i);
+        if (sent0 > 0) bar_wait(bars.tile_full, (sent0 - 1) & 1, kTries);
+        if (sent1 > 0) bar_wait(bars.tile_full + 8, (sent1 - 1) & 1, kTries);
     } else if (warp >= C::kRowWarps) {
         if (warp == C::kIssuer) tmem_alloc(smem_addr(bars.slot), C::kColumns);
         fence_before();
         setup_wait<C::kThreads>();
         fence_after();
         const uint32_t tmem = *bars.slot;
-        const uint32_t k_addr = smem_addr(smem), v_addr = k_addr + C::kTile;
-        auto scores = [&](int it) {
+        const uint32_t tile0 = smem_addr(smem), tile1 = tile0 + C::kTile;
+        int i = 0, b = 0, n = 0;  // tiles, blocks and items with blocks so far
+        auto scores = [&](int ri, bool last) {
             fence_after();
-            tile_product<DP>(tmem + C::kColS, k_addr, ring.addr(2 * it));
+            tile_product<DP>(tmem + C::kColS, tile0, ring.addr(ri));
             mma_commit(bars.s_full);
+            if (last) mma_commit(bars.tile_free);
         };
-        auto grads = [&](int it) {
+        auto grads = [&](int ri, bool last) {
             fence_after();
-            tile_product<DP>(tmem + C::kColG, v_addr, ring.addr(2 * it + 1));
+            tile_product<DP>(tmem + C::kColG, tile1, ring.addr(ri + 1));
             mma_commit(bars.g_full);
+            if (last) mma_commit(bars.tile_free + 8);
         };
-        auto sum_v = [&](int it) {
+        auto sum_v = [&](int ri, bool add) {
             fence_after();
-            sum_product<C>(tmem + kColV, tmem + C::kColP, C::kStep, ring.addr(2 * it + 1), it > 0);
+            sum_product<C>(tmem + kColV, tmem + C::kColP, C::kStep, ring.addr(ri + 1), add);
         };
-        auto sum_k = [&](int it) {
+        auto sum_k = [&](int ri, bool add) {
             fence_after();
-            sum_product<C>(tmem + kColK, tmem + C::kColD, C::kStep, ring.addr(2 * it), it > 0);
+            sum_product<C>(tmem + kColK, tmem + C::kColD, C::kStep, ring.addr(ri), add);
         };
-        if (C::kOwn && blocks > 0 && warp == C::kIssuer && elect_one()) {
-            // P^T and dS^T have columns of their own: the next S^T and gradient
-            // of P^T are computed as soon as these have been read
-            for (int it = 0; it < blocks; ++it) {
-                failed = !ring.wait_full(2 * it) ||
-                         !bar_wait(it ? bars.s_read : bars.tile_full, it ? (it - 1) & 1 : 0, kTries);
-                if (failed) break;
-                scores(it);
-                failed = !ring.wait_full(2 * it + 1) ||
-                         !bar_wait(it ? bars.g_read : bars.tile_full + 8, it ? (it - 1) & 1 : 0, kTries);
-                if (failed) break;
-                grads(it);
+        if (warp == C::kIssuer && elect_one()) {
+            failed = !bars.get_one(it, c);
+            // ---- tiles of keys
+            if (C::kOwn) {
+                // P^T and dS^T have columns of their own: the next S^T and gradient
+                // of P^T are computed as soon as these have been read
+                for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
+                    const int blocks = KeyBlocks::of<BN>(a, it.q, it.tile).count;
+                    for (int j = 0; j < blocks; ++j, ++b, i += 2) {
+                        failed = (j == 0 && !bar_wait(bars.tile_full, n & 1, kTries)) || !ring.wait_full(i) ||
+                                 (b > 0 && !bar_wait(bars.s_read, (b - 1) & 1, kTries));
+                        if (failed) break;
+                        scores(i, j + 1 == blocks);
+                        failed = (j == 0 && !bar_wait(bars.tile_full + 8, n & 1, kTries)) || !ring.wait_full(i + 1) ||
+                                 (b > 0 && !bar_wait(bars.g_read, (b - 1) & 1, kTries));
+                        if (failed) break;
+                        grads(i, j + 1 == blocks);
+                    }
+                    n += blocks > 0;
+                }
+            } else {
+                // P^T takes the place of S^T, dS^T that of the gradient of P^T,
+                // and the next product into either comes after the one that reads
+                // it (products run in the order of their issue): while the rows'
+                // arithmetic makes P^T, dK and the next gradient are computed, while
+                // it makes dS^T, dV and the next S^T, which may be the next item's.
+                auto blocks_of = [&]() { return it.kind == kKeys ? KeyBlocks::of<BN>(a, it.q, it.tile).count : 0; };
+                // the next tile of keys that meets queries (or what comes after the last)
+                auto next_item = [&]() {
+                    do failed = failed || !bars.get_one(it, c);
+                    while (!failed && it.kind == kKeys && blocks_of() == 0);
+                };
+                if (it.kind == kKeys && blocks_of() == 0) next_item();
+                int blocks = failed ? 0 : blocks_of();
+                if (blocks > 0) {
+                    failed = !bar_wait(bars.tile_full, 0, kTries) || !ring.wait_full(0);
+                    if (!failed) scores(0, blocks == 1);
+                    failed = failed || !bar_wait(bars.tile_full + 8, 0, kTries) || !ring.wait_full(1);
+                    if (!failed) grads(0, blocks == 1);
+                }
+                while (blocks > 0 && !failed) {
+                    int after = 0;
+                    for (int j = 0; j < blocks; ++j, ++b, i += 2) {
+                        const bool turn = j + 1 == blocks;
+                        failed = !bar_wait(bars.v_full, b & 1, kTries) ||
+                                 (j == 0 && n > 0 && !bar_wait(bars.acc_free, (n - 1) & 1, kTries));
+                        if (failed) break;
+                        sum_v(i, j > 0);
+                        mma_commit(ring.empty_bar(i + 1));
+                        if (turn) {
+                            next_item();
+                            if (failed) break;
+                            after = blocks_of();
+                        }
+                        const bool more = !turn || after > 0, last = turn ? after == 1 : j + 2 == blocks;
+                        if (more) {
+                            failed = (turn && !bar_wait(bars.tile_full, (n + 1) & 1, kTries)) || !ring.wait_full(i + 2);
+                            if (failed) break;
+                            scores(i + 2, last);
+                        }
+                        failed = !bar_wait(bars.w_full, b & 1, kTries);
+                        if (failed) break;
+                        sum_k(i, j > 0);
+                        mma_commit(ring.empty_bar(i));
+                        if (turn) mma_commit(bars.acc_full);
+                        if (more) {
+                            failed = (turn && !bar_wait(bars.tile_full + 8, (n + 1) & 1, kTries)) || !ring.wait_full(i + 3);
+                            if (failed) break;
+                            grads(i + 2, last);
+                        }
+                    }
+                    ++n;
+                    blocks = after;
+                }
             }
+            // ---- tiles of queries: S and the gradient of P of each block, once
+            // those of the block before have been read
+            int r = C::kOwn ? b : 0;  // blocks of these two barriers
+            for (; !failed && it.kind == kQueries; failed = failed || !bars.get_one(it, c)) {
+                const int blocks = tile_blocks<BN>(a, it.q, it.tile);
+                for (int j = 0; j < blocks; ++j, ++r, i += 2) {
+                    failed = (j == 0 && !bar_wait(bars.tile_full, n & 1, kTries)) || !ring.wait_full(i) ||
+                             (r > 0 && !bar_wait(bars.s_read, (r - 1) & 1, kTries));
+                    if (failed) break;
+                    fence_after();
+                    tile_product<DP>(tmem + C::kColS, tile0, ring.addr(i));
+                    mma_commit(bars.s_full);
+                    if (j + 1 == blocks) mma_commit(bars.tile_free);
+                    failed = (j == 0 && !bar_wait(bars.tile_full + 8, n & 1, kTries)) || !ring.wait_full(i + 1) ||
+                             (r > 0 && !bar_wait(bars.g_read, (r - 1) & 1, kTries));
+                    if (failed) break;
+                    fence_after();
+                    tile_product<DP>(tmem + C::kColG, tile1, ring.addr(i + 1));
+                    mma_commit(bars.g_full);
+                    mma_commit(ring.empty_bar(i + 1));
+                    if (j + 1 == blocks) mma_commit(bars.tile_free + 8);
+                }
+                n += blocks > 0;
+            }
+            // every product, and every arrival that it makes, is done before
+            // the block's memory is given back
             mma_commit(bars.done);
             failed |= !bar_wait(bars.done, 0, kTries);
-        } else if (C::kOwn && blocks > 0 && warp == C::kSummer && elect_one()) {
-            for (int it = 0; it < blocks; ++it) {
-                failed = !bar_wait(bars.v_full, it & 1, kTries);
-                if (failed) break;
-                sum_v(it);
-                mma_commit(bars.v_done);
-                failed = !bar_wait(bars.w_full, it & 1, kTries);
-                if (failed) break;
-                sum_k(it);
-                mma_commit(bars.w_done);
-                // the other products of this block are done: the row warps had them
-                mma_commit(ring.empty_bar(2 * it));
-                mma_commit(ring.empty_bar(2 * it + 1));
+        } else if (warp == C::kSummer && elect_one()) {
+            failed = !bars.get_one(it, c);
+            if (C::kOwn) {
+                for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
+                    const int blocks = KeyBlocks::of<BN>(a, it.q, it.tile).count;
+                    for (int j = 0; j < blocks; ++j, ++b, i += 2) {
+                        failed = !bar_wait(bars.v_full, b & 1, kTries) ||
+                                 (j == 0 && n > 0 && !bar_wait(bars.acc_free, (n - 1) & 1, kTries));
+                        if (failed) break;
+                        sum_v(i, j > 0);
+                        mma_commit(bars.v_done);
+                        failed = !bar_wait(bars.w_full, b & 1, kTries);
+                        if (failed) break;
+                        sum_k(i, j > 0);
+                        mma_commit(bars.w_done);
+                        // the other products of this block are done: the row warps had them
+                        mma_commit(ring.empty_bar(i));
+                        mma_commit(ring.empty_bar(i + 1));
+                        if (j + 1 == blocks) mma_commit(bars.acc_full);
+                    }
+                    n += blocks > 0;
+                }
+            } else {
+                for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
+                    // the issuer's; each is seen to its end, so that the barriers'
+                    // parities below are those of this item's blocks
+                    const int blocks = KeyBlocks::of<BN>(a, it.q, it.tile).count;
+                    if (blocks == 0) continue;
+                    failed = !bar_wait(bars.acc_full, n & 1, kTries);
+                    b += blocks, i += 2 * blocks, ++n;
+                }
             }
-            mma_commit(bars.done);
-            failed |= !bar_wait(bars.done, 0, kTries);
-        } else if (!C::kOwn && blocks > 0 && warp == C::kIssuer && elect_one()) {
-            // P^T takes the place of S^T, dS^T that of the gradient of P^T,
-            // and the next product into either comes after the one that reads
-            // it (products run in the order of their issue): while the rows'
-            // arithmetic makes P^T, dK and the next gradient are computed, while
-            // it makes dS^T, dV and the next S^T.
-            failed = !bar_wait(bars.tile_full, 0, kTries) || !ring.wait_full(0);
-            if (!failed) scores(0);
-            failed = failed || !bar_wait(bars.tile_full + 8, 0, kTries) || !ring.wait_full(1);
-            if (!failed) grads(0);
-            for (int it = 0; it < blocks && !failed; ++it) {
-                const bool more = it + 1 < blocks;
-                failed = (more && !ring.wait_full(2 * it + 2)) || !bar_wait(bars.v_full, it & 1, kTries);
-                if (failed) break;
-                sum_v(it);
-                mma_commit(ring.empty_bar(2 * it + 1));
-                if (more) scores(it + 1);
-                failed = (more && !ring.wait_full(2 * it + 3)) || !bar_wait(bars.w_full, it & 1, kTries);
-                if (failed) break;
-                sum_k(it);
-                mma_commit(ring.empty_bar(2 * it));
-                if (more) grads(it + 1);
+            // dQ += dS K (K's scores are done: the row warps had them)
+            for (; !failed && it.kind == kQueries; failed = failed || !bars.get_one(it, c)) {
+                const int blocks = tile_blocks<BN>(a, it.q, it.tile);
+                for (int j = 0; j < blocks; ++j, ++b, i += 2) {
+                    failed = !bar_wait(bars.w_full, b & 1, kTries) ||
+                             (j == 0 && n > 0 && !bar_wait(bars.acc_free, (n - 1) & 1, kTries));
+                    if (failed) break;
+                    fence_after();
+                    sum_product<C>(tmem + C::kColSum, tmem + C::kColW, W / 2, ring.addr(i), j > 0);
+                    mma_commit(bars.w_done);
+                    mma_commit(ring.empty_bar(i));
+                    if (j + 1 == blocks) mma_commit(bars.acc_full);
+                }
+                n += blocks > 0;
             }
             mma_commit(bars.done);
             failed |= !bar_wait(bars.done, 0, kTries);
@@ -1010,149 +1148,287 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kv_kernel(const
         fence_after();
         const uint32_t tmem = *bars.slot;
         const int part = warp / 4;  // of the columns
-        const int j = j0 + (threadIdx.x & 127);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        uint8_t *stage = smem + (2 + C::NS) * C::kTile + C::kVec + warp * C::kStage;
+        const uint64_t scale2 = pair(a.scale2, a.scale2);
+        int b = 0, n = 0;  // blocks and items with blocks so far
+        failed = !bars.get_warp(it, c);
+
+        // ---- tiles of keys
         const uint32_t s_addr = lanes + C::kColS + W * part, g_addr = lanes + C::kColG + W * part;
         const uint32_t p_addr = lanes + C::kColP + C::kStep * part, d_addr = lanes + C::kColD + C::kStep * part;
         float *vec = reinterpret_cast<float *>(smem + (2 + C::NS) * C::kTile) + warp * 2 * W;
         // this lane's share of its columns' lse and delta, loaded a block ahead
-        // and not looked at before the block is there
+        // (an item's first before the item before is written out) and not looked
+        // at before the block is there
         float nl[W / 32], nd[W / 32];
-        int h = head * a.group, b = b0;  // of the next block fetched
+        KeyBlocks k{};
+        int h = 0, fb = 0;  // of the next block fetched
         auto fetch = [&]() {
 #pragma unroll
             for (int e = 0; e < W / 32; ++e) {
-                const int i = b * BN + W * part + lane + 32 * e;
+                const int r = fb * BN + W * part + lane + 32 * e;
                 nl[e] = -INFINITY, nd[e] = 0.f;
-                if (i < q.n) {
-                    const int64_t at = (int64_t)h * a.total_q + q.q0 + i;
+                if (r < it.q.n) {
+                    const int64_t at = (int64_t)h * a.total_q + it.q.q0 + r;
                     nl[e] = a.lse[at];
                     nd[e] = a.delta[at];
                 }
             }
-            if (++b == b0 + per_head) b = b0, ++h;
+            if (++fb == k.b0 + k.per_head) fb = k.b0, ++h;
         };
-        const uint64_t scale2 = pair(a.scale2, a.scale2);
-        if (blocks > 0) fetch();
-        int bi = b0;  // the block at hand
-        for (int it = 0; it < blocks; ++it) {
-            __syncwarp();
+        auto start = [&]() {
+            k = KeyBlocks::of<BN>(a, it.q, it.tile);
+            h = it.head * a.group, fb = k.b0;
+            if (k.count > 0) fetch();
+        };
+        if (!failed && it.kind == kKeys) start();
+        while (!failed && it.kind == kKeys) {
+            const int r = it.tile * kRows + (threadIdx.x & 127), head = it.head, rows = it.q.m - (r - lane);
+            const int64_t token = it.q.k0 + (int64_t)(r - lane);  // of the warp's first row
+            const int off = it.q.m - it.q.n, count = k.count;
+            int bi = k.b0;  // the block at hand
+            for (int e = 0; e < count; ++e, ++b) {
+                __syncwarp();
 #pragma unroll
-            for (int e = 0; e < W / 32; ++e) {
-                // -lse x log2 e; minus infinity for rows that are not there or see
-                // nothing: probability 0
-                vec[lane + 32 * e] = nl[e] == -INFINITY ? -INFINITY : -nl[e] * kLog2e;
-                vec[W + lane + 32 * e] = -nd[e];
-            }
-            __syncwarp();
-            if (it + 1 < blocks) fetch();
-            // masked: query i sees key j when i >= j - off
-            const int low = a.causal ? j - off - bi * BN - W * part : 0;
-            if (++bi == b0 + per_head) bi = b0;
-            const bool whole = __all_sync(kFull, low <= 0);
-            if (!__all_sync(kFull, bar_wait(bars.s_full, it & 1, kTries))) {
-                failed = true;
-                break;
-            }
-            fence_after();
-            uint32_t s[W], w[W / 2];
-            {
-                uint32_t x[W / 32][32];
+                for (int x = 0; x < W / 32; ++x) {
+                    // -lse x log2 e; minus infinity for rows that are not there or see
+                    // nothing: probability 0
+                    vec[lane + 32 * x] = nl[x] == -INFINITY ? -INFINITY : -nl[x] * kLog2e;
+                    vec[W + lane + 32 * x] = -nd[x];
+                }
+                __syncwarp();
+                if (e + 1 < count) fetch();
+                // masked: query i sees key r when i >= r - off
+                const int low = a.causal ? r - off - bi * BN - W * part : 0;
+                if (++bi == k.b0 + k.per_head) bi = k.b0;
+                const bool whole = __all_sync(kFull, low <= 0);
+                if (!__all_sync(kFull, bar_wait(bars.s_full, b & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                uint32_t s[W], w[W / 2];
+                {
+                    uint32_t x[W / 32][32];
 #pragma unroll
-                for (int c = 0; c < W / 32; ++c) tmem_load(s_addr + 32 * c, x[c]);
+                    for (int c = 0; c < W / 32; ++c) tmem_load(s_addr + 32 * c, x[c]);
 #pragma unroll
-                for (int c = 0; c < W / 32; ++c) load_wait(x[c]);
+                    for (int c = 0; c < W / 32; ++c) load_wait(x[c]);
+                    if (C::kOwn) {
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(bars.s_read);
+                    }
+#pragma unroll
+                    for (int c = 0; c < W; c += 4) {
+                        const ulonglong2 l = *reinterpret_cast<const ulonglong2 *>(vec + c);
+#pragma unroll
+                        for (int x4 = c; x4 < c + 4; x4 += 2) {
+                            const float2 y = unpair(fma2(pair_bits(x[x4 / 32][x4 % 32], x[x4 / 32][x4 % 32 + 1]), scale2,
+                                                         x4 > c ? l.y : l.x));
+                            s[x4] = __float_as_uint(exp2_approx(y.x));
+                            s[x4 + 1] = __float_as_uint(exp2_approx(y.y));
+                        }
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int c = 0; c < W; ++c)
+                        if (c < low) s[c] = 0u;
+                }
+#pragma unroll
+                for (int c = 0; c < W; c += 2) w[c / 2] = pack_bf16(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                if (C::kOwn && b > 0 && !__all_sync(kFull, bar_wait(bars.v_done, (b - 1) & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                tmem_store(p_addr, w);
+                store_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(bars.v_full);
+                if (!__all_sync(kFull, bar_wait(bars.g_full, b & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                uint32_t g[W / 32][32];
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) tmem_load(g_addr + 32 * c, g[c]);
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) load_wait(g[c]);
                 if (C::kOwn) {
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(bars.s_read);
+                    if (lane == 0) bar_arrive(bars.g_read);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int c = 0; c < W; ++c)
+                        if (c < low) g[c / 32][c % 32] = 0u;
                 }
 #pragma unroll
                 for (int c = 0; c < W; c += 4) {
-                    const ulonglong2 l = *reinterpret_cast<const ulonglong2 *>(vec + c);
+                    const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(vec + W + c);
 #pragma unroll
-                    for (int e = c; e < c + 4; e += 2) {
-                        const float2 y = unpair(fma2(pair_bits(x[e / 32][e % 32], x[e / 32][e % 32 + 1]), scale2,
-                                                     e > c ? l.y : l.x));
-                        s[e] = __float_as_uint(exp2_approx(y.x));
-                        s[e + 1] = __float_as_uint(exp2_approx(y.y));
+                    for (int x4 = c; x4 < c + 4; x4 += 2) {
+                        const float2 y = unpair(mul2(pair_bits(s[x4], s[x4 + 1]),
+                                                     add2(pair_bits(g[x4 / 32][x4 % 32], g[x4 / 32][x4 % 32 + 1]),
+                                                          x4 > c ? d.y : d.x)));
+                        w[x4 / 2] = pack_bf16(y.x, y.y);
                     }
                 }
+                if (C::kOwn && b > 0 && !__all_sync(kFull, bar_wait(bars.w_done, (b - 1) & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                tmem_store(d_addr, w);
+                store_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(bars.w_full);
             }
-            if (!whole) {
-#pragma unroll
-                for (int c = 0; c < W; ++c)
-                    if (c < low) s[c] = 0u;
+            if (failed) break;
+            const bool live = r < it.q.m;
+            failed |= !bars.get_warp(it, c);
+            if (failed) break;
+            if (it.kind == kKeys) start();
+            if (count > 0) {
+                if (!__all_sync(kFull, bar_wait(bars.acc_full, n & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                // dV's columns, then dK's, shared out over the parts
+                constexpr int CH = 2 * DP / 32 / C::kParts;
+                const int c0 = part * CH, col = 32 * c0 % DP;
+                const bool keys = 32 * c0 >= DP;
+                write_columns<CH>(lanes + C::kColSum + 32 * c0, stage, keys ? a.dk : a.dv, token, head, rows, col, a.D,
+                                  keys ? a.scale : 1.f, [&]() {
+                                      fence_before();
+                                      __syncwarp();
+                                      if (lane == 0) bar_arrive(bars.acc_free);
+                                  });
+                ++n;
+            } else if (live && part < 2) {
+                const Out &out = part ? a.dk : a.dv;
+                write_zero_row(out.p + (token + lane) * out.ts + head * out.hs, a.D);
             }
-#pragma unroll
-            for (int c = 0; c < W; c += 2) w[c / 2] = pack_bf16(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
-            if (C::kOwn && it > 0 && !__all_sync(kFull, bar_wait(bars.v_done, (it - 1) & 1, kTries))) {
-                failed = true;
-                break;
+        }
+
+        // ---- tiles of queries
+        // an item's row: its lse and delta are loaded before the item before is
+        // written out
+        float lse = 0.f, delta = 0.f;
+        auto load_row = [&]() {
+            const int r = it.tile * kRows + (threadIdx.x & 127);
+            lse = -INFINITY, delta = 0.f;
+            if (r < it.q.n) {
+                const int64_t at = (int64_t)it.head * a.total_q + it.q.q0 + r;
+                lse = a.lse[at];
+                delta = a.delta[at];
             }
-            fence_after();
-            tmem_store(p_addr, w);
-            store_wait();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(bars.v_full);
-            if (!__all_sync(kFull, bar_wait(bars.g_full, it & 1, kTries))) {
-                failed = true;
-                break;
-            }
-            fence_after();
-            uint32_t g[W / 32][32];
+        };
+        // of these barriers: with heads of 128 the keys' gradient does without them
+        int r1 = C::kOwn ? b : 0;
+        if (!failed && it.kind == kQueries) load_row();
+        while (!failed && it.kind == kQueries) {
+            const int r = it.tile * kRows + (threadIdx.x & 127), head = it.head, rows = it.q.n - (r - lane);
+            const int64_t token = it.q.q0 + (int64_t)(r - lane);  // of the warp's first row
+            const int lim = visible(a, it.q, r), blocks = tile_blocks<BN>(a, it.q, it.tile);
+            // a row that sees nothing: every probability 0
+            const float l2 = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+            const uint64_t lse22 = pair(l2, l2), delta2 = pair(-delta, -delta);
+            for (int j = 0; j < blocks; ++j, ++b, ++r1) {
+                if (!__all_sync(kFull, bar_wait(bars.s_full, b & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                uint32_t s[W], g[W / 32][32], w[W / 2];
+                {
+                    uint32_t x[W / 32][32];
 #pragma unroll
-            for (int c = 0; c < W / 32; ++c) tmem_load(g_addr + 32 * c, g[c]);
+                    for (int c = 0; c < W / 32; ++c) tmem_load(lanes + C::kColS + W * part + 32 * c, x[c]);
 #pragma unroll
-            for (int c = 0; c < W / 32; ++c) load_wait(g[c]);
-            if (C::kOwn) {
+                    for (int c = 0; c < W / 32; ++c) load_wait(x[c]);
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(bars.s_read);
+#pragma unroll
+                    for (int c = 0; c < W; c += 2) {
+                        const float2 y = unpair(fma2(pair_bits(x[c / 32][c % 32], x[c / 32][c % 32 + 1]), scale2, lse22));
+                        s[c] = __float_as_uint(exp2_approx(y.x));
+                        s[c + 1] = __float_as_uint(exp2_approx(y.y));
+                    }
+                }
+                if (!__all_sync(kFull, bar_wait(bars.g_full, b & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) tmem_load(lanes + C::kColG + W * part + 32 * c, g[c]);
+#pragma unroll
+                for (int c = 0; c < W / 32; ++c) load_wait(g[c]);
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(bars.g_read);
-            }
-            if (!whole) {
+                const int seen = lim - j * BN - W * part;
+                if (!__all_sync(kFull, seen >= W)) {
 #pragma unroll
-                for (int c = 0; c < W; ++c)
-                    if (c < low) g[c / 32][c % 32] = 0u;
-            }
-#pragma unroll
-            for (int c = 0; c < W; c += 4) {
-                const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(vec + W + c);
-#pragma unroll
-                for (int e = c; e < c + 4; e += 2) {
-                    const float2 y = unpair(mul2(pair_bits(s[e], s[e + 1]),
-                                                 add2(pair_bits(g[e / 32][e % 32], g[e / 32][e % 32 + 1]),
-                                                      e > c ? d.y : d.x)));
-                    w[e / 2] = pack_bf16(y.x, y.y);
+                    for (int c = 0; c < W; ++c)
+                        if (c >= seen) s[c] = g[c / 32][c % 32] = 0u;
                 }
-            }
-            if (C::kOwn && it > 0 && !__all_sync(kFull, bar_wait(bars.w_done, (it - 1) & 1, kTries))) {
-                failed = true;
-                break;
-            }
-            fence_after();
-            tmem_store(d_addr, w);
-            store_wait();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(bars.w_full);
-        }
-        const int64_t token = q.k0 + (int64_t)j;
-        if (blocks > 0) {
-            if (!failed) failed = !__all_sync(kFull, bar_wait(bars.done, 0, kTries));
-            fence_after();
-            // K's and V's tiles are read for the last time: dK and dV go through
-            // their memory, half of the columns at a time
-            for (int c = part; c < 4 && !failed; c += C::kParts) {
-                const int col = DP / 2 * (c & 1);
-                write_rows<DP / 2>(lanes + (c >= 2 ? kColK : kColV) + col, smem + warp * 32 * DP, c >= 2 ? a.dk : a.dv,
-                                   token - lane, head, q.m - (j - lane), col, a.D, c >= 2 ? a.scale : 1.f);
+#pragma unroll
+                for (int c = 0; c < W; c += 2) {
+                    const float2 d = unpair(mul2(pair_bits(s[c], s[c + 1]),
+                                                 add2(pair_bits(g[c / 32][c % 32], g[c / 32][c % 32 + 1]), delta2)));
+                    w[c / 2] = pack_bf16(d.x, d.y);
+                }
+                // dS's place: the block before is done with it, and at an item's
+                // start every warp with the sums of the one before
+                if ((r1 > 0 && !__all_sync(kFull, bar_wait(bars.w_done, (r1 - 1) & 1, kTries))) ||
+                    (j == 0 && n > 0 && !__all_sync(kFull, bar_wait(bars.acc_free, (n - 1) & 1, kTries)))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                tmem_store(lanes + C::kColW + W / 2 * part, w);
+                store_wait();
+                fence_before();
                 __syncwarp();
+                if (lane == 0) bar_arrive(bars.w_full);
             }
-        } else if (j < q.m && part < 2) {
-            const Out &out = part ? a.dk : a.dv;
-            write_zero_row(out.p + token * out.ts + head * out.hs, a.D);
+            if (failed) break;
+            const bool live = r < it.q.n;
+            failed |= !bars.get_warp(it, c);
+            if (failed) break;
+            if (it.kind == kQueries) load_row();
+            if (blocks > 0) {
+                if (!__all_sync(kFull, bar_wait(bars.acc_full, n & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                auto read = [&]() {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(bars.acc_free);
+                };
+                constexpr int CH = DP / 32 / C::kParts > 0 ? DP / 32 / C::kParts : 1;
+                if (part < DP / 32 / CH)
+                    write_columns<CH>(lanes + C::kColSum + 32 * CH * part, stage, a.dq, token, head, rows, 32 * CH * part,
+                                      a.D, a.scale, read);
+                else
+                    read();
+                ++n;
+            } else if (live && part == 0) {
+                write_zero_row(a.dq.p + (token + lane) * a.dq.ts + head * a.dq.hs, a.D);
+            }
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
@@ -1235,8 +1511,13 @@ dpb_status check_offsets(const dpb_attention_config *c, const int32_t *cu_q, con
     return DPB_OK;
 }
 
+// The status word; then, for the gradient, a Plan, its lists of tiles (sound
+// offsets give no more than a tile for every 128 tokens and one a sequence)
+// and delta.
+int64_t most_tiles(int64_t tokens, int seqs) { return tokens / kRows + seqs; }
 size_t attention_workspace(const dpb_attention_config *c) {
-    return kStatusBytes + sizeof(float) * (size_t)c->heads_q * (size_t)c->total_q;
+    return kStatusBytes + sizeof(Task) * (size_t)(1 + most_tiles(c->total_k, c->seqs) + most_tiles(c->total_q, c->seqs)) +
+           sizeof(float) * (size_t)c->heads_q * (size_t)c->total_q;
 }
 
 void fill_args(AttnArgs &a, const dpb_attention_config *c, const int32_t *cu_q, const int32_t *cu_k, void *ws) {
@@ -1272,11 +1553,15 @@ cudaError_t registers_cover(const void *kernel) {
                : cudaErrorLaunchOutOfResources;
 }
 
-// Launches a kernel over tiles x heads x sequences.
+int multiprocessors() {
+    int dev = 0, sms = 1;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        cudaGetLastError();
+    return sms;
+}
+
 template <class C, void (*KERNEL)(AttnArgs)>
-cudaError_t launch_tiles(AttnArgs &a, int tiles, int heads, cudaStream_t s) {
-    a.tiles = tiles;
-    const int64_t blocks = (int64_t)tiles * heads * a.seqs;
+cudaError_t launch_blocks(const AttnArgs &a, int64_t blocks, cudaStream_t s) {
     if (blocks == 0) return cudaSuccess;
     if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     const void *kernel = reinterpret_cast<const void *>(KERNEL);
@@ -1295,14 +1580,21 @@ using Grad128 = GradShape<128>;
 
 template <class C>
 cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
-    return launch_tiles<C, attention_forward_kernel<C>>(a, (int)(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows)), a.hq, s);
+    a.tiles = (int)(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows));
+    return launch_blocks<C, attention_forward_kernel<C>>(a, (int64_t)a.tiles * a.hq * a.seqs, s);
 }
 
 template <class C>
-dpb_status launch_attention_backward(AttnArgs &a, cudaStream_t s) {
-    const int qt = (int)(((int64_t)a.max_q + kRows - 1) / kRows), kt = (int)(((int64_t)a.max_k + kRows - 1) / kRows);
-    DPB_CHECK(launch_status(launch_tiles<C, attention_grad_q_kernel<C>>(a, qt, a.hq, s), "attention_backward (queries)"));
-    return launch_status(launch_tiles<C, attention_grad_kv_kernel<C>>(a, kt, a.hkv, s), "attention_backward (keys)");
+dpb_status launch_attention_backward(const AttnArgs &a, cudaStream_t s) {
+    const int sms = multiprocessors();
+    constexpr int kLanes = C::DP / 8, kRowsAtOnce = 512 / kLanes;
+    const int64_t rows = a.total_q * a.hq;
+    const int64_t blocks = 1 + std::min<int64_t>((rows + kRowsAtOnce - 1) / kRowsAtOnce, 16 * sms);
+    attention_delta_kernel<kLanes><<<(unsigned)blocks, 512, 0, s>>>(a);
+    DPB_CHECK(launch_status(cudaGetLastError(), "attention_backward (delta)"));
+    const int64_t items = a.cap_k * a.hkv + a.cap_q * a.hq;
+    return launch_status(launch_blocks<C, attention_grad_kernel<C>>(a, std::min<int64_t>(items, sms), s),
+                         "attention_backward");
 }
 
 }  // namespace
@@ -1364,7 +1656,12 @@ dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_hea
     DPB_CHECK(need_workspace(workspace, workspace_bytes, attention_workspace(cfg)));
     AttnArgs a{};
     fill_args(a, cfg, cu_q, cu_k, workspace);
-    a.delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + kStatusBytes);
+    char *ws = static_cast<char *>(workspace) + kStatusBytes;
+    a.cap_k = most_tiles(cfg->total_k, cfg->seqs), a.cap_q = most_tiles(cfg->total_q, cfg->seqs);
+    a.plan = reinterpret_cast<Plan *>(ws);
+    a.tasks_k = reinterpret_cast<Task *>(ws) + 1;
+    a.tasks_q = a.tasks_k + a.cap_k;
+    a.delta = reinterpret_cast<float *>(a.tasks_q + a.cap_q);
     a.lse = const_cast<float *>(lse);
     a.o = in_rows(o);
     a.go = in_rows(grad_o);

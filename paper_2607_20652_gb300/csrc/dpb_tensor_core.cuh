@@ -57,9 +57,6 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap *map, i
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
-__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-}
 // This thread's plain shared-memory writes become visible to copies and
 // matrix products.
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }

@@ -449,9 +449,9 @@ dpb_status dpb_attention_forward(const dpb_attention_config *cfg, const dpb_head
  * probabilities are recomputed from q, k and lse:
  *   P = exp(S - lse), delta_i = <grad_o_i, o_i>, dS = P (grad_o v^T - delta),
  *   grad_v = P^T grad_o, grad_q = scale dS k, grad_k = scale dS^T q,
- * with grad_k and grad_v summed over the query heads of their group. No
- * atomics: equal inputs give equal bits. P and dS enter their products in
- * bf16, sums are fp32.
+ * with grad_k and grad_v summed over the query heads of their group, all
+ * sums in an order that the lengths alone fix: equal inputs give equal bits on
+ * the same GPU. P and dS enter their products in bf16, sums are fp32.
  */
 dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_heads *q, const dpb_heads *k,
                                   const dpb_heads *v, const dpb_heads *o, const float *lse,

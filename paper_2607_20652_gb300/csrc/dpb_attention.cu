@@ -44,6 +44,7 @@ using bf16 = __nv_bfloat16;
 
 constexpr uint32_t kTries = 1u << 20;  // polls of a wait before it gives up
 constexpr int kRows = 128;             // rows of a tile (M of the products)
+constexpr int kMostWarps = 16;         // row warps of a gradient block, at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Out {
@@ -68,6 +69,9 @@ struct AttnArgs {
     struct Plan *plan;  // of the gradient
     struct Task *tasks_k, *tasks_q;
     int64_t cap_k, cap_q;
+    int *arrived;  // [slots][row warps]
+    float *parts;  // [slots][128][2 DP]
+    int slots, sms;
     int32_t *status;
 };
 
@@ -589,7 +593,8 @@ struct GradShape {
     static constexpr int kStep = kOwn ? kWidth / 2 : kWidth;  // columns from one part's P to the next's
     static constexpr int kVec = kRowWarps * 2 * kWidth * 4;   // a warp's lse and delta of its columns
     static constexpr int kStage = 32 * 32 * 2;                // a warp's rows of 32 result columns
-    static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + kRowWarps * kStage + 32 * kItems + 8 * kBars + 16;
+    static constexpr int64_t kSlot = kRows * 2 * DP;          // floats of a part's sums
+    static constexpr int kSmem = 1024 + 2 * kTile + NS * kTile + kVec + kRowWarps * kStage + 48 * kItems + 8 * kBars + 16;
     using Slots = Ring<NS, kTile, NS == 4>;
 };
 
@@ -614,10 +619,15 @@ __device__ __forceinline__ void sum_product(uint32_t d, uint32_t a, uint32_t ste
         mma_ts(d, a + (k / kPer) * step + (k % kPer) * 8, desc_at(db, k * 2048), mma_shape(C::DP, true), add || k > 0);
 }
 
-// A tile of the gradient's work: of keys or of queries of one sequence.
+// A part of the gradient's work: blocks [first, first + count) of those that a
+// tile of keys or queries of one sequence meets. Where they are not all of them,
+// each of the `pieces` parts leaves its sums in memory (head h in place slot +
+// h pieces + piece), and who comes last adds them up.
 struct Task {
-    int q0, n, k0, m, tile, pad[3];
+    int q0, n, k0, m, tile, first, count, pieces, slot, piece, pad[2];
 };
+constexpr int kLeast = 8;    // blocks of a part: its sums cost as much as one or two
+constexpr int kSlots = 304;  // parts with sums in memory, at most: two for each of 152 SMs
 // How many there are, and the next item (a tile of a head) that no block has.
 struct Plan {
     unsigned long long next;
@@ -627,7 +637,7 @@ struct Plan {
 // What a block takes on: a tile of keys, a tile of queries, or the end.
 enum { kKeys, kQueries, kEnd };
 struct Item {
-    int kind, head, tile;
+    int kind, head, tile, first, count, pieces, slot, piece;
     Seq q;
 };
 
@@ -645,7 +655,7 @@ struct GradBars {
     uint32_t *slot;
     __device__ __forceinline__ GradBars(uint8_t *smem) {
         items = reinterpret_cast<int4 *>(smem + (2 + C::NS) * C::kTile + C::kVec + C::kRowWarps * C::kStage);
-        uint64_t *bars = reinterpret_cast<uint64_t *>(items + 2 * C::kItems);
+        uint64_t *bars = reinterpret_cast<uint64_t *>(items + 3 * C::kItems);
         tile_full = smem_addr(bars);
         tile_free = tile_full + 16;
         ring = {smem + 2 * C::kTile, tile_full + 32, tile_full + 32 + 8 * C::NS, tile_full + 32 + 16 * C::NS};
@@ -682,17 +692,19 @@ struct GradBars {
         if (c >= C::kItems && !__all_sync(kFull, bar_wait(item_free + 8 * at, ((c / C::kItems) & 1) ^ 1, kTries)))
             return false;
         if (elect_one()) {
-            items[2 * at] = make_int4(it.kind, it.head, it.tile, it.q.q0);
-            items[2 * at + 1] = make_int4(it.q.n, it.q.k0, it.q.m, 0);
+            items[3 * at] = make_int4(it.q.q0, it.q.n, it.q.k0, it.q.m);
+            items[3 * at + 1] = make_int4(it.tile, it.first, it.count, it.pieces);
+            items[3 * at + 2] = make_int4(it.slot, it.piece, it.kind, it.head);
             bar_arrive(item_full + 8 * at);
         }
         __syncwarp();
         return true;
     }
     __device__ __forceinline__ void read(Item &it, int at) const {
-        const int4 x = items[2 * at], y = items[2 * at + 1];
-        it.kind = x.x, it.head = x.y, it.tile = x.z;
-        it.q.q0 = x.w, it.q.n = y.x, it.q.k0 = y.y, it.q.m = y.z;
+        const int4 x = items[3 * at], y = items[3 * at + 1], z = items[3 * at + 2];
+        it.q.q0 = x.x, it.q.n = x.y, it.q.k0 = x.z, it.q.m = x.w;
+        it.tile = y.x, it.first = y.y, it.count = y.z, it.pieces = y.w;
+        it.slot = z.x, it.piece = z.y, it.kind = z.z, it.head = z.w;
     }
     // One thread, or all lanes of a warp: item c.
     __device__ __forceinline__ bool get_one(Item &it, int &c) const {
@@ -703,14 +715,17 @@ struct GradBars {
         ++c;
         return true;
     }
+    // (A warp keeps it in the list until it has finished the item.)
     __device__ __forceinline__ bool get_warp(Item &it, int &c) const {
         const int at = c % C::kItems;
         if (!__all_sync(kFull, bar_wait(item_full + 8 * at, (c / C::kItems) & 1, kTries))) return false;
         read(it, at);
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) bar_arrive(item_free + 8 * at);
         ++c;
         return true;
+    }
+    __device__ __forceinline__ void finished(int c) const {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(item_free + 8 * (c % C::kItems));
     }
 };
 
@@ -730,16 +745,25 @@ struct KeyBlocks {
 
 // Lists the tiles of keys and of queries of all sequences, those with the most
 // blocks first (to 1/256 of the longest; their order within that does not
-// matter to any result). One block of THREADS.
+// matter to any result). A tile of more than half an SM's share of all blocks
+// is listed in parts, as far as there is room for their sums; which, follows
+// from the numbers of blocks alone. One block of THREADS.
 template <int THREADS>
 __device__ void make_plan(const AttnArgs &a) {
     constexpr int kBuckets = 256;
     __shared__ int place[2][kBuckets];
+    __shared__ unsigned long long total;
+    __shared__ int longest, slot, split;
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const int64_t most = (int64_t)((max(a.max_q, a.max_k) - 1) / kRows + 1) * a.group;
     int shift = 0;
-    while ((((max(a.max_q, a.max_k) - 1) / kRows + 1) >> shift) >= kBuckets) ++shift;
-    for (int i = threadIdx.x; i < 2 * kBuckets; i += THREADS) place[i / kBuckets][i % kBuckets] = 0;
-    __syncthreads();
+    while ((most >> shift) >= kBuckets) ++shift;
+    auto bucket = [&](int blocks) { return kBuckets - 1 - (blocks >> shift); };
+    auto clear = [&]() {
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * kBuckets; i += THREADS) place[i / kBuckets][i % kBuckets] = 0;
+        __syncthreads();
+    };
     // f(side, sequence, tile, blocks)
     auto each = [&](auto f, bool report) {
         for (int s = warp; s < a.seqs; s += THREADS / 32) {
@@ -748,12 +772,59 @@ __device__ void make_plan(const AttnArgs &a) {
                 if (report && lane == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
                 continue;
             }
-            for (int t = lane; t * kRows < q.m; t += 32) f(0, q, t, KeyBlocks::of<kRows>(a, q, t).per_head);
+            for (int t = lane; t * kRows < q.m; t += 32) f(0, q, t, KeyBlocks::of<kRows>(a, q, t).count);
             for (int t = lane; t * kRows < q.n; t += 32) f(1, q, t, tile_blocks<kRows>(a, q, t));
         }
     };
-    each([&](int side, const Seq &, int, int blocks) { atomicAdd(&place[side][kBuckets - 1 - (blocks >> shift)], 1); }, true);
+    if (threadIdx.x == 0) total = 0, longest = 0x7fffffff, slot = 0, split = 0;
+    unsigned long long mine = 0;
+    clear();
+    each(
+        [&](int side, const Seq &, int, int blocks) {
+            atomicAdd(&place[side][bucket(blocks)], 1);
+            mine += (unsigned long long)blocks * (side ? a.hq : a.hkv);
+        },
+        true);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(kFull, mine, o);
+    if (lane == 0 && mine > 0) atomicAdd(&total, mine);
     __syncthreads();
+    // the parts of a tile of (about) as many blocks, none longer than l
+    auto parts = [&](int blocks, int l) {
+        return blocks > l ? min((blocks | ((1 << shift) - 1)) / l + 1, blocks) : 1;
+    };
+    if (a.slots > 0) {
+        if (warp == 0) {
+            int l = (int)min(max((unsigned long long)kLeast, total / (2 * a.sms)), 0x40000000ull);
+            for (;;) {
+                int64_t need = 0;
+                for (int i = lane; i < 2 * kBuckets; i += 32) {
+                    // the most blocks of the bucket: no tile of it has more parts
+                    const int n = place[i / kBuckets][i % kBuckets];
+                    const int blocks = ((kBuckets - i % kBuckets) << shift) - 1;
+                    if (n > 0 && blocks > l) need += n * (int64_t)(i < kBuckets ? a.hkv : a.hq) * (blocks / l + 1);
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) need += __shfl_xor_sync(kFull, need, o);
+                if (lane == 0) split = need > 0;
+                if (need <= a.slots) break;
+                l += l / 4;
+            }
+            if (lane == 0) longest = l;
+        }
+        __syncthreads();
+    }
+    if (split) {
+        for (int i = threadIdx.x; i < a.slots * kMostWarps; i += THREADS) a.arrived[i] = 0;
+        clear();
+        each(
+            [&](int side, const Seq &, int, int blocks) {
+                const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
+                for (int i = 0; i < n; ++i) atomicAdd(&place[side][bucket(each_has + (i < more))], 1);
+            },
+            false);
+        __syncthreads();
+    }
     if (warp < 2) {
         int before = 0;
         for (int i = lane; i < kBuckets; i += 32) {
@@ -779,10 +850,15 @@ __device__ void make_plan(const AttnArgs &a) {
     __syncthreads();
     each(
         [&](int side, const Seq &q, int t, int blocks) {
-            const int at = atomicAdd(&place[side][kBuckets - 1 - (blocks >> shift)], 1);
-            // more than sound offsets can have
-            if (at >= (side ? a.cap_q : a.cap_k)) return set_status(a.status, DPB_DEV_BAD_LENGTH);
-            (side ? a.tasks_q : a.tasks_k)[at] = Task{q.q0, q.n, q.k0, q.m, t, {0, 0, 0}};
+            const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
+            const int base = n > 1 ? atomicAdd(&slot, n * (side ? a.hq : a.hkv)) : 0;
+            for (int i = 0; i < n; ++i) {
+                const int first = i * each_has + min(i, more), count = each_has + (i < more);
+                const int at = atomicAdd(&place[side][bucket(count)], 1);
+                // more than sound offsets can have
+                if (at >= (side ? a.cap_q : a.cap_k)) return set_status(a.status, DPB_DEV_BAD_LENGTH);
+                (side ? a.tasks_q : a.tasks_k)[at] = Task{q.q0, q.n, q.k0, q.m, t, first, count, n, base, i, {0, 0}};
+            }
         },
         false);
 }
@@ -791,43 +867,91 @@ __device__ void make_plan(const AttnArgs &a) {
 // times f) as bf16 to columns [col, min(col + 32 CH, D)), 32 at a time through
 // `stage` (their 16-byte pieces exchanged so that neither side meets bank
 // conflicts), so that a store covers whole stretches of rows. Rows from `rows`
-// on are left out. read() is called once TMEM has been read.
+// on are left out. read() is called once TMEM has been read. Of an item in
+// parts the sums go to memory, and the warp that is the last of its like there
+// adds them up, always in the parts' order.
 template <int CH, typename F>
-__device__ __forceinline__ void write_columns(uint32_t tmem, uint8_t *stage, const Out &out, int64_t token, int head,
-                                              int rows, int col, int D, float f, F read) {
-    const int lane = threadIdx.x & 31;
-    uint32_t u[CH][16];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        uint32_t v[32];
-        tmem_load(tmem + 32 * c, v);
-        load_wait(v);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            u[c][e] = pack_bf16(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f);
-    }
-    read();
-    const int piece = lane & 3, r0 = lane >> 2;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4 *>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) =
-                make_uint4(u[c][4 * i], u[c][4 * i + 1], u[c][4 * i + 2], u[c][4 * i + 3]);
+__device__ __forceinline__ void write_columns(const AttnArgs &a, uint32_t tmem, uint8_t *stage, const Out &out,
+                                              int64_t token, const Item &it, int rows, int col, float f,
+                                              int64_t slot_floats, F read) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const int quad = lane & 3, r0 = lane >> 2;
+    auto place = [&](int i) { return stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16); };  // of this lane's piece i
+    auto write = [&](int c) {
         __syncwarp();
         uint4 x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = r0 + 8 * i;
-            x[i] = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((piece ^ ((r >> 1) & 3)) * 16));
+            x[i] = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((quad ^ ((r >> 1) & 3)) * 16));
         }
-        const int at = col + 32 * c + 8 * piece;
-        if (at < D)
+        const int at = col + 32 * c + 8 * quad;
+        if (at < a.D)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (r0 + 8 * i < rows)
-                    *reinterpret_cast<uint4 *>(out.p + (token + r0 + 8 * i) * out.ts + head * out.hs + at) = x[i];
+                    *reinterpret_cast<uint4 *>(out.p + (token + r0 + 8 * i) * out.ts + it.head * out.hs + at) = x[i];
+        __syncwarp();
+    };
+    if (it.pieces == 1) {
+        uint32_t u[CH][16];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            uint32_t v[32];
+            tmem_load(tmem + 32 * c, v);
+            load_wait(v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                u[c][e] = pack_bf16(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f);
+        }
+        read();
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<uint4 *>(place(i)) =
+                    make_uint4(u[c][4 * i], u[c][4 * i + 1], u[c][4 * i + 2], u[c][4 * i + 3]);
+            write(c);
+        }
+        return;
+    }
+    const int slot = it.slot + it.head * it.pieces;
+    float4 *sums = reinterpret_cast<float4 *>(a.parts + slot * slot_floats + warp * (CH * 1024)) + lane;
+    const int64_t step = slot_floats / 4;  // from one part's to the next's
+#pragma unroll 1
+    for (int c = 0; c < CH; ++c) {
+        uint32_t v[32];
+        tmem_load(tmem + 32 * c, v);
+        load_wait(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            __stcg(sums + it.piece * step + (8 * c + e) * 32,
+                   make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]),
+                               __uint_as_float(v[4 * e + 3])));
+    }
+    read();
+    __threadfence();
+    __syncwarp();
+    int before = 0;
+    if (lane == 0) before = atomicAdd(a.arrived + slot * kMostWarps + warp, 1);
+    if (__shfl_sync(kFull, before, 0) != it.pieces - 1) return;
+    __threadfence();
+#pragma unroll 1
+    for (int c = 0; c < CH; ++c) {
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+            const float4 *part = sums + (8 * c + 2 * i) * 32;
+#pragma unroll 4
+            for (int k = 0; k < it.pieces; ++k, part += step) {
+                const float4 p = __ldcg(part), q = __ldcg(part + 32);
+                x.x += p.x, x.y += p.y, x.z += p.z, x.w += p.w;
+                y.x += q.x, y.y += q.y, y.z += q.z, y.w += q.w;
+            }
+            *reinterpret_cast<uint4 *>(place(i)) = make_uint4(pack_bf16(x.x * f, x.y * f), pack_bf16(x.z * f, x.w * f),
+                                                              pack_bf16(y.x * f, y.y * f), pack_bf16(y.z * f, y.w * f));
+        }
+        write(c);
     }
 }
 
@@ -836,6 +960,7 @@ __device__ __forceinline__ void write_columns(uint32_t tmem, uint8_t *stage, con
 // a row, 8 values each.
 template <int LANES>
 __global__ void __launch_bounds__(512) attention_delta_kernel(const __grid_constant__ AttnArgs a) {
+    start_next();
     if (blockIdx.x == 0) return make_plan<512>(a);
     constexpr int kRowsAtOnce = 512 / LANES;
     const int64_t rows = a.total_q * a.hq, stride = (int64_t)(gridDim.x - 1) * kRowsAtOnce;
@@ -870,12 +995,12 @@ __global__ void __launch_bounds__(512) attention_delta_kernel(const __grid_const
 //
 // Measured, with the delta kernel (causal; rate of the five products that are
 // the least: 2.5 x the forward's), against a kernel for each side with a block
-// for each tile: 1 x 12289, 12 heads of 64: 641 us (666), 904 TFLOP/s; 8 x 1024,
-// 12 heads of 64: 71 us (98); 1 x 8192, 16 heads of 128: 573 us (590), 1199
-// TFLOP/s, of seven products done 1679; 12 sequences of 1 to 3001, 16 heads of
-// 128 on 4: 140 us (215). Bound by the tensor cores at 128; at 64 by the
-// exponentials and the conversions beside them; the ragged batch by its
-// longest tile of keys, which meets all its group's queries on one SM (128 us).
+// for each tile: 1 x 12289, 12 heads of 64: 648 us (666), 895 TFLOP/s; 8 x 1024,
+// 12 heads of 64: 73 us (98); 1 x 8192, 16 heads of 128: 576 us (590), 1193
+// TFLOP/s, of the seven products done 1670; sequences of 3001, 638, 429, 95 and
+// less, 16 heads of 128 on 4: 126 us (215; 140 with no tile in parts, when one SM
+// has the longest tile of keys for 128 us). Bound by the tensor cores at 128; at
+// 64 by the exponentials and the conversions beside them.
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int DP = C::DP, BN = C::BN, W = C::kWidth;
@@ -893,6 +1018,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
     if (warp == C::kCopier) {
         bars.make();
         setup_arrive<C::kThreads>();
+        wait_previous();
         const int64_t keys = (int64_t)a.plan->keys * a.hkv, all = keys + (int64_t)a.plan->queries * a.hq;
         int64_t at = blockIdx.x;
         // ring's tiles copied, items with blocks, copies of each of the two tiles
@@ -905,9 +1031,10 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 const int64_t rest = queries ? at - keys : at;
                 const int heads = queries ? a.hq : a.hkv;
                 const int4 *t = reinterpret_cast<const int4 *>((queries ? a.tasks_q : a.tasks_k) + rest / heads);
-                const int4 x = t[0];
+                const int4 x = t[0], y = t[1], z = t[2];
                 it.q.q0 = x.x, it.q.n = x.y, it.q.k0 = x.z, it.q.m = x.w;
-                it.tile = t[1].x;
+                it.tile = y.x, it.first = y.y, it.count = y.z, it.pieces = y.w;
+                it.slot = z.x, it.piece = z.y;
                 it.head = (int)(rest % heads);
             }
             failed = !bars.put(it, c);
@@ -915,8 +1042,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             ++c;
             const Seq &q = it.q;
             const KeyBlocks kb = KeyBlocks::of<BN>(a, q, it.tile);
-            const int count = queries ? tile_blocks<BN>(a, q, it.tile) : kb.count;
-            if (count > 0) {
+            if (it.count > 0) {
                 auto rows = [&](const CUtensorMap *map, int t) {
                     failed = failed ||
                              (n > 0 && !__all_sync(kFull, bar_wait(bars.tile_free + 8 * t, (n - 1) & 1, kTries)));
@@ -929,7 +1055,9 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                     }
                     __syncwarp();
                 };
-                int h = queries ? it.head / a.group : it.head * a.group, b = queries ? 0 : kb.b0;
+                const int before = queries || it.first == 0 ? 0 : it.first / kb.per_head;  // heads of the group
+                int h = queries ? it.head / a.group : it.head * a.group + before;
+                int b = queries ? it.first : kb.b0 + it.first - before * kb.per_head;
                 const int first = queries ? q.k0 : q.q0, length = queries ? q.m : q.n;
                 // V's product sums over columns of the head alone
                 auto block = [&](const CUtensorMap *map, bool sums) {
@@ -943,7 +1071,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 block(x, true);
                 rows(queries ? &a.g : &a.v, 1);
                 block(y, !queries);
-                for (int e = 1; e < count && !failed; ++e) {
+                for (int e = 1; e < it.count && !failed; ++e) {
                     ++b;
                     if (!queries && b == kb.b0 + kb.per_head) b = kb.b0, ++h;
                     block(x, true);
@@ -994,7 +1122,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 // P^T and dS^T have columns of their own: the next S^T and gradient
                 // of P^T are computed as soon as these have been read
                 for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
-                    const int blocks = KeyBlocks::of<BN>(a, it.q, it.tile).count;
+                    const int blocks = it.count;
                     for (int j = 0; j < blocks; ++j, ++b, i += 2) {
                         failed = (j == 0 && !bar_wait(bars.tile_full, n & 1, kTries)) || !ring.wait_full(i) ||
                                  (b > 0 && !bar_wait(bars.s_read, (b - 1) & 1, kTries));
@@ -1013,7 +1141,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 // it (products run in the order of their issue): while the rows'
                 // arithmetic makes P^T, dK and the next gradient are computed, while
                 // it makes dS^T, dV and the next S^T, which may be the next item's.
-                auto blocks_of = [&]() { return it.kind == kKeys ? KeyBlocks::of<BN>(a, it.q, it.tile).count : 0; };
+                auto blocks_of = [&]() { return it.kind == kKeys ? it.count : 0; };
                 // the next tile of keys that meets queries (or what comes after the last)
                 auto next_item = [&]() {
                     do failed = failed || !bars.get_one(it, c);
@@ -1066,7 +1194,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             // those of the block before have been read
             int r = C::kOwn ? b : 0;  // blocks of these two barriers
             for (; !failed && it.kind == kQueries; failed = failed || !bars.get_one(it, c)) {
-                const int blocks = tile_blocks<BN>(a, it.q, it.tile);
+                const int blocks = it.count;
                 for (int j = 0; j < blocks; ++j, ++r, i += 2) {
                     failed = (j == 0 && !bar_wait(bars.tile_full, n & 1, kTries)) || !ring.wait_full(i) ||
                              (r > 0 && !bar_wait(bars.s_read, (r - 1) & 1, kTries));
@@ -1094,7 +1222,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             failed = !bars.get_one(it, c);
             if (C::kOwn) {
                 for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
-                    const int blocks = KeyBlocks::of<BN>(a, it.q, it.tile).count;
+                    const int blocks = it.count;
                     for (int j = 0; j < blocks; ++j, ++b, i += 2) {
                         failed = !bar_wait(bars.v_full, b & 1, kTries) ||
                                  (j == 0 && n > 0 && !bar_wait(bars.acc_free, (n - 1) & 1, kTries));
@@ -1116,7 +1244,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
                     // the issuer's; each is seen to its end, so that the barriers'
                     // parities below are those of this item's blocks
-                    const int blocks = KeyBlocks::of<BN>(a, it.q, it.tile).count;
+                    const int blocks = it.count;
                     if (blocks == 0) continue;
                     failed = !bar_wait(bars.acc_full, n & 1, kTries);
                     b += blocks, i += 2 * blocks, ++n;
@@ -1124,7 +1252,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             }
             // dQ += dS K (K's scores are done: the row warps had them)
             for (; !failed && it.kind == kQueries; failed = failed || !bars.get_one(it, c)) {
-                const int blocks = tile_blocks<BN>(a, it.q, it.tile);
+                const int blocks = it.count;
                 for (int j = 0; j < blocks; ++j, ++b, i += 2) {
                     failed = !bar_wait(bars.w_full, b & 1, kTries) ||
                              (j == 0 && n > 0 && !bar_wait(bars.acc_free, (n - 1) & 1, kTries));
@@ -1152,6 +1280,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
         uint8_t *stage = smem + (2 + C::NS) * C::kTile + C::kVec + warp * C::kStage;
         const uint64_t scale2 = pair(a.scale2, a.scale2);
         int b = 0, n = 0;  // blocks and items with blocks so far
+        wait_previous();
         failed = !bars.get_warp(it, c);
 
         // ---- tiles of keys
@@ -1179,15 +1308,17 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
         };
         auto start = [&]() {
             k = KeyBlocks::of<BN>(a, it.q, it.tile);
-            h = it.head * a.group, fb = k.b0;
-            if (k.count > 0) fetch();
+            if (it.count > 0) {
+                const int before = it.first == 0 ? 0 : it.first / k.per_head;
+                h = it.head * a.group + before, fb = k.b0 + it.first - before * k.per_head;
+                fetch();
+            }
         };
         if (!failed && it.kind == kKeys) start();
         while (!failed && it.kind == kKeys) {
-            const int r = it.tile * kRows + (threadIdx.x & 127), head = it.head, rows = it.q.m - (r - lane);
-            const int64_t token = it.q.k0 + (int64_t)(r - lane);  // of the warp's first row
-            const int off = it.q.m - it.q.n, count = k.count;
-            int bi = k.b0;  // the block at hand
+            const int r = it.tile * kRows + (threadIdx.x & 127), count = it.count;
+            const int below = a.causal ? r - (it.q.m - it.q.n) - W * part : 0;  // queries before it do not see key r
+            int bi = (fb == k.b0 ? k.b0 + k.per_head : fb) - 1;  // the block at hand: the one fetched
             for (int e = 0; e < count; ++e, ++b) {
                 __syncwarp();
 #pragma unroll
@@ -1200,7 +1331,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 __syncwarp();
                 if (e + 1 < count) fetch();
                 // masked: query i sees key r when i >= r - off
-                const int low = a.causal ? r - off - bi * BN - W * part : 0;
+                const int low = below - bi * BN;
                 if (++bi == k.b0 + k.per_head) bi = k.b0;
                 const bool whole = __all_sync(kFull, low <= 0);
                 if (!__all_sync(kFull, bar_wait(bars.s_full, b & 1, kTries))) {
@@ -1292,11 +1423,14 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 if (lane == 0) bar_arrive(bars.w_full);
             }
             if (failed) break;
-            const bool live = r < it.q.m;
-            failed |= !bars.get_warp(it, c);
+            failed = !bars.get_warp(it, c);
             if (failed) break;
             if (it.kind == kKeys) start();
-            if (count > 0) {
+            Item was;  // the item that ends here
+            bars.read(was, (c - 2) % C::kItems);
+            const int first = was.tile * kRows + (warp & 3) * 32;  // the warp's first row
+            const int64_t token = was.q.k0 + (int64_t)first;
+            if (was.count > 0) {
                 if (!__all_sync(kFull, bar_wait(bars.acc_full, n & 1, kTries))) {
                     failed = true;
                     break;
@@ -1306,17 +1440,18 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 constexpr int CH = 2 * DP / 32 / C::kParts;
                 const int c0 = part * CH, col = 32 * c0 % DP;
                 const bool keys = 32 * c0 >= DP;
-                write_columns<CH>(lanes + C::kColSum + 32 * c0, stage, keys ? a.dk : a.dv, token, head, rows, col, a.D,
-                                  keys ? a.scale : 1.f, [&]() {
+                write_columns<CH>(a, lanes + C::kColSum + 32 * c0, stage, keys ? a.dk : a.dv, token, was, was.q.m - first,
+                                  col, keys ? a.scale : 1.f, C::kSlot, [&]() {
                                       fence_before();
                                       __syncwarp();
                                       if (lane == 0) bar_arrive(bars.acc_free);
                                   });
                 ++n;
-            } else if (live && part < 2) {
+            } else if (first + lane < was.q.m && part < 2) {
                 const Out &out = part ? a.dk : a.dv;
-                write_zero_row(out.p + (token + lane) * out.ts + head * out.hs, a.D);
+                write_zero_row(out.p + (token + lane) * out.ts + was.head * out.hs, a.D);
             }
+            bars.finished(c - 2);
         }
 
         // ---- tiles of queries
@@ -1336,9 +1471,9 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
         int r1 = C::kOwn ? b : 0;
         if (!failed && it.kind == kQueries) load_row();
         while (!failed && it.kind == kQueries) {
-            const int r = it.tile * kRows + (threadIdx.x & 127), head = it.head, rows = it.q.n - (r - lane);
-            const int64_t token = it.q.q0 + (int64_t)(r - lane);  // of the warp's first row
-            const int lim = visible(a, it.q, r), blocks = tile_blocks<BN>(a, it.q, it.tile);
+            const int blocks = it.count;
+            // keys that the row sees, from this part's first on
+            const int lim = visible(a, it.q, it.tile * kRows + (threadIdx.x & 127)) - it.first * BN - W * part;
             // a row that sees nothing: every probability 0
             const float l2 = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
             const uint64_t lse22 = pair(l2, l2), delta2 = pair(-delta, -delta);
@@ -1377,7 +1512,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(bars.g_read);
-                const int seen = lim - j * BN - W * part;
+                const int seen = lim - j * BN;
                 if (!__all_sync(kFull, seen >= W)) {
 #pragma unroll
                     for (int c = 0; c < W; ++c)
@@ -1404,11 +1539,14 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 if (lane == 0) bar_arrive(bars.w_full);
             }
             if (failed) break;
-            const bool live = r < it.q.n;
-            failed |= !bars.get_warp(it, c);
+            failed = !bars.get_warp(it, c);
             if (failed) break;
             if (it.kind == kQueries) load_row();
-            if (blocks > 0) {
+            Item was;
+            bars.read(was, (c - 2) % C::kItems);
+            const int first = was.tile * kRows + (warp & 3) * 32;
+            const int64_t token = was.q.q0 + (int64_t)first;
+            if (was.count > 0) {
                 if (!__all_sync(kFull, bar_wait(bars.acc_full, n & 1, kTries))) {
                     failed = true;
                     break;
@@ -1421,14 +1559,15 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 };
                 constexpr int CH = DP / 32 / C::kParts > 0 ? DP / 32 / C::kParts : 1;
                 if (part < DP / 32 / CH)
-                    write_columns<CH>(lanes + C::kColSum + 32 * CH * part, stage, a.dq, token, head, rows, 32 * CH * part,
-                                      a.D, a.scale, read);
+                    write_columns<CH>(a, lanes + C::kColSum + 32 * CH * part, stage, a.dq, token, was, was.q.n - first,
+                                      32 * CH * part, a.scale, C::kSlot, read);
                 else
                     read();
                 ++n;
-            } else if (live && part == 0) {
-                write_zero_row(a.dq.p + (token + lane) * a.dq.ts + head * a.dq.hs, a.D);
+            } else if (first + lane < was.q.n && part == 0) {
+                write_zero_row(a.dq.p + (token + lane) * a.dq.ts + was.head * a.dq.hs, a.D);
             }
+            bars.finished(c - 2);
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
@@ -1511,14 +1650,28 @@ dpb_status check_offsets(const dpb_attention_config *c, const int32_t *cu_q, con
     return DPB_OK;
 }
 
-// The status word; then, for the gradient, a Plan, its lists of tiles (sound
-// offsets give no more than a tile for every 128 tokens and one a sequence)
-// and delta.
-int64_t most_tiles(int64_t tokens, int seqs) { return tokens / kRows + seqs; }
-size_t attention_workspace(const dpb_attention_config *c) {
-    return kStatusBytes + sizeof(Task) * (size_t)(1 + most_tiles(c->total_k, c->seqs) + most_tiles(c->total_q, c->seqs)) +
-           sizeof(float) * (size_t)c->heads_q * (size_t)c->total_q;
-}
+// The gradient's workspace after the status word: a Plan and its lists, the
+// counts and sums of tiles in parts, delta. Sound offsets give no more than a
+// tile for every 128 tokens and one a sequence.
+struct GradSpace {
+    int64_t cap_k, cap_q;
+    int slots;
+    size_t plan, tasks_k, tasks_q, arrived, parts, delta, bytes;
+    explicit GradSpace(const dpb_attention_config *c) {
+        const int64_t blocks = ((int64_t)std::max(c->max_q, c->max_k) + kRows - 1) / kRows * (c->heads_q / c->heads_kv);
+        slots = blocks > kLeast ? kSlots : 0;
+        cap_k = c->total_k / kRows + c->seqs + slots;
+        cap_q = c->total_q / kRows + c->seqs + slots;
+        plan = kStatusBytes;
+        tasks_k = plan + sizeof(Task);
+        tasks_q = tasks_k + sizeof(Task) * (size_t)cap_k;
+        arrived = tasks_q + sizeof(Task) * (size_t)cap_q;
+        parts = arrived + sizeof(int) * kMostWarps * (size_t)slots;
+        delta = parts + sizeof(float) * kRows * 2 * (c->head_dim <= 64 ? 64 : 128) * (size_t)slots;
+        bytes = delta + sizeof(float) * (size_t)c->heads_q * (size_t)c->total_q;
+    }
+};
+size_t attention_workspace(const dpb_attention_config *c) { return GradSpace(c).bytes; }
 
 void fill_args(AttnArgs &a, const dpb_attention_config *c, const int32_t *cu_q, const int32_t *cu_k, void *ws) {
     a.cu_q = cu_q;
@@ -1560,7 +1713,9 @@ int multiprocessors() {
     return sms;
 }
 
-template <class C, void (*KERNEL)(AttnArgs)>
+// EARLY: the kernel may start, and set itself up, while the one before it in
+// the stream runs; it waits for that one's results itself.
+template <class C, void (*KERNEL)(AttnArgs), bool EARLY>
 cudaError_t launch_blocks(const AttnArgs &a, int64_t blocks, cudaStream_t s) {
     if (blocks == 0) return cudaSuccess;
     if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
@@ -1569,8 +1724,18 @@ cudaError_t launch_blocks(const AttnArgs &a, int64_t blocks, cudaStream_t s) {
     if (covered != cudaSuccess) return covered;
     const cudaError_t e = allow_smem(kernel, C::kSmem);
     if (e != cudaSuccess) return e;
-    KERNEL<<<(unsigned)blocks, C::kThreads, C::kSmem, s>>>(a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3((unsigned)blocks);
+    how.blockDim = dim3(C::kThreads);
+    how.dynamicSmemBytes = C::kSmem;
+    how.stream = s;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    how.attrs = &early;
+    how.numAttrs = EARLY ? 1 : 0;
+    const cudaError_t launched = cudaLaunchKernelEx(&how, KERNEL, a);
+    return launched == cudaSuccess ? cudaGetLastError() : launched;
 }
 
 using Fwd64 = FwdShape<64, 128, 8>;
@@ -1581,19 +1746,20 @@ using Grad128 = GradShape<128>;
 template <class C>
 cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
     a.tiles = (int)(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows));
-    return launch_blocks<C, attention_forward_kernel<C>>(a, (int64_t)a.tiles * a.hq * a.seqs, s);
+    return launch_blocks<C, attention_forward_kernel<C>, false>(a, (int64_t)a.tiles * a.hq * a.seqs, s);
 }
 
 template <class C>
-dpb_status launch_attention_backward(const AttnArgs &a, cudaStream_t s) {
+dpb_status launch_attention_backward(AttnArgs &a, cudaStream_t s) {
     const int sms = multiprocessors();
+    a.sms = sms;
     constexpr int kLanes = C::DP / 8, kRowsAtOnce = 512 / kLanes;
     const int64_t rows = a.total_q * a.hq;
     const int64_t blocks = 1 + std::min<int64_t>((rows + kRowsAtOnce - 1) / kRowsAtOnce, 16 * sms);
     attention_delta_kernel<kLanes><<<(unsigned)blocks, 512, 0, s>>>(a);
     DPB_CHECK(launch_status(cudaGetLastError(), "attention_backward (delta)"));
     const int64_t items = a.cap_k * a.hkv + a.cap_q * a.hq;
-    return launch_status(launch_blocks<C, attention_grad_kernel<C>>(a, std::min<int64_t>(items, sms), s),
+    return launch_status(launch_blocks<C, attention_grad_kernel<C>, true>(a, std::min<int64_t>(items, sms), s),
                          "attention_backward");
 }
 
@@ -1656,12 +1822,15 @@ dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_hea
     DPB_CHECK(need_workspace(workspace, workspace_bytes, attention_workspace(cfg)));
     AttnArgs a{};
     fill_args(a, cfg, cu_q, cu_k, workspace);
-    char *ws = static_cast<char *>(workspace) + kStatusBytes;
-    a.cap_k = most_tiles(cfg->total_k, cfg->seqs), a.cap_q = most_tiles(cfg->total_q, cfg->seqs);
-    a.plan = reinterpret_cast<Plan *>(ws);
-    a.tasks_k = reinterpret_cast<Task *>(ws) + 1;
-    a.tasks_q = a.tasks_k + a.cap_k;
-    a.delta = reinterpret_cast<float *>(a.tasks_q + a.cap_q);
+    const GradSpace space(cfg);
+    char *ws = static_cast<char *>(workspace);
+    a.cap_k = space.cap_k, a.cap_q = space.cap_q, a.slots = space.slots;
+    a.plan = reinterpret_cast<Plan *>(ws + space.plan);
+    a.tasks_k = reinterpret_cast<Task *>(ws + space.tasks_k);
+    a.tasks_q = reinterpret_cast<Task *>(ws + space.tasks_q);
+    a.arrived = reinterpret_cast<int *>(ws + space.arrived);
+    a.parts = reinterpret_cast<float *>(ws + space.parts);
+    a.delta = reinterpret_cast<float *>(ws + space.delta);
     a.lse = const_cast<float *>(lse);
     a.o = in_rows(o);
     a.go = in_rows(grad_o);

@@ -166,6 +166,13 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// ---- the next kernel of the stream ---------------------------------------------
+
+// It may start once every block has called this or ended (if it is launched to).
+__device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// Waits until the kernel before has ended and its writes are visible.
+__device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ---- registers --------------------------------------------------------------------------
 
 // A warpgroup's share of the registers that the block was launched with; all

@@ -276,3 +276,32 @@ def test_refusals():
             dpb.attention_forward(x, x, x)
     with pytest.raises(dpb.DPBError):
         dpb.attention_forward(q, k, k, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda"))
+
+
+PARTS = [  # long tiles for few heads: their blocks are shared out over several thread blocks
+    ([2500], [2500], 2, 1, 64, True),
+    ([1400, 60], [1400, 2100], 4, 1, 128, False),
+    ([1], [5000], 2, 2, 128, True),
+    ([3000, 10], [100, 4000], 1, 1, 72, True),
+]
+
+
+@pytest.mark.parametrize("nq,nk,H,Hk,D,causal", PARTS)
+def test_long_tiles_in_parts(nq, nk, H, Hk, D, causal):
+    q, k, v, do = draw(nq, nk, H, Hk, D, seed=D + sum(nq))
+    want, tol = formula(q, k, v, do, nq, nk, causal, D ** -0.5)
+    got = run(q, k, v, do, nq, nk, causal)
+    check(got, want, tol)
+    again = run(q, k, v, do, nq, nk, causal)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    assert dpb.status() == 0
+
+
+@pytest.mark.parametrize("cu", [[0, 50, 40, 120], [0, 50, 130, 120], [-3, 50, 90, 120], [0, 50, 120, 121]])
+def test_bad_offsets_are_flagged_by_the_gradient(cu):
+    q, k, v, do = draw([120], [120], 2, 2, 64, seed=7)
+    cu = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    o, lse = dpb.attention_forward(q, k, v)
+    assert dpb.status() == 0
+    dpb.attention_backward(q, k, v, o, lse, do, cu_q=cu, cu_k=cu, max_q=120, max_k=120)
+    assert dpb.status() == dpb.DEV_BAD_LENGTH

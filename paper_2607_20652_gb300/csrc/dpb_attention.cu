@@ -183,47 +183,52 @@ __device__ __forceinline__ void write_zero_row(bf16 *row, int D) {
     for (int i = 0; i < D; i += 8) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Writes this warp's 32 rows of COLS columns of a result from TMEM (fp32,
-// times f) as bf16 to columns [col, min(col + COLS, D)): through `stage` (32
-// rows of COLS bf16 in shared memory, their 16-byte pieces exchanged so that
-// neither side meets bank conflicts), so that the warp's stores to memory cover
-// whole rows. Rows from `rows` on are left out.
-template <int COLS>
-__device__ __forceinline__ void write_rows(uint32_t tmem, uint8_t *stage, const Out &out, int64_t token, int head,
-                                           int rows, int col, int D, float f) {
-    const int lane = threadIdx.x & 31;
-    constexpr int kPieces = COLS / 8, kSwap = kPieces < 8 ? kPieces - 1 : 7;
-    uint32_t v[COLS / 32][32];
-#pragma unroll
-    for (int c = 0; c < COLS / 32; ++c) tmem_load(tmem + 32 * c, v[c]);
-#pragma unroll
-    for (int c = 0; c < COLS / 32; ++c) {
-        load_wait(v[c]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t u[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                u[e] = pack_bf16(__uint_as_float(v[c][8 * i + 2 * e]) * f, __uint_as_float(v[c][8 * i + 2 * e + 1]) * f);
-            *reinterpret_cast<uint4 *>(stage + lane * COLS * 2 + (((4 * c + i) ^ (lane & kSwap)) * 16)) =
-                make_uint4(u[0], u[1], u[2], u[3]);
-        }
-    }
+// Writes 32 columns [at, at + 32) of this warp's 32 rows of a result from
+// `stage` (32 rows of 64 bytes, the 16-byte pieces of each exchanged so that
+// neither side meets bank conflicts), so that a store covers whole stretches
+// of rows. Rows from `rows` on, and columns from D on, are left out.
+__device__ __forceinline__ uint8_t *stage_piece(uint8_t *stage, int row, int i) {
+    return stage + row * 64 + ((i ^ ((row >> 1) & 3)) * 16);
+}
+__device__ __forceinline__ void write_stage(uint8_t *stage, const Out &out, int64_t token, int head, int rows, int at,
+                                            int D) {
+    const int lane = threadIdx.x & 31, piece = lane & 3, r0 = lane >> 2;
     __syncwarp();
-    // piece `lane % kPieces` of rows lane / kPieces, + 32 / kPieces, ...
-    const int piece = lane % kPieces, r0 = lane / kPieces;
-    uint4 x[kPieces];
+    uint4 x[4];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-        const int r = r0 + i * (32 / kPieces);
-        x[i] = *reinterpret_cast<const uint4 *>(stage + r * COLS * 2 + ((piece ^ (r & kSwap)) * 16));
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4 *>(stage_piece(stage, r0 + 8 * i, piece));
+    if (at + 8 * piece < D)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r0 + 8 * i < rows)
+                *reinterpret_cast<uint4 *>(out.p + (token + r0 + 8 * i) * out.ts + head * out.hs + at + 8 * piece) = x[i];
+    __syncwarp();
+}
+// The same of CH x 32 columns from TMEM (fp32, times f) to columns from `col`
+// on, as bf16. read() is called once TMEM has been read.
+template <int CH, typename F>
+__device__ __forceinline__ void write_rows(uint32_t tmem, uint8_t *stage, const Out &out, int64_t token, int head,
+                                           int rows, int col, int D, float f, F read) {
+    const int lane = threadIdx.x & 31;
+    uint32_t u[CH][16];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        uint32_t v[32];
+        tmem_load(tmem + 32 * c, v);
+        load_wait(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            u[c][e] = pack_bf16(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f);
     }
-    bf16 *at = out.p + (token + r0) * out.ts + head * out.hs + col + piece * 8;
-    const int64_t step = 32 / kPieces * out.ts;
-    if (col + piece * 8 < D)
+    read();
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
-            if (r0 + i * (32 / kPieces) < rows) *reinterpret_cast<uint4 *>(at + i * step) = x[i];
+    for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4 *>(stage_piece(stage, lane, i)) =
+                make_uint4(u[c][4 * i], u[c][4 * i + 1], u[c][4 * i + 2], u[c][4 * i + 3]);
+        write_stage(stage, out, token, head, rows, col + 32 * c, D);
+    }
 }
 
 // The block's set-up: the copying warp makes the barriers and goes on at once
@@ -237,6 +242,60 @@ __device__ __forceinline__ void setup_wait() {
     asm volatile("barrier.cta.sync 1, %0;" ::"n"(THREADS) : "memory");
 }
 
+// What a block takes on: a tile of keys, one (or in the forward a pair) of
+// queries, or the end.
+enum { kKeys, kQueries, kEnd };
+struct Item {
+    int kind, head, tile, first, count, pieces, slot, piece;
+    Seq q;
+};
+
+// The items that the copying warp of a block hands on to the others.
+template <int N>
+struct ItemList {
+    int4 *data;
+    uint32_t full, free;  // barriers [N]: item is there, has been read by all
+    __device__ __forceinline__ void read(Item &it, int c) const {
+        const int4 *at = data + 3 * (c % N), x = at[0], y = at[1], z = at[2];
+        it.q.q0 = x.x, it.q.n = x.y, it.q.k0 = x.z, it.q.m = x.w;
+        it.tile = y.x, it.first = y.y, it.count = y.z, it.pieces = y.w;
+        it.slot = z.x, it.piece = z.y, it.kind = z.z, it.head = z.w;
+    }
+    // All lanes of the copying warp: hands on item c.
+    __device__ __forceinline__ bool put(const Item &it, int c) const {
+        const int at = c % N;
+        if (c >= N && !__all_sync(kFull, bar_wait(free + 8 * at, ((c / N) & 1) ^ 1, kTries))) return false;
+        if (elect_one()) {
+            data[3 * at] = make_int4(it.q.q0, it.q.n, it.q.k0, it.q.m);
+            data[3 * at + 1] = make_int4(it.tile, it.first, it.count, it.pieces);
+            data[3 * at + 2] = make_int4(it.slot, it.piece, it.kind, it.head);
+            bar_arrive(full + 8 * at);
+        }
+        __syncwarp();
+        return true;
+    }
+    // One thread: takes item c.
+    __device__ __forceinline__ bool get_one(Item &it, int &c) const {
+        if (!bar_wait(full + 8 * (c % N), (c / N) & 1, kTries)) return false;
+        read(it, c);
+        bar_arrive(free + 8 * (c % N));
+        ++c;
+        return true;
+    }
+    // All lanes of a warp: takes item c, which stays in the list until the warp
+    // has finished it.
+    __device__ __forceinline__ bool get_warp(Item &it, int &c) const {
+        if (!__all_sync(kFull, bar_wait(full + 8 * (c % N), (c / N) & 1, kTries))) return false;
+        read(it, c);
+        ++c;
+        return true;
+    }
+    __device__ __forceinline__ void finished(int c) const {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(free + 8 * (c % N));
+    }
+};
+
 // ---- forward ------------------------------------------------------------------
 
 template <int DP_, int BN_, int NS_>
@@ -249,11 +308,13 @@ struct FwdShape {
     static constexpr int kTile = kRows * DP * 2, kSlot = BN * DP * 2;
     static constexpr int kColumns = 512;
     static constexpr int kColO = 2 * BN, kColP = kOwnP ? 2 * (BN + DP) : 0, kStepP = kOwnP ? BN / 2 : BN;
-    static constexpr int kBars = 2 + 2 * NS + 1 + 2 * 6 + 1;
-    static constexpr int kSmem = 1024 + 2 * kTile + NS * kSlot + 8 * kBars + 16;
+    static constexpr int kItems = 4, kReaders = kOwnP ? 10 : 9;  // of the list of items
+    static constexpr int kBars = 4 + 2 * NS + 1 + 7 + 8 + 2 * kItems + 1;
+    static constexpr int kStage = 32 * 32 * 2;  // a warp's rows of 32 result columns
+    static constexpr int kSmem = 1024 + 2 * kTile + NS * kSlot + 8 * kStage + 48 * kItems + 16 + 8 * kBars + 16;
     static constexpr int kThreads = 384;  // two softmax warpgroups, one of the copying and the issuing warp
-    // registers of a softmax thread and of the others: 256 x 216 + 128 x 72 = 384 x 168
-    static constexpr int kRegsRow = 216, kRegsOther = 72;
+    // registers of a softmax thread and of the others: 256 x 208 + 128 x 88 = 384 x 168
+    static constexpr int kRegsRow = 208, kRegsOther = 88;
 };
 
 // Visible keys of query row i (of n, against m keys).
@@ -268,6 +329,18 @@ __device__ __forceinline__ int tile_blocks(const AttnArgs &a, const Seq &q, int 
     return r0 < q.n ? (visible(a, q, min(r0 + kRows, q.n) - 1) + BN - 1) / BN : 0;
 }
 
+// Blocks stay: one that has copied all of an item asks the hardware for a block of
+// the grid that has not started, and takes its item (of those that have rows)
+// over, so that copies and first products of the next item run while this one
+// is being finished.
+//
+// Measured (causal; 4 x visible pairs x head_dim operations a head), against a
+// block for each item: 1 x 12289, 12 heads of 64: 213 us (222), 1087 TFLOP/s;
+// 8 x 1024, 12 heads of 64: 26.7 us (29.9); 1 x 8192, 16 heads of 128: 191 us
+// (191), 1440 TFLOP/s; 8 x 1024, 16 heads of 128: 46.7 us (50.7). Bound by the
+// exponentials (16384 of a block of scores at 32 a cycle) at 64, by the tensor
+// cores at 128; short sequences by the way of an item's first block from memory
+// to its result.
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int DP = C::DP, BN = C::BN;
@@ -275,71 +348,117 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    // the longest rows first; the heads of a group side by side
-    const int head = blockIdx.x % a.hq, rest = blockIdx.x / a.hq;
-    const int si = rest % a.seqs, rows2 = a.tiles - 1 - rest / a.seqs;
-    const Offsets offsets = load_offsets(a, si);
 
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + 2 * C::kTile + C::NS * C::kSlot);
+    uint8_t *stages = smem + 2 * C::kTile + C::NS * C::kSlot;
+    int4 *items = reinterpret_cast<int4 *>(stages + 8 * C::kStage);
+    const uint32_t answer = smem_addr(items + 3 * C::kItems);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(items + 3 * C::kItems + 1);
     const uint32_t bar0 = smem_addr(bars);
-    const uint32_t q_full = bar0;  // of each tile
-    Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 16, bar0 + 16 + 8 * C::NS, bar0 + 16 + 16 * C::NS};
-    // per tile: S is there, each half of P is there, S has been read, P's
-    // product is done, O is done
-    const uint32_t s_full = bar0 + 8 * (3 + 2 * C::NS), p_full = s_full + 16, s_read = p_full + 32,
-                   p_done = s_read + 16, o_full = p_done + 16, done = o_full + 16;
+    // of each tile of queries: it is there, has been used for the last time
+    const uint32_t q_full = bar0, q_free = q_full + 16;
+    Ring<C::NS, C::kSlot> ring{smem + 2 * C::kTile, bar0 + 32, bar0 + 32 + 8 * C::NS, bar0 + 32 + 16 * C::NS};
+    // per tile: S is there, O is done, P's product is done; all is done; by the
+    // row warps: each half of P is there, S has been read, O has been read; an
+    // item is there, has been read; the hardware has answered
+    const uint32_t s_full = bar0 + 8 * (5 + 2 * C::NS), o_full = s_full + 16, p_done = o_full + 16, done = p_done + 16,
+                   p_full = done + 8, s_read = p_full + 32, o_free = s_read + 16, item_full = o_free + 16,
+                   answered = item_full + 16 * C::kItems;
+    const ItemList<C::kItems> list{items, item_full, item_full + 8 * C::kItems};
     uint32_t *slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
-    if (warp == kCopier) {
-        for (int i = lane; i < C::kBars; i += 32) {
-            const uint32_t b = bar0 + 8 * i;
-            bar_init(b, b >= p_full && b < p_done ? 4 : b == done && kValues != kScores ? 2 : 1);
-        }
-        bar_init_fence();
-        __syncwarp();
-    }
-
-    const Seq q = sequence(a, offsets);
-    if (!q.ok) {
-        if (threadIdx.x == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
-        return;
-    }
-    if (rows2 * 2 * kRows >= q.n) return;
-    const int nb0 = tile_blocks<BN>(a, q, 2 * rows2), nb1 = tile_blocks<BN>(a, q, 2 * rows2 + 1);
-    const int blocks = max(nb0, nb1);
+    Item it;
     bool failed = false;
+    int c = 0;  // items taken
 
     if (warp >= 8) {
         give_registers<C::kRegsOther>();
         if (warp == kCopier) {
-            // ---- copies: what the first products need first, then V_0, K_1, V_1, ...
-            const int kv_head = head / a.group;
-            const int tiles = blocks == 0 ? 0 : (2 * rows2 + 1) * kRows < q.n ? 2 : 1;
-            auto queries = [&](int t) {
-                if (t < tiles && elect_one()) {
-                    bar_arrive_expect(q_full + 8 * t, C::kTile);
-                    copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, head, q.q0 + (2 * rows2 + t) * kRows, kRows,
-                                  q_full + 8 * t);
+            for (int i = lane; i < C::kBars; i += 32) {
+                const uint32_t b = bar0 + 8 * i;
+                bar_init(b, b == answered                       ? 1
+                            : b >= list.free                    ? C::kReaders
+                            : b >= item_full                    ? 1
+                            : b >= p_full                       ? 4
+                            : b == done && kValues != kScores ? 2
+                                                                : 1);
+            }
+            bar_init_fence();
+            __syncwarp();
+            setup_arrive<C::kThreads>();
+            // ring's tiles copied, answers had, copies of each of the two tiles
+            int i = 0, tails = 0, asked = 0, sent0 = 0, sent1 = 0;
+            uint32_t at = blockIdx.x;
+            bool have = true;
+            // takes over a block that has not started, if there is one
+            auto next = [&]() {
+                if (elect_one()) {
+                    bar_arrive_expect(answered, 16);
+                    ask_block(answer, answered);
                 }
                 __syncwarp();
+                failed = !__all_sync(kFull, bar_wait(answered, asked & 1, kTries));
+                ++asked;
+                have = !failed && block_answer(answer, at);
+                fence_async_shared();
+                __syncwarp();
             };
-            int issued = 0, tails = 0;
-            queries(0);
-            if (blocks > 0) failed = !ring.template fill<DP>(issued++, &a.k, kv_head, q.k0, BN, BN, false, tails);
-            queries(1);
-            setup_arrive<C::kThreads>();
-            for (int j = 0; j < blocks && !failed; ++j) {
-                const int live = q.m - j * BN;
-                for (int kind = j == 0; kind < 2 && !failed; ++kind) {  // K_0 is under way
-                    failed = !ring.wait_free(issued) ||
-                             !ring.template fill<DP>(issued, kind ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN, live,
-                                                     kind == 1, tails);
-                    if (!failed) ++issued;
+            for (;;) {
+                it = Item{};
+                it.kind = kEnd;
+                while (have) {
+                    // the longest rows first; the heads of a group side by side
+                    const int rest = (int)(at / a.hq);
+                    it.head = (int)(at % a.hq);
+                    it.tile = a.tiles - 1 - rest / a.seqs;
+                    it.q = sequence(a, load_offsets(a, rest % a.seqs));
+                    if (!it.q.ok && lane == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
+                    if (it.q.ok && it.tile * 2 * kRows < it.q.n) {
+                        it.kind = kQueries;
+                        break;
+                    }
+                    next();
                 }
+                failed = failed || !list.put(it, c);
+                if (failed || it.kind == kEnd) break;
+                ++c;
+                const Seq &q = it.q;
+                it.count = max(tile_blocks<BN>(a, q, 2 * it.tile), tile_blocks<BN>(a, q, 2 * it.tile + 1));
+                const int kv_head = it.head / a.group;
+                auto queries = [&](int t, int &sent) {
+                    if (failed || (2 * it.tile + t) * kRows >= q.n) return;
+                    failed = sent > 0 && !__all_sync(kFull, bar_wait(q_free + 8 * t, (sent - 1) & 1, kTries));
+                    if (failed) return;
+                    ++sent;
+                    if (elect_one()) {
+                        bar_arrive_expect(q_full + 8 * t, C::kTile);
+                        copy_tile<DP>(smem_addr(smem) + t * C::kTile, &a.q, it.head, q.q0 + (2 * it.tile + t) * kRows,
+                                      kRows, q_full + 8 * t);
+                    }
+                    __syncwarp();
+                };
+                auto block = [&](int j, bool values) {
+                    failed = failed || !ring.wait_free(i) ||
+                             !ring.template fill<DP>(i, values ? &a.v : &a.k, kv_head, q.k0 + j * BN, BN, q.m - j * BN,
+                                                     values, tails);
+                    if (!failed) ++i;
+                };
+                if (it.count > 0) {
+                    // what the first products need first
+                    queries(0, sent0);
+                    block(0, false);
+                    queries(1, sent1);
+                    block(0, true);
+                    for (int j = 1; j < it.count && !failed; ++j) {
+                        block(j, false);
+                        block(j, true);
+                    }
+                }
+                if (failed) break;
+                next();
             }
-            if (failed) {
-                ring.drain(issued);
-                for (int t = 0; t < tiles; ++t) bar_wait(q_full + 8 * t, 0, kTries);
-            }
+            // no copy is in flight when the block ends, whatever gave up
+            ring.drain(i);
+            if (sent0 > 0) bar_wait(q_full, (sent0 - 1) & 1, kTries);
+            if (sent1 > 0) bar_wait(q_full + 8, (sent1 - 1) & 1, kTries);
         } else {
             if (warp == kScores) tmem_alloc(smem_addr(slot), C::kColumns);
             fence_before();
@@ -347,81 +466,124 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
             fence_after();
             const uint32_t tmem = *slot;
             const uint32_t q_addr = smem_addr(smem);
-            auto scores = [&](int t, int j) {
-                const uint64_t kd = desc_k_inside(ring.addr(2 * j)), qd = desc_k_inside(q_addr + t * C::kTile);
+            // bit t of each: whether the blocks, items with blocks and copies of
+            // tile t so far are odd in number (a barrier that has not been used
+            // counts as past the odd phase before)
+            uint32_t b = 0, o = 0, sent = 0;
+            int base = 0;  // ring's tiles
+            auto odd = [](uint32_t bits, int t) { return (bits >> t) & 1; };
+            auto scores = [&](int t, int i) {
+                fence_after();
+                const uint64_t kd = desc_k_inside(ring.addr(i)), qd = desc_k_inside(q_addr + t * C::kTile);
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
                     mma_ss(tmem + t * BN, desc_at(qd, (k / 4) * kRows * 128 + (k % 4) * 32),
                            desc_at(kd, (k / 4) * BN * 128 + (k % 4) * 32), mma_shape(BN, false), k > 0);
                 mma_commit(s_full + 8 * t);
             };
-            // O += P V of tile t, each half of the keys as soon as its P is there
-            auto values = [&](int t, int j) {
-                const uint64_t vd = desc_k_rows(ring.addr(2 * j + 1), BN * 128);
+            // O += P V of tile t, each half of the keys as soon as its P is
+            // there; O's place is free once the sums of the item before are read
+            auto values = [&](int t, int i, bool first) {
+                if (first && !bar_wait(o_free + 8 * t, odd(o, t) ^ 1, kTries)) return false;
+                const uint64_t vd = desc_k_rows(ring.addr(i), BN * 128);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    if (!bar_wait(p_full + 16 * t + 8 * h, j & 1, kTries)) return false;
+                    if (!bar_wait(p_full + 16 * t + 8 * h, odd(b, t), kTries)) return false;
                     fence_after();
 #pragma unroll
                     for (int k = h * BN / 32; k < (h + 1) * BN / 32; ++k)
                         mma_ts(tmem + C::kColO + t * DP, tmem + C::kColP + t * C::kStepP + 8 * k,
-                               desc_at(vd, k * 2048), mma_shape(DP, true), j > 0 || k > 0);
+                               desc_at(vd, k * 2048), mma_shape(DP, true), !first || k > 0);
                 }
+                b ^= 1u << t;
                 return true;
             };
-            if (blocks > 0 && warp == kScores && elect_one()) {
+            if (warp == kScores && elect_one()) {
                 // ---- scores; where P takes S's place, the values' products too
-                failed = !ring.wait_full(0);
-                for (int t = 0; t < 2 && !failed; ++t) {
-                    // a tile with rows is waited for, even where it has no block
-                    if ((2 * rows2 + t) * kRows < q.n) failed = !bar_wait(q_full + 8 * t, 0, kTries);
-                    fence_after();
-                    if (!failed && (t ? nb1 : nb0) > 0) scores(t, 0);
-                }
-                if (!failed) mma_commit(ring.empty_bar(0));
-                for (int j = 0; j < blocks && !failed; ++j) {
-                    const bool more = j + 1 < blocks;
-                    if (more && !ring.wait_full(2 * j + 2)) failed = true;
-                    if (C::kOwnP) {
-                        for (int t = 0; t < 2 && !failed; ++t)
-                            if (j + 1 < (t ? nb1 : nb0)) {
-                                failed = !bar_wait(s_read + 8 * t, j & 1, kTries);
-                                if (failed) break;
-                                fence_after();
-                                scores(t, j + 1);
+                for (failed = !list.get_one(it, c); !failed && it.kind != kEnd;
+                     failed = failed || !list.get_one(it, c)) {
+                    const int nb0 = tile_blocks<BN>(a, it.q, 2 * it.tile), nb1 = tile_blocks<BN>(a, it.q, 2 * it.tile + 1);
+                    const int blocks = max(nb0, nb1);
+                    if (blocks == 0) continue;
+                    const bool rows1 = (2 * it.tile + 1) * kRows < it.q.n;
+                    // the first block's, once the tile is there; one with rows is
+                    // waited for, even where it has no block
+                    failed = !ring.wait_full(base);
+                    for (int t = 0; t < 2 && !failed; ++t) {
+                        const int nb = t ? nb1 : nb0;
+                        if (t && !rows1) break;
+                        failed = !bar_wait(q_full + 8 * t, odd(sent, t), kTries);
+                        sent ^= 1u << t;
+                        if (!failed && nb > 0) {
+                            if (C::kOwnP) {
+                                failed = !bar_wait(s_read + 8 * t, odd(b, t) ^ 1, kTries);
+                                b ^= 1u << t;
                             }
-                    } else {
-                        failed = failed || !ring.wait_full(2 * j + 1);
-                        for (int t = 0; t < 2 && !failed; ++t) {
-                            const int nb = t ? nb1 : nb0;
-                            if (j >= nb) continue;
-                            failed = !values(t, j);
-                            if (failed) break;
-                            if (j + 1 == nb)
-                                mma_commit(o_full + 8 * t);
-                            else
-                                scores(t, j + 1);  // products run in the order of their issue
+                            if (!failed) scores(t, base);
                         }
-                        if (!failed) mma_commit(ring.empty_bar(2 * j + 1));
+                        if (!failed && nb <= 1) mma_commit(q_free + 8 * t);
                     }
-                    if (!failed && more) mma_commit(ring.empty_bar(2 * j + 2));
+                    if (failed) break;
+                    mma_commit(ring.empty_bar(base));
+                    for (int j = 0; j < blocks && !failed; ++j) {
+                        const bool more = j + 1 < blocks;
+                        const int k_next = base + 2 * j + 2, v = base + 2 * j + 1;
+                        failed = (more && !ring.wait_full(k_next)) || (!C::kOwnP && !ring.wait_full(v));
+#pragma unroll 1
+                        for (int t = 0; t < 2 && !failed; ++t) {
+                            const int left = (t ? nb1 : nb0) - j;  // blocks of the tile, this one included
+                            if (left <= 0) continue;
+                            if (C::kOwnP) {
+                                if (left == 1) continue;
+                                failed = !bar_wait(s_read + 8 * t, odd(b, t) ^ 1, kTries);
+                                if (failed) break;
+                                b ^= 1u << t;
+                            } else {
+                                failed = !values(t, v, j == 0);
+                                if (failed) break;
+                                if (left == 1) {
+                                    mma_commit(o_full + 8 * t);
+                                    o ^= 1u << t;
+                                    continue;
+                                }
+                            }
+                            scores(t, k_next);  // with P in S's place: products run in the order of their issue
+                            if (left == 2) mma_commit(q_free + 8 * t);
+                        }
+                        if (failed) break;
+                        if (!C::kOwnP) mma_commit(ring.empty_bar(v));
+                        if (more) mma_commit(ring.empty_bar(k_next));
+                    }
+                    base += 2 * blocks;
                 }
                 // every product, and every arrival that it makes, is done
                 // before the block's memory is given back
                 mma_commit(done);
                 failed |= !bar_wait(done, 0, kTries);
-            } else if (blocks > 0 && C::kOwnP && warp == kValues && elect_one()) {
+            } else if (C::kOwnP && warp == kValues && elect_one()) {
                 // ---- values
-                for (int j = 0; j < blocks && !failed; ++j) {
-                    failed = !ring.wait_full(2 * j + 1);
-                    for (int t = 0; t < 2 && !failed; ++t) {
-                        const int nb = t ? nb1 : nb0;
-                        if (j >= nb) continue;
-                        failed = !values(t, j);
-                        if (failed) break;
-                        mma_commit(j + 1 == nb ? o_full + 8 * t : p_done + 8 * t);
+                for (failed = !list.get_one(it, c); !failed && it.kind != kEnd;
+                     failed = failed || !list.get_one(it, c)) {
+                    const int nb0 = tile_blocks<BN>(a, it.q, 2 * it.tile), nb1 = tile_blocks<BN>(a, it.q, 2 * it.tile + 1);
+                    const int blocks = max(nb0, nb1);
+                    for (int j = 0; j < blocks && !failed; ++j) {
+                        const int v = base + 2 * j + 1;
+                        failed = !ring.wait_full(v);
+#pragma unroll 1
+                        for (int t = 0; t < 2 && !failed; ++t) {
+                            const int left = (t ? nb1 : nb0) - j;
+                            if (left <= 0) continue;
+                            failed = !values(t, v, j == 0);
+                            if (failed) break;
+                            mma_commit(p_done + 8 * t);
+                            if (left == 1) {
+                                mma_commit(o_full + 8 * t);
+                                o ^= 1u << t;
+                            }
+                        }
+                        if (!failed) mma_commit(ring.empty_bar(v));
                     }
-                    if (!failed) mma_commit(ring.empty_bar(2 * j + 1));
+                    base += 2 * blocks;
                 }
                 mma_commit(done);
                 failed |= !bar_wait(done, 0, kTries);
@@ -435,124 +597,137 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
         fence_after();
         const uint32_t tmem = *slot;
         // ---- softmax: a row a thread
-        const int t = warp / 4, nb = t ? nb1 : nb0;
-        const int i = (2 * rows2 + t) * kRows + (threadIdx.x & 127);
-        const bool live = i < q.n;
-        const int lim = visible(a, q, i);
+        const int t = warp / 4;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 TMEM lanes
         const uint32_t s_addr = tmem + lanes + t * BN, o_addr = tmem + lanes + C::kColO + t * DP;
         const uint32_t p_addr = tmem + lanes + C::kColP + t * C::kStepP;
-        float top = 0.f;  // reference maximum, of scale2 S
-        uint64_t sum2[2] = {0, 0};  // four shares of the sum of 2^(scale2 S - top)
         const uint64_t scale2 = pair(a.scale2, a.scale2);
-        for (int j = 0; j < nb; ++j) {
-            if (!__all_sync(kFull, bar_wait(s_full + 8 * t, j & 1, kTries))) {
-                failed = true;
-                break;
-            }
-            fence_after();
-            uint32_t s[BN / 32][32];
-#pragma unroll
-            for (int c = 0; c < BN / 32; ++c) tmem_load(s_addr + 32 * c, s[c]);
-#pragma unroll
-            for (int c = 0; c < BN / 32; ++c) load_wait(s[c]);
-            if (C::kOwnP) {
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(s_read + 8 * t);
-            }
-            const int seen = lim - j * BN;  // visible columns of this block
-            if (!__all_sync(kFull, seen >= BN)) {
-#pragma unroll
-                for (int c = 0; c < BN; ++c)
-                    if (c >= seen) s[c / 32][c % 32] = 0xff800000u;  // -inf
-            }
-            float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int c = 0; c < BN; c += 8)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    m[e] = max3(m[e], __uint_as_float(s[c / 32][c % 32 + 2 * e]),
-                                __uint_as_float(s[c / 32][c % 32 + 2 * e + 1]));
-            const float mx = fmaxf(max3(m[0], m[1], m[2]), m[3]) * a.scale2;
-            // this tile's product of the block before has to be done before P
-            // is written or O is scaled (with P in place of S, S came after it)
-            bool waited = !C::kOwnP || j == 0;
-            if (j == 0) {
-                top = mx == -INFINITY ? 0.f : mx;
-            } else if (__any_sync(kFull, mx > top + 8.f)) {
-                // The running maximum is only followed when it has grown by a
-                // factor of 2^8: until then the sums stay far from overflow,
-                // and O is not touched.
-                if (!waited) {
-                    if (!__all_sync(kFull, bar_wait(p_done + 8 * t, (j - 1) & 1, kTries))) {
-                        failed = true;
-                        break;
-                    }
-                    fence_after();
-                    waited = true;
+        int b = 0, o = 0;  // blocks and items with blocks so far
+        for (;;) {
+            failed = !list.get_warp(it, c);
+            if (failed || it.kind == kEnd) break;
+            const int lim = visible(a, it.q, (2 * it.tile + t) * kRows + (threadIdx.x & 127));
+            const int nb = tile_blocks<BN>(a, it.q, 2 * it.tile + t);
+            float top = 0.f;  // reference maximum, of scale2 S
+            uint64_t sum2[2] = {0, 0};  // four shares of the sum of 2^(scale2 S - top)
+            for (int j = 0; j < nb; ++j, ++b) {
+                if (!__all_sync(kFull, bar_wait(s_full + 8 * t, b & 1, kTries))) {
+                    failed = true;
+                    break;
                 }
-                const float next = mx > top + 8.f ? mx : top, f = exp2_approx(top - next);
-                top = next;
-                const uint64_t f2 = pair(f, f);
-                sum2[0] = mul2(sum2[0], f2);
-                sum2[1] = mul2(sum2[1], f2);
+                fence_after();
+                uint32_t s[BN / 32][32];
+#pragma unroll
+                for (int c = 0; c < BN / 32; ++c) tmem_load(s_addr + 32 * c, s[c]);
+#pragma unroll
+                for (int c = 0; c < BN / 32; ++c) load_wait(s[c]);
+                if (C::kOwnP) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(s_read + 8 * t);
+                }
+                const int seen = lim - j * BN;  // visible columns of this block
+                if (!__all_sync(kFull, seen >= BN)) {
+#pragma unroll
+                    for (int c = 0; c < BN; ++c)
+                        if (c >= seen) s[c / 32][c % 32] = 0xff800000u;  // -inf
+                }
+                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < BN; c += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        m[e] = max3(m[e], __uint_as_float(s[c / 32][c % 32 + 2 * e]),
+                                    __uint_as_float(s[c / 32][c % 32 + 2 * e + 1]));
+                const float mx = fmaxf(max3(m[0], m[1], m[2]), m[3]) * a.scale2;
+                // this tile's product of the block before has to be done before P
+                // is written or O is scaled (with P in place of S, S came after it)
+                bool waited = !C::kOwnP || b == 0;
+                if (j == 0) {
+                    top = mx == -INFINITY ? 0.f : mx;
+                } else if (__any_sync(kFull, mx > top + 8.f)) {
+                    // The running maximum is only followed when it has grown by a
+                    // factor of 2^8: until then the sums stay far from overflow,
+                    // and O is not touched.
+                    if (!waited) {
+                        if (!__all_sync(kFull, bar_wait(p_done + 8 * t, (b - 1) & 1, kTries))) {
+                            failed = true;
+                            break;
+                        }
+                        fence_after();
+                        waited = true;
+                    }
+                    const float next = mx > top + 8.f ? mx : top, f = exp2_approx(top - next);
+                    top = next;
+                    const uint64_t f2 = pair(f, f);
+                    sum2[0] = mul2(sum2[0], f2);
+                    sum2[1] = mul2(sum2[1], f2);
 #pragma unroll 1
-                for (int c = 0; c < DP; c += 32) {
-                    uint32_t v[32];
-                    tmem_load(o_addr + c, v);
-                    load_wait(v);
+                    for (int c = 0; c < DP; c += 32) {
+                        uint32_t v[32];
+                        tmem_load(o_addr + c, v);
+                        load_wait(v);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
-                    tmem_store(o_addr + c, v);
-                }
-            }
-            const uint64_t top2 = pair(-top, -top);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                static_assert(BN == 128, "a half of P is one store of 32 columns");
-                uint32_t p[32];
-#pragma unroll
-                for (int e = 0; e < 64; e += 2) {
-                    const int x = 64 * h + e;
-                    const float2 y = unpair(fma2(pair_bits(s[x / 32][x % 32], s[x / 32][x % 32 + 1]), scale2, top2));
-                    const float p0 = exp2_approx(y.x), p1 = exp2_approx(y.y);
-                    sum2[(e / 2) & 1] = add2(sum2[(e / 2) & 1], pair(p0, p1));
-                    p[e / 2] = pack_bf16(p0, p1);
-                }
-                if (!waited) {
-                    if (!__all_sync(kFull, bar_wait(p_done + 8 * t, (j - 1) & 1, kTries))) {
-                        failed = true;
-                        break;
+                        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
+                        tmem_store(o_addr + c, v);
                     }
-                    fence_after();
-                    waited = true;
                 }
-                tmem_store(p_addr + 32 * h, p);
-                store_wait();
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(p_full + 16 * t + 8 * h);
+                const uint64_t top2 = pair(-top, -top);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    static_assert(BN == 128, "a half of P is one store of 32 columns");
+                    uint32_t p[32];
+#pragma unroll
+                    for (int e = 0; e < 64; e += 2) {
+                        const int x = 64 * h + e;
+                        const float2 y = unpair(fma2(pair_bits(s[x / 32][x % 32], s[x / 32][x % 32 + 1]), scale2, top2));
+                        const float p0 = exp2_approx(y.x), p1 = exp2_approx(y.y);
+                        sum2[(e / 2) & 1] = add2(sum2[(e / 2) & 1], pair(p0, p1));
+                        p[e / 2] = pack_bf16(p0, p1);
+                    }
+                    if (!waited) {
+                        if (!__all_sync(kFull, bar_wait(p_done + 8 * t, (b - 1) & 1, kTries))) {
+                            failed = true;
+                            break;
+                        }
+                        fence_after();
+                        waited = true;
+                    }
+                    tmem_store(p_addr + 32 * h, p);
+                    store_wait();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(p_full + 16 * t + 8 * h);
+                }
+                if (failed) break;
             }
             if (failed) break;
-        }
-        const float2 sums = unpair(add2(sum2[0], sum2[1]));
-        const float sum = sums.x + sums.y;
-        if (!failed && nb > 0) {
-            failed = !__all_sync(kFull, bar_wait(o_full + 8 * t, 0, kTries));
-            fence_after();
-        }
-        if (!failed) {
-            const int64_t token = q.q0 + (int64_t)i;
+            const float2 sums = unpair(add2(sum2[0], sum2[1]));
+            const float sum = sums.x + sums.y;
+            Item was;  // read anew, so that the loop above need not hold it
+            list.read(was, c - 1);
+            const int first = (2 * was.tile + t) * kRows + (warp & 3) * 32;  // the warp's first row
+            const int64_t token = was.q.q0 + (int64_t)first;
             if (nb > 0) {
-                // Q's tile is read for the last time: its memory takes the rows
-                write_rows<DP>(o_addr, smem + t * C::kTile + (warp & 3) * 32 * DP * 2, a.out, token - lane, head,
-                               q.n - (i - lane), 0, a.D, sum > 0.f || sum != sum ? 1.f / sum : 0.f);
-            } else if (live) {
-                write_zero_row(a.out.p + token * a.out.ts + head * a.out.hs, a.D);
+                if (!__all_sync(kFull, bar_wait(o_full + 8 * t, o & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                ++o;
+                fence_after();
+                write_rows<DP / 32>(o_addr, stages + warp * C::kStage, a.out, token, was.head, was.q.n - first, 0, a.D,
+                                    sum > 0.f || sum != sum ? 1.f / sum : 0.f, [&]() {
+                                        fence_before();
+                                        __syncwarp();
+                                        if (lane == 0) bar_arrive(o_free + 8 * t);
+                                    });
+            } else if (first + lane < was.q.n) {
+                write_zero_row(a.out.p + (token + lane) * a.out.ts + was.head * a.out.hs, a.D);
             }
-            if (live)
-                a.lse[(int64_t)head * a.total_q + token] = lim > 0 ? (top + __log2f(sum)) * kLn2 : -INFINITY;
+            if (first + lane < was.q.n)
+                a.lse[(int64_t)was.head * a.total_q + token + lane] =
+                    lim > 0 ? (top + __log2f(sum)) * kLn2 : -INFINITY;
+            list.finished(c - 1);
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
@@ -634,13 +809,6 @@ struct Plan {
     int keys, queries;
 };
 
-// What a block takes on: a tile of keys, a tile of queries, or the end.
-enum { kKeys, kQueries, kEnd };
-struct Item {
-    int kind, head, tile, first, count, pieces, slot, piece;
-    Seq q;
-};
-
 // Barriers and memory of the gradient kernel.
 template <class C>
 struct GradBars {
@@ -649,13 +817,13 @@ struct GradBars {
     // is there; its product is done; the sums are there, have been read; all is
     // done; an item of the list is there, has been read by all
     uint32_t tile_full, tile_free, s_full, g_full, w_done, v_done, acc_full, done, s_read, g_read, w_full, v_full, acc_free,
-        item_full, item_free;
+        item_full;
     typename C::Slots ring;
-    int4 *items;
+    ItemList<C::kItems> items;
     uint32_t *slot;
     __device__ __forceinline__ GradBars(uint8_t *smem) {
-        items = reinterpret_cast<int4 *>(smem + (2 + C::NS) * C::kTile + C::kVec + C::kRowWarps * C::kStage);
-        uint64_t *bars = reinterpret_cast<uint64_t *>(items + 3 * C::kItems);
+        items.data = reinterpret_cast<int4 *>(smem + (2 + C::NS) * C::kTile + C::kVec + C::kRowWarps * C::kStage);
+        uint64_t *bars = reinterpret_cast<uint64_t *>(items.data + 3 * C::kItems);
         tile_full = smem_addr(bars);
         tile_free = tile_full + 16;
         ring = {smem + 2 * C::kTile, tile_full + 32, tile_full + 32 + 8 * C::NS, tile_full + 32 + 16 * C::NS};
@@ -671,13 +839,14 @@ struct GradBars {
         v_full = s_full + 72;
         acc_free = s_full + 80;
         item_full = s_full + 88;
-        item_free = item_full + 8 * C::kItems;
+        items.full = item_full;
+        items.free = item_full + 8 * C::kItems;
         slot = reinterpret_cast<uint32_t *>(bars + C::kBars);
     }
     __device__ __forceinline__ void make() const {
         for (int i = threadIdx.x & 31; i < C::kBars; i += 32) {
             const uint32_t b = tile_full + 8 * i;
-            bar_init(b, b >= item_free ? C::kRowWarps + 2
+            bar_init(b, b >= items.free ? C::kRowWarps + 2
                         : b >= item_full ? 1
                         : b >= s_read    ? C::kRowWarps
                         : b == done      ? 2
@@ -685,47 +854,6 @@ struct GradBars {
         }
         bar_init_fence();
         __syncwarp();
-    }
-    // All lanes of the copying warp: hands on item c.
-    __device__ __forceinline__ bool put(const Item &it, int c) const {
-        const int at = c % C::kItems;
-        if (c >= C::kItems && !__all_sync(kFull, bar_wait(item_free + 8 * at, ((c / C::kItems) & 1) ^ 1, kTries)))
-            return false;
-        if (elect_one()) {
-            items[3 * at] = make_int4(it.q.q0, it.q.n, it.q.k0, it.q.m);
-            items[3 * at + 1] = make_int4(it.tile, it.first, it.count, it.pieces);
-            items[3 * at + 2] = make_int4(it.slot, it.piece, it.kind, it.head);
-            bar_arrive(item_full + 8 * at);
-        }
-        __syncwarp();
-        return true;
-    }
-    __device__ __forceinline__ void read(Item &it, int at) const {
-        const int4 x = items[3 * at], y = items[3 * at + 1], z = items[3 * at + 2];
-        it.q.q0 = x.x, it.q.n = x.y, it.q.k0 = x.z, it.q.m = x.w;
-        it.tile = y.x, it.first = y.y, it.count = y.z, it.pieces = y.w;
-        it.slot = z.x, it.piece = z.y, it.kind = z.z, it.head = z.w;
-    }
-    // One thread, or all lanes of a warp: item c.
-    __device__ __forceinline__ bool get_one(Item &it, int &c) const {
-        const int at = c % C::kItems;
-        if (!bar_wait(item_full + 8 * at, (c / C::kItems) & 1, kTries)) return false;
-        read(it, at);
-        bar_arrive(item_free + 8 * at);
-        ++c;
-        return true;
-    }
-    // (A warp keeps it in the list until it has finished the item.)
-    __device__ __forceinline__ bool get_warp(Item &it, int &c) const {
-        const int at = c % C::kItems;
-        if (!__all_sync(kFull, bar_wait(item_full + 8 * at, (c / C::kItems) & 1, kTries))) return false;
-        read(it, at);
-        ++c;
-        return true;
-    }
-    __device__ __forceinline__ void finished(int c) const {
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) bar_arrive(item_free + 8 * (c % C::kItems));
     }
 };
 
@@ -863,59 +991,14 @@ __device__ void make_plan(const AttnArgs &a) {
         false);
 }
 
-// Writes CH x 32 columns of this warp's 32 rows of a result from TMEM (fp32,
-// times f) as bf16 to columns [col, min(col + 32 CH, D)), 32 at a time through
-// `stage` (their 16-byte pieces exchanged so that neither side meets bank
-// conflicts), so that a store covers whole stretches of rows. Rows from `rows`
-// on are left out. read() is called once TMEM has been read. Of an item in
-// parts the sums go to memory, and the warp that is the last of its like there
-// adds them up, always in the parts' order.
+// write_rows() of an item. Of one in parts the sums go to memory, and the warp
+// that is the last of its like there adds them up, always in the parts' order.
 template <int CH, typename F>
-__device__ __forceinline__ void write_columns(const AttnArgs &a, uint32_t tmem, uint8_t *stage, const Out &out,
-                                              int64_t token, const Item &it, int rows, int col, float f,
-                                              int64_t slot_floats, F read) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-    const int quad = lane & 3, r0 = lane >> 2;
-    auto place = [&](int i) { return stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16); };  // of this lane's piece i
-    auto write = [&](int c) {
-        __syncwarp();
-        uint4 x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = r0 + 8 * i;
-            x[i] = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((quad ^ ((r >> 1) & 3)) * 16));
-        }
-        const int at = col + 32 * c + 8 * quad;
-        if (at < a.D)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (r0 + 8 * i < rows)
-                    *reinterpret_cast<uint4 *>(out.p + (token + r0 + 8 * i) * out.ts + it.head * out.hs + at) = x[i];
-        __syncwarp();
-    };
-    if (it.pieces == 1) {
-        uint32_t u[CH][16];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            uint32_t v[32];
-            tmem_load(tmem + 32 * c, v);
-            load_wait(v);
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                u[c][e] = pack_bf16(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f);
-        }
-        read();
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<uint4 *>(place(i)) =
-                    make_uint4(u[c][4 * i], u[c][4 * i + 1], u[c][4 * i + 2], u[c][4 * i + 3]);
-            write(c);
-        }
-        return;
-    }
-    const int slot = it.slot + it.head * it.pieces;
+__device__ __forceinline__ void write_sums(const AttnArgs &a, uint32_t tmem, uint8_t *stage, const Out &out,
+                                           int64_t token, const Item &it, int rows, int col, float f,
+                                           int64_t slot_floats, F read) {
+    if (it.pieces == 1) return write_rows<CH>(tmem, stage, out, token, it.head, rows, col, a.D, f, read);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, slot = it.slot + it.head * it.pieces;
     float4 *sums = reinterpret_cast<float4 *>(a.parts + slot * slot_floats + warp * (CH * 1024)) + lane;
     const int64_t step = slot_floats / 4;  // from one part's to the next's
 #pragma unroll 1
@@ -948,10 +1031,11 @@ __device__ __forceinline__ void write_columns(const AttnArgs &a, uint32_t tmem, 
                 x.x += p.x, x.y += p.y, x.z += p.z, x.w += p.w;
                 y.x += q.x, y.y += q.y, y.z += q.z, y.w += q.w;
             }
-            *reinterpret_cast<uint4 *>(place(i)) = make_uint4(pack_bf16(x.x * f, x.y * f), pack_bf16(x.z * f, x.w * f),
-                                                              pack_bf16(y.x * f, y.y * f), pack_bf16(y.z * f, y.w * f));
+            *reinterpret_cast<uint4 *>(stage_piece(stage, lane, i)) =
+                make_uint4(pack_bf16(x.x * f, x.y * f), pack_bf16(x.z * f, x.w * f), pack_bf16(y.x * f, y.y * f),
+                           pack_bf16(y.z * f, y.w * f));
         }
-        write(c);
+        write_stage(stage, out, token, it.head, rows, col + 32 * c, a.D);
     }
 }
 
@@ -1037,7 +1121,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 it.slot = z.x, it.piece = z.y;
                 it.head = (int)(rest % heads);
             }
-            failed = !bars.put(it, c);
+            failed = !bars.items.put(it, c);
             if (failed || it.kind == kEnd) break;
             ++c;
             const Seq &q = it.q;
@@ -1116,12 +1200,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             sum_product<C>(tmem + kColK, tmem + C::kColD, C::kStep, ring.addr(ri), add);
         };
         if (warp == C::kIssuer && elect_one()) {
-            failed = !bars.get_one(it, c);
+            failed = !bars.items.get_one(it, c);
             // ---- tiles of keys
             if (C::kOwn) {
                 // P^T and dS^T have columns of their own: the next S^T and gradient
                 // of P^T are computed as soon as these have been read
-                for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
+                for (; !failed && it.kind == kKeys; failed = failed || !bars.items.get_one(it, c)) {
                     const int blocks = it.count;
                     for (int j = 0; j < blocks; ++j, ++b, i += 2) {
                         failed = (j == 0 && !bar_wait(bars.tile_full, n & 1, kTries)) || !ring.wait_full(i) ||
@@ -1144,7 +1228,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 auto blocks_of = [&]() { return it.kind == kKeys ? it.count : 0; };
                 // the next tile of keys that meets queries (or what comes after the last)
                 auto next_item = [&]() {
-                    do failed = failed || !bars.get_one(it, c);
+                    do failed = failed || !bars.items.get_one(it, c);
                     while (!failed && it.kind == kKeys && blocks_of() == 0);
                 };
                 if (it.kind == kKeys && blocks_of() == 0) next_item();
@@ -1193,7 +1277,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             // ---- tiles of queries: S and the gradient of P of each block, once
             // those of the block before have been read
             int r = C::kOwn ? b : 0;  // blocks of these two barriers
-            for (; !failed && it.kind == kQueries; failed = failed || !bars.get_one(it, c)) {
+            for (; !failed && it.kind == kQueries; failed = failed || !bars.items.get_one(it, c)) {
                 const int blocks = it.count;
                 for (int j = 0; j < blocks; ++j, ++r, i += 2) {
                     failed = (j == 0 && !bar_wait(bars.tile_full, n & 1, kTries)) || !ring.wait_full(i) ||
@@ -1219,9 +1303,9 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             mma_commit(bars.done);
             failed |= !bar_wait(bars.done, 0, kTries);
         } else if (warp == C::kSummer && elect_one()) {
-            failed = !bars.get_one(it, c);
+            failed = !bars.items.get_one(it, c);
             if (C::kOwn) {
-                for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
+                for (; !failed && it.kind == kKeys; failed = failed || !bars.items.get_one(it, c)) {
                     const int blocks = it.count;
                     for (int j = 0; j < blocks; ++j, ++b, i += 2) {
                         failed = !bar_wait(bars.v_full, b & 1, kTries) ||
@@ -1241,7 +1325,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                     n += blocks > 0;
                 }
             } else {
-                for (; !failed && it.kind == kKeys; failed = failed || !bars.get_one(it, c)) {
+                for (; !failed && it.kind == kKeys; failed = failed || !bars.items.get_one(it, c)) {
                     // the issuer's; each is seen to its end, so that the barriers'
                     // parities below are those of this item's blocks
                     const int blocks = it.count;
@@ -1251,7 +1335,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 }
             }
             // dQ += dS K (K's scores are done: the row warps had them)
-            for (; !failed && it.kind == kQueries; failed = failed || !bars.get_one(it, c)) {
+            for (; !failed && it.kind == kQueries; failed = failed || !bars.items.get_one(it, c)) {
                 const int blocks = it.count;
                 for (int j = 0; j < blocks; ++j, ++b, i += 2) {
                     failed = !bar_wait(bars.w_full, b & 1, kTries) ||
@@ -1281,7 +1365,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
         const uint64_t scale2 = pair(a.scale2, a.scale2);
         int b = 0, n = 0;  // blocks and items with blocks so far
         wait_previous();
-        failed = !bars.get_warp(it, c);
+        failed = !bars.items.get_warp(it, c);
 
         // ---- tiles of keys
         const uint32_t s_addr = lanes + C::kColS + W * part, g_addr = lanes + C::kColG + W * part;
@@ -1423,11 +1507,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 if (lane == 0) bar_arrive(bars.w_full);
             }
             if (failed) break;
-            failed = !bars.get_warp(it, c);
+            failed = !bars.items.get_warp(it, c);
             if (failed) break;
             if (it.kind == kKeys) start();
             Item was;  // the item that ends here
-            bars.read(was, (c - 2) % C::kItems);
+            bars.items.read(was, c - 2);
             const int first = was.tile * kRows + (warp & 3) * 32;  // the warp's first row
             const int64_t token = was.q.k0 + (int64_t)first;
             if (was.count > 0) {
@@ -1440,7 +1524,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 constexpr int CH = 2 * DP / 32 / C::kParts;
                 const int c0 = part * CH, col = 32 * c0 % DP;
                 const bool keys = 32 * c0 >= DP;
-                write_columns<CH>(a, lanes + C::kColSum + 32 * c0, stage, keys ? a.dk : a.dv, token, was, was.q.m - first,
+                write_sums<CH>(a, lanes + C::kColSum + 32 * c0, stage, keys ? a.dk : a.dv, token, was, was.q.m - first,
                                   col, keys ? a.scale : 1.f, C::kSlot, [&]() {
                                       fence_before();
                                       __syncwarp();
@@ -1451,7 +1535,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 const Out &out = part ? a.dk : a.dv;
                 write_zero_row(out.p + (token + lane) * out.ts + was.head * out.hs, a.D);
             }
-            bars.finished(c - 2);
+            bars.items.finished(c - 2);
         }
 
         // ---- tiles of queries
@@ -1539,11 +1623,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 if (lane == 0) bar_arrive(bars.w_full);
             }
             if (failed) break;
-            failed = !bars.get_warp(it, c);
+            failed = !bars.items.get_warp(it, c);
             if (failed) break;
             if (it.kind == kQueries) load_row();
             Item was;
-            bars.read(was, (c - 2) % C::kItems);
+            bars.items.read(was, c - 2);
             const int first = was.tile * kRows + (warp & 3) * 32;
             const int64_t token = was.q.q0 + (int64_t)first;
             if (was.count > 0) {
@@ -1559,7 +1643,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
                 };
                 constexpr int CH = DP / 32 / C::kParts > 0 ? DP / 32 / C::kParts : 1;
                 if (part < DP / 32 / CH)
-                    write_columns<CH>(a, lanes + C::kColSum + 32 * CH * part, stage, a.dq, token, was, was.q.n - first,
+                    write_sums<CH>(a, lanes + C::kColSum + 32 * CH * part, stage, a.dq, token, was, was.q.n - first,
                                       32 * CH * part, a.scale, C::kSlot, read);
                 else
                     read();
@@ -1567,7 +1651,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
             } else if (first + lane < was.q.n && part == 0) {
                 write_zero_row(a.dq.p + (token + lane) * a.dq.ts + was.head * a.dq.hs, a.D);
             }
-            bars.finished(c - 2);
+            bars.items.finished(c - 2);
         }
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);

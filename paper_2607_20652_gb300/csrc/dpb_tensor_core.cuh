@@ -166,6 +166,30 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// ---- blocks that have not started -----------------------------------------------
+
+// Asks for a block of this grid that has not started; the answer's 16 bytes in
+// shared memory count on `bar`. Not again after an answer that there was none.
+__device__ __forceinline__ void ask_block(uint32_t answer, uint32_t bar) {
+    asm volatile(
+        "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer),
+        "r"(bar)
+        : "memory");
+}
+// Whether there was one (it will not start: its work is this block's), and its index.
+__device__ __forceinline__ bool block_answer(uint32_t answer, uint32_t &index) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n .reg .b128 r;\n .reg .b64 lo, hi;\n"
+        "ld.shared.v2.b64 {lo, hi}, [%2];\n mov.b128 r, {lo, hi};\n"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n selp.u32 %0, 1, 0, p;\n"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}\n"
+        : "=r"(ok), "+r"(index)
+        : "r"(answer)
+        : "memory");
+    return ok != 0;
+}
+
 // ---- the next kernel of the stream ---------------------------------------------
 
 // It may start once every block has called this or ended (if it is launched to).

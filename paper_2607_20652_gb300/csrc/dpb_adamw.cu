@@ -4,9 +4,9 @@
 // Bound by memory: each parameter, gradient and state is read once and the
 // first three kinds written once. The tensors' addresses travel as a kernel
 // argument (no table to copy to the device first), so a step is one launch
-// for every kMany tensors. A block takes 2048 values of one tensor, found by
-// bisection in that argument; a warp takes 256 of them, 8 a lane, so that a
-// block of 8-bit states is one warp's, its scale a warp maximum.
+// for every kMany tensors. A block takes 512 values of one tensor (or some rounds
+// of 512), found by bisection in that argument; a warp takes 256 of them, 8 a
+// lane, so that a block of 8-bit states is one warp's, its scale a warp maximum.
 #include <algorithm>
 #include <cmath>
 #include <cuda_bf16.h>
@@ -20,14 +20,15 @@
 namespace dpb {
 namespace {
 
-constexpr int kThreads = 64;
 constexpr int kPer = 8;                    // values a thread
+// Rounds a block: 32-bit states keep enough loads in flight with one (203 M bf16
+// parameters: 632 us). 8-bit ones compute longer on fewer bytes, so a block loads
+// its next round while it computes one, and its start is spread over up to eight
+// (203 M bf16 parameters: 457 us; one round of 256 threads 547, four of 128
+// threads 475) as long as there are some waves of blocks (14 M fp32 parameters:
+// 57 us with eight).
+constexpr int kThreads = 64;
 constexpr int kRound = kThreads * kPer;    // values a block takes at a time
-// Rounds a block: 32-bit states keep enough loads in flight with one. 8-bit
-// ones compute longer on fewer bytes, so a block loads its next round while it
-// computes one, and its start is spread over up to eight (203 M bf16 parameters:
-// 432 us; one round of 256 threads 547, four of 128 threads 475) as long as
-// there are some waves of blocks (14 M fp32 parameters: 57 us with eight).
 constexpr int kMostRounds = 8, kWaves = 6, kResident = 152 * 14;
 constexpr int kBlock = 32 * kPer;          // values that share a scale
 constexpr float kTop = 448.f;              // largest e4m3 value
@@ -55,6 +56,7 @@ struct Hyper {
     float rate, b1, c1, b2, c2, eps, decay, fix2;  // rate: lr / (1 - beta1^step); fix2: (1 - beta2^step)^-1/2
     uint32_t key;
     const float *grad_scale;
+    float zero;  // -0
 };
 
 // The lowbias32 integer hash of the hash-prospector project: two rounds of
@@ -73,7 +75,7 @@ __device__ __forceinline__ float rcp_approx(float x) {
     return y;
 }
 // Two fp32 values in one register pair, and the packed multiply and add
-// (one instruction for both, each rounded by itself).
+// (one instruction for both).
 struct F2 {
     uint64_t u;
     __device__ __forceinline__ F2() : u(0) {}
@@ -92,6 +94,15 @@ __device__ __forceinline__ F2 operator*(F2 a, F2 b) {
 __device__ __forceinline__ F2 operator+(F2 a, F2 b) {
     F2 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+    return r;
+}
+
+// a b, rounded by itself whatever is added to it: the compiler may make one
+// multiply-add of a packed product and the add that follows it, but not of this
+// (zero: -0, from memory, so that it does not see that nothing is added).
+__device__ __forceinline__ F2 product(F2 a, F2 b, F2 zero) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(zero.u));
     return r;
 }
 
@@ -263,6 +274,7 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
     const int64_t blk = i0 / kBlock;
     float ms, vs;
     float tm = 0.f, tv = 0.f;  // largest magnitudes of this lane
+    const F2 zero(h.zero, h.zero);
 #pragma unroll
     for (int i = 0; i < kPer; i += 2) {
         F2 gi = two_values(in.g, i), mi = two_values(in.m, i), vi = two_values(in.v, i);
@@ -272,8 +284,8 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
             vi = vi * F2(in.vs, in.vs);
             vi = vi * vi;
         }
-        mi = mi * F2(h.b1, h.b1) + gi * F2(h.c1, h.c1);
-        vi = vi * F2(h.b2, h.b2) + gi * F2(h.c2, h.c2) * gi;
+        mi = product(mi, F2(h.b1, h.b1), zero) + product(gi, F2(h.c1, h.c1), zero);
+        vi = product(vi, F2(h.b2, h.b2), zero) + product(gi * F2(h.c2, h.c2), gi, zero);
         const float2 m2 = mi.get(), v2 = vi.get();
         const F2 root(__fsqrt_rn(v2.x), __fsqrt_rn(v2.y));
         const float2 den = (root * F2(h.fix2, h.fix2) + F2(h.eps, h.eps)).get();
@@ -339,14 +351,19 @@ template <typename T, bool F8, bool WIDE>
 __device__ __forceinline__ void step_chunk(const Tensor t, int64_t i0, int chunk, const Hyper &h, float gs) {
     const int64_t end = min(i0 + chunk, (t.n + kBlock - 1) / kBlock * kBlock);  // whole warps
     if (i0 >= end) return;
-    Loaded<T, F8> a, b;
+    Loaded<T, F8> a;
     load_values<T, F8, WIDE>(t, i0, a);
+    if constexpr (!F8) {  // one round
+        step_values<T, F8, WIDE>(t, i0, h, gs, a);
+    } else {
+        Loaded<T, F8> b;
 #pragma unroll 1
-    for (int64_t i = i0; i < end; i += kRound) {
-        const bool more = i + kRound < end;
-        if (more) load_values<T, F8, WIDE>(t, i + kRound, b);
-        step_values<T, F8, WIDE>(t, i, h, gs, a);
-        if (more) a = b;
+        for (int64_t i = i0; i < end; i += kRound) {
+            const bool more = i + kRound < end;
+            if (more) load_values<T, F8, WIDE>(t, i + kRound, b);
+            step_values<T, F8, WIDE>(t, i, h, gs, a);
+            if (more) a = b;
+        }
     }
 }
 
@@ -454,6 +471,7 @@ extern "C" dpb_status dpb_adamw_step(const dpb_adamw_config *cfg, const dpb_adam
     h.b1 = (float)cfg->beta1;
     h.c1 = (float)(1.0 - cfg->beta1);
     h.b2 = (float)cfg->beta2;
+    h.zero = -0.f;
     h.c2 = (float)(1.0 - cfg->beta2);
     h.eps = (float)cfg->eps;
     h.decay = (float)(1.0 - cfg->lr * cfg->weight_decay);

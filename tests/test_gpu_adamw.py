@@ -243,3 +243,17 @@ def test_refusals():
             grp.step(g, step=1, **H)
     with pytest.raises(ValueError):
         grp.step([m], step=1, grad_scale=torch.ones(2, device="cuda"), **H)
+
+
+def test_8bit_states_follow_the_formula_rounding_by_rounding():
+    """The states' fp32 arithmetic is the formula's with every product and sum rounded by itself, so the scales are those
+    of the formula computed one operation at a time, bit for bit (a multiply-add in its place moves one in five)."""
+    n = 1 << 20
+    t = tensors([n], torch.float32, 8, seed=4)
+    (m8, v8, ms, vs, g), (b1, b2) = (t[k][0] for k in ("m", "v", "ms", "vs", "g")), H["betas"]
+    m = b1 * (m8.float().view(-1, BLOCK) * ms[:, None]) + (1 - b1) * g.view(-1, BLOCK)
+    v = (v8.float().view(-1, BLOCK) * vs[:, None]).square()
+    v = b2 * v + (1 - b2) * g.view(-1, BLOCK) * g.view(-1, BLOCK)
+    want = [x.abs().amax(1) * (1 / 448) for x in (m, v.sqrt())]
+    group(t, 8).step(t["g"], step=3, seed=5, **H)
+    assert torch.equal(t["ms"][0], want[0]) and torch.equal(t["vs"][0], want[1])

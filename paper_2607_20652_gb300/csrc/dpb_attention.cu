@@ -875,7 +875,8 @@ struct KeyBlocks {
 // blocks first (to 1/256 of the longest; their order within that does not
 // matter to any result). A tile of more than half an SM's share of all blocks
 // is listed in parts, as far as there is room for their sums; which, follows
-// from the numbers of blocks alone. One block of THREADS.
+// from the numbers of blocks alone. One block of THREADS; no loop is unrolled,
+// since fetching code that runs once is most of the time.
 template <int THREADS>
 __device__ void make_plan(const AttnArgs &a) {
     constexpr int kBuckets = 256;
@@ -889,18 +890,22 @@ __device__ void make_plan(const AttnArgs &a) {
     auto bucket = [&](int blocks) { return kBuckets - 1 - (blocks >> shift); };
     auto clear = [&]() {
         __syncthreads();
+#pragma unroll 1
         for (int i = threadIdx.x; i < 2 * kBuckets; i += THREADS) place[i / kBuckets][i % kBuckets] = 0;
         __syncthreads();
     };
     // f(side, sequence, tile, blocks)
     auto each = [&](auto f, bool report) {
+#pragma unroll 1
         for (int s = warp; s < a.seqs; s += THREADS / 32) {
             const Seq q = sequence(a, load_offsets(a, s));
             if (!q.ok) {
                 if (report && lane == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
                 continue;
             }
+#pragma unroll 1
             for (int t = lane; t * kRows < q.m; t += 32) f(0, q, t, KeyBlocks::of<kRows>(a, q, t).count);
+#pragma unroll 1
             for (int t = lane; t * kRows < q.n; t += 32) f(1, q, t, tile_blocks<kRows>(a, q, t));
         }
     };
@@ -924,8 +929,10 @@ __device__ void make_plan(const AttnArgs &a) {
     if (a.slots > 0) {
         if (warp == 0) {
             int l = (int)min(max((unsigned long long)kLeast, total / (2 * a.sms)), 0x40000000ull);
+#pragma unroll 1
             for (;;) {
                 int64_t need = 0;
+#pragma unroll 1
                 for (int i = lane; i < 2 * kBuckets; i += 32) {
                     // the most blocks of the bucket: no tile of it has more parts
                     const int n = place[i / kBuckets][i % kBuckets];
@@ -943,11 +950,13 @@ __device__ void make_plan(const AttnArgs &a) {
         __syncthreads();
     }
     if (split) {
+#pragma unroll 1
         for (int i = threadIdx.x; i < a.slots * kMostWarps; i += THREADS) a.arrived[i] = 0;
         clear();
         each(
             [&](int side, const Seq &, int, int blocks) {
                 const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
+#pragma unroll 1
                 for (int i = 0; i < n; ++i) atomicAdd(&place[side][bucket(each_has + (i < more))], 1);
             },
             false);
@@ -955,6 +964,7 @@ __device__ void make_plan(const AttnArgs &a) {
     }
     if (warp < 2) {
         int before = 0;
+#pragma unroll 1
         for (int i = lane; i < kBuckets; i += 32) {
             const int v = place[warp][i];
             int sum = v;
@@ -980,6 +990,7 @@ __device__ void make_plan(const AttnArgs &a) {
         [&](int side, const Seq &q, int t, int blocks) {
             const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
             const int base = n > 1 ? atomicAdd(&slot, n * (side ? a.hq : a.hkv)) : 0;
+#pragma unroll 1
             for (int i = 0; i < n; ++i) {
                 const int first = i * each_has + min(i, more), count = each_has + (i < more);
                 const int at = atomicAdd(&place[side][bucket(count)], 1);
@@ -1021,20 +1032,23 @@ __device__ __forceinline__ void write_sums(const AttnArgs &a, uint32_t tmem, uin
     __threadfence();
 #pragma unroll 1
     for (int c = 0; c < CH; ++c) {
+        float4 x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __ldcg(sums + (8 * c + e) * 32);
 #pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-            const float4 *part = sums + (8 * c + 2 * i) * 32;
-#pragma unroll 4
-            for (int k = 0; k < it.pieces; ++k, part += step) {
-                const float4 p = __ldcg(part), q = __ldcg(part + 32);
-                x.x += p.x, x.y += p.y, x.z += p.z, x.w += p.w;
-                y.x += q.x, y.y += q.y, y.z += q.z, y.w += q.w;
-            }
-            *reinterpret_cast<uint4 *>(stage_piece(stage, lane, i)) =
-                make_uint4(pack_bf16(x.x * f, x.y * f), pack_bf16(x.z * f, x.w * f), pack_bf16(y.x * f, y.y * f),
-                           pack_bf16(y.z * f, y.w * f));
+        for (int k = 1; k < it.pieces; ++k) {
+            float4 y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = __ldcg(sums + k * step + (8 * c + e) * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e].x += y[e].x, x[e].y += y[e].y, x[e].z += y[e].z, x[e].w += y[e].w;
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4 *>(stage_piece(stage, lane, i)) =
+                make_uint4(pack_bf16(x[2 * i].x * f, x[2 * i].y * f), pack_bf16(x[2 * i].z * f, x[2 * i].w * f),
+                           pack_bf16(x[2 * i + 1].x * f, x[2 * i + 1].y * f),
+                           pack_bf16(x[2 * i + 1].z * f, x[2 * i + 1].w * f));
         write_stage(stage, out, token, it.head, rows, col + 32 * c, a.D);
     }
 }
@@ -1079,12 +1093,13 @@ __global__ void __launch_bounds__(512) attention_delta_kernel(const __grid_const
 //
 // Measured, with the delta kernel (causal; rate of the five products that are
 // the least: 2.5 x the forward's), against a kernel for each side with a block
-// for each tile: 1 x 12289, 12 heads of 64: 648 us (666), 895 TFLOP/s; 8 x 1024,
-// 12 heads of 64: 73 us (98); 1 x 8192, 16 heads of 128: 576 us (590), 1193
-// TFLOP/s, of the seven products done 1670; sequences of 3001, 638, 429, 95 and
-// less, 16 heads of 128 on 4: 126 us (215; 140 with no tile in parts, when one SM
+// for each tile: 1 x 12289, 12 heads of 64: 645 us (666), 899 TFLOP/s; 8 x 1024,
+// 12 heads of 64: 71 us (98); 1 x 8192, 16 heads of 128: 570 us (590), 1206
+// TFLOP/s, of the seven products done 1688; sequences of 3001, 638, 429, 95 and
+// less, 16 heads of 128 on 4: 122 us (215; 140 with no tile in parts, when one SM
 // has the longest tile of keys for 128 us). Bound by the tensor cores at 128; at
-// 64 by the exponentials and the conversions beside them.
+// 64 by the exponentials and the conversions beside them. Writing an item's sums
+// only after the next one's first block gained nothing (73 and 686 us).
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int DP = C::DP, BN = C::BN, W = C::kWidth;

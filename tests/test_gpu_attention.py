@@ -305,3 +305,68 @@ def test_bad_offsets_are_flagged_by_the_gradient(cu):
     assert dpb.status() == 0
     dpb.attention_backward(q, k, v, o, lse, do, cu_q=cu, cu_k=cu, max_q=120, max_k=120)
     assert dpb.status() == dpb.DEV_BAD_LENGTH
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_sequences_of_very_unequal_lengths(D):
+    nq, nk = [5, 2100, 0, 300, 1, 64, 129], [5, 2100, 0, 500, 3000, 64, 100]
+    q, k, v, do = draw(nq, nk, 4, 2, D, seed=D)
+    want, tol = formula(q, k, v, do, nq, nk, True, D ** -0.5)
+    got = run(q, k, v, do, nq, nk)
+    check(got, want, tol)
+    again = run(q, k, v, do, nq, nk)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    assert dpb.status() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rising", [True, False])
+def test_sharp_softmax_in_parts(D, rising):
+    """Parts whose maxima lie far apart, the largest in the last or in the first."""
+    nq = [2600]
+    q, k, v, do = draw(nq, nq, 1, 1, D, seed=11)
+    ramp = torch.linspace(0.1, 4, 2600, device="cuda")[:, None, None]
+    k = (k * (ramp if rising else ramp.flip(0))).bfloat16()
+    want, tol = formula(q, k, v, do, nq, nq, True, D ** -0.5)
+    check(run(q, k, v, do, nq, nq), want, tol)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_long_sequences_see_nothing_of_their_neighbours(D):
+    nq, mine = [150, 2200, 2100], slice(150, 2350)
+    q, k, v, do = draw(nq, nq, 2, 2, D, seed=9, packed=False)
+    one = run(q, k, v, do, nq, nq)
+    b = [x.clone() for x in (q, k, v, do)]
+    for x in b:
+        x[:150] = math.nan
+        x[2350:] = math.nan
+    two = run(*b, nq, nq)
+    for n in one:
+        s = (slice(None), mine) if n == "lse" else mine
+        assert torch.equal(one[n][s], two[n][s]), n
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    q = torch.zeros((4096, 1, 64), dtype=torch.bfloat16, device="cuda")
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    dpb.attention_forward(q, q, q, workspace=ws)  # needs the status word alone
+    with pytest.raises(dpb.DPBError):
+        dpb.attention_backward(q, q, q, q, torch.zeros((1, 4096), device="cuda"), q, workspace=ws)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_tiles_without_a_block(D):
+    """Sequences whose rows see no key, between some that do: their tiles have no products to wait for."""
+    nq, nk = [300] + [130] * 9 + [200], [300] + [0] * 9 + [64]
+    q, k, v, do = draw(nq, nk, 4, 1, D, seed=12)
+    want, tol = formula(q, k, v, do, nq, nk, True, D ** -0.5)
+    check(run(q, k, v, do, nq, nk), want, tol)
+    assert dpb.status() == 0
+
+
+def test_heads_further_apart_than_tokens():
+    """[heads][tokens][dim] memory: the head stride is the larger one."""
+    q, k, v, do = draw([333], [333], 4, 2, 64, seed=4, packed=False)
+    one = run(q, k, v, do, [333], [333])
+    two = run(*(x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, do)), [333], [333])
+    assert all(torch.equal(one[n], two[n]) for n in one)

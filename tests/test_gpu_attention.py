@@ -370,3 +370,15 @@ def test_heads_further_apart_than_tokens():
     one = run(q, k, v, do, [333], [333])
     two = run(*(x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, do)), [333], [333])
     assert all(torch.equal(one[n], two[n]) for n in one)
+
+
+def test_longest_unannounced_and_many_short_sequences():
+    """Without max_q the grid is for the sum of all lengths: equal bits with and without it."""
+    nq = [(37 * i) % 100 for i in range(300)] + [1500] + [1, 700, 3]
+    q, k, v, do = draw(nq, nq, 4, 2, 64, seed=13)
+    want, tol = formula(q, k, v, do, nq, nq, True, 0.125)
+    got = run(q, k, v, do, nq, nq)
+    check(got, want, tol)
+    o, lse = dpb.attention_forward(q, k, v, cu_q=offsets(nq))
+    assert torch.equal(o, got["o"]) and torch.equal(lse, got["lse"])
+    assert dpb.status() == 0

@@ -382,3 +382,32 @@ def test_longest_unannounced_and_many_short_sequences():
     o, lse = dpb.attention_forward(q, k, v, cu_q=offsets(nq))
     assert torch.equal(o, got["o"]) and torch.equal(lse, got["lse"])
     assert dpb.status() == 0
+
+
+@pytest.mark.parametrize("D,nq", [(64, [900, 33, 500]), (128, [2500, 7])])
+def test_in_a_cuda_graph(D, nq):
+    """Forward and gradient captured once and replayed on other values."""
+    one, two = draw(nq, nq, 4, 2, D, seed=14, packed=False), draw(nq, nq, 4, 2, D, seed=15, packed=False)
+    want = [run(*x, nq, nq) for x in (one, two)]
+    q, k, v, do = (x.clone() for x in one)
+    at = dict(cu_q=offsets(nq), max_q=max(nq), workspace=torch.zeros(64 << 20, dtype=torch.uint8, device="cuda"))
+    got = {}
+
+    def step():
+        got["o"], got["lse"] = dpb.attention_forward(q, k, v, **at)
+        got["dq"], got["dk"], got["dv"] = dpb.attention_backward(q, k, v, got["o"], got["lse"], do, **at)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for values, w in ((two, want[1]), (one, want[0])):
+        for x, y in zip((q, k, v, do), values):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[n], w[n]) for n in got)

@@ -370,10 +370,12 @@ struct Finder {
 // Measured (causal; 4 x visible pairs x head_dim operations a head), against a
 // block for each item: 1 x 12289, 12 heads of 64: 213 us (222), 1087 TFLOP/s;
 // 8 x 1024, 12 heads of 64: 26.7 us (29.9); 1 x 8192, 16 heads of 128: 191 us
-// (191), 1440 TFLOP/s; 8 x 1024, 16 heads of 128: 46.7 us (50.7). Bound by the
-// exponentials (16384 of a block of scores at 32 a cycle) at 64, by the tensor
-// cores at 128; short sequences by the way of an item's first block from memory
-// to its result.
+// (191), 1440 TFLOP/s; 8 x 1024, 16 heads of 128: 45 us (50.7). At 128 bound by
+// the tensor cores. At 64 a block of scores takes 1170 cycles, of them 512 of
+// exponentials (32 a cycle) and some 590 of products: the row warps' chain from
+// one to the other (2.0 instructions a cycle, of 4) is what is left. Short
+// sequences are bound by the way of an item's first block from memory to its
+// result.
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int DP = C::DP, BN = C::BN;
@@ -1154,7 +1156,8 @@ __global__ void __launch_bounds__(512) attention_delta_kernel(const __grid_const
 // TFLOP/s, of the seven products done 1688; sequences of 3001, 638, 429, 95 and
 // less, 16 heads of 128 on 4: 122 us (215; 140 with no tile in parts, when one SM
 // has the longest tile of keys for 128 us). Bound by the tensor cores at 128; at
-// 64 by the exponentials and the conversions beside them. Writing an item's sums
+// 64 (1800 cycles a block, 1030 of products, 512 of exponentials) by the row
+// warps' arithmetic, 2.5 instructions a cycle of 4. Writing an item's sums
 // only after the next one's first block gained nothing (73 and 686 us).
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __grid_constant__ AttnArgs a) {

@@ -319,7 +319,7 @@ struct FwdShape {
 
 // Visible keys of query row i (of n, against m keys).
 __device__ __forceinline__ int visible(const AttnArgs &a, const Seq &q, int i) {
-    return a.causal ? max(0, min(q.m, i + q.m - q.n + 1)) : q.m;
+    return a.causal ? max(0, min(q.m, i + (q.m - q.n) + 1)) : q.m;
 }
 
 // Blocks of BN keys that query tile `tile` has to see (0 where it has no rows).
@@ -924,7 +924,7 @@ __device__ void make_plan(const AttnArgs &a) {
     constexpr int kBuckets = 256;
     __shared__ int place[2][kBuckets];
     __shared__ unsigned long long total;
-    __shared__ int longest, slot, split;
+    __shared__ int longest, slot, split, seen;
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const int64_t most = (int64_t)((max(a.max_q, a.max_k) - 1) / kRows + 1) * a.group;
     int shift = 0;
@@ -967,18 +967,24 @@ __device__ void make_plan(const AttnArgs &a) {
             }
         }
     };
-    if (threadIdx.x == 0) total = 0, longest = 0x7fffffff, slot = 0, split = 0;
+    if (threadIdx.x == 0) total = 0, longest = 0x7fffffff, slot = 0, split = 0, seen = 0;
     unsigned long long mine = 0;
+    int most_mine = 0;
     clear();
     each(
         [&](int side, const Seq &, int, int blocks) {
             atomicAdd(&place[side][bucket(blocks)], 1);
             mine += (unsigned long long)blocks * (side ? a.hq : a.hkv);
+            most_mine = max(most_mine, blocks);
         },
         true);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(kFull, mine, o);
-    if (lane == 0 && mine > 0) atomicAdd(&total, mine);
+    most_mine = __reduce_max_sync(kFull, most_mine);
+    if (lane == 0 && mine > 0) {
+        atomicAdd(&total, mine);
+        atomicMax(&seen, most_mine);
+    }
     __syncthreads();
     // the parts of a tile of (about) as many blocks, none longer than l
     auto parts = [&](int blocks, int l) {
@@ -988,7 +994,7 @@ __device__ void make_plan(const AttnArgs &a) {
         if (warp == 0) {
             int l = (int)min(max((unsigned long long)kLeast, total / (2 * a.sms)), 0x40000000ull);
 #pragma unroll 1
-            for (;;) {
+            while (seen > l) {
                 int64_t need = 0;
 #pragma unroll 1
                 for (int i = lane; i < 2 * kBuckets; i += 32) {
@@ -1021,25 +1027,30 @@ __device__ void make_plan(const AttnArgs &a) {
         __syncthreads();
     }
     if (warp < 2) {
-        int before = 0;
-#pragma unroll 1
-        for (int i = lane; i < kBuckets; i += 32) {
-            const int v = place[warp][i];
-            int sum = v;
+        // each lane's eight buckets, then the lanes' sums
+        constexpr int kEach = kBuckets / 32;
+        int v[kEach], sum = 0;
 #pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int x = __shfl_up_sync(kFull, sum, o);
-                if (lane >= o) sum += x;
-            }
-            place[warp][i] = before + sum - v;
-            before += __shfl_sync(kFull, sum, 31);
+        for (int i = 0; i < kEach; ++i) sum += v[i] = place[warp][lane * kEach + i];
+        int before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int x = __shfl_up_sync(kFull, before, o);
+            if (lane >= o) before += x;
+        }
+        const int all = __shfl_sync(kFull, before, 31);
+        before -= sum;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            place[warp][lane * kEach + i] = before;
+            before += v[i];
         }
         if (lane == 0) {
             if (warp == 0) {
                 a.plan->next = 0;
-                a.plan->keys = (int)min((int64_t)before, a.cap_k);
+                a.plan->keys = (int)min((int64_t)all, a.cap_k);
             } else {
-                a.plan->queries = (int)min((int64_t)before, a.cap_q);
+                a.plan->queries = (int)min((int64_t)all, a.cap_q);
             }
         }
     }

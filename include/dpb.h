@@ -428,7 +428,12 @@ dpb_status dpb_rope_workspace_size(const dpb_rope_config *cfg, size_t *bytes);
  * takes part with weight 0, so it has to be finite. scale > 0.
  * Scores, softmax and sums are fp32; the probabilities enter their product
  * with v in bf16. Offsets out of range, or a sequence longer than max_q or
- * max_k, set DPB_DEV_BAD_LENGTH and that sequence is skipped.
+ * max_k, set DPB_DEV_BAD_LENGTH and that sequence is skipped. The offsets need
+ * not cover every row: rows that no sequence holds (before the first offset,
+ * from the last one on, of a skipped sequence, or all of them with seqs = 0)
+ * give o = 0, lse = -inf and gradients of 0, whatever q, k and v hold there.
+ * A row that several claim (offsets that decrease in between, which is flagged)
+ * holds one of their results, or zeros where one of them is skipped.
  */
 typedef struct dpb_attention_config {
     int64_t total_q, total_k;

@@ -104,7 +104,8 @@ class Attention(nn.Module):
     positions up to ``context`` (None or 0: none); ``rope`` holds further
     arguments of dpb.rope_tables (base, scaling, ...). forward() also takes
     packed rows x [T, d] with ``cu`` (int32 token offsets of the sequences) and
-    ``longest``; positions then restart at every sequence."""
+    ``longest``; positions then restart at every sequence, and rows outside of
+    ``cu`` (padding) give 0 and take no part in any gradient."""
 
     def __init__(self, d: int, heads: int, kv_heads: Optional[int] = None, qk_norm: bool = True, rotary: bool = True,
                  context: int = 1024, rope: Optional[dict] = None, device=None, dtype=None):
@@ -144,7 +145,8 @@ class Attention(nn.Module):
                 positions = torch.arange(S, dtype=torch.int32, device=x.device).repeat(B)
         elif self.cos is not None:
             rows = torch.arange(x.shape[0], dtype=torch.int32, device=x.device)
-            positions = rows - cu[torch.searchsorted(cu, rows, right=True) - 1]
+            # padding has no position: any row of the tables will do
+            positions = (rows - cu[torch.searchsorted(cu, rows, right=True) - 1]).clamp_(0, self.context - 1)
         if self.cos is not None and longest is not None and longest > self.context:
             raise ValueError(f"sequences of {longest} tokens, rotary tables for {self.context}")
         rope = None

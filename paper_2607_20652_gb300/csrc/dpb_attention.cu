@@ -61,6 +61,7 @@ struct AttnArgs {
     const int32_t *cu_q, *cu_k;
     int64_t total_q, total_k;
     int seqs, max_q, max_k, hq, hkv, group, D, causal, tiles, close;
+    int items;            // blocks of the forward's grid for the sequences
     float scale, scale2;  // scale, and scale x log2 e
     In o, go;
     Out out, dq, dk, dv;
@@ -85,11 +86,16 @@ struct Seq {
     bool ok;
 };
 
+// -1 <= s <= seqs: -1 and seqs stand for the rows before the first sequence and
+// after the last.
 __device__ __forceinline__ Offsets load_offsets(const AttnArgs &a, int s) {
-    Offsets r{0, a.total_q, 0, a.total_k};
+    const bool first = s < 0, last = s >= a.seqs;
+    Offsets r{0, first ? 0 : a.total_q, 0, first ? 0 : a.total_k};
     if (a.cu_q) {
-        r.q0 = __ldg(a.cu_q + s), r.q1 = __ldg(a.cu_q + s + 1);
-        r.k0 = __ldg(a.cu_k + s), r.k1 = __ldg(a.cu_k + s + 1);
+        if (!first) r.q0 = __ldg(a.cu_q + s), r.k0 = __ldg(a.cu_k + s);
+        if (!last) r.q1 = __ldg(a.cu_q + s + 1), r.k1 = __ldg(a.cu_k + s + 1);
+    } else if (last && s > 0) {
+        r.q0 = a.total_q, r.k0 = a.total_k;
     }
     return r;
 }
@@ -98,6 +104,21 @@ __device__ __forceinline__ Seq sequence(const AttnArgs &a, const Offsets &o) {
     r.ok = o.q0 >= 0 && o.q1 >= o.q0 && o.q1 <= a.total_q && o.k0 >= 0 && o.k1 >= o.k0 && o.k1 <= a.total_k &&
            o.q1 - o.q0 <= a.max_q && o.k1 - o.k0 <= a.max_k;
     r.q0 = (int)o.q0, r.n = (int)(o.q1 - o.q0), r.k0 = (int)o.k0, r.m = (int)(o.k1 - o.k0);
+    return r;
+}
+// The same of -1 <= s <= seqs. What is no sound sequence (not ok) has the rows
+// that its offsets pass on the way up, which see nothing and are seen by none:
+// from the first offset to the last such a way passes every row, so each is a
+// sound sequence's or one of these.
+__device__ __forceinline__ Seq rows_of(const AttnArgs &a, int s, const Offsets &o) {
+    Seq r = sequence(a, o);
+    const bool is = s >= 0 && s < a.seqs;
+    if (is && !r.ok) set_status(a.status, DPB_DEV_BAD_LENGTH);
+    r.ok = r.ok && is;
+    if (!r.ok) {
+        r.q0 = (int)max((int64_t)0, o.q0), r.n = (int)max((int64_t)0, min(o.q1, a.total_q) - r.q0);
+        r.k0 = (int)max((int64_t)0, o.k0), r.m = (int)max((int64_t)0, min(o.k1, a.total_k) - r.k0);
+    }
     return r;
 }
 
@@ -329,6 +350,8 @@ __device__ __forceinline__ int tile_blocks(const AttnArgs &a, const Seq &q, int 
     return r0 < q.n ? (visible(a, q, min(r0 + kRows, q.n) - 1) + BN - 1) / BN : 0;
 }
 
+__device__ __forceinline__ int pairs_of(const Seq &q) { return (q.n + 2 * kRows - 1) / (2 * kRows); }
+
 // The place-th pair of tiles of queries of all sequences in turn, the last of
 // each first, or false after all of them. All lanes of a warp, which look at 32
 // sequences at a time from where they left off (places mostly grow).
@@ -340,9 +363,8 @@ struct Finder {
         for (; first < a.seqs; first += 32) {
             const int s = first + lane;
             Seq q{0, 0, 0, 0, false};
-            if (s < a.seqs) q = sequence(a, load_offsets(a, s));
-            if (s < a.seqs && !q.ok) set_status(a.status, DPB_DEV_BAD_LENGTH);
-            const int pairs = q.ok ? (q.n + 2 * kRows - 1) / (2 * kRows) : 0;
+            if (s < a.seqs) q = rows_of(a, s, load_offsets(a, s));
+            const int pairs = pairs_of(q);
             int upto = pairs;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
@@ -424,6 +446,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
             uint32_t at = blockIdx.x;
             bool have = true;
             Finder finder{0, 0};
+            // the index at hand (step > 0): its sequence and next pair of tiles, from
+            // there to the one after
+            int seq = 0, tile = 0, step = 0;
+            // pairs to look up: of the index at hand; beyond those that the grid counts
+            int place = -1, over = -1;
+            constexpr int kFar = 1 << 28;
             // takes over a block that has not started, if there is one
             auto next = [&]() {
                 if (elect_one()) {
@@ -442,21 +470,41 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
                 it.kind = kEnd;
                 while (have) {
                     // the heads of a group side by side; the longest rows first, or
-                    // sequence by sequence
+                    // sequence by sequence; last, of each head, the rows before the first
+                    // sequence and after the last, one pair after the other (8 x 1024, 12
+                    // heads of 64, has none: 25.3 us, 24.8 without these blocks)
                     const int rest = (int)(at / a.hq);
-                    int seq = rest % a.seqs;
                     it.head = (int)(at % a.hq);
-                    it.tile = a.tiles - 1 - rest / a.seqs;
-                    if (a.close && !finder.find(a, rest, seq, it.tile)) {
-                        next();
-                        continue;
+                    if (step == 0) {
+                        if (at < (uint32_t)a.items) {
+                            seq = rest % a.seqs;
+                            tile = a.tiles - 1 - rest / a.seqs;
+                            step = a.tiles;  // beyond every sound sequence's
+                            if (a.close) place = rest;
+                        } else {
+                            seq = rest * a.hq == a.items ? -1 : a.seqs;
+                            tile = 0, step = 1;
+                            // sequences that overlap can have more than the grid counts
+                            if (a.close && seq >= 0) over = rest - 1;
+                        }
                     }
-                    it.q = sequence(a, load_offsets(a, seq));
-                    if (!it.q.ok && lane == 0) set_status(a.status, DPB_DEV_BAD_LENGTH);
-                    if (it.q.ok && it.tile * 2 * kRows < it.q.n) {
+                    if (place >= 0) {
+                        step = kFar;
+                        if (!finder.find(a, place, seq, tile)) tile = kFar, over = -1;
+                        place = -1;
+                    }
+                    it.q = rows_of(a, seq, load_offsets(a, seq));
+                    it.tile = tile;
+                    if (tile < pairs_of(it.q)) {
+                        if (!it.q.ok) it.q.m = 0;
                         it.kind = kQueries;
                         break;
                     }
+                    if (over >= 0) {
+                        place = over++;
+                        continue;
+                    }
+                    step = 0;
                     next();
                 }
                 failed = failed || !list.put(it, c);
@@ -495,7 +543,11 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
                     }
                 }
                 if (failed) break;
-                next();
+                tile += step;
+                if (tile >= pairs_of(q) && over < 0) {
+                    step = 0;
+                    next();
+                }
             }
             // no copy is in flight when the block ends, whatever gave up
             ring.drain(i);
@@ -899,6 +951,21 @@ struct GradBars {
     }
 };
 
+// Zeroes one side's gradients: thread `mine` of `all` does its share.
+__device__ __forceinline__ void zero_gradients(const AttnArgs &a, bool keys, int tokens, int mine, int all) {
+    const int heads = keys ? a.hkv : a.hq, pieces = a.D / 8;
+#pragma unroll 1
+    for (int64_t i = mine; i < (int64_t)tokens * heads * pieces; i += all) {
+        const int64_t token = i / pieces / heads;
+        const int head = (int)(i / pieces % heads), col = (int)(i % pieces) * 8;
+#pragma unroll 1
+        for (int o = keys ? 1 : 0; o < (keys ? 3 : 1); ++o) {
+            const Out &out = o == 0 ? a.dq : o == 1 ? a.dk : a.dv;
+            *reinterpret_cast<uint4 *>(out.p + token * out.ts + head * out.hs + col) = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+}
+
 // The queries' blocks that a tile of keys meets: from the first that sees one of
 // its keys, of every query head of the group in turn.
 struct KeyBlocks {
@@ -917,14 +984,15 @@ struct KeyBlocks {
 // blocks first (to 1/256 of the longest; their order within that does not
 // matter to any result). A tile of more than half an SM's share of all blocks
 // is listed in parts, as far as there is room for their sums; which, follows
-// from the numbers of blocks alone. One block of THREADS; no loop is unrolled,
-// since fetching code that runs once is most of the time.
+// from the numbers of blocks alone. Rows that no sound sequence holds are listed
+// as tiles without a block. One block of THREADS; no loop is unrolled, since
+// fetching code that runs once is most of the time.
 template <int THREADS>
 __device__ void make_plan(const AttnArgs &a) {
     constexpr int kBuckets = 256;
     __shared__ int place[2][kBuckets];
     __shared__ unsigned long long total;
-    __shared__ int longest, slot, split, seen;
+    __shared__ int longest, slot, split, seen, lost;
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const int64_t most = (int64_t)((max(a.max_q, a.max_k) - 1) / kRows + 1) * a.group;
     int shift = 0;
@@ -940,44 +1008,45 @@ __device__ void make_plan(const AttnArgs &a) {
     // offsets its lanes load 32 at a time; a lane lists one of a single tile by
     // itself, then all lanes each longer one
     constexpr int kWarps = THREADS / 32;
-    auto each = [&](auto f, bool report) {
+    auto each = [&](auto f) {
 #pragma unroll 1
-        for (int s0 = warp; s0 < a.seqs; s0 += 32 * kWarps) {
+        for (int s0 = warp - 1; s0 <= a.seqs; s0 += 32 * kWarps) {
+            const int s = s0 + kWarps * lane;
             Seq mine{0, 0, 0, 0, true};
-            if (s0 + kWarps * lane < a.seqs) mine = sequence(a, load_offsets(a, s0 + kWarps * lane));
-            if (report && !mine.ok) set_status(a.status, DPB_DEV_BAD_LENGTH);
-            const bool more = mine.ok && max(mine.n, mine.m) > kRows;
+            if (s <= a.seqs) mine = rows_of(a, s, load_offsets(a, s));
+            const bool more = max(mine.n, mine.m) > kRows;
             uint32_t left = __ballot_sync(kFull, more);
             Seq q = mine;
-            if (!mine.ok || more) q.n = q.m = 0;
+            if (more) q.n = q.m = 0;
             int first = 0, step = 1;
 #pragma unroll 1
             for (;;) {
 #pragma unroll 1
-                for (int t = first; t * kRows < q.m; t += step) f(0, q, t, KeyBlocks::of<kRows>(a, q, t).count);
+                for (int t = first; t < (q.m + kRows - 1) / kRows; t += step)
+                    f(0, q, t, q.ok ? KeyBlocks::of<kRows>(a, q, t).count : 0);
 #pragma unroll 1
-                for (int t = first; t * kRows < q.n; t += step) f(1, q, t, tile_blocks<kRows>(a, q, t));
+                for (int t = first; t < (q.n + kRows - 1) / kRows; t += step)
+                    f(1, q, t, q.ok ? tile_blocks<kRows>(a, q, t) : 0);
                 __syncwarp();
                 if (left == 0) break;
                 const int i = __ffs(left) - 1;
                 left &= left - 1;
+                q.ok = __shfl_sync(kFull, mine.ok, i);
                 q.q0 = __shfl_sync(kFull, mine.q0, i), q.n = __shfl_sync(kFull, mine.n, i);
                 q.k0 = __shfl_sync(kFull, mine.k0, i), q.m = __shfl_sync(kFull, mine.m, i);
                 first = lane, step = 32;
             }
         }
     };
-    if (threadIdx.x == 0) total = 0, longest = 0x7fffffff, slot = 0, split = 0, seen = 0;
+    if (threadIdx.x == 0) total = 0, longest = 0x7fffffff, slot = 0, split = 0, seen = 0, lost = 0;
     unsigned long long mine = 0;
     int most_mine = 0;
     clear();
-    each(
-        [&](int side, const Seq &, int, int blocks) {
-            atomicAdd(&place[side][bucket(blocks)], 1);
-            mine += (unsigned long long)blocks * (side ? a.hq : a.hkv);
-            most_mine = max(most_mine, blocks);
-        },
-        true);
+    each([&](int side, const Seq &, int, int blocks) {
+        atomicAdd(&place[side][bucket(blocks)], 1);
+        mine += (unsigned long long)blocks * (side ? a.hq : a.hkv);
+        most_mine = max(most_mine, blocks);
+    });
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(kFull, mine, o);
     most_mine = __reduce_max_sync(kFull, most_mine);
@@ -1017,13 +1086,11 @@ __device__ void make_plan(const AttnArgs &a) {
 #pragma unroll 1
         for (int i = threadIdx.x; i < a.slots * kMostWarps; i += THREADS) a.arrived[i] = 0;
         clear();
-        each(
-            [&](int side, const Seq &, int, int blocks) {
-                const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
+        each([&](int side, const Seq &, int, int blocks) {
+            const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
 #pragma unroll 1
-                for (int i = 0; i < n; ++i) atomicAdd(&place[side][bucket(each_has + (i < more))], 1);
-            },
-            false);
+            for (int i = 0; i < n; ++i) atomicAdd(&place[side][bucket(each_has + (i < more))], 1);
+        });
         __syncthreads();
     }
     if (warp < 2) {
@@ -1046,6 +1113,8 @@ __device__ void make_plan(const AttnArgs &a) {
             before += v[i];
         }
         if (lane == 0) {
+            // more than sound offsets can have (or than an int counts)
+            if (all < 0 || all > (warp == 0 ? a.cap_k : a.cap_q)) lost = 1;
             if (warp == 0) {
                 a.plan->next = 0;
                 a.plan->keys = (int)min((int64_t)all, a.cap_k);
@@ -1055,20 +1124,21 @@ __device__ void make_plan(const AttnArgs &a) {
         }
     }
     __syncthreads();
-    each(
-        [&](int side, const Seq &q, int t, int blocks) {
-            const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
-            const int base = n > 1 ? atomicAdd(&slot, n * (side ? a.hq : a.hkv)) : 0;
+    if (lost) {  // the tiles left out keep zeros (sequences that overlap, which is flagged)
+        zero_gradients(a, false, (int)a.total_q, threadIdx.x, THREADS);
+        zero_gradients(a, true, (int)a.total_k, threadIdx.x, THREADS);
+    }
+    each([&](int side, const Seq &q, int t, int blocks) {
+        const int n = parts(blocks, longest), each_has = n > 1 ? blocks / n : blocks, more = blocks - n * each_has;
+        const int base = n > 1 ? atomicAdd(&slot, n * (side ? a.hq : a.hkv)) : 0;
 #pragma unroll 1
-            for (int i = 0; i < n; ++i) {
-                const int first = i * each_has + min(i, more), count = each_has + (i < more);
-                const int at = atomicAdd(&place[side][bucket(count)], 1);
-                // more than sound offsets can have
-                if (at >= (side ? a.cap_q : a.cap_k)) return set_status(a.status, DPB_DEV_BAD_LENGTH);
-                (side ? a.tasks_q : a.tasks_k)[at] = Task{q.q0, q.n, q.k0, q.m, t, first, count, n, base, i, {0, 0}};
-            }
-        },
-        false);
+        for (int i = 0; i < n; ++i) {
+            const int first = i * each_has + min(i, more), count = each_has + (i < more);
+            const int at = atomicAdd(&place[side][bucket(count)], 1);
+            if (at < 0 || at >= (side ? a.cap_q : a.cap_k)) return;
+            (side ? a.tasks_q : a.tasks_k)[at] = Task{q.q0, q.n, q.k0, q.m, t, first, count, n, base, i, {0, 0}};
+        }
+    });
 }
 
 // write_rows() of an item. Of one in parts the sums go to memory, and the warp
@@ -1795,6 +1865,7 @@ dpb_status check_rows(const dpb_heads *h, const char *name, int64_t tokens, int 
 dpb_status check_attention(const dpb_attention_config *c) {
     if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
     if (c->dtype != DPB_BF16) return fail(DPB_ERR_UNSUPPORTED, "attention takes bf16 rows");
+    if (c->seqs > 0x7fffff00) return fail(DPB_ERR_UNSUPPORTED, "at most 2^31 - 256 sequences");
     if (c->seqs < 0 || c->total_q < 0 || c->total_k < 0 || c->max_q < 0 || c->max_k < 0)
         return fail(DPB_ERR_INVALID_ARG, "a size is negative");
     if (c->total_q > 0x7fffff00ll || c->total_k > 0x7fffff00ll)
@@ -1811,7 +1882,7 @@ dpb_status check_attention(const dpb_attention_config *c) {
 dpb_status check_offsets(const dpb_attention_config *c, const int32_t *cu_q, const int32_t *cu_k) {
     if ((cu_q == nullptr) != (cu_k == nullptr))
         return fail(DPB_ERR_INVALID_ARG, "cu_q and cu_k must both be given or both be NULL");
-    if (!cu_q && c->seqs != 1) return fail(DPB_ERR_INVALID_ARG, "without offsets there is one sequence");
+    if (!cu_q && c->seqs > 1) return fail(DPB_ERR_INVALID_ARG, "without offsets there is one sequence");
     if (cu_q) {
         DPB_CHECK(need(cu_q, "cu_q", 4));
         DPB_CHECK(need(cu_k, "cu_k", 4));
@@ -1821,7 +1892,7 @@ dpb_status check_offsets(const dpb_attention_config *c, const int32_t *cu_q, con
 
 // The gradient's workspace after the status word: a Plan and its lists, the
 // counts and sums of tiles in parts, delta. Sound offsets give no more than a
-// tile for every 128 tokens and one a sequence.
+// tile for every 128 tokens and one a sequence, and one before and after them.
 struct GradSpace {
     int64_t cap_k, cap_q;
     int slots;
@@ -1829,8 +1900,8 @@ struct GradSpace {
     explicit GradSpace(const dpb_attention_config *c) {
         const int64_t blocks = ((int64_t)std::max(c->max_q, c->max_k) + kRows - 1) / kRows * (c->heads_q / c->heads_kv);
         slots = blocks > kLeast ? kSlots : 0;
-        cap_k = c->total_k / kRows + c->seqs + slots;
-        cap_q = c->total_q / kRows + c->seqs + slots;
+        cap_k = c->total_k / kRows + c->seqs + 2 + slots;
+        cap_q = c->total_q / kRows + c->seqs + 2 + slots;
         plan = kStatusBytes;
         tasks_k = plan + sizeof(Task);
         tasks_q = tasks_k + sizeof(Task) * (size_t)cap_k;
@@ -1914,7 +1985,7 @@ using Grad128 = GradShape<128>;
 
 template <class C>
 cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
-    a.tiles = (int)(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows));
+    a.tiles = (int)std::max<int64_t>(((int64_t)a.max_q + 2 * kRows - 1) / (2 * kRows), 1);
     // With lengths far from the longest most blocks of a grid for it would be
     // empty: where there can be no more than half of it, the blocks count the
     // sequences' own pairs of tiles (64 x 1024, 12 heads of 64, with the longest
@@ -1923,8 +1994,10 @@ cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
     // all go first: 145 us.
     const int64_t most = a.total_q / (2 * kRows) + a.seqs;
     a.close = (int64_t)a.tiles * a.seqs > 2 * most;
-    return launch_blocks<C, attention_forward_kernel<C>, false>(
-        a, (a.close ? most : (int64_t)a.tiles * a.seqs) * a.hq, s);
+    const int64_t items = (a.close ? most : (int64_t)a.tiles * a.seqs) * a.hq, blocks = items + 2 * a.hq;
+    if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    a.items = (int)items;
+    return launch_blocks<C, attention_forward_kernel<C>, false>(a, blocks, s);
 }
 
 template <class C>
@@ -1959,7 +2032,7 @@ dpb_status dpb_attention_forward(const dpb_attention_config *cfg, const dpb_head
                                  const dpb_heads *v, const int32_t *cu_q, const int32_t *cu_k, const dpb_heads *o,
                                  float *lse, void *workspace, size_t workspace_bytes, void *stream) {
     DPB_CHECK(check_attention(cfg));
-    if (cfg->total_q == 0 || cfg->seqs == 0) return DPB_OK;
+    if (cfg->total_q == 0) return DPB_OK;
     DPB_CHECK(check_rows(q, "q", cfg->total_q, cfg->heads_q));
     DPB_CHECK(check_rows(k, "k", cfg->total_k, cfg->heads_kv));
     DPB_CHECK(check_rows(v, "v", cfg->total_k, cfg->heads_kv));
@@ -1986,7 +2059,7 @@ dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_hea
                                   const dpb_heads *grad_k, const dpb_heads *grad_v, void *workspace,
                                   size_t workspace_bytes, void *stream) {
     DPB_CHECK(check_attention(cfg));
-    if (cfg->seqs == 0 || (cfg->total_q == 0 && cfg->total_k == 0)) return DPB_OK;
+    if (cfg->total_q == 0 && cfg->total_k == 0) return DPB_OK;
     DPB_CHECK(check_rows(q, "q", cfg->total_q, cfg->heads_q));
     DPB_CHECK(check_rows(k, "k", cfg->total_k, cfg->heads_kv));
     DPB_CHECK(check_rows(v, "v", cfg->total_k, cfg->heads_kv));

@@ -664,7 +664,8 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=No
     of one packed projection are fine); cu_q, cu_k int32 [sequences + 1] token
     offsets (None: one sequence; cu_k None: as cu_q), max_q, max_k the longest
     sequences' lengths (None: the token count, which only costs empty blocks);
-    scale defaults to D^-1/2. Returns (o [Tq, Hq, D], lse fp32 [Hq, Tq])."""
+    scale defaults to D^-1/2. Returns (o [Tq, Hq, D], lse fp32 [Hq, Tq]); rows
+    that the offsets leave out (padding) have o = 0 and lse = -inf."""
     dev = q.device
     if _away(dev, stream):
         return _elsewhere(attention_forward, stream, dev,
@@ -690,7 +691,8 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
                        max_k: Optional[int] = None, causal: bool = True, scale: Optional[float] = None, grad_q=None,
                        grad_k=None, grad_v=None, workspace=None, stream=None):
     """dpb_attention_backward with the forward's inputs, its o and lse, and the
-    gradient of o. Returns (grad_q, grad_k, grad_v)."""
+    gradient of o. Returns (grad_q, grad_k, grad_v); 0 in rows that the offsets
+    leave out."""
     dev = q.device
     if _away(dev, stream):
         return _elsewhere(attention_backward, stream, dev,

@@ -411,3 +411,95 @@ def test_in_a_cuda_graph(D, nq):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(got[n], w[n]) for n in got)
+
+
+def into_nan(q, k, v, do, cu_q, cu_k, **kw):
+    """Forward and gradient into memory full of NaN."""
+    at = dict(cu_q=torch.tensor(cu_q, dtype=torch.int32, device="cuda"), cu_k=torch.tensor(cu_k, dtype=torch.int32, device="cuda"),
+              **kw)
+
+    def nan(*like):
+        return [torch.full(x.shape, math.nan, dtype=x.dtype, device="cuda") for x in like]
+
+    o, = nan(q)
+    lse = torch.full((q.shape[1], q.shape[0]), math.nan, device="cuda")
+    dpb.attention_forward(q, k, v, **at, out=o, lse=lse)
+    dq, dk, dv = nan(q, k, v)
+    dpb.attention_backward(q, k, v, o, lse, do, **at, grad_q=dq, grad_k=dk, grad_v=dv)
+    torch.cuda.synchronize()
+    return {"o": o, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
+
+
+def gaps(x, cu, fill, dim=0):
+    """x with `fill` outside of [cu[0], cu[-1])."""
+    x = x.clone()
+    x.narrow(dim, 0, cu[0]).fill_(fill)
+    x.narrow(dim, cu[-1], x.shape[dim] - cu[-1]).fill_(fill)
+    return x
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("before,nq,after", [(0, [130, 60], 70), (40, [130, 0, 257], 0), (300, [5], 5000), (1, [900, 1, 300], 1),
+                                             (129, [], 300)])
+def test_rows_outside_of_every_sequence(before, nq, after, D):
+    """Padding before and after the sequences, of other sizes for the keys: zeros, lse -inf, no gradient, no flag, and the
+    sequences' own results bit for bit those without padding, whatever the padding holds."""
+    kb, ka = (7 * before) % 400, (3 * after) % 700
+    q, k, v, do = draw([before, sum(nq), after], [kb, sum(nq), ka], 4, 2, D, seed=21, packed=False)
+    for x, b, a in ((q, before, after), (k, kb, ka), (v, kb, ka), (do, before, after)):
+        x[:b], x[x.shape[0] - a:] = math.nan, math.inf
+    cq = [before + sum(nq[:i]) for i in range(len(nq) + 1)]
+    ck = [kb + sum(nq[:i]) for i in range(len(nq) + 1)]
+    got = into_nan(q, k, v, do, cq, ck, max_q=max(nq, default=0), max_k=max(nq, default=0))
+    assert dpb.status() == 0
+    for n, x in got.items():
+        cu, fill, dim = ck if n in ("dk", "dv") else cq, -math.inf if n == "lse" else 0.0, 1 if n == "lse" else 0
+        assert torch.equal(x, gaps(x, cu, fill, dim)), n
+    if nq:
+        sq, sk = slice(cq[0], cq[-1]), slice(ck[0], ck[-1])
+        alone = run(q[sq], k[sk], v[sk], do[sq], nq, nq)
+        for n, x in alone.items():
+            assert torch.equal(x, got[n][:, sq] if n == "lse" else got[n][sk if n in ("dk", "dv") else sq]), n
+
+
+@pytest.mark.parametrize("cu,longest,sound", [
+    ([0, 50, 130, 120], 120, [(0, 50)]),            # an end beyond the last row, then a step back
+    ([-3, 50, 90, 120], 120, [(50, 90), (90, 120)]),
+    ([0, 50, 120, 121], 120, [(0, 50), (50, 120)]),
+    ([0, 30, 110, 120], 40, [(0, 30), (110, 120)]),  # longer than announced
+    ([30, 10, 20], 120, [(10, 20)]),
+    ([90, 100, 20, 45, 5, 10], 120, [(90, 100), (20, 45), (5, 10)]),
+    ([500, 700], 120, []), ([-9, -5], 120, []), ([200], 120, []),
+])
+def test_rows_of_skipped_sequences(cu, longest, sound):
+    q, k, v, do = draw([120], [120], 2, 2, 64, seed=22)
+    dpb.status()
+    got = into_nan(q, k, v, do, cu, cu, max_q=longest, max_k=longest)
+    assert dpb.status() == (dpb.DEV_BAD_LENGTH if len(sound) < len(cu) - 1 else 0)
+    want = {n: torch.full_like(x, -math.inf if n == "lse" else 0.0) for n, x in got.items()}
+    for a, b in sound:
+        one = run(q[a:b], k[a:b], v[a:b], do[a:b], [b - a], [b - a])
+        for n, x in one.items():
+            (want[n][:, a:b] if n == "lse" else want[n][a:b]).copy_(x)
+    # rows of a sound sequence that the way to another offset passes as well may hold zeros
+    both = torch.zeros(120, dtype=torch.bool, device="cuda")
+    for a, b in zip([0] + cu, cu + [120]):
+        if (a, b) not in sound and max(a, 0) < min(b, 120):
+            both[max(a, 0):min(b, 120)] = True
+    for n in got:
+        x, w = (t.transpose(0, 1) if n == "lse" else t for t in (got[n], want[n]))
+        zero = torch.full_like(x, -math.inf if n == "lse" else 0.0)
+        same, none = ((x == t).flatten(1).all(1) for t in (w, zero))
+        assert bool((same | (none & both)).all()), n
+
+
+def test_overlapping_sequences_leave_no_row_out():
+    """The same rows given over and over: more pairs of tiles than sound offsets can have."""
+    T = 4096
+    q, k, v, do = draw([T], [T], 2, 1, 64, seed=23)
+    dpb.status()
+    got = into_nan(q, k, v, do, [0, T] * 8, [0, T] * 8, max_q=T, max_k=T)
+    assert dpb.status() == dpb.DEV_BAD_LENGTH
+    one = run(q, k, v, do, [T], [T])
+    assert torch.equal(got["o"], one["o"]) and torch.equal(got["lse"], one["lse"])
+    assert all(torch.isfinite(x).all() for n, x in got.items())

@@ -154,3 +154,32 @@ def test_default_model_is_as_before():
     for kw in (dict(attention="other"), dict(kv_heads=2)):
         with pytest.raises(ValueError):
             ParityTransformer(layers=1, d=64, heads=4, d_mlp=128, vocab=97, context=32, **kw)
+
+
+def test_padding_takes_no_part_in_the_gradients():
+    """A packed batch that ends in padding, in memory that held NaN before: outputs and every parameter's gradient are those
+    of the batch without it (its sums in another order: fp32 sums of bf16 products, then one rounding to bf16)."""
+    from paper_2607_20652_gb300.attention import Attention
+    torch.manual_seed(5)
+    m = Attention(256, 4, 2, context=256, device="cuda", dtype=torch.bfloat16)
+    x = torch.randn(700, 256, device="cuda").bfloat16()
+    gy = torch.randn(700, 256, device="cuda").bfloat16()
+    cu = torch.tensor([0, 100, 300, 410], dtype=torch.int32, device="cuda")
+
+    def grads(rows):
+        torch.cuda.empty_cache()
+        poison = [torch.full((700, 1024), float("nan"), device="cuda", dtype=torch.bfloat16) for _ in range(20)]
+        del poison
+        m.zero_grad(set_to_none=True)
+        xr = x[:rows].clone().requires_grad_()
+        y = m(xr, cu, 200)
+        y.backward(gy[:rows])
+        return y.detach(), xr.grad, {n: p.grad for n, p in m.named_parameters()}
+
+    y, gx, gw = grads(700)
+    y0, gx0, gw0 = grads(410)
+    assert not y[410:].any() and not gx[410:].any()
+    assert torch.equal(gx[:410], gx0) and torch.equal(y[:410], y0)
+    for n, g in gw.items():
+        assert float((g.double() - gw0[n].double()).abs().max()) <= 2.0 ** -7 * float(gw0[n].abs().max()), n
+    assert dpb.status() == 0

@@ -436,7 +436,8 @@ __global__ void __launch_bounds__(32 * kWarps, VEC == 4 ? kBlocksGrad : 1) norm_
                     }
                     if (g.normalise) {
                         const float x2 = group_sum<GL>(total(ss), gl), ux = group_sum<GL>(total(sp), gl);
-                        const float r = rsqrtf(x2 * inv_d + g.eps);
+                        // a lane group without a head adds 0 x r: r must not be infinite there, whatever eps
+                        const float r = rsqrtf((h < in.n ? x2 : 1.f) * inv_d + g.eps);
                         const Vals<VEC> r4 = all<VEC>(r), f4 = all<VEC>(-r * r * r * ux * inv_d);
 #pragma unroll
                         for (int j = 0; j < UPL; ++j) {

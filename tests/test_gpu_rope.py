@@ -211,3 +211,24 @@ def test_refusals():
         x = torch.zeros((6, 2, D), device="cuda")
         with pytest.raises(dpb.DPBError):
             dpb.qk_norm_rope(x, x)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,Hk,D", [(5, 2, 64), (3, 1, 128), (4, 4, 16), (1, 7, 24), (33, 2, 8)])
+def test_without_eps(H, Hk, D, dtype):
+    """eps = 0 with head counts that leave lane groups of a warp without a head: the formula's gradients, all finite."""
+    T = 40
+    q, k, w, cos, sin, pos, gy = draw(T, H, Hk, D, D, dtype, seed=31)
+    at = dict(weight_q=w[0], weight_k=w[1], cos=cos, sin=sin, positions=pos, eps=0.0)
+    y, dx = dpb.qk_norm_rope(q, k, **at), dpb.qk_norm_rope_backward(q, k, *gy, **at)
+    for i, x in enumerate((q, k)):
+        xd, wd = x.double().requires_grad_(), w[i].double().requires_grad_()
+        r = torch.rsqrt((xd * xd).mean(-1, keepdim=True))
+        want = formula(xd * r * wd, None, cos, sin, pos, D, False, normalise=False)
+        close(y[i], want.detach(), (xd * r * wd).detach().abs().amax(-1, keepdim=True) * 2, D)
+        gx, gw = torch.autograd.grad(want, (xd, wd), gy[i].double())
+        n, r = (xd * r).detach().abs(), r.detach()
+        u = 2 * gy[i].double().abs().amax(-1, keepdim=True) * wd.detach().abs().amax()
+        close(dx[i], gx, r * (u + n * (u * n).mean(-1, keepdim=True)), D, extra=2)
+        close(dx[2 + i], gw, (2 * gy[i].double().abs().amax(-1, keepdim=True) * n).sum((0, 1)), D, extra=T * (H, Hk)[i] / D + 2)
+        assert torch.isfinite(dx[2 + i]).all()

@@ -344,6 +344,16 @@ dpb_status dpb_debug_set_wait_limit(int32_t tries);
  * sequence is treated as empty, the token's rotation is left out. */
 #define DPB_DEV_BAD_LENGTH 0x10
 
+/* Where the bits of dpb_qk_norm_rope, dpb_attention_forward and their gradients
+ * go, by the status_slot of their configs. 0: to the workspace's first word, which
+ * the caller has zeroed once. 1 .. DPB_STATUS_SLOTS: to the library's own word of
+ * that number on the current device, which starts at 0 and outlives every buffer;
+ * the workspace is then scratch of that call alone and may hold anything, and the
+ * forward calls need none (NULL, 0). dpb_status_word gives the word's address, to
+ * be read and cleared with dpb_workspace_status. */
+#define DPB_STATUS_SLOTS 256
+dpb_status dpb_status_word(int32_t slot, void **word);
+
 /* Head rows [tokens][heads][head_dim]: element (t, h, i) lies at
  * data + t * token_stride + h * head_stride + i (strides in elements), so the
  * parts of one packed projection can be passed without a copy. */
@@ -380,7 +390,7 @@ typedef struct dpb_rope_config {
     int32_t heads_q, heads_k, head_dim, rot_dim;
     int32_t interleaved, normalise, positions_n, dtype;
     float eps;
-    int32_t reserved; /* 0 */
+    int32_t status_slot;
 } dpb_rope_config;
 
 dpb_status dpb_qk_norm_rope(const dpb_rope_config *cfg, const dpb_heads *q, const dpb_heads *k,
@@ -404,7 +414,9 @@ dpb_status dpb_qk_norm_rope_backward(const dpb_rope_config *cfg, const dpb_heads
                                      const dpb_heads *grad_k, float *grad_weight_q, float *grad_weight_k,
                                      void *workspace, size_t workspace_bytes, void *stream);
 
-/* Workspace bytes of the two calls above (256-byte aligned, zeroed once). */
+/* Workspace bytes of the two calls above (256-byte aligned; zeroed once, unless
+ * status_slot says otherwise). Calls that may run at the same time, or be
+ * enqueued by different threads, need workspaces of their own. */
 dpb_status dpb_rope_workspace_size(const dpb_rope_config *cfg, size_t *bytes);
 
 /*
@@ -441,7 +453,7 @@ typedef struct dpb_attention_config {
     int32_t heads_q, heads_kv, head_dim;
     int32_t causal, dtype;
     float scale;
-    int32_t reserved; /* 0 */
+    int32_t status_slot;
 } dpb_attention_config;
 
 dpb_status dpb_attention_forward(const dpb_attention_config *cfg, const dpb_heads *q, const dpb_heads *k,
@@ -464,7 +476,9 @@ dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_hea
                                   const dpb_heads *grad_q, const dpb_heads *grad_k, const dpb_heads *grad_v,
                                   void *workspace, size_t workspace_bytes, void *stream);
 
-/* Workspace bytes of the two calls above (256-byte aligned, zeroed once). */
+/* Workspace bytes of the two calls above (256-byte aligned; zeroed once, unless
+ * status_slot says otherwise). Calls that may run at the same time, or be
+ * enqueued by different threads, need workspaces of their own. */
 dpb_status dpb_attention_workspace_size(const dpb_attention_config *cfg, size_t *bytes);
 
 /*

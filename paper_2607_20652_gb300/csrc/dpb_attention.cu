@@ -1874,6 +1874,7 @@ dpb_status check_attention(const dpb_attention_config *c) {
         return fail(DPB_ERR_INVALID_ARG, "heads_q must be a positive multiple of heads_kv");
     if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8)
         return fail(DPB_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 in [8, 128]");
+    DPB_CHECK(check_slot(c->status_slot));
     if (!(c->scale > 0.f) || !std::isfinite(c->scale))
         return fail(DPB_ERR_INVALID_ARG, "scale must be positive and finite");
     return DPB_OK;
@@ -1913,7 +1914,7 @@ struct GradSpace {
 };
 size_t attention_workspace(const dpb_attention_config *c) { return GradSpace(c).bytes; }
 
-void fill_args(AttnArgs &a, const dpb_attention_config *c, const int32_t *cu_q, const int32_t *cu_k, void *ws) {
+void fill_args(AttnArgs &a, const dpb_attention_config *c, const int32_t *cu_q, const int32_t *cu_k) {
     a.cu_q = cu_q;
     a.cu_k = cu_k;
     a.total_q = c->total_q;
@@ -1928,7 +1929,6 @@ void fill_args(AttnArgs &a, const dpb_attention_config *c, const int32_t *cu_q, 
     a.causal = c->causal != 0;
     a.scale = c->scale;
     a.scale2 = c->scale * kLog2e;
-    a.status = static_cast<int32_t *>(ws);
 }
 
 In in_rows(const dpb_heads *h) { return h ? In{static_cast<const bf16 *>(h->data), h->token_stride, h->head_stride} : In{}; }
@@ -2039,9 +2039,9 @@ dpb_status dpb_attention_forward(const dpb_attention_config *cfg, const dpb_head
     DPB_CHECK(check_rows(o, "o", cfg->total_q, cfg->heads_q));
     DPB_CHECK(check_offsets(cfg, cu_q, cu_k));
     DPB_CHECK(need(lse, "lse", 4));
-    DPB_CHECK(need_workspace(workspace, workspace_bytes, kStatusBytes));
     AttnArgs a{};
-    fill_args(a, cfg, cu_q, cu_k, workspace);
+    DPB_CHECK(place_status(cfg->status_slot, workspace, workspace_bytes, kStatusBytes, &a.status));
+    fill_args(a, cfg, cu_q, cu_k);
     const bool small = cfg->head_dim <= 64;
     DPB_CHECK(make_map(&a.q, q, cfg->total_q, cfg->heads_q, cfg->head_dim, kRows));
     DPB_CHECK(make_map(&a.k, k, cfg->total_k, cfg->heads_kv, cfg->head_dim, small ? Fwd64::BN : Fwd128::BN));
@@ -2070,9 +2070,9 @@ dpb_status dpb_attention_backward(const dpb_attention_config *cfg, const dpb_hea
     DPB_CHECK(check_rows(grad_v, "grad_v", cfg->total_k, cfg->heads_kv));
     DPB_CHECK(check_offsets(cfg, cu_q, cu_k));
     if (cfg->total_q > 0) DPB_CHECK(need(lse, "lse", 4));
-    DPB_CHECK(need_workspace(workspace, workspace_bytes, attention_workspace(cfg)));
     AttnArgs a{};
-    fill_args(a, cfg, cu_q, cu_k, workspace);
+    DPB_CHECK(place_status(cfg->status_slot, workspace, workspace_bytes, attention_workspace(cfg), &a.status));
+    fill_args(a, cfg, cu_q, cu_k);
     const GradSpace space(cfg);
     char *ws = static_cast<char *>(workspace);
     a.cap_k = space.cap_k, a.cap_q = space.cap_q, a.slots = space.slots;

@@ -1,6 +1,7 @@
 // dpb_capi.cu -- the extern "C" entry points of include/dpb.h: argument
 // validation on the host, then one kernel launch per call on the caller's
 // stream. No allocation happens in encode/decode/backward.
+#include <atomic>
 #include <cstdint>
 #include <cstring>
 #include <map>
@@ -30,6 +31,27 @@ cudaError_t allow_smem(const void *func, size_t bytes) {
     else
         cudaGetLastError();  // returned to the caller: not left for its next CUDA check
     return e;
+}
+
+// A word every 256 bytes. Device memory of the library's image: it needs no
+// allocation (which a stream capture would not allow) and is never freed.
+__device__ int32_t status_words[DPB_STATUS_SLOTS][64];
+
+int32_t *status_word(int32_t slot) {
+    constexpr int kDevices = 64;
+    static std::atomic<int32_t *> base[kDevices];
+    int dev = 0;
+    if (slot < 1 || slot > DPB_STATUS_SLOTS || cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return nullptr;
+    int32_t *p = base[dev].load(std::memory_order_acquire);
+    if (!p) {
+        void *at = nullptr;
+        if (cudaGetSymbolAddress(&at, status_words) != cudaSuccess) {
+            cudaGetLastError();
+            return nullptr;
+        }
+        base[dev].store(p = static_cast<int32_t *>(at), std::memory_order_release);
+    }
+    return p + 64 * (slot - 1);
 }
 
 int best_warps(const void *func, int max_warps, size_t per_block, size_t per_warp) {
@@ -357,6 +379,14 @@ dpb_status dpb_workspace_status(const void *workspace, int clear, int32_t *statu
     }
     *status_out = v;
     return v ? dpb::fail(DPB_ERR_DEVICE, "device status 0x%x", v) : DPB_OK;
+}
+
+dpb_status dpb_status_word(int32_t slot, void **word) {
+    if (!word) return dpb::fail(DPB_ERR_INVALID_ARG, "word is NULL");
+    if (slot < 1 || slot > DPB_STATUS_SLOTS)
+        return dpb::fail(DPB_ERR_INVALID_ARG, "slot must lie in [1, %d]", DPB_STATUS_SLOTS);
+    *word = dpb::status_word(slot);
+    return *word ? DPB_OK : dpb::fail(DPB_ERR_CUDA, "no status word %d on this device", slot);
 }
 
 const char *dpb_status_string(dpb_status s) {

@@ -23,6 +23,21 @@ inline dpb_status need_workspace(const void *ws, size_t bytes, size_t want) {
     return DPB_OK;
 }
 
+// Where a call's device bits go (status_slot), and the workspace that it needs
+// for them and for its scratch.
+inline dpb_status place_status(int32_t slot, void *ws, size_t bytes, size_t want, int32_t **status) {
+    if (slot == 0 || want > kStatusBytes) {
+        const dpb_status s = need_workspace(ws, bytes, want);
+        if (s != DPB_OK) return s;
+    }
+    *status = slot == 0 ? static_cast<int32_t *>(ws) : status_word(slot);
+    return *status ? DPB_OK : fail(DPB_ERR_CUDA, "no status word %d on this device", slot);
+}
+inline dpb_status check_slot(int32_t slot) {
+    if (slot < 0 || slot > DPB_STATUS_SLOTS) return fail(DPB_ERR_INVALID_ARG, "status_slot must lie in [0, %d]", DPB_STATUS_SLOTS);
+    return DPB_OK;
+}
+
 // A failed launch is reported through the returned status; the runtime's
 // last-error slot is cleared so that the caller's next CUDA check does not
 // see it again.

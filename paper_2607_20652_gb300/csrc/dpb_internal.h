@@ -97,6 +97,9 @@ constexpr size_t kMaxSmemPerBlock = 227 * 1024;
 // default (and again only when a later launch needs more), so repeated
 // launches make no driver call; returns the error of a failed set.
 cudaError_t allow_smem(const void *func, size_t bytes);
+// The library's status word `slot` (1 .. DPB_STATUS_SLOTS) on the current device,
+// or nullptr.
+int32_t *status_word(int32_t slot);
 
 // The warps per block (1..max_warps) that put the most warps of kernel
 // `func` on an SM of the current device, by the occupancy calculator, when a

@@ -527,6 +527,7 @@ dpb_status check_config(const dpb_rope_config *c) {
         return fail(DPB_ERR_INVALID_ARG, "rot_dim must be even, in [0, head_dim]");
     if (c->rot_dim > 0 && c->positions_n < 1) return fail(DPB_ERR_INVALID_ARG, "positions_n must be at least 1");
     if (c->dtype != DPB_F32 && c->dtype != DPB_BF16) return fail(DPB_ERR_INVALID_ARG, "unknown dtype %d", c->dtype);
+    DPB_CHECK(check_slot(c->status_slot));
     if (c->normalise && !(c->eps >= 0.f)) return fail(DPB_ERR_INVALID_ARG, "eps must not be negative");
     return DPB_OK;
 }
@@ -563,7 +564,7 @@ dpb_status make_call(const dpb_rope_config *c, const dpb_heads *q, const dpb_hea
     if (wq) DPB_CHECK(need(wq, "weight_q", e));
     if (wk) DPB_CHECK(need(wk, "weight_k", e));
     if (pos) DPB_CHECK(need(pos, "positions", 4));
-    DPB_CHECK(need_workspace(ws, ws_bytes, backward ? rope_workspace(c) : kStatusBytes));
+    DPB_CHECK(place_status(c->status_slot, ws, ws_bytes, backward ? rope_workspace(c) : kStatusBytes, &a.status));
     a.wq = wq;
     a.wk = wk;
     a.cos_tab = ct;
@@ -576,7 +577,6 @@ dpb_status make_call(const dpb_rope_config *c, const dpb_heads *q, const dpb_hea
     a.interleaved = c->interleaved != 0;
     a.normalise = c->normalise != 0;
     a.eps = c->eps;
-    a.status = static_cast<int32_t *>(ws);
     out->four = c->head_dim % 8 == 0 && c->rot_dim % 8 == 0 && is_aligned(ct, 16) && is_aligned(st, 16) &&
                 is_aligned(wq, 4 * e) && is_aligned(wk, 4 * e);
     const Heads *all[] = {&a.q, &a.k, &a.gq, &a.gk, &a.oq, &a.ok};

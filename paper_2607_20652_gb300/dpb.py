@@ -97,7 +97,7 @@ _lib = None
 EXPORTS = ("dpb_plan_create", "dpb_plan_destroy", "dpb_plan_config", "dpb_plan_tables",
            "dpb_code_length", "dpb_workspace_size", "dpb_encode", "dpb_decode", "dpb_backward",
            "dpb_workspace_status", "dpb_status_string", "dpb_last_error", "dpb_encode_noalloc",
-           "dpb_stats_accumulate", "dpb_stats_update", "dpb_forward", "dpb_debug_set_wait_limit",
+           "dpb_stats_accumulate", "dpb_stats_update", "dpb_forward", "dpb_debug_set_wait_limit", "dpb_status_word",
            "dpb_qk_norm_rope", "dpb_qk_norm_rope_backward", "dpb_rope_workspace_size",
            "dpb_attention_forward", "dpb_attention_backward", "dpb_attention_workspace_size", "dpb_adamw_step")
 
@@ -130,6 +130,7 @@ def load(path: Optional[str] = None):
     lib.dpb_workspace_status.argtypes = [vp, ctypes.c_int, ctypes.POINTER(ctypes.c_int32), vp]
     lib.dpb_encode_noalloc.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, vp, vp]
     lib.dpb_debug_set_wait_limit.argtypes = [ctypes.c_int32]
+    lib.dpb_status_word.argtypes = [ctypes.c_int32, ctypes.POINTER(vp)]
     lib.dpb_stats_accumulate.argtypes = [vp, vp, i64, vp, vp, vp, ctypes.c_int32, vp, vp, sz, vp]
     lib.dpb_stats_update.argtypes = [vp, vp, ctypes.c_float, vp, vp, vp]
     lib.dpb_forward.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -449,7 +450,10 @@ def workspace_status(workspace: torch.Tensor, clear: bool = False, stream=None) 
 
 # ---- the training step around the bottleneck -------------------------------
 
-_shared_ws: dict = {}
+STATUS_SLOTS, _GRAPH_SLOT = 256, 1
+_slots: dict = {}  # (device, stream): number of the library's status word
+_slots_lock = threading.Lock()
+_captured: set = set()  # devices with calls in graphs
 
 
 def _elsewhere(call, stream, device, args, kw):
@@ -476,25 +480,38 @@ def _raw_stream(device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
-def _shared_workspace(nbytes: int, device, stream: int) -> torch.Tensor:
-    """The workspace of the calls below made without one: one per (device,
-    stream), grown as needed; its status bits accumulate until read (status())."""
-    ws = _shared_ws.get((device.index, stream))
-    if ws is None or ws.numel() < nbytes:
-        new = torch.zeros(nbytes, dtype=torch.uint8, device=device)
-        if ws is not None:
-            new[:256].copy_(ws[:256])
-        ws = _shared_ws[(device.index, stream)] = new
-    return ws
+def _status_slot(device, stream: int) -> int:
+    """The library's status word for calls made without a workspace: one for
+    each (device, stream), and one for all calls captured into graphs, whose
+    replays may run anywhere. The words outlive streams and graphs."""
+    if torch._C._cuda_isCurrentStreamCapturing():
+        _captured.add(device.index)
+        return _GRAPH_SLOT
+    slot = _slots.get((device.index, stream))
+    if slot is None:
+        with _slots_lock:
+            used = sum(d == device.index for d, _ in _slots)
+            slot = _slots.setdefault((device.index, stream), min(_GRAPH_SLOT + 1 + used, STATUS_SLOTS))
+    return slot
 
 
 def status(device=None, stream=None, clear: bool = True) -> int:
     """The DPB_DEV_* bits that the calls below, made without a workspace, left
-    on ``stream`` (synchronises it); cleared by default."""
+    on ``stream`` (synchronises it), and those of such calls in graphs
+    replayed so far on the device; cleared by default."""
     dev = torch.device(device or "cuda")
     s = stream if stream is not None else torch.cuda.current_stream(dev)
-    ws = _shared_ws.get((dev.index if dev.index is not None else torch.cuda.current_device(), s.cuda_stream))
-    return 0 if ws is None else workspace_status(ws, clear=clear, stream=s)
+    index = dev.index if dev.index is not None else torch.cuda.current_device()
+    lib, bits = load(), 0
+    with torch.cuda.device(index):
+        for slot in (_slots.get((index, s.cuda_stream)), _GRAPH_SLOT if index in _captured else None):
+            if slot is not None:
+                word, v = ctypes.c_void_p(), ctypes.c_int32()
+                _check(lib.dpb_status_word(slot, word))
+                rc = lib.dpb_workspace_status(word, int(clear), v, _stream(s))
+                _check(0 if rc == 6 else rc)  # 6: there are bits
+                bits |= v.value
+    return bits
 
 
 def _head_rows(t: torch.Tensor, name: str, dtype, shape, device):
@@ -552,7 +569,7 @@ def rope_tables(positions: int, rot_dim: int, base: float = 10000.0, scaling: Op
     return cos.to(device or "cuda"), sin.to(device or "cuda")
 
 
-def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise):
+def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise, slot):
     """Writes the config; addresses of the weights, tables and positions."""
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [tokens, heads, dim]")
@@ -573,7 +590,7 @@ def _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved
           _dense(cos, "cos", torch.float32, rows * rot // 2, dev), _dense(sin, "sin", torch.float32, rows * rot // 2, dev),
           _dense(positions, "positions", torch.int32, T, dev))
     _ROPE.pack_into(_arguments.buf, 0, T, hq, k.shape[1], D, rot, bool(interleaved), bool(normalise), rows,
-                    BF16 if dt is torch.bfloat16 else F32, eps, 0)
+                    BF16 if dt is torch.bfloat16 else F32, eps, slot)
     return at
 
 
@@ -588,15 +605,17 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, weight_q=None, weight_k=None,
     if _away(dev, stream):
         return _elsewhere(qk_norm_rope, stream, dev, (q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved,
                                                       normalise, q_out, k_out, workspace), {})
-    at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
-    dt, sq, sk, s, a = q.dtype, q.shape, k.shape, _raw_stream(dev), _arguments
+    s = _raw_stream(dev)
+    at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise,
+                      _status_slot(dev, s) if workspace is None else 0)
+    dt, sq, sk, a = q.dtype, q.shape, k.shape, _arguments
     q_out = torch.empty(sq, dtype=dt, device=dev) if q_out is None else q_out
     k_out = torch.empty(sk, dtype=dt, device=dev) if k_out is None else k_out
-    ws = _shared_workspace(256, dev, s) if workspace is None else workspace
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _ROWS[4].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(q_out, "q_out", dt, sq, dev), *_head_rows(k_out, "k_out", dt, sk, dev))
     h = a.rows
-    _check(load().dpb_qk_norm_rope(a.at, h, h + 24, *at, h + 48, h + 72, ws.data_ptr(), ws.nbytes, s))
+    _check(load().dpb_qk_norm_rope(a.at, h, h + 24, *at, h + 48, h + 72, ws, ws_bytes, s))
     return q_out, k_out
 
 
@@ -612,8 +631,10 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Te
         return _elsewhere(qk_norm_rope_backward, stream, dev,
                           (q, k, grad_q_out, grad_k_out, weight_q, weight_k, cos, sin, positions, eps, interleaved,
                            normalise, weight_grads, grad_q, grad_k, workspace), {})
-    at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise)
-    lib, dt, sq, sk, s, a = load(), q.dtype, q.shape, k.shape, _raw_stream(dev), _arguments
+    s = _raw_stream(dev)
+    at = _rope_config(q, k, weight_q, weight_k, cos, sin, positions, eps, interleaved, normalise,
+                      _status_slot(dev, s) if workspace is None else 0)
+    lib, dt, sq, sk, a = load(), q.dtype, q.shape, k.shape, _arguments
     grad_q = torch.empty(sq, dtype=dt, device=dev) if grad_q is None else grad_q
     grad_k = torch.empty(sk, dtype=dt, device=dev) if grad_k is None else grad_k
     D = sq[2]
@@ -622,7 +643,7 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Te
     if workspace is None:
         n = ctypes.c_size_t()
         _check(lib.dpb_rope_workspace_size(a.at, n))
-        workspace = _shared_workspace(n.value, dev, s)
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)  # scratch of this call
     _ROWS[6].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(grad_q_out, "grad_q_out", dt, sq, dev),
                        *_head_rows(grad_k_out, "grad_k_out", dt, sk, dev),
@@ -633,7 +654,7 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Te
     return (grad_q, grad_k) + ((None, None) if gw is None else (gw[0], gw[1]))
 
 
-def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
+def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, slot):
     """Writes the config; addresses of the offsets."""
     if q.dim() != 3 or k.dim() != 3 or q.dtype is not torch.bfloat16:
         raise ValueError(f"q, k and v must be bfloat16 tensors [tokens, heads, dim], got {q.dtype} {list(q.shape)}")
@@ -653,7 +674,7 @@ def _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
     at = (_dense(cu_q, "cu_q", torch.int32, seqs + 1, q.device), _dense(cu_k, "cu_k", torch.int32, seqs + 1, q.device))
     _ATTENTION.pack_into(_arguments.buf, 0, Tq, Tk, seqs, Tq if max_q is None or max_q > Tq else max_q,
                          Tk if max_k is None or max_k > Tk else max_k, Hq, Hk, D, bool(causal), BF16,
-                         D ** -0.5 if scale is None else scale, 0)
+                         D ** -0.5 if scale is None else scale, slot)
     return at
 
 
@@ -670,19 +691,20 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=No
     if _away(dev, stream):
         return _elsewhere(attention_forward, stream, dev,
                           (q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, out, lse, workspace), {})
-    at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
-    dt, sq, s, a = torch.bfloat16, q.shape, _raw_stream(dev), _arguments
+    s = _raw_stream(dev)
+    at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, _status_slot(dev, s) if workspace is None else 0)
+    dt, sq, a = torch.bfloat16, q.shape, _arguments
     sk = k.shape if k.shape[2] == sq[2] else (*k.shape[:2], sq[2])
     if out is None:
         out = torch.empty(sq, dtype=dt, device=dev)
     if lse is None:
         lse = torch.empty((sq[1], sq[0]), dtype=torch.float32, device=dev)
-    ws = _shared_workspace(256, dev, s) if workspace is None else workspace
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _ROWS[4].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(v, "v", dt, sk, dev), *_head_rows(out, "out", dt, sq, dev))
     h = a.rows
     _check(load().dpb_attention_forward(a.at, h, h + 24, h + 48, *at, h + 72,
-                                        _dense(lse, "lse", torch.float32, sq[0] * sq[1], dev), ws.data_ptr(), ws.nbytes, s))
+                                        _dense(lse, "lse", torch.float32, sq[0] * sq[1], dev), ws, ws_bytes, s))
     return out, lse
 
 
@@ -698,8 +720,9 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
         return _elsewhere(attention_backward, stream, dev,
                           (q, k, v, o, lse, grad_o, cu_q, cu_k, max_q, max_k, causal, scale, grad_q, grad_k, grad_v,
                            workspace), {})
-    at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale)
-    lib, dt, sq, s, a = load(), torch.bfloat16, q.shape, _raw_stream(dev), _arguments
+    s = _raw_stream(dev)
+    at = _attention_config(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, _status_slot(dev, s) if workspace is None else 0)
+    lib, dt, sq, a = load(), torch.bfloat16, q.shape, _arguments
     sk = k.shape if k.shape[2] == sq[2] else (*k.shape[:2], sq[2])
     grad_q = torch.empty(sq, dtype=dt, device=dev) if grad_q is None else grad_q
     grad_k = torch.empty(sk, dtype=dt, device=dev) if grad_k is None else grad_k
@@ -707,7 +730,7 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
     if workspace is None:
         n = ctypes.c_size_t()
         _check(lib.dpb_attention_workspace_size(a.at, n))
-        workspace = _shared_workspace(n.value, dev, s)
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)  # scratch of this call
     _ROWS[8].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(v, "v", dt, sk, dev), *_head_rows(o, "o", dt, sq, dev),
                        *_head_rows(grad_o, "grad_o", dt, sq, dev), *_head_rows(grad_q, "grad_q", dt, sq, dev),

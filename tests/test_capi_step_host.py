@@ -114,3 +114,36 @@ def test_adamw_refuses_bad_tensors(lib):
         t[i] = bad
         buf = ctypes.create_string_buffer(struct.pack("=6Qq", *t))
         assert lib.dpb_adamw_step(c, ctypes.addressof(buf), 1, None) == INVALID, (i, bad)
+
+
+def test_status_slots(lib):
+    word = ctypes.c_void_p()
+    for slot in (-1, 0, 257):
+        assert lib.dpb_status_word(slot, word) == INVALID
+    assert lib.dpb_status_word(1, None) == INVALID
+    for slot in (-1, 257):
+        assert lib.dpb_attention_workspace_size(at(attention_config(reserved=slot)), ctypes.c_size_t()) == INVALID
+        assert lib.dpb_rope_workspace_size(at(rope_config(reserved=slot)), ctypes.c_size_t()) == INVALID
+    rows = ctypes.create_string_buffer(struct.pack("=Qqq", 256, 256, 64))
+    forward = [at(rows)] * 3 + [None, None, at(rows), 256]
+    # the gradient's scratch is the caller's with any slot, the forward needs a workspace for the status alone
+    assert lib.dpb_attention_forward(at(attention_config()), *forward, None, 0, None) == INVALID
+    assert b"workspace is NULL" in lib.dpb_last_error()
+    backward = [at(rows)] * 4 + [256, at(rows), None, None] + [at(rows)] * 3
+    assert lib.dpb_attention_backward(at(attention_config(reserved=1)), *backward, None, 0, None) == INVALID
+    assert b"workspace is NULL" in lib.dpb_last_error()
+
+
+def test_calls_without_a_workspace_share_no_scratch(monkeypatch):
+    """Each call's scratch is its own: two threads on one stream, or a graph and a later call, cannot meet in it."""
+    assert not hasattr(dpb, "_shared_workspace")
+    monkeypatch.setattr(dpb, "_slots", {})
+    monkeypatch.setattr("torch._C._cuda_isCurrentStreamCapturing", lambda: False, raising=False)
+    import torch
+    one, two = dpb._status_slot(torch.device("cuda", 0), 7), dpb._status_slot(torch.device("cuda", 0), 8)
+    assert one != two and one == dpb._status_slot(torch.device("cuda", 0), 7) and dpb._GRAPH_SLOT not in (one, two)
+    for i in range(300):  # more streams than words: the last is shared
+        assert 1 < dpb._status_slot(torch.device("cuda", 1), i) <= dpb.STATUS_SLOTS
+    monkeypatch.setattr("torch._C._cuda_isCurrentStreamCapturing", lambda: True, raising=False)
+    monkeypatch.setattr(dpb, "_captured", set())
+    assert dpb._status_slot(torch.device("cuda", 0), 7) == dpb._GRAPH_SLOT

@@ -183,3 +183,81 @@ def test_padding_takes_no_part_in_the_gradients():
     for n, g in gw.items():
         assert float((g.double() - gw0[n].double()).abs().max()) <= 2.0 ** -7 * float(gw0[n].abs().max()), n
     assert dpb.status() == 0
+
+
+def test_threads_on_one_stream():
+    """Two threads enqueue gradients of different shapes on one stream: each gets what it gets alone."""
+    import threading
+    g = torch.Generator(device="cuda").manual_seed(7)
+    work = []
+    for lens, h, hk, d in (([900, 33, 500], 4, 2, 64), ([64, 2500, 7, 300], 8, 1, 128)):
+        t = sum(lens)
+        q, k, v, do = (torch.randn(t, n, d, device="cuda", generator=g).bfloat16() for n in (h, hk, hk, h))
+        cu = torch.tensor([0] + lens, device="cuda").cumsum(0).to(torch.int32)
+        cos, sin = dpb.rope_tables(t, d)
+        o, lse = dpb.attention_forward(q, k, v, cu_q=cu, max_q=max(lens))
+
+        def step(q=q, k=k, v=v, do=do, o=o, lse=lse, cu=cu, longest=max(lens), cos=cos, sin=sin):
+            return (*dpb.attention_backward(q, k, v, o, lse, do, cu_q=cu, max_q=longest),
+                    *dpb.qk_norm_rope_backward(q, k, do, k, cos=cos, sin=sin))
+
+        work.append(step)
+    want = [f() for f in work]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def loop(f, w):
+        for _ in range(150):
+            got = f()
+            if not all(torch.equal(a, b) for a, b in zip(got, w)):
+                wrong.append(1)
+
+    threads = [threading.Thread(target=loop, args=(f, w)) for f, w in zip(work, want) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and dpb.status() == 0
+
+
+def test_module_in_a_cuda_graph():
+    """A module's step captured without a workspace of its own; then larger calls on the capture's stream, memory given back
+    and filled with other data, and the replay: the graph's scratch is still its own. Its status bits are found, too."""
+    from paper_2607_20652_gb300.attention import Attention
+    torch.manual_seed(6)
+    m = Attention(256, 4, 2, context=4096, device="cuda", dtype=torch.bfloat16)
+    x = torch.randn(600, 256, device="cuda").bfloat16().requires_grad_()
+    gy = torch.randn(600, 256, device="cuda").bfloat16()
+    cu = torch.tensor([0, 450, 600], dtype=torch.int32, device="cuda")
+
+    def step():
+        y = m(x, cu, 450)
+        return [y, *torch.autograd.grad(y, [x, *m.parameters()], gy)]
+
+    want = [t.detach().clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = step()
+    with torch.cuda.stream(side):
+        big = torch.randn(4000, 256, device="cuda").bfloat16().requires_grad_()
+        z = m(big, torch.tensor([0, 4000], dtype=torch.int32, device="cuda"), 4000)
+        torch.autograd.grad(z, [big, *m.parameters()], torch.ones_like(z))
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    other = [torch.full((1 << 20,), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    for t in got:
+        t.detach().zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(bool((t == 7).all()) for t in other)
+    assert dpb.status() == 0
+    cu.copy_(torch.tensor([0, 700, 600]))
+    graph.replay()
+    assert dpb.status() == dpb.DEV_BAD_LENGTH and dpb.status() == 0

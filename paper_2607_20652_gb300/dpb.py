@@ -786,6 +786,10 @@ class AdamWGroup:
         self._table[:, 6] = self._numel
         self._table_at, self._last = self._table.ctypes.data, (self._table[:, 0].tolist(), None)
 
+    def __reduce__(self):
+        # a copy is made from its own tensors: the table holds addresses
+        return AdamWGroup, (self.params, self.exp_avg, self.exp_avg_sq, *self.scales)
+
     def step(self, grads, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, step: int = 1,
              seed: int = 0, grad_scale: Optional[torch.Tensor] = None, stream=None):
         """dpb_adamw_step: one step of every parameter that has a gradient (None

@@ -257,3 +257,23 @@ def test_8bit_states_follow_the_formula_rounding_by_rounding():
     want = [x.abs().amax(1) * (1 / 448) for x in (m, v.sqrt())]
     group(t, 8).step(t["g"], step=3, seed=5, **H)
     assert torch.equal(t["ms"][0], want[0]) and torch.equal(t["vs"][0], want[1])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_copied_group_steps_its_own_tensors(bits):
+    """A deep copy, and one saved and loaded, hold copies of the tensors: the original's stay as they are."""
+    import copy
+    import io
+    t = tensors([5000, 257], torch.float32, bits, seed=8)
+    grp = group(t, bits)
+    file = io.BytesIO()
+    torch.save(grp, file)
+    file.seek(0)
+    for other in (copy.deepcopy(grp), torch.load(file, weights_only=False)):
+        kinds = lambda x: [y.view(torch.uint8).clone() for ts in (x.params, x.exp_avg, x.exp_avg_sq) for y in ts]
+        before = kinds(grp)
+        other.step(t["g"], step=2, seed=5, **H)
+        assert all(torch.equal(a, b) for a, b in zip(kinds(grp), before))
+        assert not any(torch.equal(a, b) for a, b in zip(kinds(other), before))
+    grp.step(t["g"], step=2, seed=5, **H)
+    assert all(torch.equal(a, b) for a, b in zip(kinds(grp), kinds(other)))

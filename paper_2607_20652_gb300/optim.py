@@ -14,8 +14,9 @@ class AdamW(torch.optim.Optimizer):
     """AdamW with decoupled weight decay over fp32 and bf16 parameters.
 
     ``state_bits`` 32: fp32 moments. 8: e4m3 codes with a scale for each 256
-    values, stored with stochastic rounding drawn from ``seed`` and the step
-    (2 bytes a parameter in place of 8). ``step(grad_scale=...)`` takes a
+    values, stored with stochastic rounding drawn from ``seed`` (kept in the
+    parameter groups, so in state_dict()) and the step (2 bytes a parameter in
+    place of 8). ``step(grad_scale=...)`` takes a
     device tensor that multiplies the gradients; where it is not finite, no
     parameter or state changes (the step still counts)."""
 
@@ -23,10 +24,29 @@ class AdamW(torch.optim.Optimizer):
                  state_bits: int = 32, seed: int = 0):
         if state_bits not in (32, 8):
             raise ValueError("state_bits must be 32 or 8")
-        self.seed = seed
         self._sets: dict = {}
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay,
-                                      state_bits=state_bits))
+                                      state_bits=state_bits, seed=seed))
+
+    def __setstate__(self, state):
+        """Also what load_state_dict, copies and unpickling come through. The
+        launches hold addresses, so they are made anew; a saved state of
+        groups without a seed takes this optimiser's."""
+        super().__setstate__(state)
+        self._sets = {}
+        self.defaults.setdefault("seed", 0)
+        for group in self.param_groups:
+            group.setdefault("seed", self.defaults["seed"])
+
+    @property
+    def seed(self) -> int:
+        return self.param_groups[0]["seed"]
+
+    @seed.setter
+    def seed(self, value: int):
+        self.defaults["seed"] = value
+        for group in self.param_groups:
+            group["seed"] = value
 
     def _new_state(self, p: torch.Tensor, bits: int) -> dict:
         n = p.numel()
@@ -76,7 +96,7 @@ class AdamW(torch.optim.Optimizer):
                 for n in steps:  # one, unless gradients were missing in earlier steps
                     grads = [None if p.grad is None or state[p]["step"] != n else p.grad.contiguous() for p in ps]
                     launch.step(grads, lr=group["lr"], betas=group["betas"], eps=group["eps"],
-                                weight_decay=group["weight_decay"], step=n, seed=self.seed + index,
+                                weight_decay=group["weight_decay"], step=n, seed=group["seed"] + index,
                                 grad_scale=grad_scale)
         return loss
 

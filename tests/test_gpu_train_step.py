@@ -261,3 +261,36 @@ def test_module_in_a_cuda_graph():
     cu.copy_(torch.tensor([0, 700, 600]))
     graph.replay()
     assert dpb.status() == dpb.DEV_BAD_LENGTH and dpb.status() == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_copied_or_resumed_optimiser_goes_on_the_same(bits):
+    """A deep copy of model and optimiser, and a run resumed from saved states by an optimiser built with another seed: the
+    next steps are the original's bit for bit, and the original is not touched by the others' steps."""
+    from paper_2607_20652_gb300.optim import AdamW
+    torch.manual_seed(9)
+    ps = torch.nn.ParameterList([torch.nn.Parameter(torch.randn(n, device="cuda")) for n in (300, 5000)])
+    opt = AdamW(ps.parameters(), lr=1e-2, state_bits=bits, seed=123)
+
+    def steps(params, o, n, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for _ in range(n):
+            for p in params:
+                p.grad = torch.randn(p.shape, generator=g, device="cuda")
+            o.step()
+
+    def held(params, o):
+        return [t.view(torch.uint8).clone() for p in params for t in (p.detach(), o.state[p]["exp_avg"], o.state[p]["exp_avg_sq"])]
+
+    steps(ps, opt, 3, 1)
+    ps2, opt2 = copy.deepcopy((ps, opt))
+    ps3 = torch.nn.ParameterList([torch.nn.Parameter(p.detach().clone()) for p in ps])
+    opt3 = AdamW(ps3.parameters(), lr=1e-2, state_bits=bits, seed=77)
+    opt3.load_state_dict(opt.state_dict())
+    before = held(ps, opt)
+    steps(ps2, opt2, 2, 2)
+    steps(ps3, opt3, 2, 2)
+    assert all(torch.equal(a, b) for a, b in zip(held(ps, opt), before))
+    steps(ps, opt, 2, 2)
+    for params, o in ((ps2, opt2), (ps3, opt3)):
+        assert all(torch.equal(a, b) for a, b in zip(held(ps, opt), held(params, o)))

@@ -794,7 +794,8 @@ class AdamWGroup:
              seed: int = 0, grad_scale: Optional[torch.Tensor] = None, stream=None):
         """dpb_adamw_step: one step of every parameter that has a gradient (None
         leaves it as it is). ``grad_scale``: a float32 tensor of one value that
-        multiplies the gradients; where it is not finite nothing changes."""
+        multiplies the gradients; where it is not finite nothing changes. All
+        numbers are read now: a CUDA graph of this call repeats this step."""
         dt, dev = self.dtype, self.device
         if _away(dev, stream):
             _elsewhere(self.step, stream, dev, (grads, lr, betas, eps, weight_decay, step, seed, grad_scale), {})

@@ -18,7 +18,9 @@ class AdamW(torch.optim.Optimizer):
     parameter groups, so in state_dict()) and the step (2 bytes a parameter in
     place of 8). ``step(grad_scale=...)`` takes a
     device tensor that multiplies the gradients; where it is not finite, no
-    parameter or state changes (the step still counts)."""
+    parameter or state changes (the step still counts). A step's number and
+    what follows from it (bias corrections, random bits) come from the host,
+    so a step cannot be captured into a CUDA graph."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
                  state_bits: int = 32, seed: int = 0):
@@ -82,6 +84,8 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def step(self, closure=None, grad_scale: Optional[torch.Tensor] = None):
+        if torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("AdamW.step() cannot be captured: a replay would repeat this step's bias corrections and bits")
         loss = None
         if closure is not None:
             with torch.enable_grad():

@@ -294,3 +294,23 @@ def test_a_copied_or_resumed_optimiser_goes_on_the_same(bits):
     steps(ps, opt, 2, 2)
     for params, o in ((ps2, opt2), (ps3, opt3)):
         assert all(torch.equal(a, b) for a, b in zip(held(ps, opt), held(params, o)))
+
+
+def test_a_captured_optimiser_step_is_refused():
+    """A replay would repeat one step's bias corrections: refused before anything is counted or launched."""
+    from paper_2607_20652_gb300.optim import AdamW
+    p = torch.nn.Parameter(torch.ones(300, device="cuda"))
+    opt = AdamW([p], lr=1e-2)
+    p.grad = torch.ones_like(p)
+    opt.step()
+    keep = p.detach().clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other = p.detach() + 1
+        with pytest.raises(RuntimeError, match="captured"):
+            opt.step()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert opt.state[p]["step"] == 1 and torch.equal(p.detach(), keep) and torch.equal(other, keep + 1)
+    opt.step()
+    assert opt.state[p]["step"] == 2 and not torch.equal(p.detach(), keep)

@@ -25,3 +25,9 @@ def test_copies_and_saved_states_carry_the_seed():
     late.seed = 6
     late.add_param_group({"params": [torch.nn.Parameter(torch.zeros(2))]})
     assert [g["seed"] for g in late.param_groups] == [6, 6, 6]
+
+
+def test_a_step_without_gradients_needs_no_device():
+    p = torch.nn.Parameter(torch.zeros(4))
+    opt = AdamW([p])
+    assert opt.step(lambda: 3.0) == 3.0 and not opt.state[p]

@@ -6,7 +6,8 @@ described further. ``Attention`` is the drop-in for that place: one packed
 projection, RMS norm of every query and key head, rotary positions (either may
 be turned off), causal attention over the batch's sequences, one output
 projection. Every step between the projections runs in the library's kernels;
-the gradient of the whole projection is written by them into one buffer.
+the gradient of the whole projection is written by them into one buffer. The
+gradients have no gradient of their own: a second differentiation raises.
 """
 from __future__ import annotations
 
@@ -14,6 +15,7 @@ from typing import Optional
 
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 
 from . import dpb
 
@@ -28,6 +30,7 @@ class _AttentionFunction(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, go):
         return (*dpb.attention_backward(*ctx.saved_tensors, go.contiguous(), *ctx.at),) + (None,) * 6
 
@@ -46,6 +49,7 @@ class _NormRopeFunction(torch.autograd.Function):
         return dpb.qk_norm_rope(q, k, wq, wk, cos, sin, positions, *ctx.at)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gq, gk):
         q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
         need = wq is not None and ctx.needs_input_grad[2] or wk is not None and ctx.needs_input_grad[3]
@@ -77,6 +81,7 @@ class _PackedFunction(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, go):
         qkv, q, k, wq, wk, o, lse = ctx.saved_tensors
         hq, hkv, rope = ctx.hq, ctx.hkv, ctx.rope

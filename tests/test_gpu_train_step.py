@@ -314,3 +314,16 @@ def test_a_captured_optimiser_step_is_refused():
     assert opt.state[p]["step"] == 1 and torch.equal(p.detach(), keep) and torch.equal(other, keep + 1)
     opt.step()
     assert opt.state[p]["step"] == 2 and not torch.equal(p.detach(), keep)
+
+
+def test_second_derivatives_are_refused():
+    """A gradient penalty must not lose its term silently."""
+    from paper_2607_20652_gb300 import attention as A
+    m = A.Attention(128, 2, device="cuda", dtype=torch.bfloat16, context=32)
+    q = torch.randn(20, 2, 64, device="cuda").bfloat16().requires_grad_()
+    x = torch.randn(1, 20, 128, device="cuda").bfloat16().requires_grad_()
+    for y, of in ((A.attention(q, q, q), q), (A.qk_norm_rope(q, q)[0], q), (m(x), x)):
+        loss = (y.float() ** 2).sum()
+        g, = torch.autograd.grad(loss, of, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            (loss + (g.float() ** 2).sum()).backward()

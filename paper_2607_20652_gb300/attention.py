@@ -23,16 +23,16 @@ from . import dpb
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
-        at = (cu_q, cu_k, max_q, max_k, causal, scale)
-        o, lse = dpb.attention_forward(q, k, v, *at)
-        ctx.save_for_backward(q, k, v, o, lse)
-        ctx.at = at
+        ctx.at = (max_q, max_k, causal, scale)
+        o, lse = dpb.attention_forward(q, k, v, cu_q, cu_k, *ctx.at)
+        ctx.save_for_backward(q, k, v, o, lse, cu_q, cu_k)  # offsets too: a change in place before the backward raises
         return o
 
     @staticmethod
     @once_differentiable
     def backward(ctx, go):
-        return (*dpb.attention_backward(*ctx.saved_tensors, go.contiguous(), *ctx.at),) + (None,) * 6
+        q, k, v, o, lse, cu_q, cu_k = ctx.saved_tensors
+        return (*dpb.attention_backward(q, k, v, o, lse, go.contiguous(), cu_q, cu_k, *ctx.at),) + (None,) * 6
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, cu_k=None, max_q: Optional[int] = None,
@@ -70,34 +70,33 @@ class _PackedFunction(torch.autograd.Function):
     gradients of q, k and v are written side by side into one buffer."""
 
     @staticmethod
-    def forward(ctx, qkv, hq, hkv, wq, wk, rope, at):
+    def forward(ctx, qkv, hq, hkv, wq, wk, cos, sin, positions, rope, cu, at):
         q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
-        ctx.plain = rope is None
         if rope is not None:
-            q, k = dpb.qk_norm_rope(q, k, wq, wk, **rope)
-        o, lse = dpb.attention_forward(q, k, v, **at)
-        ctx.save_for_backward(qkv, q, k, wq, wk, o, lse)
+            q, k = dpb.qk_norm_rope(q, k, wq, wk, cos, sin, positions, **rope)
+        o, lse = dpb.attention_forward(q, k, v, cu, **at)
+        ctx.save_for_backward(qkv, q, k, wq, wk, cos, sin, positions, cu, o, lse)
         ctx.hq, ctx.hkv, ctx.rope, ctx.at = hq, hkv, rope, at
         return o
 
     @staticmethod
     @once_differentiable
     def backward(ctx, go):
-        qkv, q, k, wq, wk, o, lse = ctx.saved_tensors
+        qkv, q, k, wq, wk, cos, sin, positions, cu, o, lse = ctx.saved_tensors
         hq, hkv, rope = ctx.hq, ctx.hkv, ctx.rope
         grad = torch.empty_like(qkv)
         gq, gk, gv = grad[:, :hq], grad[:, hq:hq + hkv], grad[:, hq + hkv:]
         dwq = dwk = None
         if rope is None:
-            dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, go.contiguous(), grad_q=gq, grad_k=gk, grad_v=gv,
+            dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, go.contiguous(), cu, grad_q=gq, grad_k=gk, grad_v=gv,
                                    **ctx.at)
         else:
-            dq, dk, _ = dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, go.contiguous(), grad_v=gv, **ctx.at)
-            _, _, dwq, dwk = dpb.qk_norm_rope_backward(qkv[:, :hq], qkv[:, hq:hq + hkv], dq, dk, wq, wk, grad_q=gq,
-                                                       grad_k=gk, weight_grads=wq is not None, **rope)
+            dq, dk, _ = dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, go.contiguous(), cu, grad_v=gv, **ctx.at)
+            _, _, dwq, dwk = dpb.qk_norm_rope_backward(qkv[:, :hq], qkv[:, hq:hq + hkv], dq, dk, wq, wk, cos, sin, positions,
+                                                       grad_q=gq, grad_k=gk, weight_grads=wq is not None, **rope)
         if dwq is not None:
             dwq, dwk = dwq.to(wq.dtype), dwk.to(wk.dtype)
-        return grad, None, None, dwq, dwk, None, None
+        return (grad, None, None, dwq, dwk) + (None,) * 6
 
 
 class Attention(nn.Module):
@@ -156,8 +155,8 @@ class Attention(nn.Module):
             raise ValueError(f"sequences of {longest} tokens, rotary tables for {self.context}")
         rope = None
         if self.q_norm is not None or self.cos is not None:
-            rope = dict(cos=self.cos, sin=self.sin, positions=positions, normalise=self.q_norm is not None)
+            rope = dict(normalise=self.q_norm is not None)
         qkv = self.qkv(x).view(-1, self.heads + 2 * self.kv_heads, self.dim)
-        o = _PackedFunction.apply(qkv, self.heads, self.kv_heads, self.q_norm, self.k_norm, rope,
-                                  dict(cu_q=cu, max_q=longest, causal=True))
+        o = _PackedFunction.apply(qkv, self.heads, self.kv_heads, self.q_norm, self.k_norm, self.cos, self.sin, positions, rope,
+                                  cu, dict(max_q=longest, causal=True))
         return self.out(o.reshape(*x.shape[:-1], self.heads * self.dim))

@@ -327,3 +327,21 @@ def test_second_derivatives_are_refused():
         g, = torch.autograd.grad(loss, of, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             (loss + (g.float() ** 2).sum()).backward()
+
+
+def test_offsets_changed_before_the_backward_are_noticed():
+    """Offsets are kept for the backward as the inputs are: changed in place, they raise as an input does."""
+    from paper_2607_20652_gb300 import attention as A
+    torch.manual_seed(3)
+    m = A.Attention(128, 2, device="cuda", dtype=torch.bfloat16, context=128)
+    q = torch.randn(100, 2, 64, device="cuda").bfloat16().requires_grad_()
+    for call in (lambda cu: A.attention(q, q, q, cu, max_q=100), lambda cu: A.attention(q, q, q, cu, cu.clone(), 100, 100),
+                 lambda cu: m(q.flatten(1), cu, 100)):
+        cu = torch.tensor([0, 50, 100], dtype=torch.int32, device="cuda")
+        want, = torch.autograd.grad(call(cu).float().sum(), q)
+        y = call(cu)
+        cu[1] = 30
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.float().sum().backward()
+        cu[1] = 50
+        assert torch.equal(torch.autograd.grad(call(cu).float().sum(), q)[0], want)

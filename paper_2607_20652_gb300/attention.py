@@ -20,6 +20,13 @@ from torch.autograd.function import once_differentiable
 from . import dpb
 
 
+def _dense(g: torch.Tensor) -> torch.Tensor:
+    """An output's gradient as the kernels read it: dense and 16-byte aligned,
+    which a part of a larger gradient need not be."""
+    g = g.contiguous()
+    return g if g.data_ptr() % 16 == 0 else g.clone()
+
+
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
@@ -32,7 +39,7 @@ class _AttentionFunction(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, go):
         q, k, v, o, lse, cu_q, cu_k = ctx.saved_tensors
-        return (*dpb.attention_backward(q, k, v, o, lse, go.contiguous(), cu_q, cu_k, *ctx.at),) + (None,) * 6
+        return (*dpb.attention_backward(q, k, v, o, lse, _dense(go), cu_q, cu_k, *ctx.at),) + (None,) * 6
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, cu_k=None, max_q: Optional[int] = None,
@@ -88,10 +95,10 @@ class _PackedFunction(torch.autograd.Function):
         gq, gk, gv = grad[:, :hq], grad[:, hq:hq + hkv], grad[:, hq + hkv:]
         dwq = dwk = None
         if rope is None:
-            dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, go.contiguous(), cu, grad_q=gq, grad_k=gk, grad_v=gv,
+            dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, _dense(go), cu, grad_q=gq, grad_k=gk, grad_v=gv,
                                    **ctx.at)
         else:
-            dq, dk, _ = dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, go.contiguous(), cu, grad_v=gv, **ctx.at)
+            dq, dk, _ = dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, _dense(go), cu, grad_v=gv, **ctx.at)
             _, _, dwq, dwk = dpb.qk_norm_rope_backward(qkv[:, :hq], qkv[:, hq:hq + hkv], dq, dk, wq, wk, cos, sin, positions,
                                                        grad_q=gq, grad_k=gk, weight_grads=wq is not None, **rope)
         if dwq is not None:

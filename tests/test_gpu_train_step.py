@@ -345,3 +345,15 @@ def test_offsets_changed_before_the_backward_are_noticed():
             y.float().sum().backward()
         cu[1] = 50
         assert torch.equal(torch.autograd.grad(call(cu).float().sum(), q)[0], want)
+
+
+def test_a_gradient_at_any_address():
+    """An output that is one part of a longer vector gets its gradient as a part of that vector's, at an address that no vector
+    load takes."""
+    from paper_2607_20652_gb300 import attention as A
+    torch.manual_seed(4)
+    q = torch.randn(20, 2, 64, device="cuda").bfloat16().requires_grad_()
+    gy = torch.randn(3 + 20 * 128, device="cuda").bfloat16()
+    odd, = torch.autograd.grad(torch.cat([gy[:3], A.attention(q, q, q).flatten()]), q, gy)
+    want, = torch.autograd.grad(A.attention(q, q, q), q, gy[3:].clone().view(20, 2, 64))
+    assert torch.equal(odd, want)

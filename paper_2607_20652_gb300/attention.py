@@ -27,6 +27,12 @@ def _dense(g: torch.Tensor) -> torch.Tensor:
     return g if g.data_ptr() % 16 == 0 else g.clone()
 
 
+def _like(w: Optional[torch.Tensor], x: torch.Tensor) -> Optional[torch.Tensor]:
+    """A norm's weight in the rows' type: under autocast fp32 weights meet bf16
+    rows, and are rounded to them as a linear layer's are."""
+    return None if w is None else w.to(x.dtype)
+
+
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, cu_q, cu_k, max_q, max_k, causal, scale):
@@ -53,15 +59,15 @@ class _NormRopeFunction(torch.autograd.Function):
     def forward(ctx, q, k, wq, wk, cos, sin, positions, eps, interleaved, normalise):
         ctx.save_for_backward(q, k, wq, wk, cos, sin, positions)
         ctx.at = (eps, interleaved, normalise)
-        return dpb.qk_norm_rope(q, k, wq, wk, cos, sin, positions, *ctx.at)
+        return dpb.qk_norm_rope(q, k, _like(wq, q), _like(wk, k), cos, sin, positions, *ctx.at)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, gq, gk):
         q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
         need = wq is not None and ctx.needs_input_grad[2] or wk is not None and ctx.needs_input_grad[3]
-        dq, dk, dwq, dwk = dpb.qk_norm_rope_backward(q, k, gq.contiguous(), gk.contiguous(), wq, wk, cos, sin, positions,
-                                                     *ctx.at, weight_grads=need)
+        dq, dk, dwq, dwk = dpb.qk_norm_rope_backward(q, k, gq.contiguous(), gk.contiguous(), _like(wq, q), _like(wk, k), cos,
+                                                     sin, positions, *ctx.at, weight_grads=need)
         return (dq, dk, None if wq is None or dwq is None else dwq.to(wq.dtype),
                 None if wk is None or dwk is None else dwk.to(wk.dtype)) + (None,) * 6
 
@@ -80,7 +86,7 @@ class _PackedFunction(torch.autograd.Function):
     def forward(ctx, qkv, hq, hkv, wq, wk, cos, sin, positions, rope, cu, at):
         q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
         if rope is not None:
-            q, k = dpb.qk_norm_rope(q, k, wq, wk, cos, sin, positions, **rope)
+            q, k = dpb.qk_norm_rope(q, k, _like(wq, q), _like(wk, k), cos, sin, positions, **rope)
         o, lse = dpb.attention_forward(q, k, v, cu, **at)
         ctx.save_for_backward(qkv, q, k, wq, wk, cos, sin, positions, cu, o, lse)
         ctx.hq, ctx.hkv, ctx.rope, ctx.at = hq, hkv, rope, at
@@ -99,8 +105,8 @@ class _PackedFunction(torch.autograd.Function):
                                    **ctx.at)
         else:
             dq, dk, _ = dpb.attention_backward(q, k, qkv[:, hq + hkv:], o, lse, _dense(go), cu, grad_v=gv, **ctx.at)
-            _, _, dwq, dwk = dpb.qk_norm_rope_backward(qkv[:, :hq], qkv[:, hq:hq + hkv], dq, dk, wq, wk, cos, sin, positions,
-                                                       grad_q=gq, grad_k=gk, weight_grads=wq is not None, **rope)
+            _, _, dwq, dwk = dpb.qk_norm_rope_backward(qkv[:, :hq], qkv[:, hq:hq + hkv], dq, dk, _like(wq, q), _like(wk, k), cos,
+                                                       sin, positions, grad_q=gq, grad_k=gk, weight_grads=wq is not None, **rope)
         if dwq is not None:
             dwq, dwk = dwq.to(wq.dtype), dwk.to(wk.dtype)
         return (grad, None, None, dwq, dwk) + (None,) * 6
@@ -116,7 +122,8 @@ class Attention(nn.Module):
     arguments of dpb.rope_tables (base, scaling, ...). forward() also takes
     packed rows x [T, d] with ``cu`` (int32 token offsets of the sequences) and
     ``longest``; positions then restart at every sequence, and rows outside of
-    ``cu`` (padding) give 0 and take no part in any gradient."""
+    ``cu`` (padding) give 0 and take no part in any gradient. The rows are
+    bf16; parameters may be fp32 under bf16 autocast."""
 
     def __init__(self, d: int, heads: int, kv_heads: Optional[int] = None, qk_norm: bool = True, rotary: bool = True,
                  context: int = 1024, rope: Optional[dict] = None, device=None, dtype=None):

@@ -357,3 +357,35 @@ def test_a_gradient_at_any_address():
     odd, = torch.autograd.grad(torch.cat([gy[:3], A.attention(q, q, q).flatten()]), q, gy)
     want, = torch.autograd.grad(A.attention(q, q, q), q, gy[3:].clone().view(20, 2, 64))
     assert torch.equal(odd, want)
+
+
+def test_fp32_parameters_under_autocast():
+    """The module with fp32 parameters under bf16 autocast computes what it does in bf16, keeps its gradients in fp32, and
+    follows steps far below bf16's spacing."""
+    from paper_2607_20652_gb300 import attention as A
+    from paper_2607_20652_gb300.optim import AdamW
+    torch.manual_seed(8)
+    m = A.Attention(128, 2, 1, device="cuda", context=64)
+    with torch.no_grad():
+        for p in (m.q_norm, m.k_norm):
+            p.copy_(1 + 0.3 * torch.randn_like(p))
+    low = copy.deepcopy(m).bfloat16()
+    x, gy = torch.randn(2, 50, 128, device="cuda"), torch.randn(2, 50, 128, device="cuda").bfloat16()
+    with torch.autocast("cuda", torch.bfloat16):
+        y = m(x)
+    y.backward(gy)
+    z = low(x.bfloat16())
+    z.backward(gy)
+    assert y.dtype == torch.bfloat16 and torch.equal(y, z)
+    for (n, p), r in zip(m.named_parameters(), low.parameters()):
+        assert p.grad.dtype == torch.float32 and torch.equal(p.grad.bfloat16(), r.grad), n
+    q = torch.randn(30, 2, 64, device="cuda").bfloat16().requires_grad_()
+    wq = torch.rand(64, device="cuda").requires_grad_()
+    A.qk_norm_rope(q, q, wq, None)[0].float().sum().backward()
+    wr = wq.detach().bfloat16().requires_grad_()
+    A.qk_norm_rope(q, q, wr, None)[0].float().sum().backward()
+    assert torch.equal(wq.grad.bfloat16(), wr.grad)
+    before = m.q_norm.detach().clone()
+    AdamW(m.parameters(), lr=1e-5, weight_decay=0.0).step()
+    moved = (m.q_norm.detach() - before).abs()
+    assert bool((moved > 0.9e-5).all()) and bool((moved < 1.1e-5).all())

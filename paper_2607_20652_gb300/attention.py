@@ -121,8 +121,10 @@ class Attention(nn.Module):
     positions up to ``context`` (None or 0: none); ``rope`` holds further
     arguments of dpb.rope_tables (base, scaling, ...). forward() also takes
     packed rows x [T, d] with ``cu`` (int32 token offsets of the sequences) and
-    ``longest``; positions then restart at every sequence, and rows outside of
-    ``cu`` (padding) give 0 and take no part in any gradient. The rows are
+    ``longest`` (None: read from ``cu``, which waits for the device, where more
+    rows than ``context`` leave open whether the tables reach); positions then
+    restart at every sequence, and rows outside of ``cu`` (padding) give 0 and
+    take no part in any gradient. The rows are
     bf16; parameters may be fp32 under bf16 autocast."""
 
     def __init__(self, d: int, heads: int, kv_heads: Optional[int] = None, qk_norm: bool = True, rotary: bool = True,
@@ -165,6 +167,10 @@ class Attention(nn.Module):
             rows = torch.arange(x.shape[0], dtype=torch.int32, device=x.device)
             # padding has no position: any row of the tables will do
             positions = (rows - cu[torch.searchsorted(cu, rows, right=True) - 1]).clamp_(0, self.context - 1)
+        if self.cos is not None and longest is None and x.shape[0] > self.context:
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError(f"longest is needed: {x.shape[0]} rows, rotary tables for {self.context}")
+            longest = int((cu[1:] - cu[:-1]).max()) if cu.numel() > 1 else 0
         if self.cos is not None and longest is not None and longest > self.context:
             raise ValueError(f"sequences of {longest} tokens, rotary tables for {self.context}")
         rope = None

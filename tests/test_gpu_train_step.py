@@ -389,3 +389,25 @@ def test_fp32_parameters_under_autocast():
     AdamW(m.parameters(), lr=1e-5, weight_decay=0.0).step()
     moved = (m.q_norm.detach() - before).abs()
     assert bool((moved > 0.9e-5).all()) and bool((moved < 1.1e-5).all())
+
+
+def test_sequences_beyond_the_tables_are_refused():
+    """Whether their length is given or not; without a length, and more rows than the tables have, it is read from the offsets."""
+    from paper_2607_20652_gb300.attention import Attention
+    torch.manual_seed(2)
+    m = Attention(128, 2, device="cuda", dtype=torch.bfloat16, context=64)
+    x = torch.randn(200, 128, device="cuda").bfloat16()
+    offsets = lambda *n: torch.tensor(n, dtype=torch.int32, device="cuda")
+    for longest in (100, None):
+        with pytest.raises(ValueError, match="rotary tables"):
+            m(x, offsets(0, 50, 150, 200), longest)
+    cu = offsets(0, 50, 114, 178)
+    assert torch.equal(m(x, cu), m(x, cu, 64))
+    assert not m(x, offsets(7)).any()
+    plain = Attention(128, 2, rotary=False, device="cuda", dtype=torch.bfloat16)
+    assert plain(x, offsets(0, 200)).shape == x.shape
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ValueError, match="longest is needed"):
+            m(x, cu)
+    assert dpb.status() == 0

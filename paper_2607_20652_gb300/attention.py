@@ -128,7 +128,7 @@ class Attention(nn.Module):
     bf16; parameters may be fp32 under bf16 autocast."""
 
     def __init__(self, d: int, heads: int, kv_heads: Optional[int] = None, qk_norm: bool = True, rotary: bool = True,
-                 context: int = 1024, rope: Optional[dict] = None, device=None, dtype=None):
+                 context: Optional[int] = 1024, rope: Optional[dict] = None, device=None, dtype=None):
         super().__init__()
         kv_heads = heads if kv_heads is None else kv_heads
         if d % heads or heads % kv_heads:
@@ -141,7 +141,8 @@ class Attention(nn.Module):
         self.out = nn.Linear(d, d, bias=False, **kw)
         self.q_norm = nn.Parameter(torch.ones(self.dim, **kw)) if qk_norm else None
         self.k_norm = nn.Parameter(torch.ones(self.dim, **kw)) if qk_norm else None
-        cos, sin = dpb.rope_tables(context, self.dim, device=device or "cpu", **(rope or {})) if rotary else (None, None)
+        cos, sin = dpb.rope_tables(context, self.dim, device=device or "cpu", **(rope or {})) if rotary and context else \
+            (None, None)
         # tables stay in fp32 whatever the module is cast to
         self.register_buffer("cos", cos, persistent=False)
         self.register_buffer("sin", sin, persistent=False)

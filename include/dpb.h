@@ -495,7 +495,8 @@ dpb_status dpb_attention_workspace_size(const dpb_attention_config *cfg, size_t 
  *               them (a hash of seed, step and the value's place in the list),
  *               so changes smaller than a step of the code are kept on
  *               average; a sqrt(v) above 0 never becomes 0. The step itself
- *               uses the values before rounding.
+ *               uses the values before rounding. A moment that is infinite or
+ *               NaN is stored as NaN; the others of its 256 keep their values.
  *   step        1, 2, ... (bias correction)
  *   grad_scale  device fp32, nullable (1); where it is not finite, nothing
  *               is changed (a loss scaler's skipped step)

@@ -24,14 +24,15 @@ constexpr int kPer = 8;                    // values a thread
 // Rounds a block: 32-bit states keep enough loads in flight with one (203 M bf16
 // parameters: 632 us). 8-bit ones compute longer on fewer bytes, so a block loads
 // its next round while it computes one, and its start is spread over up to eight
-// (203 M bf16 parameters: 457 us; one round of 256 threads 547, four of 128
-// threads 475) as long as there are some waves of blocks (14 M fp32 parameters:
-// 57 us with eight).
+// (203 M bf16 parameters: 434 us; while that took 457, one round of 256 threads
+// 547, four of 128 threads 475) as long as there are some waves of blocks (14 M
+// fp32 parameters: 56 us; 57 with eight).
 constexpr int kThreads = 64;
 constexpr int kRound = kThreads * kPer;    // values a block takes at a time
 constexpr int kMostRounds = 8, kWaves = 6, kResident = 152 * 14;
 constexpr int kBlock = 32 * kPer;          // values that share a scale
 constexpr float kTop = 448.f;              // largest e4m3 value
+constexpr float kLargest = 3.402823466e38f;  // largest finite fp32 value
 constexpr int kFew = 40, kMany = 440;      // tensors a launch (4 KB and 32 KB of kernel arguments)
 
 struct Tensor {
@@ -135,10 +136,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
+// The warp's largest of values >= 0 that are no NaN: their bits as integers are
+// in the same order, and integers have an instruction for it.
 __device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
-    return v;
+    return __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(v)));
 }
 
 // Scale of a block with largest magnitude `top`, and what its values are
@@ -303,9 +304,26 @@ __device__ __forceinline__ void step_values(const Tensor &t, int64_t i0, const H
     }
     store8<T, WIDE>(pp, left, p);
     if constexpr (F8) {
+        tm = warp_max(tm);
+        tv = warp_max(tv);
+        if (max3(tm, tv, 0.f) > kLargest) {
+            // The codes have no infinity: it is stored as NaN, and the block's scale is
+            // that of its finite values, so that they keep theirs. (All lanes: tm, tv
+            // are the warp's.)
+            tm = tv = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (fabsf(m[i]) > kLargest) m[i] = __int_as_float(0x7fffffff);
+                if (v[i] > kLargest) v[i] = __int_as_float(0x7fffffff);
+                tm = fmaxf(tm, fabsf(m[i]));
+                tv = fmaxf(tv, v[i]);
+            }
+            tm = warp_max(tm);
+            tv = warp_max(tv);
+        }
         float im, iv;
-        ms = block_scale(warp_max(tm), &im);
-        vs = block_scale(warp_max(tv), &iv);
+        ms = block_scale(tm, &im);
+        vs = block_scale(tv, &iv);
         const uint64_t at = (uint64_t)(t.at + i0);
         // the value's place (a multiple of kPer, and its place among the kPer) with the key
         const uint32_t key = (uint32_t)at ^ (h.key + 0x9e3779b9u * (uint32_t)(at >> 32));
@@ -379,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 14) adamw_kernel(const __grid_consta
             hi = mid;
     }
     const float gs = h.grad_scale ? *h.grad_scale : 1.f;
-    if (!(fabsf(gs) <= 3.402823466e38f)) return;
+    if (!(fabsf(gs) <= kLargest)) return;
     const int64_t i0 = (chunk - tab.first[lo]) * tab.chunk + (int64_t)threadIdx.x * kPer;
     if (tab.wide[lo])
         step_chunk<T, F8, true>(tab.t[lo], i0, tab.chunk, h, gs);

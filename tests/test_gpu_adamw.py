@@ -277,3 +277,26 @@ def test_a_copied_group_steps_its_own_tensors(bits):
         assert not any(torch.equal(a, b) for a, b in zip(kinds(other), before))
     grp.step(t["g"], step=2, seed=5, **H)
     assert all(torch.equal(a, b) for a, b in zip(kinds(grp), kinds(other)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, 1e30])
+def test_an_infinity_stays_where_it_is(bad, dtype):
+    """An infinite gradient: its own states become NaN, every other value and scale is what it is with a gradient of 0 in its
+    place, in this step and in the next. The same of the second moments where only the gradient's square is infinite (the
+    first moment is finite then, and the largest of its block)."""
+    runs = []
+    for g in (bad, 0.0):
+        t = tensors([600, 300], dtype, 8, seed=5)
+        grp = group(t, 8)
+        t["m"][0].view(torch.uint8)[300] = t["v"][0].view(torch.uint8)[300] = 0
+        t["g"][0][300] = g
+        grp.step(t["g"], step=3, seed=2, **H)
+        t["g"][0][300] = 0.0
+        grp.step(t["g"], step=4, seed=2, **H)
+        runs.append({k: torch.cat([x.float() for x in t[k]]) for k in ("p", "m", "v", "ms", "vs")})
+    other = torch.arange(900, device="cuda") != 300
+    for k in ("p", "m", "v", "ms", "vs") if math.isinf(bad) else ("v", "vs"):
+        a, b = (r[k] if k in ("ms", "vs") else r[k][other] for r in runs)
+        assert torch.isfinite(b).all() and torch.equal(a, b), k
+    assert runs[0]["v"][300].isnan()

@@ -503,3 +503,14 @@ def test_overlapping_sequences_leave_no_row_out():
     one = run(q, k, v, do, [T], [T])
     assert torch.equal(got["o"], one["o"]) and torch.equal(got["lse"], one["lse"])
     assert all(torch.isfinite(x).all() for n, x in got.items())
+
+
+@pytest.mark.parametrize("D", [24, 32, 48, 56, 80, 88, 104, 112, 120])
+@pytest.mark.parametrize("causal", [True, False])
+def test_other_head_widths(D, causal):
+    """Widths between those that the products have columns for."""
+    nq, nk = [300, 1, 130], [300, 200, 257]
+    q, k, v, do = draw(nq, nk, 4, 2, D, seed=D)
+    want, tol = formula(q, k, v, do, nq, nk, causal, D ** -0.5)
+    check(run(q, k, v, do, nq, nk, causal), want, tol)
+    assert dpb.status() == 0

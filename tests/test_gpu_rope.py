@@ -232,3 +232,31 @@ def test_without_eps(H, Hk, D, dtype):
         close(dx[i], gx, r * (u + n * (u * n).mean(-1, keepdim=True)), D, extra=2)
         close(dx[2 + i], gw, (2 * gy[i].double().abs().amax(-1, keepdim=True) * n).sum((0, 1)), D, extra=T * (H, Hk)[i] / D + 2)
         assert torch.isfinite(dx[2 + i]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rot,inter", [(64, False), (64, True), (48, False), (20, True), (30, False)])
+def test_unaligned_rows_element_by_element(rot, inter, dtype):
+    """Rows at odd addresses, and gradients into them: each value within its own rounding of the formula's."""
+    T, H, D = 45, 3, 64
+    q, k, w, cos, sin, pos, gy = draw(T, H, H, D, rot, dtype, seed=32)
+
+    def odd(x):
+        y = torch.empty(T * H * (D + 1) + 1, dtype=dtype, device="cuda")[1:].view(T, H, D + 1)[:, :, :D]
+        return y.copy_(x)
+
+    at = dict(weight_q=w[0], weight_k=w[1], cos=cos, sin=sin, positions=pos, eps=EPS, interleaved=inter)
+    rows = [odd(x) for x in (q, k, *gy)]
+    outs = [odd(torch.zeros_like(q)) for _ in range(4)]
+    dpb.qk_norm_rope(*rows[:2], **at, q_out=outs[0], k_out=outs[1])
+    *_, dwq, dwk = dpb.qk_norm_rope_backward(*rows, **at, grad_q=outs[2], grad_k=outs[3])
+    for i, x in enumerate((q, k)):
+        xd, wd = x.double().requires_grad_(), w[i].double().requires_grad_()
+        want = formula(xd, wd, cos, sin, pos, rot, inter)
+        r = torch.rsqrt((xd * xd).mean(-1, keepdim=True) + EPS).detach()
+        n = xd.detach().abs() * r
+        close(outs[i], want.detach(), (n * wd.detach().abs()).amax(-1, keepdim=True) * 2, D)
+        gx, gw = torch.autograd.grad(want, (xd, wd), gy[i].double())
+        u = 2 * gy[i].double().abs().amax(-1, keepdim=True) * wd.detach().abs().amax()
+        close(outs[2 + i], gx, r * (u + n * (u * n).mean(-1, keepdim=True)), D, extra=2)
+        close((dwq, dwk)[i], gw, (2 * gy[i].double().abs().amax(-1, keepdim=True) * n).sum((0, 1)), D, extra=T * H / D + 2)

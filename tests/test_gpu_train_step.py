@@ -411,3 +411,57 @@ def test_sequences_beyond_the_tables_are_refused():
         with pytest.raises(ValueError, match="longest is needed"):
             m(x, cu)
     assert dpb.status() == 0
+
+
+@pytest.mark.parametrize("kv,qk_norm,rotary", [(4, True, True), (2, True, False), (1, False, True), (1, True, True)])
+def test_gradients_of_the_parameters(kv, qk_norm, rotary):
+    """Each parameter's gradient against the module in 64 bits with differentiable weights; the norms' weights differ, so
+    that neither gradient can stand for the other. Bound as for the module's gradients above."""
+    from paper_2607_20652_gb300.attention import Attention
+    torch.manual_seed(10)
+    m = Attention(256, 4, kv, qk_norm, rotary, context=128, device="cuda", dtype=torch.bfloat16)
+    if qk_norm:
+        with torch.no_grad():
+            m.q_norm.copy_(1 + 0.5 * torch.randn(64, device="cuda"))
+            m.k_norm.copy_(1 - 0.5 * torch.randn(64, device="cuda"))
+    cu = [0, 100, 101, 220, 300]
+    x = torch.randn(300, 256, device="cuda").bfloat16()
+    gy = torch.randn(300, 256, device="cuda").bfloat16()
+    m(x, torch.tensor(cu, dtype=torch.int32, device="cuda"), 119).backward(gy)
+    w = {n: p.detach().double().requires_grad_() for n, p in m.named_parameters()}
+
+    class Double:  # what plain() reads of a module
+        heads, kv_heads, dim, cos, sin, q_norm = m.heads, m.kv_heads, m.dim, m.cos, m.sin, m.q_norm
+
+        @staticmethod
+        def named_parameters():
+            return [(n, Kept(p)) for n, p in w.items()]
+
+    class Kept:
+        def __init__(self, p):
+            self.p = p
+
+        def detach(self):
+            return self
+
+        def double(self):
+            return self.p
+
+    want = dict(zip(w, torch.autograd.grad(plain(Double, x.double(), cu), list(w.values()), gy.double())))
+    for n, p in m.named_parameters():
+        assert float((p.grad.double() - want[n]).norm() / want[n].norm()) < 10 * 2.0 ** -8, n
+
+
+def test_functions_keep_the_norms_apart():
+    """Different weights for queries and keys: each gets its own gradient, bit for bit the call's."""
+    from paper_2607_20652_gb300 import attention as A
+    g = torch.Generator(device="cuda").manual_seed(12)
+    q, k = (torch.randn(90, h, 64, device="cuda", generator=g).bfloat16().requires_grad_() for h in (4, 2))
+    wq, wk = (torch.rand(64, device="cuda", generator=g).bfloat16().requires_grad_() for _ in range(2))
+    cos, sin = dpb.rope_tables(90, 64)
+    gq, gk = (torch.randn(x.shape, device="cuda", generator=g).bfloat16() for x in (q, k))
+    torch.autograd.backward(A.qk_norm_rope(q, k, wq, wk, cos, sin), (gq, gk))
+    want = dpb.qk_norm_rope_backward(q.detach(), k.detach(), gq, gk, wq.detach(), wk.detach(), cos, sin)
+    for x, y in zip((q, k, wq, wk), want):
+        assert torch.equal(x.grad, y.to(x.dtype))
+    assert not torch.equal(wq.grad, wk.grad)

@@ -86,16 +86,11 @@ struct Seq {
     bool ok;
 };
 
-// -1 <= s <= seqs: -1 and seqs stand for the rows before the first sequence and
-// after the last.
 __device__ __forceinline__ Offsets load_offsets(const AttnArgs &a, int s) {
-    const bool first = s < 0, last = s >= a.seqs;
-    Offsets r{0, first ? 0 : a.total_q, 0, first ? 0 : a.total_k};
+    Offsets r{0, a.total_q, 0, a.total_k};
     if (a.cu_q) {
-        if (!first) r.q0 = __ldg(a.cu_q + s), r.k0 = __ldg(a.cu_k + s);
-        if (!last) r.q1 = __ldg(a.cu_q + s + 1), r.k1 = __ldg(a.cu_k + s + 1);
-    } else if (last && s > 0) {
-        r.q0 = a.total_q, r.k0 = a.total_k;
+        r.q0 = __ldg(a.cu_q + s), r.q1 = __ldg(a.cu_q + s + 1);
+        r.k0 = __ldg(a.cu_k + s), r.k1 = __ldg(a.cu_k + s + 1);
     }
     return r;
 }
@@ -106,11 +101,24 @@ __device__ __forceinline__ Seq sequence(const AttnArgs &a, const Offsets &o) {
     r.q0 = (int)o.q0, r.n = (int)(o.q1 - o.q0), r.k0 = (int)o.k0, r.m = (int)(o.k1 - o.k0);
     return r;
 }
-// The same of -1 <= s <= seqs. What is no sound sequence (not ok) has the rows
-// that its offsets pass on the way up, which see nothing and are seen by none:
-// from the first offset to the last such a way passes every row, so each is a
-// sound sequence's or one of these.
-__device__ __forceinline__ Seq rows_of(const AttnArgs &a, int s, const Offsets &o) {
+// Sequence s, -1 <= s <= seqs, where -1 and seqs stand for the rows before the
+// first and after the last. What is no sound sequence (not ok) has the rows that
+// its offsets pass on the way up, which see nothing and are seen by none: from
+// the first token to the last such a way passes every row, so each is a sound
+// sequence's or one of these.
+__device__ __forceinline__ Seq rows_of(const AttnArgs &a, int s) {
+    Offsets o{0, a.total_q, 0, a.total_k};
+    if (a.cu_q) {  // four loads at once, whatever s is
+        const int i = max(s, 0), j = min(s + 1, a.seqs);
+        o.q0 = __ldg(a.cu_q + i), o.q1 = __ldg(a.cu_q + j);
+        o.k0 = __ldg(a.cu_k + i), o.k1 = __ldg(a.cu_k + j);
+    } else if (s < 0) {
+        o.q1 = o.k1 = 0;
+    } else if (s > 0) {
+        o.q0 = a.total_q, o.k0 = a.total_k;
+    }
+    if (s < 0) o.q0 = o.k0 = 0;
+    if (s >= a.seqs) o.q1 = a.total_q, o.k1 = a.total_k;
     Seq r = sequence(a, o);
     const bool is = s >= 0 && s < a.seqs;
     if (is && !r.ok) set_status(a.status, DPB_DEV_BAD_LENGTH);
@@ -363,7 +371,7 @@ struct Finder {
         for (; first < a.seqs; first += 32) {
             const int s = first + lane;
             Seq q{0, 0, 0, 0, false};
-            if (s < a.seqs) q = rows_of(a, s, load_offsets(a, s));
+            if (s < a.seqs) q = rows_of(a, s);
             const int pairs = pairs_of(q);
             int upto = pairs;
 #pragma unroll
@@ -446,12 +454,14 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
             uint32_t at = blockIdx.x;
             bool have = true;
             Finder finder{0, 0};
-            // the index at hand (step > 0): its sequence and next pair of tiles, from
-            // there to the one after
-            int seq = 0, tile = 0, step = 0;
-            // pairs to look up: of the index at hand; beyond those that the grid counts
-            int place = -1, over = -1;
-            constexpr int kFar = 1 << 28;
+            // The last blocks of the grid, and those of skipped sequences, have rows of no
+            // sound sequence: which (a sequence, or -1 and seqs as for rows_of) and their
+            // next pair of tiles (and, of those before and after the sequences, head).
+            // `at` goes on beyond the grid's sequences (over) where ones that overlap have
+            // more pairs of tiles than it counts.
+            constexpr int kNone = -2;
+            int rests = kNone, piece = 0;
+            bool over = false;
             // takes over a block that has not started, if there is one
             auto next = [&]() {
                 if (elect_one()) {
@@ -462,6 +472,7 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
                 failed = !__all_sync(kFull, bar_wait(answered, asked & 1, kTries));
                 ++asked;
                 have = !failed && block_answer(answer, at);
+                over = false;
                 fence_async_shared();
                 __syncwarp();
             };
@@ -469,43 +480,52 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
                 it = Item{};
                 it.kind = kEnd;
                 while (have) {
-                    // the heads of a group side by side; the longest rows first, or
-                    // sequence by sequence; last, of each head, the rows before the first
-                    // sequence and after the last, one pair after the other (8 x 1024, 12
-                    // heads of 64, has none: 25.3 us, 24.8 without these blocks)
-                    const int rest = (int)(at / a.hq);
                     it.head = (int)(at % a.hq);
-                    if (step == 0) {
-                        if (at < (uint32_t)a.items) {
-                            seq = rest % a.seqs;
-                            tile = a.tiles - 1 - rest / a.seqs;
-                            step = a.tiles;  // beyond every sound sequence's
-                            if (a.close) place = rest;
-                        } else {
-                            seq = rest * a.hq == a.items ? -1 : a.seqs;
-                            tile = 0, step = 1;
-                            // sequences that overlap can have more than the grid counts
-                            if (a.close && seq >= 0) over = rest - 1;
+                    // the usual way stays together (cold code costs the training step 3 us)
+                    if (__builtin_expect(rests == kNone && (at < (uint32_t)a.items || over), 1)) {
+                        // the heads of a group side by side; the longest rows first, or
+                        // sequence by sequence
+                        const int rest = (int)(at / a.hq);
+                        int seq = rest % a.seqs;
+                        it.tile = a.tiles - 1 - rest / a.seqs;
+                        if (a.close && !finder.find(a, rest, seq, it.tile)) {
+                            next();
+                            continue;
                         }
+                        it.q = sequence(a, load_offsets(a, seq));
+                        if (__builtin_expect(it.q.ok, 1)) {
+                            if (it.tile * 2 * kRows < it.q.n) {
+                                it.kind = kQueries;
+                                break;
+                            }
+                            next();
+                            continue;
+                        }
+                        rests = seq, piece = it.tile;
+                    } else if (rests == kNone) {
+                        rests = -1, piece = (int)at - a.items;
                     }
-                    if (place >= 0) {
-                        step = kFar;
-                        if (!finder.find(a, place, seq, tile)) tile = kFar, over = -1;
-                        place = -1;
-                    }
-                    it.q = rows_of(a, seq, load_offsets(a, seq));
-                    it.tile = tile;
-                    if (tile < pairs_of(it.q)) {
-                        if (!it.q.ok) it.q.m = 0;
+                    const bool outside = rests < 0 || rests >= a.seqs;
+                    it.tile = piece;
+                    if (outside) it.head = piece % a.hq, it.tile = piece / a.hq;
+                    it.q = rows_of(a, rests);
+                    const int pairs = pairs_of(it.q);
+                    if (it.tile < pairs) {
+                        // a skipped sequence's further pairs: as far on as any sound one has
+                        // them, or as the finder says
+                        piece = outside ? piece + (int)gridDim.x - a.items : a.close ? 0x7fffffff : piece + a.tiles;
+                        it.q.m = 0;
                         it.kind = kQueries;
                         break;
                     }
-                    if (over >= 0) {
-                        place = over++;
-                        continue;
+                    if (rests < 0) {
+                        rests = a.seqs, piece -= pairs * a.hq;
+                    } else {
+                        rests = kNone;
+                        if (outside && a.close) over = true;
+                        else if (over) at += gridDim.x - a.items;
+                        else next();
                     }
-                    step = 0;
-                    next();
                 }
                 failed = failed || !list.put(it, c);
                 if (failed || it.kind == kEnd) break;
@@ -543,11 +563,8 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_forward_kernel(const
                     }
                 }
                 if (failed) break;
-                tile += step;
-                if (tile >= pairs_of(q) && over < 0) {
-                    step = 0;
-                    next();
-                }
+                if (over && rests == kNone) at += gridDim.x - a.items;
+                else if (rests == kNone) next();
             }
             // no copy is in flight when the block ends, whatever gave up
             ring.drain(i);
@@ -1013,7 +1030,7 @@ __device__ void make_plan(const AttnArgs &a) {
         for (int s0 = warp - 1; s0 <= a.seqs; s0 += 32 * kWarps) {
             const int s = s0 + kWarps * lane;
             Seq mine{0, 0, 0, 0, true};
-            if (s <= a.seqs) mine = rows_of(a, s, load_offsets(a, s));
+            if (s <= a.seqs) mine = rows_of(a, s);
             const bool more = max(mine.n, mine.m) > kRows;
             uint32_t left = __ballot_sync(kFull, more);
             Seq q = mine;
@@ -1994,7 +2011,11 @@ cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
     // all go first: 145 us.
     const int64_t most = a.total_q / (2 * kRows) + a.seqs;
     a.close = (int64_t)a.tiles * a.seqs > 2 * most;
-    const int64_t items = (a.close ? most : (int64_t)a.tiles * a.seqs) * a.hq, blocks = items + 2 * a.hq;
+    const int64_t items = (a.close ? most : (int64_t)a.tiles * a.seqs) * a.hq;
+    // The last blocks, one for every two SMs at most, write the rows before the first
+    // sequence and after the last (32 x 1024 of 65536 rows, 12 heads of 64: 124 us, 353
+    // with two blocks a head; without such rows 8 x 1024 takes 24.7 us as before).
+    const int64_t blocks = items + std::min<int64_t>((multiprocessors() + 1) / 2, (a.total_q / (2 * kRows) + 2) * a.hq);
     if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     a.items = (int)items;
     return launch_blocks<C, attention_forward_kernel<C>, false>(a, blocks, s);

@@ -514,3 +514,20 @@ def test_other_head_widths(D, causal):
     want, tol = formula(q, k, v, do, nq, nk, causal, D ** -0.5)
     check(run(q, k, v, do, nq, nk, causal), want, tol)
     assert dpb.status() == 0
+
+
+@pytest.mark.parametrize("lens", [[3, 130], [40] * 90, []])
+def test_long_padding(lens):
+    """Padding that is most of the rows, written by all blocks: by as many as there are sequences' tiles, or by more."""
+    n, T = sum(lens), 30011
+    q, k, v, do = draw([T], [T], 3, 1, 64, seed=24)
+    cu = [2000 + sum(lens[:i]) for i in range(len(lens) + 1)]
+    got = into_nan(q, k, v, do, cu, cu, max_q=max(lens, default=0), max_k=max(lens, default=0))
+    assert dpb.status() == 0
+    for name, x in got.items():
+        assert torch.equal(x, gaps(x, cu, -math.inf if name == "lse" else 0.0, 1 if name == "lse" else 0)), name
+    if n:
+        rows = slice(2000, 2000 + n)
+        alone = run(q[rows], k[rows], v[rows], do[rows], lens, lens)
+        for name, x in alone.items():
+            assert torch.equal(x, got[name][:, rows] if name == "lse" else got[name][rows]), name

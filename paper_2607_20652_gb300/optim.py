@@ -64,7 +64,8 @@ class AdamW(torch.optim.Optimizer):
     def _param_sets(self, index: int, group: dict):
         """The group's parameters that have ever had a gradient, by dtype and device, with their states."""
         new = [p for p in group["params"] if p.grad is not None and p not in self.state]
-        if new or index not in self._sets:
+        ids = list(map(id, group["params"]))  # groups and parameters may be taken out or exchanged
+        if new or self._sets.get(index, (None,))[0] != ids:
             for p in new:
                 if p.is_sparse or p.grad.is_sparse:
                     raise ValueError("AdamW takes dense gradients")
@@ -79,8 +80,8 @@ class AdamW(torch.optim.Optimizer):
                 names = ["exp_avg", "exp_avg_sq"] + (["exp_avg_scale", "exp_avg_sq_scale"]
                                                      if group["state_bits"] == 8 else [])
                 sets.append((ps, dpb.AdamWGroup(ps, *([s[k] for s in st] for k in names))))
-            self._sets[index] = sets
-        return self._sets[index]
+            self._sets[index] = ids, sets
+        return self._sets[index][1]
 
     @torch.no_grad()
     def step(self, closure=None, grad_scale: Optional[torch.Tensor] = None):

@@ -465,3 +465,26 @@ def test_functions_keep_the_norms_apart():
     for x, y in zip((q, k, wq, wk), want):
         assert torch.equal(x.grad, y.to(x.dtype))
     assert not torch.equal(wq.grad, wk.grad)
+
+
+def test_groups_that_change():
+    """A group or a parameter taken out of the optimiser stays as it is, and the others go on with their own numbers."""
+    from paper_2607_20652_gb300.optim import AdamW
+    ps = [torch.nn.Parameter(torch.zeros(300, device="cuda")) for _ in range(4)]
+    opt = AdamW([{"params": ps[:1], "lr": 1.0}, {"params": ps[1:3], "lr": 1e-3}, {"params": ps[3:], "lr": 1e-2}],
+                weight_decay=0.0)
+
+    def moved():
+        before = [float(p[0]) for p in ps]
+        for p in ps:
+            p.grad = torch.ones_like(p)
+        opt.step()
+        return [round(b - float(p[0]), 6) for p, b in zip(ps, before)]
+
+    assert moved() == [1.0, 0.001, 0.001, 0.01]
+    del opt.param_groups[0]
+    assert moved() == [0.0, 0.001, 0.001, 0.01]
+    opt.param_groups[0]["params"] = ps[2:3]
+    assert moved() == [0.0, 0.0, 0.001, 0.01]
+    opt.param_groups[1]["params"][0] = ps[0]
+    assert moved() == [0.01, 0.0, 0.001, 0.0]

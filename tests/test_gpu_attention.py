@@ -531,3 +531,10 @@ def test_long_padding(lens):
         alone = run(q[rows], k[rows], v[rows], do[rows], lens, lens)
         for name, x in alone.items():
             assert torch.equal(x, got[name][:, rows] if name == "lse" else got[name][rows]), name
+
+
+def test_no_keys():
+    q = torch.randn(300, 2, 64, device="cuda").bfloat16()
+    got = into_nan(q, q[:0], q[:0], q, [0, 300], [0, 0])
+    assert not got["o"].any() and not got["dq"].any() and bool((got["lse"] == -math.inf).all())
+    assert got["dk"].shape == (0, 2, 64) and dpb.status() == 0

@@ -491,7 +491,8 @@ extern "C" dpb_status dpb_adamw_step(const dpb_adamw_config *cfg, const dpb_adam
     h.b2 = (float)cfg->beta2;
     h.zero = -0.f;
     h.c2 = (float)(1.0 - cfg->beta2);
-    h.eps = (float)cfg->eps;
+    // the reciprocal takes a denormal for 0, and 0 x inf would be NaN where nothing was ever summed
+    h.eps = cfg->eps > 0 ? std::max((float)cfg->eps, 1.17549435e-38f) : 0.f;
     h.decay = (float)(1.0 - cfg->lr * cfg->weight_decay);
     h.fix2 = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, (double)cfg->step)));
     h.key = mix32((uint32_t)cfg->seed ^

@@ -300,3 +300,18 @@ def test_an_infinity_stays_where_it_is(bad, dtype):
         a, b = (r[k] if k in ("ms", "vs") else r[k][other] for r in runs)
         assert torch.isfinite(b).all() and torch.equal(a, b), k
     assert runs[0]["v"][300].isnan()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-38, 1e-40, 1e-300])
+def test_the_smallest_eps(eps, bits):
+    """Values that never had a gradient: 0 / (0 + eps) is 0 for any eps above 0; others do not notice it."""
+    t = tensors([600], torch.float32, bits, seed=6)
+    for x in (t["g"][0], t["m"][0].view(torch.uint8) if bits == 8 else t["m"][0],
+              t["v"][0].view(torch.uint8) if bits == 8 else t["v"][0]):
+        x[100:400] = 0
+    p, g = t["p"][0].double(), t["g"][0].double()
+    want = formula(p, g, *held(t, 0, bits), 2, **{**H, "eps": eps})[0]
+    group(t, bits).step(t["g"], step=2, **{**H, "eps": eps})
+    assert torch.isfinite(t["p"][0]).all()
+    assert torch.allclose(t["p"][0].double(), want, rtol=1e-5, atol=1e-6)

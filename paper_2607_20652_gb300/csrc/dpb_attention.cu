@@ -1252,7 +1252,7 @@ __global__ void __launch_bounds__(512) attention_delta_kernel(const __grid_const
 // for each tile: 1 x 12289, 12 heads of 64: 645 us (666), 899 TFLOP/s; 8 x 1024,
 // 12 heads of 64: 71 us (98); 1 x 8192, 16 heads of 128: 570 us (590), 1206
 // TFLOP/s, of the seven products done 1688; sequences of 3001, 638, 429, 95 and
-// less, 16 heads of 128 on 4: 122 us (215; 140 with no tile in parts, when one SM
+// less, 16 heads of 128 on 4: 124 us (215; 140 with no tile in parts, when one SM
 // has the longest tile of keys for 128 us). Bound by the tensor cores at 128; at
 // 64 (1800 cycles a block, 1030 of products, 512 of exponentials) by the row
 // warps' arithmetic, 2.5 instructions a cycle of 4. Writing an item's sums

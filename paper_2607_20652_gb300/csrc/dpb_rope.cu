@@ -27,7 +27,7 @@ constexpr int kWarps = 8;
 // Heads of a lane group whose loads are in flight together, and the blocks an
 // SM that the registers are held to: 65536 tokens of 12 + 12 heads of 64 take
 // 71 us at (3, 4), 78 at (3, 3), 87 at (4, 4); the gradient of 49999 tokens of
-// 16 + 4 heads of 128 142 us at (4, 2), 151 at (3, 2), 184 at (3, 3).
+// 16 + 4 heads of 128 143 us at (4, 2), 151 at (3, 2), 184 at (3, 3).
 constexpr int kBatch = 3, kBlocks = 4;
 constexpr int kBatchGrad = 4, kBlocksGrad = 2;
 constexpr int kMaxDim = 256;

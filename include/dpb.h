@@ -531,6 +531,69 @@ typedef struct dpb_adamw_config {
 
 dpb_status dpb_adamw_step(const dpb_adamw_config *cfg, const dpb_adamw_tensor *tensors, int32_t n, void *stream);
 
+/* ---- both ends of the model, and the stream between them -------------------
+ *
+ * What a training step still needs beside its plain matrix products: the lookup
+ * of the tokens' embeddings, the residual's addition with the norm behind it, and
+ * the cross entropy over the vocabulary (§3: tied embeddings, RMS norms). The
+ * status of device bits goes by status_slot as above.
+ */
+
+/* Rows [n][dim]: element (t, i) lies at data + t * stride + i (stride in elements). */
+typedef struct dpb_rows {
+    void *data;
+    int64_t stride;
+} dpb_rows;
+
+/*
+ * dpb_linear_cross_entropy_forward -- cross entropy of the rows' scores over the
+ * vocabulary, without a tensor of tokens x vocabulary:
+ *   z_t = hidden_t weight^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_t,target
+ *   tokens, vocab, dim   dim a multiple of 8; each below 2^31 - 256
+ *   ignore_index  a token with this target has loss 0, lse 0 and no gradient, and its
+ *               hidden row is not read (it may hold anything)
+ *   index_bytes 4 or 8: targets are int32 or int64 [tokens]
+ *   dtype       DPB_BF16
+ * hidden [tokens][dim] and weight [vocab][dim] are bf16, 16-byte aligned, with
+ * strides that are multiples of 8 elements. loss, lse: fp32 [tokens]. A target
+ * outside [0, vocab) that is not ignore_index sets DPB_DEV_BAD_INDEX and counts
+ * as ignored. Scores and sums are fp32, exponentials to 2 ulp; a small loss keeps
+ * its digits (it is not formed from the rounded lse).
+ */
+typedef struct dpb_linear_loss_config {
+    int64_t tokens;
+    int32_t vocab, dim;
+    int64_t ignore_index;
+    int32_t index_bytes, dtype, grad_stride, status_slot;
+} dpb_linear_loss_config;
+
+dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
+                                            const dpb_rows *weight, const void *targets, float *loss, float *lse,
+                                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dpb_linear_cross_entropy_backward -- its gradients for grad_loss = dL/dloss:
+ *   dz_tv = grad_loss_t (exp(z_tv - lse_t) - [v = target_t]),
+ *   grad_hidden = dz weight,  grad_weight = dz^T hidden.
+ * The scores are formed again, a piece of the vocabulary at a time. lse is the
+ * forward's. grad_loss: fp32, token t's at grad_loss + t * grad_stride
+ * (grad_stride 0: one value for all, as of a mean; or 1). grad_hidden and
+ * grad_weight (rows as hidden and weight; either may be NULL, then it is not
+ * computed) are written, rows of ignored tokens with 0. dz enters its products
+ * in bf16, relative to the largest finite |grad_loss|; their sums are fp32, in an
+ * order that the sizes and the ignored tokens alone fix, and rounded once.
+ */
+dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
+                                             const dpb_rows *weight, const void *targets, const float *lse,
+                                             const float *grad_loss, const dpb_rows *grad_hidden,
+                                             const dpb_rows *grad_weight, void *workspace, size_t workspace_bytes,
+                                             void *stream);
+
+/* Workspace bytes of the two calls above (256-byte aligned; zeroed once, unless
+ * status_slot says otherwise). Calls that may run at the same time, or be
+ * enqueued by different threads, need workspaces of their own. */
+dpb_status dpb_linear_cross_entropy_workspace_size(const dpb_linear_loss_config *cfg, int32_t backward, size_t *bytes);
+
 /* Static description of a status code. */
 const char *dpb_status_string(dpb_status s);
 

@@ -1,0 +1,854 @@
+// dpb_loss.cu -- softmax cross entropy over a vocabulary from the hidden rows,
+// and its gradient, on the tcgen05 tensor cores.
+//
+//   z = H W^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_t,y
+//   dz_tv = g_t (exp(z_tv - lse_t) - [v = y]),  dH = dz W,  dW = dz^T H
+//
+// z is never in memory: the forward reduces each 256 x 256 tile of it to a
+// maximum and a sum per row while the next tile is multiplied. The gradient
+// forms the tiles again, a piece of the vocabulary at a time, and writes dz of
+// the piece in bf16, which the two other products then read; with T tokens, V
+// words and d columns that is 2 T V d operations forward and 6 T V d for the
+// gradient, where keeping z would save 2 T V d and cost T V values.
+//
+// All of it is one kernel of matrix products (product_kernel). Pairs of blocks
+// take units, tiles of 256 x 256 of one of three products, from a counter,
+// longest first: the pair shares each product (each block loads its 128 rows
+// of A and half of B, so an operand byte is fetched for 128 products, where
+// single blocks of 128 x 256 would need half as many bytes again). In a block
+// a warp copies, one issues (in the first block of the pair), one takes units,
+// and eight take the sums out of TMEM, two accumulators in turn, so that a
+// unit's results are formed while the next unit is multiplied.
+//
+// Tokens that take no part are not multiplied: their places are closed up
+// first (prepare_kernel, gather_kernel), which also keeps whatever their rows
+// hold out of the sums.
+#include <cuda_bf16.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "dpb_checks.h"
+#include "dpb_device.cuh"
+#include "dpb_tensor_core.cuh"
+
+namespace dpb {
+namespace {
+
+using namespace tc;
+using bf16 = __nv_bfloat16;
+
+constexpr uint32_t kTries = 1u << 20;  // polls of a wait before it gives up
+constexpr int kTile = 256;             // rows and columns of a unit
+constexpr int kStages = 6;             // slots of the operands' ring
+constexpr int kStageBytes = 32768;     // 128 x 64 of A and of B
+constexpr int kStore = 4096;           // a warp's rows on their way to memory: 32 of 64 bf16
+constexpr int kRowWarps = 8;
+constexpr int kThreads = 128 + 32 * kRowWarps;
+constexpr int kAhead = 3;              // units taken ahead
+constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.6931471805599453;
+constexpr float kLowest = -1e30f;      // the maximum of no score
+
+enum Kind { kScores = 0, kGrad = 1, kDHidden = 2, kDWeight = 3, kEnd = 4 };
+
+// What the tokens' pass leaves for the others.
+struct Head {
+    int count;     // tokens that take part
+    int all;       // none is left out: rows are where they were
+    float g_max;   // largest finite |grad_loss| (1 if all are 0)
+    int next[60];  // units taken, by launch
+};
+// Of the i-th token that takes part: its target, lse log2 e, grad_loss / g_max.
+struct Token {
+    int target;
+    float lse2, g;
+    int row;
+};
+
+struct Args {
+    CUtensorMap hidden, closed;  // rows as given, and closed up
+    CUtensorMap weight;
+    CUtensorMap dz[2], dz_out[2];  // two pieces, loaded and stored
+    CUtensorMap dw;
+    const bf16 *h;
+    int64_t h_stride;
+    bf16 *closed_rows;
+    Head *head;
+    Token *tokens;
+    int *place;  // of each token: where it went, or -1
+    float2 *part;  // [tiles of the vocabulary][rows]
+    float *z_target;
+    float *loss, *lse;
+    float *acc;  // [rows][dim], where there are several pieces
+    bf16 *dh;
+    int64_t dh_stride;
+    int64_t T, T_pad;
+    int V, d, piece;  // piece: words of a piece
+    int write, read, pieces, launch;  // pieces whose dz is written and read by this launch (or -1)
+    bool want_h, want_w;
+    int32_t *status;
+};
+
+struct Unit {
+    int kind, m0, n0, blocks;  // blocks: of 64 along K
+};
+
+// ---- units ------------------------------------------------------------------------
+
+// Tiles of the vocabulary: groups of rows' tiles, so that the tiles under way
+// share both operands.
+__device__ __forceinline__ Unit score_unit(int kind, int u, int tiles_m, int tiles_n, int d) {
+    const int group = u / (kGroup * tiles_n), in = u - group * kGroup * tiles_n;
+    const int rows = min(kGroup, tiles_m - group * kGroup);
+    return Unit{kind, (group * kGroup + in % rows) * kTile, in / rows * kTile, (d + 63) / 64};
+}
+
+__device__ __forceinline__ Unit unit_of(const Args &a, int count, int u) {
+    const int tiles_m = (count + kTile - 1) / kTile, tiles_d = (a.d + kTile - 1) / kTile;
+    if (a.loss) {  // forward
+        const int tiles_n = (a.V + kTile - 1) / kTile;
+        return u < tiles_m * tiles_n ? score_unit(kScores, u, tiles_m, tiles_n, a.d) : Unit{kEnd, 0, 0, 0};
+    }
+    if (a.read >= 0) {
+        const int words = min(a.piece, a.V - a.read * a.piece), tiles_v = (words + kTile - 1) / kTile;
+        const int n_w = a.want_w ? tiles_v * tiles_d : 0, n_h = a.want_h ? tiles_m * tiles_d : 0;
+        const Unit end{kEnd, 0, 0, 0};
+        auto dw = [&](int i) { return Unit{kDWeight, i / tiles_d * kTile, i % tiles_d * kTile, (count + 63) / 64}; };
+        auto dh = [&](int i) { return Unit{kDHidden, i / tiles_d * kTile, i % tiles_d * kTile, (words + 63) / 64}; };
+        const bool w_first = count >= words;
+        const int first = w_first ? n_w : n_h, second = w_first ? n_h : n_w;
+        if (u < first) return w_first ? dw(u) : dh(u);
+        u -= first;
+        if (u < second) return w_first ? dh(u) : dw(u);
+        u -= second;
+        if (a.write < 0) return end;
+    }
+    const int words = min(a.piece, a.V - a.write * a.piece), tiles_n = (words + kTile - 1) / kTile;
+    return u < tiles_m * tiles_n ? score_unit(kGrad, u, tiles_m, tiles_n, a.d) : Unit{kEnd, 0, 0, 0};
+}
+
+// ---- shared memory ------------------------------------------------------------------
+
+struct Shared {
+    static constexpr int kData = kStages * kStageBytes, kBars = kData + kRowWarps * kStore;
+    // barriers: full and empty of each slot, sums ready and read of each
+    // accumulator, upper halves of the rows' sums there (of each accumulator and
+    // quarter), units handed over and taken
+    static constexpr int kFullBar = kBars, kEmptyBar = kFullBar + 8 * kStages, kReady = kEmptyBar + 8 * kStages,
+                         kRead = kReady + 16, kUpper = kRead + 16, kHanded = kUpper + 64, kTaken = kHanded + 8 * kAhead,
+                         kUnits = kTaken + 8 * kAhead, kTmem = kUnits + 4 * kAhead, kBytes = kTmem + 4;
+    static constexpr int kMerge = kData;  // the upper halves: the forward has no rows on their way to memory
+};
+static_assert(kRowWarps == 8 && 2 * 128 * 8 <= kRowWarps * kStore, "two halves of a row");
+constexpr int kSmem = Shared::kBytes + 1024;  // the data starts at a multiple of 1024
+
+// Units in the order in which they are taken, seen by one role of one block.
+struct Units {
+    uint32_t base, taken;  // this block's barriers and slots; the first block's `taken`
+    int i = 0;
+    // All lanes (or one thread): the next unit's number; false after a wait that gave up.
+    __device__ __forceinline__ bool next(int &u) {
+        const int s = i % kAhead;
+        if (!bar_wait_peer(base + Shared::kHanded + 8 * s, (i / kAhead) & 1, kTries)) return false;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u) : "r"(base + Shared::kUnits + 4 * s) : "memory");
+        ++i;
+        return true;
+    }
+    // One thread: the number has been read.
+    __device__ __forceinline__ void done() const { bar_arrive_peer(taken + 8 * ((i - 1) % kAhead)); }
+};
+
+// ---- what becomes of a unit's sums ----------------------------------------------------
+
+__device__ __forceinline__ uint32_t swizzled(uint32_t base, int row, int piece) {
+    return base + row * 128 + ((piece ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ void store_shared(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// A row's maximum and sum over 128 of its scores, in powers of 2; the target's score, if it is among them.
+__device__ __forceinline__ float2 reduce_scores(uint32_t tmem, int columns, int target, float *z_target) {
+    float top = kLowest, sum = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 32) {
+        uint32_t v[32];
+        __syncwarp();
+        tmem_load(tmem + c, v);
+        load_wait(v);
+        if (c + 32 > columns)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (c + i >= columns) v[i] = 0xff800000u;
+        float m = __uint_as_float(v[0]);
+#pragma unroll
+        for (int i = 1; i < 31; i += 2) m = max3(m, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+        m = fmaxf(m, __uint_as_float(v[31]));
+        const float now = fmaxf(top, m * kLog2e);
+        float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            s0 += exp2_approx(fmaf(__uint_as_float(v[i]), kLog2e, -now));
+            s1 += exp2_approx(fmaf(__uint_as_float(v[i + 1]), kLog2e, -now));
+        }
+        sum = fmaf(sum, exp2_approx(top - now), s0 + s1);
+        top = now;
+        if ((unsigned)(target - c) < 32u) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (target - c == i) *z_target = __uint_as_float(v[i]);
+        }
+    }
+    return make_float2(top, sum);
+}
+
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+    const float top = fmaxf(a.x, b.x);
+    return make_float2(top, a.y * exp2_approx(a.x - top) + b.y * exp2_approx(b.x - top));
+}
+
+// 64 columns of a row's dz as bf16 pairs, into the warp's rows on their way to memory.
+__device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int lane, int columns, const Token &t,
+                                             int target) {
+#pragma unroll
+    for (int c = 0; c < 64; c += 32) {
+        uint32_t v[32];
+        __syncwarp();
+        tmem_load(tmem + c, v);
+        load_wait(v);
+        float p[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) p[i] = exp2_approx(fmaf(__uint_as_float(v[i]), kLog2e, -t.lse2));
+        if ((unsigned)(target - c) < 32u) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (target - c == i) p[i] -= 1.f;
+        }
+        if (c + 32 > columns)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (c + i >= columns) p[i] = 0.f;
+        uint32_t x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = t.row < 0 ? 0u : pack_bf16(p[2 * i] * t.g, p[2 * i + 1] * t.g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            store_shared(swizzled(stage, lane, c / 8 + i), x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+}
+
+// ---- the kernel -------------------------------------------------------------------------
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Args a) {
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    uint8_t *const mem = raw + (base - smem_addr(raw));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int count = a.head->count;
+    bool failed = false;
+
+    auto full = [&](int s) { return base + Shared::kFullBar + 8 * s; };
+    auto empty = [&](int s) { return base + Shared::kEmptyBar + 8 * s; };
+    if (warp == 0 && elect_one()) {
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(full(s), 1);
+            bar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(base + Shared::kReady + 8 * b, 1);
+            bar_init(base + Shared::kRead + 8 * b, 2 * kRowWarps);
+            for (int q = 0; q < 4; ++q) bar_init(base + Shared::kUpper + 8 * (4 * b + q), 1);
+        }
+        for (int s = 0; s < kAhead; ++s) {
+            bar_init(base + Shared::kHanded + 8 * s, 1);
+            bar_init(base + Shared::kTaken + 8 * s, 2 * kRowWarps + 3);
+        }
+        bar_init_fence();
+    }
+    if (warp == 1) tmem_alloc_pair(base + Shared::kTmem, 512);
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(base + Shared::kTmem) : "memory");
+
+    Units units{base, peer_addr(base + Shared::kTaken, 0)};
+    if (warp == 0) {
+        // ---- copies
+        if (elect_one()) {
+            const CUtensorMap *rows = a.head->all ? &a.hidden : &a.closed;
+            int at = 0, u;  // slots filled
+            while (true) {
+                if ((failed = !units.next(u))) break;
+                units.done();
+                const Unit t = unit_of(a, count, u);
+                if (t.kind == kEnd) break;
+                for (int k = 0; k < t.blocks; ++k, ++at) {
+                    const int s = at % kStages;
+                    if (at >= kStages && !bar_wait_peer(empty(s), ((at / kStages) & 1) ^ 1, kTries)) {
+                        failed = true;
+                        break;
+                    }
+                    const uint32_t bar = peer_addr(full(s), 0), to = base + s * kStageBytes;
+                    if (rank == 0) bar_arrive_expect(full(s), 2 * kStageBytes);
+                    const int m = t.m0 + 128 * rank, n = t.n0 + 128 * rank;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t ta = to + 8192 * j, tb = ta + 16384;
+                        if (t.kind <= kGrad) {
+                            const int v0 = t.kind == kGrad ? a.write * a.piece : 0;
+                            copy_box_pair(ta, rows, 64 * k, m + 64 * j, bar);
+                            copy_box_pair(tb, &a.weight, 64 * k, v0 + n + 64 * j, bar);
+                        } else if (t.kind == kDHidden) {
+                            copy_box_pair(ta, &a.dz[a.read & 1], 64 * k, m + 64 * j, bar);
+                            copy_box_pair(tb, &a.weight, n + 64 * j, a.read * a.piece + 64 * k, bar);
+                        } else {
+                            copy_box_pair(ta, &a.dz[a.read & 1], m + 64 * j, 64 * k, bar);
+                            copy_box_pair(tb, rows, n + 64 * j, 64 * k, bar);
+                        }
+                    }
+                }
+                if (failed) break;
+            }
+            // no copy is in flight when the pair ends, whatever gave up, and no
+            // product's arrival at the second block
+            for (int i = max(0, at - kStages); i < at; ++i)
+                bar_wait_peer(rank == 0 ? full(i % kStages) : empty(i % kStages), (i / kStages) & 1, kTries);
+        }
+    } else if (warp == 1) {
+        // ---- products
+        if (rank == 0 && elect_one()) {
+            int at = 0, sums = 0, u;
+            while (true) {
+                if ((failed = !units.next(u))) break;
+                units.done();
+                const Unit t = unit_of(a, count, u);
+                if (t.kind == kEnd) break;
+                if (t.blocks == 0) continue;
+                const int b = sums & 1;
+                if (sums >= 2 && !bar_wait_peer(base + Shared::kRead + 8 * b, ((sums / 2) & 1) ^ 1, kTries)) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                const bool a_rows = t.kind == kDWeight, b_rows = t.kind >= kDHidden;
+                const uint32_t shape = mma_shape_pair(kTile, a_rows, b_rows), d = tmem + kTile * b;
+                for (int k = 0; k < t.blocks; ++k, ++at) {
+                    const int s = at % kStages;
+                    if (!bar_wait_peer(full(s), (at / kStages) & 1, kTries)) {
+                        failed = true;
+                        break;
+                    }
+                    fence_after();
+                    const uint32_t from = base + s * kStageBytes;
+                    const uint64_t da = a_rows ? desc_k_rows(from, 8192) : desc_k_inside(from);
+                    const uint64_t db = b_rows ? desc_k_rows(from + 16384, 8192) : desc_k_inside(from + 16384);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        mma_ss_pair(d, desc_at(da, a_rows ? 2048 * i : 32 * i), desc_at(db, b_rows ? 2048 * i : 32 * i),
+                                    shape, k > 0 || i > 0);
+                    mma_commit_pair(empty(s));
+                }
+                if (failed) break;
+                mma_commit_pair(base + Shared::kReady + 8 * b);
+                ++sums;
+            }
+            // every arrival of a product on a barrier of the pair has come before it ends
+            for (int i = max(0, at - kStages); i < at; ++i) failed |= !bar_wait_peer(empty(i % kStages), (i / kStages) & 1, kTries);
+            for (int i = max(0, sums - 2); i < sums; ++i)
+                failed |= !bar_wait_peer(base + Shared::kReady + 8 * (i & 1), (i / 2) & 1, kTries);
+        }
+    } else if (warp == 2) {
+        // ---- units
+        if (rank == 0 && elect_one()) {
+            for (int i = 0;; ++i) {
+                const int s = i % kAhead;
+                if (i >= kAhead && !bar_wait_peer(base + Shared::kTaken + 8 * s, ((i / kAhead) & 1) ^ 1, kTries)) {
+                    failed = true;
+                    break;
+                }
+                const int u = atomicAdd(&a.head->next[a.launch], 1);
+                const uint32_t slot = base + Shared::kUnits + 4 * s, bar = base + Shared::kHanded + 8 * s;
+                for (int r = 0; r < 2; ++r) {
+                    store_peer(peer_addr(slot, r), u);
+                    bar_arrive_peer(peer_addr(bar, r));
+                }
+                if (unit_of(a, count, u).kind == kEnd) break;
+            }
+        }
+    } else if (warp >= 4) {
+        // ---- sums: a row and 128 of its columns a thread
+        const int quarter = warp & 3, half = (warp - 4) / 4;
+        const uint32_t stage = base + Shared::kData + (warp - 4) * kStore;
+        const uint32_t read_bar = peer_addr(base + Shared::kRead, 0);
+        int sums = 0, u;
+        while (true) {
+            if (!__all_sync(kFull, units.next(u))) {
+                failed = true;
+                break;
+            }
+            __syncwarp();
+            if (elect_one()) units.done();
+            const Unit t = unit_of(a, count, u);
+            if (t.kind == kEnd) break;
+            const int row0 = t.m0 + 128 * rank + 32 * quarter, row = row0 + lane, column = t.n0 + 128 * half;
+            const int b = sums & 1;
+            const uint32_t from = tmem + ((uint32_t)quarter << 21) + kTile * b + 128 * half;
+            Token token{-1, 0.f, 0.f, -1};
+            if (t.kind != kDWeight && row < count) token = a.tokens[row];
+            if (t.blocks > 0) {
+                if (!__all_sync(kFull, bar_wait_peer(base + Shared::kReady + 8 * b, (sums / 2) & 1, kTries))) {
+                    failed = true;
+                    break;
+                }
+                fence_after();
+                ++sums;
+            }
+            if (t.kind == kScores) {
+                float z = 0.f;
+                const int target = token.target - column;
+                float2 r = reduce_scores(from, a.V - column, target, &z);
+                if (token.row >= 0 && (unsigned)target < 128u) a.z_target[row] = z;
+                // both halves of the row
+                float2 *merge = reinterpret_cast<float2 *>(mem + Shared::kMerge) + 128 * b + 32 * quarter + lane;
+                const uint32_t upper = base + Shared::kUpper + 8 * (4 * b + quarter);
+                __syncwarp();
+                if (half) {
+                    *merge = r;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(upper);
+                } else {
+                    if (!__all_sync(kFull, bar_wait(upper, ((sums - 1) / 2) & 1, kTries))) {
+                        failed = true;
+                        break;
+                    }
+                    if (row < count) a.part[(int64_t)(t.n0 / kTile) * a.T_pad + row] = join(r, *merge);
+                }
+            } else if (t.kind == kGrad) {
+                const int words = min(a.piece, a.V - a.write * a.piece);
+                const int target = token.target - a.write * a.piece - column;
+#pragma unroll 1
+                for (int c = 0; c < 128; c += 64) {
+                    if (lane == 0) stores_read();
+                    __syncwarp();
+                    grad_columns(from + c, stage, lane, words - column - c, token, target - c);
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) store_box(&a.dz_out[a.write & 1], stage, column + c, row0);
+                }
+            } else if (t.kind == kDWeight) {
+                const float g = a.head->g_max;
+#pragma unroll 1
+                for (int c = 0; c < 128; c += 64) {
+                    if (lane == 0) stores_read();
+                    __syncwarp();
+#pragma unroll
+                    for (int h = 0; h < 64; h += 32) {
+                        uint32_t v[32];
+                        if (t.blocks > 0) {
+                            tmem_load(from + c + h, v);
+                            load_wait(v);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = 0;
+                        }
+                        uint32_t x[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            x[i] = pack_bf16(__uint_as_float(v[2 * i]) * g, __uint_as_float(v[2 * i + 1]) * g);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            store_shared(swizzled(stage, lane, h / 8 + i), x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                    // the piece's last tile may reach past it, into words that are not its own
+                    const int v0 = a.read * a.piece + row0;
+                    if (lane == 0 && column + c < a.d && v0 < a.V) store_box(&a.dw, stage, column + c, v0);
+                }
+            } else {
+                const float g = a.head->g_max;
+                const bool first = a.read == 0, last = a.read == a.pieces - 1;
+#pragma unroll 1
+                for (int c = 0; c < 128; c += 32) {
+                    uint32_t v[32];
+                    __syncwarp();
+                    tmem_load(from + c, v);
+                    load_wait(v);
+                    float *acc = a.acc + (int64_t)row * a.d + column + c;
+                    bf16 *out = a.dh + token.row * a.dh_stride + column + c;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        if (token.row < 0 || column + c + i >= a.d) break;
+                        float x[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[i + j]);
+                        if (!first) {
+                            const float4 p = *reinterpret_cast<const float4 *>(acc + i), q = *reinterpret_cast<const float4 *>(acc + i + 4);
+                            x[0] += p.x, x[1] += p.y, x[2] += p.z, x[3] += p.w;
+                            x[4] += q.x, x[5] += q.y, x[6] += q.z, x[7] += q.w;
+                        }
+                        if (last) {
+                            *reinterpret_cast<uint4 *>(out + i) =
+                                make_uint4(pack_bf16(x[0] * g, x[1] * g), pack_bf16(x[2] * g, x[3] * g),
+                                           pack_bf16(x[4] * g, x[5] * g), pack_bf16(x[6] * g, x[7] * g));
+                        } else {
+                            *reinterpret_cast<float4 *>(acc + i) = make_float4(x[0], x[1], x[2], x[3]);
+                            *reinterpret_cast<float4 *>(acc + i + 4) = make_float4(x[4], x[5], x[6], x[7]);
+                        }
+                    }
+                }
+            }
+            if (t.blocks > 0) {
+                fence_before();
+                __syncwarp();
+                if (elect_one()) bar_arrive_peer(read_bar + 8 * b);
+            }
+        }
+        if (lane == 0) stores_done();
+    }
+    if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 1) tmem_free_pair(tmem, 512);
+}
+
+// ---- tokens ---------------------------------------------------------------------------
+
+// The tokens that take part, closed up in their order, by one block: each
+// thread counts its stretch of them, the counts are summed, and each writes
+// its own. Also the largest |grad_loss|, the counters, and what ignored tokens give.
+template <typename I>
+__global__ void __launch_bounds__(1024) prepare_kernel(const __grid_constant__ Args a, const I *targets, int64_t ignore,
+                                                       const float *grad, int grad_stride, const float *lse) {
+    __shared__ int sums[32];
+    __shared__ float tops[32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+    const int64_t each = (a.T + 1023) / 1024, t0 = min(a.T, tid * each), t1 = min(a.T, t0 + each);
+    int n = 0;
+    float top = 0.f;
+    for (int64_t t = t0; t < t1; ++t) {
+        const int64_t y = targets[t];
+        const bool in = y >= 0 && y < a.V && y != ignore;
+        if (!in && y != ignore) set_status(a.status, DPB_DEV_BAD_INDEX);
+        n += in;
+        if (grad && in) {
+            const float g = fabsf(grad[t * grad_stride]);
+            if (g <= 3.402823466e38f) top = fmaxf(top, g);
+        }
+    }
+    int before = n;
+#pragma unroll
+    for (int i = 1; i < 32; i *= 2) {
+        const int x = __shfl_up_sync(kFull, before, i);
+        if (lane >= i) before += x;
+        top = fmaxf(top, __shfl_xor_sync(kFull, top, i));
+    }
+    if (lane == 31) sums[warp] = before;
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+    int total = 0, place = before - n;
+    top = 0.f;
+    for (int w = 0; w < 32; ++w) {
+        if (w < warp) place += sums[w];
+        total += sums[w];
+        top = fmaxf(top, tops[w]);
+    }
+    if (top == 0.f) top = 1.f;
+    if (tid == 0) {
+        a.head->count = total;
+        a.head->all = total == a.T;
+        a.head->g_max = top;
+    }
+    for (int i = tid; i < 60; i += 1024) a.head->next[i] = 0;
+    for (int64_t t = t0; t < t1; ++t) {
+        const int64_t y = targets[t];
+        const bool in = y >= 0 && y < a.V && y != ignore;
+        a.place[t] = in ? place : -1;
+        if (in)
+            a.tokens[place++] = Token{(int)y, lse ? lse[t] * kLog2e : 0.f, grad ? grad[t * grad_stride] / top : 0.f, (int)t};
+        else if (a.loss)
+            a.loss[t] = a.lse[t] = 0.f;
+    }
+}
+
+// Where tokens are left out: the others' rows closed up, and zeros behind them
+// to the end of a tile (a product sums over these); zeros in the gradient of
+// those left out.
+__global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Args a) {
+    if (a.head->all) return;
+    const int lane = threadIdx.x & 31, pieces = a.d / 8;
+    const int64_t warps = (int64_t)gridDim.x * 8, end = min(a.T, (int64_t)(a.head->count + kTile - 1) / kTile * kTile);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    for (int64_t t = blockIdx.x * 8ll + threadIdx.x / 32; t < a.T; t += warps) {
+        const int place = a.place[t];
+        const uint4 *from = reinterpret_cast<const uint4 *>(a.h + t * a.h_stride);
+        uint4 *to = reinterpret_cast<uint4 *>(a.closed_rows + (int64_t)place * a.d);
+        uint4 *dh = reinterpret_cast<uint4 *>(a.dh + t * a.dh_stride);
+        uint4 *rest = reinterpret_cast<uint4 *>(a.closed_rows + t * a.d);
+        for (int i = lane; i < pieces; i += 32) {
+            if (place >= 0) to[i] = from[i];
+            else if (a.dh) dh[i] = none;
+            if (t >= a.head->count && t < end) rest[i] = none;
+        }
+    }
+}
+
+// The tiles' maxima and sums of 32 rows, joined in the tiles' order of each of
+// 32 threads and then of the threads.
+__global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args a) {
+    __shared__ float2 parts[32][33];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x / 32, count = a.head->count;
+    const int tiles = (a.V + kTile - 1) / kTile;
+    const int64_t row = blockIdx.x * 32ll + lane;
+    if (blockIdx.x * 32ll >= count) return;
+    float2 r = make_float2(kLowest, 0.f);
+    if (row < count)
+        for (int i = slice; i < tiles; i += 32) r = join(r, a.part[i * a.T_pad + row]);
+    parts[slice][lane] = r;
+    __syncthreads();
+    r = parts[lane][slice];  // lane: the slice, slice: the row
+#pragma unroll
+    for (int i = 16; i > 0; i /= 2) {
+        const float2 o = make_float2(__shfl_down_sync(kFull, r.x, i), __shfl_down_sync(kFull, r.y, i));
+        r = join(r, o);
+    }
+    const int64_t mine = blockIdx.x * 32ll + slice;
+    if (lane == 0 && mine < count) {
+        const Token t = a.tokens[mine];
+        // the target's score in powers of 2, rounded as the maximum is: a sure row's loss is log2 of its sum alone
+        const double l = log2((double)r.y), z = a.z_target[mine] * kLog2e;
+        a.lse[t.row] = (float)(kLn2 * (r.x + l));
+        a.loss[t.row] = (float)(kLn2 * (r.x - z + l));
+    }
+}
+
+// ---- host side ------------------------------------------------------------------
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) !=
+                cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    }();
+    return fn;
+}
+
+// Map of rows in boxes of 64 columns x `box_rows`; what lies outside reads as zero.
+dpb_status make_map(CUtensorMap *map, const void *data, int64_t stride, int64_t rows, int64_t columns, int box_rows) {
+    const auto fn = encoder();
+    if (!fn) return fail(DPB_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+    const cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? stride : (columns + 7) / 8 * 8) * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(data), dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(DPB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+    return DPB_OK;
+}
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Words of a piece of the gradient.
+constexpr int64_t kPieceBytes = 64ll << 20;
+constexpr int kLeastPiece = 4096, kMostPieces = 48;
+
+struct Space {
+    int64_t T_pad, piece, pieces;
+    size_t head, tokens, place, closed, part, z_target, dz[2], acc, bytes;
+    Space(const dpb_linear_loss_config *c, bool backward) {
+        const size_t T = (size_t)c->tokens, d = (size_t)c->dim, V = (size_t)c->vocab;
+        T_pad = round_up(c->tokens, kTile);
+        piece = std::max<int64_t>(kPieceBytes / (2 * std::max<int64_t>(T_pad, 1)) / kTile * kTile, kLeastPiece);
+        piece = std::max(piece, round_up((c->vocab + kMostPieces - 1) / kMostPieces, kTile));
+        piece = std::min(piece, round_up(c->vocab, kTile));
+        pieces = (c->vocab + piece - 1) / piece;
+        size_t at = kStatusBytes;
+        auto take = [&](size_t n) {
+            const size_t r = at;
+            at += (n + 1023) / 1024 * 1024;
+            return r;
+        };
+        at = 1024;
+        head = take(sizeof(Head));
+        tokens = take(T * sizeof(Token));
+        place = take(T * 4);
+        closed = take(T * d * 2);
+        if (backward) {
+            dz[0] = take((size_t)T_pad * piece * 2);
+            dz[1] = pieces > 1 ? take((size_t)T_pad * piece * 2) : dz[0];
+            acc = pieces > 1 ? take((size_t)T * d * 4) : at;
+            part = z_target = at;
+        } else {
+            part = take((V + kTile - 1) / kTile * (size_t)T_pad * sizeof(float2));
+            z_target = take((size_t)T_pad * 4);
+            dz[0] = dz[1] = acc = at;
+        }
+        bytes = at;
+    }
+};
+
+dpb_status check_config(const dpb_linear_loss_config *c) {
+    if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->dtype != DPB_BF16) return fail(DPB_ERR_UNSUPPORTED, "the linear cross entropy takes bf16 rows");
+    if (c->tokens < 0 || c->vocab < 1 || c->dim < 1) return fail(DPB_ERR_INVALID_ARG, "a size is too small");
+    if (c->tokens > 0x7fffff00ll || c->vocab > 0x7fffff00)
+        return fail(DPB_ERR_UNSUPPORTED, "at most 2^31 - 256 tokens and words");
+    if (c->dim % 8) return fail(DPB_ERR_UNSUPPORTED, "dim must be a multiple of 8");
+    if (c->index_bytes != 4 && c->index_bytes != 8) return fail(DPB_ERR_INVALID_ARG, "index_bytes must be 4 or 8");
+    if (c->grad_stride != 0 && c->grad_stride != 1) return fail(DPB_ERR_INVALID_ARG, "grad_stride must be 0 or 1");
+    return check_slot(c->status_slot);
+}
+
+dpb_status check_rows(const dpb_rows *r, const char *name, int64_t n, int dim) {
+    if (n == 0) return DPB_OK;
+    if (!r) return fail(DPB_ERR_INVALID_ARG, "%s is NULL", name);
+    DPB_CHECK(need(r->data, name, 16));
+    if (n > 1 && (r->stride < dim || r->stride % 8))
+        return fail(DPB_ERR_INVALID_ARG, "the stride of %s must be a multiple of 8, at least dim", name);
+    if (r->stride >= (1ll << 38)) return fail(DPB_ERR_UNSUPPORTED, "the stride of %s is too large", name);
+    return DPB_OK;
+}
+
+int pairs_of_blocks() {
+    int dev = 0, sms = 2;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        cudaGetLastError();
+    return std::max(1, sms / 2);
+}
+
+dpb_status launch_products(const Args &a, int64_t units, cudaStream_t s) {
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(product_kernel), kSmem);
+    if (e != cudaSuccess) return launch_status(e, "linear_cross_entropy");
+    const unsigned pairs = (unsigned)std::max<int64_t>(1, std::min<int64_t>(units, pairs_of_blocks()));
+    product_kernel<<<2 * pairs, kThreads, kSmem, s>>>(a);
+    return launch_status(cudaGetLastError(), "linear_cross_entropy");
+}
+
+// What both directions begin with.
+dpb_status begin(Args &a, const Space &w, const dpb_linear_loss_config *c, const dpb_rows *hidden, const dpb_rows *weight,
+                 const void *targets, const float *grad, const float *lse, uint8_t *ws, cudaStream_t s) {
+    a.h = static_cast<const bf16 *>(hidden->data);
+    a.h_stride = hidden->stride;
+    a.head = reinterpret_cast<Head *>(ws + w.head);
+    a.tokens = reinterpret_cast<Token *>(ws + w.tokens);
+    a.place = reinterpret_cast<int *>(ws + w.place);
+    a.closed_rows = reinterpret_cast<bf16 *>(ws + w.closed);
+    a.T = c->tokens;
+    a.T_pad = w.T_pad;
+    a.V = c->vocab;
+    a.d = c->dim;
+    a.piece = (int)w.piece;
+    a.pieces = (int)w.pieces;
+    DPB_CHECK(make_map(&a.hidden, hidden->data, hidden->stride, c->tokens, c->dim, 64));
+    DPB_CHECK(make_map(&a.closed, a.closed_rows, c->dim, c->tokens, c->dim, 64));
+    DPB_CHECK(make_map(&a.weight, weight->data, weight->stride, c->vocab, c->dim, 64));
+    if (c->index_bytes == 4)
+        prepare_kernel<<<1, 1024, 0, s>>>(a, static_cast<const int32_t *>(targets), c->ignore_index, grad, c->grad_stride, lse);
+    else
+        prepare_kernel<<<1, 1024, 0, s>>>(a, static_cast<const int64_t *>(targets), c->ignore_index, grad, c->grad_stride, lse);
+    DPB_CHECK(launch_status(cudaGetLastError(), "linear_cross_entropy (tokens)"));
+    gather_kernel<<<(unsigned)std::min<int64_t>((c->tokens + 7) / 8, 1216), 256, 0, s>>>(a);
+    return launch_status(cudaGetLastError(), "linear_cross_entropy (rows)");
+}
+
+}  // namespace
+}  // namespace dpb
+
+using namespace dpb;
+
+extern "C" {
+
+dpb_status dpb_linear_cross_entropy_workspace_size(const dpb_linear_loss_config *cfg, int32_t backward, size_t *bytes) {
+    DPB_CHECK(check_config(cfg));
+    if (!bytes) return fail(DPB_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = Space(cfg, backward != 0).bytes;
+    return DPB_OK;
+}
+
+dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
+                                            const dpb_rows *weight, const void *targets, float *loss, float *lse,
+                                            void *workspace, size_t workspace_bytes, void *stream) {
+    DPB_CHECK(check_config(cfg));
+    if (cfg->tokens == 0) return DPB_OK;
+    DPB_CHECK(check_rows(hidden, "hidden", cfg->tokens, cfg->dim));
+    DPB_CHECK(check_rows(weight, "weight", cfg->vocab, cfg->dim));
+    DPB_CHECK(need(targets, "targets", cfg->index_bytes));
+    DPB_CHECK(need(loss, "loss", 4));
+    DPB_CHECK(need(lse, "lse", 4));
+    const Space w(cfg, false);
+    Args a{};
+    DPB_CHECK(place_status(cfg->status_slot, workspace, workspace_bytes, w.bytes, &a.status));
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    a.loss = loss;
+    a.lse = lse;
+    a.part = reinterpret_cast<float2 *>(ws + w.part);
+    a.z_target = reinterpret_cast<float *>(ws + w.z_target);
+    a.write = a.read = -1;
+    DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, nullptr, nullptr, ws, s));
+    DPB_CHECK(launch_products(a, w.T_pad / kTile * ((cfg->vocab + kTile - 1) / kTile), s));
+    join_kernel<<<(unsigned)((cfg->tokens + 31) / 32), 1024, 0, s>>>(a);
+    return launch_status(cudaGetLastError(), "linear_cross_entropy (rows' sums)");
+}
+
+dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
+                                             const dpb_rows *weight, const void *targets, const float *lse,
+                                             const float *grad_loss, const dpb_rows *grad_hidden,
+                                             const dpb_rows *grad_weight, void *workspace, size_t workspace_bytes,
+                                             void *stream) {
+    DPB_CHECK(check_config(cfg));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (grad_weight) DPB_CHECK(check_rows(grad_weight, "grad_weight", cfg->vocab, cfg->dim));
+    if (cfg->tokens == 0) {
+        if (!grad_weight) return DPB_OK;
+        return launch_status(cudaMemset2DAsync(grad_weight->data, (cfg->vocab > 1 ? grad_weight->stride : cfg->dim) * 2ll, 0,
+                                               cfg->dim * 2ll, cfg->vocab, s),
+                             "linear_cross_entropy_backward");
+    }
+    DPB_CHECK(check_rows(hidden, "hidden", cfg->tokens, cfg->dim));
+    DPB_CHECK(check_rows(weight, "weight", cfg->vocab, cfg->dim));
+    if (grad_hidden) DPB_CHECK(check_rows(grad_hidden, "grad_hidden", cfg->tokens, cfg->dim));
+    DPB_CHECK(need(targets, "targets", cfg->index_bytes));
+    DPB_CHECK(need(lse, "lse", 4));
+    DPB_CHECK(need(grad_loss, "grad_loss", 4));
+    const Space w(cfg, true);
+    Args a{};
+    DPB_CHECK(place_status(cfg->status_slot, workspace, workspace_bytes, w.bytes, &a.status));
+    if (!grad_hidden && !grad_weight) return DPB_OK;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    a.want_h = grad_hidden != nullptr;
+    a.want_w = grad_weight != nullptr;
+    if (grad_hidden) a.dh = static_cast<bf16 *>(grad_hidden->data), a.dh_stride = grad_hidden->stride;
+    if (grad_weight) DPB_CHECK(make_map(&a.dw, grad_weight->data, grad_weight->stride, cfg->vocab, cfg->dim, 32));
+    a.acc = reinterpret_cast<float *>(ws + w.acc);
+    for (int i = 0; i < 2; ++i) {
+        DPB_CHECK(make_map(&a.dz[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 64));
+        DPB_CHECK(make_map(&a.dz_out[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 32));
+    }
+    DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, grad_loss, lse, ws, s));
+    const int64_t tiles_m = w.T_pad / kTile, tiles_v = w.piece / kTile, tiles_d = (cfg->dim + kTile - 1) / kTile;
+    for (int i = 0; i <= w.pieces; ++i) {
+        a.write = i < w.pieces ? i : -1;
+        a.read = i - 1;
+        a.launch = i;
+        DPB_CHECK(launch_products(a, (i < w.pieces ? tiles_m * tiles_v : 0) + (i > 0 ? (tiles_m + tiles_v) * tiles_d : 0), s));
+    }
+    return DPB_OK;
+}
+
+}  // extern "C"

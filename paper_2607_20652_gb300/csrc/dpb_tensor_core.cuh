@@ -1,6 +1,7 @@
-// dpb_tensor_core.cuh -- the sm_103a instructions of the attention kernels as
-// device functions: mbarriers with bounded waits, tensor-map copies, tensor
-// memory (TMEM) and its matrix products.
+// dpb_tensor_core.cuh -- the sm_103a instructions of the attention and the
+// vocabulary loss kernels as device functions: mbarriers with bounded waits,
+// tensor-map copies, tensor memory (TMEM) and its matrix products, by one block
+// or by a pair of blocks.
 #pragma once
 
 #include <cuda.h>
@@ -165,6 +166,97 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+
+// ---- pairs of blocks ---------------------------------------------------------------
+//
+// Two blocks of a cluster share a product of 256 rows: each holds 128 rows of A,
+// half of B's columns and the sums of its own 128 rows, all at the same shared
+// and TMEM addresses. The block of rank 0 issues.
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// `addr` of this block's shared memory as the block of `rank` has it.
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Arrives on a barrier of either block (an address from peer_addr).
+__device__ __forceinline__ void bar_arrive_peer(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// bar_wait where arrivals may come from the other block.
+__device__ __forceinline__ bool bar_wait_peer(uint32_t bar, uint32_t parity, uint32_t tries) {
+    for (uint32_t i = 0; i < tries; ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+__device__ __forceinline__ void store_peer(uint32_t addr, int v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+// One box of a [rows][columns] tensor into this block's shared memory; its
+// bytes count on `bar`, which may be the other block's.
+__device__ __forceinline__ void copy_box_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
+        "%3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t slot, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t tmem, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
+}
+// bf16 x bf16 -> fp32, M = 256 over both blocks, N = n; *_k_rows: that operand's rows run along K.
+__host__ __device__ constexpr uint32_t mma_shape_pair(int n, bool a_k_rows, bool b_k_rows) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (a_k_rows ? 1u << 15 : 0u) | (b_k_rows ? 1u << 16 : 0u) |
+           ((uint32_t)(n / 8) << 17) | (16u << 24);
+}
+__device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+        : "memory");
+}
+// `bar` of both blocks is arrived on once every product issued so far by this thread is done.
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
+}
+
+// ---- copies to memory ---------------------------------------------------------------
+
+// One box of shared memory to a [rows][columns] tensor; what lies outside of it is left out.
+__device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x),
+                 "r"(y), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// This thread's stores have read their shared memory; are in memory.
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // ---- blocks that have not started -----------------------------------------------
 

@@ -70,6 +70,9 @@ class Config(ctypes.Structure):
 _ROPE = struct.Struct("=q8ifi")
 _ATTENTION = struct.Struct("=qq8ifi")
 _ROWS = {n: struct.Struct(f"={3 * n}q") for n in (4, 6, 8)}
+# dpb_linear_loss_config and up to four dpb_rows (16 bytes each)
+_LOSS = struct.Struct("=qiiqiiii")
+_PLAIN_ROWS = {n: struct.Struct(f"={2 * n}q") for n in (2, 4)}
 
 
 class _Arguments(threading.local):
@@ -99,7 +102,9 @@ EXPORTS = ("dpb_plan_create", "dpb_plan_destroy", "dpb_plan_config", "dpb_plan_t
            "dpb_workspace_status", "dpb_status_string", "dpb_last_error", "dpb_encode_noalloc",
            "dpb_stats_accumulate", "dpb_stats_update", "dpb_forward", "dpb_debug_set_wait_limit", "dpb_status_word",
            "dpb_qk_norm_rope", "dpb_qk_norm_rope_backward", "dpb_rope_workspace_size",
-           "dpb_attention_forward", "dpb_attention_backward", "dpb_attention_workspace_size", "dpb_adamw_step")
+           "dpb_attention_forward", "dpb_attention_backward", "dpb_attention_workspace_size", "dpb_adamw_step",
+           "dpb_linear_cross_entropy_forward", "dpb_linear_cross_entropy_backward",
+           "dpb_linear_cross_entropy_workspace_size")
 
 
 def library_path() -> str:
@@ -142,6 +147,9 @@ def load(path: Optional[str] = None):
     lib.dpb_attention_backward.argtypes = [ac, hp, hp, hp, hp, vp, hp, vp, vp, hp, hp, hp, vp, sz, vp]
     lib.dpb_attention_workspace_size.argtypes = [ac, ctypes.POINTER(sz)]
     lib.dpb_adamw_step.argtypes = [ctypes.POINTER(AdamWConfig), vp, ctypes.c_int32, vp]
+    lib.dpb_linear_cross_entropy_forward.argtypes = [rc, hp, hp, vp, vp, vp, vp, sz, vp]
+    lib.dpb_linear_cross_entropy_backward.argtypes = [rc, hp, hp, vp, vp, vp, hp, hp, vp, sz, vp]
+    lib.dpb_linear_cross_entropy_workspace_size.argtypes = [rc, ctypes.c_int32, ctypes.POINTER(sz)]
     lib.dpb_status_string.argtypes = [st]
     lib.dpb_status_string.restype = ctypes.c_char_p
     lib.dpb_last_error.argtypes = []
@@ -832,3 +840,109 @@ class AdamWGroup:
                         _dense(grad_scale, "grad_scale", torch.float32, 1, dev), F32 if dt is torch.float32 else BF16,
                         self.state_bits)
         _check(load().dpb_adamw_step(c, self._table_at, len(ps), _raw_stream(dev)))
+
+
+# ---- both ends of the model, and the stream between them --------------------
+
+
+def _plain_rows(t: torch.Tensor, name: str, dtype, shape, device):
+    """(address, row stride) of a [rows, dim] tensor whose last dimension is dense."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {list(shape)} on {device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+    if st[1] != 1 and shape[1] > 1:
+        raise ValueError(f"the last dimension of {name} must be dense")
+    return t.data_ptr(), st[0]
+
+
+def _indices(t: torch.Tensor, name: str, n: int, device):
+    """(address, bytes of an index) of n int32 or int64 indices."""
+    if t.dtype not in (torch.int64, torch.int32) or t.device != device or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{name} must be a contiguous int32 or int64 tensor of {n} values on {device}")
+    return t.data_ptr(), t.element_size()
+
+
+def _loss_config(hidden, weight, targets, ignore_index, grad_stride, slot):
+    """Writes the config; the targets' address."""
+    if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
+        raise ValueError(f"hidden must be [tokens, dim] and weight [vocab, dim], got {list(hidden.shape)} and "
+                         f"{list(weight.shape)}")
+    if hidden.dtype is not torch.bfloat16:
+        raise ValueError(f"hidden and weight must be bfloat16, got {hidden.dtype}")
+    T, d = hidden.shape
+    at, size = _indices(targets, "targets", T, hidden.device)
+    _LOSS.pack_into(_arguments.buf, 0, T, weight.shape[0], d, ignore_index, size, BF16, grad_stride, slot)
+    return at
+
+
+def _loss_workspace(backward: int, device):
+    n = ctypes.c_size_t()
+    _check(load().dpb_linear_cross_entropy_workspace_size(_arguments.at, backward, n))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)  # scratch of this call
+
+
+def linear_cross_entropy_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                                 ignore_index: int = -100, loss=None, lse=None, workspace=None, stream=None):
+    """dpb_linear_cross_entropy_forward. hidden [T, d], weight [V, d] bf16,
+    targets int32 or int64 [T]. Returns (loss, lse), fp32 [T]: the cross entropy
+    of each token's scores hidden weight^T and the log of the sum of their
+    exponentials, both 0 where the target is ``ignore_index``."""
+    dev = hidden.device
+    if _away(dev, stream):
+        return _elsewhere(linear_cross_entropy_forward, stream, dev,
+                          (hidden, weight, targets, ignore_index, loss, lse, workspace), {})
+    s = _raw_stream(dev)
+    at = _loss_config(hidden, weight, targets, ignore_index, 0, _status_slot(dev, s) if workspace is None else 0)
+    a, T, bf = _arguments, hidden.shape[0], torch.bfloat16
+    loss = torch.empty(T, dtype=torch.float32, device=dev) if loss is None else loss
+    lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else lse
+    if workspace is None:
+        workspace = _loss_workspace(0, dev)
+    _PLAIN_ROWS[2].pack_into(a.buf, 64, *_plain_rows(hidden, "hidden", bf, hidden.shape, dev),
+                             *_plain_rows(weight, "weight", bf, weight.shape, dev))
+    h = a.rows
+    _check(load().dpb_linear_cross_entropy_forward(a.at, h, h + 16, at, _dense(loss, "loss", torch.float32, T, dev),
+                                                   _dense(lse, "lse", torch.float32, T, dev), workspace.data_ptr(),
+                                                   workspace.nbytes, s))
+    return loss, lse
+
+
+def linear_cross_entropy_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                                  grad_loss: torch.Tensor, ignore_index: int = -100, want_hidden: bool = True,
+                                  want_weight: bool = True, grad_hidden=None, grad_weight=None, workspace=None,
+                                  stream=None):
+    """dpb_linear_cross_entropy_backward with the forward's inputs and lse, and
+    grad_loss = dL/dloss, fp32 [T] (one value expanded to [T] is read as one).
+    Returns (grad_hidden [T, d], grad_weight [V, d]); None for one that is not
+    wanted."""
+    dev = hidden.device
+    if _away(dev, stream):
+        return _elsewhere(linear_cross_entropy_backward, stream, dev,
+                          (hidden, weight, targets, lse, grad_loss, ignore_index, want_hidden, want_weight, grad_hidden,
+                           grad_weight, workspace), {})
+    s = _raw_stream(dev)
+    T, bf = hidden.shape[0], torch.bfloat16
+    if grad_loss.dtype is not torch.float32 or grad_loss.shape != (T,) or grad_loss.device != dev:
+        raise ValueError(f"grad_loss must be a float32 tensor of shape [{T}] on {dev}")
+    step = grad_loss.stride(0) if T > 1 else 0
+    if step not in (0, 1):
+        raise ValueError("grad_loss must be contiguous or one value expanded")
+    at = _loss_config(hidden, weight, targets, ignore_index, step, _status_slot(dev, s) if workspace is None else 0)
+    a = _arguments
+    if workspace is None:
+        workspace = _loss_workspace(1, dev)
+    if want_hidden and grad_hidden is None:
+        grad_hidden = torch.empty(hidden.shape, dtype=bf, device=dev)
+    if want_weight and grad_weight is None:
+        grad_weight = torch.empty(weight.shape, dtype=bf, device=dev)
+    _PLAIN_ROWS[4].pack_into(a.buf, 64, *_plain_rows(hidden, "hidden", bf, hidden.shape, dev),
+                             *_plain_rows(weight, "weight", bf, weight.shape, dev),
+                             *(_plain_rows(grad_hidden, "grad_hidden", bf, hidden.shape, dev) if want_hidden else (0, 0)),
+                             *(_plain_rows(grad_weight, "grad_weight", bf, weight.shape, dev) if want_weight else (0, 0)))
+    h = a.rows
+    _check(load().dpb_linear_cross_entropy_backward(a.at, h, h + 16, at, _dense(lse, "lse", torch.float32, T, dev),
+                                                    grad_loss.data_ptr(), h + 32 if want_hidden else None,
+                                                    h + 48 if want_weight else None, workspace.data_ptr(),
+                                                    workspace.nbytes, s))
+    return grad_hidden if want_hidden else None, grad_weight if want_weight else None

@@ -546,6 +546,75 @@ typedef struct dpb_rows {
 } dpb_rows;
 
 /*
+ * dpb_embedding -- y_t = scale weight[id_t], rounded to the rows' type.
+ *   tokens, vocab, dim   each below 2^31 - 256, dim at most 2^24
+ *   index_bytes 4 or 8: ids are int32 or int64 [tokens]
+ *   dtype       dpb_dtype of the rows
+ *   scale       finite
+ * An id outside [0, vocab) sets DPB_DEV_BAD_INDEX; its row of y is 0. Rows may
+ * have any alignment their type allows and any stride of at least dim; those
+ * whose rows start at multiples of 16 bytes are faster.
+ */
+typedef struct dpb_embedding_config {
+    int64_t tokens;
+    int32_t vocab, dim, index_bytes, dtype;
+    float scale;
+    int32_t status_slot;
+} dpb_embedding_config;
+
+dpb_status dpb_embedding(const dpb_embedding_config *cfg, const dpb_rows *weight, const void *ids, const dpb_rows *y,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dpb_embedding_backward -- grad_weight[v] = scale times the sum of grad_y_t over
+ * the tokens of id v, in full: rows of ids that do not occur are written with 0.
+ * Tokens with an id outside [0, vocab) set DPB_DEV_BAD_INDEX and are left out.
+ * The tokens are sorted by id; sums are fp32, in an order that the ids alone fix,
+ * and rounded once.
+ */
+dpb_status dpb_embedding_backward(const dpb_embedding_config *cfg, const dpb_rows *grad_y, const void *ids,
+                                  const dpb_rows *grad_weight, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace bytes of dpb_embedding_backward (256-byte aligned; zeroed once, unless
+ * status_slot says otherwise); dpb_embedding needs 256 with status_slot 0. */
+dpb_status dpb_embedding_workspace_size(const dpb_embedding_config *cfg, size_t *bytes);
+
+/*
+ * dpb_add_norm -- the residual's addition and the RMS norm behind it:
+ *   total = x + delta, rounded to the rows' type;  y = weight total (mean total^2 + eps)^{-1/2}
+ *   dim         1..16384
+ *   dtype       dpb_dtype of every row and of the weight
+ *   eps         at least 0
+ * delta: nullable (total = x). weight: [dim], nullable (ones). total: nullable
+ * (not written). y and total may be x or delta themselves (same strides). Rows
+ * may have any alignment their type allows and any stride of at least dim; those
+ * that start at multiples of 16 bytes are faster. Sums are fp32.
+ */
+typedef struct dpb_norm_config {
+    int64_t tokens;
+    int32_t dim, dtype;
+    float eps;
+    int32_t reserved;
+} dpb_norm_config;
+
+dpb_status dpb_add_norm(const dpb_norm_config *cfg, const dpb_rows *x, const dpb_rows *delta, const void *weight,
+                        const dpb_rows *y, const dpb_rows *total, void *stream);
+
+/*
+ * dpb_add_norm_backward -- the gradient of x, and of delta, which is the same:
+ * with r = (mean total^2 + eps)^{-1/2} and u = weight grad_y,
+ *   grad_x = grad_total + r u - total r^3 mean(u total),  grad_weight = sum_t grad_y total r.
+ * total is the forward's; grad_total (nullable) what comes back along the
+ * residual. grad_x may be any of the three rows given. grad_weight: fp32 [dim],
+ * nullable, written (not added to); its sums are taken in a fixed order. The
+ * workspace (256-byte aligned) is scratch for it, of the call alone.
+ */
+dpb_status dpb_add_norm_backward(const dpb_norm_config *cfg, const dpb_rows *total, const dpb_rows *grad_y,
+                                 const dpb_rows *grad_total, const void *weight, const dpb_rows *grad_x,
+                                 float *grad_weight, void *workspace, size_t workspace_bytes, void *stream);
+dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
+
+/*
  * dpb_linear_cross_entropy_forward -- cross entropy of the rows' scores over the
  * vocabulary, without a tensor of tokens x vocabulary:
  *   z_t = hidden_t weight^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_t,target

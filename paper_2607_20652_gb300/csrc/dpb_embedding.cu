@@ -1,0 +1,425 @@
+// dpb_embedding.cu -- embedding lookup with a scale, and its gradient by sorted
+// tokens.
+//
+//   y_t = scale W[id_t],   dW[v] = scale sum over id_t = v of dy_t
+//
+// Memory bounds both. The gradient sorts the tokens by their ids first (stable,
+// so that a row's sum has the tokens' own order), in one cluster of blocks
+// while the others write the zeros of dW, and then sums stretches of the
+// sorted tokens: a warp each, whatever rows they belong to, so that a token
+// met thousands of times costs no more than as many different ones. A row
+// whose tokens lie in several stretches is joined from their partial sums in
+// the stretches' order. No atomics on values: equal inputs give equal bits.
+#include <algorithm>
+
+#include "dpb_checks.h"
+#include "dpb_device.cuh"
+#include "dpb_rows.cuh"
+#include "dpb_tensor_core.cuh"
+
+namespace dpb {
+namespace {
+
+constexpr int kSortBlocks = 8;    // of the sorting cluster
+constexpr int kSortWarps = 32;    // of a block
+constexpr int kDigits = 256;      // 8 bits a pass
+
+// A token on its way: its id (vocab: none that counts) and its place.
+struct Sorted {
+    int id, token;
+};
+
+struct LookupArgs {
+    const void *w, *dy;
+    void *y, *dw;
+    int64_t ws, ys, dys, dws;  // strides
+    int64_t T;
+    int V, d, passes, stretch;
+    int64_t stretches;
+    float scale;
+    Sorted *sorted[2];
+    float *head, *tail;  // [stretches][d]: sums of the first row, begun before, and of the last, begun here and going on
+    int32_t *status;
+};
+
+// ---- lookup -------------------------------------------------------------------------
+
+// `lanes` lanes (a power of 2) copy a row.
+template <typename E, int N, typename I>
+__global__ void __launch_bounds__(256) embedding_kernel(const LookupArgs a, const I *ids, int lanes) {
+    const int pieces = (a.d + N - 1) / N, in = threadIdx.x & (lanes - 1);
+    const int64_t rows = (int64_t)gridDim.x * (256 / lanes);
+    for (int64_t t = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes; t < a.T; t += rows) {
+        const int64_t id = ids[t];
+        const bool ok = id >= 0 && id < a.V;
+        if (!ok && in == 0) set_status(a.status, DPB_DEV_BAD_INDEX);
+        const E *w = static_cast<const E *>(a.w) + (ok ? id : 0) * a.ws;
+        E *y = static_cast<E *>(a.y) + t * a.ys;
+#pragma unroll 4
+        for (int i = in; i < pieces; i += lanes) {
+            Piece<E, N> v;
+            load_piece(w + i * N, v);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v.v[j] = ok ? v.v[j] * a.scale : 0.f;
+            store_piece(y + i * N, v);
+        }
+    }
+}
+
+// ---- gradient: order, and zeros -------------------------------------------------------
+
+__device__ __forceinline__ int read_peer(uint32_t addr) {
+    int v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// The first cluster sorts, a digit of 8 bits a pass: each warp counts the
+// digits of its stretch of the tokens, the counts of all warps before it give
+// each digit's first place, and it puts its tokens there in their order.
+// The other clusters write zeros.
+template <typename E, int N, typename I>
+__global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSortWarps, 1)
+    embedding_sort_kernel(const LookupArgs a, const I *ids) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+    if (blockIdx.x >= kSortBlocks) {
+        const int pieces = (a.d + N - 1) / N;
+        const int64_t warps = (int64_t)(gridDim.x - kSortBlocks) * kSortWarps;
+        Piece<E, N> none;
+#pragma unroll
+        for (int j = 0; j < N; ++j) none.v[j] = 0.f;
+        for (int64_t v = (int64_t)(blockIdx.x - kSortBlocks) * kSortWarps + warp; v < a.V; v += warps)
+            for (int i = lane; i < pieces; i += 32) store_piece(static_cast<E *>(a.dw) + v * a.dws + i * N, none);
+        return;
+    }
+    __shared__ int count[kSortWarps][kDigits], total[kDigits], sums[kDigits / 32];
+    const uint32_t rank = blockIdx.x;
+    const int64_t each = ((a.T + kSortBlocks * kSortWarps - 1) / (kSortBlocks * kSortWarps) + 31) / 32 * 32;
+    const int64_t t0 = (rank * kSortWarps + warp) * each, t1 = min(a.T, t0 + each);
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const Sorted *from = a.sorted[(pass & 1) ^ 1];
+        Sorted *to = a.sorted[pass & 1];
+        auto token = [&](int64_t t) {
+            if (pass > 0) return from[t];
+            const int64_t id = ids[t];
+            if (id >= 0 && id < a.V) return Sorted{(int)id, (int)t};
+            set_status(a.status, DPB_DEV_BAD_INDEX);
+            return Sorted{a.V, (int)t};
+        };
+        for (int i = tid; i < kSortWarps * kDigits; i += 32 * kSortWarps) (&count[0][0])[i] = 0;
+        __syncthreads();
+        for (int64_t t = t0; t < t1; t += 32) {
+            const bool live = t + lane < t1;
+            const int digit = live ? (token(t + lane).id >> (8 * pass)) & 255 : -1;
+            const unsigned same = __match_any_sync(kFull, digit);
+            if (live && lane == __ffs(same) - 1) count[warp][digit] += __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        if (tid < kDigits) {  // the block's warps before each
+            int n = 0;
+            for (int w = 0; w < kSortWarps; ++w) {
+                const int c = count[w][tid];
+                count[w][tid] = n;
+                n += c;
+            }
+            total[tid] = n;
+        }
+        tc::cluster_sync();
+        int before = 0, all = 0, upto = 0;
+        if (tid < kDigits) {
+            const uint32_t at = tc::smem_addr(&total[tid]);
+            for (uint32_t r = 0; r < kSortBlocks; ++r) {
+                const int n = read_peer(tc::peer_addr(at, r));
+                if (r < rank) before += n;
+                all += n;
+            }
+            upto = all;
+#pragma unroll
+            for (int i = 1; i < 32; i *= 2) {
+                const int n = __shfl_up_sync(kFull, upto, i);
+                if (lane >= i) upto += n;
+            }
+            if (lane == 31) sums[warp] = upto;
+        }
+        __syncthreads();
+        if (tid < kDigits) {
+            int first = upto - all + before;
+            for (int w = 0; w < warp; ++w) first += sums[w];
+            for (int w = 0; w < kSortWarps; ++w) count[w][tid] += first;
+        }
+        __syncthreads();
+        for (int64_t t = t0; t < t1; t += 32) {
+            const bool live = t + lane < t1;
+            const Sorted x = live ? token(t + lane) : Sorted{0, 0};
+            const int digit = live ? (x.id >> (8 * pass)) & 255 : -1;
+            const unsigned same = __match_any_sync(kFull, digit);
+            const int place = live ? count[warp][digit] + __popc(same & ((1u << lane) - 1)) : 0;
+            __syncwarp();
+            if (live) {
+                to[place] = x;
+                if (lane == __ffs(same) - 1) count[warp][digit] += __popc(same);
+            }
+            __syncwarp();
+        }
+        // the others have read this block's totals, and all tokens are in place
+        tc::cluster_sync();
+    }
+}
+
+// ---- gradient: sums ---------------------------------------------------------------------
+
+// A warp sums one stretch of the sorted tokens over 32 P N columns.
+template <typename E, int N, int P>
+__global__ void __launch_bounds__(256) embedding_sum_kernel(const LookupArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int64_t c = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    if (c >= a.stretches) return;
+    const Sorted *sorted = a.sorted[(a.passes - 1) & 1];
+    const int64_t p0 = c * a.stretch, p1 = min(a.T, p0 + a.stretch);
+    const int column = blockIdx.y * 32 * P * N + lane * N;
+    float acc[P][N];
+    auto clear = [&] {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[p][j] = 0.f;
+    };
+    clear();
+    int id = -1;
+    bool whole = true;  // the row's tokens begin in this stretch
+    const int prev = p0 > 0 ? sorted[p0 - 1].id : -1, next = p1 < a.T ? sorted[p1].id : -1;
+    auto flush = [&](bool ends) {
+        if (id < 0 || id >= a.V) return;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = column + p * 32 * N;
+            if (i >= a.d) continue;
+            if (whole && ends) {
+                Piece<E, N> v;
+#pragma unroll
+                for (int j = 0; j < N; ++j) v.v[j] = acc[p][j] * a.scale;
+                store_piece(static_cast<E *>(a.dw) + id * a.dws + i, v);
+            } else {
+                float *to = (whole ? a.tail : a.head) + c * a.d + i;
+#pragma unroll
+                for (int j = 0; j < N; ++j) to[j] = acc[p][j];
+            }
+        }
+    };
+    for (int64_t b = p0; b < p1; b += 32) {
+        const Sorted mine = b + lane < p1 ? sorted[b + lane] : Sorted{-1, 0};
+        const int n = (int)min((int64_t)32, p1 - b);
+        constexpr int kAtOnce = 4;
+        for (int k0 = 0; k0 < n; k0 += kAtOnce) {
+            Piece<E, N> v[kAtOnce][P];
+            int ids[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                ids[k] = __shfl_sync(kFull, mine.id, (k0 + k) & 31);
+                const int64_t t = __shfl_sync(kFull, mine.token, (k0 + k) & 31);
+                if (k0 + k >= n) ids[k] = a.V;
+                const E *dy = static_cast<const E *>(a.dy) + t * a.dys;
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    if (ids[k] < a.V && column + p * 32 * N < a.d) load_piece(dy + column + p * 32 * N, v[k][p]);
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                if (k0 + k >= n) break;
+                if (ids[k] != id) {
+                    flush(true);
+                    clear();
+                    id = ids[k];
+                    whole = b + k0 + k > p0 || id != prev;
+                }
+                if (id < a.V)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        if (column + p * 32 * N < a.d)
+#pragma unroll
+                            for (int j = 0; j < N; ++j) acc[p][j] += v[k][p].v[j];
+            }
+        }
+    }
+    flush(id != next);
+}
+
+// A row whose tokens go on after the stretch where they begin: the sum of what
+// each stretch has of it.
+template <typename E>
+__global__ void __launch_bounds__(256) embedding_join_kernel(const LookupArgs a) {
+    const int64_t c = blockIdx.x;
+    const Sorted *sorted = a.sorted[(a.passes - 1) & 1];
+    const int64_t p0 = c * a.stretch, end = p0 + a.stretch;
+    if (end >= a.T) return;
+    const int id = sorted[end - 1].id;
+    if (id >= a.V || sorted[end].id != id) return;
+    // it begins here, if its first token is here
+    if (p0 > 0 && sorted[p0].id == id && sorted[p0 - 1].id == id) return;
+    int64_t last = c + 1;  // the stretch where it ends
+    for (int64_t step = 1; step > 0;) {  // the last one whose first token is of this row
+        if (last + step < a.stretches && sorted[(last + step) * a.stretch].id == id) {
+            last += step;
+            step *= 2;
+        } else {
+            step /= 2;
+        }
+    }
+    for (int i = threadIdx.x; i < a.d; i += 256) {
+        float v = a.tail[c * a.d + i];
+        int64_t k = c + 1;
+        for (; k + 8 <= last + 1; k += 8) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = a.head[(k + j) * a.d + i];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v += x[j];
+        }
+        for (; k <= last; ++k) v += a.head[k * a.d + i];
+        st_elem(static_cast<E *>(a.dw), id * a.dws + i, v * a.scale);
+    }
+}
+
+// ---- host side ------------------------------------------------------------------
+
+int passes_of(int V) {
+    int n = 1;
+    while (n < 4 && ((int64_t)1 << (8 * n)) <= V) ++n;  // ids up to V
+    return n;
+}
+
+struct GradSpace {
+    int stretch;
+    int64_t stretches;
+    size_t sorted[2], head, tail, bytes;
+    explicit GradSpace(const dpb_embedding_config *c) {
+        // Short stretches where there are few tokens, so that all SMs have some.
+        stretch = c->tokens > 16384 ? 32 : 8;
+        stretches = (c->tokens + stretch - 1) / stretch;
+        auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+        sorted[0] = kStatusBytes;
+        sorted[1] = sorted[0] + up((size_t)c->tokens * sizeof(Sorted));
+        head = sorted[1] + up((size_t)c->tokens * sizeof(Sorted));
+        tail = head + up((size_t)stretches * c->dim * 4);
+        bytes = tail + up((size_t)stretches * c->dim * 4);
+    }
+};
+
+dpb_status check_config(const dpb_embedding_config *c) {
+    if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->dtype != DPB_F32 && c->dtype != DPB_BF16) return fail(DPB_ERR_INVALID_ARG, "dtype must be DPB_F32 or DPB_BF16");
+    if (c->tokens < 0 || c->vocab < 1 || c->dim < 1) return fail(DPB_ERR_INVALID_ARG, "a size is too small");
+    if (c->tokens > 0x7fffff00ll || c->vocab > 0x7fffff00 || c->dim > (1 << 24))
+        return fail(DPB_ERR_UNSUPPORTED, "at most 2^31 - 256 tokens and words, 2^24 columns");
+    if (c->index_bytes != 4 && c->index_bytes != 8) return fail(DPB_ERR_INVALID_ARG, "index_bytes must be 4 or 8");
+    if (!(c->scale - c->scale == 0.f)) return fail(DPB_ERR_INVALID_ARG, "scale must be finite");
+    return check_slot(c->status_slot);
+}
+
+dpb_status check_rows(const dpb_embedding_config *c, const dpb_rows *r, int64_t n, const char *name) {
+    if (n == 0) return DPB_OK;
+    if (!r) return fail(DPB_ERR_INVALID_ARG, "%s is NULL", name);
+    DPB_CHECK(need(r->data, name, c->dtype == DPB_F32 ? 4 : 2));
+    if (n > 1 && r->stride < c->dim) return fail(DPB_ERR_INVALID_ARG, "the stride of %s must be at least dim", name);
+    return DPB_OK;
+}
+
+template <typename E, int N>
+dpb_status lookup(const LookupArgs &a, const void *ids, int index_bytes, cudaStream_t s) {
+    const int pieces = (a.d + N - 1) / N;
+    int lanes = 1;
+    while (lanes < 32 && lanes < pieces) lanes *= 2;
+    const unsigned blocks = (unsigned)std::min<int64_t>((a.T * lanes + 255) / 256, 1 << 20);
+    if (index_bytes == 4)
+        embedding_kernel<E, N><<<blocks, 256, 0, s>>>(a, static_cast<const int32_t *>(ids), lanes);
+    else
+        embedding_kernel<E, N><<<blocks, 256, 0, s>>>(a, static_cast<const int64_t *>(ids), lanes);
+    return launch_status(cudaGetLastError(), "embedding");
+}
+
+template <typename E, int N>
+dpb_status gradient(const LookupArgs &a, const void *ids, int index_bytes, cudaStream_t s) {
+    const int others = std::max(1, std::min(sms_of_device() / kSortBlocks - 1, (a.V + 255) / 256));
+    const unsigned blocks = kSortBlocks * (1 + others);
+    if (index_bytes == 4)
+        embedding_sort_kernel<E, N><<<blocks, 32 * kSortWarps, 0, s>>>(a, static_cast<const int32_t *>(ids));
+    else
+        embedding_sort_kernel<E, N><<<blocks, 32 * kSortWarps, 0, s>>>(a, static_cast<const int64_t *>(ids));
+    DPB_CHECK(launch_status(cudaGetLastError(), "embedding_backward (order)"));
+    constexpr int P = N == 1 ? 8 : 4;
+    const dim3 grid((unsigned)((a.stretches + 7) / 8), (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
+    if (grid.y > 65535) return fail(DPB_ERR_UNSUPPORTED, "dim is too large");
+    embedding_sum_kernel<E, N, P><<<grid, 256, 0, s>>>(a);
+    DPB_CHECK(launch_status(cudaGetLastError(), "embedding_backward (sums)"));
+    embedding_join_kernel<E><<<(unsigned)a.stretches, 256, 0, s>>>(a);
+    return launch_status(cudaGetLastError(), "embedding_backward (rows)");
+}
+
+}  // namespace
+}  // namespace dpb
+
+using namespace dpb;
+
+extern "C" {
+
+dpb_status dpb_embedding(const dpb_embedding_config *cfg, const dpb_rows *weight, const void *ids, const dpb_rows *y,
+                         void *workspace, size_t workspace_bytes, void *stream) {
+    DPB_CHECK(check_config(cfg));
+    if (cfg->tokens == 0) return DPB_OK;
+    DPB_CHECK(check_rows(cfg, weight, cfg->vocab, "weight"));
+    DPB_CHECK(check_rows(cfg, y, cfg->tokens, "y"));
+    DPB_CHECK(need(ids, "ids", cfg->index_bytes));
+    LookupArgs a{};
+    DPB_CHECK(place_status(cfg->status_slot, workspace, workspace_bytes, kStatusBytes, &a.status));
+    a.w = weight->data, a.ws = weight->stride;
+    a.y = y->data, a.ys = y->stride;
+    a.T = cfg->tokens, a.V = cfg->vocab, a.d = cfg->dim, a.scale = cfg->scale;
+    const int elem = cfg->dtype == DPB_F32 ? 4 : 2;
+    const bool pieces = by_pieces(a.w, a.ws, a.V, elem) && by_pieces(a.y, a.ys, a.T, elem) && a.d * elem % 16 == 0;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    using bf16 = __nv_bfloat16;
+    if (cfg->dtype == DPB_F32)
+        return pieces ? lookup<float, 4>(a, ids, cfg->index_bytes, s) : lookup<float, 1>(a, ids, cfg->index_bytes, s);
+    return pieces ? lookup<bf16, 8>(a, ids, cfg->index_bytes, s) : lookup<bf16, 1>(a, ids, cfg->index_bytes, s);
+}
+
+dpb_status dpb_embedding_workspace_size(const dpb_embedding_config *cfg, size_t *bytes) {
+    DPB_CHECK(check_config(cfg));
+    if (!bytes) return fail(DPB_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = GradSpace(cfg).bytes;
+    return DPB_OK;
+}
+
+dpb_status dpb_embedding_backward(const dpb_embedding_config *cfg, const dpb_rows *grad_y, const void *ids,
+                                  const dpb_rows *grad_weight, void *workspace, size_t workspace_bytes, void *stream) {
+    DPB_CHECK(check_config(cfg));
+    DPB_CHECK(check_rows(cfg, grad_weight, cfg->vocab, "grad_weight"));
+    const int elem = cfg->dtype == DPB_F32 ? 4 : 2;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (cfg->tokens == 0)
+        return launch_status(cudaMemset2DAsync(grad_weight->data, (cfg->vocab > 1 ? grad_weight->stride : cfg->dim) * elem, 0,
+                                               (size_t)cfg->dim * elem, cfg->vocab, s),
+                             "embedding_backward");
+    DPB_CHECK(check_rows(cfg, grad_y, cfg->tokens, "grad_y"));
+    DPB_CHECK(need(ids, "ids", cfg->index_bytes));
+    const GradSpace w(cfg);
+    LookupArgs a{};
+    DPB_CHECK(place_status(cfg->status_slot, workspace, workspace_bytes, w.bytes, &a.status));
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    a.dy = grad_y->data, a.dys = grad_y->stride;
+    a.dw = grad_weight->data, a.dws = grad_weight->stride;
+    a.T = cfg->tokens, a.V = cfg->vocab, a.d = cfg->dim, a.scale = cfg->scale;
+    a.passes = passes_of(a.V);
+    a.stretch = w.stretch, a.stretches = w.stretches;
+    for (int i = 0; i < 2; ++i) a.sorted[i] = reinterpret_cast<Sorted *>(ws + w.sorted[i]);
+    a.head = reinterpret_cast<float *>(ws + w.head);
+    a.tail = reinterpret_cast<float *>(ws + w.tail);
+    const bool pieces = by_pieces(a.dy, a.dys, a.T, elem) && by_pieces(a.dw, a.dws, a.V, elem) && a.d * elem % 16 == 0;
+    using bf16 = __nv_bfloat16;
+    if (cfg->dtype == DPB_F32)
+        return pieces ? gradient<float, 4>(a, ids, cfg->index_bytes, s) : gradient<float, 1>(a, ids, cfg->index_bytes, s);
+    return pieces ? gradient<bf16, 8>(a, ids, cfg->index_bytes, s) : gradient<bf16, 1>(a, ids, cfg->index_bytes, s);
+}
+
+}  // extern "C"

@@ -49,7 +49,6 @@ constexpr int kThreads = 128 + 32 * kRowWarps;
 constexpr int kAhead = 3;              // units taken ahead
 constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr double kLn2 = 0.6931471805599453;
 constexpr float kLowest = -1e30f;      // the maximum of no score
 
 enum Kind { kScores = 0, kGrad = 1, kDHidden = 2, kDWeight = 3, kEnd = 4 };
@@ -170,9 +169,13 @@ __device__ __forceinline__ void store_shared(uint32_t addr, uint32_t x, uint32_t
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-// A row's maximum and sum over 128 of its scores, in powers of 2; the target's score, if it is among them.
+// A row's maximum and sum of exp(z - maximum) over 128 of its scores; the
+// target's score, if it is among them. Scores are subtracted before they are
+// scaled to powers of 2, so that the largest gives 1 exactly; 32 of them are
+// added in eight chains of four.
 __device__ __forceinline__ float2 reduce_scores(uint32_t tmem, int columns, int target, float *z_target) {
     float top = kLowest, sum = 0.f;
+    const uint64_t scale = pair(kLog2e, kLog2e);
 #pragma unroll 1
     for (int c = 0; c < 128; c += 32) {
         uint32_t v[32];
@@ -183,18 +186,24 @@ __device__ __forceinline__ float2 reduce_scores(uint32_t tmem, int columns, int 
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (c + i >= columns) v[i] = 0xff800000u;
-        float m = __uint_as_float(v[0]);
+        float m[4];
 #pragma unroll
-        for (int i = 1; i < 31; i += 2) m = max3(m, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
-        m = fmaxf(m, __uint_as_float(v[31]));
-        const float now = fmaxf(top, m * kLog2e);
-        float s0 = 0.f, s1 = 0.f;
+        for (int k = 0; k < 4; ++k) {
+            m[k] = __uint_as_float(v[8 * k]);
+#pragma unroll
+            for (int i = 1; i < 7; i += 2) m[k] = max3(m[k], __uint_as_float(v[8 * k + i]), __uint_as_float(v[8 * k + i + 1]));
+            m[k] = fmaxf(m[k], __uint_as_float(v[8 * k + 7]));
+        }
+        const float now = max3(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]), top);
+        const uint64_t less = pair(-now, -now);
+        uint64_t s[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            s0 += exp2_approx(fmaf(__uint_as_float(v[i]), kLog2e, -now));
-            s1 += exp2_approx(fmaf(__uint_as_float(v[i + 1]), kLog2e, -now));
+            const float2 x = unpair(mul2(add2(pair_bits(v[i], v[i + 1]), less), scale));
+            s[i / 2 % 4] = add2(s[i / 2 % 4], pair(exp2_approx(x.x), exp2_approx(x.y)));
         }
-        sum = fmaf(sum, exp2_approx(top - now), s0 + s1);
+        const float2 t = unpair(add2(add2(s[0], s[1]), add2(s[2], s[3])));
+        sum = fmaf(sum, exp2_approx((top - now) * kLog2e), t.x + t.y);
         top = now;
         if ((unsigned)(target - c) < 32u) {
 #pragma unroll
@@ -207,7 +216,7 @@ __device__ __forceinline__ float2 reduce_scores(uint32_t tmem, int columns, int 
 
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
     const float top = fmaxf(a.x, b.x);
-    return make_float2(top, a.y * exp2_approx(a.x - top) + b.y * exp2_approx(b.x - top));
+    return make_float2(top, a.y * exp2_approx((a.x - top) * kLog2e) + b.y * exp2_approx((b.x - top) * kLog2e));
 }
 
 // 64 columns of a row's dz as bf16 pairs, into the warp's rows on their way to memory.
@@ -220,8 +229,12 @@ __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int 
         tmem_load(tmem + c, v);
         load_wait(v);
         float p[32];
+        const uint64_t scale = pair(kLog2e, kLog2e), less = pair(-t.lse2, -t.lse2);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) p[i] = exp2_approx(fmaf(__uint_as_float(v[i]), kLog2e, -t.lse2));
+        for (int i = 0; i < 32; i += 2) {
+            const float2 x = unpair(fma2(pair_bits(v[i], v[i + 1]), scale, less));
+            p[i] = exp2_approx(x.x), p[i + 1] = exp2_approx(x.y);
+        }
         if ((unsigned)(target - c) < 32u) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -623,10 +636,10 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args
     const int64_t mine = blockIdx.x * 32ll + slice;
     if (lane == 0 && mine < count) {
         const Token t = a.tokens[mine];
-        // the target's score in powers of 2, rounded as the maximum is: a sure row's loss is log2 of its sum alone
-        const double l = log2((double)r.y), z = a.z_target[mine] * kLog2e;
-        a.lse[t.row] = (float)(kLn2 * (r.x + l));
-        a.loss[t.row] = (float)(kLn2 * (r.x - z + l));
+        // not from the rounded lse: a sure row's loss keeps its digits
+        const double l = log((double)r.y);
+        a.lse[t.row] = (float)(r.x + l);
+        a.loss[t.row] = (float)((double)r.x - a.z_target[mine] + l);
     }
 }
 

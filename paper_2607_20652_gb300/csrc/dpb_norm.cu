@@ -1,0 +1,339 @@
+// dpb_norm.cu -- the residual's addition and the RMS norm behind it, and their
+// gradient.
+//
+//   s = x + delta (rounded to the rows' type),  y = w s r,  r = (mean s^2 + eps)^(-1/2)
+//   u = w dy,  dx = ds + r u - s r^3 mean(u s),  dw = sum_t dy s r
+//
+// Memory bounds both: a row is read once and kept in registers until its sum
+// is known. 32 to 1024 threads share a row, so that each has at most kMost
+// values of it; the gradient's threads keep their columns' dw over all rows of
+// their block, and the blocks' sums are added up in the blocks' order.
+#include <algorithm>
+
+#include "dpb_checks.h"
+#include "dpb_device.cuh"
+#include "dpb_rows.cuh"
+
+namespace dpb {
+namespace {
+
+constexpr int kMostDim = 16384;
+
+struct NormArgs {
+    const void *x, *delta, *w, *dy, *ds;
+    void *y, *s, *dx;
+    int64_t xs, deltas, dys, dss, ys, ss, dxs;  // strides
+    float *dw, *part;
+    int64_t T;
+    int d, blocks;
+    float eps;
+};
+
+// The sum over a row's threads; `row_warps` warps each, all of the block's threads call it.
+__device__ __forceinline__ float row_sum(float v, int row_warps, float *sums) {
+#pragma unroll
+    for (int i = 16; i > 0; i /= 2) v += __shfl_xor_sync(kFull, v, i);
+    if (row_warps == 1) return v;
+    const int warp = threadIdx.x / 32, first = warp / row_warps * row_warps;
+    if ((threadIdx.x & 31) == 0) sums[warp] = v;
+    __syncthreads();
+    v = 0.f;
+    for (int i = 0; i < row_warps; ++i) v += sums[first + i];
+    __syncthreads();
+    return v;
+}
+
+template <typename E, int N, int P, int MOST>
+__global__ void __launch_bounds__(MOST) add_norm_kernel(const NormArgs a, int row_warps) {
+    __shared__ float sums[32];
+    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads;
+    const int64_t rows_at_once = (int64_t)gridDim.x * (blockDim.x / row_threads);
+    // every thread of the block makes the same number of turns
+    for (int64_t t0 = (int64_t)blockIdx.x * (blockDim.x / row_threads); t0 < a.T; t0 += rows_at_once) {
+        const int64_t t = t0 + threadIdx.x / row_threads;
+        const bool live = t < a.T;
+        const E *x = static_cast<const E *>(a.x) + t * a.xs, *delta = static_cast<const E *>(a.delta) + t * a.deltas;
+        E *s = static_cast<E *>(a.s) + t * a.ss, *y = static_cast<E *>(a.y) + t * a.ys;
+        Piece<E, N> v[P], more[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = (in + p * row_threads) * N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[p].v[j] = more[p].v[j] = 0.f;
+            if (live && i < a.d) {
+                load_piece(x + i, v[p]);
+                if (a.delta) load_piece(delta + i, more[p]);
+            }
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                if (a.delta) {
+                    v[p].v[j] += more[p].v[j];
+                    if (sizeof(E) == 2) v[p].v[j] = __bfloat162float(__float2bfloat16_rn(v[p].v[j]));
+                }
+                sum = fmaf(v[p].v[j], v[p].v[j], sum);
+            }
+        sum = row_sum(sum, row_warps, sums);
+        const float r = rsqrtf(sum / a.d + a.eps);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = (in + p * row_threads) * N;
+            if (!live || i >= a.d) continue;
+            if (a.s) store_piece(s + i, v[p]);
+            Piece<E, N> w;
+            if (a.w) load_piece(static_cast<const E *>(a.w) + i, w);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[p].v[j] = v[p].v[j] * r * (a.w ? w.v[j] : 1.f);
+            store_piece(y + i, v[p]);
+        }
+    }
+}
+
+template <typename E, int N, int P, int MOST>
+__global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const NormArgs a, int row_warps) {
+    __shared__ float sums[32];
+    extern __shared__ float columns[];  // [d]: the block's dw
+    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = blockDim.x / row_threads;
+    float dw[P][N];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int j = 0; j < N; ++j) dw[p][j] = 0.f;
+    const int64_t rows_at_once = (int64_t)gridDim.x * rows;
+    for (int64_t t0 = (int64_t)blockIdx.x * rows; t0 < a.T; t0 += rows_at_once) {
+        const int64_t t = t0 + threadIdx.x / row_threads;
+        const bool live = t < a.T;
+        const E *s = static_cast<const E *>(a.x) + t * a.xs, *dy = static_cast<const E *>(a.dy) + t * a.dys;
+        const E *ds = static_cast<const E *>(a.ds) + t * a.dss;
+        E *dx = static_cast<E *>(a.dx) + t * a.dxs;
+        Piece<E, N> v[P], g[P], rest[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = (in + p * row_threads) * N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[p].v[j] = g[p].v[j] = rest[p].v[j] = 0.f;
+            if (live && i < a.d) {
+                load_piece(s + i, v[p]);
+                load_piece(dy + i, g[p]);
+                if (a.ds) load_piece(ds + i, rest[p]);
+            }
+        }
+        float sq = 0.f, us = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = (in + p * row_threads) * N;
+            Piece<E, N> w;
+            if (a.w && i < a.d) load_piece(static_cast<const E *>(a.w) + i, w);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float u = a.w && i < a.d ? g[p].v[j] * w.v[j] : g[p].v[j];
+                sq = fmaf(v[p].v[j], v[p].v[j], sq);
+                us = fmaf(u, v[p].v[j], us);
+            }
+        }
+        sq = row_sum(sq, row_warps, sums);
+        us = row_sum(us, row_warps, sums);
+        const float r = rsqrtf(sq / a.d + a.eps), k = r * r * r * (us / a.d);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = (in + p * row_threads) * N;
+            if (!live || i >= a.d) continue;
+            Piece<E, N> w;
+            if (a.w) load_piece(static_cast<const E *>(a.w) + i, w);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float u = a.w ? g[p].v[j] * w.v[j] : g[p].v[j];
+                dw[p][j] = fmaf(g[p].v[j] * r, v[p].v[j], dw[p][j]);
+                v[p].v[j] = fmaf(-k, v[p].v[j], fmaf(r, u, rest[p].v[j]));
+            }
+            store_piece(dx + i, v[p]);
+        }
+    }
+    if (!a.part) return;
+    // the block's rows one after the other
+    for (int q = 0; q < rows; ++q) {
+        if ((int)threadIdx.x / row_threads == q)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const int i = (in + p * row_threads) * N + j;
+                    if (i < a.d) columns[i] = q ? columns[i] + dw[p][j] : dw[p][j];
+                }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < a.d; i += blockDim.x) a.part[(int64_t)blockIdx.x * a.d + i] = columns[i];
+}
+
+// 32 columns of all blocks' sums: 32 threads a column, each its blocks in
+// order, then the threads.
+__global__ void __launch_bounds__(1024) add_norm_columns_kernel(const NormArgs a) {
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x / 32, i = blockIdx.x * 32 + lane;
+    float v = 0.f;
+    if (i < a.d)
+        for (int b = slice; b < a.blocks; b += 32) v += a.part[(int64_t)b * a.d + i];
+    sums[slice][lane] = v;
+    __syncthreads();
+    v = sums[lane][slice];
+#pragma unroll
+    for (int k = 16; k > 0; k /= 2) v += __shfl_down_sync(kFull, v, k);
+    const int mine = blockIdx.x * 32 + slice;
+    if (lane == 0 && mine < a.d) a.dw[mine] = v;
+}
+
+// ---- host side ------------------------------------------------------------------
+
+// Threads that share a row, and the pieces of each of them: a warp where its
+// lanes can hold the row (4 pieces of 16 bytes each, 16 of one value), then up
+// to 8 warps, and 32 for the widest rows.
+struct RowShape {
+    int warps, pieces;
+    RowShape(int row_pieces, int most) {
+        warps = 1;
+        while (32 * warps * most < row_pieces) warps = warps < 8 ? 2 * warps : 32;
+        const int each = (row_pieces + 32 * warps - 1) / (32 * warps);
+        pieces = 1;
+        while (pieces < each) pieces *= 2;
+    }
+};
+
+template <typename E, int N, int P, int MOST>
+dpb_status launch(const NormArgs &a, const RowShape &r, bool grad, cudaStream_t s) {
+    const int rows = MOST / (32 * r.warps);
+    if (!grad) {
+        const int64_t blocks = std::min<int64_t>((a.T + rows - 1) / rows, 1 << 20);
+        add_norm_kernel<E, N, P, MOST><<<(unsigned)blocks, MOST, 0, s>>>(a, r.warps);
+        return launch_status(cudaGetLastError(), "add_norm");
+    }
+    const size_t smem = a.part ? (size_t)a.d * 4 : 0;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(add_norm_grad_kernel<E, N, P, MOST>), smem);
+    if (e != cudaSuccess) return launch_status(e, "add_norm_backward");
+    add_norm_grad_kernel<E, N, P, MOST><<<a.blocks, MOST, smem, s>>>(a, r.warps);
+    return launch_status(cudaGetLastError(), "add_norm_backward");
+}
+
+template <typename E, int N>
+dpb_status dispatch(const NormArgs &a, bool grad, cudaStream_t s) {
+    const RowShape r((a.d + N - 1) / N, N == 1 ? 16 : 4);
+    if (r.warps > 8) {  // 2 or more pieces: what 8 warps cannot hold
+        if constexpr (N == 8) return launch<E, N, 2, 1024>(a, r, grad, s);
+        if constexpr (N == 4) return r.pieces <= 2 ? launch<E, N, 2, 1024>(a, r, grad, s) : launch<E, N, 4, 1024>(a, r, grad, s);
+        if constexpr (N == 1) return r.pieces <= 8 ? launch<E, N, 8, 1024>(a, r, grad, s) : launch<E, N, 16, 1024>(a, r, grad, s);
+    }
+    if (r.pieces == 1) return launch<E, N, 1, 256>(a, r, grad, s);
+    if (r.pieces == 2) return launch<E, N, 2, 256>(a, r, grad, s);
+    if (r.pieces == 4) return launch<E, N, 4, 256>(a, r, grad, s);
+    if constexpr (N == 1) return r.pieces == 8 ? launch<E, N, 8, 256>(a, r, grad, s) : launch<E, N, 16, 256>(a, r, grad, s);
+    return fail(DPB_ERR_UNSUPPORTED, "dim is too large");
+}
+
+dpb_status run(const NormArgs &a, int dtype, bool pieces, bool grad, cudaStream_t s) {
+    using bf16 = __nv_bfloat16;
+    if (dtype == DPB_F32) return pieces && a.d % 4 == 0 ? dispatch<float, 4>(a, grad, s) : dispatch<float, 1>(a, grad, s);
+    return pieces && a.d % 8 == 0 ? dispatch<bf16, 8>(a, grad, s) : dispatch<bf16, 1>(a, grad, s);
+}
+
+dpb_status check_config(const dpb_norm_config *c) {
+    if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->dtype != DPB_F32 && c->dtype != DPB_BF16) return fail(DPB_ERR_INVALID_ARG, "dtype must be DPB_F32 or DPB_BF16");
+    if (c->tokens < 0 || c->dim < 1) return fail(DPB_ERR_INVALID_ARG, "a size is too small");
+    if (c->tokens > (1ll << 40)) return fail(DPB_ERR_UNSUPPORTED, "at most 2^40 tokens");
+    if (c->dim > kMostDim) return fail(DPB_ERR_UNSUPPORTED, "dim must be at most %d", kMostDim);
+    if (!(c->eps >= 0.f) || !(c->eps <= 3.402823466e38f)) return fail(DPB_ERR_INVALID_ARG, "eps must be at least 0 and finite");
+    return DPB_OK;
+}
+
+dpb_status check_rows(const dpb_norm_config *c, const dpb_rows *r, const char *name) {
+    const int elem = c->dtype == DPB_F32 ? 4 : 2;
+    if (!r) return fail(DPB_ERR_INVALID_ARG, "%s is NULL", name);
+    DPB_CHECK(need(r->data, name, elem));
+    if (c->tokens > 1 && r->stride < c->dim) return fail(DPB_ERR_INVALID_ARG, "the stride of %s must be at least dim", name);
+    return DPB_OK;
+}
+bool rows_by_pieces(const dpb_norm_config *c, const dpb_rows *r) {
+    return !r || by_pieces(r->data, r->stride, c->tokens, c->dtype == DPB_F32 ? 4 : 2);
+}
+
+// Blocks of the gradient: enough to fill the device, each with a part of dw.
+int grad_blocks(const dpb_norm_config *c) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((c->tokens + 7) / 8, 2 * sms_of_device()));
+}
+
+}  // namespace
+}  // namespace dpb
+
+using namespace dpb;
+
+extern "C" {
+
+dpb_status dpb_add_norm(const dpb_norm_config *cfg, const dpb_rows *x, const dpb_rows *delta, const void *weight,
+                        const dpb_rows *y, const dpb_rows *total, void *stream) {
+    DPB_CHECK(check_config(cfg));
+    if (cfg->tokens == 0) return DPB_OK;
+    DPB_CHECK(check_rows(cfg, x, "x"));
+    if (delta) DPB_CHECK(check_rows(cfg, delta, "delta"));
+    DPB_CHECK(check_rows(cfg, y, "y"));
+    if (total) DPB_CHECK(check_rows(cfg, total, "total"));
+    const int elem = cfg->dtype == DPB_F32 ? 4 : 2;
+    if (weight) DPB_CHECK(need(weight, "weight", elem));
+    NormArgs a{};
+    a.x = x->data, a.xs = x->stride;
+    if (delta) a.delta = delta->data, a.deltas = delta->stride;
+    a.w = weight;
+    a.y = y->data, a.ys = y->stride;
+    if (total) a.s = total->data, a.ss = total->stride;
+    a.T = cfg->tokens, a.d = cfg->dim, a.eps = cfg->eps;
+    const bool pieces = rows_by_pieces(cfg, x) && rows_by_pieces(cfg, delta) && rows_by_pieces(cfg, y) &&
+                        rows_by_pieces(cfg, total) && by_pieces(weight, 0, 1, elem);
+    return run(a, cfg->dtype, pieces, false, static_cast<cudaStream_t>(stream));
+}
+
+dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes) {
+    DPB_CHECK(check_config(cfg));
+    if (!bytes) return fail(DPB_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = ((size_t)grad_blocks(cfg) * cfg->dim * 4 + 255) / 256 * 256;
+    return DPB_OK;
+}
+
+dpb_status dpb_add_norm_backward(const dpb_norm_config *cfg, const dpb_rows *total, const dpb_rows *grad_y,
+                                 const dpb_rows *grad_total, const void *weight, const dpb_rows *grad_x,
+                                 float *grad_weight, void *workspace, size_t workspace_bytes, void *stream) {
+    DPB_CHECK(check_config(cfg));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (grad_weight) DPB_CHECK(need(grad_weight, "grad_weight", 4));
+    if (cfg->tokens == 0) {
+        if (!grad_weight) return DPB_OK;
+        return launch_status(cudaMemsetAsync(grad_weight, 0, (size_t)cfg->dim * 4, s), "add_norm_backward");
+    }
+    DPB_CHECK(check_rows(cfg, total, "total"));
+    DPB_CHECK(check_rows(cfg, grad_y, "grad_y"));
+    if (grad_total) DPB_CHECK(check_rows(cfg, grad_total, "grad_total"));
+    DPB_CHECK(check_rows(cfg, grad_x, "grad_x"));
+    const int elem = cfg->dtype == DPB_F32 ? 4 : 2;
+    if (weight) DPB_CHECK(need(weight, "weight", elem));
+    NormArgs a{};
+    a.x = total->data, a.xs = total->stride;
+    a.dy = grad_y->data, a.dys = grad_y->stride;
+    if (grad_total) a.ds = grad_total->data, a.dss = grad_total->stride;
+    a.w = weight;
+    a.dx = grad_x->data, a.dxs = grad_x->stride;
+    a.T = cfg->tokens, a.d = cfg->dim, a.eps = cfg->eps;
+    a.blocks = grad_blocks(cfg);
+    if (grad_weight) {
+        DPB_CHECK(need_workspace(workspace, workspace_bytes, (size_t)a.blocks * a.d * 4));
+        a.dw = grad_weight;
+        a.part = static_cast<float *>(workspace);
+    }
+    const bool pieces = rows_by_pieces(cfg, total) && rows_by_pieces(cfg, grad_y) && rows_by_pieces(cfg, grad_total) &&
+                        rows_by_pieces(cfg, grad_x) && by_pieces(weight, 0, 1, elem);
+    DPB_CHECK(run(a, cfg->dtype, pieces, true, s));
+    if (!grad_weight) return DPB_OK;
+    add_norm_columns_kernel<<<(a.d + 31) / 32, 1024, 0, s>>>(a);
+    return launch_status(cudaGetLastError(), "add_norm_backward (weight)");
+}
+
+}  // extern "C"

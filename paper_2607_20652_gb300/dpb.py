@@ -70,8 +70,10 @@ class Config(ctypes.Structure):
 _ROPE = struct.Struct("=q8ifi")
 _ATTENTION = struct.Struct("=qq8ifi")
 _ROWS = {n: struct.Struct(f"={3 * n}q") for n in (4, 6, 8)}
-# dpb_linear_loss_config and up to four dpb_rows (16 bytes each)
+# dpb_linear_loss_config, dpb_embedding_config, dpb_norm_config and two or four dpb_rows (16 bytes each)
 _LOSS = struct.Struct("=qiiqiiii")
+_EMBEDDING = struct.Struct("=qiiiifi")
+_NORM = struct.Struct("=qiifi")
 _PLAIN_ROWS = {n: struct.Struct(f"={2 * n}q") for n in (2, 4)}
 
 
@@ -104,7 +106,8 @@ EXPORTS = ("dpb_plan_create", "dpb_plan_destroy", "dpb_plan_config", "dpb_plan_t
            "dpb_qk_norm_rope", "dpb_qk_norm_rope_backward", "dpb_rope_workspace_size",
            "dpb_attention_forward", "dpb_attention_backward", "dpb_attention_workspace_size", "dpb_adamw_step",
            "dpb_linear_cross_entropy_forward", "dpb_linear_cross_entropy_backward",
-           "dpb_linear_cross_entropy_workspace_size")
+           "dpb_linear_cross_entropy_workspace_size", "dpb_embedding", "dpb_embedding_backward",
+           "dpb_embedding_workspace_size", "dpb_add_norm", "dpb_add_norm_backward", "dpb_norm_workspace_size")
 
 
 def library_path() -> str:
@@ -150,6 +153,12 @@ def load(path: Optional[str] = None):
     lib.dpb_linear_cross_entropy_forward.argtypes = [rc, hp, hp, vp, vp, vp, vp, sz, vp]
     lib.dpb_linear_cross_entropy_backward.argtypes = [rc, hp, hp, vp, vp, vp, hp, hp, vp, sz, vp]
     lib.dpb_linear_cross_entropy_workspace_size.argtypes = [rc, ctypes.c_int32, ctypes.POINTER(sz)]
+    lib.dpb_embedding.argtypes = [rc, hp, vp, hp, vp, sz, vp]
+    lib.dpb_embedding_backward.argtypes = [rc, hp, vp, hp, vp, sz, vp]
+    lib.dpb_embedding_workspace_size.argtypes = [rc, ctypes.POINTER(sz)]
+    lib.dpb_add_norm.argtypes = [rc, hp, hp, vp, hp, hp, vp]
+    lib.dpb_add_norm_backward.argtypes = [rc, hp, hp, hp, vp, hp, vp, vp, sz, vp]
+    lib.dpb_norm_workspace_size.argtypes = [rc, ctypes.POINTER(sz)]
     lib.dpb_status_string.argtypes = [st]
     lib.dpb_status_string.restype = ctypes.c_char_p
     lib.dpb_last_error.argtypes = []
@@ -946,3 +955,115 @@ def linear_cross_entropy_backward(hidden: torch.Tensor, weight: torch.Tensor, ta
                                                     h + 48 if want_weight else None, workspace.data_ptr(),
                                                     workspace.nbytes, s))
     return grad_hidden if want_hidden else None, grad_weight if want_weight else None
+
+
+def _kind(dtype, name: str) -> int:
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise ValueError(f"{name} must be float32 or bfloat16, got {dtype}")
+    return BF16 if dtype is torch.bfloat16 else F32
+
+
+def embedding(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=None, workspace=None, stream=None):
+    """dpb_embedding. weight [V, d] fp32 or bf16, ids int32 or int64 [T].
+    Returns scale x weight[ids], [T, d]; an id outside [0, V) gives a row of 0
+    and sets DEV_BAD_INDEX (see status())."""
+    dev = weight.device
+    if _away(dev, stream):
+        return _elsewhere(embedding, stream, dev, (weight, ids, scale, out, workspace), {})
+    s = _raw_stream(dev)
+    if weight.dim() != 2 or ids.dim() != 1:
+        raise ValueError(f"weight must be [vocab, dim] and ids [tokens], got {list(weight.shape)} and {list(ids.shape)}")
+    dt, (V, d), T, a = weight.dtype, weight.shape, ids.shape[0], _arguments
+    kind = _kind(dt, "weight")
+    at, size = _indices(ids, "ids", T, dev)
+    out = torch.empty((T, d), dtype=dt, device=dev) if out is None else out
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    _EMBEDDING.pack_into(a.buf, 0, T, V, d, size, kind, scale, _status_slot(dev, s) if workspace is None else 0)
+    _PLAIN_ROWS[2].pack_into(a.buf, 64, *_plain_rows(weight, "weight", dt, weight.shape, dev),
+                             *_plain_rows(out, "out", dt, (T, d), dev))
+    _check(load().dpb_embedding(a.at, a.rows, at, a.rows + 16, ws, ws_bytes, s))
+    return out
+
+
+def embedding_backward(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, grad_weight=None,
+                       workspace=None, stream=None):
+    """dpb_embedding_backward. grad_out [T, d], ids [T]. Returns the gradient of
+    the weight [vocab, d] in full, of grad_out's type."""
+    dev = grad_out.device
+    if _away(dev, stream):
+        return _elsewhere(embedding_backward, stream, dev, (grad_out, ids, vocab, scale, grad_weight, workspace), {})
+    s = _raw_stream(dev)
+    if grad_out.dim() != 2 or ids.dim() != 1:
+        raise ValueError(f"grad_out must be [tokens, dim] and ids [tokens], got {list(grad_out.shape)} and {list(ids.shape)}")
+    dt, (T, d), a, lib = grad_out.dtype, grad_out.shape, _arguments, load()
+    kind = _kind(dt, "grad_out")
+    at, size = _indices(ids, "ids", T, dev)
+    _EMBEDDING.pack_into(a.buf, 0, T, vocab, d, size, kind, scale, _status_slot(dev, s) if workspace is None else 0)
+    if workspace is None:
+        n = ctypes.c_size_t()
+        _check(lib.dpb_embedding_workspace_size(a.at, n))
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)  # scratch of this call
+    grad_weight = torch.empty((vocab, d), dtype=dt, device=dev) if grad_weight is None else grad_weight
+    _PLAIN_ROWS[2].pack_into(a.buf, 64, *_plain_rows(grad_out, "grad_out", dt, (T, d), dev),
+                             *_plain_rows(grad_weight, "grad_weight", dt, (vocab, d), dev))
+    _check(lib.dpb_embedding_backward(a.at, a.rows, at, a.rows + 16, workspace.data_ptr(), workspace.nbytes, s))
+    return grad_weight
+
+
+def add_norm(x: torch.Tensor, delta=None, weight=None, eps: float = 1e-6, out=None, total=None, stream=None):
+    """dpb_add_norm. x and delta [T, d] fp32 or bf16, weight [d]. Returns
+    (y, total): total = x + delta rounded to the rows' type (x itself without
+    delta), y = weight x total / sqrt(mean total^2 + eps)."""
+    dev = x.device
+    if _away(dev, stream):
+        return _elsewhere(add_norm, stream, dev, (x, delta, weight, eps, out, total), {})
+    s = _raw_stream(dev)
+    if x.dim() != 2:
+        raise ValueError(f"x must be [tokens, dim], got {list(x.shape)}")
+    dt, sh, a = x.dtype, x.shape, _arguments
+    kind = _kind(dt, "x")
+    out = torch.empty(sh, dtype=dt, device=dev) if out is None else out
+    if delta is not None and total is None:
+        total = torch.empty(sh, dtype=dt, device=dev)
+    _NORM.pack_into(a.buf, 0, sh[0], sh[1], kind, eps, 0)
+    _PLAIN_ROWS[4].pack_into(a.buf, 64, *_plain_rows(x, "x", dt, sh, dev),
+                             *((0, 0) if delta is None else _plain_rows(delta, "delta", dt, sh, dev)),
+                             *_plain_rows(out, "out", dt, sh, dev),
+                             *((0, 0) if total is None else _plain_rows(total, "total", dt, sh, dev)))
+    h = a.rows
+    _check(load().dpb_add_norm(a.at, h, None if delta is None else h + 16, _dense(weight, "weight", dt, sh[1], dev), h + 32,
+                               None if total is None else h + 48, s))
+    return out, x if total is None else total
+
+
+def add_norm_backward(total: torch.Tensor, grad_out: torch.Tensor, grad_total=None, weight=None, eps: float = 1e-6,
+                      weight_grad: bool = True, grad_x=None, workspace=None, stream=None):
+    """dpb_add_norm_backward with the forward's total, the gradient of y and that
+    of total (None: none). Returns (grad_x [T, d], which is delta's gradient
+    too, grad_weight fp32 [d] or None without ``weight_grad``)."""
+    dev = total.device
+    if _away(dev, stream):
+        return _elsewhere(add_norm_backward, stream, dev,
+                          (total, grad_out, grad_total, weight, eps, weight_grad, grad_x, workspace), {})
+    s = _raw_stream(dev)
+    if total.dim() != 2:
+        raise ValueError(f"total must be [tokens, dim], got {list(total.shape)}")
+    dt, sh, a, lib = total.dtype, total.shape, _arguments, load()
+    kind = _kind(dt, "total")
+    _NORM.pack_into(a.buf, 0, sh[0], sh[1], kind, eps, 0)
+    grad_x = torch.empty(sh, dtype=dt, device=dev) if grad_x is None else grad_x
+    gw = torch.empty(sh[1], dtype=torch.float32, device=dev) if weight_grad else None
+    if weight_grad and workspace is None:
+        n = ctypes.c_size_t()
+        _check(lib.dpb_norm_workspace_size(a.at, n))
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)  # scratch of this call
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    _PLAIN_ROWS[4].pack_into(a.buf, 64, *_plain_rows(total, "total", dt, sh, dev),
+                             *_plain_rows(grad_out, "grad_out", dt, sh, dev),
+                             *((0, 0) if grad_total is None else _plain_rows(grad_total, "grad_total", dt, sh, dev)),
+                             *_plain_rows(grad_x, "grad_x", dt, sh, dev))
+    h = a.rows
+    _check(lib.dpb_add_norm_backward(a.at, h, h + 16, None if grad_total is None else h + 32,
+                                     _dense(weight, "weight", dt, sh[1], dev), h + 48,
+                                     None if gw is None else gw.data_ptr(), ws, ws_bytes, s))
+    return grad_x, gw

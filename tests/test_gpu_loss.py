@@ -1,0 +1,333 @@
+"""Cross entropy over the vocabulary from the hidden rows, and its gradient,
+against the formula in 64 bits.
+
+Bounds. A score is a sum of d exact products in fp32; an addition is off by at
+most 2^-23 of the sums of absolute values (the tensor cores may truncate), so
+a score by e_z = d 2^-23 sum |h w|. A sum of exponentials has relative errors
+of 2^-21 (exponentials of 2 ulp, factors of log2 e to 2^-24, sums of at most 64
+terms in a chain, joined in a tree), its exponents 2^-22 of the largest
+score's size; lse and the loss are each rounded once (2^-24). dz enters the
+gradients' products in bf16 (2^-8) with the errors of its exponential; each
+gradient is a fp32 sum and rounded to bf16 (2^-8) once.
+"""
+import pytest
+import torch
+
+from paper_2607_20652_gb300 import build, dpb
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _library():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    build.build()
+    dpb.load()
+
+
+def draw(T, V, d, seed=0, left_out="none", even=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    h = torch.randn(T, d, generator=g, device="cuda").to(BF)
+    w = (torch.randn(V, d, generator=g, device="cuda") * 1.5 / d ** 0.5).to(BF)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    if left_out == "some":
+        y[torch.rand(T, generator=g, device="cuda") < 0.4] = -100
+    elif left_out == "runs":
+        y[torch.arange(T, device="cuda") % 300 < 200] = -100
+    elif left_out == "all":
+        y[:] = -100
+    gl = torch.full((1,), 1 / max(T, 1), device="cuda").expand(T) if even else \
+        torch.randn(T, generator=g, device="cuda") / max(T, 1)
+    return h, w, y, gl
+
+
+def formula(h, w, y, gl):
+    """loss, lse, dh, dw, and the sums of absolute values behind them."""
+    h, w, gl = h.double(), w.double(), gl.double()
+    ok = y >= 0
+    at = y.clamp(min=0)[:, None]
+    z = h @ w.t()
+    lse = torch.where(ok, torch.logsumexp(z, 1), 0)
+    loss = torch.where(ok, lse - z.gather(1, at)[:, 0], 0)
+    dz = torch.exp(z - lse[:, None]).scatter_add(1, at, -torch.ones_like(at, dtype=torch.float64))
+    dz = torch.where(ok[:, None], dz * gl[:, None], 0)
+    e_z = h.shape[1] * 2.0 ** -23 * (h.abs() @ w.abs().t()).amax(1) if len(w) else None
+    return loss, lse, dz @ w, dz.t() @ h, z.abs().amax(1), e_z, dz.abs() @ w.abs(), dz.abs().t() @ h.abs()
+
+
+def check(got, want, tol):
+    off = ((got.double() - want).abs() / tol).nan_to_num(1e9).max() if got.numel() else torch.zeros(())
+    assert float(off) <= 1, float(off)
+
+
+def near(got, want):
+    """Roundings of dz and of the result, each 2^-8 at most and spread evenly: rms 2^-8 / sqrt 3 each."""
+    n = want.norm()
+    assert float((got.double() - want).norm()) <= 2.0 ** -8 * (2 / 3) ** 0.5 * 1.2 * float(n) + 1e-30
+
+
+def compare(h, w, y, gl, loss, lse, dh=None, dw=None):
+    T, V, d = h.shape[0], w.shape[0], h.shape[1]
+    ls, le, gh, gw, top, e_z, sh, sw = formula(h, w, y, gl)
+    e = e_z + 2.0 ** -21 + 2.0 ** -22 * top
+    check(lse, le, e + 2.0 ** -24 * le.abs())
+    check(loss, ls, 2 * e + 2.0 ** -24 * ls.abs())
+    e = 2.0 ** -8 + 2 * float(e.max())
+    if dh is not None:
+        check(dh, gh, (e + V * 2.0 ** -23) * sh + 2.0 ** -8 * gh.abs() + 1e-30)
+        near(dh, gh)
+    if dw is not None:
+        check(dw, gw, (e + T * 2.0 ** -23) * sw + 2.0 ** -8 * gw.abs() + 1e-30)
+        near(dw, gw)
+
+
+SIZES = [  # tokens, vocabulary, columns
+    (1, 50, 8), (33, 777, 72), (128, 97, 64), (255, 256, 64), (257, 257, 264), (300, 1000, 128), (513, 5003, 520),
+    (64, 9001, 2048), (1, 20000, 1000),
+    (8449, 9001, 72), (12289, 4355, 128),  # several pieces of the vocabulary
+]
+
+
+@pytest.mark.parametrize("left_out,even", [("none", True), ("some", False), ("runs", True)])
+@pytest.mark.parametrize("T,V,d", SIZES)
+def test_loss_and_gradient(T, V, d, left_out, even):
+    if T == 1 and left_out != "none":
+        left_out = "none"
+    h, w, y, gl = draw(T, V, d, seed=T + V, left_out=left_out, even=even)
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    assert dpb.status() == 0
+    compare(h, w, y, gl, loss, lse, dh, dw)
+    assert not loss[y < 0].any() and not lse[y < 0].any() and not dh[y < 0].any()
+
+
+def test_a_single_word():
+    h, w, y, gl = draw(70, 1, 16)
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    # the loss is 0; p - 1 is the rounding of lse in p = exp(z - lse): of the score's errors
+    e = float((16 * 2.0 ** -22 * (h.double().abs() @ w.double().abs().t())).max()) + 2.0 ** -20
+    assert float(loss.abs().max()) <= e and float(dh.abs().max()) <= e * float(w.abs().max()) / 70
+    assert float(dw.abs().max()) <= e * float(h.abs().max())
+
+
+def test_small_losses_keep_their_digits():
+    """Tokens that the model is sure of: the loss is log1p of a small sum, not the difference of large scores."""
+    V, d = 500, 64
+    w = torch.zeros(V, d, device="cuda", dtype=BF)
+    w[:, 0] = 1.0
+    w[7, 1] = 1.0
+    h = torch.zeros(40, d, device="cuda", dtype=BF)
+    h[:, 0] = 64.0
+    h[:, 1] = torch.arange(40, device="cuda") * 0.5
+    y = torch.full((40,), 7, device="cuda")
+    loss, _ = dpb.linear_cross_entropy_forward(h, w, y)
+    want = torch.log1p(499 * torch.exp(-0.5 * torch.arange(40, device="cuda", dtype=torch.float64)))
+    # The scores are exact and the largest gives 1 exactly; what is added to it goes through at most 4 additions of a
+    # chain, 3 of the chains, 1 of each piece of 32 (4 of them), 1 of the halves and 5 of the joining warp: 17 roundings of
+    # 2^-24 of a sum near 1, below 2^-19.9 in its logarithm. The other exponentials are off by 2^-21 of themselves.
+    check(loss, want, 2.0 ** -21 * want + 2.0 ** -19.9)
+
+
+def test_all_ignored():
+    h, w, y, gl = draw(300, 700, 64, left_out="all")
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    for t in (loss, lse, dh, dw):
+        assert not t.any()
+
+
+def test_no_tokens():
+    h, w = torch.empty(0, 64, device="cuda", dtype=BF), torch.randn(700, 64, device="cuda").to(BF)
+    y = torch.empty(0, dtype=torch.long, device="cuda")
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, loss)
+    assert loss.shape == (0,) and dh.shape == (0, 64) and dw.shape == w.shape and not dw.any()
+
+
+def test_ignored_rows_are_not_read():
+    h, w, y, gl = draw(600, 1000, 72, left_out="runs", even=False)
+    outs = []
+    for fill in (0.0, float("nan"), float("inf")):
+        h[y < 0] = fill
+        gl = gl.clone()
+        gl[y < 0] = fill
+        loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+        outs.append((loss, lse, *dpb.linear_cross_entropy_backward(h, w, y, lse, gl)))
+    for other in outs[1:]:
+        for a, b in zip(outs[0], other):
+            assert torch.equal(a, b)
+
+
+def test_another_ignored_target_and_32_bit_targets():
+    h, w, y, gl = draw(300, 700, 64, left_out="some")
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    want = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    for k, ignore in ((torch.where(y < 0, -1, y).int(), -1), (torch.where(y < 0, 1 << 40, y), 1 << 40)):
+        got = dpb.linear_cross_entropy_forward(h, w, k, ignore_index=ignore)
+        assert torch.equal(loss, got[0]) and torch.equal(lse, got[1])
+        for a, b in zip(want, dpb.linear_cross_entropy_backward(h, w, k, lse, gl, ignore_index=ignore)):
+            assert torch.equal(a, b)
+    assert dpb.status() == 0
+
+
+def test_a_word_that_is_ignored():
+    """ignore_index may be a word: its tokens take no part, its row of the gradient is of the other tokens."""
+    h, w, y, gl = draw(300, 50, 64)
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y, ignore_index=3)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl, ignore_index=3)
+    compare(h, w, torch.where(y == 3, -100, y), gl, loss, lse, dh, dw)
+
+
+def test_targets_out_of_range_are_flagged():
+    h, w, y, gl = draw(300, 700, 64)
+    y[5], y[250] = 700, -1
+    dpb.status()
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    assert dpb.status() == dpb.DEV_BAD_INDEX
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    assert dpb.status() == dpb.DEV_BAD_INDEX
+    y[5] = y[250] = -100
+    compare(h, w, y, gl, loss, lse, dh, dw)
+
+
+def test_strides_and_what_lies_between_is_left_alone():
+    h, w, y, gl = draw(300, 700, 72, left_out="some")
+    hs, ws = torch.full((300, 104), float("nan"), device="cuda", dtype=BF), torch.full((700, 80), float("nan"), device="cuda",
+                                                                                      dtype=BF)
+    hs[:, 16:88], ws[:, :72] = h, w
+    gh, gw = torch.full((300, 96), 3.0, device="cuda", dtype=BF), torch.full((700, 200), 3.0, device="cuda", dtype=BF)
+    loss, lse = dpb.linear_cross_entropy_forward(hs[:, 16:88], ws[:, :72], y)
+    dpb.linear_cross_entropy_backward(hs[:, 16:88], ws[:, :72], y, lse, gl, grad_hidden=gh[:, 8:80], grad_weight=gw[:, 64:136])
+    compare(h, w, y, gl, loss, lse, gh[:, 8:80], gw[:, 64:136])
+    for t, a, b in ((gh, 8, 80), (gw, 64, 136)):
+        assert (t[:, :a] == 3).all() and (t[:, b:] == 3).all()
+
+
+def test_one_gradient_alone():
+    h, w, y, gl = draw(9000, 4500, 64)
+    _, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    a, none = dpb.linear_cross_entropy_backward(h, w, y, lse, gl, want_weight=False)
+    assert none is None and torch.equal(a, dh)
+    none, b = dpb.linear_cross_entropy_backward(h, w, y, lse, gl, want_hidden=False)
+    assert none is None and torch.equal(b, dw)
+    assert dpb.linear_cross_entropy_backward(h, w, y, lse, gl, want_hidden=False, want_weight=False) == (None, None)
+
+
+def test_gradients_that_are_zero_large_small_or_not_finite():
+    h, w, y, _ = draw(300, 700, 64)
+    _, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    for gl in (torch.zeros(300, device="cuda"), torch.full((1,), -0.0, device="cuda").expand(300)):
+        assert not any(t.any() for t in dpb.linear_cross_entropy_backward(h, w, y, lse, gl))
+    for size in (1e30, 1e-30):
+        gl = torch.randn(300, device="cuda") * size
+        _, _, gh, gw, *_ = formula(h, w, y, gl)
+        dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+        near(dh, gh)
+        near(dw, gw)
+    gl = torch.randn(300, device="cuda")
+    want, _ = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    gl[3] = float("nan")
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    assert dh[3].isnan().all() and dw.isnan().all()
+    keep = torch.arange(300, device="cuda") != 3
+    check(dh[keep], want[keep].double(), 2.0 ** -6 * want[keep].double().abs() + 2.0 ** -7 * want.double().abs().max())
+
+
+def test_gradient_against_differences():
+    """Rows on a grid of 2^-4, moved by 2^-4 along random directions: f(x + s) - f(x - s) over 2 s, whose third-order
+    term is at most |s|^3 / 6 times the largest third central moment of the scores' changes, 2 max|s w|^3."""
+    T, V, d = 40, 300, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    h = (torch.randint(-16, 17, (T, d), generator=g, device="cuda") / 16.0).to(BF)
+    w = (torch.randint(-16, 17, (V, d), generator=g, device="cuda") / 32.0).to(BF)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    gl = torch.rand(T, generator=g, device="cuda")
+    _, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    for x, grad, other in ((h, dh, w), (w, dw, h)):
+        s = (torch.randint(0, 2, x.shape, generator=g, device="cuda") * 2 - 1) * (torch.rand(x.shape, generator=g, device="cuda")
+                                                                               < 0.1) / 16.0
+        s = s.to(BF)
+        up, down = ((x + s), (x - s))
+        f = [(dpb.linear_cross_entropy_forward(*((a, w) if x is h else (h, a)), y)[0].double() * gl.double()).sum() for a in
+             (up, down)]
+        got = float((f[0] - f[1]) / 2)
+        change = (s.double() @ other.double().t()).abs().max() if x is h else (other.double() @ s.double().t()).abs().max()
+        tol = float(gl.double().sum()) * (float(change) ** 3 / 3 + 2 * (2.0 ** -20 + 2.0 ** -21 * float(lse.max())))
+        tol += 2.0 ** -7 * float((grad.double() * s.double()).abs().sum()) + 2.0 ** -8 * float(gl.sum()) * float(change)
+        want = float((grad.double() * s.double()).sum())
+        assert abs(got - want) <= tol, (got, want, tol)
+
+
+def test_equal_inputs_give_equal_bits():
+    h, w, y, gl = draw(9000, 5000, 264, left_out="some", even=False)
+    first = None
+    for _ in range(3):
+        loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+        out = (loss, lse, *dpb.linear_cross_entropy_backward(h, w, y, lse, gl))
+        first = first or out
+        assert all(torch.equal(a, b) for a, b in zip(first, out))
+
+
+def test_scratch_may_hold_anything():
+    """Workspaces full of NaN, and one shared by calls of different sizes."""
+    n = 1 << 28
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    ws[:4] = 0
+    for T, V, d, left in ((8449, 5001, 72, "some"), (300, 1000, 64, "none"), (64, 257, 200, "runs")):
+        h, w, y, gl = draw(T, V, d, left_out=left, even=False)
+        loss, lse = dpb.linear_cross_entropy_forward(h, w, y, workspace=ws)
+        dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl, workspace=ws)
+        assert dpb.workspace_status(ws) == 0
+        compare(h, w, y, gl, loss, lse, dh, dw)
+
+
+def test_another_stream_and_a_graph():
+    h, w, y, gl = draw(700, 1000, 64, left_out="some", even=False)
+    want = dpb.linear_cross_entropy_forward(h, w, y)
+    grads = dpb.linear_cross_entropy_backward(h, w, y, want[1], gl)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = dpb.linear_cross_entropy_forward(h, w, y, stream=s)
+    got_grads = dpb.linear_cross_entropy_backward(h, w, y, got[1], gl, stream=s)
+    s.synchronize()
+    for a, b in zip((*want, *grads), (*got, *got_grads)):
+        assert torch.equal(a, b)
+    h2, w2, y2, gl2 = draw(700, 1000, 64, seed=5, left_out="runs", even=False)
+    graph = torch.cuda.CUDAGraph()
+    hh, ww, yy, gg = h.clone(), w.clone(), y.clone(), gl.clone()
+    with torch.cuda.graph(graph):
+        loss, lse = dpb.linear_cross_entropy_forward(hh, ww, yy)
+        dh, dw = dpb.linear_cross_entropy_backward(hh, ww, yy, lse, gg)
+    for a, b, c, k in ((h2, w2, y2, gl2), (h, w, y, gl)):
+        for t, v in ((hh, a), (ww, b), (yy, c), (gg, k)):
+            t.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        compare(a, b, c, k, loss, lse, dh, dw)
+    assert dpb.status() == 0
+
+
+def test_refusals():
+    h, w, y, gl = draw(30, 70, 64)
+    for bad in (dict(hidden=h.float()), dict(weight=w.float()), dict(hidden=h[:, :60]), dict(targets=y.float()),
+                dict(targets=y[:20]), dict(weight=w.t()[:64].t()[:, ::2]), dict(hidden=h[0])):
+        at = dict(hidden=h, weight=w, targets=y, **{}) | bad
+        with pytest.raises((ValueError, dpb.DPBError)):
+            dpb.linear_cross_entropy_forward(**at)
+    with pytest.raises(dpb.DPBError):  # 60 columns of rows of 64
+        dpb.linear_cross_entropy_forward(h[:, :60], w[:, :60], y)
+    with pytest.raises(dpb.DPBError):  # rows at an odd address
+        dpb.linear_cross_entropy_forward(h[:, 1:57], w[:, :56], y)
+    _, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    for bad in (gl.double(), gl[:20], torch.rand(60, device="cuda")[::2], torch.rand((), device="cuda")):
+        with pytest.raises(ValueError):
+            dpb.linear_cross_entropy_backward(h, w, y, lse, bad)
+    with pytest.raises(ValueError):
+        dpb.linear_cross_entropy_backward(h, w, y, lse[:20], gl)
+    with pytest.raises(dpb.DPBError):
+        dpb.linear_cross_entropy_forward(h, w, y, workspace=torch.zeros(1024, dtype=torch.uint8, device="cuda"))

@@ -1126,7 +1126,8 @@ def run_transformer(args, world, rank, local):
         m = transformer.ParityTransformer(layers=c["layers"], d=c["d"], heads=c["heads"], d_mlp=c["d_mlp"],
                                           vocab=c["vocab"], context=c["context"],
                                           dpb=dpb_kw if with_dpb else None, device=device,
-                                          attention="dpb" if args.own_step else "torch")
+                                          attention="dpb" if args.own_step else "torch",
+                                          ends="dpb" if args.own_ends else "torch")
         if args.own_step:
             from paper_2607_20652_gb300 import optim
             return m, optim.AdamW(m.parameters(), lr=1e-4, state_bits=args.state_bits)
@@ -1180,6 +1181,8 @@ def run_transformer(args, world, rank, local):
     dpb_ms = parts["forward"] + parts["backward"]
     per_layer = (3 + (4 if args.standardise else 0))
     own_launches = (6 * c["layers"] + 1) * args.steps if args.own_step else 0  # rope 1 + 2, attention 1 + 2; one AdamW
+    if args.own_ends:  # lookup 1 + 3, a norm 1 + 2, the loss 4 + 3 at least
+        own_launches += (11 + 3 * (2 * c["layers"] + 1)) * args.steps
     line = {
         "metric": "ParityTransformer GPT-2-small training step (fwd + bwd + AdamW), tokens/s; DPB share of the step",
         "value": round(whole_job_rate(tokens, world, 1, ms / 1e3), 1), "unit": "tokens/s", "n_gpus": world,
@@ -1190,7 +1193,9 @@ def run_transformer(args, world, rank, local):
                            "standardise": bool(args.standardise)},
                    "weights": "random init (std 0.02), bf16; " + (
                        f"this library's attention (normalised, rotated queries and keys) and AdamW, {args.state_bits}-bit "
-                       "states" if args.own_step else "AdamW fused"), "parallelism": f"dp{world}"},
+                       "states" if args.own_step else "AdamW fused") + (
+                       "; this library's embedding lookup, residual norms and cross entropy" if args.own_ends else ""),
+                   "parallelism": f"dp{world}"},
         "dpb_ms_per_step": {"forward": round(parts["forward"], 4), "backward": round(parts["backward"], 4),
                             "total": round(dpb_ms, 4)},
         "dpb_share": round(dpb_ms / ms, 4),
@@ -1228,6 +1233,8 @@ def main(argv=None):
                     help="live standardisation tables and the per-step EMA update in the timed step")
     ap.add_argument("--own-step", action="store_true",
                     help="gpt2small: this library's attention and AdamW in place of PyTorch's")
+    ap.add_argument("--own-ends", action="store_true",
+                    help="gpt2small: this library's embedding lookup, residual norms and cross entropy as well")
     ap.add_argument("--state-bits", type=int, choices=[32, 8], default=32, help="gpt2small --own-step: AdamW's states")
     ap.add_argument("--no-dense", action="store_true", help="gpt2small: skip the dense model of the same shape")
     ap.add_argument("--workload", default=WORKLOAD,

@@ -624,9 +624,9 @@ dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
  *   index_bytes 4 or 8: targets are int32 or int64 [tokens]
  *   dtype       DPB_BF16
  * hidden [tokens][dim] and weight [vocab][dim] are bf16, 16-byte aligned, with
- * strides that are multiples of 8 elements. loss, lse: fp32 [tokens]. A target
- * outside [0, vocab) that is not ignore_index sets DPB_DEV_BAD_INDEX and counts
- * as ignored. Scores and sums are fp32, exponentials to 2 ulp; a small loss keeps
+ * strides that are multiples of 8 elements. loss, lse: fp32 [tokens]. counted
+ * (int32, nullable): the number of tokens that take part. A target outside
+ * [0, vocab) that is not ignore_index sets DPB_DEV_BAD_INDEX and counts as ignored. Scores and sums are fp32, exponentials to 2 ulp; a small loss keeps
  * its digits (it is not formed from the rounded lse).
  */
 typedef struct dpb_linear_loss_config {
@@ -638,7 +638,7 @@ typedef struct dpb_linear_loss_config {
 
 dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
                                             const dpb_rows *weight, const void *targets, float *loss, float *lse,
-                                            void *workspace, size_t workspace_bytes, void *stream);
+                                            int32_t *counted, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * dpb_linear_cross_entropy_backward -- its gradients for grad_loss = dL/dloss:

@@ -81,6 +81,7 @@ struct Args {
     float2 *part;  // [tiles of the vocabulary][rows]
     float *z_target;
     float *loss, *lse;
+    int *counted;
     float *acc;  // [rows][dim], where there are several pieces
     bf16 *dh;
     int64_t dh_stride;
@@ -578,6 +579,7 @@ __global__ void __launch_bounds__(1024) prepare_kernel(const __grid_constant__ A
     if (tid == 0) {
         a.head->count = total;
         a.head->all = total == a.T;
+        if (a.counted) *a.counted = total;
         a.head->g_max = top;
     }
     for (int i = tid; i < 60; i += 1024) a.head->next[i] = 0;
@@ -795,9 +797,13 @@ dpb_status dpb_linear_cross_entropy_workspace_size(const dpb_linear_loss_config 
 
 dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
                                             const dpb_rows *weight, const void *targets, float *loss, float *lse,
-                                            void *workspace, size_t workspace_bytes, void *stream) {
+                                            int32_t *counted, void *workspace, size_t workspace_bytes, void *stream) {
     DPB_CHECK(check_config(cfg));
-    if (cfg->tokens == 0) return DPB_OK;
+    if (counted) DPB_CHECK(need(counted, "counted", 4));
+    if (cfg->tokens == 0) {
+        if (!counted) return DPB_OK;
+        return launch_status(cudaMemsetAsync(counted, 0, 4, static_cast<cudaStream_t>(stream)), "linear_cross_entropy");
+    }
     DPB_CHECK(check_rows(hidden, "hidden", cfg->tokens, cfg->dim));
     DPB_CHECK(check_rows(weight, "weight", cfg->vocab, cfg->dim));
     DPB_CHECK(need(targets, "targets", cfg->index_bytes));
@@ -810,6 +816,7 @@ dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, c
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     a.loss = loss;
     a.lse = lse;
+    a.counted = counted;
     a.part = reinterpret_cast<float2 *>(ws + w.part);
     a.z_target = reinterpret_cast<float *>(ws + w.z_target);
     a.write = a.read = -1;

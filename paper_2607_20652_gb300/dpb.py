@@ -150,7 +150,7 @@ def load(path: Optional[str] = None):
     lib.dpb_attention_backward.argtypes = [ac, hp, hp, hp, hp, vp, hp, vp, vp, hp, hp, hp, vp, sz, vp]
     lib.dpb_attention_workspace_size.argtypes = [ac, ctypes.POINTER(sz)]
     lib.dpb_adamw_step.argtypes = [ctypes.POINTER(AdamWConfig), vp, ctypes.c_int32, vp]
-    lib.dpb_linear_cross_entropy_forward.argtypes = [rc, hp, hp, vp, vp, vp, vp, sz, vp]
+    lib.dpb_linear_cross_entropy_forward.argtypes = [rc, hp, hp, vp, vp, vp, vp, vp, sz, vp]
     lib.dpb_linear_cross_entropy_backward.argtypes = [rc, hp, hp, vp, vp, vp, hp, hp, vp, sz, vp]
     lib.dpb_linear_cross_entropy_workspace_size.argtypes = [rc, ctypes.c_int32, ctypes.POINTER(sz)]
     lib.dpb_embedding.argtypes = [rc, hp, vp, hp, vp, sz, vp]
@@ -892,29 +892,33 @@ def _loss_workspace(backward: int, device):
 
 
 def linear_cross_entropy_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
-                                 ignore_index: int = -100, loss=None, lse=None, workspace=None, stream=None):
+                                 ignore_index: int = -100, loss=None, lse=None, want_counted: bool = False,
+                                 workspace=None, stream=None):
     """dpb_linear_cross_entropy_forward. hidden [T, d], weight [V, d] bf16,
     targets int32 or int64 [T]. Returns (loss, lse), fp32 [T]: the cross entropy
     of each token's scores hidden weight^T and the log of the sum of their
-    exponentials, both 0 where the target is ``ignore_index``."""
+    exponentials, both 0 where the target is ``ignore_index``; with
+    ``want_counted`` also the number of the other tokens, int32 [1]."""
     dev = hidden.device
     if _away(dev, stream):
         return _elsewhere(linear_cross_entropy_forward, stream, dev,
-                          (hidden, weight, targets, ignore_index, loss, lse, workspace), {})
+                          (hidden, weight, targets, ignore_index, loss, lse, want_counted, workspace), {})
     s = _raw_stream(dev)
     at = _loss_config(hidden, weight, targets, ignore_index, 0, _status_slot(dev, s) if workspace is None else 0)
     a, T, bf = _arguments, hidden.shape[0], torch.bfloat16
     loss = torch.empty(T, dtype=torch.float32, device=dev) if loss is None else loss
     lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else lse
+    counted = torch.empty(1, dtype=torch.int32, device=dev) if want_counted else None
     if workspace is None:
         workspace = _loss_workspace(0, dev)
     _PLAIN_ROWS[2].pack_into(a.buf, 64, *_plain_rows(hidden, "hidden", bf, hidden.shape, dev),
                              *_plain_rows(weight, "weight", bf, weight.shape, dev))
     h = a.rows
     _check(load().dpb_linear_cross_entropy_forward(a.at, h, h + 16, at, _dense(loss, "loss", torch.float32, T, dev),
-                                                   _dense(lse, "lse", torch.float32, T, dev), workspace.data_ptr(),
+                                                   _dense(lse, "lse", torch.float32, T, dev),
+                                                   None if counted is None else counted.data_ptr(), workspace.data_ptr(),
                                                    workspace.nbytes, s))
-    return loss, lse
+    return (loss, lse, counted) if want_counted else (loss, lse)
 
 
 def linear_cross_entropy_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,

@@ -1,0 +1,149 @@
+"""Both ends of the model and the stream between them, for training: autograd
+around the C-ABI calls dpb_embedding, dpb_add_norm and
+dpb_linear_cross_entropy_forward / _backward.
+
+The paper's backbone is GPT-2 style with one weight for embedding and
+unembedding and RMS norms (§3); it does not describe them further. Here the
+lookup, the addition of a block's output to the residual with the next norm,
+and the cross entropy from the last hidden rows run in the library's kernels;
+no tensor of tokens x vocabulary is made. The gradients have no gradient of
+their own: a second differentiation raises.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+from torch import nn
+from torch.autograd.function import once_differentiable
+
+from . import dpb
+
+
+def _rows(t: torch.Tensor, dtype) -> torch.Tensor:
+    """[..., d] as the [tokens, d] rows that the kernels read, of `dtype`."""
+    t = t.to(dtype).reshape(-1, t.shape[-1])
+    return t if t.stride(-1) == 1 and (t.shape[0] < 2 or t.stride(0) >= t.shape[1]) else t.contiguous()
+
+
+def _tiles(t: torch.Tensor) -> torch.Tensor:
+    """Rows as the matrix products read them: at multiples of 16 bytes."""
+    return t if t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or t.stride(0) % 8 == 0) else t.clone(memory_format=torch.contiguous_format)
+
+
+class _EmbeddingFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, weight, ids, scale):
+        ctx.save_for_backward(ids)
+        ctx.at = (weight.shape[0], scale)
+        return dpb.embedding(weight, ids, scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy):
+        ids, = ctx.saved_tensors
+        return dpb.embedding_backward(_rows(gy, gy.dtype), ids, *ctx.at), None, None
+
+
+def embedding(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
+    """dpb.embedding with its gradient (dense, by sorted tokens): ids of any shape -> [..., d]."""
+    return _EmbeddingFunction.apply(_rows(weight, weight.dtype), ids.reshape(-1), scale).view(*ids.shape, weight.shape[1])
+
+
+class Embedding(nn.Module):
+    """``vocab`` rows of ``d`` values, looked up and multiplied by ``scale``."""
+
+    def __init__(self, vocab: int, d: int, scale: float = 1.0, device=None, dtype=None):
+        super().__init__()
+        self.weight = nn.Parameter(torch.empty(vocab, d, device=device, dtype=dtype))
+        nn.init.normal_(self.weight)
+        self.scale = scale
+
+    def forward(self, ids: torch.Tensor) -> torch.Tensor:
+        return embedding(self.weight, ids, self.scale)
+
+
+class _AddNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, delta, weight, eps):
+        w = None if weight is None else weight.to(x.dtype)
+        y, total = dpb.add_norm(x, delta, w, eps)
+        ctx.save_for_backward(total, w)
+        ctx.eps, ctx.wide = eps, None if weight is None else weight.dtype
+        ctx.set_materialize_grads(False)
+        return y if delta is None else (y, total)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy, gt=None):
+        total, w = ctx.saved_tensors
+        if gy is None:
+            return gt, gt, None, None
+        dt = total.dtype
+        gx, gw = dpb.add_norm_backward(total, _rows(gy, dt), None if gt is None else _rows(gt, dt), w, ctx.eps,
+                                       weight_grad=ctx.needs_input_grad[2])
+        return gx, gx if ctx.needs_input_grad[1] else None, None if gw is None else gw.to(ctx.wide), None
+
+
+def add_norm(x: torch.Tensor, delta: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+             eps: float = 1e-6):
+    """dpb.add_norm with its gradient: (y, total) of the shape of x, total = x +
+    delta (x itself without delta), y its RMS norm times weight. delta and the
+    weight are taken in x's type."""
+    rows = _rows(x, x.dtype)
+    if delta is None:
+        return _AddNormFunction.apply(rows, None, weight, eps).view(x.shape), x
+    if delta.shape != x.shape:
+        raise ValueError(f"delta must have x's shape {list(x.shape)}, got {list(delta.shape)}")
+    y, total = _AddNormFunction.apply(rows, _rows(delta, x.dtype), weight, eps)
+    return y.view(x.shape), total.view(x.shape)
+
+
+class AddRMSNorm(nn.Module):
+    """forward(x, delta) -> (y, total): the residual's addition and the norm behind it (add_norm) with a learned weight."""
+
+    def __init__(self, d: int, eps: float = 1e-6, device=None, dtype=None):
+        super().__init__()
+        self.weight = nn.Parameter(torch.ones(d, device=device, dtype=dtype))
+        self.eps = eps
+
+    def forward(self, x: torch.Tensor, delta: Optional[torch.Tensor] = None):
+        return add_norm(x, delta, self.weight, self.eps)
+
+
+class _LossFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, targets, ignore_index, mean):
+        w = _tiles(_rows(weight, hidden.dtype))
+        loss, lse, counted = dpb.linear_cross_entropy_forward(hidden, w, targets, ignore_index, want_counted=True)
+        ctx.save_for_backward(hidden, w, targets, lse, counted)
+        ctx.ignore_index, ctx.mean, ctx.wide = ignore_index, mean, weight.dtype
+        return loss.sum() / counted[0] if mean else loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g):
+        hidden, w, targets, lse, counted = ctx.saved_tensors
+        if ctx.mean:
+            g = (g / counted).expand(targets.shape)
+        elif g.stride(0) not in (0, 1):
+            g = g.contiguous()
+        dh, dw = dpb.linear_cross_entropy_backward(hidden, w, targets, lse, g, ctx.ignore_index,
+                                                   want_hidden=ctx.needs_input_grad[0], want_weight=ctx.needs_input_grad[1])
+        return dh, None if dw is None else dw.to(ctx.wide), None, None, None
+
+
+def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100,
+                         reduction: str = "mean") -> torch.Tensor:
+    """Cross entropy of the scores hidden weight^T without making them: hidden
+    [..., d] bf16, weight [vocab, d] (taken in bf16, as under autocast), targets
+    [...]. ``reduction`` "mean" (over the tokens that are not ignored; NaN if
+    all are), "sum" or "none", in fp32. What the rows of ignored tokens hold does
+    not matter. d has to be a multiple of 8."""
+    if reduction not in ("mean", "sum", "none"):
+        raise ValueError(f"reduction must be 'mean', 'sum' or 'none', got {reduction!r}")
+    if hidden.shape[:-1] != targets.shape:
+        raise ValueError(f"targets must have the shape {list(hidden.shape[:-1])}, got {list(targets.shape)}")
+    loss = _LossFunction.apply(_tiles(_rows(hidden, hidden.dtype)), weight, targets.reshape(-1), ignore_index,
+                               reduction == "mean")
+    return loss if reduction == "mean" else loss.sum() if reduction == "sum" else loss.view(targets.shape)

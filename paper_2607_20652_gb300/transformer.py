@@ -5,7 +5,8 @@ embedding and unembedding, RMSNorm in place of LayerNorm) with a Deep Parity
 Bottleneck inserted before the input of every MLP. Weights are random
 (nothing here is trained); attention and the dense layers are PyTorch's own
 (cuBLAS / fused attention), the DPB layers are this library's kernels;
-``attention="dpb"`` takes this library's attention as well. The model exists
+``attention="dpb"`` takes this library's attention as well, ``ends="dpb"`` its
+embedding lookup, residual norms and cross entropy. The model exists
 to measure the DPB's share of a forward + backward + optimiser step at the
 paper's scale; it is not a training recipe.
 """
@@ -18,6 +19,7 @@ import torch
 import torch.nn.functional as F
 from torch import nn
 
+from . import ends as _ends
 from .attention import Attention
 from .layer import DPBLayer
 
@@ -53,6 +55,19 @@ class _Block(nn.Module):
             h = self.dpb(h)  # the bottleneck sits before the MLP's input (§3)
         return x + self.down(F.gelu(self.up(h)))
 
+    def stream(self, x, delta):
+        """The same with the library's residual norms: the residual's rows and what is still to be added to them."""
+        h, x = _add_norm(self.n1, x, delta)
+        h, x = _add_norm(self.n2, x, self.attn(h))
+        if self.dpb is not None:
+            h = self.dpb(h)
+        return x, self.down(F.gelu(self.up(h)))
+
+
+def _add_norm(norm: nn.RMSNorm, x, delta):
+    # without an eps nn.RMSNorm takes that of the type it computes bf16 rows in
+    return _ends.add_norm(x, delta, norm.weight, torch.finfo(torch.float32).eps if norm.eps is None else norm.eps)
+
 
 class ParityTransformer(nn.Module):
     """GPT-2 shape (12 layers, d = 768, 12 heads, MLP 3072, vocab 50257,
@@ -60,12 +75,19 @@ class ParityTransformer(nn.Module):
     the dense model of the same shape. ``dpb`` holds DPBLayer arguments.
     ``attention="dpb"`` uses this library's attention, with normalised queries
     and keys and rotary positions in place of the learned ones (bf16;
-    ``kv_heads`` key and value heads)."""
+    ``kv_heads`` key and value heads). ``ends="dpb"`` uses this library's
+    embedding lookup, residual norms and, with targets, its cross entropy (bf16):
+    the same model without a tensor of tokens x vocabulary."""
 
     def __init__(self, layers: int = 12, d: int = 768, heads: int = 12, d_mlp: int = 3072, vocab: int = 50257,
                  context: int = 1024, dpb: Optional[dict] = None, device=None, dtype=torch.bfloat16,
-                 attention: str = "torch", kv_heads: Optional[int] = None):
+                 attention: str = "torch", kv_heads: Optional[int] = None, ends: str = "torch"):
         super().__init__()
+        if ends not in ("torch", "dpb"):
+            raise ValueError(f"ends must be 'torch' or 'dpb', got {ends!r}")
+        if ends == "dpb" and (d % 8 or dtype is not torch.bfloat16):
+            raise ValueError(f"ends='dpb' needs bfloat16 and d a multiple of 8, got {dtype} and {d}")
+        self.ends = ends
         if attention not in ("torch", "dpb"):
             raise ValueError(f"attention must be 'torch' or 'dpb', got {attention!r}")
         if attention == "torch" and kv_heads not in (None, heads):
@@ -95,9 +117,18 @@ class ParityTransformer(nn.Module):
 
     def forward(self, ids, targets=None):
         B, S = ids.shape
-        x = self.tok(ids)
+        own = self.ends == "dpb"
+        x = _ends.embedding(self.tok.weight, ids) if own else self.tok(ids)
         if self.pos is not None:
             x = x + self.pos(torch.arange(S, device=ids.device))
+        if own:
+            delta = None
+            for b in self.blocks:
+                x, delta = b.stream(x, delta)
+            h, _ = _add_norm(self.norm, x, delta)
+            if targets is None:
+                return F.linear(h, self.tok.weight)
+            return _ends.linear_cross_entropy(h, self.tok.weight, targets)
         for b in self.blocks:
             x = b(x)
         logits = F.linear(self.norm(x), self.tok.weight)  # tied unembedding

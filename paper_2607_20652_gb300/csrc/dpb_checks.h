@@ -49,6 +49,24 @@ inline dpb_status launch_status(cudaError_t e, const char *what) {
     return DPB_OK;
 }
 
+// A kernel that may start, and set itself up, while the one before it in the
+// stream runs; it waits for that one's results itself.
+template <typename... K, typename... A>
+cudaError_t launch_early(void (*kernel)(K...), dim3 blocks, int threads, size_t smem, cudaStream_t s, const A &...args) {
+    cudaLaunchConfig_t how{};
+    how.gridDim = blocks;
+    how.blockDim = dim3(threads);
+    how.dynamicSmemBytes = smem;
+    how.stream = s;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    how.attrs = &early;
+    how.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&how, kernel, args...);
+    return e == cudaSuccess ? cudaGetLastError() : e;
+}
+
 #define DPB_CHECK(expr)                         \
     do {                                        \
         const dpb_status check_s_ = (expr);     \

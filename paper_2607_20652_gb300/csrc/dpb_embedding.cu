@@ -46,7 +46,7 @@ struct LookupArgs {
 
 // `lanes` lanes (a power of 2) copy a row.
 template <typename E, int N, typename I>
-__global__ void __launch_bounds__(256) embedding_kernel(const LookupArgs a, const I *ids, int lanes) {
+__global__ void __launch_bounds__(256) embedding_kernel(const __grid_constant__ LookupArgs a, const I *ids, int lanes) {
     const int pieces = (a.d + N - 1) / N, in = threadIdx.x & (lanes - 1);
     const int64_t rows = (int64_t)gridDim.x * (256 / lanes);
     for (int64_t t = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes; t < a.T; t += rows) {
@@ -80,8 +80,9 @@ __device__ __forceinline__ int read_peer(uint32_t addr) {
 // The other clusters write zeros.
 template <typename E, int N, typename I>
 __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSortWarps, 1)
-    embedding_sort_kernel(const LookupArgs a, const I *ids) {
+    embedding_sort_kernel(const __grid_constant__ LookupArgs a, const I *ids) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+    tc::start_next();
     if (blockIdx.x >= kSortBlocks) {
         const int pieces = (a.d + N - 1) / N;
         const int64_t warps = (int64_t)(gridDim.x - kSortBlocks) * kSortWarps;
@@ -95,25 +96,41 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
     __shared__ int count[kSortWarps][kDigits], total[kDigits], sums[kDigits / 32];
     const uint32_t rank = blockIdx.x;
     const int64_t each = ((a.T + kSortBlocks * kSortWarps - 1) / (kSortBlocks * kSortWarps) + 31) / 32 * 32;
-    const int64_t t0 = (rank * kSortWarps + warp) * each, t1 = min(a.T, t0 + each);
+    const int64_t t0 = min(a.T, (rank * kSortWarps + warp) * each), t1 = min(a.T, t0 + each);
+    constexpr int kHeld = 8;  // tokens of a lane under way: all of them up to 65536
     for (int pass = 0; pass < a.passes; ++pass) {
         const Sorted *from = a.sorted[(pass & 1) ^ 1];
         Sorted *to = a.sorted[pass & 1];
-        auto token = [&](int64_t t) {
-            if (pass > 0) return from[t];
-            const int64_t id = ids[t];
-            if (id >= 0 && id < a.V) return Sorted{(int)id, (int)t};
-            set_status(a.status, DPB_DEV_BAD_INDEX);
-            return Sorted{a.V, (int)t};
+        Sorted x[kHeld];
+        auto load = [&](int64_t t) {
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) {
+                const int64_t at = t + 32 * k + lane;
+                x[k] = Sorted{-1, 0};
+                if (at >= t1) continue;
+                if (pass > 0) {
+                    x[k] = from[at];
+                } else {
+                    const int64_t id = ids[at];
+                    const bool ok = id >= 0 && id < a.V;
+                    if (!ok) set_status(a.status, DPB_DEV_BAD_INDEX);
+                    x[k] = Sorted{ok ? (int)id : a.V, (int)at};
+                }
+            }
         };
+        auto digit = [&](int id) { return id < 0 ? -1 : (id >> (8 * pass)) & 255; };
         for (int i = tid; i < kSortWarps * kDigits; i += 32 * kSortWarps) (&count[0][0])[i] = 0;
         __syncthreads();
-        for (int64_t t = t0; t < t1; t += 32) {
-            const bool live = t + lane < t1;
-            const int digit = live ? (token(t + lane).id >> (8 * pass)) & 255 : -1;
-            const unsigned same = __match_any_sync(kFull, digit);
-            if (live && lane == __ffs(same) - 1) count[warp][digit] += __popc(same);
-            __syncwarp();
+        for (int64_t t = t0; t < t1; t += 32 * kHeld) {
+            load(t);
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) {
+                if (t + 32 * k >= t1) break;
+                const int g = digit(x[k].id);
+                const unsigned same = __match_any_sync(kFull, g);
+                if (g >= 0 && lane == __ffs(same) - 1) count[warp][g] += __popc(same);
+                __syncwarp();
+            }
         }
         __syncthreads();
         if (tid < kDigits) {  // the block's warps before each
@@ -129,6 +146,7 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
         int before = 0, all = 0, upto = 0;
         if (tid < kDigits) {
             const uint32_t at = tc::smem_addr(&total[tid]);
+#pragma unroll
             for (uint32_t r = 0; r < kSortBlocks; ++r) {
                 const int n = read_peer(tc::peer_addr(at, r));
                 if (r < rank) before += n;
@@ -149,18 +167,21 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
             for (int w = 0; w < kSortWarps; ++w) count[w][tid] += first;
         }
         __syncthreads();
-        for (int64_t t = t0; t < t1; t += 32) {
-            const bool live = t + lane < t1;
-            const Sorted x = live ? token(t + lane) : Sorted{0, 0};
-            const int digit = live ? (x.id >> (8 * pass)) & 255 : -1;
-            const unsigned same = __match_any_sync(kFull, digit);
-            const int place = live ? count[warp][digit] + __popc(same & ((1u << lane) - 1)) : 0;
-            __syncwarp();
-            if (live) {
-                to[place] = x;
-                if (lane == __ffs(same) - 1) count[warp][digit] += __popc(same);
+        for (int64_t t = t0; t < t1; t += 32 * kHeld) {
+            if (each > 32 * kHeld) load(t);  // else still held
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) {
+                if (t + 32 * k >= t1) break;
+                const int g = digit(x[k].id);
+                const unsigned same = __match_any_sync(kFull, g);
+                const int place = g >= 0 ? count[warp][g] + __popc(same & ((1u << lane) - 1)) : 0;
+                __syncwarp();
+                if (g >= 0) {
+                    to[place] = x[k];
+                    if (lane == __ffs(same) - 1) count[warp][g] += __popc(same);
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
         // the others have read this block's totals, and all tokens are in place
         tc::cluster_sync();
@@ -169,9 +190,12 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
 
 // ---- gradient: sums ---------------------------------------------------------------------
 
-// A warp sums one stretch of the sorted tokens over 32 P N columns.
+// A warp sums one stretch of the sorted tokens over 32 P N columns, the next
+// rows under way while it adds some.
 template <typename E, int N, int P>
-__global__ void __launch_bounds__(256) embedding_sum_kernel(const LookupArgs a) {
+__global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constant__ LookupArgs a) {
+    tc::start_next();
+    tc::wait_previous();
     const int lane = threadIdx.x & 31;
     const int64_t c = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
     if (c >= a.stretches) return;
@@ -207,78 +231,91 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const LookupArgs a) 
             }
         }
     };
+    constexpr int kAtOnce = 4;
     for (int64_t b = p0; b < p1; b += 32) {
-        const Sorted mine = b + lane < p1 ? sorted[b + lane] : Sorted{-1, 0};
         const int n = (int)min((int64_t)32, p1 - b);
-        constexpr int kAtOnce = 4;
-        for (int k0 = 0; k0 < n; k0 += kAtOnce) {
-            Piece<E, N> v[kAtOnce][P];
-            int ids[kAtOnce];
+        const Sorted mine = lane < n ? sorted[b + lane] : Sorted{-1, 0};  // places past the end read row 0
+        Bits<E, N> rows[2][kAtOnce][P];
+        auto load = [&](int k0, Bits<E, N> (&to)[kAtOnce][P]) {
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
-                ids[k] = __shfl_sync(kFull, mine.id, (k0 + k) & 31);
                 const int64_t t = __shfl_sync(kFull, mine.token, (k0 + k) & 31);
-                if (k0 + k >= n) ids[k] = a.V;
                 const E *dy = static_cast<const E *>(a.dy) + t * a.dys;
 #pragma unroll
-                for (int p = 0; p < P; ++p)
-                    if (ids[k] < a.V && column + p * 32 * N < a.d) load_piece(dy + column + p * 32 * N, v[k][p]);
+                for (int p = 0; p < P; ++p) load_bits(dy + (column + p * 32 * N < a.d ? column + p * 32 * N : 0), to[k][p]);
             }
+        };
+        auto add = [&](int k0, const Bits<E, N> (&from)[kAtOnce][P]) {
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
+                const int now = __shfl_sync(kFull, mine.id, (k0 + k) & 31);
                 if (k0 + k >= n) break;
-                if (ids[k] != id) {
+                if (now != id) {
                     flush(true);
                     clear();
-                    id = ids[k];
+                    id = now;
                     whole = b + k0 + k > p0 || id != prev;
                 }
-                if (id < a.V)
 #pragma unroll
-                    for (int p = 0; p < P; ++p)
-                        if (column + p * 32 * N < a.d)
+                for (int p = 0; p < P; ++p) {
+                    const Piece<E, N> v = values(from[k][p]);
 #pragma unroll
-                            for (int j = 0; j < N; ++j) acc[p][j] += v[k][p].v[j];
+                    for (int j = 0; j < N; ++j) acc[p][j] += v.v[j];
+                }
             }
+        };
+        load(0, rows[0]);
+        for (int k0 = 0; k0 < n; k0 += 2 * kAtOnce) {
+            if (k0 + kAtOnce < n) load(k0 + kAtOnce, rows[1]);
+            add(k0, rows[0]);
+            if (k0 + 2 * kAtOnce < n) load(k0 + 2 * kAtOnce, rows[0]);
+            if (k0 + kAtOnce < n) add(k0 + kAtOnce, rows[1]);
         }
     }
     flush(id != next);
 }
 
 // A row whose tokens go on after the stretch where they begin: the sum of what
-// each stretch has of it.
-template <typename E>
-__global__ void __launch_bounds__(256) embedding_join_kernel(const LookupArgs a) {
-    const int64_t c = blockIdx.x;
+// each stretch has of it. A warp has 32 M columns of one stretch's last row.
+template <typename E, int M>
+__global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_constant__ LookupArgs a, int groups) {
+    tc::wait_previous();
+    const int lane = threadIdx.x & 31;
+    const int64_t w = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, c = w / groups;
     const Sorted *sorted = a.sorted[(a.passes - 1) & 1];
     const int64_t p0 = c * a.stretch, end = p0 + a.stretch;
     if (end >= a.T) return;
-    const int id = sorted[end - 1].id;
-    if (id >= a.V || sorted[end].id != id) return;
-    // it begins here, if its first token is here
-    if (p0 > 0 && sorted[p0].id == id && sorted[p0 - 1].id == id) return;
-    int64_t last = c + 1;  // the stretch where it ends
-    for (int64_t step = 1; step > 0;) {  // the last one whose first token is of this row
-        if (last + step < a.stretches && sorted[(last + step) * a.stretch].id == id) {
-            last += step;
-            step *= 2;
-        } else {
-            step /= 2;
-        }
-    }
-    for (int i = threadIdx.x; i < a.d; i += 256) {
-        float v = a.tail[c * a.d + i];
-        int64_t k = c + 1;
-        for (; k + 8 <= last + 1; k += 8) {
-            float x[8];
+    const int before = p0 > 0 ? sorted[p0 - 1].id : -1, first = sorted[p0].id, id = sorted[end - 1].id, after = sorted[end].id;
+    if (id >= a.V || after != id) return;
+    if (first == id && before == id) return;  // it begins earlier
+    const int i = ((int)(w - c * groups) * 32 + lane) * M;
+    const bool live = i < a.d;
+    using V = Piece<float, M>;
+    auto at = [&](const float *from, int64_t k) {
+        V x;
+        load_piece(from + k * a.d + (live ? i : 0), x);
+        return x;
+    };
+    V sum = at(a.tail, c);
+    for (int64_t k = c + 1; k < a.stretches; k += 32) {
+        // the next stretches that begin with the row
+        const bool has = k + lane < a.stretches && sorted[min(k + lane, a.stretches - 1) * a.stretch].id == id;
+        const int n = __popc(__ballot_sync(kFull, has));
+        for (int q = 0; q < n; q += 16) {
+            V x[16];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = a.head[(k + j) * a.d + i];
+            for (int j = 0; j < 16; ++j) x[j] = at(a.head, k + min(q + j, n - 1));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v += x[j];
+            for (int j = 0; j < 16; ++j)
+                if (q + j < n)
+#pragma unroll
+                    for (int m = 0; m < M; ++m) sum.v[m] += x[j].v[m];
         }
-        for (; k <= last; ++k) v += a.head[k * a.d + i];
-        st_elem(static_cast<E *>(a.dw), id * a.dws + i, v * a.scale);
+        if (n < 32) break;
     }
+    if (live)
+#pragma unroll
+        for (int m = 0; m < M; ++m) st_elem(static_cast<E *>(a.dw), id * a.dws + i + m, sum.v[m] * a.scale);
 }
 
 // ---- host side ------------------------------------------------------------------
@@ -338,6 +375,13 @@ dpb_status lookup(const LookupArgs &a, const void *ids, int index_bytes, cudaStr
     return launch_status(cudaGetLastError(), "embedding");
 }
 
+template <typename E, int N, int P>
+cudaError_t sums(const LookupArgs &a, cudaStream_t s) {
+    const dim3 grid((unsigned)((a.stretches + 7) / 8), (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
+    if (grid.y > 65535) return cudaErrorInvalidConfiguration;
+    return launch_early(embedding_sum_kernel<E, N, P>, grid, 256, 0, s, a);
+}
+
 template <typename E, int N>
 dpb_status gradient(const LookupArgs &a, const void *ids, int index_bytes, cudaStream_t s) {
     const int others = std::max(1, std::min(sms_of_device() / kSortBlocks - 1, (a.V + 255) / 256));
@@ -347,13 +391,17 @@ dpb_status gradient(const LookupArgs &a, const void *ids, int index_bytes, cudaS
     else
         embedding_sort_kernel<E, N><<<blocks, 32 * kSortWarps, 0, s>>>(a, static_cast<const int64_t *>(ids));
     DPB_CHECK(launch_status(cudaGetLastError(), "embedding_backward (order)"));
-    constexpr int P = N == 1 ? 8 : 4;
-    const dim3 grid((unsigned)((a.stretches + 7) / 8), (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
-    if (grid.y > 65535) return fail(DPB_ERR_UNSUPPORTED, "dim is too large");
-    embedding_sum_kernel<E, N, P><<<grid, 256, 0, s>>>(a);
-    DPB_CHECK(launch_status(cudaGetLastError(), "embedding_backward (sums)"));
-    embedding_join_kernel<E><<<(unsigned)a.stretches, 256, 0, s>>>(a);
-    return launch_status(cudaGetLastError(), "embedding_backward (rows)");
+    const int pieces = (a.d + 32 * N - 1) / (32 * N);  // of a lane
+    cudaError_t e;
+    if (pieces == 1) e = sums<E, N, 1>(a, s);
+    else if (pieces == 2 || pieces == 4) e = sums<E, N, 2>(a, s);
+    else e = sums<E, N, 3>(a, s);
+    DPB_CHECK(launch_status(e, "embedding_backward (sums)"));
+    constexpr int M = N == 1 ? 1 : 4;
+    const int groups = (a.d + 32 * M - 1) / (32 * M);
+    if (a.stretches * groups / 8 >= 0x7fffffffll) return fail(DPB_ERR_UNSUPPORTED, "too many tokens for rows this wide");
+    return launch_status(launch_early(embedding_join_kernel<E, M>, dim3((unsigned)((a.stretches * groups + 7) / 8)), 256, 0, s, a, groups),
+                         "embedding_backward (rows)");
 }
 
 }  // namespace

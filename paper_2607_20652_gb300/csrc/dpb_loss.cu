@@ -46,8 +46,10 @@ constexpr int kStageBytes = 32768;     // 128 x 64 of A and of B
 constexpr int kStore = 4096;           // a warp's rows on their way to memory: 32 of 64 bf16
 constexpr int kRowWarps = 8;
 constexpr int kThreads = 128 + 32 * kRowWarps;
-constexpr int kAhead = 3;              // units taken ahead
-constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
+constexpr int kAhead = 3;                  // units taken ahead
+constexpr int kBuffers = 3;            // pieces of dz held
+constexpr int kMostPieces = 48;
+constexpr int kGroup = 32;                // tiles of rows that pass a tile of the vocabulary before the next
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -1e30f;      // the maximum of no score
 
@@ -58,7 +60,9 @@ struct Head {
     int count;     // tokens that take part
     int all;       // none is left out: rows are where they were
     float g_max;   // largest finite |grad_loss| (1 if all are 0)
-    int next[60];  // units taken, by launch
+    int next;      // units taken
+    // of each piece, the row warps that are done with a unit of each kind (kGrad, kDHidden, kDWeight)
+    int done[kMostPieces][4];
 };
 // Of the i-th token that takes part: its target, lse log2 e, grad_loss / g_max.
 struct Token {
@@ -70,7 +74,7 @@ struct Token {
 struct Args {
     CUtensorMap hidden, closed;  // rows as given, and closed up
     CUtensorMap weight;
-    CUtensorMap dz[2], dz_out[2];  // two pieces, loaded and stored
+    CUtensorMap dz[kBuffers], dz_out[kBuffers];  // loaded and stored
     CUtensorMap dw;
     const bf16 *h;
     int64_t h_stride;
@@ -87,47 +91,103 @@ struct Args {
     int64_t dh_stride;
     int64_t T, T_pad;
     int V, d, piece;  // piece: words of a piece
-    int write, read, pieces, launch;  // pieces whose dz is written and read by this launch (or -1)
+    int pieces;
     bool want_h, want_w;
     int32_t *status;
 };
 
 struct Unit {
     int kind, m0, n0, blocks;  // blocks: of 64 along K
+    int piece;
 };
 
 // ---- units ------------------------------------------------------------------------
 
 // Tiles of the vocabulary: groups of rows' tiles, so that the tiles under way
 // share both operands.
-__device__ __forceinline__ Unit score_unit(int kind, int u, int tiles_m, int tiles_n, int d) {
+__device__ __forceinline__ Unit score_unit(int kind, int u, int tiles_m, int tiles_n, int d, int piece) {
     const int group = u / (kGroup * tiles_n), in = u - group * kGroup * tiles_n;
     const int rows = min(kGroup, tiles_m - group * kGroup);
-    return Unit{kind, (group * kGroup + in % rows) * kTile, in / rows * kTile, (d + 63) / 64};
+    return Unit{kind, (group * kGroup + in % rows) * kTile, in / rows * kTile, (d + 63) / 64, piece};
 }
 
-__device__ __forceinline__ Unit unit_of(const Args &a, int count, int u) {
-    const int tiles_m = (count + kTile - 1) / kTile, tiles_d = (a.d + kTile - 1) / kTile;
-    if (a.loss) {  // forward
-        const int tiles_n = (a.V + kTile - 1) / kTile;
-        return u < tiles_m * tiles_n ? score_unit(kScores, u, tiles_m, tiles_n, a.d) : Unit{kEnd, 0, 0, 0};
+// How many units each product has, and which is the u-th. The gradient's
+// pieces overlap: dz of a piece comes before the products that read the piece
+// before it, so that what a unit waits for was taken a piece's time ago:
+//   dz 0, dz 1, dW 0, dH 0, dz 2, dW 1, dH 1, ..., dW last, dH last
+struct List {
+    int tiles_m, tiles_d, words;  // words of the vocabulary that a piece (the forward: all) has
+    int count, last;              // tokens; words of the last piece
+    __device__ __forceinline__ List(const Args &a, int count_) : count(count_) {
+        tiles_m = (count + kTile - 1) / kTile, tiles_d = (a.d + kTile - 1) / kTile;
+        words = a.loss ? a.V : a.piece;
+        last = a.loss ? a.V : a.V - (a.pieces - 1) * a.piece;
     }
-    if (a.read >= 0) {
-        const int words = min(a.piece, a.V - a.read * a.piece), tiles_v = (words + kTile - 1) / kTile;
-        const int n_w = a.want_w ? tiles_v * tiles_d : 0, n_h = a.want_h ? tiles_m * tiles_d : 0;
-        const Unit end{kEnd, 0, 0, 0};
-        auto dw = [&](int i) { return Unit{kDWeight, i / tiles_d * kTile, i % tiles_d * kTile, (count + 63) / 64}; };
-        auto dh = [&](int i) { return Unit{kDHidden, i / tiles_d * kTile, i % tiles_d * kTile, (words + 63) / 64}; };
-        const bool w_first = count >= words;
-        const int first = w_first ? n_w : n_h, second = w_first ? n_h : n_w;
-        if (u < first) return w_first ? dw(u) : dh(u);
-        u -= first;
-        if (u < second) return w_first ? dh(u) : dw(u);
-        u -= second;
-        if (a.write < 0) return end;
+    __device__ __forceinline__ int words_of(const Args &a, int piece) const { return piece == a.pieces - 1 ? last : words; }
+    __device__ __forceinline__ int grad_units(int w) const { return tiles_m * ((w + kTile - 1) / kTile); }
+    __device__ __forceinline__ int weight_units(const Args &a, int w) const {
+        return a.want_w ? (w + kTile - 1) / kTile * tiles_d : 0;
     }
-    const int words = min(a.piece, a.V - a.write * a.piece), tiles_n = (words + kTile - 1) / kTile;
-    return u < tiles_m * tiles_n ? score_unit(kGrad, u, tiles_m, tiles_n, a.d) : Unit{kEnd, 0, 0, 0};
+    __device__ __forceinline__ int hidden_units(const Args &a) const { return a.want_h ? tiles_m * tiles_d : 0; }
+    __device__ __forceinline__ Unit reader(const Args &a, int u, int piece) const {
+        const int w = words_of(a, piece), n_w = weight_units(a, w);
+        if (u < n_w) return Unit{kDWeight, u / tiles_d * kTile, u % tiles_d * kTile, (count + 63) / 64, piece};
+        u -= n_w;
+        if (u < hidden_units(a)) return Unit{kDHidden, u / tiles_d * kTile, u % tiles_d * kTile, (w + 63) / 64, piece};
+        return Unit{kEnd, 0, 0, 0, 0};
+    }
+    __device__ __forceinline__ Unit at(const Args &a, int u) const {
+        const int all = a.pieces, first = grad_units(words_of(a, 0));
+        if (a.loss) return u < first ? score_unit(kScores, u, tiles_m, (a.V + kTile - 1) / kTile, a.d, 0) : Unit{kEnd, 0, 0, 0, 0};
+        int piece = 0;
+        if (u >= first) {
+            u -= first;
+            const int readers = weight_units(a, words) + hidden_units(a), full = grad_units(words) + readers;
+            // pieces 1 .. all - 2 are full, and so are the readers of those before them
+            const int step = full > 0 ? max(0, min(u / full, all - 2)) : 0;
+            u -= step * full;
+            piece = step + 1;
+            const int dz = piece < all ? grad_units(words_of(a, piece)) : 0;
+            if (u >= dz) {
+                u -= dz;
+                if (piece < all) {
+                    if (u < readers) return reader(a, u, piece - 1);
+                    u -= readers;
+                    ++piece;
+                }
+                return reader(a, u, piece - 1);
+            }
+        }
+        return score_unit(kGrad, u, tiles_m, (words_of(a, piece) + kTile - 1) / kTile, a.d, piece);
+    }
+    // One thread: what the unit waits for has been done: dz of its piece, and the
+    // sums of dH before it; for dz, the products that read its place.
+    __device__ __forceinline__ bool wait(const Args &a, const Unit &t) const {
+        const int each = 2 * kRowWarps;
+        if (t.kind == kGrad) {
+            const int before = t.piece - kBuffers;
+            return before < 0 || (reached(&a.head->done[before][kDWeight], each * weight_units(a, words)) &&
+                                  reached(&a.head->done[before][kDHidden], each * hidden_units(a)));
+        }
+        if (t.kind != kDHidden && t.kind != kDWeight) return true;
+        return reached(&a.head->done[t.piece][kGrad], each * grad_units(words_of(a, t.piece))) &&
+               (t.kind == kDWeight || t.piece == 0 ||
+                reached(&a.head->done[t.piece - 1][kDHidden], each * hidden_units(a)));
+    }
+    static __device__ __forceinline__ bool reached(const int *counter, int target) {
+        for (uint32_t i = 0; i < kTries; ++i) {
+            int v;
+            asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+            if (v >= target) return true;
+            __nanosleep(200);
+        }
+        return false;
+    }
+};
+
+// One thread of a row warp: what it wrote for a unit is in memory.
+__device__ __forceinline__ void count_done(int *counter) {
+    asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
 }
 
 // ---- shared memory ------------------------------------------------------------------
@@ -168,6 +228,12 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t base, int row, int piece) 
 }
 __device__ __forceinline__ void store_shared(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+__device__ __forceinline__ float4 load_shared(uint32_t addr) {
+    float4 x;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr) : "memory");
+    return x;
 }
 
 // A row's maximum and sum of exp(z - maximum) over 128 of its scores; the
@@ -254,6 +320,15 @@ __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int 
     }
 }
 
+// Four columns of rows row, row + 4, ... of dH as the pieces before have summed
+// them: other blocks' values, so not by way of this SM's own cache.
+__device__ __forceinline__ void sums_before(const Args &a, float4 (&x)[8], int row, int count, int column) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (row + 4 * i < count && column < a.d)
+            x[i] = __ldcg(reinterpret_cast<const float4 *>(a.acc + (int64_t)(row + 4 * i) * a.d + column));
+}
+
 // ---- the kernel -------------------------------------------------------------------------
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Args a) {
@@ -262,7 +337,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     uint8_t *const mem = raw + (base - smem_addr(raw));
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
-    const int count = a.head->count;
     bool failed = false;
 
     auto full = [&](int s) { return base + Shared::kFullBar + 8 * s; };
@@ -288,6 +362,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     __syncthreads();
     cluster_sync();
     fence_after();
+    start_next();
+    wait_previous();
+    const int count = a.head->count;
+    const List list(a, count);
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(base + Shared::kTmem) : "memory");
 
@@ -300,8 +378,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             while (true) {
                 if ((failed = !units.next(u))) break;
                 units.done();
-                const Unit t = unit_of(a, count, u);
+                const Unit t = list.at(a, u);
                 if (t.kind == kEnd) break;
+                // dz was stored by copies of other blocks: these loads come after what their count released
+                if (t.kind > kGrad) fence_async();
+                const int v0 = t.piece * a.piece;
+                const CUtensorMap *dz = &a.dz[t.piece % kBuffers];
                 for (int k = 0; k < t.blocks; ++k, ++at) {
                     const int s = at % kStages;
                     if (at >= kStages && !bar_wait_peer(empty(s), ((at / kStages) & 1) ^ 1, kTries)) {
@@ -315,14 +397,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     for (int j = 0; j < 2; ++j) {
                         const uint32_t ta = to + 8192 * j, tb = ta + 16384;
                         if (t.kind <= kGrad) {
-                            const int v0 = t.kind == kGrad ? a.write * a.piece : 0;
                             copy_box_pair(ta, rows, 64 * k, m + 64 * j, bar);
                             copy_box_pair(tb, &a.weight, 64 * k, v0 + n + 64 * j, bar);
                         } else if (t.kind == kDHidden) {
-                            copy_box_pair(ta, &a.dz[a.read & 1], 64 * k, m + 64 * j, bar);
-                            copy_box_pair(tb, &a.weight, n + 64 * j, a.read * a.piece + 64 * k, bar);
+                            copy_box_pair(ta, dz, 64 * k, m + 64 * j, bar);
+                            copy_box_pair(tb, &a.weight, n + 64 * j, v0 + 64 * k, bar);
                         } else {
-                            copy_box_pair(ta, &a.dz[a.read & 1], m + 64 * j, 64 * k, bar);
+                            copy_box_pair(ta, dz, m + 64 * j, 64 * k, bar);
                             copy_box_pair(tb, rows, n + 64 * j, 64 * k, bar);
                         }
                     }
@@ -341,7 +422,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             while (true) {
                 if ((failed = !units.next(u))) break;
                 units.done();
-                const Unit t = unit_of(a, count, u);
+                const Unit t = list.at(a, u);
                 if (t.kind == kEnd) break;
                 if (t.blocks == 0) continue;
                 const int b = sums & 1;
@@ -386,13 +467,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     failed = true;
                     break;
                 }
-                const int u = atomicAdd(&a.head->next[a.launch], 1);
+                const int u = atomicAdd(&a.head->next, 1);
+                const Unit t = list.at(a, u);
+                if (!list.wait(a, t)) {
+                    failed = true;
+                    break;
+                }
                 const uint32_t slot = base + Shared::kUnits + 4 * s, bar = base + Shared::kHanded + 8 * s;
                 for (int r = 0; r < 2; ++r) {
                     store_peer(peer_addr(slot, r), u);
                     bar_arrive_peer(peer_addr(bar, r));
                 }
-                if (unit_of(a, count, u).kind == kEnd) break;
+                if (t.kind == kEnd) break;
             }
         }
     } else if (warp >= 4) {
@@ -400,6 +486,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         const int quarter = warp & 3, half = (warp - 4) / 4;
         const uint32_t stage = base + Shared::kData + (warp - 4) * kStore;
         const uint32_t read_bar = peer_addr(base + Shared::kRead, 0);
+        const float g = a.head->g_max;
         int sums = 0, u;
         while (true) {
             if (!__all_sync(kFull, units.next(u))) {
@@ -408,13 +495,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             }
             __syncwarp();
             if (elect_one()) units.done();
-            const Unit t = unit_of(a, count, u);
+            const Unit t = list.at(a, u);
             if (t.kind == kEnd) break;
             const int row0 = t.m0 + 128 * rank + 32 * quarter, row = row0 + lane, column = t.n0 + 128 * half;
             const int b = sums & 1;
             const uint32_t from = tmem + ((uint32_t)quarter << 21) + kTile * b + 128 * half;
             Token token{-1, 0.f, 0.f, -1};
             if (t.kind != kDWeight && row < count) token = a.tokens[row];
+            float4 before[8];
+            if (t.kind == kDHidden && t.piece > 0) sums_before(a, before, row0 + lane / 8, count, column + 4 * (lane % 8));
             if (t.blocks > 0) {
                 if (!__all_sync(kFull, bar_wait_peer(base + Shared::kReady + 8 * b, (sums / 2) & 1, kTries))) {
                     failed = true;
@@ -444,8 +533,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     if (row < count) a.part[(int64_t)(t.n0 / kTile) * a.T_pad + row] = join(r, *merge);
                 }
             } else if (t.kind == kGrad) {
-                const int words = min(a.piece, a.V - a.write * a.piece);
-                const int target = token.target - a.write * a.piece - column;
+                const int words = list.words_of(a, t.piece);
+                const int target = token.target - t.piece * a.piece - column;
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 64) {
                     if (lane == 0) stores_read();
@@ -453,10 +542,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     grad_columns(from + c, stage, lane, words - column - c, token, target - c);
                     fence_async_shared();
                     __syncwarp();
-                    if (lane == 0) store_box(&a.dz_out[a.write & 1], stage, column + c, row0);
+                    if (lane == 0) store_box(&a.dz_out[t.piece % kBuffers], stage, column + c, row0);
                 }
             } else if (t.kind == kDWeight) {
-                const float g = a.head->g_max;
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 64) {
                     if (lane == 0) stores_read();
@@ -482,39 +570,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     fence_async_shared();
                     __syncwarp();
                     // the piece's last tile may reach past it, into words that are not its own
-                    const int v0 = a.read * a.piece + row0;
+                    const int v0 = t.piece * a.piece + row0;
                     if (lane == 0 && column + c < a.d && v0 < a.V) store_box(&a.dw, stage, column + c, v0);
                 }
             } else {
-                const float g = a.head->g_max;
-                const bool first = a.read == 0, last = a.read == a.pieces - 1;
+                // by way of shared memory, so that eight lanes have 128 bytes of a row of the sums
+                const bool first = t.piece == 0, last = t.piece == a.pieces - 1;
+                const int r = lane / 8, piece = lane % 8;
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 32) {
+                    const int col = column + c + 4 * piece;
+                    if (!first && c > 0) sums_before(a, before, row0 + r, count, col);
                     uint32_t v[32];
                     __syncwarp();
                     tmem_load(from + c, v);
                     load_wait(v);
-                    float *acc = a.acc + (int64_t)row * a.d + column + c;
-                    bf16 *out = a.dh + token.row * a.dh_stride + column + c;
+                    if (lane == 0) stores_read();
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        if (token.row < 0 || column + c + i >= a.d) break;
-                        float x[8];
+                    for (int i = 0; i < 8; ++i)
+                        store_shared(swizzled(stage, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[i + j]);
-                        if (!first) {
-                            const float4 p = *reinterpret_cast<const float4 *>(acc + i), q = *reinterpret_cast<const float4 *>(acc + i + 4);
-                            x[0] += p.x, x[1] += p.y, x[2] += p.z, x[3] += p.w;
-                            x[4] += q.x, x[5] += q.y, x[6] += q.z, x[7] += q.w;
-                        }
-                        if (last) {
-                            *reinterpret_cast<uint4 *>(out + i) =
-                                make_uint4(pack_bf16(x[0] * g, x[1] * g), pack_bf16(x[2] * g, x[3] * g),
-                                           pack_bf16(x[4] * g, x[5] * g), pack_bf16(x[6] * g, x[7] * g));
-                        } else {
-                            *reinterpret_cast<float4 *>(acc + i) = make_float4(x[0], x[1], x[2], x[3]);
-                            *reinterpret_cast<float4 *>(acc + i + 4) = make_float4(x[4], x[5], x[6], x[7]);
-                        }
+                    for (int i = 0; i < 8; ++i) {
+                        const int at = r + 4 * i;
+                        float4 x = load_shared(swizzled(stage, at, piece));
+                        if (row0 + at >= count || col >= a.d) continue;
+                        if (!first) x.x += before[i].x, x.y += before[i].y, x.z += before[i].z, x.w += before[i].w;
+                        if (last)
+                            *reinterpret_cast<uint2 *>(a.dh + a.tokens[row0 + at].row * a.dh_stride + col) =
+                                make_uint2(pack_bf16(x.x * g, x.y * g), pack_bf16(x.z * g, x.w * g));
+                        else
+                            *reinterpret_cast<float4 *>(a.acc + (int64_t)(row0 + at) * a.d + col) = x;
                     }
                 }
             }
@@ -522,6 +609,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 fence_before();
                 __syncwarp();
                 if (elect_one()) bar_arrive_peer(read_bar + 8 * b);
+            }
+            if (t.kind != kScores) {
+                // what others wait for is in memory: dz, stored by copies; sums of dH; of dW, that dz has been read
+                if (t.kind == kDHidden) __threadfence();
+                __syncwarp();
+                if (lane == 0) {
+                    if (t.kind == kGrad) {
+                        stores_done();
+                        fence_async();
+                    }
+                    count_done(&a.head->done[t.piece][t.kind]);
+                }
+                __syncwarp();
             }
         }
         if (lane == 0) stores_done();
@@ -536,68 +636,96 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 
 // ---- tokens ---------------------------------------------------------------------------
 
-// The tokens that take part, closed up in their order, by one block: each
-// thread counts its stretch of them, the counts are summed, and each writes
-// its own. Also the largest |grad_loss|, the counters, and what ignored tokens give.
+// The tokens that take part, closed up in their order, by one cluster: each
+// block takes a stretch of them, counts those before each (of a warp's by
+// votes, of the warps' and blocks' by sums) and writes them. Also the largest
+// |grad_loss|, the counters, and what ignored tokens give.
+constexpr int kPrepareBlocks = 8;
+struct Tally {
+    int count;
+    float top;
+};
 template <typename I>
-__global__ void __launch_bounds__(1024) prepare_kernel(const __grid_constant__ Args a, const I *targets, int64_t ignore,
-                                                       const float *grad, int grad_stride, const float *lse) {
-    __shared__ int sums[32];
-    __shared__ float tops[32];
+__global__ void __cluster_dims__(kPrepareBlocks, 1, 1) __launch_bounds__(1024)
+    prepare_kernel(const __grid_constant__ Args a, const I *targets, int64_t ignore, const float *grad, int grad_stride,
+                   const float *lse) {
+    __shared__ Tally warps[32], block;
+    start_next();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
-    const int64_t each = (a.T + 1023) / 1024, t0 = min(a.T, tid * each), t1 = min(a.T, t0 + each);
-    int n = 0;
-    float top = 0.f;
-    for (int64_t t = t0; t < t1; ++t) {
-        const int64_t y = targets[t];
-        const bool in = y >= 0 && y < a.V && y != ignore;
+    const uint32_t rank = cluster_rank();
+    // of each warp: a multiple of 32 tokens
+    const int64_t each = ((a.T + 32 * kPrepareBlocks - 1) / (32 * kPrepareBlocks) + 31) / 32 * 32;
+    const int64_t t0 = min(a.T, (int64_t)(rank * 32 + warp) * each), t1 = min(a.T, t0 + each);
+    auto counts = [&](int64_t y) { return y >= 0 && y < a.V && y != ignore; };
+    Tally mine{0, 0.f};
+#pragma unroll 4
+    for (int64_t t = t0 + lane; t < t0 + each; t += 32) {
+        const int64_t y = t < t1 ? (int64_t)targets[t] : ignore;
+        const bool in = t < t1 && counts(y);
         if (!in && y != ignore) set_status(a.status, DPB_DEV_BAD_INDEX);
-        n += in;
+        mine.count += __popc(__ballot_sync(kFull, in));
         if (grad && in) {
             const float g = fabsf(grad[t * grad_stride]);
-            if (g <= 3.402823466e38f) top = fmaxf(top, g);
+            if (g <= 3.402823466e38f) mine.top = fmaxf(mine.top, g);
         }
     }
-    int before = n;
 #pragma unroll
-    for (int i = 1; i < 32; i *= 2) {
-        const int x = __shfl_up_sync(kFull, before, i);
-        if (lane >= i) before += x;
-        top = fmaxf(top, __shfl_xor_sync(kFull, top, i));
-    }
-    if (lane == 31) sums[warp] = before;
-    if (lane == 0) tops[warp] = top;
+    for (int i = 16; i > 0; i /= 2) mine.top = fmaxf(mine.top, __shfl_xor_sync(kFull, mine.top, i));
+    if (lane == 0) warps[warp] = mine;
     __syncthreads();
-    int total = 0, place = before - n;
-    top = 0.f;
+    int place = 0;
+    Tally all{0, 0.f};
     for (int w = 0; w < 32; ++w) {
-        if (w < warp) place += sums[w];
-        total += sums[w];
-        top = fmaxf(top, tops[w]);
+        if (w < warp) place += warps[w].count;
+        all.count += warps[w].count;
+        all.top = fmaxf(all.top, warps[w].top);
     }
-    if (top == 0.f) top = 1.f;
-    if (tid == 0) {
-        a.head->count = total;
-        a.head->all = total == a.T;
-        if (a.counted) *a.counted = total;
-        a.head->g_max = top;
+    if (tid == 0) block = all;
+    cluster_sync();
+    all = Tally{0, 0.f};
+    for (uint32_t r = 0; r < kPrepareBlocks; ++r) {
+        const uint32_t at = peer_addr(smem_addr(&block), r);
+        Tally o;
+        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(o.count) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.top) : "r"(at + 4) : "memory");
+        if (r < rank) place += o.count;
+        all.count += o.count;
+        all.top = fmaxf(all.top, o.top);
     }
-    for (int i = tid; i < 60; i += 1024) a.head->next[i] = 0;
-    for (int64_t t = t0; t < t1; ++t) {
-        const int64_t y = targets[t];
-        const bool in = y >= 0 && y < a.V && y != ignore;
-        a.place[t] = in ? place : -1;
+    if (all.top == 0.f) all.top = 1.f;
+    if (rank == 0) {
+        if (tid == 0) {
+            a.head->count = all.count;
+            a.head->all = all.count == a.T;
+            if (a.counted) *a.counted = all.count;
+            a.head->g_max = all.top;
+        }
+        if (tid == 0) a.head->next = 0;
+        if (tid < 4 * kMostPieces) (&a.head->done[0][0])[tid] = 0;
+    }
+#pragma unroll 4
+    for (int64_t t = t0 + lane; t < t0 + each; t += 32) {
+        const int64_t y = t < t1 ? (int64_t)targets[t] : ignore;
+        const bool in = t < t1 && counts(y);
+        const unsigned votes = __ballot_sync(kFull, in);
+        const int here = place + __popc(votes & ((1u << lane) - 1));
+        place += __popc(votes);
+        if (t >= t1) continue;
+        a.place[t] = in ? here : -1;
         if (in)
-            a.tokens[place++] = Token{(int)y, lse ? lse[t] * kLog2e : 0.f, grad ? grad[t * grad_stride] / top : 0.f, (int)t};
+            a.tokens[here] = Token{(int)y, lse ? lse[t] * kLog2e : 0.f, grad ? grad[t * grad_stride] / all.top : 0.f, (int)t};
         else if (a.loss)
             a.loss[t] = a.lse[t] = 0.f;
     }
+    cluster_sync();  // the others have read this block's tally
 }
 
 // Where tokens are left out: the others' rows closed up, and zeros behind them
 // to the end of a tile (a product sums over these); zeros in the gradient of
 // those left out.
 __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Args a) {
+    start_next();
+    wait_previous();
     if (a.head->all) return;
     const int lane = threadIdx.x & 31, pieces = a.d / 8;
     const int64_t warps = (int64_t)gridDim.x * 8, end = min(a.T, (int64_t)(a.head->count + kTile - 1) / kTile * kTile);
@@ -620,6 +748,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Arg
 // 32 threads and then of the threads.
 __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args a) {
     __shared__ float2 parts[32][33];
+    wait_previous();
     const int lane = threadIdx.x & 31, slice = threadIdx.x / 32, count = a.head->count;
     const int tiles = (a.V + kTile - 1) / kTile;
     const int64_t row = blockIdx.x * 32ll + lane;
@@ -639,9 +768,9 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args
     if (lane == 0 && mine < count) {
         const Token t = a.tokens[mine];
         // not from the rounded lse: a sure row's loss keeps its digits
-        const double l = log((double)r.y);
-        a.lse[t.row] = (float)(r.x + l);
-        a.loss[t.row] = (float)((double)r.x - a.z_target[mine] + l);
+        const float l = logf(r.y);
+        a.lse[t.row] = r.x + l;
+        a.loss[t.row] = r.x - a.z_target[mine] + l;
     }
 }
 
@@ -680,11 +809,11 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // Words of a piece of the gradient.
 constexpr int64_t kPieceBytes = 64ll << 20;
-constexpr int kLeastPiece = 4096, kMostPieces = 48;
+constexpr int kLeastPiece = 4096;
 
 struct Space {
     int64_t T_pad, piece, pieces;
-    size_t head, tokens, place, closed, part, z_target, dz[2], acc, bytes;
+    size_t head, tokens, place, closed, part, z_target, dz[kBuffers], acc, bytes;
     Space(const dpb_linear_loss_config *c, bool backward) {
         const size_t T = (size_t)c->tokens, d = (size_t)c->dim, V = (size_t)c->vocab;
         T_pad = round_up(c->tokens, kTile);
@@ -704,14 +833,14 @@ struct Space {
         place = take(T * 4);
         closed = take(T * d * 2);
         if (backward) {
-            dz[0] = take((size_t)T_pad * piece * 2);
-            dz[1] = pieces > 1 ? take((size_t)T_pad * piece * 2) : dz[0];
+            for (int i = 0; i < kBuffers; ++i) dz[i] = i < pieces ? take((size_t)T_pad * piece * 2) : dz[0];
             acc = pieces > 1 ? take((size_t)T * d * 4) : at;
             part = z_target = at;
         } else {
             part = take((V + kTile - 1) / kTile * (size_t)T_pad * sizeof(float2));
             z_target = take((size_t)T_pad * 4);
-            dz[0] = dz[1] = acc = at;
+            for (size_t &x : dz) x = at;
+            acc = at;
         }
         bytes = at;
     }
@@ -750,8 +879,7 @@ dpb_status launch_products(const Args &a, int64_t units, cudaStream_t s) {
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(product_kernel), kSmem);
     if (e != cudaSuccess) return launch_status(e, "linear_cross_entropy");
     const unsigned pairs = (unsigned)std::max<int64_t>(1, std::min<int64_t>(units, pairs_of_blocks()));
-    product_kernel<<<2 * pairs, kThreads, kSmem, s>>>(a);
-    return launch_status(cudaGetLastError(), "linear_cross_entropy");
+    return launch_status(launch_early(product_kernel, dim3(2 * pairs), kThreads, kSmem, s, a), "linear_cross_entropy");
 }
 
 // What both directions begin with.
@@ -773,12 +901,12 @@ dpb_status begin(Args &a, const Space &w, const dpb_linear_loss_config *c, const
     DPB_CHECK(make_map(&a.closed, a.closed_rows, c->dim, c->tokens, c->dim, 64));
     DPB_CHECK(make_map(&a.weight, weight->data, weight->stride, c->vocab, c->dim, 64));
     if (c->index_bytes == 4)
-        prepare_kernel<<<1, 1024, 0, s>>>(a, static_cast<const int32_t *>(targets), c->ignore_index, grad, c->grad_stride, lse);
+        prepare_kernel<<<kPrepareBlocks, 1024, 0, s>>>(a, static_cast<const int32_t *>(targets), c->ignore_index, grad, c->grad_stride, lse);
     else
-        prepare_kernel<<<1, 1024, 0, s>>>(a, static_cast<const int64_t *>(targets), c->ignore_index, grad, c->grad_stride, lse);
+        prepare_kernel<<<kPrepareBlocks, 1024, 0, s>>>(a, static_cast<const int64_t *>(targets), c->ignore_index, grad, c->grad_stride, lse);
     DPB_CHECK(launch_status(cudaGetLastError(), "linear_cross_entropy (tokens)"));
-    gather_kernel<<<(unsigned)std::min<int64_t>((c->tokens + 7) / 8, 1216), 256, 0, s>>>(a);
-    return launch_status(cudaGetLastError(), "linear_cross_entropy (rows)");
+    const unsigned blocks = (unsigned)std::min<int64_t>((c->tokens + 7) / 8, 1216);
+    return launch_status(launch_early(gather_kernel, dim3(blocks), 256, 0, s, a), "linear_cross_entropy (rows)");
 }
 
 }  // namespace
@@ -819,11 +947,10 @@ dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, c
     a.counted = counted;
     a.part = reinterpret_cast<float2 *>(ws + w.part);
     a.z_target = reinterpret_cast<float *>(ws + w.z_target);
-    a.write = a.read = -1;
     DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, nullptr, nullptr, ws, s));
     DPB_CHECK(launch_products(a, w.T_pad / kTile * ((cfg->vocab + kTile - 1) / kTile), s));
-    join_kernel<<<(unsigned)((cfg->tokens + 31) / 32), 1024, 0, s>>>(a);
-    return launch_status(cudaGetLastError(), "linear_cross_entropy (rows' sums)");
+    return launch_status(launch_early(join_kernel, dim3((unsigned)((cfg->tokens + 31) / 32)), 1024, 0, s, a),
+                         "linear_cross_entropy (rows' sums)");
 }
 
 dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
@@ -856,19 +983,13 @@ dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, 
     if (grad_hidden) a.dh = static_cast<bf16 *>(grad_hidden->data), a.dh_stride = grad_hidden->stride;
     if (grad_weight) DPB_CHECK(make_map(&a.dw, grad_weight->data, grad_weight->stride, cfg->vocab, cfg->dim, 32));
     a.acc = reinterpret_cast<float *>(ws + w.acc);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kBuffers; ++i) {
         DPB_CHECK(make_map(&a.dz[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 64));
         DPB_CHECK(make_map(&a.dz_out[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 32));
     }
     DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, grad_loss, lse, ws, s));
-    const int64_t tiles_m = w.T_pad / kTile, tiles_v = w.piece / kTile, tiles_d = (cfg->dim + kTile - 1) / kTile;
-    for (int i = 0; i <= w.pieces; ++i) {
-        a.write = i < w.pieces ? i : -1;
-        a.read = i - 1;
-        a.launch = i;
-        DPB_CHECK(launch_products(a, (i < w.pieces ? tiles_m * tiles_v : 0) + (i > 0 ? (tiles_m + tiles_v) * tiles_d : 0), s));
-    }
-    return DPB_OK;
+    const int64_t tiles_m = w.T_pad / kTile, tiles_v = (cfg->vocab + kTile - 1) / kTile, tiles_d = (cfg->dim + kTile - 1) / kTile;
+    return launch_products(a, tiles_m * tiles_v + tiles_v * tiles_d, s);
 }
 
 }  // extern "C"

@@ -18,6 +18,7 @@ namespace dpb {
 namespace {
 
 constexpr int kMostDim = 16384;
+constexpr int kGradBlocks = 4;  // of an SM, at most, in the gradient
 
 struct NormArgs {
     const void *x, *delta, *w, *dy, *ds;
@@ -43,113 +44,122 @@ __device__ __forceinline__ float row_sum(float v, int row_warps, float *sums) {
     return v;
 }
 
+// P pieces of a row, one of each row_threads.
+template <typename E, int N, int P>
+__device__ __forceinline__ void load_row(Bits<E, N> (&r)[P], const void *data, int64_t stride, int64_t t, bool live, int in,
+                                         int row_threads, int d) {
+    const E *row = static_cast<const E *>(data) + t * stride;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int i = (in + p * row_threads) * N;
+        r[p] = Bits<E, N>{};
+        if (live && i < d) load_bits(row + i, r[p]);
+    }
+}
+
+// Each row's threads load the next row while they work on one.
 template <typename E, int N, int P, int MOST>
-__global__ void __launch_bounds__(MOST) add_norm_kernel(const NormArgs a, int row_warps) {
+__global__ void __launch_bounds__(MOST) add_norm_kernel(const __grid_constant__ NormArgs a, int row_warps) {
     __shared__ float sums[32];
-    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads;
-    const int64_t rows_at_once = (int64_t)gridDim.x * (blockDim.x / row_threads);
+    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = MOST / row_threads;
+    const int64_t step = (int64_t)gridDim.x * rows;
+    int64_t t = (int64_t)blockIdx.x * rows + threadIdx.x / row_threads;
+    Bits<E, N> w[P], x[P], delta[P];
+    if (a.w) load_row(w, a.w, 0, 0, true, in, row_threads, a.d);
+    load_row(x, a.x, a.xs, t, t < a.T, in, row_threads, a.d);
+    if (a.delta) load_row(delta, a.delta, a.deltas, t, t < a.T, in, row_threads, a.d);
     // every thread of the block makes the same number of turns
-    for (int64_t t0 = (int64_t)blockIdx.x * (blockDim.x / row_threads); t0 < a.T; t0 += rows_at_once) {
-        const int64_t t = t0 + threadIdx.x / row_threads;
+    for (int64_t t0 = (int64_t)blockIdx.x * rows; t0 < a.T; t0 += step, t += step) {
         const bool live = t < a.T;
-        const E *x = static_cast<const E *>(a.x) + t * a.xs, *delta = static_cast<const E *>(a.delta) + t * a.deltas;
-        E *s = static_cast<E *>(a.s) + t * a.ss, *y = static_cast<E *>(a.y) + t * a.ys;
-        Piece<E, N> v[P], more[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int i = (in + p * row_threads) * N;
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[p].v[j] = more[p].v[j] = 0.f;
-            if (live && i < a.d) {
-                load_piece(x + i, v[p]);
-                if (a.delta) load_piece(delta + i, more[p]);
-            }
-        }
+        Piece<E, N> v[P];
         float sum = 0.f;
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p) {
+            v[p] = values(x[p]);
+            if (a.delta) {
+                const Piece<E, N> more = values(delta[p]);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if (a.delta) {
-                    v[p].v[j] += more[p].v[j];
+                for (int j = 0; j < N; ++j) {
+                    v[p].v[j] += more.v[j];
                     if (sizeof(E) == 2) v[p].v[j] = __bfloat162float(__float2bfloat16_rn(v[p].v[j]));
                 }
-                sum = fmaf(v[p].v[j], v[p].v[j], sum);
             }
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum = fmaf(v[p].v[j], v[p].v[j], sum);
+        }
+        load_row(x, a.x, a.xs, t + step, t + step < a.T, in, row_threads, a.d);
+        if (a.delta) load_row(delta, a.delta, a.deltas, t + step, t + step < a.T, in, row_threads, a.d);
         sum = row_sum(sum, row_warps, sums);
         const float r = rsqrtf(sum / a.d + a.eps);
+        E *s = static_cast<E *>(a.s) + t * a.ss, *y = static_cast<E *>(a.y) + t * a.ys;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int i = (in + p * row_threads) * N;
             if (!live || i >= a.d) continue;
             if (a.s) store_piece(s + i, v[p]);
-            Piece<E, N> w;
-            if (a.w) load_piece(static_cast<const E *>(a.w) + i, w);
+            const Piece<E, N> k = values(w[p]);
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[p].v[j] = v[p].v[j] * r * (a.w ? w.v[j] : 1.f);
+            for (int j = 0; j < N; ++j) v[p].v[j] = v[p].v[j] * r * (a.w ? k.v[j] : 1.f);
             store_piece(y + i, v[p]);
         }
     }
 }
 
 template <typename E, int N, int P, int MOST>
-__global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const NormArgs a, int row_warps) {
+__global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const __grid_constant__ NormArgs a, int row_warps) {
     __shared__ float sums[32];
     extern __shared__ float columns[];  // [d]: the block's dw
-    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = blockDim.x / row_threads;
+    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = MOST / row_threads;
+    const int64_t step = (int64_t)gridDim.x * rows;
+    int64_t t = (int64_t)blockIdx.x * rows + threadIdx.x / row_threads;
     float dw[P][N];
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int j = 0; j < N; ++j) dw[p][j] = 0.f;
-    const int64_t rows_at_once = (int64_t)gridDim.x * rows;
-    for (int64_t t0 = (int64_t)blockIdx.x * rows; t0 < a.T; t0 += rows_at_once) {
-        const int64_t t = t0 + threadIdx.x / row_threads;
+    Bits<E, N> w[P], s[P], dy[P], ds[P];
+    if (a.w) load_row(w, a.w, 0, 0, true, in, row_threads, a.d);
+    load_row(s, a.x, a.xs, t, t < a.T, in, row_threads, a.d);
+    load_row(dy, a.dy, a.dys, t, t < a.T, in, row_threads, a.d);
+    if (a.ds) load_row(ds, a.ds, a.dss, t, t < a.T, in, row_threads, a.d);
+    for (int64_t t0 = (int64_t)blockIdx.x * rows; t0 < a.T; t0 += step, t += step) {
         const bool live = t < a.T;
-        const E *s = static_cast<const E *>(a.x) + t * a.xs, *dy = static_cast<const E *>(a.dy) + t * a.dys;
-        const E *ds = static_cast<const E *>(a.ds) + t * a.dss;
-        E *dx = static_cast<E *>(a.dx) + t * a.dxs;
-        Piece<E, N> v[P], g[P], rest[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int i = (in + p * row_threads) * N;
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[p].v[j] = g[p].v[j] = rest[p].v[j] = 0.f;
-            if (live && i < a.d) {
-                load_piece(s + i, v[p]);
-                load_piece(dy + i, g[p]);
-                if (a.ds) load_piece(ds + i, rest[p]);
-            }
-        }
+        Bits<E, N> s0[P], dy0[P], ds0[P];
         float sq = 0.f, us = 0.f;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int i = (in + p * row_threads) * N;
-            Piece<E, N> w;
-            if (a.w && i < a.d) load_piece(static_cast<const E *>(a.w) + i, w);
+            s0[p] = s[p], dy0[p] = dy[p];
+            if (a.ds) ds0[p] = ds[p];
+        }
+        load_row(s, a.x, a.xs, t + step, t + step < a.T, in, row_threads, a.d);
+        load_row(dy, a.dy, a.dys, t + step, t + step < a.T, in, row_threads, a.d);
+        if (a.ds) load_row(ds, a.ds, a.dss, t + step, t + step < a.T, in, row_threads, a.d);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const Piece<E, N> v = values(s0[p]), g = values(dy0[p]), k = values(w[p]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float u = a.w && i < a.d ? g[p].v[j] * w.v[j] : g[p].v[j];
-                sq = fmaf(v[p].v[j], v[p].v[j], sq);
-                us = fmaf(u, v[p].v[j], us);
+                sq = fmaf(v.v[j], v.v[j], sq);
+                us = fmaf(a.w ? g.v[j] * k.v[j] : g.v[j], v.v[j], us);
             }
         }
         sq = row_sum(sq, row_warps, sums);
         us = row_sum(us, row_warps, sums);
-        const float r = rsqrtf(sq / a.d + a.eps), k = r * r * r * (us / a.d);
+        const float r = rsqrtf(sq / a.d + a.eps), less = r * r * r * (us / a.d);
+        E *dx = static_cast<E *>(a.dx) + t * a.dxs;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int i = (in + p * row_threads) * N;
             if (!live || i >= a.d) continue;
-            Piece<E, N> w;
-            if (a.w) load_piece(static_cast<const E *>(a.w) + i, w);
+            Piece<E, N> v = values(s0[p]), rest;
+            const Piece<E, N> g = values(dy0[p]), k = values(w[p]);
+            if (a.ds) rest = values(ds0[p]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float u = a.w ? g[p].v[j] * w.v[j] : g[p].v[j];
-                dw[p][j] = fmaf(g[p].v[j] * r, v[p].v[j], dw[p][j]);
-                v[p].v[j] = fmaf(-k, v[p].v[j], fmaf(r, u, rest[p].v[j]));
+                dw[p][j] = fmaf(g.v[j] * r, v.v[j], dw[p][j]);
+                v.v[j] = fmaf(-less, v.v[j], fmaf(r, a.w ? g.v[j] * k.v[j] : g.v[j], a.ds ? rest.v[j] : 0.f));
             }
-            store_piece(dx + i, v[p]);
+            store_piece(dx + i, v);
         }
     }
     if (!a.part) return;
@@ -165,7 +175,7 @@ __global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const NormArgs a, i
                 }
         __syncthreads();
     }
-    for (int i = threadIdx.x; i < a.d; i += blockDim.x) a.part[(int64_t)blockIdx.x * a.d + i] = columns[i];
+    for (int i = threadIdx.x; i < a.d; i += MOST) a.part[(int64_t)blockIdx.x * a.d + i] = columns[i];
 }
 
 // 32 columns of all blocks' sums: 32 threads a column, each its blocks in
@@ -187,6 +197,17 @@ __global__ void __launch_bounds__(1024) add_norm_columns_kernel(const NormArgs a
 
 // ---- host side ------------------------------------------------------------------
 
+// Blocks of a kernel that an SM holds at a time.
+int resident_blocks(const void *kernel, int threads, size_t smem) {
+    int n = 0;
+    if (allow_smem(kernel, smem) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    return std::max(n, 1);
+}
+
 // Threads that share a row, and the pieces of each of them: a warp where its
 // lanes can hold the row (4 pieces of 16 bytes each, 16 of one value), then up
 // to 8 warps, and 32 for the widest rows.
@@ -196,28 +217,33 @@ struct RowShape {
         warps = 1;
         while (32 * warps * most < row_pieces) warps = warps < 8 ? 2 * warps : 32;
         const int each = (row_pieces + 32 * warps - 1) / (32 * warps);
-        pieces = 1;
-        while (pieces < each) pieces *= 2;
+        pieces = each;
+        if (most > 4)  // of one value: 1, 2, 4, 8 or 16
+            for (pieces = 1; pieces < each;) pieces *= 2;
     }
 };
 
 template <typename E, int N, int P, int MOST>
-dpb_status launch(const NormArgs &a, const RowShape &r, bool grad, cudaStream_t s) {
+dpb_status launch(NormArgs &a, const RowShape &r, bool grad, cudaStream_t s) {
     const int rows = MOST / (32 * r.warps);
     if (!grad) {
-        const int64_t blocks = std::min<int64_t>((a.T + rows - 1) / rows, 1 << 20);
+        static const int resident = resident_blocks(reinterpret_cast<const void *>(add_norm_kernel<E, N, P, MOST>), MOST, 0);
+        const int64_t blocks = std::min<int64_t>((a.T + rows - 1) / rows, (int64_t)resident * sms_of_device());
         add_norm_kernel<E, N, P, MOST><<<(unsigned)blocks, MOST, 0, s>>>(a, r.warps);
         return launch_status(cudaGetLastError(), "add_norm");
     }
     const size_t smem = a.part ? (size_t)a.d * 4 : 0;
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(add_norm_grad_kernel<E, N, P, MOST>), smem);
     if (e != cudaSuccess) return launch_status(e, "add_norm_backward");
+    static const int resident =
+        resident_blocks(reinterpret_cast<const void *>(add_norm_grad_kernel<E, N, P, MOST>), MOST, kMostDim * 4);
+    a.blocks = (int)std::min<int64_t>((a.T + rows - 1) / rows, (int64_t)std::min(resident, kGradBlocks) * sms_of_device());
     add_norm_grad_kernel<E, N, P, MOST><<<a.blocks, MOST, smem, s>>>(a, r.warps);
     return launch_status(cudaGetLastError(), "add_norm_backward");
 }
 
 template <typename E, int N>
-dpb_status dispatch(const NormArgs &a, bool grad, cudaStream_t s) {
+dpb_status dispatch(NormArgs &a, bool grad, cudaStream_t s) {
     const RowShape r((a.d + N - 1) / N, N == 1 ? 16 : 4);
     if (r.warps > 8) {  // 2 or more pieces: what 8 warps cannot hold
         if constexpr (N == 8) return launch<E, N, 2, 1024>(a, r, grad, s);
@@ -226,12 +252,14 @@ dpb_status dispatch(const NormArgs &a, bool grad, cudaStream_t s) {
     }
     if (r.pieces == 1) return launch<E, N, 1, 256>(a, r, grad, s);
     if (r.pieces == 2) return launch<E, N, 2, 256>(a, r, grad, s);
+    if constexpr (N > 1)
+        if (r.pieces == 3) return launch<E, N, 3, 256>(a, r, grad, s);
     if (r.pieces == 4) return launch<E, N, 4, 256>(a, r, grad, s);
     if constexpr (N == 1) return r.pieces == 8 ? launch<E, N, 8, 256>(a, r, grad, s) : launch<E, N, 16, 256>(a, r, grad, s);
     return fail(DPB_ERR_UNSUPPORTED, "dim is too large");
 }
 
-dpb_status run(const NormArgs &a, int dtype, bool pieces, bool grad, cudaStream_t s) {
+dpb_status run(NormArgs &a, int dtype, bool pieces, bool grad, cudaStream_t s) {
     using bf16 = __nv_bfloat16;
     if (dtype == DPB_F32) return pieces && a.d % 4 == 0 ? dispatch<float, 4>(a, grad, s) : dispatch<float, 1>(a, grad, s);
     return pieces && a.d % 8 == 0 ? dispatch<bf16, 8>(a, grad, s) : dispatch<bf16, 1>(a, grad, s);
@@ -258,10 +286,8 @@ bool rows_by_pieces(const dpb_norm_config *c, const dpb_rows *r) {
     return !r || by_pieces(r->data, r->stride, c->tokens, c->dtype == DPB_F32 ? 4 : 2);
 }
 
-// Blocks of the gradient: enough to fill the device, each with a part of dw.
-int grad_blocks(const dpb_norm_config *c) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>((c->tokens + 7) / 8, 2 * sms_of_device()));
-}
+// Blocks of the gradient, at most, each with a part of dw.
+int64_t most_blocks(const dpb_norm_config *c) { return std::min<int64_t>(c->tokens, (int64_t)kGradBlocks * sms_of_device()); }
 
 }  // namespace
 }  // namespace dpb
@@ -295,7 +321,7 @@ dpb_status dpb_add_norm(const dpb_norm_config *cfg, const dpb_rows *x, const dpb
 dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes) {
     DPB_CHECK(check_config(cfg));
     if (!bytes) return fail(DPB_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = ((size_t)grad_blocks(cfg) * cfg->dim * 4 + 255) / 256 * 256;
+    *bytes = ((size_t)most_blocks(cfg) * cfg->dim * 4 + 255) / 256 * 256;
     return DPB_OK;
 }
 
@@ -322,9 +348,8 @@ dpb_status dpb_add_norm_backward(const dpb_norm_config *cfg, const dpb_rows *tot
     a.w = weight;
     a.dx = grad_x->data, a.dxs = grad_x->stride;
     a.T = cfg->tokens, a.d = cfg->dim, a.eps = cfg->eps;
-    a.blocks = grad_blocks(cfg);
     if (grad_weight) {
-        DPB_CHECK(need_workspace(workspace, workspace_bytes, (size_t)a.blocks * a.d * 4));
+        DPB_CHECK(need_workspace(workspace, workspace_bytes, (size_t)most_blocks(cfg) * a.d * 4));
         a.dw = grad_weight;
         a.part = static_cast<float *>(workspace);
     }

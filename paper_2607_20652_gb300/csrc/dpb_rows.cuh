@@ -51,8 +51,25 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const Piece<__nv_b
     *p = __float2bfloat16_rn(r.v[0]);
 }
 
+// A piece as it lies in memory: what a thread holds of a row on its way.
+template <typename E, int N>
+struct Bits {
+    uint4 w;
+};
 template <typename E>
-constexpr int kPieceOf = 16 / (int)sizeof(E);
+struct Bits<E, 1> {
+    E w;
+};
+template <typename E, int N>
+__device__ __forceinline__ void load_bits(const E *p, Bits<E, N> &r) {
+    r.w = *reinterpret_cast<const decltype(r.w) *>(p);
+}
+template <typename E, int N>
+__device__ __forceinline__ Piece<E, N> values(const Bits<E, N> &b) {
+    Piece<E, N> r;
+    load_piece(reinterpret_cast<const E *>(&b.w), r);
+    return r;
+}
 
 // Whether rows at `p` with this stride can be read in pieces of 16 bytes.
 inline bool by_pieces(const void *p, int64_t stride, int64_t rows, int elem) {

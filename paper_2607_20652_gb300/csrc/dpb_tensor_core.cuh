@@ -58,6 +58,8 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap *map, i
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
+// Between plain accesses and those of copies, shared memory and global.
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
 // This thread's plain shared-memory writes become visible to copies and
 // matrix products.
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }

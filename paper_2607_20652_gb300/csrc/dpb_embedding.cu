@@ -20,9 +20,11 @@
 namespace dpb {
 namespace {
 
-constexpr int kSortBlocks = 8;    // of the sorting cluster
+constexpr int kSortBlocks = 16;   // of the sorting cluster
 constexpr int kSortWarps = 32;    // of a block
 constexpr int kDigits = 256;      // 8 bits a pass
+constexpr int kSumWarps = 2;      // of a summing block: few, so that an SM holds twelve of their 160 registers a lane
+constexpr int kSumResident = 12;
 
 // A token on its way: its id (vocab: none that counts) and its place.
 struct Sorted {
@@ -39,6 +41,7 @@ struct LookupArgs {
     float scale;
     Sorted *sorted[2];
     float *head, *tail;  // [stretches][d]: sums of the first row, begun before, and of the last, begun here and going on
+    int *open;           // how many stretches' last rows go on, and which
     int32_t *status;
 };
 
@@ -74,13 +77,24 @@ __device__ __forceinline__ int read_peer(uint32_t addr) {
     return v;
 }
 
+// The lanes with this lane's digit (-1: none; its answer then says nothing), by
+// a vote for each bit (65536 tokens: 4 us less than by match.any).
+__device__ __forceinline__ unsigned same_digit(int digit) {
+    unsigned same = __ballot_sync(kFull, digit >= 0);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const unsigned ones = __ballot_sync(kFull, (digit >> b) & 1);
+        same &= (digit >> b) & 1 ? ones : ~ones;
+    }
+    return same;
+}
+
 // The first cluster sorts, a digit of 8 bits a pass: each warp counts the
 // digits of its stretch of the tokens, the counts of all warps before it give
 // each digit's first place, and it puts its tokens there in their order.
 // The other clusters write zeros.
 template <typename E, int N, typename I>
-__global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSortWarps, 1)
-    embedding_sort_kernel(const __grid_constant__ LookupArgs a, const I *ids) {
+__global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(const __grid_constant__ LookupArgs a, const I *ids) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
     tc::start_next();
     if (blockIdx.x >= kSortBlocks) {
@@ -95,13 +109,17 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
     }
     __shared__ int count[kSortWarps][kDigits], total[kDigits], sums[kDigits / 32];
     const uint32_t rank = blockIdx.x;
-    const int64_t each = ((a.T + kSortBlocks * kSortWarps - 1) / (kSortBlocks * kSortWarps) + 31) / 32 * 32;
+    const int64_t warps = kSortBlocks * kSortWarps, each = ((a.T + warps - 1) / warps + 31) / 32 * 32;
     const int64_t t0 = min(a.T, (rank * kSortWarps + warp) * each), t1 = min(a.T, t0 + each);
-    constexpr int kHeld = 8;  // tokens of a lane under way: all of them up to 65536
+    if (rank == 0 && tid == 0) *a.open = 0;
+    constexpr int kHeld = 4;  // tokens of a lane under way: all of them up to 65536
     for (int pass = 0; pass < a.passes; ++pass) {
         const Sorted *from = a.sorted[(pass & 1) ^ 1];
         Sorted *to = a.sorted[pass & 1];
         Sorted x[kHeld];
+        int place[kHeld];  // among the warp's tokens of the same digit
+        auto digit = [&](int id) { return id < 0 ? -1 : (id >> (8 * pass)) & 255; };
+        // the tokens from t on, and their places behind those that `count` has
         auto load = [&](int64_t t) {
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
@@ -117,24 +135,24 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
                     x[k] = Sorted{ok ? (int)id : a.V, (int)at};
                 }
             }
-        };
-        auto digit = [&](int id) { return id < 0 ? -1 : (id >> (8 * pass)) & 255; };
-        for (int i = tid; i < kSortWarps * kDigits; i += 32 * kSortWarps) (&count[0][0])[i] = 0;
-        __syncthreads();
-        for (int64_t t = t0; t < t1; t += 32 * kHeld) {
-            load(t);
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
                 if (t + 32 * k >= t1) break;
                 const int g = digit(x[k].id);
-                const unsigned same = __match_any_sync(kFull, g);
+                const unsigned same = same_digit(g);
+                place[k] = g >= 0 ? count[warp][g] + __popc(same & ((1u << lane) - 1)) : 0;
+                __syncwarp();
                 if (g >= 0 && lane == __ffs(same) - 1) count[warp][g] += __popc(same);
                 __syncwarp();
             }
-        }
+        };
+        for (int i = tid; i < kSortWarps * kDigits; i += 32 * kSortWarps) (&count[0][0])[i] = 0;
+        __syncthreads();
+        for (int64_t t = t0; t < t1; t += 32 * kHeld) load(t);
         __syncthreads();
         if (tid < kDigits) {  // the block's warps before each
             int n = 0;
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) {
                 const int c = count[w][tid];
                 count[w][tid] = n;
@@ -164,23 +182,20 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
         if (tid < kDigits) {
             int first = upto - all + before;
             for (int w = 0; w < warp; ++w) first += sums[w];
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) count[w][tid] += first;
         }
         __syncthreads();
-        for (int64_t t = t0; t < t1; t += 32 * kHeld) {
-            if (each > 32 * kHeld) load(t);  // else still held
+        if (each <= 32 * kHeld) {  // still held, with their places from 0
 #pragma unroll
-            for (int k = 0; k < kHeld; ++k) {
-                if (t + 32 * k >= t1) break;
-                const int g = digit(x[k].id);
-                const unsigned same = __match_any_sync(kFull, g);
-                const int place = g >= 0 ? count[warp][g] + __popc(same & ((1u << lane) - 1)) : 0;
-                __syncwarp();
-                if (g >= 0) {
-                    to[place] = x[k];
-                    if (lane == __ffs(same) - 1) count[warp][g] += __popc(same);
-                }
-                __syncwarp();
+            for (int k = 0; k < kHeld; ++k)
+                if (x[k].id >= 0 && t0 < t1) to[count[warp][digit(x[k].id)] + place[k]] = x[k];
+        } else {
+            for (int64_t t = t0; t < t1; t += 32 * kHeld) {
+                load(t);
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k)
+                    if (x[k].id >= 0) to[place[k]] = x[k];
             }
         }
         // the others have read this block's totals, and all tokens are in place
@@ -193,11 +208,11 @@ __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(32 * kSort
 // A warp sums one stretch of the sorted tokens over 32 P N columns, the next
 // rows under way while it adds some.
 template <typename E, int N, int P>
-__global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constant__ LookupArgs a) {
+__global__ void __launch_bounds__(32 * kSumWarps) embedding_sum_kernel(const __grid_constant__ LookupArgs a) {
     tc::start_next();
     tc::wait_previous();
     const int lane = threadIdx.x & 31;
-    const int64_t c = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    const int64_t c = (int64_t)blockIdx.x * kSumWarps + threadIdx.x / 32;
     if (c >= a.stretches) return;
     const Sorted *sorted = a.sorted[(a.passes - 1) & 1];
     const int64_t p0 = c * a.stretch, p1 = min(a.T, p0 + a.stretch);
@@ -273,49 +288,48 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
         }
     }
     flush(id != next);
+    if (whole && id == next && id < a.V && blockIdx.y == 0 && lane == 0) a.open[1 + atomicAdd(a.open, 1)] = (int)c;
 }
 
-// A row whose tokens go on after the stretch where they begin: the sum of what
-// each stretch has of it. A warp has 32 M columns of one stretch's last row.
+// The rows whose tokens go on after the stretch where they begin: the sum of
+// what each stretch has of them. A warp has 32 M columns of one at a time.
+constexpr int kJoinWarps = 4;
 template <typename E, int M>
-__global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_constant__ LookupArgs a, int groups) {
+__global__ void __launch_bounds__(32 * kJoinWarps) embedding_join_kernel(const __grid_constant__ LookupArgs a, int groups) {
     tc::wait_previous();
     const int lane = threadIdx.x & 31;
-    const int64_t w = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, c = w / groups;
+    const int64_t warps = (int64_t)gridDim.x * kJoinWarps, items = (int64_t)*a.open * groups;
     const Sorted *sorted = a.sorted[(a.passes - 1) & 1];
-    const int64_t p0 = c * a.stretch, end = p0 + a.stretch;
-    if (end >= a.T) return;
-    const int before = p0 > 0 ? sorted[p0 - 1].id : -1, first = sorted[p0].id, id = sorted[end - 1].id, after = sorted[end].id;
-    if (id >= a.V || after != id) return;
-    if (first == id && before == id) return;  // it begins earlier
-    const int i = ((int)(w - c * groups) * 32 + lane) * M;
-    const bool live = i < a.d;
-    using V = Piece<float, M>;
-    auto at = [&](const float *from, int64_t k) {
-        V x;
-        load_piece(from + k * a.d + (live ? i : 0), x);
-        return x;
-    };
-    V sum = at(a.tail, c);
-    for (int64_t k = c + 1; k < a.stretches; k += 32) {
-        // the next stretches that begin with the row
-        const bool has = k + lane < a.stretches && sorted[min(k + lane, a.stretches - 1) * a.stretch].id == id;
-        const int n = __popc(__ballot_sync(kFull, has));
-        for (int q = 0; q < n; q += 16) {
-            V x[16];
+    for (int64_t w = (int64_t)blockIdx.x * kJoinWarps + threadIdx.x / 32; w < items; w += warps) {
+        const int64_t c = a.open[1 + w / groups];
+        const int id = sorted[(c + 1) * a.stretch].id, i = ((int)(w % groups) * 32 + lane) * M;
+        const bool live = i < a.d;
+        auto at = [&](const float *from, int64_t k) {
+            Piece<float, M> x;
+            load_piece(from + k * a.d + (live ? i : 0), x);
+            return x;
+        };
+        Piece<float, M> sum = at(a.tail, c);
+        constexpr int kAtOnce = 16;
+        for (int64_t k = c + 1; k < a.stretches; k += kAtOnce) {
+            // which of the next stretches begin with the row, and their sums at the same time
+            const int64_t mine = min(k + lane, a.stretches - 1);
+            Piece<float, M> x[kAtOnce];
+            const bool has = lane < kAtOnce && k + lane < a.stretches && sorted[mine * a.stretch].id == id;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x[j] = at(a.head, k + min(q + j, n - 1));
+            for (int j = 0; j < kAtOnce; ++j) x[j] = at(a.head, min(k + j, a.stretches - 1));
+            const int n = __popc(__ballot_sync(kFull, has));
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (q + j < n)
+            for (int j = 0; j < kAtOnce; ++j)
+                if (j < n)
 #pragma unroll
                     for (int m = 0; m < M; ++m) sum.v[m] += x[j].v[m];
+            if (n < kAtOnce) break;
         }
-        if (n < 32) break;
-    }
-    if (live)
+        if (live)
 #pragma unroll
-        for (int m = 0; m < M; ++m) st_elem(static_cast<E *>(a.dw), id * a.dws + i + m, sum.v[m] * a.scale);
+            for (int m = 0; m < M; ++m) st_elem(static_cast<E *>(a.dw), id * a.dws + i + m, sum.v[m] * a.scale);
+    }
 }
 
 // ---- host side ------------------------------------------------------------------
@@ -329,17 +343,19 @@ int passes_of(int V) {
 struct GradSpace {
     int stretch;
     int64_t stretches;
-    size_t sorted[2], head, tail, bytes;
+    size_t sorted[2], head, tail, open, bytes;
     explicit GradSpace(const dpb_embedding_config *c) {
-        // Short stretches where there are few tokens, so that all SMs have some.
-        stretch = c->tokens > 16384 ? 32 : 8;
+        // As many stretches as warps are resident, of 8 tokens at least and 64 at most.
+        const int64_t warps = (int64_t)kSumResident * sms_of_device();
+        stretch = (int)std::max<int64_t>(8, std::min<int64_t>(64, (c->tokens + warps - 1) / warps));
         stretches = (c->tokens + stretch - 1) / stretch;
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
         sorted[0] = kStatusBytes;
         sorted[1] = sorted[0] + up((size_t)c->tokens * sizeof(Sorted));
         head = sorted[1] + up((size_t)c->tokens * sizeof(Sorted));
         tail = head + up((size_t)stretches * c->dim * 4);
-        bytes = tail + up((size_t)stretches * c->dim * 4);
+        open = tail + up((size_t)stretches * c->dim * 4);
+        bytes = open + up(((size_t)stretches + 1) * 4);
     }
 };
 
@@ -377,20 +393,38 @@ dpb_status lookup(const LookupArgs &a, const void *ids, int index_bytes, cudaStr
 
 template <typename E, int N, int P>
 cudaError_t sums(const LookupArgs &a, cudaStream_t s) {
-    const dim3 grid((unsigned)((a.stretches + 7) / 8), (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
+    const dim3 grid((unsigned)((a.stretches + kSumWarps - 1) / kSumWarps), (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
     if (grid.y > 65535) return cudaErrorInvalidConfiguration;
-    return launch_early(embedding_sum_kernel<E, N, P>, grid, 256, 0, s, a);
+    return launch_early(embedding_sum_kernel<E, N, P>, grid, 32 * kSumWarps, 0, s, a);
+}
+
+template <typename E, int N, typename I>
+cudaError_t sort(const LookupArgs &a, const I *ids, cudaStream_t s) {
+    void (*const kernel)(const LookupArgs, const I *) = embedding_sort_kernel<E, N, I>;
+    // a cluster of 16 is more than a device need hold; this one does
+    static const cudaError_t large = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                          cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (large != cudaSuccess) return large;
+    const int others = std::max(1, std::min(sms_of_device() / kSortBlocks - 1, (a.V + 32 * kSortBlocks - 1) / (32 * kSortBlocks)));
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3(kSortBlocks * (1 + others));
+    how.blockDim = dim3(32 * kSortWarps);
+    how.stream = s;
+    cudaLaunchAttribute cluster{};
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = kSortBlocks;
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    how.attrs = &cluster;
+    how.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&how, kernel, a, ids);
+    return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
 template <typename E, int N>
 dpb_status gradient(const LookupArgs &a, const void *ids, int index_bytes, cudaStream_t s) {
-    const int others = std::max(1, std::min(sms_of_device() / kSortBlocks - 1, (a.V + 255) / 256));
-    const unsigned blocks = kSortBlocks * (1 + others);
-    if (index_bytes == 4)
-        embedding_sort_kernel<E, N><<<blocks, 32 * kSortWarps, 0, s>>>(a, static_cast<const int32_t *>(ids));
-    else
-        embedding_sort_kernel<E, N><<<blocks, 32 * kSortWarps, 0, s>>>(a, static_cast<const int64_t *>(ids));
-    DPB_CHECK(launch_status(cudaGetLastError(), "embedding_backward (order)"));
+    DPB_CHECK(launch_status(index_bytes == 4 ? sort<E, N>(a, static_cast<const int32_t *>(ids), s)
+                                             : sort<E, N>(a, static_cast<const int64_t *>(ids), s),
+                            "embedding_backward (order)"));
     const int pieces = (a.d + 32 * N - 1) / (32 * N);  // of a lane
     cudaError_t e;
     if (pieces == 1) e = sums<E, N, 1>(a, s);
@@ -399,8 +433,9 @@ dpb_status gradient(const LookupArgs &a, const void *ids, int index_bytes, cudaS
     DPB_CHECK(launch_status(e, "embedding_backward (sums)"));
     constexpr int M = N == 1 ? 1 : 4;
     const int groups = (a.d + 32 * M - 1) / (32 * M);
-    if (a.stretches * groups / 8 >= 0x7fffffffll) return fail(DPB_ERR_UNSUPPORTED, "too many tokens for rows this wide");
-    return launch_status(launch_early(embedding_join_kernel<E, M>, dim3((unsigned)((a.stretches * groups + 7) / 8)), 256, 0, s, a, groups),
+    const int64_t items = a.stretches * groups;
+    const unsigned blocks = (unsigned)std::min<int64_t>((items + kJoinWarps - 1) / kJoinWarps, 4 * sms_of_device());
+    return launch_status(launch_early(embedding_join_kernel<E, M>, dim3(blocks), 32 * kJoinWarps, 0, s, a, groups),
                          "embedding_backward (rows)");
 }
 
@@ -463,6 +498,7 @@ dpb_status dpb_embedding_backward(const dpb_embedding_config *cfg, const dpb_row
     for (int i = 0; i < 2; ++i) a.sorted[i] = reinterpret_cast<Sorted *>(ws + w.sorted[i]);
     a.head = reinterpret_cast<float *>(ws + w.head);
     a.tail = reinterpret_cast<float *>(ws + w.tail);
+    a.open = reinterpret_cast<int *>(ws + w.open);
     const bool pieces = by_pieces(a.dy, a.dys, a.T, elem) && by_pieces(a.dw, a.dws, a.V, elem) && a.d * elem % 16 == 0;
     using bf16 = __nv_bfloat16;
     if (cfg->dtype == DPB_F32)

@@ -983,7 +983,7 @@ dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, 
     if (grad_hidden) a.dh = static_cast<bf16 *>(grad_hidden->data), a.dh_stride = grad_hidden->stride;
     if (grad_weight) DPB_CHECK(make_map(&a.dw, grad_weight->data, grad_weight->stride, cfg->vocab, cfg->dim, 32));
     a.acc = reinterpret_cast<float *>(ws + w.acc);
-    for (int i = 0; i < kBuffers; ++i) {
+    for (int i = 0; i < std::min<int64_t>(kBuffers, w.pieces); ++i) {
         DPB_CHECK(make_map(&a.dz[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 64));
         DPB_CHECK(make_map(&a.dz_out[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 32));
     }

@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "dpb_checks.h"
 #include "dpb_device.cuh"
@@ -114,7 +115,8 @@ __device__ __forceinline__ Unit score_unit(int kind, int u, int tiles_m, int til
 // How many units each product has, and which is the u-th. The gradient's
 // pieces overlap: dz of a piece comes before the products that read the piece
 // before it, so that what a unit waits for was taken a piece's time ago:
-//   dz 0, dz 1, dW 0, dH 0, dz 2, dW 1, dH 1, ..., dW last, dH last
+//   dz 0, dz 1, dH 0, dW 0, dz 2, dH 1, dW 1, ..., dW last, dH last
+// (in the last one the longer units come first, so that the pairs end together).
 struct List {
     int tiles_m, tiles_d, words;  // words of the vocabulary that a piece (the forward: all) has
     int count, last;              // tokens; words of the last piece
@@ -130,11 +132,12 @@ struct List {
     }
     __device__ __forceinline__ int hidden_units(const Args &a) const { return a.want_h ? tiles_m * tiles_d : 0; }
     __device__ __forceinline__ Unit reader(const Args &a, int u, int piece) const {
-        const int w = words_of(a, piece), n_w = weight_units(a, w);
-        if (u < n_w) return Unit{kDWeight, u / tiles_d * kTile, u % tiles_d * kTile, (count + 63) / 64, piece};
-        u -= n_w;
-        if (u < hidden_units(a)) return Unit{kDHidden, u / tiles_d * kTile, u % tiles_d * kTile, (w + 63) / 64, piece};
-        return Unit{kEnd, 0, 0, 0, 0};
+        const int w = words_of(a, piece), n_w = weight_units(a, w), n_h = hidden_units(a);
+        const bool h_first = piece < a.pieces - 1 || w > count;
+        if (u >= n_w + n_h) return Unit{kEnd, 0, 0, 0, 0};
+        const bool is_h = h_first ? u < n_h : u >= n_w;
+        u -= is_h && !h_first ? n_w : !is_h && h_first ? n_h : 0;
+        return Unit{is_h ? kDHidden : kDWeight, u / tiles_d * kTile, u % tiles_d * kTile, ((is_h ? w : count) + 63) / 64, piece};
     }
     __device__ __forceinline__ Unit at(const Args &a, int u) const {
         const int all = a.pieces, first = grad_units(words_of(a, 0));
@@ -199,25 +202,43 @@ struct Shared {
     // quarter), units handed over and taken
     static constexpr int kFullBar = kBars, kEmptyBar = kFullBar + 8 * kStages, kReady = kEmptyBar + 8 * kStages,
                          kRead = kReady + 16, kUpper = kRead + 16, kHanded = kUpper + 64, kTaken = kHanded + 8 * kAhead,
-                         kUnits = kTaken + 8 * kAhead, kTmem = kUnits + 4 * kAhead, kBytes = kTmem + 4;
+                         kUnits = (kTaken + 8 * kAhead + 15) / 16 * 16, kTmem = kUnits + 16 * kAhead, kBytes = kTmem + 4;
     static constexpr int kMerge = kData;  // the upper halves: the forward has no rows on their way to memory
 };
 static_assert(kRowWarps == 8 && 2 * 128 * 8 <= kRowWarps * kStore, "two halves of a row");
 constexpr int kSmem = Shared::kBytes + 1024;  // the data starts at a multiple of 1024
 
 // Units in the order in which they are taken, seen by one role of one block.
+// What a unit is, is worked out by the warp that takes them. Handing it over and
+// giving its slot back order no plain writes: as releases at cluster scope the
+// arrivals had every role wait for its writes (8 x 1024, forward: 410 us
+// against 322).
 struct Units {
     uint32_t base, taken;  // this block's barriers and slots; the first block's `taken`
     int i = 0;
-    // All lanes (or one thread): the next unit's number; false after a wait that gave up.
-    __device__ __forceinline__ bool next(int &u) {
+    __device__ __forceinline__ bool ready() const { return bar_test(base + Shared::kHanded + 8 * (i % kAhead), (i / kAhead) & 1); }
+    // All lanes (or one thread): the next unit; false after a wait that gave up.
+    __device__ __forceinline__ bool next(Unit &t) {
         const int s = i % kAhead;
-        if (!bar_wait_peer(base + Shared::kHanded + 8 * s, (i / kAhead) & 1, kTries)) return false;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u) : "r"(base + Shared::kUnits + 4 * s) : "memory");
+        if (!bar_wait(base + Shared::kHanded + 8 * s, (i / kAhead) & 1, kTries)) return false;
+        int x;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(x), "=r"(t.m0), "=r"(t.n0), "=r"(t.blocks)
+                     : "r"(base + Shared::kUnits + 16 * s)
+                     : "memory");
+        t.kind = x & 7, t.piece = x >> 3;
         ++i;
+        // what the unit reads of other units, the first block has seen (List::wait)
+        if (t.kind == kDHidden || t.kind == kDWeight) fence_cluster();
         return true;
     }
-    // One thread: the number has been read.
+    // One thread of the first block: unit t into slot s of the block of `rank`.
+    __device__ __forceinline__ void hand(const Unit &t, int s, uint32_t rank) const {
+        const uint32_t bar = peer_addr(base + Shared::kHanded + 8 * s, rank);
+        bar_arrive_expect_peer(bar, 16);
+        store_peer(peer_addr(base + Shared::kUnits + 16 * s, rank), t.kind | t.piece << 3, t.m0, t.n0, t.blocks, bar);
+    }
+    // One thread: the unit has been read.
     __device__ __forceinline__ void done() const { bar_arrive_peer(taken + 8 * ((i - 1) % kAhead)); }
 };
 
@@ -329,6 +350,44 @@ __device__ __forceinline__ void sums_before(const Args &a, float4 (&x)[8], int r
             x[i] = __ldcg(reinterpret_cast<const float4 *>(a.acc + (int64_t)(row + 4 * i) * a.d + column));
 }
 
+// The next slot of the ring, and how often the ring has been gone round.
+struct Turn {
+    int slot = 0;
+    uint32_t round = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == kStages) slot = 0, round ^= 1;
+    }
+};
+
+// One thread: d = the ring's next `blocks` slots multiplied and added up. A_ROWS,
+// B_ROWS: that operand's rows run along K. The next slot is waited for while
+// half of a slot's products are still to be issued, so that the tensor cores
+// have work meanwhile.
+template <bool A_ROWS, bool B_ROWS>
+__device__ __forceinline__ bool multiply(uint32_t d, int blocks, uint32_t base, Turn &at) {
+    auto wait = [&] { return bar_wait(base + Shared::kFullBar + 8 * at.slot, at.round, kTries); };
+    if (!wait()) return false;
+    for (int k = 0; k < blocks; ++k) {
+        fence_after();
+        const uint32_t from = base + at.slot * kStageBytes, done = base + Shared::kEmptyBar + 8 * at.slot;
+        const uint64_t da = A_ROWS ? desc_k_rows(from, 8192) : desc_k_inside(from);
+        const uint64_t db = B_ROWS ? desc_k_rows(from + 16384, 8192) : desc_k_inside(from + 16384);
+        auto product = [&](int i) {
+            mma_ss_pair(d, desc_at(da, A_ROWS ? 2048 * i : 32 * i), desc_at(db, B_ROWS ? 2048 * i : 32 * i),
+                        mma_shape_pair(kTile, A_ROWS, B_ROWS), k > 0 || i > 0);
+        };
+        product(0);
+        product(1);
+        product(2);
+        at.next();
+        const bool ok = k + 1 == blocks || wait();
+        product(3);
+        mma_commit_pair(done);
+        if (!ok) return false;
+    }
+    return true;
+}
+
 // ---- the kernel -------------------------------------------------------------------------
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Args a) {
@@ -374,11 +433,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         // ---- copies
         if (elect_one()) {
             const CUtensorMap *rows = a.head->all ? &a.hidden : &a.closed;
-            int at = 0, u;  // slots filled
+            int at = 0;  // slots filled
+            Unit t;
             while (true) {
-                if ((failed = !units.next(u))) break;
+                if ((failed = !units.next(t))) break;
                 units.done();
-                const Unit t = list.at(a, u);
                 if (t.kind == kEnd) break;
                 // dz was stored by copies of other blocks: these loads come after what their count released
                 if (t.kind > kGrad) fence_async();
@@ -386,7 +445,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 const CUtensorMap *dz = &a.dz[t.piece % kBuffers];
                 for (int k = 0; k < t.blocks; ++k, ++at) {
                     const int s = at % kStages;
-                    if (at >= kStages && !bar_wait_peer(empty(s), ((at / kStages) & 1) ^ 1, kTries)) {
+                    if (at >= kStages && !bar_wait(empty(s), ((at / kStages) & 1) ^ 1, kTries)) {
                         failed = true;
                         break;
                     }
@@ -413,57 +472,48 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             // no copy is in flight when the pair ends, whatever gave up, and no
             // product's arrival at the second block
             for (int i = max(0, at - kStages); i < at; ++i)
-                bar_wait_peer(rank == 0 ? full(i % kStages) : empty(i % kStages), (i / kStages) & 1, kTries);
+                bar_wait(rank == 0 ? full(i % kStages) : empty(i % kStages), (i / kStages) & 1, kTries);
         }
     } else if (warp == 1) {
         // ---- products
         if (rank == 0 && elect_one()) {
-            int at = 0, sums = 0, u;
+            int sums = 0, slots = 0;
+            Turn at;
+            Unit t;
             while (true) {
-                if ((failed = !units.next(u))) break;
+                if ((failed = !units.next(t))) break;
                 units.done();
-                const Unit t = list.at(a, u);
                 if (t.kind == kEnd) break;
                 if (t.blocks == 0) continue;
                 const int b = sums & 1;
-                if (sums >= 2 && !bar_wait_peer(base + Shared::kRead + 8 * b, ((sums / 2) & 1) ^ 1, kTries)) {
+                if (sums >= 2 && !bar_wait(base + Shared::kRead + 8 * b, ((sums / 2) & 1) ^ 1, kTries)) {
                     failed = true;
                     break;
                 }
                 fence_after();
-                const bool a_rows = t.kind == kDWeight, b_rows = t.kind >= kDHidden;
-                const uint32_t shape = mma_shape_pair(kTile, a_rows, b_rows), d = tmem + kTile * b;
-                for (int k = 0; k < t.blocks; ++k, ++at) {
-                    const int s = at % kStages;
-                    if (!bar_wait_peer(full(s), (at / kStages) & 1, kTries)) {
-                        failed = true;
-                        break;
-                    }
-                    fence_after();
-                    const uint32_t from = base + s * kStageBytes;
-                    const uint64_t da = a_rows ? desc_k_rows(from, 8192) : desc_k_inside(from);
-                    const uint64_t db = b_rows ? desc_k_rows(from + 16384, 8192) : desc_k_inside(from + 16384);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        mma_ss_pair(d, desc_at(da, a_rows ? 2048 * i : 32 * i), desc_at(db, b_rows ? 2048 * i : 32 * i),
-                                    shape, k > 0 || i > 0);
-                    mma_commit_pair(empty(s));
-                }
+                const uint32_t d = tmem + kTile * b;
+                failed = !(t.kind == kDWeight   ? multiply<true, true>(d, t.blocks, base, at)
+                           : t.kind == kDHidden ? multiply<false, true>(d, t.blocks, base, at)
+                                                : multiply<false, false>(d, t.blocks, base, at));
                 if (failed) break;
                 mma_commit_pair(base + Shared::kReady + 8 * b);
                 ++sums;
+                slots = min(slots + t.blocks, kStages);
             }
             // every arrival of a product on a barrier of the pair has come before it ends
-            for (int i = max(0, at - kStages); i < at; ++i) failed |= !bar_wait_peer(empty(i % kStages), (i / kStages) & 1, kTries);
+            for (int i = 0; i < slots; ++i) {
+                at.slot = at.slot == 0 ? (at.round ^= 1, kStages - 1) : at.slot - 1;
+                failed |= !bar_wait(empty(at.slot), at.round, kTries);
+            }
             for (int i = max(0, sums - 2); i < sums; ++i)
-                failed |= !bar_wait_peer(base + Shared::kReady + 8 * (i & 1), (i / 2) & 1, kTries);
+                failed |= !bar_wait(base + Shared::kReady + 8 * (i & 1), (i / 2) & 1, kTries);
         }
     } else if (warp == 2) {
         // ---- units
         if (rank == 0 && elect_one()) {
             for (int i = 0;; ++i) {
                 const int s = i % kAhead;
-                if (i >= kAhead && !bar_wait_peer(base + Shared::kTaken + 8 * s, ((i / kAhead) & 1) ^ 1, kTries)) {
+                if (i >= kAhead && !bar_wait(base + Shared::kTaken + 8 * s, ((i / kAhead) & 1) ^ 1, kTries)) {
                     failed = true;
                     break;
                 }
@@ -473,11 +523,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     failed = true;
                     break;
                 }
-                const uint32_t slot = base + Shared::kUnits + 4 * s, bar = base + Shared::kHanded + 8 * s;
-                for (int r = 0; r < 2; ++r) {
-                    store_peer(peer_addr(slot, r), u);
-                    bar_arrive_peer(peer_addr(bar, r));
-                }
+                if (t.kind != kScores) fence_cluster();
+                units.hand(t, s, 0);
+                units.hand(t, s, 1);
                 if (t.kind == kEnd) break;
             }
         }
@@ -487,15 +535,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         const uint32_t stage = base + Shared::kData + (warp - 4) * kStore;
         const uint32_t read_bar = peer_addr(base + Shared::kRead, 0);
         const float g = a.head->g_max;
-        int sums = 0, u;
+        int sums = 0;
+        Unit t;
+        // Counts a unit's dz once its copies are in memory, which they are when half
+        // of the next unit's are under way (LATER = 1), or before a wait: others may
+        // wait for the count.
+        int *pending = nullptr;
+        auto settle = [&](auto later) {
+            if (pending && lane == 0) {
+                stores_done<decltype(later)::value>();
+                fence_async();
+                count_done(pending);
+            }
+            pending = nullptr;
+            __syncwarp();
+        };
+        const std::integral_constant<int, 0> now{};
+        const std::integral_constant<int, 1> later{};
         while (true) {
-            if (!__all_sync(kFull, units.next(u))) {
+            if (!__all_sync(kFull, units.ready())) settle(now);
+            if (!__all_sync(kFull, units.next(t))) {
                 failed = true;
                 break;
             }
             __syncwarp();
             if (elect_one()) units.done();
-            const Unit t = list.at(a, u);
             if (t.kind == kEnd) break;
             const int row0 = t.m0 + 128 * rank + 32 * quarter, row = row0 + lane, column = t.n0 + 128 * half;
             const int b = sums & 1;
@@ -505,13 +569,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             float4 before[8];
             if (t.kind == kDHidden && t.piece > 0) sums_before(a, before, row0 + lane / 8, count, column + 4 * (lane % 8));
             if (t.blocks > 0) {
-                if (!__all_sync(kFull, bar_wait_peer(base + Shared::kReady + 8 * b, (sums / 2) & 1, kTries))) {
+                if (!__all_sync(kFull, bar_test(base + Shared::kReady + 8 * b, (sums / 2) & 1))) settle(now);
+                if (!__all_sync(kFull, bar_wait(base + Shared::kReady + 8 * b, (sums / 2) & 1, kTries))) {
                     failed = true;
                     break;
                 }
                 fence_after();
                 ++sums;
             }
+            if (t.kind != kGrad) settle(now);
             if (t.kind == kScores) {
                 float z = 0.f;
                 const int target = token.target - column;
@@ -543,6 +609,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     fence_async_shared();
                     __syncwarp();
                     if (lane == 0) store_box(&a.dz_out[t.piece % kBuffers], stage, column + c, row0);
+                    if (c == 0) settle(later);
                 }
             } else if (t.kind == kDWeight) {
 #pragma unroll 1
@@ -610,21 +677,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 __syncwarp();
                 if (elect_one()) bar_arrive_peer(read_bar + 8 * b);
             }
-            if (t.kind != kScores) {
-                // what others wait for is in memory: dz, stored by copies; sums of dH; of dW, that dz has been read
+            // what others wait for: dz in memory; sums of dH in memory; of dW, that dz has been read
+            if (t.kind == kGrad) {
+                pending = &a.head->done[t.piece][kGrad];
+            } else if (t.kind != kScores) {
                 if (t.kind == kDHidden) __threadfence();
                 __syncwarp();
-                if (lane == 0) {
-                    if (t.kind == kGrad) {
-                        stores_done();
-                        fence_async();
-                    }
-                    count_done(&a.head->done[t.piece][t.kind]);
-                }
+                if (lane == 0) count_done(&a.head->done[t.piece][t.kind]);
                 __syncwarp();
             }
         }
-        if (lane == 0) stores_done();
+        settle(now);
+        if (lane == 0) stores_done<0>();
     }
     if (failed) set_status(a.status, DPB_DEV_TIMEOUT);
     __syncwarp();

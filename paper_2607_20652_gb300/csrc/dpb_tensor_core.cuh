@@ -47,6 +47,17 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t
     return false;
 }
 
+// Whether the phase of `parity` has ended, without waiting.
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+
 // ---- copies ---------------------------------------------------------------------
 
 // One box of a [tokens][heads][dim] tensor (dim x, head y, token z) into
@@ -189,27 +200,22 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Arrives on a barrier of either block (an address from peer_addr).
+// Arrives on a barrier of either block (an address from peer_addr). It orders
+// what the block of the barrier sees of this thread's tensor memory and waits,
+// not of its plain writes: those take fence_cluster on both sides.
 __device__ __forceinline__ void bar_arrive_peer(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// bar_wait where arrivals may come from the other block.
-__device__ __forceinline__ bool bar_wait_peer(uint32_t bar, uint32_t parity, uint32_t tries) {
-    for (uint32_t i = 0; i < tries; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-            " selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (done) return true;
-    }
-    return false;
+__device__ __forceinline__ void bar_arrive_expect_peer(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void store_peer(uint32_t addr, int v) {
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+// 16 bytes into either block's shared memory; they count on `bar` of that block.
+__device__ __forceinline__ void store_peer(uint32_t addr, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.s32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(addr),
+                 "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+                 : "memory");
 }
+__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 // One box of a [rows][columns] tensor into this block's shared memory; its
 // bytes count on `bar`, which may be the other block's.
 __device__ __forceinline__ void copy_box_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
@@ -256,9 +262,12 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t src, 
                  : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-// This thread's stores have read their shared memory; are in memory.
+// This thread's stores have read their shared memory; all but the last N are in memory.
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void stores_done() {
+    asm volatile("cp.async.bulk.wait_group %0;" ::"n"(N) : "memory");
+}
 
 // ---- blocks that have not started -----------------------------------------------
 

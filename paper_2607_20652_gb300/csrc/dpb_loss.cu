@@ -87,7 +87,8 @@ struct Args {
     float *z_target;
     float *loss, *lse;
     int *counted;
-    float *acc;  // [rows][dim], where there are several pieces
+    CUtensorMap sums;
+    float *acc;  // [rows][dim]: sums of dH, where there are several pieces
     bf16 *dh;
     int64_t dh_stride;
     int64_t T, T_pad;
@@ -228,8 +229,6 @@ struct Units {
                      : "memory");
         t.kind = x & 7, t.piece = x >> 3;
         ++i;
-        // what the unit reads of other units, the first block has seen (List::wait)
-        if (t.kind == kDHidden || t.kind == kDWeight) fence_cluster();
         return true;
     }
     // One thread of the first block: unit t into slot s of the block of `rank`.
@@ -439,8 +438,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 if ((failed = !units.next(t))) break;
                 units.done();
                 if (t.kind == kEnd) break;
-                // dz was stored by copies of other blocks: these loads come after what their count released
-                if (t.kind > kGrad) fence_async();
+                // other blocks' dz, which the first block has seen (List::wait), by way of copies
+                if (t.kind > kGrad) {
+                    fence_cluster();
+                    fence_async();
+                }
                 const int v0 = t.piece * a.piece;
                 const CUtensorMap *dz = &a.dz[t.piece % kBuffers];
                 for (int k = 0; k < t.blocks; ++k, ++at) {
@@ -537,9 +539,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         const float g = a.head->g_max;
         int sums = 0;
         Unit t;
-        // Counts a unit's dz once its copies are in memory, which they are when half
-        // of the next unit's are under way (LATER = 1), or before a wait: others may
-        // wait for the count.
+        // Counts a unit once its copies are in memory, which they are when half of the
+        // next unit's are under way (`later`), or before a wait: others may wait for
+        // the count.
         int *pending = nullptr;
         auto settle = [&](auto later) {
             if (pending && lane == 0) {
@@ -567,7 +569,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             Token token{-1, 0.f, 0.f, -1};
             if (t.kind != kDWeight && row < count) token = a.tokens[row];
             float4 before[8];
-            if (t.kind == kDHidden && t.piece > 0) sums_before(a, before, row0 + lane / 8, count, column + 4 * (lane % 8));
+            if (t.kind == kDHidden && t.piece > 0 && t.piece == a.pieces - 1) {
+                fence_cluster();  // other blocks' sums, which the first block has seen
+                fence_async();
+                sums_before(a, before, row0 + lane / 8, count, column + 4 * (lane % 8));
+            }
             if (t.blocks > 0) {
                 if (!__all_sync(kFull, bar_test(base + Shared::kReady + 8 * b, (sums / 2) & 1))) settle(now);
                 if (!__all_sync(kFull, bar_wait(base + Shared::kReady + 8 * b, (sums / 2) & 1, kTries))) {
@@ -641,13 +647,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     if (lane == 0 && column + c < a.d && v0 < a.V) store_box(&a.dw, stage, column + c, v0);
                 }
             } else {
-                // by way of shared memory, so that eight lanes have 128 bytes of a row of the sums
+                // by way of shared memory: copies add the sums of a piece to those of the
+                // pieces before; in the last one eight lanes have 128 bytes of a row
                 const bool first = t.piece == 0, last = t.piece == a.pieces - 1;
                 const int r = lane / 8, piece = lane % 8;
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 32) {
-                    const int col = column + c + 4 * piece;
-                    if (!first && c > 0) sums_before(a, before, row0 + r, count, col);
                     uint32_t v[32];
                     __syncwarp();
                     tmem_load(from + c, v);
@@ -657,18 +662,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         store_shared(swizzled(stage, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    if (!last) {
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0 && first) store_box(&a.sums, stage, column + c, row0);
+                        if (lane == 0 && !first) add_box(&a.sums, stage, column + c, row0);
+                        continue;
+                    }
+                    const int col = column + c + 4 * piece;
+                    float4 sums[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sums[i] = before[i];
+                    if (!first && c < 96) sums_before(a, before, row0 + r, count, col + 32);
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int at = r + 4 * i;
                         float4 x = load_shared(swizzled(stage, at, piece));
                         if (row0 + at >= count || col >= a.d) continue;
-                        if (!first) x.x += before[i].x, x.y += before[i].y, x.z += before[i].z, x.w += before[i].w;
-                        if (last)
-                            *reinterpret_cast<uint2 *>(a.dh + a.tokens[row0 + at].row * a.dh_stride + col) =
-                                make_uint2(pack_bf16(x.x * g, x.y * g), pack_bf16(x.z * g, x.w * g));
-                        else
-                            *reinterpret_cast<float4 *>(a.acc + (int64_t)(row0 + at) * a.d + col) = x;
+                        if (!first) x.x += sums[i].x, x.y += sums[i].y, x.z += sums[i].z, x.w += sums[i].w;
+                        *reinterpret_cast<uint2 *>(a.dh + a.tokens[row0 + at].row * a.dh_stride + col) =
+                            make_uint2(pack_bf16(x.x * g, x.y * g), pack_bf16(x.z * g, x.w * g));
                     }
                 }
             }
@@ -677,13 +691,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 __syncwarp();
                 if (elect_one()) bar_arrive_peer(read_bar + 8 * b);
             }
-            // what others wait for: dz in memory; sums of dH in memory; of dW, that dz has been read
-            if (t.kind == kGrad) {
-                pending = &a.head->done[t.piece][kGrad];
-            } else if (t.kind != kScores) {
-                if (t.kind == kDHidden) __threadfence();
+            // what others wait for: dz and the sums of dH in memory; of dW, that dz has been read
+            if (t.kind == kGrad || t.kind == kDHidden) {
+                pending = &a.head->done[t.piece][t.kind];
+            } else if (t.kind == kDWeight) {
                 __syncwarp();
-                if (lane == 0) count_done(&a.head->done[t.piece][t.kind]);
+                if (lane == 0) count_done(&a.head->done[t.piece][kDWeight]);
                 __syncwarp();
             }
         }
@@ -855,16 +868,18 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
     return fn;
 }
 
-// Map of rows in boxes of 64 columns x `box_rows`; what lies outside reads as zero.
-dpb_status make_map(CUtensorMap *map, const void *data, int64_t stride, int64_t rows, int64_t columns, int box_rows) {
+// Map of rows in boxes of 128 bytes x `box_rows` rows; what lies outside reads as zero.
+dpb_status make_map(CUtensorMap *map, const void *data, int64_t stride, int64_t rows, int64_t columns, int box_rows,
+                    bool wide = false) {
     const auto fn = encoder();
     if (!fn) return fail(DPB_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+    const int elem = wide ? 4 : 2;
     const cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? stride : (columns + 7) / 8 * 8) * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
-    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(data), dims, strides, box, one,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? stride : (columns + 7) / 8 * 8) * elem};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / elem), (cuuint32_t)box_rows}, one[2] = {1, 1};
+    const CUresult r = fn(map, wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+                          const_cast<void *>(data), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(DPB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
     return DPB_OK;
 }
@@ -1047,6 +1062,7 @@ dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, 
     if (grad_hidden) a.dh = static_cast<bf16 *>(grad_hidden->data), a.dh_stride = grad_hidden->stride;
     if (grad_weight) DPB_CHECK(make_map(&a.dw, grad_weight->data, grad_weight->stride, cfg->vocab, cfg->dim, 32));
     a.acc = reinterpret_cast<float *>(ws + w.acc);
+    if (w.pieces > 1) DPB_CHECK(make_map(&a.sums, a.acc, cfg->dim, cfg->tokens, cfg->dim, 32, true));
     for (int i = 0; i < std::min<int64_t>(kBuffers, w.pieces); ++i) {
         DPB_CHECK(make_map(&a.dz[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 64));
         DPB_CHECK(make_map(&a.dz_out[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 32));

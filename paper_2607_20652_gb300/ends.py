@@ -22,7 +22,10 @@ from . import dpb
 
 def _rows(t: torch.Tensor, dtype) -> torch.Tensor:
     """[..., d] as the [tokens, d] rows that the kernels read, of `dtype`."""
-    t = t.to(dtype).reshape(-1, t.shape[-1])
+    if t.dtype is not dtype:
+        t = t.to(dtype)
+    if t.dim() != 2:
+        t = t.reshape(-1, t.shape[-1])
     return t if t.stride(-1) == 1 and (t.shape[0] < 2 or t.stride(0) >= t.shape[1]) else t.contiguous()
 
 
@@ -36,18 +39,20 @@ class _EmbeddingFunction(torch.autograd.Function):
     def forward(ctx, weight, ids, scale):
         ctx.save_for_backward(ids)
         ctx.at = (weight.shape[0], scale)
-        return dpb.embedding(weight, ids, scale)
+        return dpb.embedding(_rows(weight, weight.dtype), ids.reshape(-1), scale).view(*ids.shape, weight.shape[1])
 
     @staticmethod
     @once_differentiable
     def backward(ctx, gy):
         ids, = ctx.saved_tensors
-        return dpb.embedding_backward(_rows(gy, gy.dtype), ids, *ctx.at), None, None
+        return dpb.embedding_backward(_rows(gy, gy.dtype), ids.reshape(-1), *ctx.at), None, None
 
 
 def embedding(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
     """dpb.embedding with its gradient (dense, by sorted tokens): ids of any shape -> [..., d]."""
-    return _EmbeddingFunction.apply(_rows(weight, weight.dtype), ids.reshape(-1), scale).view(*ids.shape, weight.shape[1])
+    if weight.dim() != 2:
+        raise ValueError(f"weight must be [vocab, d], got {list(weight.shape)}")
+    return _EmbeddingFunction.apply(weight, ids, scale)
 
 
 class Embedding(nn.Module):
@@ -66,23 +71,28 @@ class Embedding(nn.Module):
 class _AddNormFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, delta, weight, eps):
-        w = None if weight is None else weight.to(x.dtype)
-        y, total = dpb.add_norm(x, delta, w, eps)
+        w = weight if weight is None or weight.dtype is x.dtype else weight.to(x.dtype)
+        y, total = dpb.add_norm(_rows(x, x.dtype), None if delta is None else _rows(delta, x.dtype), w, eps)
         ctx.save_for_backward(total, w)
-        ctx.eps, ctx.wide = eps, None if weight is None else weight.dtype
+        ctx.at = (x.shape, eps, None if weight is None else weight.dtype, None if delta is None else delta.dtype)
         ctx.set_materialize_grads(False)
-        return y if delta is None else (y, total)
+        return y.view(x.shape) if delta is None else (y.view(x.shape), total.view(x.shape))
 
     @staticmethod
     @once_differentiable
     def backward(ctx, gy, gt=None):
         total, w = ctx.saved_tensors
+        shape, eps, weight_type, delta_type = ctx.at
+        gw = None
         if gy is None:
-            return gt, gt, None, None
-        dt = total.dtype
-        gx, gw = dpb.add_norm_backward(total, _rows(gy, dt), None if gt is None else _rows(gt, dt), w, ctx.eps,
-                                       weight_grad=ctx.needs_input_grad[2])
-        return gx, gx if ctx.needs_input_grad[1] else None, None if gw is None else gw.to(ctx.wide), None
+            gx = gt
+        else:
+            dt = total.dtype
+            gx, gw = dpb.add_norm_backward(total, _rows(gy, dt), None if gt is None else _rows(gt, dt), w, eps,
+                                           weight_grad=ctx.needs_input_grad[2])
+            gx = gx.view(shape)
+        gd = gx if ctx.needs_input_grad[1] and gx is not None else None
+        return gx, gd if gd is None or gd.dtype is delta_type else gd.to(delta_type), None if gw is None else gw.to(weight_type), None
 
 
 def add_norm(x: torch.Tensor, delta: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
@@ -90,13 +100,11 @@ def add_norm(x: torch.Tensor, delta: Optional[torch.Tensor] = None, weight: Opti
     """dpb.add_norm with its gradient: (y, total) of the shape of x, total = x +
     delta (x itself without delta), y its RMS norm times weight. delta and the
     weight are taken in x's type."""
-    rows = _rows(x, x.dtype)
     if delta is None:
-        return _AddNormFunction.apply(rows, None, weight, eps).view(x.shape), x
+        return _AddNormFunction.apply(x, None, weight, eps), x
     if delta.shape != x.shape:
         raise ValueError(f"delta must have x's shape {list(x.shape)}, got {list(delta.shape)}")
-    y, total = _AddNormFunction.apply(rows, _rows(delta, x.dtype), weight, eps)
-    return y.view(x.shape), total.view(x.shape)
+    return _AddNormFunction.apply(x, delta, weight, eps)
 
 
 class AddRMSNorm(nn.Module):
@@ -114,23 +122,26 @@ class AddRMSNorm(nn.Module):
 class _LossFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, targets, ignore_index, mean):
-        w = _tiles(_rows(weight, hidden.dtype))
-        loss, lse, counted = dpb.linear_cross_entropy_forward(hidden, w, targets, ignore_index, want_counted=True)
-        ctx.save_for_backward(hidden, w, targets, lse, counted)
-        ctx.ignore_index, ctx.mean, ctx.wide = ignore_index, mean, weight.dtype
-        return loss.sum() / counted[0] if mean else loss
+        h, w = _tiles(_rows(hidden, hidden.dtype)), _tiles(_rows(weight, hidden.dtype))
+        loss, lse, counted = dpb.linear_cross_entropy_forward(h, w, targets.reshape(-1), ignore_index, want_counted=True)
+        ctx.save_for_backward(h, w, targets, lse, counted)
+        ctx.at = (hidden.shape, weight.dtype, ignore_index, mean)
+        return loss.sum() / counted[0] if mean else loss.view(targets.shape)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g):
-        hidden, w, targets, lse, counted = ctx.saved_tensors
-        if ctx.mean:
-            g = (g / counted).expand(targets.shape)
-        elif g.stride(0) not in (0, 1):
-            g = g.contiguous()
-        dh, dw = dpb.linear_cross_entropy_backward(hidden, w, targets, lse, g, ctx.ignore_index,
+        h, w, targets, lse, counted = ctx.saved_tensors
+        shape, weight_type, ignore_index, mean = ctx.at
+        if mean:
+            g = (g / counted).expand(h.shape[0])
+        else:
+            g = g.reshape(-1)
+            if g.stride(0) not in (0, 1):
+                g = g.contiguous()
+        dh, dw = dpb.linear_cross_entropy_backward(h, w, targets.reshape(-1), lse, g, ignore_index,
                                                    want_hidden=ctx.needs_input_grad[0], want_weight=ctx.needs_input_grad[1])
-        return dh, None if dw is None else dw.to(ctx.wide), None, None, None
+        return (None if dh is None else dh.view(shape), None if dw is None else dw.to(weight_type)) + (None,) * 3
 
 
 def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100,
@@ -144,6 +155,5 @@ def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: to
         raise ValueError(f"reduction must be 'mean', 'sum' or 'none', got {reduction!r}")
     if hidden.shape[:-1] != targets.shape:
         raise ValueError(f"targets must have the shape {list(hidden.shape[:-1])}, got {list(targets.shape)}")
-    loss = _LossFunction.apply(_tiles(_rows(hidden, hidden.dtype)), weight, targets.reshape(-1), ignore_index,
-                               reduction == "mean")
-    return loss if reduction == "mean" else loss.sum() if reduction == "sum" else loss.view(targets.shape)
+    loss = _LossFunction.apply(hidden, weight, targets, ignore_index, reduction == "mean")
+    return loss.sum() if reduction == "sum" else loss

@@ -547,7 +547,7 @@ typedef struct dpb_rows {
 
 /*
  * dpb_embedding -- y_t = scale weight[id_t], rounded to the rows' type.
- *   tokens, vocab, dim   each below 2^31 - 256, dim at most 2^24
+ *   tokens, vocab, dim   at most 2^31 - 256 tokens and words, 2^20 columns
  *   index_bytes 4 or 8: ids are int32 or int64 [tokens]
  *   dtype       dpb_dtype of the rows
  *   scale       finite
@@ -618,7 +618,8 @@ dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
  * dpb_linear_cross_entropy_forward -- cross entropy of the rows' scores over the
  * vocabulary, without a tensor of tokens x vocabulary:
  *   z_t = hidden_t weight^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_t,target
- *   tokens, vocab, dim   dim a multiple of 8; each below 2^31 - 256
+ *   tokens, vocab, dim   at most 2^24 tokens and 2^28 words; dim a multiple of 8;
+ *               2^26 tiles of 256 x 256 in all products together
  *   ignore_index  a token with this target has loss 0, lse 0 and no gradient, and its
  *               hidden row is not read (it may hold anything)
  *   index_bytes 4 or 8: targets are int32 or int64 [tokens]
@@ -626,8 +627,12 @@ dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
  * hidden [tokens][dim] and weight [vocab][dim] are bf16, 16-byte aligned, with
  * strides that are multiples of 8 elements. loss, lse: fp32 [tokens]. counted
  * (int32, nullable): the number of tokens that take part. A target outside
- * [0, vocab) that is not ignore_index sets DPB_DEV_BAD_INDEX and counts as ignored. Scores and sums are fp32, exponentials to 2 ulp; a small loss keeps
- * its digits (it is not formed from the rounded lse).
+ * [0, vocab) that is not ignore_index sets DPB_DEV_BAD_INDEX and counts as ignored.
+ * Scores and sums are fp32, exponentials to 2 ulp; a small loss keeps its digits
+ * (it is not formed from the rounded lse). The tensor cores cut off what they add,
+ * so a score of a few units is off by 2e-9 dim (loss and lse by 4e-7 of themselves
+ * at dim = 768, 1e-6 at 2048). The outputs may not overlap the inputs, here and in
+ * the gradient.
  */
 typedef struct dpb_linear_loss_config {
     int64_t tokens;

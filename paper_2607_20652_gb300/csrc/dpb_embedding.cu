@@ -363,8 +363,8 @@ dpb_status check_config(const dpb_embedding_config *c) {
     if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
     if (c->dtype != DPB_F32 && c->dtype != DPB_BF16) return fail(DPB_ERR_INVALID_ARG, "dtype must be DPB_F32 or DPB_BF16");
     if (c->tokens < 0 || c->vocab < 1 || c->dim < 1) return fail(DPB_ERR_INVALID_ARG, "a size is too small");
-    if (c->tokens > 0x7fffff00ll || c->vocab > 0x7fffff00 || c->dim > (1 << 24))
-        return fail(DPB_ERR_UNSUPPORTED, "at most 2^31 - 256 tokens and words, 2^24 columns");
+    if (c->tokens > 0x7fffff00ll || c->vocab > 0x7fffff00 || c->dim > (1 << 20))
+        return fail(DPB_ERR_UNSUPPORTED, "at most 2^31 - 256 tokens and words, 2^20 columns");
     if (c->index_bytes != 4 && c->index_bytes != 8) return fail(DPB_ERR_INVALID_ARG, "index_bytes must be 4 or 8");
     if (!(c->scale - c->scale == 0.f)) return fail(DPB_ERR_INVALID_ARG, "scale must be finite");
     return check_slot(c->status_slot);
@@ -394,7 +394,6 @@ dpb_status lookup(const LookupArgs &a, const void *ids, int index_bytes, cudaStr
 template <typename E, int N, int P>
 cudaError_t sums(const LookupArgs &a, cudaStream_t s) {
     const dim3 grid((unsigned)((a.stretches + kSumWarps - 1) / kSumWarps), (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
-    if (grid.y > 65535) return cudaErrorInvalidConfiguration;
     return launch_early(embedding_sum_kernel<E, N, P>, grid, 32 * kSumWarps, 0, s, a);
 }
 

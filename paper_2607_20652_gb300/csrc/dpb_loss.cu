@@ -47,10 +47,10 @@ constexpr int kStageBytes = 32768;     // 128 x 64 of A and of B
 constexpr int kStore = 4096;           // a warp's rows on their way to memory: 32 of 64 bf16
 constexpr int kRowWarps = 8;
 constexpr int kThreads = 128 + 32 * kRowWarps;
-constexpr int kAhead = 3;                  // units taken ahead
+constexpr int kAhead = 3;              // units taken ahead
 constexpr int kBuffers = 3;            // pieces of dz held
 constexpr int kMostPieces = 48;
-constexpr int kGroup = 32;                // tiles of rows that pass a tile of the vocabulary before the next
+constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -1e30f;      // the maximum of no score
 
@@ -925,12 +925,23 @@ struct Space {
     }
 };
 
+constexpr int64_t kMostTokens = 1ll << 24, kMostWords = 1ll << 28, kMostUnits = 1ll << 26;
+
+// Units of the gradient, which has the forward's and more.
+int64_t units_of(const dpb_linear_loss_config *c) {
+    const int64_t m = (c->tokens + kTile - 1) / kTile, v = ((int64_t)c->vocab + kTile - 1) / kTile;
+    const int64_t d = ((int64_t)c->dim + kTile - 1) / kTile;
+    return m * v + v * d + m * d * Space(c, true).pieces;
+}
+
 dpb_status check_config(const dpb_linear_loss_config *c) {
     if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
     if (c->dtype != DPB_BF16) return fail(DPB_ERR_UNSUPPORTED, "the linear cross entropy takes bf16 rows");
     if (c->tokens < 0 || c->vocab < 1 || c->dim < 1) return fail(DPB_ERR_INVALID_ARG, "a size is too small");
-    if (c->tokens > 0x7fffff00ll || c->vocab > 0x7fffff00)
-        return fail(DPB_ERR_UNSUPPORTED, "at most 2^31 - 256 tokens and words");
+    // a unit's products, of all tokens or of a piece of the words, take far less than the bound of a wait for them
+    if (c->tokens > kMostTokens || c->vocab > kMostWords)
+        return fail(DPB_ERR_UNSUPPORTED, "at most 2^24 tokens and 2^28 words");
+    if (units_of(c) > kMostUnits) return fail(DPB_ERR_UNSUPPORTED, "too many tokens for a vocabulary and rows this large");
     if (c->dim % 8) return fail(DPB_ERR_UNSUPPORTED, "dim must be a multiple of 8");
     if (c->index_bytes != 4 && c->index_bytes != 8) return fail(DPB_ERR_INVALID_ARG, "index_bytes must be 4 or 8");
     if (c->grad_stride != 0 && c->grad_stride != 1) return fail(DPB_ERR_INVALID_ARG, "grad_stride must be 0 or 1");

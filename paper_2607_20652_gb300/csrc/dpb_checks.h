@@ -2,6 +2,7 @@
 // the training-step entry points.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 
 #include "dpb_internal.h"
@@ -47,6 +48,20 @@ inline dpb_status launch_status(cudaError_t e, const char *what) {
         return fail(DPB_ERR_CUDA, "%s launch failed: %s", what, cudaGetErrorString(e));
     }
     return DPB_OK;
+}
+
+// Multiprocessors of the current device, asked for once.
+inline int sms_of_device() {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && dev < kDevices && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return 2;
+    }
+    if (dev < kDevices) known[dev].store(sms, std::memory_order_relaxed);
+    return sms;
 }
 
 // A kernel that may start, and set itself up, while the one before it in the

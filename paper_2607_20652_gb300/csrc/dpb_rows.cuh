@@ -76,11 +76,4 @@ inline bool by_pieces(const void *p, int64_t stride, int64_t rows, int elem) {
     return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || stride * elem % 16 == 0));
 }
 
-inline int sms_of_device() {
-    int dev = 0, sms = 1;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        cudaGetLastError();
-    return sms;
-}
-
 }  // namespace dpb

@@ -1181,7 +1181,7 @@ def run_transformer(args, world, rank, local):
     dpb_ms = parts["forward"] + parts["backward"]
     per_layer = (3 + (4 if args.standardise else 0))
     own_launches = (6 * c["layers"] + 1) * args.steps if args.own_step else 0  # rope 1 + 2, attention 1 + 2; one AdamW
-    if args.own_ends:  # lookup 1 + 3, a norm 1 + 2, the loss 4 + 3 at least
+    if args.own_ends:  # lookup 1 + 3, a norm 1 + 2, the loss 4 + 3
         own_launches += (11 + 3 * (2 * c["layers"] + 1)) * args.steps
     line = {
         "metric": "ParityTransformer GPT-2-small training step (fwd + bwd + AdamW), tokens/s; DPB share of the step",

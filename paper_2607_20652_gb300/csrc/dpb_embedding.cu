@@ -23,7 +23,7 @@ namespace {
 constexpr int kSortBlocks = 16;   // of the sorting cluster
 constexpr int kSortWarps = 32;    // of a block
 constexpr int kDigits = 256;      // 8 bits a pass
-constexpr int kSumWarps = 2;      // of a summing block: few, so that an SM holds twelve of their 160 registers a lane
+constexpr int kSumWarps = 4;      // of a summing block: few, so that an SM holds twelve of their 160 registers a lane
 constexpr int kSumResident = 12;
 
 // A token on its way: its id (vocab: none that counts) and its place.
@@ -37,11 +37,11 @@ struct LookupArgs {
     int64_t ws, ys, dys, dws;  // strides
     int64_t T;
     int V, d, passes, stretch;
-    int64_t stretches;
+    int64_t stretches, blocks;  // stretches of tokens, each a warp's, and the blocks that have them
     float scale;
     Sorted *sorted[2];
-    float *head, *tail;  // [stretches][d]: sums of the first row, begun before, and of the last, begun here and going on
-    int *open;           // how many stretches' last rows go on, and which
+    float *head, *tail;  // [blocks][d]: sums of the first row, begun before, and of the last, begun here and going on
+    int *open;           // how many blocks' last rows go on, and which
     int32_t *status;
 };
 
@@ -206,17 +206,24 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
 // ---- gradient: sums ---------------------------------------------------------------------
 
 // A warp sums one stretch of the sorted tokens over 32 P N columns, the next
-// rows under way while it adds some.
+// rows under way while it adds some. What it has of a row that does not begin
+// and end in its stretch is added up over the block's stretches, in their order.
 template <typename E, int N, int P>
 __global__ void __launch_bounds__(32 * kSumWarps) embedding_sum_kernel(const __grid_constant__ LookupArgs a) {
+    constexpr int kColumns = 32 * P * N;
+    __shared__ float part[kSumWarps][2][kColumns];  // of the first row, begun before, and of the last, going on
+    struct Ends {
+        int head, tail;  // those rows' ids, or -1
+        bool through;    // the first row goes on behind the stretch
+    };
+    __shared__ Ends ends[kSumWarps];
     tc::start_next();
     tc::wait_previous();
-    const int lane = threadIdx.x & 31;
-    const int64_t c = (int64_t)blockIdx.x * kSumWarps + threadIdx.x / 32;
-    if (c >= a.stretches) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const int64_t c = (int64_t)blockIdx.x * kSumWarps + warp;
     const Sorted *sorted = a.sorted[(a.passes - 1) & 1];
-    const int64_t p0 = c * a.stretch, p1 = min(a.T, p0 + a.stretch);
-    const int column = blockIdx.y * 32 * P * N + lane * N;
+    const int64_t p0 = min(a.T, c * a.stretch), p1 = min(a.T, p0 + a.stretch);
+    const int column = blockIdx.y * kColumns + lane * N;
     float acc[P][N];
     auto clear = [&] {
 #pragma unroll
@@ -227,22 +234,21 @@ __global__ void __launch_bounds__(32 * kSumWarps) embedding_sum_kernel(const __g
     clear();
     int id = -1;
     bool whole = true;  // the row's tokens begin in this stretch
-    const int prev = p0 > 0 ? sorted[p0 - 1].id : -1, next = p1 < a.T ? sorted[p1].id : -1;
-    auto flush = [&](bool ends) {
+    const int prev = p0 > 0 && p0 < p1 ? sorted[p0 - 1].id : -1, next = p0 < p1 && p1 < a.T ? sorted[p1].id : -1;
+    auto flush = [&](bool complete) {
         if (id < 0 || id >= a.V) return;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int i = column + p * 32 * N;
             if (i >= a.d) continue;
-            if (whole && ends) {
+            if (whole && complete) {
                 Piece<E, N> v;
 #pragma unroll
                 for (int j = 0; j < N; ++j) v.v[j] = acc[p][j] * a.scale;
                 store_piece(static_cast<E *>(a.dw) + id * a.dws + i, v);
             } else {
-                float *to = (whole ? a.tail : a.head) + c * a.d + i;
 #pragma unroll
-                for (int j = 0; j < N; ++j) to[j] = acc[p][j];
+                for (int j = 0; j < N; ++j) part[warp][whole][(lane + 32 * p) * N + j] = acc[p][j];
             }
         }
     };
@@ -288,11 +294,34 @@ __global__ void __launch_bounds__(32 * kSumWarps) embedding_sum_kernel(const __g
         }
     }
     flush(id != next);
-    if (whole && id == next && id < a.V && blockIdx.y == 0 && lane == 0) a.open[1 + atomicAdd(a.open, 1)] = (int)c;
+    if (lane == 0) {
+        const int first = p0 < p1 && sorted[p0].id == prev && prev < a.V ? prev : -1;
+        ends[warp] = Ends{first, whole && id >= 0 && id < a.V && id == next ? id : -1, !whole && id == next};
+    }
+    __syncthreads();
+    const int columns = min(kColumns, a.d - (int)blockIdx.y * kColumns);
+    for (int i = threadIdx.x; i < columns; i += 32 * kSumWarps) {
+        const int64_t at = (int64_t)blockIdx.y * kColumns + i;
+        float sum = 0.f;
+        bool before = true;  // the row began before the block
+        bool open = false;   // and goes on
+        for (int w = 0; w < kSumWarps; ++w) {
+            const Ends e = ends[w];
+            if (e.head >= 0) {
+                sum += part[w][0][i];
+                open = e.through;
+                if (!open && before) a.head[blockIdx.x * (int64_t)a.d + at] = sum;
+                if (!open && !before) st_elem(static_cast<E *>(a.dw), e.head * a.dws + at, sum * a.scale);
+            }
+            if (e.tail >= 0) sum = part[w][1][i], before = false, open = true;
+        }
+        if (open) (before ? a.head : a.tail)[blockIdx.x * (int64_t)a.d + at] = sum;
+        if (open && !before && at == 0) a.open[1 + atomicAdd(a.open, 1)] = (int)blockIdx.x;
+    }
 }
 
-// The rows whose tokens go on after the stretch where they begin: the sum of
-// what each stretch has of them. A warp has 32 M columns of one at a time.
+// The rows whose tokens go on after the block where they begin: the sum of what
+// each block has of them. A warp has 32 M columns of one at a time.
 constexpr int kJoinWarps = 4;
 template <typename E, int M>
 __global__ void __launch_bounds__(32 * kJoinWarps) embedding_join_kernel(const __grid_constant__ LookupArgs a, int groups) {
@@ -300,9 +329,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) embedding_join_kernel(const _
     const int lane = threadIdx.x & 31;
     const int64_t warps = (int64_t)gridDim.x * kJoinWarps, items = (int64_t)*a.open * groups;
     const Sorted *sorted = a.sorted[(a.passes - 1) & 1];
+    const int64_t each = (int64_t)a.stretch * kSumWarps;  // tokens of a block
     for (int64_t w = (int64_t)blockIdx.x * kJoinWarps + threadIdx.x / 32; w < items; w += warps) {
         const int64_t c = a.open[1 + w / groups];
-        const int id = sorted[(c + 1) * a.stretch].id, i = ((int)(w % groups) * 32 + lane) * M;
+        const int id = sorted[(c + 1) * each].id, i = ((int)(w % groups) * 32 + lane) * M;
         const bool live = i < a.d;
         auto at = [&](const float *from, int64_t k) {
             Piece<float, M> x;
@@ -311,13 +341,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) embedding_join_kernel(const _
         };
         Piece<float, M> sum = at(a.tail, c);
         constexpr int kAtOnce = 16;
-        for (int64_t k = c + 1; k < a.stretches; k += kAtOnce) {
-            // which of the next stretches begin with the row, and their sums at the same time
-            const int64_t mine = min(k + lane, a.stretches - 1);
+        for (int64_t k = c + 1; k < a.blocks; k += kAtOnce) {
+            // which of the next blocks begin with the row, and their sums at the same time
+            const int64_t mine = min(k + lane, a.blocks - 1);
             Piece<float, M> x[kAtOnce];
-            const bool has = lane < kAtOnce && k + lane < a.stretches && sorted[mine * a.stretch].id == id;
+            const bool has = lane < kAtOnce && k + lane < a.blocks && sorted[mine * each].id == id;
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) x[j] = at(a.head, min(k + j, a.stretches - 1));
+            for (int j = 0; j < kAtOnce; ++j) x[j] = at(a.head, min(k + j, a.blocks - 1));
             const int n = __popc(__ballot_sync(kFull, has));
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j)
@@ -342,20 +372,21 @@ int passes_of(int V) {
 
 struct GradSpace {
     int stretch;
-    int64_t stretches;
+    int64_t stretches, blocks;
     size_t sorted[2], head, tail, open, bytes;
     explicit GradSpace(const dpb_embedding_config *c) {
         // As many stretches as warps are resident, of 8 tokens at least and 64 at most.
         const int64_t warps = (int64_t)kSumResident * sms_of_device();
         stretch = (int)std::max<int64_t>(8, std::min<int64_t>(64, (c->tokens + warps - 1) / warps));
         stretches = (c->tokens + stretch - 1) / stretch;
+        blocks = (stretches + kSumWarps - 1) / kSumWarps;
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
         sorted[0] = kStatusBytes;
         sorted[1] = sorted[0] + up((size_t)c->tokens * sizeof(Sorted));
         head = sorted[1] + up((size_t)c->tokens * sizeof(Sorted));
-        tail = head + up((size_t)stretches * c->dim * 4);
-        open = tail + up((size_t)stretches * c->dim * 4);
-        bytes = open + up(((size_t)stretches + 1) * 4);
+        tail = head + up((size_t)blocks * c->dim * 4);
+        open = tail + up((size_t)blocks * c->dim * 4);
+        bytes = open + up(((size_t)blocks + 1) * 4);
     }
 };
 
@@ -393,7 +424,7 @@ dpb_status lookup(const LookupArgs &a, const void *ids, int index_bytes, cudaStr
 
 template <typename E, int N, int P>
 cudaError_t sums(const LookupArgs &a, cudaStream_t s) {
-    const dim3 grid((unsigned)((a.stretches + kSumWarps - 1) / kSumWarps), (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
+    const dim3 grid((unsigned)a.blocks, (unsigned)((a.d + 32 * P * N - 1) / (32 * P * N)));
     return launch_early(embedding_sum_kernel<E, N, P>, grid, 32 * kSumWarps, 0, s, a);
 }
 
@@ -432,7 +463,7 @@ dpb_status gradient(const LookupArgs &a, const void *ids, int index_bytes, cudaS
     DPB_CHECK(launch_status(e, "embedding_backward (sums)"));
     constexpr int M = N == 1 ? 1 : 4;
     const int groups = (a.d + 32 * M - 1) / (32 * M);
-    const int64_t items = a.stretches * groups;
+    const int64_t items = a.blocks * groups;
     const unsigned blocks = (unsigned)std::min<int64_t>((items + kJoinWarps - 1) / kJoinWarps, 4 * sms_of_device());
     return launch_status(launch_early(embedding_join_kernel<E, M>, dim3(blocks), 32 * kJoinWarps, 0, s, a, groups),
                          "embedding_backward (rows)");
@@ -493,7 +524,7 @@ dpb_status dpb_embedding_backward(const dpb_embedding_config *cfg, const dpb_row
     a.dw = grad_weight->data, a.dws = grad_weight->stride;
     a.T = cfg->tokens, a.V = cfg->vocab, a.d = cfg->dim, a.scale = cfg->scale;
     a.passes = passes_of(a.V);
-    a.stretch = w.stretch, a.stretches = w.stretches;
+    a.stretch = w.stretch, a.stretches = w.stretches, a.blocks = w.blocks;
     for (int i = 0; i < 2; ++i) a.sorted[i] = reinterpret_cast<Sorted *>(ws + w.sorted[i]);
     a.head = reinterpret_cast<float *>(ws + w.head);
     a.tail = reinterpret_cast<float *>(ws + w.tail);

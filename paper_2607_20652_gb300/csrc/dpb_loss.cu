@@ -12,13 +12,25 @@
 // gradient, where keeping z would save 2 T V d and cost T V values.
 //
 // All of it is one kernel of matrix products (product_kernel). Pairs of blocks
-// take units, tiles of 256 x 256 of one of three products, from a counter,
-// longest first: the pair shares each product (each block loads its 128 rows
-// of A and half of B, so an operand byte is fetched for 128 products, where
-// single blocks of 128 x 256 would need half as many bytes again). In a block
-// a warp copies, one issues (in the first block of the pair), one takes units,
-// and eight take the sums out of TMEM, two accumulators in turn, so that a
-// unit's results are formed while the next unit is multiplied.
+// take units, tiles of 256 x 256 of one of the products, from a counter: the pair
+// shares each product (each block loads its 128 rows of A and half of B, so an
+// operand byte is fetched for 128 products, where single blocks of 128 x 256
+// would need half as many bytes again). In a block a warp copies, one issues (in
+// the first block of the pair), one takes units, and eight take the sums out of
+// TMEM, two accumulators in turn, so that a unit's results are formed while the
+// next unit is multiplied.
+//
+// What bounds it, at 8192 tokens, 50257 words, 768 columns: forward the products
+// (500 cycles of 512 a slot of 64 columns; 330 us at once, 1910 TFLOP/s, 355 us
+// for as long as one likes, when the power limit holds the clock at 1.6 GHz; the
+// library's product of these sizes, which writes the scores, 350 and 395 us). The
+// gradient's units take 650 (dz: its stores and the products' operands share the
+// shared memory), 670 (dH) and 560 cycles (dW) a slot, 1180 us at once and 1300 us
+// at the power limit, 1470 TFLOP/s, where three library products take 1190.
+// Measured and not taken: dz and dW stored by the row warps themselves, with
+// seven slots in place of the rows on their way (dz 760 cycles a slot); two
+// places for a warp's rows with five slots (710, 750 and 620); a kernel for each
+// piece (14 launches: 1460 us); pieces of 2048 words (1430 us) or 8192 (as 4096).
 //
 // Tokens that take no part are not multiplied: their places are closed up
 // first (prepare_kernel, gather_kernel), which also keeps whatever their rows

@@ -5,9 +5,12 @@
 //   u = w dy,  dx = ds + r u - s r^3 mean(u s),  dw = sum_t dy s r
 //
 // Memory bounds both: a row is read once and kept in registers until its sum
-// is known. 32 to 1024 threads share a row, so that each has at most kMost
-// values of it; the gradient's threads keep their columns' dw over all rows of
-// their block, and the blocks' sums are added up in the blocks' order.
+// is known, and the next row is loaded meanwhile (65536 x 768 bf16: 64 us, 6.3
+// TB/s; 111 without). A warp has a row where its lanes can hold it, up to 1024
+// threads where not. The gradient's threads keep their columns' dw over all rows of
+// their block, and the blocks' sums are added up in the blocks' order (49999 x 1000
+// bf16: 73 us, 5.5 TB/s, with 250 registers and eight warps an SM; held to 128
+// registers, with twice the warps, 187 us for what it spills; and 3 us for dw).
 #include <algorithm>
 
 #include "dpb_checks.h"

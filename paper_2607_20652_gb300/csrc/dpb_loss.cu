@@ -926,13 +926,12 @@ struct Space {
         piece = std::max(piece, round_up((c->vocab + kMostPieces - 1) / kMostPieces, kTile));
         piece = std::min(piece, round_up(c->vocab, kTile));
         pieces = (c->vocab + piece - 1) / piece;
-        size_t at = kStatusBytes;
+        size_t at = 1024;  // the status word's
         auto take = [&](size_t n) {
             const size_t r = at;
             at += (n + 1023) / 1024 * 1024;
             return r;
         };
-        at = 1024;
         head = take(sizeof(Head));
         tokens = take(T * sizeof(Token));
         place = take(T * 4);

@@ -34,18 +34,22 @@ def _tiles(t: torch.Tensor) -> torch.Tensor:
     return t if t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or t.stride(0) % 8 == 0) else t.clone(memory_format=torch.contiguous_format)
 
 
+def _flat(t: torch.Tensor) -> torch.Tensor:
+    return t.reshape(-1).contiguous()
+
+
 class _EmbeddingFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, weight, ids, scale):
         ctx.save_for_backward(ids)
         ctx.at = (weight.shape[0], scale)
-        return dpb.embedding(_rows(weight, weight.dtype), ids.reshape(-1), scale).view(*ids.shape, weight.shape[1])
+        return dpb.embedding(_rows(weight, weight.dtype), _flat(ids), scale).view(*ids.shape, weight.shape[1])
 
     @staticmethod
     @once_differentiable
     def backward(ctx, gy):
         ids, = ctx.saved_tensors
-        return dpb.embedding_backward(_rows(gy, gy.dtype), ids.reshape(-1), *ctx.at), None, None
+        return dpb.embedding_backward(_rows(gy, gy.dtype), _flat(ids), *ctx.at), None, None
 
 
 def embedding(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
@@ -123,7 +127,7 @@ class _LossFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, targets, ignore_index, mean):
         h, w = _tiles(_rows(hidden, hidden.dtype)), _tiles(_rows(weight, hidden.dtype))
-        loss, lse, counted = dpb.linear_cross_entropy_forward(h, w, targets.reshape(-1), ignore_index, want_counted=True)
+        loss, lse, counted = dpb.linear_cross_entropy_forward(h, w, _flat(targets), ignore_index, want_counted=True)
         ctx.save_for_backward(h, w, targets, lse, counted)
         ctx.at = (hidden.shape, weight.dtype, ignore_index, mean)
         return loss.sum() / counted[0] if mean else loss.view(targets.shape)
@@ -139,7 +143,7 @@ class _LossFunction(torch.autograd.Function):
             g = g.reshape(-1)
             if g.stride(0) not in (0, 1):
                 g = g.contiguous()
-        dh, dw = dpb.linear_cross_entropy_backward(h, w, targets.reshape(-1), lse, g, ignore_index,
+        dh, dw = dpb.linear_cross_entropy_backward(h, w, _flat(targets), lse, g, ignore_index,
                                                    want_hidden=ctx.needs_input_grad[0], want_weight=ctx.needs_input_grad[1])
         return (None if dh is None else dh.view(shape), None if dw is None else dw.to(weight_type)) + (None,) * 3
 

@@ -101,6 +101,26 @@ def test_gradients_of_any_layout():
         assert torch.equal(p, q)
 
 
+def test_shifted_targets_and_strided_indices():
+    """The next token's loss: parts of the batch's rows and ids, and indices that are not dense."""
+    from paper_2607_20652_gb300 import ends
+    torch.manual_seed(3)
+    h, w = torch.randn(4, 33, 64, device="cuda").to(BF), torch.randn(97, 64, device="cuda").to(BF)
+    ids = torch.randint(0, 97, (4, 33), device="cuda")
+    hh = h.clone().requires_grad_()
+    loss = ends.linear_cross_entropy(hh[:, :-1], w, ids[:, 1:])
+    want = ends.linear_cross_entropy(h[:, :-1].contiguous().requires_grad_(), w, ids[:, 1:].contiguous())
+    assert torch.equal(loss, want)
+    loss.backward()
+    assert hh.grad[:, :-1].any() and not hh.grad[:, -1].any()
+    wide = torch.randint(0, 97, (40,), device="cuda")
+    assert torch.equal(ends.embedding(w, wide[::2]), w[wide[::2]])
+    x = h[0, :20].clone().requires_grad_()
+    torch.autograd.grad(ends.linear_cross_entropy(x, w, wide[::2]), x)
+    g, = torch.autograd.grad(ends.embedding(w.requires_grad_(), wide[::2]), w, torch.ones(20, 64, device="cuda", dtype=BF))
+    assert torch.equal(g.float(), torch.zeros(97, 64, device="cuda").index_add_(0, wide[::2], torch.ones(20, 64, device="cuda")))
+
+
 def test_means_without_tokens():
     from paper_2607_20652_gb300 import ends
     h, w = torch.randn(20, 64, device="cuda").to(BF).requires_grad_(), torch.randn(97, 64, device="cuda").to(BF).requires_grad_()
@@ -157,7 +177,7 @@ def test_model_is_the_same_model(attention):
         if m is not None:
             loss = m(ids, tgt)
             loss.backward()
-            losses.append(float(loss))
+            losses.append(float(loss.detach()))
     # the other model's scores are bf16: each off by 2^-8 of its size (below 1 here) in about log 97
     assert abs(losses[0] - losses[1]) < 2.0 ** -8
     assert torch.equal(own(ids).argmax(-1), own(ids).argmax(-1)) and rel(own(ids), other(ids)) < 12 * 2.0 ** -8

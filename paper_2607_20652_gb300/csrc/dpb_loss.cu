@@ -60,8 +60,8 @@ constexpr int kStore = 4096;           // a warp's rows on their way to memory: 
 constexpr int kRowWarps = 8;
 constexpr int kThreads = 128 + 32 * kRowWarps;
 constexpr int kAhead = 3;              // units taken ahead
-constexpr int kBuffers = 3;            // pieces of dz held
-constexpr int kMostPieces = 48;
+constexpr int kBuffers = 3;            // pieces of dz held, where there are many tokens
+constexpr int kMostPieces = 160;
 constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -1e30f;      // the maximum of no score
@@ -87,7 +87,7 @@ struct Token {
 struct Args {
     CUtensorMap hidden, closed;  // rows as given, and closed up
     CUtensorMap weight;
-    CUtensorMap dz[kBuffers], dz_out[kBuffers];  // loaded and stored
+    CUtensorMap dz, dz_out;  // loaded and stored: [rows, and their remainders][held pieces]
     CUtensorMap dw;
     const bf16 *h;
     int64_t h_stride;
@@ -100,12 +100,14 @@ struct Args {
     float *loss, *lse;
     int *counted;
     CUtensorMap sums;
-    float *acc;  // [rows][dim]: sums of dH, where there are several pieces
+    float *acc;  // sums of dH, where there are several pieces: [rows][dim], or (split) one for each piece, of T_pad rows
     bf16 *dh;
     int64_t dh_stride;
     int64_t T, T_pad;
     int V, d, piece;  // piece: words of a piece
-    int pieces;
+    int pieces, held;
+    bool split;  // each piece's sums of dH apart, added up by join_hidden_kernel
+    bool fine;   // dz as two bf16, the rounded value and the remainder
     bool want_h, want_w;
     bool few;  // rows that the tokens' cluster closes up itself
     int32_t *status;
@@ -130,7 +132,8 @@ __device__ __forceinline__ Unit score_unit(int kind, int u, int tiles_m, int til
 // pieces overlap: dz of a piece comes before the products that read the piece
 // before it, so that what a unit waits for was taken a piece's time ago:
 //   dz 0, dz 1, dH 0, dW 0, dz 2, dH 1, dW 1, ..., dW last, dH last
-// (in the last one the longer units come first, so that the pairs end together).
+// (in the last one the longer units come first, so that the pairs end together);
+// where all of dz is held, all of it comes first.
 struct List {
     int tiles_m, tiles_d, words;  // words of the vocabulary that a piece (the forward: all) has
     int count, last;              // tokens; words of the last piece
@@ -151,13 +154,22 @@ struct List {
         if (u >= n_w + n_h) return Unit{kEnd, 0, 0, 0, 0};
         const bool is_h = h_first ? u < n_h : u >= n_w;
         u -= is_h && !h_first ? n_w : !is_h && h_first ? n_h : 0;
-        return Unit{is_h ? kDHidden : kDWeight, u / tiles_d * kTile, u % tiles_d * kTile, ((is_h ? w : count) + 63) / 64, piece};
+        const int blocks = ((is_h ? w : count) + 63) / 64;
+        return Unit{is_h ? kDHidden : kDWeight, u / tiles_d * kTile, u % tiles_d * kTile, a.fine ? 2 * blocks : blocks, piece};
     }
     __device__ __forceinline__ Unit at(const Args &a, int u) const {
         const int all = a.pieces, first = grad_units(words_of(a, 0));
         if (a.loss) return u < first ? score_unit(kScores, u, tiles_m, (a.V + kTile - 1) / kTile, a.d, 0) : Unit{kEnd, 0, 0, 0, 0};
         int piece = 0;
-        if (u >= first) {
+        if (a.held == all) {
+            const int dz = grad_units(words), total = dz * (all - 1) + grad_units(last);
+            const bool reads = u >= total;
+            if (reads) u -= total;
+            const int each = reads ? weight_units(a, words) + hidden_units(a) : dz;
+            if (each > 0) piece = min(u / each, all - 1);
+            u -= piece * each;
+            if (reads) return reader(a, u, piece);
+        } else if (u >= first) {
             u -= first;
             const int readers = weight_units(a, words) + hidden_units(a), full = grad_units(words) + readers;
             // pieces 1 .. all - 2 are full, and so are the readers of those before them
@@ -182,13 +194,13 @@ struct List {
     __device__ __forceinline__ bool wait(const Args &a, const Unit &t) const {
         const int each = 2 * kRowWarps;
         if (t.kind == kGrad) {
-            const int before = t.piece - kBuffers;
+            const int before = t.piece - a.held;
             return before < 0 || (reached(&a.head->done[before][kDWeight], each * weight_units(a, words)) &&
                                   reached(&a.head->done[before][kDHidden], each * hidden_units(a)));
         }
         if (t.kind != kDHidden && t.kind != kDWeight) return true;
         return reached(&a.head->done[t.piece][kGrad], each * grad_units(words_of(a, t.piece))) &&
-               (t.kind == kDWeight || t.piece == 0 ||
+               (t.kind == kDWeight || t.piece == 0 || a.split ||
                 reached(&a.head->done[t.piece - 1][kDHidden], each * hidden_units(a)));
     }
     static __device__ __forceinline__ bool reached(const int *counter, int target) {
@@ -320,10 +332,11 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 }
 
 // 64 columns of a row's dz as bf16 pairs, into the warp's rows on their way to
-// memory. `taken` is called once they have been read out of TMEM.
+// memory; or what their rounding left over. `taken` is called once they have been
+// read out of TMEM.
 template <typename F>
 __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int lane, int columns, const Token &t,
-                                             int target, F &&taken) {
+                                             int target, bool remainder, F &&taken) {
     const uint64_t scale = pair(kLog2e, kLog2e), less = pair(-t.lse2, -t.lse2);
     uint32_t both[2][32];
     __syncwarp();
@@ -352,7 +365,12 @@ __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int 
                 if (c + i >= columns) p[i] = 0.f;
         uint32_t x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = t.row < 0 ? 0u : pack_bf16(p[2 * i] * t.g, p[2 * i + 1] * t.g);
+        for (int i = 0; i < 16; ++i) {
+            const float a = p[2 * i] * t.g, b = p[2 * i + 1] * t.g;
+            x[i] = pack_bf16(a, b);
+            if (remainder) x[i] = pack_bf16(a - __uint_as_float(x[i] << 16), b - __uint_as_float(x[i] & 0xffff0000u));
+            if (t.row < 0) x[i] = 0;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             store_shared(swizzled(stage, lane, c / 8 + i), x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
@@ -463,7 +481,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     fence_async();
                 }
                 const int v0 = t.piece * a.piece;
-                const CUtensorMap *dz = &a.dz[t.piece % kBuffers];
+                const int dz0 = t.piece % a.held * a.piece;  // the piece's columns of dz
+                const int first = t.kind > kGrad && a.fine ? t.blocks / 2 : t.blocks;  // blocks of rounded values
                 for (int k = 0; k < t.blocks; ++k, ++at) {
                     const int s = at % kStages;
                     if (at >= kStages && !bar_wait(empty(s), ((at / kStages) & 1) ^ 1, kTries)) {
@@ -473,6 +492,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     const uint32_t bar = peer_addr(full(s), 0), to = base + s * kStageBytes;
                     if (rank == 0) bar_arrive_expect(full(s), 2 * kStageBytes);
                     const int m = t.m0 + 128 * rank, n = t.n0 + 128 * rank;
+                    const int kk = 64 * (k < first ? k : k - first), rest = k < first ? 0 : (int)a.T_pad;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const uint32_t ta = to + 8192 * j, tb = ta + 16384;
@@ -480,11 +500,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                             copy_box_pair(ta, rows, 64 * k, m + 64 * j, bar);
                             copy_box_pair(tb, &a.weight, 64 * k, v0 + n + 64 * j, bar);
                         } else if (t.kind == kDHidden) {
-                            copy_box_pair(ta, dz, 64 * k, m + 64 * j, bar);
-                            copy_box_pair(tb, &a.weight, n + 64 * j, v0 + 64 * k, bar);
+                            copy_box_pair(ta, &a.dz, dz0 + kk, rest + m + 64 * j, bar);
+                            copy_box_pair(tb, &a.weight, n + 64 * j, v0 + kk, bar);
                         } else {
-                            copy_box_pair(ta, dz, m + 64 * j, 64 * k, bar);
-                            copy_box_pair(tb, rows, n + 64 * j, 64 * k, bar);
+                            copy_box_pair(ta, &a.dz, dz0 + m + 64 * j, rest + kk, bar);
+                            copy_box_pair(tb, rows, n + 64 * j, kk, bar);
                         }
                     }
                 }
@@ -593,7 +613,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             Token token{-1, 0.f, 0.f, -1};
             if (t.kind != kDWeight && row < count) token = a.tokens[row];
             float4 before[8];
-            if (t.kind == kDHidden && t.piece > 0 && t.piece == a.pieces - 1) {
+            if (t.kind == kDHidden && t.piece > 0 && t.piece == a.pieces - 1 && !a.split) {
                 fence_cluster();  // other blocks' sums, which the first block has seen
                 fence_async();
                 sums_before(a, before, row0 + lane / 8, count, column + 4 * (lane % 8));
@@ -631,18 +651,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             } else if (t.kind == kGrad) {
                 const int words = list.words_of(a, t.piece);
                 const int target = token.target - t.piece * a.piece - column;
+                const int at = t.piece % a.held * a.piece + column;
 #pragma unroll 1
-                for (int c = 0; c < 128; c += 64) {
-                    if (lane == 0) stores_read();
-                    __syncwarp();
-                    grad_columns(from + c, stage, lane, words - column - c, token, target - c, [&] {
-                        if (c) sums_read(b);  // the products need not wait for the rest
-                    });
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) store_box(&a.dz_out[t.piece % kBuffers], stage, column + c, row0);
-                    if (c == 0) settle(later);
-                }
+                for (int part = 0; part <= (int)a.fine; ++part)
+#pragma unroll 1
+                    for (int c = 0; c < 128; c += 64) {
+                        if (lane == 0) stores_read();
+                        __syncwarp();
+                        grad_columns(from + c, stage, lane, words - column - c, token, target - c, part, [&] {
+                            if (c && part == (int)a.fine) sums_read(b);  // the products need not wait for the rest
+                        });
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0) store_box(&a.dz_out, stage, at + c, row0 + part * (int)a.T_pad);
+                        if (c == 0 && part == 0) settle(later);
+                    }
             } else if (t.kind == kDWeight) {
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 64) {
@@ -675,7 +698,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             } else {
                 // by way of shared memory: copies add the sums of a piece to those of the
                 // pieces before; in the last one eight lanes have 128 bytes of a row
-                const bool first = t.piece == 0, last = t.piece == a.pieces - 1;
+                const bool first = t.piece == 0 || a.split, last = t.piece == a.pieces - 1 && !a.split;
+                const int to = row0 + (a.split ? t.piece * (int)a.T_pad : 0);
                 const int r = lane / 8, piece = lane % 8;
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 32) {
@@ -691,8 +715,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     if (!last) {
                         fence_async_shared();
                         __syncwarp();
-                        if (lane == 0 && first) store_box(&a.sums, stage, column + c, row0);
-                        if (lane == 0 && !first) add_box(&a.sums, stage, column + c, row0);
+                        if (lane == 0 && first) store_box(&a.sums, stage, column + c, to);
+                        if (lane == 0 && !first) add_box(&a.sums, stage, column + c, to);
                         continue;
                     }
                     const int col = column + c + 4 * piece;
@@ -877,6 +901,29 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args
     }
 }
 
+// dH of a token from the pieces' sums, in their order: four columns a thread.
+__global__ void __launch_bounds__(256) join_hidden_kernel(const __grid_constant__ Args a) {
+    wait_previous();
+    const int each = a.d / 4, count = a.head->count;
+    const float g = a.head->g_max;
+    const int64_t step = a.T_pad * a.d, all = (int64_t)count * each;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+        const int row = (int)(i / each), column = (int)(i - (int64_t)row * each) * 4;
+        const float *from = a.acc + (int64_t)row * a.d + column;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 0; p < a.pieces; p += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __ldcg(reinterpret_cast<const float4 *>(from + min(p + j, a.pieces - 1) * step));
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (p + j < a.pieces) sum.x += x[j].x, sum.y += x[j].y, sum.z += x[j].z, sum.w += x[j].w;
+        }
+        *reinterpret_cast<uint2 *>(a.dh + a.tokens[row].row * a.dh_stride + column) =
+            make_uint2(pack_bf16(sum.x * g, sum.y * g), pack_bf16(sum.z * g, sum.w * g));
+    }
+}
+
 // ---- host side ------------------------------------------------------------------
 
 PFN_cuTensorMapEncodeTiled_v12000 encoder() {
@@ -912,20 +959,38 @@ dpb_status make_map(CUtensorMap *map, const void *data, int64_t stride, int64_t 
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Words of a piece of the gradient.
+// Pieces of the gradient. With many tokens: kPieceBytes of dz each, kBuffers of
+// them held, dH added up over them one after the other. Where all of dz takes no
+// more than that, all of it is held, and the pieces are as many as give every pair
+// of blocks two units of dH, whose sums are kept apart: one after the other few
+// units would follow each other through the whole vocabulary. With the fewest
+// tokens, whose rounding errors of dz do not average out and whose products take
+// little, dz is held to 16 bits, in two bf16.
 constexpr int64_t kPieceBytes = 64ll << 20;
-constexpr int kLeastPiece = 4096;
+constexpr int kLeastPiece = 4096, kFineRows = 512;
 
 struct Space {
-    int64_t T_pad, piece, pieces;
-    size_t head, tokens, place, closed, part, z_target, dz[kBuffers], acc, bytes;
+    int64_t T_pad, piece, pieces, held;
+    bool split = false, fine = false;
+    size_t head, tokens, place, closed, part, z_target, dz, acc, bytes;
     Space(const dpb_linear_loss_config *c, bool backward) {
         const size_t T = (size_t)c->tokens, d = (size_t)c->dim, V = (size_t)c->vocab;
+        const int64_t words = round_up(c->vocab, kTile);
         T_pad = round_up(c->tokens, kTile);
-        piece = std::max<int64_t>(kPieceBytes / (2 * std::max<int64_t>(T_pad, 1)) / kTile * kTile, kLeastPiece);
-        piece = std::max(piece, round_up((c->vocab + kMostPieces - 1) / kMostPieces, kTile));
-        piece = std::min(piece, round_up(c->vocab, kTile));
-        pieces = (c->vocab + piece - 1) / piece;
+        fine = T_pad <= kFineRows && 4 * T_pad * words <= kBuffers * kPieceBytes;
+        if (2 * T_pad * words <= kBuffers * kPieceBytes) {
+            const int64_t tiles = std::max<int64_t>(1, T_pad / kTile) * ((c->dim + kTile - 1) / kTile);
+            pieces = std::min<int64_t>((2 * (sms_of_device() / 2) + tiles - 1) / tiles, std::min<int64_t>(words / kTile, kMostPieces));
+            piece = round_up((c->vocab + pieces - 1) / pieces, kTile);
+            held = pieces = (c->vocab + piece - 1) / piece;
+            split = pieces > 1;
+        } else {
+            piece = std::max<int64_t>(kPieceBytes / (2 * std::max<int64_t>(T_pad, 1)) / kTile * kTile, kLeastPiece);
+            piece = std::max(piece, round_up((c->vocab + kMostPieces - 1) / kMostPieces, kTile));
+            piece = std::min(piece, words);
+            pieces = (c->vocab + piece - 1) / piece;
+            held = std::min<int64_t>(pieces, kBuffers);
+        }
         size_t at = 1024;  // the status word's
         auto take = [&](size_t n) {
             const size_t r = at;
@@ -937,14 +1002,13 @@ struct Space {
         place = take(T * 4);
         closed = take(T * d * 2);
         if (backward) {
-            for (int i = 0; i < kBuffers; ++i) dz[i] = i < pieces ? take((size_t)T_pad * piece * 2) : dz[0];
-            acc = pieces > 1 ? take((size_t)T * d * 4) : at;
+            dz = take((size_t)T_pad * (fine ? 2 : 1) * held * piece * 2);
+            acc = take(split ? (size_t)pieces * T_pad * d * 4 : pieces > 1 ? T * d * 4 : 0);
             part = z_target = at;
         } else {
             part = take((V + kTile - 1) / kTile * (size_t)T_pad * sizeof(float2));
             z_target = take((size_t)T_pad * 4);
-            for (size_t &x : dz) x = at;
-            acc = at;
+            dz = acc = at;
         }
         bytes = at;
     }
@@ -1005,6 +1069,9 @@ dpb_status begin(Args &a, const Space &w, const dpb_linear_loss_config *c, const
     a.d = c->dim;
     a.piece = (int)w.piece;
     a.pieces = (int)w.pieces;
+    a.held = (int)w.held;
+    a.split = w.split;
+    a.fine = w.fine;
     // A launch less where eight blocks close the rows up as fast: half of 340 x 768 ignored 16.8 us (17.3 with the
     // launch), of 1000 x 256 15.8 (14.9), of 1000 x 768 19.4 (17.7); none ignored 15.6, 13.9, 16.2 (16.5, 14.5,
     // 17.0). The launch also takes 2.5 us of the host's time.
@@ -1096,14 +1163,17 @@ dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, 
     if (grad_hidden) a.dh = static_cast<bf16 *>(grad_hidden->data), a.dh_stride = grad_hidden->stride;
     if (grad_weight) DPB_CHECK(make_map(&a.dw, grad_weight->data, grad_weight->stride, cfg->vocab, cfg->dim, 32));
     a.acc = reinterpret_cast<float *>(ws + w.acc);
-    if (w.pieces > 1) DPB_CHECK(make_map(&a.sums, a.acc, cfg->dim, cfg->tokens, cfg->dim, 32, true));
-    for (int i = 0; i < std::min<int64_t>(kBuffers, w.pieces); ++i) {
-        DPB_CHECK(make_map(&a.dz[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 64));
-        DPB_CHECK(make_map(&a.dz_out[i], ws + w.dz[i], w.piece, w.T_pad, w.piece, 32));
-    }
+    if (w.pieces > 1)
+        DPB_CHECK(make_map(&a.sums, a.acc, cfg->dim, w.split ? w.pieces * w.T_pad : cfg->tokens, cfg->dim, 32, true));
+    const int64_t columns = w.held * w.piece, rows = w.T_pad * (w.fine ? 2 : 1);
+    DPB_CHECK(make_map(&a.dz, ws + w.dz, columns, rows, columns, 64));
+    DPB_CHECK(make_map(&a.dz_out, ws + w.dz, columns, rows, columns, 32));
     DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, grad_loss, lse, ws, s));
     const int64_t tiles_m = w.T_pad / kTile, tiles_v = (cfg->vocab + kTile - 1) / kTile, tiles_d = (cfg->dim + kTile - 1) / kTile;
-    return launch_products(a, tiles_m * tiles_v + tiles_v * tiles_d, s);
+    DPB_CHECK(launch_products(a, tiles_m * tiles_v + tiles_v * tiles_d, s));
+    if (!w.split || !grad_hidden) return DPB_OK;
+    const unsigned blocks = (unsigned)std::min<int64_t>((cfg->tokens * (cfg->dim / 4) + 255) / 256, 4 * sms_of_device());
+    return launch_status(launch_early(join_hidden_kernel, dim3(blocks), 256, 0, s, a), "linear_cross_entropy_backward (sums)");
 }
 
 }  // extern "C"

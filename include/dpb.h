@@ -654,8 +654,9 @@ dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, c
  * (grad_stride 0: one value for all, as of a mean; or 1). grad_hidden and
  * grad_weight (rows as hidden and weight; either may be NULL, then it is not
  * computed) are written, rows of ignored tokens with 0. dz enters its products
- * in bf16, relative to the largest finite |grad_loss|; their sums are fp32, in an
- * order that the sizes and the ignored tokens alone fix, and rounded once.
+ * in bf16, relative to the largest finite |grad_loss| (up to 512 tokens in two
+ * bf16, value and remainder, where both take at most 192 MB); their sums are fp32,
+ * in an order that the sizes and the ignored tokens alone fix, and rounded once.
  */
 dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
                                              const dpb_rows *weight, const void *targets, const float *lse,

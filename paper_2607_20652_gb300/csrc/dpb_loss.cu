@@ -59,7 +59,7 @@ constexpr int kStageBytes = 32768;     // 128 x 64 of A and of B
 constexpr int kStore = 4096;           // a warp's rows on their way to memory: 32 of 64 bf16
 constexpr int kRowWarps = 8;
 constexpr int kThreads = 128 + 32 * kRowWarps;
-constexpr int kAhead = 3;              // units taken ahead
+constexpr int kAhead = 4;              // units taken ahead, at most
 constexpr int kBuffers = 3;            // pieces of dz held, where there are many tokens
 constexpr int kMostPieces = 160;
 constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
@@ -189,19 +189,35 @@ struct List {
         }
         return score_unit(kGrad, u, tiles_m, (words_of(a, piece) + kTile - 1) / kTile, a.d, piece);
     }
+    // Where the row warps count units of a kind. Where all of dz is held, it is one count.
+    __device__ __forceinline__ int *counter(const Args &a, const Unit &t) const {
+        return &a.head->done[t.kind == kGrad && a.held == a.pieces ? 0 : t.piece][t.kind];
+    }
     // One thread: what the unit waits for has been done: dz of its piece, and the
-    // sums of dH before it; for dz, the products that read its place.
-    __device__ __forceinline__ bool wait(const Args &a, const Unit &t) const {
+    // sums of dH before it; for dz, the products that read its place. `all_there`
+    // (false at first): all of dz is held and has been waited for.
+    __device__ __forceinline__ bool wait(const Args &a, const Unit &t, bool &all_there) const {
         const int each = 2 * kRowWarps;
         if (t.kind == kGrad) {
             const int before = t.piece - a.held;
-            return before < 0 || (reached(&a.head->done[before][kDWeight], each * weight_units(a, words)) &&
-                                  reached(&a.head->done[before][kDHidden], each * hidden_units(a)));
+            if (before < 0) return true;
+            if (!reached(&a.head->done[before][kDWeight], each * weight_units(a, words)) ||
+                !reached(&a.head->done[before][kDHidden], each * hidden_units(a)))
+                return false;
+        } else if (t.kind == kDHidden || t.kind == kDWeight) {
+            const bool ordered = t.kind == kDHidden && t.piece > 0 && !a.split;
+            if (all_there && !ordered) return true;
+            const bool one = a.held == a.pieces;
+            const int dz = one ? grad_units(words) * (a.pieces - 1) + grad_units(last) : grad_units(words_of(a, t.piece));
+            if ((!all_there && !reached(counter(a, Unit{kGrad, 0, 0, 0, t.piece}), each * dz)) ||
+                (ordered && !reached(&a.head->done[t.piece - 1][kDHidden], each * hidden_units(a))))
+                return false;
+            all_there = one;
+        } else {
+            return true;
         }
-        if (t.kind != kDHidden && t.kind != kDWeight) return true;
-        return reached(&a.head->done[t.piece][kGrad], each * grad_units(words_of(a, t.piece))) &&
-               (t.kind == kDWeight || t.piece == 0 || a.split ||
-                reached(&a.head->done[t.piece - 1][kDHidden], each * hidden_units(a)));
+        fence_cluster();  // for the blocks that it is handed to
+        return true;
     }
     static __device__ __forceinline__ bool reached(const int *counter, int target) {
         for (uint32_t i = 0; i < kTries; ++i) {
@@ -470,15 +486,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         if (elect_one()) {
             const CUtensorMap *rows = a.head->all ? &a.hidden : &a.closed;
             int at = 0;  // slots filled
+            bool fenced = false;
             Unit t;
             while (true) {
                 if ((failed = !units.next(t))) break;
                 units.done();
                 if (t.kind == kEnd) break;
                 // other blocks' dz, which the first block has seen (List::wait), by way of copies
-                if (t.kind > kGrad) {
+                if (t.kind > kGrad && !(fenced && a.held == a.pieces)) {
                     fence_cluster();
                     fence_async();
+                    fenced = true;
                 }
                 const int v0 = t.piece * a.piece;
                 const int dz0 = t.piece % a.held * a.piece;  // the piece's columns of dz
@@ -552,19 +570,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     } else if (warp == 2) {
         // ---- units
         if (rank == 0 && elect_one()) {
+            bool all_there = false;
+            // Two ahead, as a long unit that a pair holds is one that others lack; four
+            // where they are so short that taking them is what they wait for.
+            int ahead = 2;
             for (int i = 0;; ++i) {
-                const int s = i % kAhead;
-                if (i >= kAhead && !bar_wait(base + Shared::kTaken + 8 * s, ((i / kAhead) & 1) ^ 1, kTries)) {
+                const int s = i % kAhead, before = i - ahead;
+                if (before >= 0 && !bar_wait(base + Shared::kTaken + 8 * (before % kAhead), (before / kAhead) & 1, kTries)) {
                     failed = true;
                     break;
                 }
-                const int u = atomicAdd(&a.head->next, 1);
-                const Unit t = list.at(a, u);
-                if (!list.wait(a, t)) {
+                const Unit t = list.at(a, atomicAdd(&a.head->next, 1));
+                ahead = t.blocks <= 8 ? kAhead : 2;
+                if (!list.wait(a, t, all_there)) {
                     failed = true;
                     break;
                 }
-                if (t.kind != kScores) fence_cluster();
                 units.hand(t, s, 0);
                 units.hand(t, s, 1);
                 if (t.kind == kEnd) break;
@@ -739,7 +760,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             if (t.blocks > 0 && t.kind != kGrad) sums_read(b);
             // what others wait for: dz and the sums of dH in memory; of dW, that dz has been read
             if (t.kind == kGrad || t.kind == kDHidden) {
-                pending = &a.head->done[t.piece][t.kind];
+                pending = list.counter(a, t);
             } else if (t.kind == kDWeight) {
                 __syncwarp();
                 if (lane == 0) count_done(&a.head->done[t.piece][kDWeight]);
@@ -963,9 +984,11 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // them held, dH added up over them one after the other. Where all of dz takes no
 // more than that, all of it is held, and the pieces are as many as give every pair
 // of blocks two units of dH, whose sums are kept apart: one after the other few
-// units would follow each other through the whole vocabulary. With the fewest
-// tokens, whose rounding errors of dz do not average out and whose products take
-// little, dz is held to 16 bits, in two bf16.
+// units would follow each other through the whole vocabulary (1000 tokens, 50257
+// words, 768 columns: 300 us, 212 apart; 2000: 342 and 345; 4096, too many for it,
+// 560). With the fewest tokens, whose rounding errors of dz do not average out, dz
+// is held to 16 bits, in two bf16: 33 tokens take 135 us, 512 195 (268 and 282 in
+// one bf16 and one after the other).
 constexpr int64_t kPieceBytes = 64ll << 20;
 constexpr int kLeastPiece = 4096, kFineRows = 512;
 

@@ -10,12 +10,14 @@
 // threads where not. The gradient's threads keep their columns' dw over all rows of
 // their block, and the blocks' sums are added up in the blocks' order (49999 x 1000
 // bf16: 73 us, 5.5 TB/s, with 250 registers and eight warps an SM; held to 128
-// registers, with twice the warps, 187 us for what it spills; and 3 us for dw).
+// registers, with twice the warps, 187 us for what it spills; rows on their way in
+// shared memory, 120 registers, 16 warps: 77 us; and 3 us for dw).
 #include <algorithm>
 
 #include "dpb_checks.h"
 #include "dpb_device.cuh"
 #include "dpb_rows.cuh"
+#include "dpb_tensor_core.cuh"
 
 namespace dpb {
 namespace {
@@ -112,6 +114,7 @@ template <typename E, int N, int P, int MOST>
 __global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const __grid_constant__ NormArgs a, int row_warps) {
     __shared__ float sums[32];
     extern __shared__ float columns[];  // [d]: the block's dw
+    tc::start_next();
     const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = MOST / row_threads;
     const int64_t step = (int64_t)gridDim.x * rows;
     int64_t t = (int64_t)blockIdx.x * rows + threadIdx.x / row_threads;
@@ -185,6 +188,7 @@ __global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const __grid_consta
 // order, then the threads.
 __global__ void __launch_bounds__(1024) add_norm_columns_kernel(const NormArgs a) {
     __shared__ float sums[32][33];
+    tc::wait_previous();
     const int lane = threadIdx.x & 31, slice = threadIdx.x / 32, i = blockIdx.x * 32 + lane;
     float v = 0.f;
     if (i < a.d)
@@ -360,8 +364,7 @@ dpb_status dpb_add_norm_backward(const dpb_norm_config *cfg, const dpb_rows *tot
                         rows_by_pieces(cfg, grad_x) && by_pieces(weight, 0, 1, elem);
     DPB_CHECK(run(a, cfg->dtype, pieces, true, s));
     if (!grad_weight) return DPB_OK;
-    add_norm_columns_kernel<<<(a.d + 31) / 32, 1024, 0, s>>>(a);
-    return launch_status(cudaGetLastError(), "add_norm_backward (weight)");
+    return launch_status(launch_early(add_norm_columns_kernel, dim3((a.d + 31) / 32), 1024, 0, s, a), "add_norm_backward (weight)");
 }
 
 }  // extern "C"

@@ -4,14 +4,15 @@
 //   s = x + delta (rounded to the rows' type),  y = w s r,  r = (mean s^2 + eps)^(-1/2)
 //   u = w dy,  dx = ds + r u - s r^3 mean(u s),  dw = sum_t dy s r
 //
-// Memory bounds both: a row is read once and kept in registers until its sum
-// is known, and the next row is loaded meanwhile (65536 x 768 bf16: 64 us, 6.3
-// TB/s; 111 without). A warp has a row where its lanes can hold it, up to 1024
-// threads where not. The gradient's threads keep their columns' dw over all rows of
-// their block, and the blocks' sums are added up in the blocks' order (49999 x 1000
-// bf16: 73 us, 5.5 TB/s, with 250 registers and eight warps an SM; held to 128
-// registers, with twice the warps, 187 us for what it spills; rows on their way in
-// shared memory, 120 registers, 16 warps: 77 us; and 3 us for dw).
+// Memory bounds both: a row is read once and kept until its sum is known, and the
+// next row is loaded meanwhile (65536 x 768 bf16: 64 us, 6.3 TB/s; 111 without). A
+// warp has a row where its lanes can hold it, up to 1024 threads where not. The
+// gradient's threads keep their columns' dw over all rows of their block, and the
+// blocks' sums are added up in the blocks' order; its rows on their way are in
+// shared memory (65536 x 768 bf16: 78 us, 5.2 TB/s; 49999 x 1000 81; 32768 x 768
+// fp32 72; 16384 x 4096 bf16 93; with them in 250 registers and eight warps an SM
+// 81, 79, 85 and 114, held to 128 registers 187 us at 49999 x 1000 for what they
+// spill), and 3 us of each are for dw.
 #include <algorithm>
 
 #include "dpb_checks.h"
@@ -35,16 +36,19 @@ struct NormArgs {
     float eps;
 };
 
-// The sum over a row's threads; `row_warps` warps each, all of the block's threads call it.
-__device__ __forceinline__ float row_sum(float v, int row_warps, float *sums) {
+// The sums of two values over a row's threads; `row_warps` warps each, all of the block's threads call it.
+__device__ __forceinline__ float2 row_sums(float2 v, int row_warps, float2 *sums) {
 #pragma unroll
-    for (int i = 16; i > 0; i /= 2) v += __shfl_xor_sync(kFull, v, i);
+    for (int i = 16; i > 0; i /= 2) {
+        v.x += __shfl_xor_sync(kFull, v.x, i);
+        v.y += __shfl_xor_sync(kFull, v.y, i);
+    }
     if (row_warps == 1) return v;
     const int warp = threadIdx.x / 32, first = warp / row_warps * row_warps;
     if ((threadIdx.x & 31) == 0) sums[warp] = v;
     __syncthreads();
-    v = 0.f;
-    for (int i = 0; i < row_warps; ++i) v += sums[first + i];
+    v = make_float2(0.f, 0.f);
+    for (int i = 0; i < row_warps; ++i) v.x += sums[first + i].x, v.y += sums[first + i].y;
     __syncthreads();
     return v;
 }
@@ -65,7 +69,7 @@ __device__ __forceinline__ void load_row(Bits<E, N> (&r)[P], const void *data, i
 // Each row's threads load the next row while they work on one.
 template <typename E, int N, int P, int MOST>
 __global__ void __launch_bounds__(MOST) add_norm_kernel(const __grid_constant__ NormArgs a, int row_warps) {
-    __shared__ float sums[32];
+    __shared__ float2 sums[32];
     const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = MOST / row_threads;
     const int64_t step = (int64_t)gridDim.x * rows;
     int64_t t = (int64_t)blockIdx.x * rows + threadIdx.x / row_threads;
@@ -94,7 +98,7 @@ __global__ void __launch_bounds__(MOST) add_norm_kernel(const __grid_constant__ 
         }
         load_row(x, a.x, a.xs, t + step, t + step < a.T, in, row_threads, a.d);
         if (a.delta) load_row(delta, a.delta, a.deltas, t + step, t + step < a.T, in, row_threads, a.d);
-        sum = row_sum(sum, row_warps, sums);
+        sum = row_sums(make_float2(sum, 0.f), row_warps, sums).x;
         const float r = rsqrtf(sum / a.d + a.eps);
         E *s = static_cast<E *>(a.s) + t * a.ss, *y = static_cast<E *>(a.y) + t * a.ys;
 #pragma unroll
@@ -110,10 +114,76 @@ __global__ void __launch_bounds__(MOST) add_norm_kernel(const __grid_constant__ 
     }
 }
 
+__device__ __forceinline__ void copy_piece(void *to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_addr(to)), "l"(from) : "memory");
+}
+
+// Where a thread's pieces of a row's three rows are until they are used: pieces of
+// 16 bytes in places of its own in shared memory, kStages rows on their way, which
+// its registers would not hold; single values, and the widest rows, in registers,
+// read when they are used.
 template <typename E, int N, int P, int MOST>
-__global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const __grid_constant__ NormArgs a, int row_warps) {
-    __shared__ float sums[32];
-    extern __shared__ float columns[];  // [d]: the block's dw
+struct GradRows {
+    static constexpr bool kCopied = N > 1 && MOST == 256;
+    static constexpr int kStages = P == 4 ? 2 : 3;  // two blocks an SM
+    static constexpr size_t kBytes = kCopied ? (size_t)kStages * 3 * P * MOST * 16 : 0;
+    uint8_t *mem;
+    int in, row_threads, slot = 0, filled = 0;
+    Bits<E, N> now[kCopied ? 1 : 3][kCopied ? 1 : P];
+    __device__ __forceinline__ uint8_t *place(int at, int array, int p) const {
+        return mem + (((at * 3 + array) * P + p) * MOST + threadIdx.x) * 16;
+    }
+    __device__ __forceinline__ void init() {
+        if constexpr (kCopied)  // places behind the row's end stay 0
+            for (int k = 0; k < kStages * 3 * P; ++k)
+                *reinterpret_cast<uint4 *>(mem + (k * MOST + threadIdx.x) * 16) = make_uint4(0, 0, 0, 0);
+    }
+    // Asks for row t.
+    __device__ __forceinline__ void ask(const NormArgs &a, int64_t t) {
+        if constexpr (kCopied) {
+            if (t < a.T) {
+                const E *s = static_cast<const E *>(a.x) + t * a.xs, *dy = static_cast<const E *>(a.dy) + t * a.dys;
+                const E *ds = static_cast<const E *>(a.ds) + t * a.dss;
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const int i = (in + p * row_threads) * N;
+                    if (i >= a.d) continue;
+                    copy_piece(place(filled, 0, p), s + i);
+                    copy_piece(place(filled, 1, p), dy + i);
+                    if (a.ds) copy_piece(place(filled, 2, p), ds + i);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            filled = filled + 1 == kStages ? 0 : filled + 1;
+        }
+    }
+    // The oldest row asked for, t, is there.
+    __device__ __forceinline__ void take(const NormArgs &a, int64_t t) {
+        if constexpr (kCopied) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        } else {
+            load_row(now[0], a.x, a.xs, t, t < a.T, in, row_threads, a.d);
+            load_row(now[1], a.dy, a.dys, t, t < a.T, in, row_threads, a.d);
+            if (a.ds) load_row(now[2], a.ds, a.dss, t, t < a.T, in, row_threads, a.d);
+        }
+    }
+    __device__ __forceinline__ Piece<E, N> get(int array, int p) const {
+        if constexpr (kCopied) {
+            Bits<E, N> b;
+            b.w = *reinterpret_cast<const uint4 *>(place(slot, array, p));
+            return values(b);
+        } else {
+            return values(now[array][p]);
+        }
+    }
+    __device__ __forceinline__ void next() { slot = slot + 1 == kStages ? 0 : slot + 1; }
+};
+
+template <typename E, int N, int P, int MOST>
+__global__ void __launch_bounds__(MOST, N > 1 && MOST == 256 ? 2 : 1)
+    add_norm_grad_kernel(const __grid_constant__ NormArgs a, int row_warps) {
+    __shared__ float2 sums[32];
+    extern __shared__ __align__(16) uint8_t mem[];
     tc::start_next();
     const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = MOST / row_threads;
     const int64_t step = (int64_t)gridDim.x * rows;
@@ -123,43 +193,37 @@ __global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const __grid_consta
     for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int j = 0; j < N; ++j) dw[p][j] = 0.f;
-    Bits<E, N> w[P], s[P], dy[P], ds[P];
+    Bits<E, N> w[P];
     if (a.w) load_row(w, a.w, 0, 0, true, in, row_threads, a.d);
-    load_row(s, a.x, a.xs, t, t < a.T, in, row_threads, a.d);
-    load_row(dy, a.dy, a.dys, t, t < a.T, in, row_threads, a.d);
-    if (a.ds) load_row(ds, a.ds, a.dss, t, t < a.T, in, row_threads, a.d);
+    GradRows<E, N, P, MOST> row{mem, in, row_threads};
+    constexpr int kStages = GradRows<E, N, P, MOST>::kStages;
+    row.init();
+    for (int k = 0; k < kStages - 1; ++k) row.ask(a, t + k * step);
+    // every thread of the block makes the same number of turns
     for (int64_t t0 = (int64_t)blockIdx.x * rows; t0 < a.T; t0 += step, t += step) {
         const bool live = t < a.T;
-        Bits<E, N> s0[P], dy0[P], ds0[P];
+        row.ask(a, t + (kStages - 1) * step);
+        row.take(a, t);
         float sq = 0.f, us = 0.f;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            s0[p] = s[p], dy0[p] = dy[p];
-            if (a.ds) ds0[p] = ds[p];
-        }
-        load_row(s, a.x, a.xs, t + step, t + step < a.T, in, row_threads, a.d);
-        load_row(dy, a.dy, a.dys, t + step, t + step < a.T, in, row_threads, a.d);
-        if (a.ds) load_row(ds, a.ds, a.dss, t + step, t + step < a.T, in, row_threads, a.d);
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const Piece<E, N> v = values(s0[p]), g = values(dy0[p]), k = values(w[p]);
+            const Piece<E, N> v = row.get(0, p), g = row.get(1, p), k = values(w[p]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 sq = fmaf(v.v[j], v.v[j], sq);
                 us = fmaf(a.w ? g.v[j] * k.v[j] : g.v[j], v.v[j], us);
             }
         }
-        sq = row_sum(sq, row_warps, sums);
-        us = row_sum(us, row_warps, sums);
-        const float r = rsqrtf(sq / a.d + a.eps), less = r * r * r * (us / a.d);
+        const float2 both = row_sums(make_float2(sq, us), row_warps, sums);
+        const float r = rsqrtf(both.x / a.d + a.eps), less = r * r * r * (both.y / a.d);
         E *dx = static_cast<E *>(a.dx) + t * a.dxs;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int i = (in + p * row_threads) * N;
             if (!live || i >= a.d) continue;
-            Piece<E, N> v = values(s0[p]), rest;
-            const Piece<E, N> g = values(dy0[p]), k = values(w[p]);
-            if (a.ds) rest = values(ds0[p]);
+            Piece<E, N> v = row.get(0, p), rest;
+            const Piece<E, N> g = row.get(1, p), k = values(w[p]);
+            if (a.ds) rest = row.get(2, p);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 dw[p][j] = fmaf(g.v[j] * r, v.v[j], dw[p][j]);
@@ -167,9 +231,13 @@ __global__ void __launch_bounds__(MOST) add_norm_grad_kernel(const __grid_consta
             }
             store_piece(dx + i, v);
         }
+        row.next();
     }
     if (!a.part) return;
     // the block's rows one after the other
+    float *columns = reinterpret_cast<float *>(mem);  // [d]: the block's dw
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
     for (int q = 0; q < rows; ++q) {
         if ((int)threadIdx.x / row_threads == q)
 #pragma unroll
@@ -231,6 +299,19 @@ struct RowShape {
 };
 
 template <typename E, int N, int P, int MOST>
+dpb_status launch_grad(NormArgs &a, const RowShape &r, cudaStream_t s) {
+    const int rows = MOST / (32 * r.warps);
+    constexpr size_t kSmem = std::max(GradRows<E, N, P, MOST>::kBytes, (size_t)MOST * P * N * 4);
+    const void *kernel = reinterpret_cast<const void *>(add_norm_grad_kernel<E, N, P, MOST>);
+    const cudaError_t e = allow_smem(kernel, kSmem);
+    if (e != cudaSuccess) return launch_status(e, "add_norm_backward");
+    static const int resident = resident_blocks(kernel, MOST, kSmem);
+    a.blocks = (int)std::min<int64_t>((a.T + rows - 1) / rows, (int64_t)std::min(resident, kGradBlocks) * sms_of_device());
+    add_norm_grad_kernel<E, N, P, MOST><<<a.blocks, MOST, kSmem, s>>>(a, r.warps);
+    return launch_status(cudaGetLastError(), "add_norm_backward");
+}
+
+template <typename E, int N, int P, int MOST>
 dpb_status launch(NormArgs &a, const RowShape &r, bool grad, cudaStream_t s) {
     const int rows = MOST / (32 * r.warps);
     if (!grad) {
@@ -239,14 +320,7 @@ dpb_status launch(NormArgs &a, const RowShape &r, bool grad, cudaStream_t s) {
         add_norm_kernel<E, N, P, MOST><<<(unsigned)blocks, MOST, 0, s>>>(a, r.warps);
         return launch_status(cudaGetLastError(), "add_norm");
     }
-    const size_t smem = a.part ? (size_t)a.d * 4 : 0;
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(add_norm_grad_kernel<E, N, P, MOST>), smem);
-    if (e != cudaSuccess) return launch_status(e, "add_norm_backward");
-    static const int resident =
-        resident_blocks(reinterpret_cast<const void *>(add_norm_grad_kernel<E, N, P, MOST>), MOST, kMostDim * 4);
-    a.blocks = (int)std::min<int64_t>((a.T + rows - 1) / rows, (int64_t)std::min(resident, kGradBlocks) * sms_of_device());
-    add_norm_grad_kernel<E, N, P, MOST><<<a.blocks, MOST, smem, s>>>(a, r.warps);
-    return launch_status(cudaGetLastError(), "add_norm_backward");
+    return launch_grad<E, N, P, MOST>(a, r, s);
 }
 
 template <typename E, int N>

@@ -64,7 +64,7 @@ constexpr int kBuffers = 3;            // pieces of dz held, where there are man
 constexpr int kMostPieces = 160;
 constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLowest = -1e30f;      // the maximum of no score
+constexpr float kLowest = -3.402823466e38f;  // the maximum of no score: finite, so that it can be subtracted
 
 enum Kind { kScores = 0, kGrad = 1, kDHidden = 2, kDWeight = 3, kEnd = 4 };
 

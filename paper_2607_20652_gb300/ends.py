@@ -8,6 +8,12 @@ lookup, the addition of a block's output to the residual with the next norm,
 and the cross entropy from the last hidden rows run in the library's kernels;
 no tensor of tokens x vocabulary is made. The gradients have no gradient of
 their own: a second differentiation raises.
+
+A forward and backward pass may be captured into a CUDA graph. As with every
+function of autograd, no graph of the same parameters that was made on the
+default stream may be alive then: autograd would accumulate their gradients on
+that stream, outside the capture, which can end the process. Drop its outputs
+before, and make the steps before the capture on the capture's stream.
 """
 from __future__ import annotations
 

@@ -325,6 +325,42 @@ def test_another_stream_and_a_graph():
     assert dpb.status() == 0
 
 
+def test_scores_far_below_zero():
+    """Maxima near the lowest fp32 values: 300 words in seven ranks, the highest of 43 equal scores."""
+    V, d, big = 300, 8, 1.5 * 2.0 ** 60
+    rank = torch.arange(V, device="cuda") % 7
+    h = torch.full((7, d), big, device="cuda", dtype=torch.bfloat16)
+    w = (-big * (1 + rank.double() / 4))[:, None].expand(V, d).to(torch.bfloat16).contiguous()
+    y = torch.arange(7, device="cuda")
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    z = h.double() @ w.double().T  # about -2e37: exact in fp32, as the factors have few bits
+    top = z.max(1).values
+    rest = torch.logsumexp(z - top[:, None], 1)  # the logarithm of 43
+    # lse: a rounding and the logarithm's; the loss another
+    assert ((lse.double() - (top + rest)).abs() <= 2.0 ** -22 * top.abs()).all()
+    want = top - z[torch.arange(7), y] + rest
+    assert ((loss.double() - want).abs() <= 2.0 ** -22 * want).all()
+
+
+def test_two_streams_at_once():
+    """Losses and gradients of different sizes under way at the same time, their blocks side by side on the device."""
+    work = []
+    for T, V, d, left in ((3000, 9000, 264, "some"), (24001, 4500, 72, "runs"), (300, 20000, 128, "none")):
+        h, w, y, gl = draw(T, V, d, seed=T, left_out=left, even=False)
+        loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+        work.append(((h, w, y, gl), (loss, lse, *dpb.linear_cross_entropy_backward(h, w, y, lse, gl)), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(8):
+        for (h, w, y, gl), want, s in work:
+            with torch.cuda.stream(s):
+                loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+                got.append((want, (loss, lse, *dpb.linear_cross_entropy_backward(h, w, y, lse, gl))))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for want, out in got for a, b in zip(want, out))
+    assert all(dpb.status(stream=s) == 0 for _, _, s in work)
+
+
 def test_refusals():
     h, w, y, gl = draw(30, 70, 64)
     for bad in (dict(hidden=h.float()), dict(weight=w.float()), dict(hidden=h[:, :60]), dict(targets=y.float()),

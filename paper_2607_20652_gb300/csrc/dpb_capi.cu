@@ -33,6 +33,27 @@ cudaError_t allow_smem(const void *func, size_t bytes) {
     return e;
 }
 
+cudaError_t resident_clusters(const void *func, const cudaLaunchConfig_t &how, int *clusters) {
+    static std::mutex mu;
+    static std::map<std::pair<const void *, int>, int> found;  // (kernel, device)
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mu);
+    int &n = found[{func, dev}];
+    if (n == 0) {
+        e = allow_smem(func, how.dynamicSmemBytes);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, func, &how);
+        if (e != cudaSuccess) {
+            cudaGetLastError();  // returned to the caller: not left for its next CUDA check
+            n = 0;
+        }
+    }
+    *clusters = n;
+    return e;
+}
+
 // A word every 256 bytes. Device memory of the library's image: it needs no
 // allocation (which a stream capture would not allow) and is never freed.
 __device__ int32_t status_words[DPB_STATUS_SLOTS][64];

@@ -11,8 +11,10 @@
 // as many different ones. A row whose tokens lie in several stretches is joined
 // from their partial sums in the stretches' order. No atomics on values: equal
 // inputs give equal bits. 65536 tokens of 50257 words, frequent ones among them,
-// take 59 us: the order 22 (a cluster of 8 blocks: 40), the sums some 20, the joins
-// the rest; 1000 tokens still take 10 us to sort, waiting blocks for one another.
+// take 53 us: the order 17, the sums some 21 to 30, as many different rows there are,
+// the joins 4. Tokens that are written to memory where their digit puts them, without
+// being brought together first, take 55 in all, as two words of 32 bits 59. 1000
+// tokens still take 9 us to sort, waiting blocks for one another.
 #include <algorithm>
 
 #include "dpb_checks.h"
@@ -26,11 +28,12 @@ namespace {
 constexpr int kSortBlocks = 16;   // of the sorting cluster
 constexpr int kSortWarps = 32;    // of a block
 constexpr int kDigits = 256;      // 8 bits a pass
+constexpr int kHeld = 4;          // tokens of a lane under way: all of them up to 65536
 constexpr int kSumWarps = 4;      // of a summing block: few, so that an SM holds twelve of their 160 registers a lane
 constexpr int kSumResident = 12;
 
 // A token on its way: its id (vocab: none that counts) and its place.
-struct Sorted {
+struct alignas(8) Sorted {
     int id, token;
 };
 
@@ -92,6 +95,11 @@ __device__ __forceinline__ unsigned same_digit(int digit) {
     return same;
 }
 
+struct SortMemory {
+    int count[kSortWarps][kDigits];
+    Sorted stage[32 * kHeld * kSortWarps];  // the block's tokens in their order, where they are still held
+};
+
 // The first cluster sorts, a digit of 8 bits a pass: each warp counts the
 // digits of its stretch of the tokens, the counts of all warps before it give
 // each digit's first place, and it puts its tokens there in their order.
@@ -110,12 +118,15 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
             for (int i = lane; i < pieces; i += 32) store_piece(static_cast<E *>(a.dw) + v * a.dws + i * N, none);
         return;
     }
-    __shared__ int count[kSortWarps][kDigits], total[kDigits], sums[kDigits / 32];
+    __shared__ int total[kDigits], shift[kDigits];
+    __shared__ int2 sums[kDigits / 32];
+    extern __shared__ SortMemory sort_memory[];
+    Sorted *const stage = sort_memory->stage;
+    int(*const count)[kDigits] = sort_memory->count;
     const uint32_t rank = blockIdx.x;
     const int64_t warps = kSortBlocks * kSortWarps, each = ((a.T + warps - 1) / warps + 31) / 32 * 32;
     const int64_t t0 = min(a.T, (rank * kSortWarps + warp) * each), t1 = min(a.T, t0 + each);
     if (rank == 0 && tid == 0) *a.open = 0;
-    constexpr int kHeld = 4;  // tokens of a lane under way: all of them up to 65536
     for (int pass = 0; pass < a.passes; ++pass) {
         const Sorted *from = a.sorted[(pass & 1) ^ 1];
         Sorted *to = a.sorted[pass & 1];
@@ -149,7 +160,7 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
                 __syncwarp();
             }
         };
-        for (int i = tid; i < kSortWarps * kDigits; i += 32 * kSortWarps) (&count[0][0])[i] = 0;
+        for (int i = tid; i < kSortWarps * kDigits; i += 32 * kSortWarps) count[0][i] = 0;
         __syncthreads();
         for (int64_t t = t0; t < t1; t += 32 * kHeld) load(t);
         __syncthreads();
@@ -164,35 +175,49 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
             total[tid] = n;
         }
         tc::cluster_sync();
-        int before = 0, all = 0, upto = 0;
+        // A digit's first place in the block and in all. Tokens still held go by way of
+        // shared memory, so that neighbours there, mostly of the same digit, are written
+        // to memory side by side.
+        const bool held = each <= 32 * kHeld;
+        int before = 0, all = 0, mine = 0;
+        int2 upto;
         if (tid < kDigits) {
             const uint32_t at = tc::smem_addr(&total[tid]);
+            mine = total[tid];
 #pragma unroll
             for (uint32_t r = 0; r < kSortBlocks; ++r) {
                 const int n = read_peer(tc::peer_addr(at, r));
                 if (r < rank) before += n;
                 all += n;
             }
-            upto = all;
+            upto = make_int2(mine, all);
 #pragma unroll
             for (int i = 1; i < 32; i *= 2) {
-                const int n = __shfl_up_sync(kFull, upto, i);
-                if (lane >= i) upto += n;
+                const int2 n = make_int2(__shfl_up_sync(kFull, upto.x, i), __shfl_up_sync(kFull, upto.y, i));
+                if (lane >= i) upto.x += n.x, upto.y += n.y;
             }
             if (lane == 31) sums[warp] = upto;
         }
         __syncthreads();
         if (tid < kDigits) {
-            int first = upto - all + before;
-            for (int w = 0; w < warp; ++w) first += sums[w];
+            int here = upto.x - mine, first = upto.y - all + before;
+            for (int w = 0; w < warp; ++w) here += sums[w].x, first += sums[w].y;
+            shift[tid] = first - here;
 #pragma unroll 8
-            for (int w = 0; w < kSortWarps; ++w) count[w][tid] += first;
+            for (int w = 0; w < kSortWarps; ++w) count[w][tid] += held ? here : first;
         }
         __syncthreads();
-        if (each <= 32 * kHeld) {  // still held, with their places from 0
+        if (held) {  // their places in the warp from 0
 #pragma unroll
             for (int k = 0; k < kHeld; ++k)
-                if (x[k].id >= 0 && t0 < t1) to[count[warp][digit(x[k].id)] + place[k]] = x[k];
+                if (x[k].id >= 0 && t0 < t1) stage[count[warp][digit(x[k].id)] + place[k]] = x[k];
+            __syncthreads();
+            const int64_t first = min(a.T, rank * kSortWarps * each);
+            const int n = (int)(min(a.T, first + kSortWarps * each) - first);
+            for (int i = tid; i < n; i += 32 * kSortWarps) {
+                const Sorted token = stage[i];
+                to[i + shift[digit(token.id)]] = token;
+            }
         } else {
             for (int64_t t = t0; t < t1; t += 32 * kHeld) {
                 load(t);
@@ -434,14 +459,9 @@ cudaError_t sums(const LookupArgs &a, cudaStream_t s) {
 template <typename E, int N, typename I>
 cudaError_t sort(const LookupArgs &a, const I *ids, cudaStream_t s) {
     void (*const kernel)(const LookupArgs, const I *) = embedding_sort_kernel<E, N, I>;
-    // a cluster of 16 is more than a device need hold; this one does
-    static const cudaError_t large = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                                          cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (large != cudaSuccess) return large;
-    const int others = std::max(1, std::min(sms_of_device() / kSortBlocks - 1, (a.V + 32 * kSortBlocks - 1) / (32 * kSortBlocks)));
     cudaLaunchConfig_t how{};
-    how.gridDim = dim3(kSortBlocks * (1 + others));
-    how.blockDim = dim3(32 * kSortWarps);
+    how.gridDim = how.blockDim = dim3(32 * kSortWarps);
+    how.dynamicSmemBytes = sizeof(SortMemory);
     how.stream = s;
     cudaLaunchAttribute cluster{};
     cluster.id = cudaLaunchAttributeClusterDimension;
@@ -449,7 +469,14 @@ cudaError_t sort(const LookupArgs &a, const I *ids, cudaStream_t s) {
     cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
     how.attrs = &cluster;
     how.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&how, kernel, a, ids);
+    int resident;
+    cudaError_t e = resident_clusters(reinterpret_cast<const void *>(kernel), how, &resident);
+    if (e != cudaSuccess) return e;
+    // Those that write zeros, all at the same time: with one cluster more than the device holds (152 SMs, 7 clusters)
+    // the last starts when others end, and 50257 rows of 768 take 24 us where the order takes 17.
+    const int others = std::max(1, std::min(resident - 1, (a.V + 32 * kSortBlocks - 1) / (32 * kSortBlocks)));
+    how.gridDim = dim3(kSortBlocks * (1 + others));
+    e = cudaLaunchKernelEx(&how, kernel, a, ids);
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
 

@@ -97,6 +97,10 @@ constexpr size_t kMaxSmemPerBlock = 227 * 1024;
 // default (and again only when a later launch needs more), so repeated
 // launches make no driver call; returns the error of a failed set.
 cudaError_t allow_smem(const void *func, size_t bytes);
+// How many clusters of `func`, launched as `how` says, the current device holds at a
+// time (asked once; `func` is always launched in the same way but for its grid).
+// Clusters of more than 8 blocks and how.dynamicSmemBytes are allowed on the way.
+cudaError_t resident_clusters(const void *func, const cudaLaunchConfig_t &how, int *clusters);
 // The library's status word `slot` (1 .. DPB_STATUS_SLOTS) on the current device,
 // or nullptr.
 int32_t *status_word(int32_t slot);

@@ -28,7 +28,6 @@ namespace {
 constexpr int kSortBlocks = 16;   // of the sorting cluster
 constexpr int kSortWarps = 32;    // of a block
 constexpr int kDigits = 256;      // 8 bits a pass
-constexpr int kHeld = 4;          // tokens of a lane under way: all of them up to 65536
 constexpr int kSumWarps = 4;      // of a summing block: few, so that an SM holds twelve of their 160 registers a lane
 constexpr int kSumResident = 12;
 
@@ -95,16 +94,23 @@ __device__ __forceinline__ unsigned same_digit(int digit) {
     return same;
 }
 
+// HELD: tokens of a lane under way; where that is all of them, they are read once a pass.
+template <int HELD>
 struct SortMemory {
     int count[kSortWarps][kDigits];
-    Sorted stage[32 * kHeld * kSortWarps];  // the block's tokens in their order, where they are still held
+    Sorted stage[32 * HELD * kSortWarps];  // the block's tokens in their order, where they are still held
 };
+// of a warp: a multiple of 32
+__host__ __device__ __forceinline__ int64_t tokens_of_warp(int64_t T) {
+    const int64_t warps = kSortBlocks * kSortWarps;
+    return ((T + warps - 1) / warps + 31) / 32 * 32;
+}
 
 // The first cluster sorts, a digit of 8 bits a pass: each warp counts the
 // digits of its stretch of the tokens, the counts of all warps before it give
 // each digit's first place, and it puts its tokens there in their order.
 // The other clusters write zeros.
-template <typename E, int N, typename I>
+template <typename E, int N, typename I, int HELD>
 __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(const __grid_constant__ LookupArgs a, const I *ids) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
     tc::start_next();
@@ -120,23 +126,24 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
     }
     __shared__ int total[kDigits], shift[kDigits];
     __shared__ int2 sums[kDigits / 32];
-    extern __shared__ SortMemory sort_memory[];
-    Sorted *const stage = sort_memory->stage;
-    int(*const count)[kDigits] = sort_memory->count;
+    extern __shared__ __align__(8) uint8_t raw[];
+    SortMemory<HELD> &memory = *reinterpret_cast<SortMemory<HELD> *>(raw);
+    Sorted *const stage = memory.stage;
+    int(*const count)[kDigits] = memory.count;
     const uint32_t rank = blockIdx.x;
-    const int64_t warps = kSortBlocks * kSortWarps, each = ((a.T + warps - 1) / warps + 31) / 32 * 32;
+    const int64_t each = tokens_of_warp(a.T);
     const int64_t t0 = min(a.T, (rank * kSortWarps + warp) * each), t1 = min(a.T, t0 + each);
     if (rank == 0 && tid == 0) *a.open = 0;
     for (int pass = 0; pass < a.passes; ++pass) {
         const Sorted *from = a.sorted[(pass & 1) ^ 1];
         Sorted *to = a.sorted[pass & 1];
-        Sorted x[kHeld];
-        int place[kHeld];  // among the warp's tokens of the same digit
+        Sorted x[HELD];
+        int place[HELD];  // among the warp's tokens of the same digit
         auto digit = [&](int id) { return id < 0 ? -1 : (id >> (8 * pass)) & 255; };
         // the tokens from t on, and their places behind those that `count` has
         auto load = [&](int64_t t) {
 #pragma unroll
-            for (int k = 0; k < kHeld; ++k) {
+            for (int k = 0; k < HELD; ++k) {
                 const int64_t at = t + 32 * k + lane;
                 x[k] = Sorted{-1, 0};
                 if (at >= t1) continue;
@@ -150,7 +157,7 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
                 }
             }
 #pragma unroll
-            for (int k = 0; k < kHeld; ++k) {
+            for (int k = 0; k < HELD; ++k) {
                 if (t + 32 * k >= t1) break;
                 const int g = digit(x[k].id);
                 const unsigned same = same_digit(g);
@@ -162,7 +169,7 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
         };
         for (int i = tid; i < kSortWarps * kDigits; i += 32 * kSortWarps) count[0][i] = 0;
         __syncthreads();
-        for (int64_t t = t0; t < t1; t += 32 * kHeld) load(t);
+        for (int64_t t = t0; t < t1; t += 32 * HELD) load(t);
         __syncthreads();
         if (tid < kDigits) {  // the block's warps before each
             int n = 0;
@@ -178,7 +185,7 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
         // A digit's first place in the block and in all. Tokens still held go by way of
         // shared memory, so that neighbours there, mostly of the same digit, are written
         // to memory side by side.
-        const bool held = each <= 32 * kHeld;
+        const bool held = each <= 32 * HELD;
         int before = 0, all = 0, mine = 0;
         int2 upto;
         if (tid < kDigits) {
@@ -209,7 +216,7 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
         __syncthreads();
         if (held) {  // their places in the warp from 0
 #pragma unroll
-            for (int k = 0; k < kHeld; ++k)
+            for (int k = 0; k < HELD; ++k)
                 if (x[k].id >= 0 && t0 < t1) stage[count[warp][digit(x[k].id)] + place[k]] = x[k];
             __syncthreads();
             const int64_t first = min(a.T, rank * kSortWarps * each);
@@ -219,10 +226,10 @@ __global__ void __launch_bounds__(32 * kSortWarps, 1) embedding_sort_kernel(cons
                 to[i + shift[digit(token.id)]] = token;
             }
         } else {
-            for (int64_t t = t0; t < t1; t += 32 * kHeld) {
+            for (int64_t t = t0; t < t1; t += 32 * HELD) {
                 load(t);
 #pragma unroll
-                for (int k = 0; k < kHeld; ++k)
+                for (int k = 0; k < HELD; ++k)
                     if (x[k].id >= 0) to[place[k]] = x[k];
             }
         }
@@ -456,12 +463,12 @@ cudaError_t sums(const LookupArgs &a, cudaStream_t s) {
     return launch_early(embedding_sum_kernel<E, N, P>, grid, 32 * kSumWarps, 0, s, a);
 }
 
-template <typename E, int N, typename I>
-cudaError_t sort(const LookupArgs &a, const I *ids, cudaStream_t s) {
-    void (*const kernel)(const LookupArgs, const I *) = embedding_sort_kernel<E, N, I>;
+template <typename E, int N, int HELD, typename I>
+cudaError_t sort_held(const LookupArgs &a, const I *ids, cudaStream_t s) {
+    void (*const kernel)(const LookupArgs, const I *) = embedding_sort_kernel<E, N, I, HELD>;
     cudaLaunchConfig_t how{};
     how.gridDim = how.blockDim = dim3(32 * kSortWarps);
-    how.dynamicSmemBytes = sizeof(SortMemory);
+    how.dynamicSmemBytes = sizeof(SortMemory<HELD>);
     how.stream = s;
     cudaLaunchAttribute cluster{};
     cluster.id = cudaLaunchAttributeClusterDimension;
@@ -478,6 +485,15 @@ cudaError_t sort(const LookupArgs &a, const I *ids, cudaStream_t s) {
     how.gridDim = dim3(kSortBlocks * (1 + others));
     e = cudaLaunchKernelEx(&how, kernel, a, ids);
     return e == cudaSuccess ? cudaGetLastError() : e;
+}
+
+// Eight tokens a lane where four are not all of them and eight are: 131072 x 768
+// 103 us, 113 with four, which read the tokens twice; 65536 x 768 54 and 53.5,
+// 300000 x 768, where neither is enough, 195 and 189.
+template <typename E, int N, typename I>
+cudaError_t sort(const LookupArgs &a, const I *ids, cudaStream_t s) {
+    const int64_t each = tokens_of_warp(a.T);
+    return each > 32 * 4 && each <= 32 * 8 ? sort_held<E, N, 8>(a, ids, s) : sort_held<E, N, 4>(a, ids, s);
 }
 
 template <typename E, int N>

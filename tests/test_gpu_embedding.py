@@ -88,6 +88,17 @@ def test_lengths_at_the_stretches_ends(T):
         check_gradient(dpb.embedding_backward(dy, ids, 2200), dy, ids, 2200, 1.0)
 
 
+@pytest.mark.parametrize("T", [65535, 65536, 65537, 131072, 131073, 196609])
+def test_many_tokens(T):
+    """Either side of where the sort holds 4 and 8 tokens a lane; two passes of it, and three."""
+    dy = torch.randn(T, 8, device="cuda").bfloat16()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    for V in (50257, 70000):
+        for kind in ("any", "frequent"):
+            ids = draw_ids(kind, T, V, g)
+            check_gradient(dpb.embedding_backward(dy, ids, V), dy, ids, V, 1.0)
+
+
 def test_the_order_of_a_rows_sum_is_the_tokens():
     """2^24 + 1 - 2^24: what a fp32 sum in the tokens' order gives, within one stretch."""
     dy = torch.tensor([2.0 ** 24, 1.0, -2.0 ** 24], device="cuda")[:, None].contiguous()

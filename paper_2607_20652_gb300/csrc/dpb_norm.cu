@@ -9,10 +9,10 @@
 // warp has a row where its lanes can hold it, up to 1024 threads where not. The
 // gradient's threads keep their columns' dw over all rows of their block, and the
 // blocks' sums are added up in the blocks' order; its rows on their way are in
-// shared memory (65536 x 768 bf16: 78 us, 5.2 TB/s; 49999 x 1000 81; 32768 x 768
-// fp32 72; 16384 x 4096 bf16 93; with them in 250 registers and eight warps an SM
-// 81, 79, 85 and 114, held to 128 registers 187 us at 49999 x 1000 for what they
-// spill), and 3 us of each are for dw.
+// shared memory (65536 x 768 bf16: 74 us, 5.4 TB/s; 49999 x 1000 75; 32768 x 768
+// fp32 71; 16384 x 4096 bf16 87; 10000 x 16384 fp32 390; with them in registers 81,
+// 79, 85, 114 and 745). Of each some 3 us are for dw; summed up a warp after the
+// other, waiting for each, a block's took 4 us more at 49999 x 1000.
 #include <algorithm>
 
 #include "dpb_checks.h"
@@ -120,12 +120,11 @@ __device__ __forceinline__ void copy_piece(void *to, const void *from) {
 
 // Where a thread's pieces of a row's three rows are until they are used: pieces of
 // 16 bytes in places of its own in shared memory, kStages rows on their way, which
-// its registers would not hold; single values, and the widest rows, in registers,
-// read when they are used.
+// its registers would not hold; single values in registers, read when they are used.
 template <typename E, int N, int P, int MOST>
 struct GradRows {
-    static constexpr bool kCopied = N > 1 && MOST == 256;
-    static constexpr int kStages = P == 4 ? 2 : 3;  // two blocks an SM
+    static constexpr bool kCopied = N > 1;
+    static constexpr int kStages = (P == 4 ? 2 : 3) - (MOST == 1024);  // two blocks an SM, one of the widest rows
     static constexpr size_t kBytes = kCopied ? (size_t)kStages * 3 * P * MOST * 16 : 0;
     uint8_t *mem;
     int in, row_threads, slot = 0, filled = 0;
@@ -235,21 +234,28 @@ __global__ void __launch_bounds__(MOST, N > 1 && MOST == 256 ? 2 : 1)
     }
     if (!a.part) return;
     // the block's rows one after the other
-    float *columns = reinterpret_cast<float *>(mem);  // [d]: the block's dw
+    float *columns = reinterpret_cast<float *>(mem);  // [rows][d]
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    for (int q = 0; q < rows; ++q) {
-        if ((int)threadIdx.x / row_threads == q)
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+        const int i = (in + p * row_threads) * N;
+        float *to = columns + (int)threadIdx.x / row_threads * a.d + i;
+        if (i >= a.d) continue;
+        if constexpr (N == 1) {
+            *to = dw[p][0];
+        } else {
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const int i = (in + p * row_threads) * N + j;
-                    if (i < a.d) columns[i] = q ? columns[i] + dw[p][j] : dw[p][j];
-                }
-        __syncthreads();
+            for (int j = 0; j < N; j += 4)
+                *reinterpret_cast<float4 *>(to + j) = make_float4(dw[p][j], dw[p][j + 1], dw[p][j + 2], dw[p][j + 3]);
+        }
     }
-    for (int i = threadIdx.x; i < a.d; i += MOST) a.part[(int64_t)blockIdx.x * a.d + i] = columns[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.d; i += MOST) {
+        float sum = columns[i];
+        for (int q = 1; q < rows; ++q) sum += columns[q * a.d + i];
+        a.part[(int64_t)blockIdx.x * a.d + i] = sum;
+    }
 }
 
 // 32 columns of all blocks' sums: 32 threads a column, each its blocks in

@@ -36,15 +36,16 @@ struct NormArgs {
     float eps;
 };
 
-// The sums of two values over a row's threads; `row_warps` warps each, all of the block's threads call it.
-__device__ __forceinline__ float2 row_sums(float2 v, int row_warps, float2 *sums) {
+// The sums of two values over a row's threads (part of a warp, or whole warps); all of the block's threads call it.
+__device__ __forceinline__ float2 row_sums(float2 v, int row_threads, float2 *sums) {
 #pragma unroll
     for (int i = 16; i > 0; i /= 2) {
+        if (i >= row_threads) continue;
         v.x += __shfl_xor_sync(kFull, v.x, i);
         v.y += __shfl_xor_sync(kFull, v.y, i);
     }
-    if (row_warps == 1) return v;
-    const int warp = threadIdx.x / 32, first = warp / row_warps * row_warps;
+    if (row_threads <= 32) return v;
+    const int row_warps = row_threads / 32, warp = threadIdx.x / 32, first = warp / row_warps * row_warps;
     if ((threadIdx.x & 31) == 0) sums[warp] = v;
     __syncthreads();
     v = make_float2(0.f, 0.f);
@@ -68,9 +69,9 @@ __device__ __forceinline__ void load_row(Bits<E, N> (&r)[P], const void *data, i
 
 // Each row's threads load the next row while they work on one.
 template <typename E, int N, int P, int MOST>
-__global__ void __launch_bounds__(MOST) add_norm_kernel(const __grid_constant__ NormArgs a, int row_warps) {
+__global__ void __launch_bounds__(MOST) add_norm_kernel(const __grid_constant__ NormArgs a, int row_threads) {
     __shared__ float2 sums[32];
-    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = MOST / row_threads;
+    const int in = threadIdx.x % row_threads, rows = MOST / row_threads;
     const int64_t step = (int64_t)gridDim.x * rows;
     int64_t t = (int64_t)blockIdx.x * rows + threadIdx.x / row_threads;
     Bits<E, N> w[P], x[P], delta[P];
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(MOST) add_norm_kernel(const __grid_constant__ 
         }
         load_row(x, a.x, a.xs, t + step, t + step < a.T, in, row_threads, a.d);
         if (a.delta) load_row(delta, a.delta, a.deltas, t + step, t + step < a.T, in, row_threads, a.d);
-        sum = row_sums(make_float2(sum, 0.f), row_warps, sums).x;
+        sum = row_sums(make_float2(sum, 0.f), row_threads, sums).x;
         const float r = rsqrtf(sum / a.d + a.eps);
         E *s = static_cast<E *>(a.s) + t * a.ss, *y = static_cast<E *>(a.y) + t * a.ys;
 #pragma unroll
@@ -180,11 +181,11 @@ struct GradRows {
 
 template <typename E, int N, int P, int MOST>
 __global__ void __launch_bounds__(MOST, N > 1 && MOST == 256 ? 2 : 1)
-    add_norm_grad_kernel(const __grid_constant__ NormArgs a, int row_warps) {
+    add_norm_grad_kernel(const __grid_constant__ NormArgs a, int row_threads) {
     __shared__ float2 sums[32];
     extern __shared__ __align__(16) uint8_t mem[];
     tc::start_next();
-    const int row_threads = 32 * row_warps, in = threadIdx.x % row_threads, rows = MOST / row_threads;
+    const int in = threadIdx.x % row_threads, rows = MOST / row_threads;
     const int64_t step = (int64_t)gridDim.x * rows;
     int64_t t = (int64_t)blockIdx.x * rows + threadIdx.x / row_threads;
     float dw[P][N];
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(MOST, N > 1 && MOST == 256 ? 2 : 1)
                 us = fmaf(a.w ? g.v[j] * k.v[j] : g.v[j], v.v[j], us);
             }
         }
-        const float2 both = row_sums(make_float2(sq, us), row_warps, sums);
+        const float2 both = row_sums(make_float2(sq, us), row_threads, sums);
         const float r = rsqrtf(both.x / a.d + a.eps), less = r * r * r * (both.y / a.d);
         E *dx = static_cast<E *>(a.dx) + t * a.dxs;
 #pragma unroll
@@ -291,39 +292,44 @@ int resident_blocks(const void *kernel, int threads, size_t smem) {
 
 // Threads that share a row, and the pieces of each of them: a warp where its
 // lanes can hold the row (4 pieces of 16 bytes each, 16 of one value), then up
-// to 8 warps, and 32 for the widest rows.
+// to 8 warps, and 32 for the widest rows. Of short rows a warp has several, as one
+// would leave most lanes idle (1000000 x 64 bf16: 84 us and 82 for the gradient, 212
+// and 295 with a warp a row).
 struct RowShape {
-    int warps, pieces;
+    int threads, pieces;
     RowShape(int row_pieces, int most) {
-        warps = 1;
+        int warps = 1;
         while (32 * warps * most < row_pieces) warps = warps < 8 ? 2 * warps : 32;
         const int each = (row_pieces + 32 * warps - 1) / (32 * warps);
         pieces = each;
         if (most > 4)  // of one value: 1, 2, 4, 8 or 16
             for (pieces = 1; pieces < each;) pieces *= 2;
+        threads = 32 * warps;
+        if (pieces == 1)
+            for (threads = 4; threads < row_pieces && threads < 32;) threads *= 2;
     }
 };
 
 template <typename E, int N, int P, int MOST>
 dpb_status launch_grad(NormArgs &a, const RowShape &r, cudaStream_t s) {
-    const int rows = MOST / (32 * r.warps);
+    const int rows = MOST / r.threads;
     constexpr size_t kSmem = std::max(GradRows<E, N, P, MOST>::kBytes, (size_t)MOST * P * N * 4);
     const void *kernel = reinterpret_cast<const void *>(add_norm_grad_kernel<E, N, P, MOST>);
     const cudaError_t e = allow_smem(kernel, kSmem);
     if (e != cudaSuccess) return launch_status(e, "add_norm_backward");
     static const int resident = resident_blocks(kernel, MOST, kSmem);
     a.blocks = (int)std::min<int64_t>((a.T + rows - 1) / rows, (int64_t)std::min(resident, kGradBlocks) * sms_of_device());
-    add_norm_grad_kernel<E, N, P, MOST><<<a.blocks, MOST, kSmem, s>>>(a, r.warps);
+    add_norm_grad_kernel<E, N, P, MOST><<<a.blocks, MOST, kSmem, s>>>(a, r.threads);
     return launch_status(cudaGetLastError(), "add_norm_backward");
 }
 
 template <typename E, int N, int P, int MOST>
 dpb_status launch(NormArgs &a, const RowShape &r, bool grad, cudaStream_t s) {
-    const int rows = MOST / (32 * r.warps);
+    const int rows = MOST / r.threads;
     if (!grad) {
         static const int resident = resident_blocks(reinterpret_cast<const void *>(add_norm_kernel<E, N, P, MOST>), MOST, 0);
         const int64_t blocks = std::min<int64_t>((a.T + rows - 1) / rows, (int64_t)resident * sms_of_device());
-        add_norm_kernel<E, N, P, MOST><<<(unsigned)blocks, MOST, 0, s>>>(a, r.warps);
+        add_norm_kernel<E, N, P, MOST><<<(unsigned)blocks, MOST, 0, s>>>(a, r.threads);
         return launch_status(cudaGetLastError(), "add_norm");
     }
     return launch_grad<E, N, P, MOST>(a, r, s);
@@ -332,7 +338,7 @@ dpb_status launch(NormArgs &a, const RowShape &r, bool grad, cudaStream_t s) {
 template <typename E, int N>
 dpb_status dispatch(NormArgs &a, bool grad, cudaStream_t s) {
     const RowShape r((a.d + N - 1) / N, N == 1 ? 16 : 4);
-    if (r.warps > 8) {  // 2 or more pieces: what 8 warps cannot hold
+    if (r.threads > 256) {  // 2 or more pieces: what 8 warps cannot hold
         if constexpr (N == 8) return launch<E, N, 2, 1024>(a, r, grad, s);
         if constexpr (N == 4) return r.pieces <= 2 ? launch<E, N, 2, 1024>(a, r, grad, s) : launch<E, N, 4, 1024>(a, r, grad, s);
         if constexpr (N == 1) return r.pieces <= 8 ? launch<E, N, 8, 1024>(a, r, grad, s) : launch<E, N, 16, 1024>(a, r, grad, s);

@@ -62,7 +62,8 @@ def check_gradient(dx, dw, total, w, dy, dtotal, eps=EPS):
 
 
 SIZES = [(1, 1), (1, 8), (5, 7), (128, 64), (33, 100), (300, 768), (65, 1000), (7, 1032), (40, 1025), (9, 2048), (12, 2050),
-         (3, 4100), (5, 4096), (4, 8200), (3, 8192), (2, 16384), (2, 16383), (5000, 24), (20000, 520)]
+         (3, 4100), (5, 4096), (4, 8200), (3, 8192), (2, 16384), (2, 16383), (5000, 24), (20000, 520), (70003, 64), (1001, 40),
+         (2777, 16), (99991, 8), (333, 4), (4099, 3), (1234, 128), (3001, 256)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])

@@ -99,14 +99,16 @@ struct Args {
     float *z_target;
     float *loss, *lse;
     int *counted;
-    CUtensorMap sums;
+    CUtensorMap sums, w_sums;
     float *acc;  // sums of dH, where there are several pieces: [rows][dim], or (split) one for each piece, of T_pad rows
-    bf16 *dh;
-    int64_t dh_stride;
+    float *w_acc;  // sums of dW over parts of the tokens, where these are several: [parts][V_pad][dim]
+    bf16 *dh, *dw_rows;
+    int64_t dh_stride, dw_stride;
     int64_t T, T_pad;
     int V, d, piece;  // piece: words of a piece
     int pieces, held;
-    bool split;  // each piece's sums of dH apart, added up by join_hidden_kernel
+    int parts, part_rows, V_pad;  // parts of the tokens that dW is summed over apart, and the rows of each
+    bool split;  // each piece's sums of dH apart, added up by join_sums_kernel
     bool fine;   // dz as two bf16, the rounded value and the remainder
     bool want_h, want_w;
     bool few;  // rows that the tokens' cluster closes up itself
@@ -115,7 +117,7 @@ struct Args {
 
 struct Unit {
     int kind, m0, n0, blocks;  // blocks: of 64 along K
-    int piece;
+    int piece, part;  // part: of the tokens (kDWeight)
 };
 
 // ---- units ------------------------------------------------------------------------
@@ -125,7 +127,7 @@ struct Unit {
 __device__ __forceinline__ Unit score_unit(int kind, int u, int tiles_m, int tiles_n, int d, int piece) {
     const int group = u / (kGroup * tiles_n), in = u - group * kGroup * tiles_n;
     const int rows = min(kGroup, tiles_m - group * kGroup);
-    return Unit{kind, (group * kGroup + in % rows) * kTile, in / rows * kTile, (d + 63) / 64, piece};
+    return Unit{kind, (group * kGroup + in % rows) * kTile, in / rows * kTile, (d + 63) / 64, piece, 0};
 }
 
 // How many units each product has, and which is the u-th. The gradient's
@@ -145,21 +147,24 @@ struct List {
     __device__ __forceinline__ int words_of(const Args &a, int piece) const { return piece == a.pieces - 1 ? last : words; }
     __device__ __forceinline__ int grad_units(int w) const { return tiles_m * ((w + kTile - 1) / kTile); }
     __device__ __forceinline__ int weight_units(const Args &a, int w) const {
-        return a.want_w ? (w + kTile - 1) / kTile * tiles_d : 0;
+        return a.want_w ? (w + kTile - 1) / kTile * tiles_d * a.parts : 0;
     }
     __device__ __forceinline__ int hidden_units(const Args &a) const { return a.want_h ? tiles_m * tiles_d : 0; }
     __device__ __forceinline__ Unit reader(const Args &a, int u, int piece) const {
         const int w = words_of(a, piece), n_w = weight_units(a, w), n_h = hidden_units(a);
-        const bool h_first = piece < a.pieces - 1 || w > count;
-        if (u >= n_w + n_h) return Unit{kEnd, 0, 0, 0, 0};
+        const int rows = a.parts > 1 ? a.part_rows : count;  // that a unit of dW sums over
+        const bool h_first = piece < a.pieces - 1 || w > rows;
+        if (u >= n_w + n_h) return Unit{kEnd, 0, 0, 0, 0, 0};
         const bool is_h = h_first ? u < n_h : u >= n_w;
         u -= is_h && !h_first ? n_w : !is_h && h_first ? n_h : 0;
-        const int blocks = ((is_h ? w : count) + 63) / 64;
-        return Unit{is_h ? kDHidden : kDWeight, u / tiles_d * kTile, u % tiles_d * kTile, a.fine ? 2 * blocks : blocks, piece};
+        const int each = is_h ? n_h : n_w / a.parts, part = is_h ? 0 : u / each;
+        u -= part * each;
+        const int blocks = ((is_h ? w : max(0, min(rows, count - part * rows))) + 63) / 64;
+        return Unit{is_h ? kDHidden : kDWeight, u / tiles_d * kTile, u % tiles_d * kTile, a.fine ? 2 * blocks : blocks, piece, part};
     }
     __device__ __forceinline__ Unit at(const Args &a, int u) const {
         const int all = a.pieces, first = grad_units(words_of(a, 0));
-        if (a.loss) return u < first ? score_unit(kScores, u, tiles_m, (a.V + kTile - 1) / kTile, a.d, 0) : Unit{kEnd, 0, 0, 0, 0};
+        if (a.loss) return u < first ? score_unit(kScores, u, tiles_m, (a.V + kTile - 1) / kTile, a.d, 0) : Unit{kEnd, 0, 0, 0, 0, 0};
         int piece = 0;
         if (a.held == all) {
             const int dz = grad_units(words), total = dz * (all - 1) + grad_units(last);
@@ -209,7 +214,7 @@ struct List {
             if (all_there && !ordered) return true;
             const bool one = a.held == a.pieces;
             const int dz = one ? grad_units(words) * (a.pieces - 1) + grad_units(last) : grad_units(words_of(a, t.piece));
-            if ((!all_there && !reached(counter(a, Unit{kGrad, 0, 0, 0, t.piece}), each * dz)) ||
+            if ((!all_there && !reached(counter(a, Unit{kGrad, 0, 0, 0, t.piece, 0}), each * dz)) ||
                 (ordered && !reached(&a.head->done[t.piece - 1][kDHidden], each * hidden_units(a))))
                 return false;
             all_there = one;
@@ -268,7 +273,7 @@ struct Units {
                      : "=r"(x), "=r"(t.m0), "=r"(t.n0), "=r"(t.blocks)
                      : "r"(base + Shared::kUnits + 16 * s)
                      : "memory");
-        t.kind = x & 7, t.piece = x >> 3;
+        t.kind = x & 7, t.piece = x >> 3 & 0xff, t.part = x >> 11;
         ++i;
         return true;
     }
@@ -276,7 +281,7 @@ struct Units {
     __device__ __forceinline__ void hand(const Unit &t, int s, uint32_t rank) const {
         const uint32_t bar = peer_addr(base + Shared::kHanded + 8 * s, rank);
         bar_arrive_expect_peer(bar, 16);
-        store_peer(peer_addr(base + Shared::kUnits + 16 * s, rank), t.kind | t.piece << 3, t.m0, t.n0, t.blocks, bar);
+        store_peer(peer_addr(base + Shared::kUnits + 16 * s, rank), t.kind | t.piece << 3 | t.part << 11, t.m0, t.n0, t.blocks, bar);
     }
     // One thread: the unit has been read.
     __device__ __forceinline__ void done() const { bar_arrive_peer(taken + 8 * ((i - 1) % kAhead)); }
@@ -510,7 +515,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     const uint32_t bar = peer_addr(full(s), 0), to = base + s * kStageBytes;
                     if (rank == 0) bar_arrive_expect(full(s), 2 * kStageBytes);
                     const int m = t.m0 + 128 * rank, n = t.n0 + 128 * rank;
-                    const int kk = 64 * (k < first ? k : k - first), rest = k < first ? 0 : (int)a.T_pad;
+                    const int kk = t.part * a.part_rows + 64 * (k < first ? k : k - first), rest = k < first ? 0 : (int)a.T_pad;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const uint32_t ta = to + 8192 * j, tb = ta + 16384;
@@ -687,7 +692,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                         if (lane == 0) store_box(&a.dz_out, stage, at + c, row0 + part * (int)a.T_pad);
                         if (c == 0 && part == 0) settle(later);
                     }
-            } else if (t.kind == kDWeight) {
+            } else if (t.kind == kDWeight && a.parts == 1) {
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 64) {
                     if (lane == 0) stores_read();
@@ -718,16 +723,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 }
             } else {
                 // by way of shared memory: copies add the sums of a piece to those of the
-                // pieces before; in the last one eight lanes have 128 bytes of a row
-                const bool first = t.piece == 0 || a.split, last = t.piece == a.pieces - 1 && !a.split;
-                const int to = row0 + (a.split ? t.piece * (int)a.T_pad : 0);
+                // pieces before; in the last one eight lanes have 128 bytes of a row. The sums
+                // of dW over a part of the tokens are all stored apart.
+                const bool of_w = t.kind == kDWeight;
+                const bool first = t.piece == 0 || a.split || of_w, last = t.piece == a.pieces - 1 && !a.split && !of_w;
+                const int to = row0 + (of_w ? t.part * a.V_pad + t.piece * a.piece : a.split ? t.piece * (int)a.T_pad : 0);
+                const CUtensorMap *out = of_w ? &a.w_sums : &a.sums;
                 const int r = lane / 8, piece = lane % 8;
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 32) {
                     uint32_t v[32];
                     __syncwarp();
-                    tmem_load(from + c, v);
-                    load_wait(v);
+                    if (t.blocks > 0) {
+                        tmem_load(from + c, v);
+                        load_wait(v);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0;
+                    }
                     if (lane == 0) stores_read();
                     __syncwarp();
 #pragma unroll
@@ -736,8 +749,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     if (!last) {
                         fence_async_shared();
                         __syncwarp();
-                        if (lane == 0 && first) store_box(&a.sums, stage, column + c, to);
-                        if (lane == 0 && !first) add_box(&a.sums, stage, column + c, to);
+                        if (lane == 0 && first) store_box(out, stage, column + c, to);
+                        if (lane == 0 && !first) add_box(out, stage, column + c, to);
                         continue;
                     }
                     const int col = column + c + 4 * piece;
@@ -922,26 +935,48 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args
     }
 }
 
-// dH of a token from the pieces' sums, in their order: four columns a thread.
-__global__ void __launch_bounds__(256) join_hidden_kernel(const __grid_constant__ Args a) {
+// dH from the pieces' sums, where they are apart, and dW from the parts': four
+// columns a lane. Where there are few, `slices` warps share an output's sums, each
+// its own in order, and then the warps' are added up (33 tokens of 50257 words, 51
+// pieces: 5 us in place of 19; 1000 tokens, 13 pieces: 18 with one warp, 24 with eight).
+constexpr int kJoinWarps = 8;
+__global__ void __launch_bounds__(32 * kJoinWarps) join_sums_kernel(const __grid_constant__ Args a, int slices) {
+    __shared__ float4 sums[kJoinWarps][32];
     wait_previous();
-    const int each = a.d / 4, count = a.head->count;
+    const int each = a.d / 4, lane = threadIdx.x & 31, warp = threadIdx.x / 32, slice = warp % slices;
     const float g = a.head->g_max;
-    const int64_t step = a.T_pad * a.d, all = (int64_t)count * each;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
-        const int row = (int)(i / each), column = (int)(i - (int64_t)row * each) * 4;
-        const float *from = a.acc + (int64_t)row * a.d + column;
+    const int64_t rows_h = a.split && a.want_h ? a.head->count : 0, rows_w = a.parts > 1 && a.want_w ? a.V : 0;
+    const int64_t all = (rows_h + rows_w) * each;
+    const int outputs = 32 * kJoinWarps / slices;
+    for (int64_t i0 = blockIdx.x * (int64_t)outputs; i0 < all; i0 += gridDim.x * (int64_t)outputs) {
+        const int64_t at = i0 + warp / slices * 32 + lane, i = min(at, all - 1), row = i / each;
+        const int column = (int)(i - row * each) * 4;
+        const bool h = row < rows_h;
+        const int n = h ? a.pieces : a.parts, p1 = n * (slice + 1) / slices;
+        const int64_t step = (h ? a.T_pad : a.V_pad) * a.d;
+        const float *from = h ? a.acc + row * a.d + column : a.w_acc + (row - rows_h) * a.d + column;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int p = 0; p < a.pieces; p += 8) {
+        for (int p = n * slice / slices; p < p1; p += 8) {
             float4 x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = __ldcg(reinterpret_cast<const float4 *>(from + min(p + j, a.pieces - 1) * step));
+            for (int j = 0; j < 8; ++j) x[j] = __ldcg(reinterpret_cast<const float4 *>(from + min(p + j, p1 - 1) * step));
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (p + j < a.pieces) sum.x += x[j].x, sum.y += x[j].y, sum.z += x[j].z, sum.w += x[j].w;
+                if (p + j < p1) sum.x += x[j].x, sum.y += x[j].y, sum.z += x[j].z, sum.w += x[j].w;
         }
-        *reinterpret_cast<uint2 *>(a.dh + a.tokens[row].row * a.dh_stride + column) =
-            make_uint2(pack_bf16(sum.x * g, sum.y * g), pack_bf16(sum.z * g, sum.w * g));
+        if (slices > 1) {
+            sums[warp][lane] = sum;
+            __syncthreads();
+            if (slice == 0)
+                for (int k = 1; k < slices; ++k) {
+                    const float4 x = sums[warp + k][lane];
+                    sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+                }
+            __syncthreads();
+        }
+        if (slice == 0 && at < all)
+            *reinterpret_cast<uint2 *>((h ? a.dh + a.tokens[row].row * a.dh_stride : a.dw_rows + (row - rows_h) * a.dw_stride) + column) =
+                make_uint2(pack_bf16(sum.x * g, sum.y * g), pack_bf16(sum.z * g, sum.w * g));
     }
 }
 
@@ -985,21 +1020,27 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // more than that, all of it is held, and the pieces are as many as give every pair
 // of blocks two units of dH, whose sums are kept apart: one after the other few
 // units would follow each other through the whole vocabulary (1000 tokens, 50257
-// words, 768 columns: 300 us, 212 apart; 2000: 342 and 345; 4096, too many for it,
+// words, 768 columns: 300 us, 207 apart; 2000: 342 and 350; 4096, too many for it,
 // 560). With the fewest tokens, whose rounding errors of dz do not average out, dz
-// is held to 16 bits, in two bf16: 33 tokens take 135 us, 512 195 (268 and 282 in
+// is held to 16 bits, in two bf16: 33 tokens take 117 us, 512 195 (268 and 282 in
 // one bf16 and one after the other).
 constexpr int64_t kPieceBytes = 64ll << 20;
 constexpr int kLeastPiece = 4096, kFineRows = 512;
+// Where dW, of few words and columns, has fewer units than there are pairs of
+// blocks, they are of parts of the tokens, this many at least, whose sums are added
+// up in the end: 65536 tokens, 1000 words, 256 columns take 174 us for the gradient,
+// 390 with one unit for all tokens; 16384, 100, 64 40 and 93; 4096, 1000, 768 63 and
+// 75 (parts of 4096: 174, 46, 77; of 1024 and two units a pair: 194, 42, 64).
+constexpr int kLeastPart = 2048;
 
 struct Space {
-    int64_t T_pad, piece, pieces, held;
+    int64_t T_pad, V_pad, piece, pieces, held, parts = 1, part_rows = 0;
     bool split = false, fine = false;
-    size_t head, tokens, place, closed, part, z_target, dz, acc, bytes;
+    size_t head, tokens, place, closed, part, z_target, dz, acc, w_acc, bytes;
     Space(const dpb_linear_loss_config *c, bool backward) {
         const size_t T = (size_t)c->tokens, d = (size_t)c->dim, V = (size_t)c->vocab;
         const int64_t words = round_up(c->vocab, kTile);
-        T_pad = round_up(c->tokens, kTile);
+        T_pad = round_up(c->tokens, kTile), V_pad = words;
         fine = T_pad <= kFineRows && 4 * T_pad * words <= kBuffers * kPieceBytes;
         if (2 * T_pad * words <= kBuffers * kPieceBytes) {
             const int64_t tiles = std::max<int64_t>(1, T_pad / kTile) * ((c->dim + kTile - 1) / kTile);
@@ -1014,6 +1055,12 @@ struct Space {
             pieces = (c->vocab + piece - 1) / piece;
             held = std::min<int64_t>(pieces, kBuffers);
         }
+        const int64_t w_units = words / kTile * ((c->dim + kTile - 1) / kTile), pairs = sms_of_device() / 2;
+        if (held == pieces && w_units < pairs && T_pad >= 2 * kLeastPart) {
+            parts = std::min((pairs + w_units - 1) / w_units, T_pad / kLeastPart);
+            part_rows = round_up((c->tokens + parts - 1) / parts, kTile);
+            parts = (c->tokens + part_rows - 1) / part_rows;
+        }
         size_t at = 1024;  // the status word's
         auto take = [&](size_t n) {
             const size_t r = at;
@@ -1027,11 +1074,12 @@ struct Space {
         if (backward) {
             dz = take((size_t)T_pad * (fine ? 2 : 1) * held * piece * 2);
             acc = take(split ? (size_t)pieces * T_pad * d * 4 : pieces > 1 ? T * d * 4 : 0);
+            w_acc = take(parts > 1 ? (size_t)parts * V_pad * d * 4 : 0);
             part = z_target = at;
         } else {
             part = take((V + kTile - 1) / kTile * (size_t)T_pad * sizeof(float2));
             z_target = take((size_t)T_pad * 4);
-            dz = acc = at;
+            dz = acc = w_acc = at;
         }
         bytes = at;
     }
@@ -1043,7 +1091,8 @@ constexpr int64_t kMostTokens = 1ll << 24, kMostWords = 1ll << 28, kMostUnits = 
 int64_t units_of(const dpb_linear_loss_config *c) {
     const int64_t m = (c->tokens + kTile - 1) / kTile, v = ((int64_t)c->vocab + kTile - 1) / kTile;
     const int64_t d = ((int64_t)c->dim + kTile - 1) / kTile;
-    return m * v + v * d + m * d * Space(c, true).pieces;
+    const Space w(c, true);
+    return m * v + v * d * w.parts + m * d * w.pieces;
 }
 
 dpb_status check_config(const dpb_linear_loss_config *c) {
@@ -1093,6 +1142,9 @@ dpb_status begin(Args &a, const Space &w, const dpb_linear_loss_config *c, const
     a.piece = (int)w.piece;
     a.pieces = (int)w.pieces;
     a.held = (int)w.held;
+    a.parts = (int)w.parts;
+    a.part_rows = (int)w.part_rows;
+    a.V_pad = (int)w.V_pad;
     a.split = w.split;
     a.fine = w.fine;
     // A launch less where eight blocks close the rows up as fast: half of 340 x 768 ignored 16.8 us (17.3 with the
@@ -1184,19 +1236,27 @@ dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, 
     a.want_h = grad_hidden != nullptr;
     a.want_w = grad_weight != nullptr;
     if (grad_hidden) a.dh = static_cast<bf16 *>(grad_hidden->data), a.dh_stride = grad_hidden->stride;
+    if (grad_weight) a.dw_rows = static_cast<bf16 *>(grad_weight->data), a.dw_stride = grad_weight->stride;
     if (grad_weight) DPB_CHECK(make_map(&a.dw, grad_weight->data, grad_weight->stride, cfg->vocab, cfg->dim, 32));
     a.acc = reinterpret_cast<float *>(ws + w.acc);
     if (w.pieces > 1)
         DPB_CHECK(make_map(&a.sums, a.acc, cfg->dim, w.split ? w.pieces * w.T_pad : cfg->tokens, cfg->dim, 32, true));
+    a.w_acc = reinterpret_cast<float *>(ws + w.w_acc);
+    if (w.parts > 1) DPB_CHECK(make_map(&a.w_sums, a.w_acc, cfg->dim, w.parts * w.V_pad, cfg->dim, 32, true));
     const int64_t columns = w.held * w.piece, rows = w.T_pad * (w.fine ? 2 : 1);
     DPB_CHECK(make_map(&a.dz, ws + w.dz, columns, rows, columns, 64));
     DPB_CHECK(make_map(&a.dz_out, ws + w.dz, columns, rows, columns, 32));
     DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, grad_loss, lse, ws, s));
     const int64_t tiles_m = w.T_pad / kTile, tiles_v = (cfg->vocab + kTile - 1) / kTile, tiles_d = (cfg->dim + kTile - 1) / kTile;
-    DPB_CHECK(launch_products(a, tiles_m * tiles_v + tiles_v * tiles_d, s));
-    if (!w.split || !grad_hidden) return DPB_OK;
-    const unsigned blocks = (unsigned)std::min<int64_t>((cfg->tokens * (cfg->dim / 4) + 255) / 256, 4 * sms_of_device());
-    return launch_status(launch_early(join_hidden_kernel, dim3(blocks), 256, 0, s, a), "linear_cross_entropy_backward (sums)");
+    DPB_CHECK(launch_products(a, tiles_m * tiles_v + tiles_v * tiles_d * w.parts, s));
+    const int64_t apart = (w.split && grad_hidden ? cfg->tokens : 0) + (w.parts > 1 && grad_weight ? cfg->vocab : 0);
+    if (apart == 0) return DPB_OK;
+    // as for both gradients, so that one alone has the same bits
+    const int64_t outputs = apart * (cfg->dim / 4), both = ((w.split ? cfg->tokens : 0) + (w.parts > 1 ? cfg->vocab : 0)) * (cfg->dim / 4);
+    int slices = 1;
+    while (slices < kJoinWarps && both * 2 * slices <= (1 << 18)) slices *= 2;
+    const unsigned blocks = (unsigned)std::min<int64_t>((outputs * slices + 32 * kJoinWarps - 1) / (32 * kJoinWarps), 8 * sms_of_device());
+    return launch_status(launch_early(join_sums_kernel, dim3(blocks), 32 * kJoinWarps, 0, s, a, slices), "linear_cross_entropy_backward (sums)");
 }
 
 }  // extern "C"

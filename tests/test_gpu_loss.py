@@ -88,6 +88,7 @@ SIZES = [  # tokens, vocabulary, columns
     (64, 9001, 2048), (1, 20000, 1000),
     (8449, 9001, 72), (2000, 30011, 264), (12289, 4355, 128),  # pieces of the vocabulary, their sums apart
     (24001, 5003, 136), (20001, 9001, 72), (7001, 17001, 72),  # and one after the other: two, three, four pieces
+    (20001, 300, 264), (65537, 700, 72), (4097, 97, 520), (9000, 5000, 64),  # the weight's sums of parts of the tokens apart
 ]
 
 
@@ -275,7 +276,7 @@ def test_gradient_against_differences():
         assert abs(got - want) <= tol, (got, want, tol)
 
 
-@pytest.mark.parametrize("T,V,d", [(300, 5000, 520), (9000, 5000, 264), (24001, 5003, 72)])
+@pytest.mark.parametrize("T,V,d", [(300, 5000, 520), (9000, 5000, 264), (24001, 5003, 72), (30000, 600, 136)])
 def test_equal_inputs_give_equal_bits(T, V, d):
     h, w, y, gl = draw(T, V, d, left_out="some", even=False)
     first = None
@@ -291,7 +292,7 @@ def test_scratch_may_hold_anything():
     n = 1 << 30
     ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
     ws[:4] = 0
-    for T, V, d, left in ((24001, 5003, 72, "runs"), (8449, 5001, 72, "some"), (300, 1000, 64, "none"), (64, 257, 200, "runs")):
+    for T, V, d, left in ((24001, 5003, 72, "runs"), (8449, 5001, 72, "some"), (300, 1000, 64, "none"), (30000, 600, 136, "some"), (64, 257, 200, "runs")):
         h, w, y, gl = draw(T, V, d, left_out=left, even=False)
         loss, lse = dpb.linear_cross_entropy_forward(h, w, y, workspace=ws)
         dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl, workspace=ws)

@@ -133,8 +133,9 @@ def test_small_losses_keep_their_digits():
     check(loss, want, 2.0 ** -21 * want + 2.0 ** -19.9)
 
 
-def test_all_ignored():
-    h, w, y, gl = draw(300, 700, 64, left_out="all")
+@pytest.mark.parametrize("T,V", [(300, 700), (9000, 700), (24001, 5003)])
+def test_all_ignored(T, V):
+    h, w, y, gl = draw(T, V, 64, left_out="all")
     loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
     dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
     for t in (loss, lse, dh, dw):
@@ -208,7 +209,7 @@ def test_strides_and_what_lies_between_is_left_alone():
         assert (t[:, :a] == 3).all() and (t[:, b:] == 3).all()
 
 
-@pytest.mark.parametrize("T,V", [(300, 700), (9000, 4500), (24001, 5003)])
+@pytest.mark.parametrize("T,V", [(300, 700), (9000, 4500), (24001, 5003), (12000, 700)])
 def test_one_gradient_alone(T, V):
     h, w, y, gl = draw(T, V, 64)
     _, lse = dpb.linear_cross_entropy_forward(h, w, y)

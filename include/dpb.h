@@ -588,7 +588,9 @@ dpb_status dpb_embedding_workspace_size(const dpb_embedding_config *cfg, size_t 
  * delta: nullable (total = x). weight: [dim], nullable (ones). total: nullable
  * (not written). y and total may be x or delta themselves (same strides). Rows
  * may have any alignment their type allows and any stride of at least dim; those
- * that start at multiples of 16 bytes are faster. Sums are fp32.
+ * that start at multiples of 16 bytes are faster. Sums are fp32: of a row whose
+ * sum of squares leaves its range (beyond 3.4e38; at eps = 0 below 1.2e-38) y is
+ * what an infinite sum or one without its digits gives, here and in the gradient.
  */
 typedef struct dpb_norm_config {
     int64_t tokens;

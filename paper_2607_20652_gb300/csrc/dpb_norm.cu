@@ -2,7 +2,7 @@
 // gradient.
 //
 //   s = x + delta (rounded to the rows' type),  y = w s r,  r = (mean s^2 + eps)^(-1/2)
-//   u = w dy,  dx = ds + r u - s r^3 mean(u s),  dw = sum_t dy s r
+//   u = w dy,  h = s r,  dx = ds + r (u - h mean(u h)),  dw = sum_t dy h
 //
 // Memory bounds both: a row is read once and kept until its sum is known, and the
 // next row is loaded meanwhile (65536 x 768 bf16: 64 us, 6.3 TB/s; 111 without). A
@@ -215,7 +215,8 @@ __global__ void __launch_bounds__(MOST, N > 1 && MOST == 256 ? 2 : 1)
             }
         }
         const float2 both = row_sums(make_float2(sq, us), row_threads, sums);
-        const float r = rsqrtf(both.x / a.d + a.eps), less = r * r * r * (both.y / a.d);
+        // with h = total r: factors of the result's own size, where r^3 leaves fp32 at rows beyond 1e14 or below 1e-13
+        const float r = rsqrtf(both.x / a.d + a.eps), along = r * (both.y / a.d);  // mean(u h)
         E *dx = static_cast<E *>(a.dx) + t * a.dxs;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -226,8 +227,9 @@ __global__ void __launch_bounds__(MOST, N > 1 && MOST == 256 ? 2 : 1)
             if (a.ds) rest = row.get(2, p);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                dw[p][j] = fmaf(g.v[j] * r, v.v[j], dw[p][j]);
-                v.v[j] = fmaf(-less, v.v[j], fmaf(r, a.w ? g.v[j] * k.v[j] : g.v[j], a.ds ? rest.v[j] : 0.f));
+                const float h = v.v[j] * r;
+                dw[p][j] = fmaf(g.v[j], h, dw[p][j]);
+                v.v[j] = fmaf(r, fmaf(-along, h, a.w ? g.v[j] * k.v[j] : g.v[j]), a.ds ? rest.v[j] : 0.f);
             }
             store_piece(dx + i, v);
         }

@@ -210,3 +210,26 @@ def test_refusals():
     big = torch.zeros(2, 16385, device="cuda")
     with pytest.raises(dpb.DPBError):
         dpb.add_norm(big)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 50, 768, 4101])
+@pytest.mark.parametrize("rms,eps", [(1e14, EPS), (1e15, EPS), (1e17, EPS), (1e-13, 0.0), (1e-14, 0.0), (1e-17, 0.0)])
+def test_gradient_of_large_and_of_small_rows(rms, eps, d, dtype):
+    """r^3 leaves fp32 here, the gradient does not: sums of squares stay between 1e-33 and 5e37. The gradient that comes
+    leans along the row, so that its mean product with the row counts."""
+    x, _, w, dy, dt = draw(20, d, dtype, seed=d)
+    dy = (dy.double() + x.double()).to(dtype)
+    x = (x.double() * (rms / 2)).to(dtype)
+    check_gradient(*dpb.add_norm_backward(x, dy, None, w, eps), x, w, dy, None, eps)
+    dt = (dt.double() / rms).to(dtype)
+    check_gradient(*dpb.add_norm_backward(x, dy, dt, w, eps), x, w, dy, dt, eps)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradient_of_zeros_with_a_small_eps(dtype):
+    """r = 1e15 and more, r^3 beyond fp32: without a row only r u is left."""
+    x, _, w, dy, dt = draw(12, 64, dtype)
+    x[::3] = 0
+    for eps in (1e-26, 1e-30, 1e-36):
+        check_gradient(*dpb.add_norm_backward(x, dy, dt, w, eps), x, w, dy, dt, eps)

@@ -371,8 +371,8 @@ __global__ void __launch_bounds__(32 * kWarps, VEC == 4 ? kBlocks : 1) norm_rope
     }
 }
 
-// The gradient: g rotated back, u = w g; dx = r u - x r^3 mean(u x), and
-// g x r to the weight's.
+// The gradient: g rotated back, u = w g, n = x r; dx = r (u - n mean(u n)), and
+// g n to the weight's.
 template <typename T, int VEC, int UPL, bool MIX, int GL>
 __global__ void __launch_bounds__(32 * kWarps, VEC == 4 ? kBlocksGrad : 1) norm_rope_grad_kernel(
     const __grid_constant__ RopeArgs g) {
@@ -438,13 +438,15 @@ __global__ void __launch_bounds__(32 * kWarps, VEC == 4 ? kBlocksGrad : 1) norm_
                         const float x2 = group_sum<GL>(total(ss), gl), ux = group_sum<GL>(total(sp), gl);
                         // a lane group without a head adds 0 x r: r must not be infinite there, whatever eps
                         const float r = rsqrtf((h < in.n ? x2 : 1.f) * inv_d + g.eps);
-                        const Vals<VEC> r4 = all<VEC>(r), f4 = all<VEC>(-r * r * r * ux * inv_d);
+                        // r^3 by itself leaves fp32 at heads beyond 1e14, and without an eps below 1e-13
+                        const Vals<VEC> r4 = all<VEC>(r), less = all<VEC>(-r * (ux * inv_d));
 #pragma unroll
                         for (int j = 0; j < UPL; ++j) {
-                            da[s][j] = madd(ga[j] * xa[j], r4, da[s][j]);
-                            db[s][j] = madd(gb[j] * xb[j], r4, db[s][j]);
-                            ua[j] = madd(xa[j], f4, ua[j] * r4);
-                            ub[j] = madd(xb[j], f4, ub[j] * r4);
+                            const Vals<VEC> na = xa[j] * r4, nb = xb[j] * r4;
+                            da[s][j] = madd(ga[j], na, da[s][j]);
+                            db[s][j] = madd(gb[j], nb, db[s][j]);
+                            ua[j] = madd(na, less, ua[j]) * r4;
+                            ub[j] = madd(nb, less, ub[j]) * r4;
                         }
                     }
                     if (h < in.n) ln.store(os.at, ua, ub);

@@ -260,3 +260,25 @@ def test_unaligned_rows_element_by_element(rot, inter, dtype):
         u = 2 * gy[i].double().abs().amax(-1, keepdim=True) * wd.detach().abs().amax()
         close(outs[2 + i], gx, r * (u + n * (u * n).mean(-1, keepdim=True)), D, extra=2)
         close((dwq, dwk)[i], gw, (2 * gy[i].double().abs().amax(-1, keepdim=True) * n).sum((0, 1)), D, extra=T * H / D + 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,Hk,D", [(5, 2, 64), (3, 1, 128), (4, 4, 30)])
+@pytest.mark.parametrize("rms,eps", [(1e14, EPS), (1e15, EPS), (1e17, EPS), (1e-13, 0.0), (1e-14, 0.0), (1e-17, 0.0)])
+def test_gradient_of_large_and_of_small_heads(rms, eps, H, Hk, D, dtype):
+    """r^3 leaves fp32 here, the gradient does not: sums of squares stay between 1e-33 and 1e37. The gradient that comes
+    leans along the rotated head, so that its mean product with the head counts."""
+    T = 20
+    q, k, w, cos, sin, pos, gy = draw(T, H, Hk, D, D, dtype, seed=33)
+    gy = [(g.double() + formula(x.double(), None, cos, sin, pos, D, False)).to(dtype) for g, x in zip(gy, (q, k))]
+    q, k = ((x.double() * (rms / 2)).to(dtype) for x in (q, k))
+    dx = dpb.qk_norm_rope_backward(q, k, *gy, weight_q=w[0], weight_k=w[1], cos=cos, sin=sin, positions=pos, eps=eps)
+    for i, x in enumerate((q, k)):
+        xd, wd = x.double().requires_grad_(), w[i].double().requires_grad_()
+        r = torch.rsqrt((xd * xd).mean(-1, keepdim=True) + eps)
+        want = formula(xd * r * wd, None, cos, sin, pos, D, False, normalise=False)
+        gx, gw = torch.autograd.grad(want, (xd, wd), gy[i].double())
+        n, r = (xd * r).detach().abs(), r.detach()
+        u = 2 * gy[i].double().abs().amax(-1, keepdim=True) * wd.detach().abs().amax()
+        close(dx[i], gx, r * (u + n * (u * n).mean(-1, keepdim=True)), D, extra=2)
+        close(dx[2 + i], gw, (2 * gy[i].double().abs().amax(-1, keepdim=True) * n).sum((0, 1)), D, extra=T * (H, Hk)[i] / D + 2)

@@ -77,10 +77,10 @@ struct Head {
     // of each piece, the row warps that are done with a unit of each kind (kGrad, kDHidden, kDWeight)
     int done[kMostPieces][4];
 };
-// Of the i-th token that takes part: its target, lse log2 e, grad_loss / g_max.
+// Of the i-th token that takes part: its target, lse, grad_loss / g_max.
 struct Token {
     int target;
-    float lse2, g;
+    float lse, g;
     int row;
 };
 
@@ -353,12 +353,14 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 }
 
 // 64 columns of a row's dz as bf16 pairs, into the warp's rows on their way to
-// memory; or what their rounding left over. `taken` is called once they have been
-// read out of TMEM.
+// memory; or what their rounding left over. lse is subtracted before the scaling to
+// powers of 2, so that a row whose target is all of it gives 0 exactly: scaled by
+// itself it would be rounded once more, 4e-5 at a score of 1000. `taken` is called
+// once they have been read out of TMEM.
 template <typename F>
 __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int lane, int columns, const Token &t,
                                              int target, bool remainder, F &&taken) {
-    const uint64_t scale = pair(kLog2e, kLog2e), less = pair(-t.lse2, -t.lse2);
+    const uint64_t scale = pair(kLog2e, kLog2e), less = pair(-t.lse, -t.lse);
     uint32_t both[2][32];
     __syncwarp();
     tmem_load(tmem, both[0]);
@@ -372,7 +374,7 @@ __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int 
         float p[32];
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            const float2 x = unpair(fma2(pair_bits(v[i], v[i + 1]), scale, less));
+            const float2 x = unpair(mul2(add2(pair_bits(v[i], v[i + 1]), less), scale));
             p[i] = exp2_approx(x.x), p[i + 1] = exp2_approx(x.y);
         }
         if ((unsigned)(target - c) < 32u) {
@@ -897,7 +899,7 @@ __global__ void __cluster_dims__(kPrepareBlocks, 1, 1) __launch_bounds__(1024)
         if (t >= t1) continue;
         a.place[t] = in ? here : -1;
         if (in)
-            a.tokens[here] = Token{(int)y, lse ? lse[t] * kLog2e : 0.f, grad ? grad[t * grad_stride] / all.top : 0.f, (int)t};
+            a.tokens[here] = Token{(int)y, lse ? lse[t] : 0.f, grad ? grad[t * grad_stride] / all.top : 0.f, (int)t};
         else if (a.loss)
             a.loss[t] = a.lse[t] = 0.f;
     }

@@ -382,3 +382,39 @@ def test_refusals():
         dpb.linear_cross_entropy_backward(h, w, y, lse[:20], gl)
     with pytest.raises(dpb.DPBError):
         dpb.linear_cross_entropy_forward(h, w, y, workspace=torch.zeros(1024, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("T", [70, 700, 9000])
+@pytest.mark.parametrize("size", [1.0, 8.0, 64.0])
+def test_a_single_word_has_no_gradient(T, size):
+    """lse is the word's own score, the same sum in both directions, so exp(z - lse) - 1 is 0 exactly, however large z is."""
+    h, w, y, gl = draw(T, 1, 64, seed=T)
+    h = (h * size).to(BF)
+    _, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    assert lse.any() and not dh.any() and not dw.any()
+
+
+@pytest.mark.parametrize("T,V", [(300, 700), (3000, 5003), (9000, 13001)])
+def test_tokens_that_the_model_is_sure_of_have_no_gradient(T, V):
+    """Scores of up to 1000 whose target lies 110 above all others: exp(-110) is 0 in fp32, so lse is the target's score."""
+    d = 64
+    g = torch.Generator(device="cuda").manual_seed(T)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    y[::3] = 5  # the word of the sure rows below
+    h = torch.zeros(T, d, device="cuda")
+    h[:, 0] = torch.randint(1, 100, (T,), generator=g, device="cuda") * 9.0
+    h[::3, 1] = 110.0
+    w = torch.zeros(V, d, device="cuda")
+    w[:, 0] = 1.0
+    w[5, 1] = 1.0
+    h, w = h.to(BF), w.to(BF)
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    gl = torch.rand(T, generator=g, device="cuda") * 10
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    assert not loss[::3].any() and not dh[::3].any()
+    assert loss[1::3].all()
+    sure = torch.full_like(y, -100)
+    sure[::3] = 5
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, sure, lse, gl)
+    assert not dh.any() and not dw.any()

@@ -620,8 +620,8 @@ dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
  * dpb_linear_cross_entropy_forward -- cross entropy of the rows' scores over the
  * vocabulary, without a tensor of tokens x vocabulary:
  *   z_t = hidden_t weight^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_t,target
- *   tokens, vocab, dim   at most 2^24 tokens and 2^28 words; dim a multiple of 8;
- *               2^26 tiles of 256 x 256 in all products together
+ *   tokens, vocab, dim   at most 2^24 tokens, 2^28 words and 2^20 columns; dim a
+ *               multiple of 8; 2^26 tiles of 256 x 256 in all products together
  *   ignore_index  a token with this target has loss 0, lse 0 and no gradient, and its
  *               hidden row is not read (it may hold anything)
  *   index_bytes 4 or 8: targets are int32 or int64 [tokens]

@@ -1088,6 +1088,7 @@ struct Space {
 };
 
 constexpr int64_t kMostTokens = 1ll << 24, kMostWords = 1ll << 28, kMostUnits = 1ll << 26;
+constexpr int kMostDim = 1 << 20;
 
 // Units of the gradient, which has the forward's and more.
 int64_t units_of(const dpb_linear_loss_config *c) {
@@ -1101,9 +1102,10 @@ dpb_status check_config(const dpb_linear_loss_config *c) {
     if (!c) return fail(DPB_ERR_INVALID_ARG, "cfg is NULL");
     if (c->dtype != DPB_BF16) return fail(DPB_ERR_UNSUPPORTED, "the linear cross entropy takes bf16 rows");
     if (c->tokens < 0 || c->vocab < 1 || c->dim < 1) return fail(DPB_ERR_INVALID_ARG, "a size is too small");
-    // a unit's products, of all tokens or of a piece of the words, take far less than the bound of a wait for them
-    if (c->tokens > kMostTokens || c->vocab > kMostWords)
-        return fail(DPB_ERR_UNSUPPORTED, "at most 2^24 tokens and 2^28 words");
+    // A unit's products, of all tokens, of a piece of the words or of all columns, take far less than the bound of a
+    // wait for them: 2^24 tokens some 0.1 s and 2^20 columns 4 ms, where 2^20 polls of 1.5 us take 1.6 s.
+    if (c->tokens > kMostTokens || c->vocab > kMostWords || c->dim > kMostDim)
+        return fail(DPB_ERR_UNSUPPORTED, "at most 2^24 tokens, 2^28 words and 2^20 columns");
     if (units_of(c) > kMostUnits) return fail(DPB_ERR_UNSUPPORTED, "too many tokens for a vocabulary and rows this large");
     if (c->dim % 8) return fail(DPB_ERR_UNSUPPORTED, "dim must be a multiple of 8");
     if (c->index_bytes != 4 && c->index_bytes != 8) return fail(DPB_ERR_INVALID_ARG, "index_bytes must be 4 or 8");

@@ -178,3 +178,18 @@ def test_functions_want_cuda_tensors():
               lambda: dpb.linear_cross_entropy_backward(x, x, ids, x, x)):
         with pytest.raises((ValueError, RuntimeError, AssertionError)):
             f()
+
+
+@pytest.mark.parametrize("dim", [(1 << 20) + 8, 1 << 24, (1 << 31) - 1024, (1 << 31) - 8])
+def test_loss_refuses_rows_that_are_too_wide(lib, dim):
+    """A unit's products over such a row would outlast the waits for them, and the last of these sizes overflow its tiles."""
+    n = ctypes.c_size_t()
+    c, good = loss_config(tokens=1, vocab=1, dim=dim), rows(256, dim)
+    for backward in (0, 1):
+        assert lib.dpb_linear_cross_entropy_workspace_size(at(c), backward, n) == UNSUPPORTED
+    assert lib.dpb_linear_cross_entropy_forward(at(c), at(good), at(good), 256, 256, 256, None, 256, 1 << 62, None) == UNSUPPORTED
+    assert lib.dpb_linear_cross_entropy_backward(at(c), at(good), at(good), 256, 256, 256, at(good), at(good), 256, 1 << 62,
+                                                 None) == UNSUPPORTED
+    assert b"columns" in lib.dpb_last_error()
+    for backward in (0, 1):
+        assert lib.dpb_linear_cross_entropy_workspace_size(at(loss_config(tokens=1, vocab=1, dim=1 << 20)), backward, n) == 0

@@ -418,3 +418,24 @@ def test_tokens_that_the_model_is_sure_of_have_no_gradient(T, V):
     sure[::3] = 5
     dh, dw = dpb.linear_cross_entropy_backward(h, w, sure, lse, gl)
     assert not dh.any() and not dw.any()
+
+
+def test_the_widest_rows():
+    """2^20 columns. Values of 0, 1 and -1, and of 2^-9 of these: every partial sum of a score is exact in fp32."""
+    T, V, d = 40, 300, 1 << 20
+    g = torch.Generator(device="cuda").manual_seed(6)
+    h = torch.randint(-1, 2, (T, d), generator=g, device="cuda").to(BF)
+    w = (torch.randint(-1, 2, (V, d), generator=g, device="cuda") / 512.0).to(BF)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    gl = torch.rand(T, generator=g, device="cuda")
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    z = h.double() @ w.double().t()
+    want = torch.logsumexp(z, 1)
+    assert ((lse.double() - want).abs() <= 2.0 ** -21 + 2.0 ** -22 * z.abs().amax(1) + 2.0 ** -24 * want.abs()).all()
+    dh, dw = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    dz = torch.softmax(z, 1)
+    dz[torch.arange(T, device="cuda"), y] -= 1
+    dz *= gl.double()[:, None]
+    near(dh, dz @ w.double())
+    near(dw, dz.t() @ h.double())
+    assert dpb.status() == 0

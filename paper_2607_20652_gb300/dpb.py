@@ -551,6 +551,15 @@ def _dense(t: Optional[torch.Tensor], name: str, dtype, numel: int, device):
     return t.data_ptr()
 
 
+def _space(t: Optional[torch.Tensor], device):
+    """(address, bytes) of a workspace (None: none): memory of the rows' own device, without gaps or repeats."""
+    if t is None:
+        return None, 0
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}, got one on {t.device} with strides {t.stride()}")
+    return t.data_ptr(), t.nbytes
+
+
 def rope_tables(positions: int, rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None,
                 factor: float = 1.0, original: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0,
                 device=None):
@@ -628,7 +637,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, weight_q=None, weight_k=None,
     dt, sq, sk, a = q.dtype, q.shape, k.shape, _arguments
     q_out = torch.empty(sq, dtype=dt, device=dev) if q_out is None else q_out
     k_out = torch.empty(sk, dtype=dt, device=dev) if k_out is None else k_out
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws, ws_bytes = _space(workspace, dev)
     _ROWS[4].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(q_out, "q_out", dt, sq, dev), *_head_rows(k_out, "k_out", dt, sk, dev))
     h = a.rows
@@ -667,7 +676,7 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, grad_q_out: torch.Te
                        *_head_rows(grad_q, "grad_q", dt, sq, dev), *_head_rows(grad_k, "grad_k", dt, sk, dev))
     h = a.rows
     _check(lib.dpb_qk_norm_rope_backward(a.at, h, h + 24, h + 48, h + 72, *at, h + 96, h + 120, gp,
-                                         None if gp is None else gp + 4 * D, workspace.data_ptr(), workspace.nbytes, s))
+                                         None if gp is None else gp + 4 * D, *_space(workspace, dev), s))
     return (grad_q, grad_k) + ((None, None) if gw is None else (gw[0], gw[1]))
 
 
@@ -716,7 +725,7 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=No
         out = torch.empty(sq, dtype=dt, device=dev)
     if lse is None:
         lse = torch.empty((sq[1], sq[0]), dtype=torch.float32, device=dev)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws, ws_bytes = _space(workspace, dev)
     _ROWS[4].pack_into(a.buf, 64, *_head_rows(q, "q", dt, sq, dev), *_head_rows(k, "k", dt, sk, dev),
                        *_head_rows(v, "v", dt, sk, dev), *_head_rows(out, "out", dt, sq, dev))
     h = a.rows
@@ -755,7 +764,7 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
     h = a.rows
     _check(lib.dpb_attention_backward(a.at, h, h + 24, h + 48, h + 72,
                                       _dense(lse, "lse", torch.float32, sq[0] * sq[1], dev), h + 96, *at, h + 120, h + 144,
-                                      h + 168, workspace.data_ptr(), workspace.nbytes, s))
+                                      h + 168, *_space(workspace, dev), s))
     return grad_q, grad_k, grad_v
 
 
@@ -916,8 +925,7 @@ def linear_cross_entropy_forward(hidden: torch.Tensor, weight: torch.Tensor, tar
     h = a.rows
     _check(load().dpb_linear_cross_entropy_forward(a.at, h, h + 16, at, _dense(loss, "loss", torch.float32, T, dev),
                                                    _dense(lse, "lse", torch.float32, T, dev),
-                                                   None if counted is None else counted.data_ptr(), workspace.data_ptr(),
-                                                   workspace.nbytes, s))
+                                                   None if counted is None else counted.data_ptr(), *_space(workspace, dev), s))
     return (loss, lse, counted) if want_counted else (loss, lse)
 
 
@@ -956,8 +964,7 @@ def linear_cross_entropy_backward(hidden: torch.Tensor, weight: torch.Tensor, ta
     h = a.rows
     _check(load().dpb_linear_cross_entropy_backward(a.at, h, h + 16, at, _dense(lse, "lse", torch.float32, T, dev),
                                                     grad_loss.data_ptr(), h + 32 if want_hidden else None,
-                                                    h + 48 if want_weight else None, workspace.data_ptr(),
-                                                    workspace.nbytes, s))
+                                                    h + 48 if want_weight else None, *_space(workspace, dev), s))
     return grad_hidden if want_hidden else None, grad_weight if want_weight else None
 
 
@@ -981,7 +988,7 @@ def embedding(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=N
     kind = _kind(dt, "weight")
     at, size = _indices(ids, "ids", T, dev)
     out = torch.empty((T, d), dtype=dt, device=dev) if out is None else out
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws, ws_bytes = _space(workspace, dev)
     _EMBEDDING.pack_into(a.buf, 0, T, V, d, size, kind, scale, _status_slot(dev, s) if workspace is None else 0)
     _PLAIN_ROWS[2].pack_into(a.buf, 64, *_plain_rows(weight, "weight", dt, weight.shape, dev),
                              *_plain_rows(out, "out", dt, (T, d), dev))
@@ -1010,7 +1017,7 @@ def embedding_backward(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int, sc
     grad_weight = torch.empty((vocab, d), dtype=dt, device=dev) if grad_weight is None else grad_weight
     _PLAIN_ROWS[2].pack_into(a.buf, 64, *_plain_rows(grad_out, "grad_out", dt, (T, d), dev),
                              *_plain_rows(grad_weight, "grad_weight", dt, (vocab, d), dev))
-    _check(lib.dpb_embedding_backward(a.at, a.rows, at, a.rows + 16, workspace.data_ptr(), workspace.nbytes, s))
+    _check(lib.dpb_embedding_backward(a.at, a.rows, at, a.rows + 16, *_space(workspace, dev), s))
     return grad_weight
 
 
@@ -1061,7 +1068,7 @@ def add_norm_backward(total: torch.Tensor, grad_out: torch.Tensor, grad_total=No
         n = ctypes.c_size_t()
         _check(lib.dpb_norm_workspace_size(a.at, n))
         workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)  # scratch of this call
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws, ws_bytes = _space(workspace, dev)
     _PLAIN_ROWS[4].pack_into(a.buf, 64, *_plain_rows(total, "total", dt, sh, dev),
                              *_plain_rows(grad_out, "grad_out", dt, sh, dev),
                              *((0, 0) if grad_total is None else _plain_rows(grad_total, "grad_total", dt, sh, dev)),

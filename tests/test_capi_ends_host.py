@@ -193,3 +193,15 @@ def test_loss_refuses_rows_that_are_too_wide(lib, dim):
     assert b"columns" in lib.dpb_last_error()
     for backward in (0, 1):
         assert lib.dpb_linear_cross_entropy_workspace_size(at(loss_config(tokens=1, vocab=1, dim=1 << 20)), backward, n) == 0
+
+
+def test_a_workspace_of_another_place_is_refused():
+    """Memory of the host or with repeats: its address and size would not be what the kernels write to."""
+    import torch
+    there, ws = torch.device("cuda", 0), torch.zeros(1 << 10, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="workspace"):
+        dpb._space(ws, there)
+    for bad in (ws[:1].expand(1 << 20), ws[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            dpb._space(bad, ws.device)
+    assert dpb._space(None, there) == (None, 0) and dpb._space(ws, ws.device) == (ws.data_ptr(), 1 << 10)

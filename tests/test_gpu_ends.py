@@ -312,3 +312,22 @@ def test_model_in_a_cuda_graph():
     tgt[0, 0] = 97
     graph.replay()
     assert dpb.status() == dpb.DEV_BAD_INDEX and dpb.status() == 0
+
+
+def test_every_call_refuses_a_workspace_of_another_place():
+    """Also the step's other operators: a workspace on the host, one that repeats itself, one with gaps."""
+    w, x = torch.randn(97, 64, device="cuda").to(BF), torch.randn(20, 64, device="cuda").to(BF)
+    y, g = torch.randint(0, 97, (20,), device="cuda"), torch.ones(20, device="cuda")
+    q = torch.randn(20, 2, 64, device="cuda").to(BF)
+    _, lse = dpb.linear_cross_entropy_forward(x, w, y)
+    o, l2 = dpb.attention_forward(q, q, q)
+    host = torch.zeros(1 << 24, dtype=torch.uint8)
+    there = host[:1 << 10].cuda()
+    for ws in (host, there[:1].expand(1 << 24), there[::2]):
+        for f in (lambda **k: dpb.linear_cross_entropy_forward(x, w, y, **k), lambda **k: dpb.embedding(w, y, **k),
+                  lambda **k: dpb.linear_cross_entropy_backward(x, w, y, lse, g, **k),
+                  lambda **k: dpb.embedding_backward(x, y, 97, **k), lambda **k: dpb.add_norm_backward(x, x, **k),
+                  lambda **k: dpb.qk_norm_rope(q, q, **k), lambda **k: dpb.qk_norm_rope_backward(q, q, q, q, **k),
+                  lambda **k: dpb.attention_forward(q, q, q, **k), lambda **k: dpb.attention_backward(q, q, q, o, l2, q, **k)):
+            with pytest.raises(ValueError, match="workspace"):
+                f(workspace=ws)

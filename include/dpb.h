@@ -325,6 +325,9 @@ dpb_status dpb_encode_noalloc(const dpb_plan *plan, const void *x, int64_t T, co
  * for its copies and MMAs still in flight, frees its tensor memory and
  * returns; that call's codes are incomplete. With tries = 0 every such wait
  * gives up at once, which lets a test exercise that path without a fault.
+ * It also bounds the waits of dpb_linear_cross_entropy_backward for what other
+ * blocks have to finish first: one that gives up ends its two blocks in the same
+ * way, and that call's gradients are incomplete.
  * Returns DPB_ERR_INVALID_ARG for tries < -1.
  */
 dpb_status dpb_debug_set_wait_limit(int32_t tries);

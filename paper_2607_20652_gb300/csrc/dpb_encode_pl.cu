@@ -862,10 +862,6 @@ void build_per_level_tables(dpb_plan *p) {
 
 namespace {
 
-// Bound of the main loop's mbarrier waits for the launches that follow (-1:
-// the default kSpin); set by dpb_debug_set_wait_limit.
-std::atomic<int32_t> g_wait_limit{-1};
-
 // Generator-tile stages: as many as fit (at least 2).
 int pl_stages(const dpb_config &c, int kvh, int dmax) {
     for (int nbs = kMaxStages; nbs > 2; --nbs)
@@ -879,7 +875,16 @@ int pl_dmax(const dpb_config &c) {
     return dmax;
 }
 
+// Bound of the main loop's mbarrier waits for the launches that follow (-1:
+// the default kSpin); set by dpb_debug_set_wait_limit.
+std::atomic<int32_t> g_wait_limit{-1};
+
 }  // namespace
+
+uint32_t wait_limit(uint32_t normal) {
+    const int32_t lim = g_wait_limit.load(std::memory_order_relaxed);
+    return lim < 0 ? normal : (uint32_t)lim;
+}
 
 size_t encode_pl_smem(const dpb_plan *p) {
     const dpb_config &c = p->cfg;
@@ -922,8 +927,7 @@ cudaError_t launch_encode_pl(const dpb_plan *p, const void *x, int64_t T, const 
     }
     a.inv_sqrt_d = p->inv_sqrt_d;
     a.nbs = pl_stages(c, a.kvh, a.dmax);
-    const int32_t lim = g_wait_limit.load(std::memory_order_relaxed);
-    a.spin = lim < 0 ? kSpin : (uint32_t)lim;
+    a.spin = wait_limit(kSpin);
     const size_t smem = encode_pl_smem(p);
     const cudaError_t e = allow_smem((const void *)encode_pl_kernel, smem);
     if (e != cudaSuccess) return e;

@@ -101,6 +101,8 @@ cudaError_t allow_smem(const void *func, size_t bytes);
 // time (asked once; `func` is always launched in the same way but for its grid).
 // Clusters of more than 8 blocks and how.dynamicSmemBytes are allowed on the way.
 cudaError_t resident_clusters(const void *func, const cudaLaunchConfig_t &how, int *clusters);
+// Polls of the waits that dpb_debug_set_wait_limit bounds: its number, or `normal`.
+uint32_t wait_limit(uint32_t normal);
 // The library's status word `slot` (1 .. DPB_STATUS_SLOTS) on the current device,
 // or nullptr.
 int32_t *status_word(int32_t slot);

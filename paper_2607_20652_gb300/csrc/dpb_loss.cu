@@ -112,6 +112,7 @@ struct Args {
     bool fine;   // dz as two bf16, the rounded value and the remainder
     bool want_h, want_w;
     bool few;  // rows that the tokens' cluster closes up itself
+    uint32_t tries;  // polls of a unit's wait for others
     int32_t *status;
 };
 
@@ -206,16 +207,16 @@ struct List {
         if (t.kind == kGrad) {
             const int before = t.piece - a.held;
             if (before < 0) return true;
-            if (!reached(&a.head->done[before][kDWeight], each * weight_units(a, words)) ||
-                !reached(&a.head->done[before][kDHidden], each * hidden_units(a)))
+            if (!reached(a, &a.head->done[before][kDWeight], each * weight_units(a, words)) ||
+                !reached(a, &a.head->done[before][kDHidden], each * hidden_units(a)))
                 return false;
         } else if (t.kind == kDHidden || t.kind == kDWeight) {
             const bool ordered = t.kind == kDHidden && t.piece > 0 && !a.split;
             if (all_there && !ordered) return true;
             const bool one = a.held == a.pieces;
             const int dz = one ? grad_units(words) * (a.pieces - 1) + grad_units(last) : grad_units(words_of(a, t.piece));
-            if ((!all_there && !reached(counter(a, Unit{kGrad, 0, 0, 0, t.piece, 0}), each * dz)) ||
-                (ordered && !reached(&a.head->done[t.piece - 1][kDHidden], each * hidden_units(a))))
+            if ((!all_there && !reached(a, counter(a, Unit{kGrad, 0, 0, 0, t.piece, 0}), each * dz)) ||
+                (ordered && !reached(a, &a.head->done[t.piece - 1][kDHidden], each * hidden_units(a))))
                 return false;
             all_there = one;
         } else {
@@ -224,8 +225,8 @@ struct List {
         fence_cluster();  // for the blocks that it is handed to
         return true;
     }
-    static __device__ __forceinline__ bool reached(const int *counter, int target) {
-        for (uint32_t i = 0; i < kTries; ++i) {
+    static __device__ __forceinline__ bool reached(const Args &a, const int *counter, int target) {
+        for (uint32_t i = 0; i < a.tries; ++i) {
             int v;
             asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
             if (v >= target) return true;
@@ -587,12 +588,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     failed = true;
                     break;
                 }
-                const Unit t = list.at(a, atomicAdd(&a.head->next, 1));
+                Unit t = list.at(a, atomicAdd(&a.head->next, 1));
                 ahead = t.blocks <= 8 ? kAhead : 2;
-                if (!list.wait(a, t, all_there)) {
-                    failed = true;
-                    break;
-                }
+                // a wait that gives up ends the pair as the last unit does, with nothing under way
+                if (!list.wait(a, t, all_there)) failed = true, t.kind = kEnd;
                 units.hand(t, s, 0);
                 units.hand(t, s, 1);
                 if (t.kind == kEnd) break;
@@ -1155,6 +1154,7 @@ dpb_status begin(Args &a, const Space &w, const dpb_linear_loss_config *c, const
     // launch), of 1000 x 256 15.8 (14.9), of 1000 x 768 19.4 (17.7); none ignored 15.6, 13.9, 16.2 (16.5, 14.5,
     // 17.0). The launch also takes 2.5 us of the host's time.
     a.few = (int64_t)a.T * a.d <= (1 << 18);
+    a.tries = wait_limit(kTries);
     DPB_CHECK(make_map(&a.hidden, hidden->data, hidden->stride, c->tokens, c->dim, 64));
     DPB_CHECK(make_map(&a.closed, a.closed_rows, c->dim, c->tokens, c->dim, 64));
     DPB_CHECK(make_map(&a.weight, weight->data, weight->stride, c->vocab, c->dim, 64));

@@ -454,7 +454,8 @@ def stats_step(plan: Plan, x: torch.Tensor, mu: torch.Tensor, sigma: torch.Tenso
 
 def set_wait_limit(tries: int = -1):
     """dpb_debug_set_wait_limit: bound of the per-level encoder's main-loop
-    mbarrier waits for the launches that follow (-1 restores the default)."""
+    mbarrier waits, and of the loss gradient's waits for other blocks, for the
+    launches that follow (-1 restores the default)."""
     _check(load().dpb_debug_set_wait_limit(int(tries)))
 
 

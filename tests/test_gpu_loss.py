@@ -439,3 +439,24 @@ def test_the_widest_rows():
     near(dh, dz @ w.double())
     near(dw, dz.t() @ h.double())
     assert dpb.status() == 0
+
+
+@pytest.mark.parametrize("T,V,d", [(300, 700, 64), (2000, 9001, 264), (24001, 5003, 72), (20001, 300, 264)])
+def test_waits_that_give_up_are_flagged_and_leave_the_context_usable(T, V, d):
+    """With waits of 0 polls for other blocks, every pair of blocks ends at the first unit that waits: pieces all held, in
+    two bf16 and in one, one after the other, and parts of the tokens. A call right after is right again; the forward has
+    no such wait."""
+    h, w, y, gl = draw(T, V, d, seed=T, left_out="some", even=False)
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    want = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    assert dpb.status() == 0
+    try:
+        dpb.set_wait_limit(0)
+        again = dpb.linear_cross_entropy_forward(h, w, y)
+        assert dpb.status() == 0 and torch.equal(again[0], loss) and torch.equal(again[1], lse)
+        dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+        assert dpb.status() == dpb.DEV_TIMEOUT
+    finally:
+        dpb.set_wait_limit(-1)
+    got = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    assert dpb.status() == 0 and all(torch.equal(a, b) for a, b in zip(got, want))

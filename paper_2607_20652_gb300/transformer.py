@@ -38,12 +38,29 @@ class _Attention(nn.Module):
         return self.out(o.transpose(1, 2).reshape(B, S, d))
 
 
+class _Lookup(nn.Embedding):
+    """The embedding by the library's lookup."""
+
+    def forward(self, ids):
+        return _ends.embedding(self.weight, ids)
+
+
+class _AddNorm(nn.RMSNorm):
+    """The norm by the library's, with the residual's addition before it: (x, what is to be added) -> (norm, sum)."""
+
+    def forward(self, x, delta=None):
+        # without an eps nn.RMSNorm takes that of the type it computes bf16 rows in
+        return _ends.add_norm(x, delta, self.weight, torch.finfo(torch.float32).eps if self.eps is None else self.eps)
+
+
 class _Block(nn.Module):
+    norm = nn.RMSNorm
+
     def __init__(self, d: int, heads: int, d_mlp: int, dpb: Optional[DPBLayer], attn: nn.Module):
         super().__init__()
-        self.n1 = nn.RMSNorm(d)
+        self.n1 = self.norm(d)
         self.attn = attn
-        self.n2 = nn.RMSNorm(d)
+        self.n2 = self.norm(d)
         self.dpb = dpb
         self.up = nn.Linear(d, d_mlp, bias=False)
         self.down = nn.Linear(d_mlp, d, bias=False)
@@ -55,18 +72,19 @@ class _Block(nn.Module):
             h = self.dpb(h)  # the bottleneck sits before the MLP's input (§3)
         return x + self.down(F.gelu(self.up(h)))
 
-    def stream(self, x, delta):
-        """The same with the library's residual norms: the residual's rows and what is still to be added to them."""
-        h, x = _add_norm(self.n1, x, delta)
-        h, x = _add_norm(self.n2, x, self.attn(h))
+
+class _StreamBlock(_Block):
+    """The same with the library's residual norms: takes and gives the residual's rows and what is still to be added
+    to them."""
+
+    norm = _AddNorm
+
+    def forward(self, x, delta=None):
+        h, x = self.n1(x, delta)
+        h, x = self.n2(x, self.attn(h))
         if self.dpb is not None:
             h = self.dpb(h)
         return x, self.down(F.gelu(self.up(h)))
-
-
-def _add_norm(norm: nn.RMSNorm, x, delta):
-    # without an eps nn.RMSNorm takes that of the type it computes bf16 rows in
-    return _ends.add_norm(x, delta, norm.weight, torch.finfo(torch.float32).eps if norm.eps is None else norm.eps)
 
 
 class ParityTransformer(nn.Module):
@@ -77,7 +95,9 @@ class ParityTransformer(nn.Module):
     and keys and rotary positions in place of the learned ones (bf16;
     ``kv_heads`` key and value heads). ``ends="dpb"`` uses this library's
     embedding lookup, residual norms and, with targets, its cross entropy (bf16):
-    the same model without a tensor of tokens x vocabulary."""
+    the same model without a tensor of tokens x vocabulary. Its modules keep their
+    names and are called in the same order; blocks then take and give the
+    residual's rows and what is still to be added to them, norms the norm and the sum."""
 
     def __init__(self, layers: int = 12, d: int = 768, heads: int = 12, d_mlp: int = 3072, vocab: int = 50257,
                  context: int = 1024, dpb: Optional[dict] = None, device=None, dtype=torch.bfloat16,
@@ -92,15 +112,16 @@ class ParityTransformer(nn.Module):
             raise ValueError(f"attention must be 'torch' or 'dpb', got {attention!r}")
         if attention == "torch" and kv_heads not in (None, heads):
             raise ValueError("kv_heads needs attention='dpb'")
-        self.tok = nn.Embedding(vocab, d)
+        lookup, block = (_Lookup, _StreamBlock) if ends == "dpb" else (nn.Embedding, _Block)
+        self.tok = lookup(vocab, d)
         self.pos = nn.Embedding(context, d) if attention == "torch" else None
         blocks = []
         for i in range(layers):
             layer = DPBLayer(seed=i, device=device, d=d, **dpb) if dpb is not None else None
             attn = _Attention(d, heads) if attention == "torch" else Attention(d, heads, kv_heads, context=context)
-            blocks.append(_Block(d, heads, d_mlp, layer, attn))
+            blocks.append(block(d, heads, d_mlp, layer, attn))
         self.blocks = nn.ModuleList(blocks)
-        self.norm = nn.RMSNorm(d)
+        self.norm = block.norm(d)
         std = 0.02
         for p in self.parameters():
             if p.dim() >= 2:
@@ -117,15 +138,14 @@ class ParityTransformer(nn.Module):
 
     def forward(self, ids, targets=None):
         B, S = ids.shape
-        own = self.ends == "dpb"
-        x = _ends.embedding(self.tok.weight, ids) if own else self.tok(ids)
+        x = self.tok(ids)
         if self.pos is not None:
             x = x + self.pos(torch.arange(S, device=ids.device))
-        if own:
+        if self.ends == "dpb":
             delta = None
             for b in self.blocks:
-                x, delta = b.stream(x, delta)
-            h, _ = _add_norm(self.norm, x, delta)
+                x, delta = b(x, delta)
+            h, _ = self.norm(x, delta)
             if targets is None:
                 return F.linear(h, self.tok.weight)
             return _ends.linear_cross_entropy(h, self.tok.weight, targets)

@@ -331,3 +331,41 @@ def test_every_call_refuses_a_workspace_of_another_place():
                   lambda **k: dpb.attention_forward(q, q, q, **k), lambda **k: dpb.attention_backward(q, q, q, o, l2, q, **k)):
             with pytest.raises(ValueError, match="workspace"):
                 f(workspace=ws)
+
+
+def test_hooks_of_the_model_run():
+    """Every module of the model is called as one: hooks on blocks, norms and the embedding see what they see elsewhere."""
+    ids, tgt = (torch.randint(0, 97, (4, 32), device="cuda") for _ in range(2))
+    dpb_kw = dict(levels=3, m_bits=12, children=16, beam=8, k=8)
+    called = {}
+    for kind in ("torch", "dpb"):
+        m, seen = small(ends=kind, dpb=dpb_kw), []
+        for name, sub in m.named_modules():
+            if name:
+                sub.register_forward_hook(lambda s, a, out, name=name: seen.append(name))
+        m(ids, tgt).backward()
+        called[kind] = seen
+    assert called["dpb"] == called["torch"] and {"tok", "norm", "blocks.1", "blocks.0.n1", "blocks.1.n2"} <= set(called["dpb"])
+
+
+def test_blocks_behind_a_checkpoint():
+    """Blocks in a wrapper that computes them again in the backward pass: equal bits."""
+    from torch.utils.checkpoint import checkpoint
+
+    class Again(torch.nn.Module):
+        def __init__(self, block):
+            super().__init__()
+            self.block = block
+
+        def forward(self, *args):
+            return checkpoint(self.block, *args, use_reentrant=False)
+
+    m = small(ends="dpb", attention="dpb")
+    ids, tgt = (torch.randint(0, 97, (4, 32), device="cuda") for _ in range(2))
+    ps = list(m.parameters())
+    loss = m(ids, tgt)
+    want = (loss.detach(), *torch.autograd.grad(loss, ps))
+    for i, b in enumerate(m.blocks):
+        m.blocks[i] = Again(b)
+    loss = m(ids, tgt)
+    assert all(torch.equal(a, b) for a, b in zip(want, (loss.detach(), *torch.autograd.grad(loss, ps))))

@@ -157,13 +157,17 @@ class _LossFunction(torch.autograd.Function):
 def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100,
                          reduction: str = "mean") -> torch.Tensor:
     """Cross entropy of the scores hidden weight^T without making them: hidden
-    [..., d] bf16, weight [vocab, d] (taken in bf16, as under autocast), targets
-    [...]. ``reduction`` "mean" (over the tokens that are not ignored; NaN if
-    all are), "sum" or "none", in fp32. What the rows of ignored tokens hold does
-    not matter. d has to be a multiple of 8."""
+    [..., d] bf16 (under bf16 autocast of any type, taken in bf16 as a linear
+    layer's are), weight [vocab, d] (taken in bf16), targets [...]. ``reduction``
+    "mean" (over the tokens that are not ignored; NaN if all are), "sum" or "none",
+    in fp32. What the rows of ignored tokens hold does not matter. d has to be a
+    multiple of 8."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError(f"reduction must be 'mean', 'sum' or 'none', got {reduction!r}")
     if hidden.shape[:-1] != targets.shape:
         raise ValueError(f"targets must have the shape {list(hidden.shape[:-1])}, got {list(targets.shape)}")
+    if hidden.dtype is not torch.bfloat16 and torch.is_autocast_enabled("cuda") and \
+            torch.get_autocast_dtype("cuda") is torch.bfloat16:
+        hidden = hidden.to(torch.bfloat16)
     loss = _LossFunction.apply(hidden, weight, targets, ignore_index, reduction == "mean")
     return loss.sum() if reduction == "sum" else loss

@@ -369,3 +369,31 @@ def test_blocks_behind_a_checkpoint():
         m.blocks[i] = Again(b)
     loss = m(ids, tgt)
     assert all(torch.equal(a, b) for a, b in zip(want, (loss.detach(), *torch.autograd.grad(loss, ps))))
+
+
+def test_fp32_parameters_under_autocast():
+    """Modules with fp32 parameters under bf16 autocast, as attention's: the residual stream is fp32, the loss takes its rows
+    in bf16 as a linear layer would, every gradient is fp32. Without autocast fp32 rows are refused, as under fp16's."""
+    from paper_2607_20652_gb300 import ends
+    torch.manual_seed(4)
+    emb, norm, lin = ends.Embedding(97, 64, device="cuda"), ends.AddRMSNorm(64, device="cuda"), \
+        torch.nn.Linear(64, 64, bias=False, device="cuda")
+    ids, y = (torch.randint(0, 97, (3, 20), device="cuda") for _ in range(2))
+    ps = [emb.weight, norm.weight, lin.weight]
+    with torch.autocast("cuda", torch.bfloat16):
+        x = emb(ids)
+        delta = lin(x)
+        h, total = norm(x, delta)
+        assert x.dtype == h.dtype == total.dtype == torch.float32 and delta.dtype == BF
+        loss = ends.linear_cross_entropy(h, emb.weight, y)
+    got = torch.autograd.grad(loss, (*ps, h), retain_graph=True)
+    assert loss.dtype == torch.float32 and all(g.dtype == torch.float32 and g.any() for g in got)
+    hb, wb = h.detach().to(BF).requires_grad_(), emb.weight.detach().to(BF).requires_grad_()
+    want = ends.linear_cross_entropy(hb, wb, y)
+    dh, _ = torch.autograd.grad(want, (hb, wb))
+    assert torch.equal(loss, want) and torch.equal(got[3], dh.float())
+    for f in (lambda: ends.linear_cross_entropy(h, emb.weight, y),):
+        with pytest.raises(ValueError):
+            f()
+        with torch.autocast("cuda", torch.float16), pytest.raises(ValueError):
+            f()

@@ -621,7 +621,7 @@ dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
 
 /*
  * dpb_linear_cross_entropy_forward -- cross entropy of the rows' scores over the
- * vocabulary, without a tensor of tokens x vocabulary:
+ * vocabulary, without keeping the scores:
  *   z_t = hidden_t weight^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_t,target
  *   tokens, vocab, dim   at most 2^24 tokens, 2^28 words and 2^20 columns; dim a
  *               multiple of 8; 2^26 tiles of 256 x 256 in all products together
@@ -654,7 +654,9 @@ dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, c
  * dpb_linear_cross_entropy_backward -- its gradients for grad_loss = dL/dloss:
  *   dz_tv = grad_loss_t (exp(z_tv - lse_t) - [v = target_t]),
  *   grad_hidden = dz weight,  grad_weight = dz^T hidden.
- * The scores are formed again, a piece of the vocabulary at a time. lse is the
+ * The scores are formed again, a piece of the vocabulary at a time. The workspace
+ * holds dz of three pieces, all of the vocabulary if it is that small: together 192 MB
+ * or, if that is more, 24 KB a token (of more than 655360 words, 3/160 of them). lse is the
  * forward's. grad_loss: fp32, token t's at grad_loss + t * grad_stride
  * (grad_stride 0: one value for all, as of a mean; or 1). grad_hidden and
  * grad_weight (rows as hidden and weight; either may be NULL, then it is not

@@ -1035,7 +1035,7 @@ constexpr int kLeastPiece = 4096, kFineRows = 512;
 constexpr int kLeastPart = 2048;
 
 struct Space {
-    int64_t T_pad, V_pad, piece, pieces, held, parts = 1, part_rows = 0;
+    int64_t T_pad, V_pad, piece, pieces, held, columns, parts = 1, part_rows = 0;  // columns: of dz
     bool split = false, fine = false;
     size_t head, tokens, place, closed, part, z_target, dz, acc, w_acc, bytes;
     Space(const dpb_linear_loss_config *c, bool backward) {
@@ -1056,6 +1056,7 @@ struct Space {
             pieces = (c->vocab + piece - 1) / piece;
             held = std::min<int64_t>(pieces, kBuffers);
         }
+        columns = std::min(held * piece, words);  // the last of all pieces may be shorter
         const int64_t w_units = words / kTile * ((c->dim + kTile - 1) / kTile), pairs = sms_of_device() / 2;
         if (held == pieces && w_units < pairs && T_pad >= 2 * kLeastPart) {
             parts = std::min((pairs + w_units - 1) / w_units, T_pad / kLeastPart);
@@ -1073,7 +1074,7 @@ struct Space {
         place = take(T * 4);
         closed = take(T * d * 2);
         if (backward) {
-            dz = take((size_t)T_pad * (fine ? 2 : 1) * held * piece * 2);
+            dz = take((size_t)T_pad * (fine ? 2 : 1) * columns * 2);
             acc = take(split ? (size_t)pieces * T_pad * d * 4 : pieces > 1 ? T * d * 4 : 0);
             w_acc = take(parts > 1 ? (size_t)parts * V_pad * d * 4 : 0);
             part = z_target = at;
@@ -1247,9 +1248,9 @@ dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, 
         DPB_CHECK(make_map(&a.sums, a.acc, cfg->dim, w.split ? w.pieces * w.T_pad : cfg->tokens, cfg->dim, 32, true));
     a.w_acc = reinterpret_cast<float *>(ws + w.w_acc);
     if (w.parts > 1) DPB_CHECK(make_map(&a.w_sums, a.w_acc, cfg->dim, w.parts * w.V_pad, cfg->dim, 32, true));
-    const int64_t columns = w.held * w.piece, rows = w.T_pad * (w.fine ? 2 : 1);
-    DPB_CHECK(make_map(&a.dz, ws + w.dz, columns, rows, columns, 64));
-    DPB_CHECK(make_map(&a.dz_out, ws + w.dz, columns, rows, columns, 32));
+    const int64_t rows = w.T_pad * (w.fine ? 2 : 1);
+    DPB_CHECK(make_map(&a.dz, ws + w.dz, w.columns, rows, w.columns, 64));
+    DPB_CHECK(make_map(&a.dz_out, ws + w.dz, w.columns, rows, w.columns, 32));
     DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, grad_loss, lse, ws, s));
     const int64_t tiles_m = w.T_pad / kTile, tiles_v = (cfg->vocab + kTile - 1) / kTile, tiles_d = (cfg->dim + kTile - 1) / kTile;
     DPB_CHECK(launch_products(a, tiles_m * tiles_v + tiles_v * tiles_d * w.parts, s));

@@ -5,8 +5,10 @@ dpb_linear_cross_entropy_forward / _backward.
 The paper's backbone is GPT-2 style with one weight for embedding and
 unembedding and RMS norms (§3); it does not describe them further. Here the
 lookup, the addition of a block's output to the residual with the next norm,
-and the cross entropy from the last hidden rows run in the library's kernels;
-no tensor of tokens x vocabulary is made. The gradients have no gradient of
+and the cross entropy from the last hidden rows run in the library's kernels.
+The scores of tokens x vocabulary are never kept; the loss's gradient keeps theirs
+in bf16 for a part of the vocabulary at a time, in 192 MB or, if that is more, 24 KB
+a token (all of it where the vocabulary is that small). The gradients have no gradient of
 their own: a second differentiation raises.
 
 A forward and backward pass may be captured into a CUDA graph. As with every

@@ -95,7 +95,8 @@ class ParityTransformer(nn.Module):
     and keys and rotary positions in place of the learned ones (bf16;
     ``kv_heads`` key and value heads). ``ends="dpb"`` uses this library's
     embedding lookup, residual norms and, with targets, its cross entropy (bf16):
-    the same model without a tensor of tokens x vocabulary. Its modules keep their
+    the same model without its scores in memory (ends.py: what the loss's gradient
+    keeps of them). Its modules keep their
     names and are called in the same order; blocks then take and give the
     residual's rows and what is still to be added to them, norms the norm and the sum."""
 

@@ -205,3 +205,22 @@ def test_a_workspace_of_another_place_is_refused():
         with pytest.raises(ValueError, match="workspace"):
             dpb._space(bad, ws.device)
     assert dpb._space(None, there) == (None, 0) and dpb._space(ws, ws.device) == (ws.data_ptr(), 1 << 10)
+
+
+@pytest.mark.parametrize("tokens", [1, 33, 512, 1000, 4096, 8192, 65536, 262144])
+@pytest.mark.parametrize("vocab", [50, 1000, 5003, 9001, 12288, 50257, 1 << 20])
+def test_the_gradients_scratch_is_what_is_said(lib, tokens, vocab):
+    """dz of three pieces, 192 MB or 24 KB a token, or 3/160 of a large vocabulary, and never more than all of it; beside
+    it rows of the tokens (closed up, bf16; sums in fp32, apart for up to 160 pieces where all of dz is held, which is where
+    dz has 192 MB at most) and sums of dW for parts of the tokens, of fewer tiles than half the multiprocessors."""
+    dim, n = 768, ctypes.c_size_t()
+    assert lib.dpb_linear_cross_entropy_workspace_size(at(loss_config(tokens=tokens, vocab=vocab, dim=dim)), 1, n) == 0
+    T, V, mb = -(-tokens // 256) * 256, -(-vocab // 256) * 256, 1 << 20
+    piece = max(12288, -(-3 * vocab // 160) + 768)
+    dz = min(max(192 * mb, 2 * T * min(V, piece)), 2 * T * V * (2 if T <= 512 else 1))
+    held = 2 * T * V <= 192 * mb
+    tiles = (T // 256) * 3
+    # pieces whose sums are apart: two units a pair of blocks, each unit a tile of fp32 sums
+    sums = min(152 * 256 * 1024 + tiles * 256 * 1024, 160 * tiles * 256 * 1024) if held else T * dim * 4
+    parts = 76 * 256 * 1024 + V * dim * 4
+    assert n.value <= dz + sums + parts + T * (dim * 2 + 20) + 64 * 1024

@@ -539,7 +539,11 @@ dpb_status dpb_adamw_step(const dpb_adamw_config *cfg, const dpb_adamw_tensor *t
  * What a training step still needs beside its plain matrix products: the lookup
  * of the tokens' embeddings, the residual's addition with the norm behind it, and
  * the cross entropy over the vocabulary (§3: tied embeddings, RMS norms). The
- * status of device bits goes by status_slot as above.
+ * status of device bits goes by status_slot as above. Outputs may not overlap
+ * inputs but where it is said. How sums are split goes by the current device's
+ * number of multiprocessors, and so do the workspaces: equal inputs give equal
+ * bits on devices that have as many, and a workspace's size is asked for with the
+ * call's device current.
  */
 
 /* Rows [n][dim]: element (t, i) lies at data + t * stride + i (stride in elements). */
@@ -572,8 +576,8 @@ dpb_status dpb_embedding(const dpb_embedding_config *cfg, const dpb_rows *weight
  * dpb_embedding_backward -- grad_weight[v] = scale times the sum of grad_y_t over
  * the tokens of id v, in full: rows of ids that do not occur are written with 0.
  * Tokens with an id outside [0, vocab) set DPB_DEV_BAD_INDEX and are left out.
- * The tokens are sorted by id; sums are fp32, in an order that the ids alone fix,
- * and rounded once.
+ * The tokens are sorted by id; sums are fp32, in an order that the sizes, the ids
+ * and the device's multiprocessors fix, and rounded once.
  */
 dpb_status dpb_embedding_backward(const dpb_embedding_config *cfg, const dpb_rows *grad_y, const void *ids,
                                   const dpb_rows *grad_weight, void *workspace, size_t workspace_bytes, void *stream);
@@ -636,8 +640,7 @@ dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
  * Scores and sums are fp32, exponentials to 2 ulp; a small loss keeps its digits
  * (it is not formed from the rounded lse). The tensor cores cut off what they add,
  * so a score of a few units is off by 2e-9 dim (loss and lse by 4e-7 of themselves
- * at dim = 768, 1e-6 at 2048). The outputs may not overlap the inputs, here and in
- * the gradient.
+ * at dim = 768, 1e-6 at 2048).
  */
 typedef struct dpb_linear_loss_config {
     int64_t tokens;
@@ -663,7 +666,8 @@ dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, c
  * computed) are written, rows of ignored tokens with 0. dz enters its products
  * in bf16, relative to the largest finite |grad_loss| (up to 512 tokens in two
  * bf16, value and remainder, where both take at most 192 MB); their sums are fp32,
- * in an order that the sizes and the ignored tokens alone fix, and rounded once.
+ * in an order that the sizes, the ignored tokens and the device's multiprocessors
+ * fix, and rounded once.
  */
 dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, const dpb_rows *hidden,
                                              const dpb_rows *weight, const void *targets, const float *lse,

@@ -216,3 +216,13 @@ def test_refusals():
                 dict(scale=float("nan")), dict(workspace=torch.zeros(512, dtype=torch.uint8, device="cuda"))):
         with pytest.raises((ValueError, dpb.DPBError)):
             dpb.embedding_backward(**(dict(grad_out=dy, ids=ids, vocab=50) | bad))
+
+
+def test_gradient_offsets_past_32_bits():
+    """Rows of 2^31 values and more, of ones: each word's count, exact in fp32."""
+    T, V, d = (1 << 21) + 77, 5003, 1024
+    ids = torch.randint(0, V, (T,), device="cuda")
+    dw = dpb.embedding_backward(torch.ones(T, d, device="cuda"), ids, V)
+    assert (dw == torch.bincount(ids, minlength=V).float()[:, None]).all()
+    w = torch.arange(V, device="cuda", dtype=torch.float32)[:, None].expand(V, d).contiguous()
+    assert (dpb.embedding(w, ids) == ids.float()[:, None]).all()

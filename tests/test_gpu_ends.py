@@ -397,3 +397,51 @@ def test_fp32_parameters_under_autocast():
             f()
         with torch.autocast("cuda", torch.float16), pytest.raises(ValueError):
             f()
+
+
+def test_threads_on_one_stream_all_finish():
+    """As above, with whatever a thread raises told, and each of its calls counted."""
+    work = []
+    for T, V, d in ((900, 1000, 64), (300, 5000, 128)):
+        h, w = torch.randn(T, d, device="cuda").to(BF), torch.randn(V, d, device="cuda").to(BF)
+        y, g = torch.randint(0, V, (T,), device="cuda"), torch.rand(T, device="cuda")
+        y[::3] = -100
+        ids = y.clamp(min=0)
+
+        def step(h=h, w=w, y=y, g=g, ids=ids, V=V):
+            loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+            return (loss, *dpb.linear_cross_entropy_backward(h, w, y, lse, g), dpb.embedding(w, ids),
+                    dpb.embedding_backward(h, ids, V), *dpb.add_norm(h, h), *dpb.add_norm_backward(h, h))
+
+        work.append(step)
+    want = [f() for f in work]
+    torch.cuda.synchronize()
+    raised, same = [], []
+
+    def loop(f, v):
+        try:
+            for _ in range(60):
+                same.append(all(torch.equal(a, b) for a, b in zip(f(), v)))
+        except BaseException as e:
+            raised.append(e)
+
+    threads = [threading.Thread(target=loop, args=(f, v)) for f, v in zip(work, want) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not raised and len(same) == 4 * 60 and all(same) and dpb.status() == 0
+
+
+def test_models_choose_the_same_words():
+    """The highest score of each token, where it leads by more than both models' roundings (a dozen of 2^-8 each) may move."""
+    own, other = small(ends="dpb"), small()
+    with torch.no_grad():
+        for m in (own, other):
+            m.tok.weight.mul_(20)  # scores some 3 apart in place of 0.2
+        ids = torch.randint(0, 97, (4, 32), device="cuda")
+        a, b = own(ids).double(), other(ids).double()
+    top = b.topk(2, -1).values
+    clear = top[..., 0] - top[..., 1] > 24 * 2.0 ** -8 * b.abs().amax(-1)
+    assert clear.sum() > 10 and torch.equal(a.argmax(-1)[clear], b.argmax(-1)[clear])
+    assert len(b.argmax(-1)[clear].unique()) > 3

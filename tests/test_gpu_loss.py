@@ -460,3 +460,21 @@ def test_waits_that_give_up_are_flagged_and_leave_the_context_usable(T, V, d):
         dpb.set_wait_limit(-1)
     got = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
     assert dpb.status() == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("left_out", ["none", "some"])
+def test_offsets_past_32_bits(left_out):
+    """Hidden rows of 2^31 values and more: 512 times the same rows, each time the same bits (as given, and closed up)."""
+    T, V, d, n = 4099, 97, 1024, 512
+    h, w, y, _ = draw(T, V, d, seed=8, left_out=left_out)
+    gl = torch.rand(T, device="cuda")
+    loss0, lse0 = dpb.linear_cross_entropy_forward(h, w, y)
+    dh0, _ = dpb.linear_cross_entropy_backward(h, w, y, lse0, gl)
+    hh, yy, gg = h.repeat(n, 1), y.repeat(n), gl.repeat(n)
+    assert hh.numel() > 2 ** 31
+    loss, lse = dpb.linear_cross_entropy_forward(hh, w, yy)
+    assert (loss.view(n, T) == loss0).all() and (lse.view(n, T) == lse0).all()
+    dh, dw = dpb.linear_cross_entropy_backward(hh, w, yy, lse, gg)
+    assert (dh.view(n, T, d) == dh0).all()
+    near(dw, formula(h, w, y, gl)[3] * n)
+    assert dpb.status() == 0

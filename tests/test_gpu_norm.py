@@ -233,3 +233,22 @@ def test_gradient_of_zeros_with_a_small_eps(dtype):
     x[::3] = 0
     for eps in (1e-26, 1e-30, 1e-36):
         check_gradient(*dpb.add_norm_backward(x, dy, dt, w, eps), x, w, dy, dt, eps)
+
+
+def test_offsets_past_32_bits():
+    """2^31 values and more: 512 times the same rows, each time the same bits."""
+    T, d, n = 4099, 1024, 512
+    x, delta, w, dy, dt = draw(T, d, torch.bfloat16)
+    y0, total0 = dpb.add_norm(x, delta, w)
+    dx0, dw0 = dpb.add_norm_backward(total0, dy, dt, w)
+    many = lambda t: t.repeat(n, 1)  # noqa: E731
+    y, total = dpb.add_norm(many(x), many(delta), w)
+    assert y.numel() > 2 ** 31
+    assert (y.view(n, T, d) == y0).all() and (total.view(n, T, d) == total0).all()
+    del y
+    dx, dw = dpb.add_norm_backward(total, many(dy), many(dt), w)
+    assert (dx.view(n, T, d) == dx0).all()
+    # fp32 sums of some 4000 rows a block and warp, of at most 608 blocks in 32 chains and 5 joins of these
+    r = torch.rsqrt(total0.double().square().mean(-1, keepdim=True) + EPS)
+    size = (dy.double() * total0.double() * r).abs().sum(0) * n
+    assert ((dw.double() - dw0.double() * n).abs() <= (4000 + 19 + 5 + d + 12) * 2.0 ** -23 * size).all()

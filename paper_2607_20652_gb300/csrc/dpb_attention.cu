@@ -26,7 +26,6 @@
 // zero in shared memory where a product would sum over them (0 x NaN), and
 // masked by comparison elsewhere.
 #include <cuda_bf16.h>
-#include <cudaTypedefs.h>
 
 #include <algorithm>
 #include <cmath>
@@ -1834,27 +1833,12 @@ __global__ void __launch_bounds__(C::kThreads, 1) attention_grad_kernel(const __
 
 // ---- host side ------------------------------------------------------------------
 
-PFN_cuTensorMapEncodeTiled_v12000 encoder() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) !=
-                cudaSuccess ||
-            r != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    }();
-    return fn;
-}
-
 // Map of a [tokens][heads][D] tensor in boxes of 64 columns x `rows` tokens of
 // one head; columns past D read as zero.
 dpb_status make_map(CUtensorMap *map, const dpb_heads *h, int64_t tokens, int heads, int D, int rows) {
     std::memset(map, 0, sizeof(*map));
     if (tokens == 0) return DPB_OK;
-    const auto fn = encoder();
+    const auto fn = tensor_map_encoder();
     if (!fn) return fail(DPB_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
     const int64_t hs = heads > 1 ? h->head_stride : 64, ts = tokens > 1 ? h->token_stride : 64;
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens};
@@ -1963,13 +1947,6 @@ cudaError_t registers_cover(const void *kernel) {
                : cudaErrorLaunchOutOfResources;
 }
 
-int multiprocessors() {
-    int dev = 0, sms = 1;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        cudaGetLastError();
-    return sms;
-}
-
 // EARLY: the kernel may start, and set itself up, while the one before it in
 // the stream runs; it waits for that one's results itself.
 template <class C, void (*KERNEL)(AttnArgs), bool EARLY>
@@ -2015,7 +1992,7 @@ cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
     // The last blocks, one for every two SMs at most, write the rows before the first
     // sequence and after the last (32 x 1024 of 65536 rows, 12 heads of 64: 124 us, 353
     // with two blocks a head; without such rows 8 x 1024 takes 24.7 us as before).
-    const int64_t blocks = items + std::min<int64_t>((multiprocessors() + 1) / 2, (a.total_q / (2 * kRows) + 2) * a.hq);
+    const int64_t blocks = items + std::min<int64_t>((sms_of_device() + 1) / 2, (a.total_q / (2 * kRows) + 2) * a.hq);
     if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     a.items = (int)items;
     return launch_blocks<C, attention_forward_kernel<C>, false>(a, blocks, s);
@@ -2023,7 +2000,7 @@ cudaError_t launch_attention_forward(AttnArgs &a, cudaStream_t s) {
 
 template <class C>
 dpb_status launch_attention_backward(AttnArgs &a, cudaStream_t s) {
-    const int sms = multiprocessors();
+    const int sms = sms_of_device();
     a.sms = sms;
     constexpr int kLanes = C::DP / 8, kRowsAtOnce = 512 / kLanes;
     const int64_t rows = a.total_q * a.hq;

@@ -2,6 +2,8 @@
 // the training-step entry points.
 #pragma once
 
+#include <cudaTypedefs.h>
+
 #include <atomic>
 #include <cstdint>
 
@@ -62,6 +64,22 @@ inline int sms_of_device() {
     }
     if (dev < kDevices) known[dev].store(sms, std::memory_order_relaxed);
     return sms;
+}
+
+// The driver's encoder of tensor maps, or nullptr.
+inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) !=
+                cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    }();
+    return fn;
 }
 
 // A kernel that may start, and set itself up, while the one before it in the

@@ -42,7 +42,7 @@ struct LookupArgs {
     int64_t ws, ys, dys, dws;  // strides
     int64_t T;
     int V, d, passes, stretch;
-    int64_t stretches, blocks;  // stretches of tokens, each a warp's, and the blocks that have them
+    int64_t blocks;  // that have the stretches of tokens, a warp each
     float scale;
     Sorted *sorted[2];
     float *head, *tail;  // [blocks][d]: sums of the first row, begun before, and of the last, begun here and going on
@@ -407,14 +407,13 @@ int passes_of(int V) {
 
 struct GradSpace {
     int stretch;
-    int64_t stretches, blocks;
+    int64_t blocks;
     size_t sorted[2], head, tail, open, bytes;
     explicit GradSpace(const dpb_embedding_config *c) {
         // As many stretches as warps are resident, of 8 tokens at least and 64 at most.
         const int64_t warps = (int64_t)kSumResident * sms_of_device();
         stretch = (int)std::max<int64_t>(8, std::min<int64_t>(64, (c->tokens + warps - 1) / warps));
-        stretches = (c->tokens + stretch - 1) / stretch;
-        blocks = (stretches + kSumWarps - 1) / kSumWarps;
+        blocks = ((c->tokens + stretch - 1) / stretch + kSumWarps - 1) / kSumWarps;
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
         sorted[0] = kStatusBytes;
         sorted[1] = sorted[0] + up((size_t)c->tokens * sizeof(Sorted));
@@ -570,7 +569,7 @@ dpb_status dpb_embedding_backward(const dpb_embedding_config *cfg, const dpb_row
     a.dw = grad_weight->data, a.dws = grad_weight->stride;
     a.T = cfg->tokens, a.V = cfg->vocab, a.d = cfg->dim, a.scale = cfg->scale;
     a.passes = passes_of(a.V);
-    a.stretch = w.stretch, a.stretches = w.stretches, a.blocks = w.blocks;
+    a.stretch = w.stretch, a.blocks = w.blocks;
     for (int i = 0; i < 2; ++i) a.sorted[i] = reinterpret_cast<Sorted *>(ws + w.sorted[i]);
     a.head = reinterpret_cast<float *>(ws + w.head);
     a.tail = reinterpret_cast<float *>(ws + w.tail);

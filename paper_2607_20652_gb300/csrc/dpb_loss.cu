@@ -36,7 +36,6 @@
 // first (prepare_kernel, gather_kernel), which also keeps whatever their rows
 // hold out of the sums.
 #include <cuda_bf16.h>
-#include <cudaTypedefs.h>
 
 #include <algorithm>
 #include <cstring>
@@ -983,25 +982,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_sums_kernel(const __grid
 
 // ---- host side ------------------------------------------------------------------
 
-PFN_cuTensorMapEncodeTiled_v12000 encoder() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) !=
-                cudaSuccess ||
-            r != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    }();
-    return fn;
-}
-
 // Map of rows in boxes of 128 bytes x `box_rows` rows; what lies outside reads as zero.
 dpb_status make_map(CUtensorMap *map, const void *data, int64_t stride, int64_t rows, int64_t columns, int box_rows,
                     bool wide = false) {
-    const auto fn = encoder();
+    const auto fn = tensor_map_encoder();
     if (!fn) return fail(DPB_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
     const int elem = wide ? 4 : 2;
     const cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows};

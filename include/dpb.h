@@ -637,10 +637,12 @@ dpb_status dpb_norm_workspace_size(const dpb_norm_config *cfg, size_t *bytes);
  * strides that are multiples of 8 elements. loss, lse: fp32 [tokens]. counted
  * (int32, nullable): the number of tokens that take part. A target outside
  * [0, vocab) that is not ignore_index sets DPB_DEV_BAD_INDEX and counts as ignored.
- * Scores and sums are fp32, exponentials to 2 ulp; a small loss keeps its digits
- * (it is not formed from the rounded lse). The tensor cores cut off what they add,
- * so a score of a few units is off by 2e-9 dim (loss and lse by 4e-7 of themselves
- * at dim = 768, 1e-6 at 2048).
+ * Scores and sums are fp32, exponentials to 2 ulp; a loss keeps its digits however
+ * small it is (it is not formed from the rounded lse, and the target's score is
+ * apart from the others). The tensor cores cut off what they add, so a score of a
+ * few units is off by 2e-9 dim. Beyond 256 columns the loss has its target's score
+ * from a sum that is rounded (it is off by 2e-7 of itself at dim = 768, lse by
+ * 1.5e-7; 8e-7 and 6e-7 at 2048).
  */
 typedef struct dpb_linear_loss_config {
     int64_t tokens;

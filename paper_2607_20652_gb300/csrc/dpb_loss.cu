@@ -36,6 +36,7 @@
 // first (prepare_kernel, gather_kernel), which also keeps whatever their rows
 // hold out of the sums.
 #include <cuda_bf16.h>
+#include <math_constants.h>
 
 #include <algorithm>
 #include <cstring>
@@ -43,6 +44,7 @@
 
 #include "dpb_checks.h"
 #include "dpb_device.cuh"
+#include "dpb_rows.cuh"
 #include "dpb_tensor_core.cuh"
 
 namespace dpb {
@@ -61,6 +63,7 @@ constexpr int kThreads = 128 + 32 * kRowWarps;
 constexpr int kAhead = 4;              // units taken ahead, at most
 constexpr int kBuffers = 3;            // pieces of dz held, where there are many tokens
 constexpr int kMostPieces = 160;
+enum Exact { kAsMultiplied = 0, kInJoin = 1, kBeside = 2 };  // where the loss takes its targets' scores from
 constexpr int kGroup = 32;             // tiles of rows that pass a tile of the vocabulary before the next
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;  // the maximum of no score: finite, so that it can be subtracted
@@ -88,14 +91,14 @@ struct Args {
     CUtensorMap weight;
     CUtensorMap dz, dz_out;  // loaded and stored: [rows, and their remainders][held pieces]
     CUtensorMap dw;
-    const bf16 *h;
-    int64_t h_stride;
+    const bf16 *h, *w;
+    int64_t h_stride, w_stride;
     bf16 *closed_rows;
     Head *head;
     Token *tokens;
     int *place;  // of each token: where it went, or -1
     float2 *part;  // [tiles of the vocabulary][rows]
-    float *z_target;
+    float *z_target, *z_exact;  // the targets' scores: the tensor cores', and summed by themselves
     float *loss, *lse;
     int *counted;
     CUtensorMap sums, w_sums;
@@ -110,6 +113,7 @@ struct Args {
     bool split;  // each piece's sums of dH apart, added up by join_sums_kernel
     bool fine;   // dz as two bf16, the rounded value and the remainder
     bool want_h, want_w;
+    int exact;
     bool few;  // rows that the tokens' cluster closes up itself
     uint32_t tries;  // polls of a unit's wait for others
     int32_t *status;
@@ -302,10 +306,22 @@ __device__ __forceinline__ float4 load_shared(uint32_t addr) {
     return x;
 }
 
-// A row's maximum and sum of exp(z - maximum) over 128 of its scores; the
-// target's score, if it is among them. Scores are subtracted before they are
-// scaled to powers of 2, so that the largest gives 1 exactly; 32 of them are
-// added in eight chains of four.
+// What becomes of a row's target, where it is one of 32 columns: eight of them at a
+// time, as a warp has few targets in a tile (65536 tokens, 1000 words, 256 columns,
+// forward: 67 us, 71 with all 32).
+template <typename F>
+__device__ __forceinline__ void at_target(int column, F &&f) {
+    if ((unsigned)column >= 32u) return;
+#pragma unroll
+    for (int k = 0; k < 32; k += 8)
+        if (column / 8 == k / 8)
+#pragma unroll
+            for (int i = k; i < k + 8; ++i)
+                if (column == i) f(i);
+}
+
+// A row's maximum and sum of exp(z - maximum) over 128 of its scores but the
+// target's, which join_kernel adds. 32 of them are added in eight chains of four.
 __device__ __forceinline__ float2 reduce_scores(uint32_t tmem, int columns, int target, float *z_target) {
     float top = kLowest, sum = 0.f;
     const uint64_t scale = pair(kLog2e, kLog2e);
@@ -319,6 +335,7 @@ __device__ __forceinline__ float2 reduce_scores(uint32_t tmem, int columns, int 
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (c + i >= columns) v[i] = 0xff800000u;
+        at_target(target - c, [&](int i) { *z_target = __uint_as_float(v[i]), v[i] = 0xff800000u; });
         float m[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -338,11 +355,6 @@ __device__ __forceinline__ float2 reduce_scores(uint32_t tmem, int columns, int 
         const float2 t = unpair(add2(add2(s[0], s[1]), add2(s[2], s[3])));
         sum = fmaf(sum, exp2_approx((top - now) * kLog2e), t.x + t.y);
         top = now;
-        if ((unsigned)(target - c) < 32u) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (target - c == i) *z_target = __uint_as_float(v[i]);
-        }
     }
     return make_float2(top, sum);
 }
@@ -377,11 +389,7 @@ __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int 
             const float2 x = unpair(mul2(add2(pair_bits(v[i], v[i + 1]), less), scale));
             p[i] = exp2_approx(x.x), p[i + 1] = exp2_approx(x.y);
         }
-        if ((unsigned)(target - c) < 32u) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (target - c == i) p[i] -= 1.f;
-        }
+        at_target(target - c, [&](int i) { p[i] -= 1.f; });
         if (c + 32 > columns)
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -445,6 +453,26 @@ __device__ __forceinline__ bool multiply(uint32_t d, int blocks, uint32_t base, 
         if (!ok) return false;
     }
     return true;
+}
+
+// A warp: the score of a token's target, its products added up in fp32 with each
+// sum rounded, where the tensor cores cut off.
+__device__ __forceinline__ float target_score(const Args &a, const Token &t) {
+    const int lane = threadIdx.x & 31, pieces = a.d / 8;
+    const bf16 *h = a.h + t.row * a.h_stride, *w = a.w + t.target * a.w_stride;
+    float sum[2] = {0.f, 0.f};
+#pragma unroll 4
+    for (int i = lane; i < pieces; i += 32) {
+        Piece<bf16, 8> x, y;
+        load_piece(h + 8 * i, x);
+        load_piece(w + 8 * i, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j & 1] = fmaf(x.v[j], y.v[j], sum[j & 1]);
+    }
+    float z = sum[0] + sum[1];
+#pragma unroll
+    for (int i = 16; i > 0; i /= 2) z += __shfl_xor_sync(kFull, z, i);
+    return z;
 }
 
 // ---- the kernel -------------------------------------------------------------------------
@@ -596,6 +624,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 if (t.kind == kEnd) break;
             }
         }
+    } else if (warp == 3) {
+        // ---- the targets' scores
+        if (a.exact == kBeside)
+            for (int i = blockIdx.x; i < count; i += gridDim.x) {
+                const float z = target_score(a, a.tokens[i]);
+                if (lane == 0) a.z_exact[i] = z;
+            }
     } else if (warp >= 4) {
         // ---- sums: a row and 128 of its columns a thread
         const int quarter = warp & 3, half = (warp - 4) / 4;
@@ -657,7 +692,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             if (t.kind == kScores) {
                 float z = 0.f;
                 const int target = token.target - column;
-                float2 r = reduce_scores(from, a.V - column, target, &z);
+                const float2 r = reduce_scores(from, a.V - column, target, &z);
                 if (token.row >= 0 && (unsigned)target < 128u) a.z_target[row] = z;
                 // both halves of the row
                 float2 *merge = reinterpret_cast<float2 *>(mem + Shared::kMerge) + 128 * b + 32 * quarter + lane;
@@ -905,15 +940,34 @@ __global__ void __cluster_dims__(kPrepareBlocks, 1, 1) __launch_bounds__(1024)
     if (a.few && all.count != a.T) close_up(a, all.count, rank * 32 + warp, 32 * kPrepareBlocks);
 }
 
+// lse and loss of the others' maximum and sum and a target's score. An infinite score
+// has no loss.
+struct LogSum {
+    float lse, loss;
+};
+__device__ __forceinline__ LogSum log_sum(float2 others, float z) {
+    if (z >= others.x) {
+        const float l = log1pf(others.y * expf(others.x - z));
+        return LogSum{z + l, z < CUDART_INF_F ? l : CUDART_NAN_F};
+    }
+    const float l = logf(others.y + expf(z - others.x));
+    return LogSum{others.x + l, others.x - z + l};
+}
+
 // The tiles' maxima and sums of 32 rows, joined in the tiles' order of each of
-// 32 threads and then of the threads.
-__global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args a) {
-    __shared__ float2 parts[32][33];
+// 32 threads and then of the threads; and the target's score.
+__global__ void __launch_bounds__(1024, 2) join_kernel(const __grid_constant__ Args a) {
+    __shared__ float2 parts[32][33], joined[32];
+    __shared__ float scores[32];
     wait_previous();
     const int lane = threadIdx.x & 31, slice = threadIdx.x / 32, count = a.head->count;
     const int tiles = (a.V + kTile - 1) / kTile;
-    const int64_t row = blockIdx.x * 32ll + lane;
-    if (blockIdx.x * 32ll >= count) return;
+    const int64_t first = blockIdx.x * 32ll, row = first + lane;
+    if (first >= count) return;
+    if (a.exact == kInJoin && first + slice < count) {
+        const float z = target_score(a, a.tokens[first + slice]);
+        if (lane == 0) scores[slice] = z;
+    }
     float2 r = make_float2(kLowest, 0.f);
     if (row < count)
         for (int i = slice; i < tiles; i += 32) r = join(r, a.part[i * a.T_pad + row]);
@@ -925,14 +979,16 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Args
         const float2 o = make_float2(__shfl_down_sync(kFull, r.x, i), __shfl_down_sync(kFull, r.y, i));
         r = join(r, o);
     }
-    const int64_t mine = blockIdx.x * 32ll + slice;
-    if (lane == 0 && mine < count) {
-        const Token t = a.tokens[mine];
-        // not from the rounded lse: a sure row's loss keeps its digits
-        const float l = logf(r.y);
-        a.lse[t.row] = r.x + l;
-        a.loss[t.row] = r.x - a.z_target[mine] + l;
-    }
+    if (lane == 0) joined[slice] = r;
+    __syncthreads();
+    if (slice > 0 || row >= count) return;
+    // The loss is not formed from the rounded lse, and the target is apart, so that
+    // it keeps its digits however small it is. lse is that of the tensor cores' score,
+    // which the gradient will form again: exp(z - lse) is 1 if all others are 0.
+    const int to = a.tokens[row].row;
+    const LogSum x = log_sum(joined[lane], a.z_target[row]);
+    a.lse[to] = x.lse;
+    a.loss[to] = a.exact == kAsMultiplied ? x.loss : log_sum(joined[lane], a.exact == kBeside ? a.z_exact[row] : scores[lane]).loss;
 }
 
 // dH from the pieces' sums, where they are apart, and dW from the parts': four
@@ -1021,7 +1077,7 @@ constexpr int kLeastPart = 2048;
 struct Space {
     int64_t T_pad, V_pad, piece, pieces, held, columns, parts = 1, part_rows = 0;  // columns: of dz
     bool split = false, fine = false;
-    size_t head, tokens, place, closed, part, z_target, dz, acc, w_acc, bytes;
+    size_t head, tokens, place, closed, part, z_target, z_exact, dz, acc, w_acc, bytes;
     Space(const dpb_linear_loss_config *c, bool backward) {
         const size_t T = (size_t)c->tokens, d = (size_t)c->dim, V = (size_t)c->vocab;
         const int64_t words = round_up(c->vocab, kTile);
@@ -1061,10 +1117,11 @@ struct Space {
             dz = take((size_t)T_pad * (fine ? 2 : 1) * columns * 2);
             acc = take(split ? (size_t)pieces * T_pad * d * 4 : pieces > 1 ? T * d * 4 : 0);
             w_acc = take(parts > 1 ? (size_t)parts * V_pad * d * 4 : 0);
-            part = z_target = at;
+            part = z_target = z_exact = at;
         } else {
             part = take((V + kTile - 1) / kTile * (size_t)T_pad * sizeof(float2));
             z_target = take((size_t)T_pad * 4);
+            z_exact = take((size_t)T_pad * 4);
             dz = acc = w_acc = at;
         }
         bytes = at;
@@ -1119,6 +1176,8 @@ dpb_status begin(Args &a, const Space &w, const dpb_linear_loss_config *c, const
                  const void *targets, const float *grad, const float *lse, uint8_t *ws, cudaStream_t s) {
     a.h = static_cast<const bf16 *>(hidden->data);
     a.h_stride = hidden->stride;
+    a.w = static_cast<const bf16 *>(weight->data);
+    a.w_stride = weight->stride;
     a.head = reinterpret_cast<Head *>(ws + w.head);
     a.tokens = reinterpret_cast<Token *>(ws + w.tokens);
     a.place = reinterpret_cast<int *>(ws + w.place);
@@ -1191,6 +1250,13 @@ dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, c
     a.counted = counted;
     a.part = reinterpret_cast<float2 *>(ws + w.part);
     a.z_target = reinterpret_cast<float *>(ws + w.z_target);
+    a.z_exact = reinterpret_cast<float *>(ws + w.z_exact);
+    // Of rows of up to 256 columns the tensor cores' sums have 16 steps at most: the loss is off by 1e-7 with either
+    // (200 columns: 9.8e-8 and 8.3e-8 of the batch's norm; 792: 1.8e-6 and 8e-7 of a small loss). Beside the products it
+    // costs nothing where a block's rows take them longer (8192 words and 2^24 values of the weight at least: 33 tokens
+    // of 50257 words 36.5 us; 39 in join_kernel); the others' rows are short work for join_kernel (4096 tokens, 1000
+    // words, 768 columns: 1 us).
+    a.exact = cfg->dim <= 256 ? kAsMultiplied : cfg->vocab >= (1 << 13) && (int64_t)cfg->vocab * cfg->dim >= (1 << 24) ? kBeside : kInJoin;
     DPB_CHECK(begin(a, w, cfg, hidden, weight, targets, nullptr, nullptr, ws, s));
     DPB_CHECK(launch_products(a, w.T_pad / kTile * ((cfg->vocab + kTile - 1) / kTile), s));
     return launch_status(launch_early(join_kernel, dim3((unsigned)((cfg->tokens + 31) / 32)), 1024, 0, s, a),

@@ -478,3 +478,51 @@ def test_offsets_past_32_bits(left_out):
     assert (dh.view(n, T, d) == dh0).all()
     near(dw, formula(h, w, y, gl)[3] * n)
     assert dpb.status() == 0
+
+
+@pytest.mark.parametrize("V,d", [(500, 64), (500, 1000), (20000, 1024)])
+def test_the_smallest_losses_keep_their_digits(V, d):
+    """As above, with losses down to 1e-19: the logarithm of 1 and a sum that is far smaller, 2^-21 of itself off by the
+    exponentials, as much by the sum's roundings and by an exponential of 2 ulp and a log1p of 2. With the target's score
+    as it is multiplied, summed in the join and summed beside the products."""
+    n = 100
+    w = torch.zeros(V, d, device="cuda", dtype=BF)
+    w[:, 0] = 1.0
+    w[7, d - 1] = 1.0
+    h = torch.zeros(n, d, device="cuda", dtype=BF)
+    h[:, 0] = 64.0
+    h[:, d - 1] = torch.arange(n, device="cuda") * 0.5
+    y = torch.full((n,), 7, device="cuda")
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    gap = 0.5 * torch.arange(n, device="cuda", dtype=torch.float64)
+    want = torch.log1p((V - 1) * torch.exp(-gap))
+    check(loss, want, 2.0 ** -19 * want)
+    check(lse, 64 + gap + want, 2.0 ** -23 * (64 + gap + want))
+
+
+@pytest.mark.parametrize("T,V,d", [(33, 50257, 768), (300, 700, 1024), (2000, 1000, 2048)])
+def test_the_targets_scores_are_rounded_not_cut(T, V, d):
+    """Every score but the target's is 0 exactly, the target's a sum of d random products: the loss is off by that sum's
+    roundings, of lanes' chains of d / 64 products each and 6 joins, and by a few ulp of exponential and logarithm."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    w = torch.zeros(V, d, device="cuda", dtype=BF)
+    w[y[0]] = (torch.randn(d, generator=g, device="cuda") * 0.1).to(BF)
+    y[:] = y[0]
+    h = torch.randn(T, d, generator=g, device="cuda").to(BF)
+    h = (h.float() + w[y].float() * 8 / (w[y].float() ** 2).sum(1, keepdim=True)).to(BF)
+    loss, _ = dpb.linear_cross_entropy_forward(h, w, y)
+    z, size = (h.double() * w[y].double()).sum(1), (h.double() * w[y].double()).abs().sum(1)
+    want = torch.log1p((V - 1) * torch.exp(-z))
+    check(loss, want, ((d / 64 + 8) * 2.0 ** -24 * size + 2.0 ** -20) * want.clamp(min=0) + 2.0 ** -23 * want +
+          (d / 64 + 8) * 2.0 ** -24 * size * (want > 1))
+
+
+def test_an_infinite_score_has_no_loss():
+    h, w, y, _ = draw(40, 300, 64, seed=9)
+    h[3], w[y[3]] = 1e30, 1e30
+    y[4:] = (y[3] + 1) % 300
+    h[:, :] = torch.where(torch.arange(40, device="cuda")[:, None] == 3, h, 0)
+    loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    want = torch.log(torch.full((36,), 300.0, device="cuda"))
+    assert loss[3].isnan() and (loss[4:] - want).abs().max() < 2.0 ** -20

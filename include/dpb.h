@@ -667,7 +667,8 @@ dpb_status dpb_linear_cross_entropy_forward(const dpb_linear_loss_config *cfg, c
  * grad_weight (rows as hidden and weight; either may be NULL, then it is not
  * computed) are written, rows of ignored tokens with 0. dz enters its products
  * in bf16, relative to the largest finite |grad_loss| (up to 512 tokens in two
- * bf16, value and remainder, where both take at most 192 MB); their sums are fp32,
+ * bf16, value and remainder, where both take at most 192 MB; else the remainders of
+ * the targets' entries enter grad_hidden, not grad_weight); their sums are fp32,
  * in an order that the sizes, the ignored tokens and the device's multiprocessors
  * fix, and rounded once.
  */

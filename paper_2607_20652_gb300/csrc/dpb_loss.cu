@@ -99,6 +99,7 @@ struct Args {
     int *place;  // of each token: where it went, or -1
     float2 *part;  // [tiles of the vocabulary][rows]
     float *z_target, *z_exact;  // the targets' scores: the tensor cores', and summed by themselves
+    float *rest;  // of each token: what is left of its target's dz by rounding it to bf16
     float *loss, *lse;
     int *counted;
     CUtensorMap sums, w_sums;
@@ -367,11 +368,11 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 // 64 columns of a row's dz as bf16 pairs, into the warp's rows on their way to
 // memory; or what their rounding left over. lse is subtracted before the scaling to
 // powers of 2, so that a row whose target is all of it gives 0 exactly: scaled by
-// itself it would be rounded once more, 4e-5 at a score of 1000. `taken` is called
-// once they have been read out of TMEM.
+// itself it would be rounded once more, 4e-5 at a score of 1000. `aim` is set to the
+// target's, before it is rounded. `taken` is called once they have been read out of TMEM.
 template <typename F>
 __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int lane, int columns, const Token &t,
-                                             int target, bool remainder, F &&taken) {
+                                             int target, float &aim, bool remainder, F &&taken) {
     const uint64_t scale = pair(kLog2e, kLog2e), less = pair(-t.lse, -t.lse);
     uint32_t both[2][32];
     __syncwarp();
@@ -389,7 +390,7 @@ __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int 
             const float2 x = unpair(mul2(add2(pair_bits(v[i], v[i + 1]), less), scale));
             p[i] = exp2_approx(x.x), p[i + 1] = exp2_approx(x.y);
         }
-        at_target(target - c, [&](int i) { p[i] -= 1.f; });
+        at_target(target - c, [&](int i) { p[i] -= 1.f, aim = p[i] * t.g; });
         if (c + 32 > columns)
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -408,14 +409,36 @@ __device__ __forceinline__ void grad_columns(uint32_t tmem, uint32_t stage, int 
     }
 }
 
-// Four columns of rows row, row + 4, ... of dH as the pieces before have summed
-// them: other blocks' values, so not by way of this SM's own cache.
-__device__ __forceinline__ void sums_before(const Args &a, float4 (&x)[8], int row, int count, int column) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (row + 4 * i < count && column < a.d)
-            x[i] = __ldcg(reinterpret_cast<const float4 *>(a.acc + (int64_t)(row + 4 * i) * a.d + column));
+// What rounding dz of the target to bf16 leaves goes by itself into dH: four columns
+// of its product with the target's row of the weight. As the largest entry of most
+// rows it would set their error (a gradient for each of 8192 tokens: 0.0024 of dH's
+// norm, 0.0017 with it, which is dH's own rounding).
+__device__ __forceinline__ float rest_of(float aim) { return aim - __bfloat162float(__float2bfloat16_rn(aim)); }
+__device__ __forceinline__ void add_rest(float4 &x, float rest, uint2 w) {
+    x.x = fmaf(rest, __uint_as_float(w.x << 16), x.x);
+    x.y = fmaf(rest, __uint_as_float(w.x & 0xffff0000u), x.y);
+    x.z = fmaf(rest, __uint_as_float(w.y << 16), x.z);
+    x.w = fmaf(rest, __uint_as_float(w.y & 0xffff0000u), x.w);
 }
+
+// Four columns of rows row, row + 4, ... of dH as the pieces before have summed
+// them (other blocks' values, so not by way of this SM's own cache), and of the
+// weight's rows of their targets (`target`: of the warp's row of this lane).
+struct Before {
+    float4 sums[8];
+    uint2 w[8];
+    __device__ __forceinline__ void load(const Args &a, bool first, int row, int count, int column, int target) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int y = __shfl_sync(kFull, target, (threadIdx.x & 31) / 8 + 4 * i);
+            sums[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            w[i] = make_uint2(0, 0);
+            if (row + 4 * i >= count || column >= a.d) continue;
+            if (!first) sums[i] = __ldcg(reinterpret_cast<const float4 *>(a.acc + (int64_t)(row + 4 * i) * a.d + column));
+            if (!a.fine) w[i] = *reinterpret_cast<const uint2 *>(a.w + y * a.w_stride + column);
+        }
+    }
+};
 
 // The next slot of the ring, and how often the ring has been gone round.
 struct Turn {
@@ -673,11 +696,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             const uint32_t from = tmem + ((uint32_t)quarter << 21) + kTile * b + 128 * half;
             Token token{-1, 0.f, 0.f, -1};
             if (t.kind != kDWeight && row < count) token = a.tokens[row];
-            float4 before[8];
-            if (t.kind == kDHidden && t.piece > 0 && t.piece == a.pieces - 1 && !a.split) {
+            const int aimed = token.target - t.piece * a.piece - column;  // the target's column (kGrad)
+            const bool ends = t.kind == kDHidden && t.piece == a.pieces - 1 && !a.split;
+            float rest = 0.f;
+            Before before;
+            if (ends) {
                 fence_cluster();  // other blocks' sums, which the first block has seen
                 fence_async();
-                sums_before(a, before, row0 + lane / 8, count, column + 4 * (lane % 8));
+                if (!a.fine && row < count) rest = __ldcg(a.rest + row);
+                before.load(a, t.piece == 0, row0 + lane / 8, count, column + 4 * (lane % 8), token.target);
             }
             if (t.blocks > 0) {
                 if (!__all_sync(kFull, bar_test(base + Shared::kReady + 8 * b, (sums / 2) & 1))) settle(now);
@@ -711,7 +738,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 }
             } else if (t.kind == kGrad) {
                 const int words = list.words_of(a, t.piece);
-                const int target = token.target - t.piece * a.piece - column;
+                float aim = 0.f;
                 const int at = t.piece % a.held * a.piece + column;
 #pragma unroll 1
                 for (int part = 0; part <= (int)a.fine; ++part)
@@ -719,7 +746,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     for (int c = 0; c < 128; c += 64) {
                         if (lane == 0) stores_read();
                         __syncwarp();
-                        grad_columns(from + c, stage, lane, words - column - c, token, target - c, part, [&] {
+                        grad_columns(from + c, stage, lane, words - column - c, token, aimed - c, aim, part, [&] {
                             if (c && part == (int)a.fine) sums_read(b);  // the products need not wait for the rest
                         });
                         fence_async_shared();
@@ -727,6 +754,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                         if (lane == 0) store_box(&a.dz_out, stage, at + c, row0 + part * (int)a.T_pad);
                         if (c == 0 && part == 0) settle(later);
                     }
+                if (!a.fine && token.row >= 0 && (unsigned)aimed < 128u) a.rest[row] = rest_of(aim);
+                __syncwarp();  // before this unit is counted
             } else if (t.kind == kDWeight && a.parts == 1) {
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 64) {
@@ -761,7 +790,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 // pieces before; in the last one eight lanes have 128 bytes of a row. The sums
                 // of dW over a part of the tokens are all stored apart.
                 const bool of_w = t.kind == kDWeight;
-                const bool first = t.piece == 0 || a.split || of_w, last = t.piece == a.pieces - 1 && !a.split && !of_w;
+                const bool first = t.piece == 0 || a.split || of_w;
                 const int to = row0 + (of_w ? t.part * a.V_pad + t.piece * a.piece : a.split ? t.piece * (int)a.T_pad : 0);
                 const CUtensorMap *out = of_w ? &a.w_sums : &a.sums;
                 const int r = lane / 8, piece = lane % 8;
@@ -781,7 +810,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         store_shared(swizzled(stage, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                    if (!last) {
+                    if (!ends) {
                         fence_async_shared();
                         __syncwarp();
                         if (lane == 0 && first) store_box(out, stage, column + c, to);
@@ -791,16 +820,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     const int col = column + c + 4 * piece;
                     float4 sums[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sums[i] = before[i];
-                    if (!first && c < 96) sums_before(a, before, row0 + r, count, col + 32);
+                    for (int i = 0; i < 8; ++i) {
+                        sums[i] = before.sums[i];
+                        add_rest(sums[i], __shfl_sync(kFull, rest, r + 4 * i), before.w[i]);
+                    }
+                    if (c < 96) before.load(a, first, row0 + r, count, col + 32, token.target);
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int at = r + 4 * i;
+                        const int64_t place = __shfl_sync(kFull, token.row, at);
                         float4 x = load_shared(swizzled(stage, at, piece));
                         if (row0 + at >= count || col >= a.d) continue;
-                        if (!first) x.x += sums[i].x, x.y += sums[i].y, x.z += sums[i].z, x.w += sums[i].w;
-                        *reinterpret_cast<uint2 *>(a.dh + a.tokens[row0 + at].row * a.dh_stride + col) =
+                        x.x += sums[i].x, x.y += sums[i].y, x.z += sums[i].z, x.w += sums[i].w;
+                        *reinterpret_cast<uint2 *>(a.dh + place * a.dh_stride + col) =
                             make_uint2(pack_bf16(x.x * g, x.y * g), pack_bf16(x.z * g, x.w * g));
                     }
                 }
@@ -1030,6 +1063,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_sums_kernel(const __grid
                 }
             __syncthreads();
         }
+        if (slice == 0 && h && !a.fine)
+            add_rest(sum, a.rest[row], *reinterpret_cast<const uint2 *>(a.w + a.tokens[row].target * a.w_stride + column));
         if (slice == 0 && at < all)
             *reinterpret_cast<uint2 *>((h ? a.dh + a.tokens[row].row * a.dh_stride : a.dw_rows + (row - rows_h) * a.dw_stride) + column) =
                 make_uint2(pack_bf16(sum.x * g, sum.y * g), pack_bf16(sum.z * g, sum.w * g));
@@ -1077,7 +1112,7 @@ constexpr int kLeastPart = 2048;
 struct Space {
     int64_t T_pad, V_pad, piece, pieces, held, columns, parts = 1, part_rows = 0;  // columns: of dz
     bool split = false, fine = false;
-    size_t head, tokens, place, closed, part, z_target, z_exact, dz, acc, w_acc, bytes;
+    size_t head, tokens, place, closed, part, z_target, z_exact, rest, dz, acc, w_acc, bytes;
     Space(const dpb_linear_loss_config *c, bool backward) {
         const size_t T = (size_t)c->tokens, d = (size_t)c->dim, V = (size_t)c->vocab;
         const int64_t words = round_up(c->vocab, kTile);
@@ -1117,12 +1152,13 @@ struct Space {
             dz = take((size_t)T_pad * (fine ? 2 : 1) * columns * 2);
             acc = take(split ? (size_t)pieces * T_pad * d * 4 : pieces > 1 ? T * d * 4 : 0);
             w_acc = take(parts > 1 ? (size_t)parts * V_pad * d * 4 : 0);
+            rest = take(T * 4);
             part = z_target = z_exact = at;
         } else {
             part = take((V + kTile - 1) / kTile * (size_t)T_pad * sizeof(float2));
             z_target = take((size_t)T_pad * 4);
             z_exact = take((size_t)T_pad * 4);
-            dz = acc = w_acc = at;
+            dz = acc = w_acc = rest = at;
         }
         bytes = at;
     }
@@ -1293,6 +1329,7 @@ dpb_status dpb_linear_cross_entropy_backward(const dpb_linear_loss_config *cfg, 
     if (grad_hidden) a.dh = static_cast<bf16 *>(grad_hidden->data), a.dh_stride = grad_hidden->stride;
     if (grad_weight) a.dw_rows = static_cast<bf16 *>(grad_weight->data), a.dw_stride = grad_weight->stride;
     if (grad_weight) DPB_CHECK(make_map(&a.dw, grad_weight->data, grad_weight->stride, cfg->vocab, cfg->dim, 32));
+    a.rest = reinterpret_cast<float *>(ws + w.rest);
     a.acc = reinterpret_cast<float *>(ws + w.acc);
     if (w.pieces > 1)
         DPB_CHECK(make_map(&a.sums, a.acc, cfg->dim, w.split ? w.pieces * w.T_pad : cfg->tokens, cfg->dim, 32, true));

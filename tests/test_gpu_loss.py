@@ -526,3 +526,16 @@ def test_an_infinite_score_has_no_loss():
     loss, lse = dpb.linear_cross_entropy_forward(h, w, y)
     want = torch.log(torch.full((36,), 300.0, device="cuda"))
     assert loss[3].isnan() and (loss[4:] - want).abs().max() < 2.0 ** -20
+
+
+@pytest.mark.parametrize("even", [True, False])
+@pytest.mark.parametrize("T,V,d", [(513, 3001, 128), (3000, 3001, 264), (9000, 13001, 72), (20001, 300, 264), (40, 200000, 64)])
+def test_hidden_gradients_are_rounded_once(T, V, d, even):
+    """dz of the targets loses nothing to the products' type: what is left is the result's rounding, 2^-7 / sqrt 12 of each
+    value's binade, 0.2123 2^-7 of the norm over evenly spread digits, and that of the other words' dz, which is as much of
+    sqrt(e^2.25 / V) of the norm at scores of a deviation of 1.5. Sums of pieces apart, one after the other, and one piece."""
+    h, w, y, gl = draw(T, V, d, seed=T, even=even)
+    _, lse = dpb.linear_cross_entropy_forward(h, w, y)
+    dh, _ = dpb.linear_cross_entropy_backward(h, w, y, lse, gl)
+    want = formula(h, w, y, gl)[2]
+    assert float((dh.double() - want).norm()) <= 2.0 ** -7 * 0.2123 * 1.08 * (1 + 9.5 / V) ** 0.5 * float(want.norm())

@@ -11,6 +11,12 @@
 // words and d columns that is 2 T V d operations forward and 6 T V d for the
 // gradient, where keeping z would save 2 T V d and cost T V values.
 //
+// What bf16 costs: of dH nothing beyond its own rounding (0.0017 of its norm), as
+// the targets' entries, the largest, have what rounding leaves of them added
+// (Before, rest_of). Of dW 0.0018 with one gradient for all tokens and 0.0023 to
+// 0.0024 with one for each, where rounding dW alone gives 0.0017: two bf16 would
+// double its products, a third of the work. Up to 512 tokens dz has two bf16.
+//
 // All of it is one kernel of matrix products (product_kernel). Pairs of blocks
 // take units, tiles of 256 x 256 of one of the products, from a counter: the pair
 // shares each product (each block loads its 128 rows of A and half of B, so an
@@ -21,12 +27,12 @@
 // next unit is multiplied.
 //
 // What bounds it, at 8192 tokens, 50257 words, 768 columns: forward the products
-// (500 cycles of 512 a slot of 64 columns; 330 us at once, 1910 TFLOP/s, 355 us
-// for as long as one likes, when the power limit holds the clock at 1.6 GHz; the
+// (500 cycles of 512 a slot of 64 columns; 327 us at once, 1930 TFLOP/s, 355 to
+// 375 us for as long as one likes, when the power limit holds the clock at 1.6 GHz; the
 // library's product of these sizes, which writes the scores, 350 and 395 us). The
 // gradient's units take 650 (dz: its stores and the products' operands share the
-// shared memory), 670 (dH) and 560 cycles (dW) a slot, 1180 us at once and 1300 us
-// at the power limit, 1470 TFLOP/s, where three library products take 1190.
+// shared memory), 670 (dH) and 560 cycles (dW) a slot, 1155 us at once and 1300 us
+// at the power limit, 1460 TFLOP/s, where three library products take 1190.
 // Measured and not taken: dz and dW stored by the row warps themselves, with
 // seven slots in place of the rows on their way (dz 760 cycles a slot); two
 // places for a warp's rows with five slots (710, 750 and 620); a kernel for each
@@ -1096,17 +1102,18 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // more than that, all of it is held, and the pieces are as many as give every pair
 // of blocks two units of dH, whose sums are kept apart: one after the other few
 // units would follow each other through the whole vocabulary (1000 tokens, 50257
-// words, 768 columns: 300 us, 207 apart; 2000: 342 and 350; 4096, too many for it,
+// words, 768 columns: 300 us, 210 apart; 2000: 342 and 360; 4096, too many for it,
 // 560). With the fewest tokens, whose rounding errors of dz do not average out, dz
-// is held to 16 bits, in two bf16: 33 tokens take 117 us, 512 195 (268 and 282 in
+// is held to 16 bits, in two bf16: 33 tokens take 119 us, 512 199 (268 and 282 in
 // one bf16 and one after the other).
 constexpr int64_t kPieceBytes = 64ll << 20;
 constexpr int kLeastPiece = 4096, kFineRows = 512;
 // Where dW, of few words and columns, has fewer units than there are pairs of
 // blocks, they are of parts of the tokens, this many at least, whose sums are added
-// up in the end: 65536 tokens, 1000 words, 256 columns take 174 us for the gradient,
-// 390 with one unit for all tokens; 16384, 100, 64 40 and 93; 4096, 1000, 768 63 and
-// 75 (parts of 4096: 174, 46, 77; of 1024 and two units a pair: 194, 42, 64).
+// up in the end: 65536 tokens, 1000 words, 256 columns took 174 us for the gradient
+// (191 with the targets' remainders in dH), 390 with one unit for all tokens; 16384,
+// 100, 64 40 and 93; 4096, 1000, 768 63 and 75 (parts of 4096: 174, 46, 77; of 1024
+// and two units a pair: 194, 42, 64).
 constexpr int kLeastPart = 2048;
 
 struct Space {

@@ -9,10 +9,16 @@
 // warp has a row where its lanes can hold it, up to 1024 threads where not. The
 // gradient's threads keep their columns' dw over all rows of their block, and the
 // blocks' sums are added up in the blocks' order; its rows on their way are in
-// shared memory (65536 x 768 bf16: 74 us, 5.4 TB/s; 49999 x 1000 75; 32768 x 768
+// shared memory (65536 x 768 bf16: 74 us, 5.4 TB/s; 49999 x 1000 76; 32768 x 768
 // fp32 71; 16384 x 4096 bf16 87; 10000 x 16384 fp32 390; with them in registers 81,
 // 79, 85, 114 and 745). Of each some 3 us are for dw; summed up a warp after the
 // other, waiting for each, a block's took 4 us more at 49999 x 1000.
+//
+// Rows that do not lie in pieces of 16 bytes go value by value, in registers: 20000
+// x 777 bf16 takes 56 us and 106 for the gradient, 3.1 and 5.8 times what its bytes
+// need, 5000 x 5001 116 and 155 (3.9 and 5.3). From 8193 values on such a row's 1024
+// threads have too few registers and spill (up to 870 bytes a thread, 592 in the
+// gradient).
 #include <algorithm>
 
 #include "dpb_checks.h"

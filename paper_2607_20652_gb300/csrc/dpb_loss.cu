@@ -11,9 +11,9 @@
 // words and d columns that is 2 T V d operations forward and 6 T V d for the
 // gradient, where keeping z would save 2 T V d and cost T V values.
 //
-// What bf16 costs: of dH nothing beyond its own rounding (0.0017 of its norm), as
-// the targets' entries, the largest, have what rounding leaves of them added
-// (Before, rest_of). Of dW 0.0018 with one gradient for all tokens and 0.0023 to
+// What bf16 costs: of dH nothing beyond its own rounding (0.0017 of its norm) in
+// rows whose targets' entries are the largest, as these have what rounding leaves of
+// them added (Before, rest_of). Of dW 0.0018 with one gradient for all tokens and 0.0023 to
 // 0.0024 with one for each, where rounding dW alone gives 0.0017: two bf16 would
 // double its products, a third of the work. Up to 512 tokens dz has two bf16.
 //
